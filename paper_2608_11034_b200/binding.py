@@ -101,6 +101,13 @@ def lib():
             "scout_consensus_timing": (C.c_int, [u32, u64, vp, C.c_double, vp, vp, vp, vp, vp]),
             "scout_rotating_slice": (C.c_int, [u64, u64, u64, C.POINTER(u64), C.POINTER(u64)]),
             "scout_selftest_bounded_wait": (C.c_int, [u64, vp, vp]),
+            "scout_attn_workspace": (C.c_int, [vp, C.POINTER(u64), C.POINTER(u64)]),
+            "scout_attn_forward": (C.c_int, [vp] * 9 + [u64, vp]),
+            "scout_attn_backward": (C.c_int, [vp] * 13 + [u64, vp]),
+            "scout_ckpt_pack": (C.c_int, [u32, u64, u64, vp, u64, vp, u64, vp, vp]),
+            "scout_ckpt_unpack": (C.c_int, [u32, u64, u64, vp, u64, vp, vp, u64, vp]),
+            "scout_ckpt_wgrad_workspace": (C.c_int, [u32, u64, u64, u64, C.POINTER(u64)]),
+            "scout_ckpt_wgrad": (C.c_int, [u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, u64, u32, vp, u64, vp]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
             "scout_last_cuda_error": (C.c_char_p, []),
@@ -370,6 +377,57 @@ def scout_rotating_slice(numel: int, slice_elems: int, step: int):
     _check(lib().scout_rotating_slice(numel, slice_elems, step, C.byref(b), C.byref(n)),
            "scout_rotating_slice")
     return b.value, n.value
+
+
+# ---- operators of a replayed layer (include/scout_replay.h) -----------------------
+
+CKPT_BLOCK = 32              # SCOUT_CKPT_BLOCK
+ATTN_DTYPE = np.dtype([("dtype", "<u4"), ("batch", "<u4"), ("q_len", "<u4"), ("kv_len", "<u4"), ("q_heads", "<u4"),
+                       ("kv_heads", "<u4"), ("head_dim", "<u4"), ("causal", "<u4"), ("window", "<u4"), ("scale", "<f4"),
+                       ("q_stride", "<u8", 3), ("k_stride", "<u8", 3), ("v_stride", "<u8", 3), ("o_stride", "<u8", 3),
+                       ("do_stride", "<u8", 3)])
+
+
+def scout_attn_workspace(attn: int):
+    """attn: address of one ATTN_DTYPE record.  -> (forward_bytes, backward_bytes)"""
+    f, b = C.c_uint64(), C.c_uint64()
+    _check(lib().scout_attn_workspace(attn, C.byref(f), C.byref(b)), "scout_attn_workspace")
+    return f.value, b.value
+
+
+def scout_attn_forward(attn: int, q: int, k: int, v: int, q_lens: int, kv_lens: int, o: int, lse: int, workspace: int,
+                       workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_attn_forward(attn, q, k, v, q_lens, kv_lens, o, lse, workspace, workspace_bytes, stream),
+           "scout_attn_forward")
+
+
+def scout_attn_backward(attn: int, q: int, k: int, v: int, o: int, lse: int, d_o: int, q_lens: int, kv_lens: int, dq: int,
+                        dk: int, dv: int, workspace: int, workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_attn_backward(attn, q, k, v, o, lse, d_o, q_lens, kv_lens, dq, dk, dv, workspace, workspace_bytes,
+                                     stream), "scout_attn_backward")
+
+
+def scout_ckpt_pack(dtype: int, rows: int, cols: int, x: int, x_stride: int, codes: int, code_stride: int, exps: int,
+                    stream: int) -> None:
+    _check(lib().scout_ckpt_pack(dtype, rows, cols, x, x_stride, codes, code_stride, exps, stream), "scout_ckpt_pack")
+
+
+def scout_ckpt_unpack(dtype: int, rows: int, cols: int, codes: int, code_stride: int, exps: int, x: int, x_stride: int,
+                      stream: int) -> None:
+    _check(lib().scout_ckpt_unpack(dtype, rows, cols, codes, code_stride, exps, x, x_stride, stream), "scout_ckpt_unpack")
+
+
+def scout_ckpt_wgrad_workspace(dtype: int, rows: int, outs: int, ins: int) -> int:
+    n = C.c_uint64()
+    _check(lib().scout_ckpt_wgrad_workspace(dtype, rows, outs, ins, C.byref(n)), "scout_ckpt_wgrad_workspace")
+    return n.value
+
+
+def scout_ckpt_wgrad(dtype: int, out_dtype: int, rows: int, outs: int, ins: int, dy: int, dy_stride: int, codes: int,
+                     code_stride: int, exps: int, dw: int, dw_stride: int, accumulate: int, workspace: int,
+                     workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_ckpt_wgrad(dtype, out_dtype, rows, outs, ins, dy, dy_stride, codes, code_stride, exps, dw, dw_stride,
+                                  accumulate, workspace, workspace_bytes, stream), "scout_ckpt_wgrad")
 
 
 def scout_selftest_bounded_wait(limit_ns: int, d_out: int, stream: int) -> None:

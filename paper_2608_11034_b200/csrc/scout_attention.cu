@@ -1,0 +1,824 @@
+// Attention of the layer replay: forward pass, and the backward pass that recomputes the probabilities.
+//
+// One pass over the keys with the running maximum m and sum l of each row's softmax
+// (on powers of two: s' = scale log2(e) q.k):
+//     m' = max(m, max_j s'_j)   l' = l 2^(m-m') + sum_j 2^(s'_j-m')   O' = O 2^(m-m') + sum_j 2^(s'_j-m') v_j
+// Backward: P_ij = 2^(s'_ij - lse'_i), dS = P o (dP - delta), two kernels: one owns 64 keys and runs over
+// the rows that see them (dK, dV), one owns 64 rows and runs over their keys (dQ).  S and dP are computed twice
+// (7 products where 5 would do) so that no sum crosses blocks: results are the same bits on every run, which float
+// atomics would not give.
+//
+// A tile's rows are (token, head of the group) pairs, token-major: the query heads that share a key head
+// read its keys once, and a single token still fills a tile with its group.
+//
+// Where the grid would leave SMs idle (few rows, long keys) the long axis is split into parts of
+// fixed size; parts go to scratch in fp32 and a join kernel adds them in order.
+#include <algorithm>
+
+#include "scout_attention.cuh"
+
+namespace scout {
+namespace attn {
+namespace {
+
+constexpr int TILE = 64;  // rows and keys of a tile: 16 rows for each of four warps
+constexpr int THREADS = 128;
+
+// offset of 16-byte chunk c of row r in a tile of HD-element rows; chunks are permuted within eight
+// rows so that the eight rows of a matrix load fall into different banks
+template <int HD> __device__ __forceinline__ uint32_t at16(int r, int c) { return r * (HD * 2) + ((c ^ (r & 7)) << 4); }
+
+// Rows of a tile to shared memory; row(r) gives the address, or null for a row of zeros (`any` is then named as the
+// source, and nothing is read from it).
+template <int HD, int ROWS, typename F>
+__device__ __forceinline__ void load_rows(uint32_t dst, int head_dim, const void *any, F row) {
+    constexpr int CH = HD / 8;
+    for (int x = threadIdx.x; x < ROWS * CH; x += THREADS) {
+        const int r = x / CH, c = x % CH;
+        const uint16_t *src = row(r);
+        const bool ok = src != nullptr && c * 8 < head_dim;
+        copy16(dst + at16<HD>(r, c), ok ? (const void *)(src + c * 8) : any, ok);
+    }
+}
+
+struct RowMap {  // packed row m of a (sequence, key head) -> token, head
+    int group, heads0;
+    __device__ __forceinline__ int token(int m) const { return m / group; }
+    __device__ __forceinline__ int head(int m) const { return heads0 + m % group; }
+};
+
+// acc[n] += A[16 x HD] B[8n.. x HD]^T, A rows from row a0, B stored row by row
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void product_nt(float (&acc)[NT][4], uint32_t a, int a0, uint32_t bb) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int kk = 0; kk < HD / 16; ++kk) {
+        uint32_t fa[4];
+        ldsm(fa, a + at16<HD>(a0 + (lane & 15), kk * 2 + (lane >> 4)));
+#pragma unroll
+        for (int n = 0; n < NT; n += 2) {
+            uint32_t fb[4];
+            ldsm(fb, bb + at16<HD>(n * 8 + (lane & 7) + ((lane >> 4) << 3), kk * 2 + ((lane >> 3) & 1)));
+            mma16816<T>(acc[n], fa, fb[0], fb[1]);
+            mma16816<T>(acc[n + 1], fa, fb[2], fb[3]);
+        }
+    }
+}
+// acc[HD/8] += X[16 x 8 NT] B[8 NT x HD], X in accumulator layout (rounded to T), B stored row by row
+template <typename T, int HD, int NT>
+__device__ __forceinline__ void product_nn(float (&acc)[HD / 8][4], const float (&x)[NT][4], uint32_t bb) {
+    const int lane = threadIdx.x & 31;
+#pragma unroll
+    for (int kk = 0; kk < NT / 2; ++kk) {
+        const uint32_t fa[4] = {Half<T>::pack(x[2 * kk][0], x[2 * kk][1]), Half<T>::pack(x[2 * kk][2], x[2 * kk][3]),
+                                Half<T>::pack(x[2 * kk + 1][0], x[2 * kk + 1][1]), Half<T>::pack(x[2 * kk + 1][2], x[2 * kk + 1][3])};
+#pragma unroll
+        for (int n = 0; n < HD / 8; n += 2) {
+            uint32_t fb[4];
+            ldsm_t(fb, bb + at16<HD>(kk * 16 + (lane & 7) + (((lane >> 3) & 1) << 3), n + (lane >> 4)));
+            mma16816<T>(acc[n], fa, fb[0], fb[1]);
+            mma16816<T>(acc[n + 1], fa, fb[2], fb[3]);
+        }
+    }
+}
+
+// keys that any row of packed rows [m0, m1) sees: [lo, hi), empty as hi <= lo
+__device__ __forceinline__ void tile_keys(const Problem &p, const Lengths &n, const RowMap &rm, int m0, int m1, int &lo, int &hi) {
+    const int t0 = rm.token(m0), t1 = min(rm.token(m1 - 1), n.nq - 1);
+    lo = t0 <= t1 ? row_lo(p, n, t0) : 0;
+    hi = t0 <= t1 ? row_hi(p, n, t1) : 0;
+}
+
+// ---- forward -----------------------------------------------------------------------------------------
+struct ForwardArgs {
+    Problem p;
+    void *o;
+    float *lse;
+    float *part_o;   // [splits][rows][head_dim], rows = batch * q_heads * q_len; null without splits
+    float2 *part_ml; // [splits][rows] {m, l}
+    int tiles, splits;
+};
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) forward_tiles(const __grid_constant__ ForwardArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    const Problem &p = a.p;
+    int x = blockIdx.x;
+    const int split = x % a.splits;
+    x /= a.splits;
+    const int hk = x % p.kv_heads;
+    x /= p.kv_heads;
+    const int b = x % p.batch, tile = a.tiles - 1 - x / p.batch;  // the longest rows of a causal problem first
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Lengths n = lengths(p, b);
+    const RowMap rm{p.group, hk * p.group};
+    const int m_all = p.group * p.q_len, m0 = tile * TILE, m1 = min(m0 + TILE, m_all);
+    int lo, hi;
+    tile_keys(p, n, rm, m0, m1, lo, hi);
+    int blk0 = lo / TILE, blk1 = hi > lo ? (hi + TILE - 1) / TILE : blk0;
+    const int per = (blk1 - blk0 + a.splits - 1) / a.splits;
+    blk0 += split * per;
+    blk1 = min(blk1, blk0 + per);
+
+    const uint32_t sq = smem_u32(smem), sk = sq + TILE * HD * 2, sv = sk + 2 * TILE * HD * 2;
+    const auto load_kv = [&](int blk, int st) {
+        load_rows<HD, TILE>(sk + st * TILE * HD * 2, p.head_dim, p.k, [&](int r) {
+            const int j = blk * TILE + r;
+            return j < n.nk ? reinterpret_cast<const uint16_t *>(p.k) + b * p.sk.b + j * p.sk.t + hk * p.sk.h : nullptr;
+        });
+        load_rows<HD, TILE>(sv + st * TILE * HD * 2, p.head_dim, p.v, [&](int r) {
+            const int j = blk * TILE + r;
+            return j < n.nk ? reinterpret_cast<const uint16_t *>(p.v) + b * p.sv.b + j * p.sv.t + hk * p.sv.h : nullptr;
+        });
+        copy_commit();
+    };
+    if (blk0 < blk1) {
+        load_rows<HD, TILE>(sq, p.head_dim, p.q, [&](int r) {
+            const int m = m0 + r;
+            return m < m1 && rm.token(m) < n.nq
+                       ? reinterpret_cast<const uint16_t *>(p.q) + b * p.sq.b + rm.token(m) * p.sq.t + rm.head(m) * p.sq.h
+                       : nullptr;
+        });
+        load_kv(blk0, 0);
+    }
+    // this thread's two rows
+    int rlo[2], rhi[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int m = m0 + warp * 16 + (lane >> 2) + 8 * s;
+        rlo[s] = m < m1 ? row_lo(p, n, rm.token(m)) : 0;
+        rhi[s] = m < m1 ? row_hi(p, n, rm.token(m)) : 0;
+    }
+    float acc[HD / 8][4] = {}, top[2] = {-CUDART_INF_F, -CUDART_INF_F}, sum[2] = {0.f, 0.f};
+    for (int blk = blk0; blk < blk1; ++blk) {
+        const int st = (blk - blk0) & 1;
+        copy_wait<0>();
+        __syncthreads();
+        if (blk + 1 < blk1) load_kv(blk + 1, st ^ 1);
+        float s[TILE / 8][4] = {};
+        product_nt<T, HD, TILE / 8>(s, sq, warp * 16, sk + st * TILE * HD * 2);
+        float up[2] = {top[0], top[1]};
+#pragma unroll
+        for (int c = 0; c < TILE / 8; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = blk * TILE + c * 8 + (lane & 3) * 2 + (e & 1);
+                s[c][e] = j >= rlo[e >> 1] && j < rhi[e >> 1] ? s[c][e] * p.scale_log2 : -CUDART_INF_F;
+                up[e >> 1] = fmaxf(up[e >> 1], s[c][e]);
+            }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            up[r] = fmaxf(up[r], __shfl_xor_sync(0xFFFFFFFFu, up[r], 1));
+            up[r] = fmaxf(up[r], __shfl_xor_sync(0xFFFFFFFFu, up[r], 2));
+            const float base = up[r] == -CUDART_INF_F ? 0.f : up[r];
+            const float fade = exp2_fast(top[r] - base);
+            top[r] = up[r];
+            sum[r] *= fade;
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) {
+                acc[c][2 * r] *= fade;
+                acc[c][2 * r + 1] *= fade;
+            }
+#pragma unroll
+            for (int c = 0; c < TILE / 8; ++c)
+#pragma unroll
+                for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                    s[c][e] = exp2_fast(s[c][e] - base);
+                    sum[r] += s[c][e];
+                }
+        }
+        product_nn<T, HD, TILE / 8>(acc, s, sv + st * TILE * HD * 2);
+    }
+    uint32_t redo = 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        sum[r] += __shfl_xor_sync(0xFFFFFFFFu, sum[r], 1);
+        sum[r] += __shfl_xor_sync(0xFFFFFFFFu, sum[r], 2);
+        const int m = m0 + warp * 16 + (lane >> 2) + 8 * r;
+        const bool mine = m < m1;
+        const int64_t row = mine ? ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m) : 0;
+        if (a.splits > 1) {
+            const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+            if (mine) {
+                float *dst = a.part_o + (split * rows + row) * p.head_dim;
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c) {
+                    const int col = c * 8 + (lane & 3) * 2;
+                    if (col < p.head_dim) *reinterpret_cast<float2 *>(dst + col) = make_float2(acc[c][2 * r], acc[c][2 * r + 1]);
+                }
+                if ((lane & 3) == 0) a.part_ml[split * rows + row] = make_float2(top[r], sum[r]);
+            }
+            continue;
+        }
+        bool fine = finite(sum[r]) && top[r] != CUDART_INF_F;
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) fine = fine && finite(acc[c][2 * r]) && finite(acc[c][2 * r + 1]);
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
+        const bool again = (bad >> (lane & ~3)) & 0xF;
+        if (mine && !again) {
+            const float inv = sum[r] == 0.f ? 1.f : 1.f / sum[r];
+            T *dst = RowIO<T>::at(a.o, p.so, b, rm.token(m), rm.head(m));
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) {
+                const int col = c * 8 + (lane & 3) * 2;
+                if (col < p.head_dim)
+                    *reinterpret_cast<uint32_t *>(dst + col) = Half<T>::pack(acc[c][2 * r] * inv, acc[c][2 * r + 1] * inv);
+            }
+            if ((lane & 3) == 0) a.lse[row] = top[r] == -CUDART_INF_F ? -CUDART_INF_F : (top[r] + log2f(sum[r])) * LN2;
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            if ((bad >> (4 * g)) & 0xF) redo |= 1u << (g + 8 * r);
+    }
+    while (redo) {  // warp-uniform
+        const int m = m0 + warp * 16 + __ffs(redo) - 1;
+        redo &= redo - 1;
+        row_forward<T>(p, b, rm.head(m), rm.token(m), a.o, a.lse);
+    }
+}
+
+// One warp joins a row's parts in order.
+template <typename T>
+__global__ void __launch_bounds__(THREADS) forward_join(const __grid_constant__ ForwardArgs a) {
+    pdl_wait();
+    const Problem &p = a.p;
+    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int lane = threadIdx.x & 31, d = p.head_dim;
+    const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
+    float top = -CUDART_INF_F;
+    for (int s = 0; s < a.splits; ++s) {
+        const float m = a.part_ml[s * rows + row].x;
+        top = fmaxf(top, m);
+    }
+    const float base = top == -CUDART_INF_F ? 0.f : top;
+    float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s) {
+        const float2 ml = a.part_ml[s * rows + row];
+        const float w = exp2f(ml.x - base);
+        sum = fmaf(ml.y, w, sum);
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (lane + 32 * c < d) acc[c] = fmaf(a.part_o[(s * rows + row) * d + lane + 32 * c], w, acc[c]);
+    }
+    bool fine = finite(sum) && top != CUDART_INF_F;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
+    if (!__all_sync(0xFFFFFFFFu, fine)) {
+        row_forward<T>(p, b, hq, i, a.o, a.lse);
+        return;
+    }
+    const float inv = sum == 0.f ? 1.f : 1.f / sum;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] *= inv;
+    RowIO<T>::store(RowIO<T>::at(a.o, p.so, b, i, hq), acc, d, lane);
+    if (lane == 0) a.lse[row] = top == -CUDART_INF_F ? -CUDART_INF_F : (base + log2f(sum)) * LN2;
+}
+
+// ---- backward ----------------------------------------------------------------------------------------
+struct BackwardArgs {
+    Problem p;
+    const float *lse;
+    float2 *stats;  // [batch][q_heads][q_len] {lse', delta}
+    void *dq, *dk, *dv;
+    float *part;    // fp32 parts, or null: [splits][rows][head_dim] (dQ), [splits][2][keys][head_dim] (dK, dV)
+    int tiles, splits;
+};
+
+// One warp per row: delta = g . o, and the row statistic on powers of two.  A row that sees nothing gets +inf:
+// its probabilities come out 0.
+template <typename T>
+__global__ void __launch_bounds__(THREADS) backward_stats(const __grid_constant__ BackwardArgs a) {
+    const Problem &p = a.p;
+    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+    const int64_t x = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    pdl_launch_dependents();
+    if (x >= rows) return;
+    const int lane = threadIdx.x & 31;
+    const int hq = x % p.q_heads, i = x / p.q_heads % p.q_len, b = x / p.q_heads / p.q_len;  // heads adjacent in memory
+    const Lengths n = lengths(p, b);
+    const int64_t row = ((int64_t)b * p.q_heads + hq) * p.q_len + i;
+    float2 st = make_float2(CUDART_INF_F, 0.f);
+    if (row_hi(p, n, i) > row_lo(p, n, i)) {
+        const float l = a.lse[row];
+        float o[4], g[4];
+        RowIO<T>::load(o, RowIO<T>::at(p.o, p.so, b, i, hq), p.head_dim, lane);
+        RowIO<T>::load(g, RowIO<T>::at(p.d_o, p.sg, b, i, hq), p.head_dim, lane);
+        st = make_float2(l == -CUDART_INF_F ? CUDART_INF_F : l * LOG2E, warp_dot(o, g, p.head_dim, lane));
+    }
+    if (lane == 0) a.stats[row] = st;
+}
+
+// P and dS of a tile in accumulator layout.  s, dp: 16 rows x 8 NT columns
+template <int NT, typename Seen, typename Stat>
+__device__ __forceinline__ void to_p_ds(float (&s)[NT][4], float (&dp)[NT][4], float scale_log2, Seen seen, Stat stat) {
+#pragma unroll
+    for (int c = 0; c < NT; ++c)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const float2 st = stat(c, e);
+            const bool ok = seen(c, e);
+            const float w = ok ? exp2_fast(fmaf(s[c][e], scale_log2, -st.x)) : 0.f;
+            s[c][e] = w;
+            dp[c][e] = ok ? w * (dp[c][e] - st.y) : 0.f;
+        }
+}
+
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) backward_dq(const __grid_constant__ BackwardArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    pdl_wait();
+    const Problem &p = a.p;
+    int x = blockIdx.x;
+    const int split = x % a.splits;
+    x /= a.splits;
+    const int hk = x % p.kv_heads;
+    x /= p.kv_heads;
+    const int b = x % p.batch, tile = a.tiles - 1 - x / p.batch;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Lengths n = lengths(p, b);
+    const RowMap rm{p.group, hk * p.group};
+    const int m_all = p.group * p.q_len, m0 = tile * TILE, m1 = min(m0 + TILE, m_all);
+    int lo, hi;
+    tile_keys(p, n, rm, m0, m1, lo, hi);
+    int blk0 = lo / TILE, blk1 = hi > lo ? (hi + TILE - 1) / TILE : blk0;
+    const int per = (blk1 - blk0 + a.splits - 1) / a.splits;
+    blk0 += split * per;
+    blk1 = min(blk1, blk0 + per);
+    constexpr int BYTES = TILE * HD * 2;
+    const uint32_t sq = smem_u32(smem), sg = sq + BYTES, sk = sg + BYTES, sv = sk + 2 * BYTES;
+    const auto load_kv = [&](int blk, int st) {
+        load_rows<HD, TILE>(sk + st * BYTES, p.head_dim, p.k, [&](int r) {
+            const int j = blk * TILE + r;
+            return j < n.nk ? reinterpret_cast<const uint16_t *>(p.k) + b * p.sk.b + j * p.sk.t + hk * p.sk.h : nullptr;
+        });
+        load_rows<HD, TILE>(sv + st * BYTES, p.head_dim, p.v, [&](int r) {
+            const int j = blk * TILE + r;
+            return j < n.nk ? reinterpret_cast<const uint16_t *>(p.v) + b * p.sv.b + j * p.sv.t + hk * p.sv.h : nullptr;
+        });
+        copy_commit();
+    };
+    if (blk0 < blk1) {
+        load_rows<HD, TILE>(sq, p.head_dim, p.q, [&](int r) {
+            const int m = m0 + r;
+            return m < m1 && rm.token(m) < n.nq
+                       ? reinterpret_cast<const uint16_t *>(p.q) + b * p.sq.b + rm.token(m) * p.sq.t + rm.head(m) * p.sq.h
+                       : nullptr;
+        });
+        load_rows<HD, TILE>(sg, p.head_dim, p.d_o, [&](int r) {
+            const int m = m0 + r;
+            return m < m1 && rm.token(m) < n.nq
+                       ? reinterpret_cast<const uint16_t *>(p.d_o) + b * p.sg.b + rm.token(m) * p.sg.t + rm.head(m) * p.sg.h
+                       : nullptr;
+        });
+        load_kv(blk0, 0);
+    }
+    int rlo[2], rhi[2];
+    float2 st2[2];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int m = m0 + warp * 16 + (lane >> 2) + 8 * s;
+        rlo[s] = m < m1 ? row_lo(p, n, rm.token(m)) : 0;
+        rhi[s] = m < m1 ? row_hi(p, n, rm.token(m)) : 0;
+        st2[s] = m < m1 ? a.stats[((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m)] : make_float2(CUDART_INF_F, 0.f);
+    }
+    float acc[HD / 8][4] = {};
+    for (int blk = blk0; blk < blk1; ++blk) {
+        const int st = (blk - blk0) & 1;
+        copy_wait<0>();
+        __syncthreads();
+        if (blk + 1 < blk1) load_kv(blk + 1, st ^ 1);
+        float s[TILE / 8][4] = {}, dp[TILE / 8][4] = {};
+        product_nt<T, HD, TILE / 8>(s, sq, warp * 16, sk + st * BYTES);
+        product_nt<T, HD, TILE / 8>(dp, sg, warp * 16, sv + st * BYTES);
+        to_p_ds<TILE / 8>(s, dp, p.scale_log2,
+                          [&](int c, int e) {
+                              const int j = blk * TILE + c * 8 + (lane & 3) * 2 + (e & 1);
+                              return j >= rlo[e >> 1] && j < rhi[e >> 1];
+                          },
+                          [&](int, int e) { return st2[e >> 1]; });
+        product_nn<T, HD, TILE / 8>(acc, dp, sk + st * BYTES);
+    }
+    uint32_t redo = 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int m = m0 + warp * 16 + (lane >> 2) + 8 * r;
+        const bool mine = m < m1;
+        if (a.splits > 1) {
+            const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+            if (mine) {
+                float *dst = a.part + (split * rows + ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m)) * p.head_dim;
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c) {
+                    const int col = c * 8 + (lane & 3) * 2;
+                    if (col < p.head_dim) *reinterpret_cast<float2 *>(dst + col) = make_float2(acc[c][2 * r], acc[c][2 * r + 1]);
+                }
+            }
+            continue;
+        }
+        bool fine = true;
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c) fine = fine && finite(acc[c][2 * r]) && finite(acc[c][2 * r + 1]);
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
+        if (mine && !((bad >> (lane & ~3)) & 0xF)) {
+            T *dst = RowIO<T>::at(a.dq, p.sq, b, rm.token(m), rm.head(m));
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) {
+                const int col = c * 8 + (lane & 3) * 2;
+                if (col < p.head_dim)
+                    *reinterpret_cast<uint32_t *>(dst + col) = Half<T>::pack(acc[c][2 * r] * p.scale, acc[c][2 * r + 1] * p.scale);
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            if ((bad >> (4 * g)) & 0xF) redo |= 1u << (g + 8 * r);
+    }
+    while (redo) {
+        const int m = m0 + warp * 16 + __ffs(redo) - 1;
+        redo &= redo - 1;
+        row_dq<T>(p, a.stats, b, rm.head(m), rm.token(m), a.dq);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS) join_dq(const __grid_constant__ BackwardArgs a) {
+    pdl_wait();
+    const Problem &p = a.p;
+    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= rows) return;
+    const int lane = threadIdx.x & 31, d = p.head_dim;
+    const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
+    float acc[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (lane + 32 * c < d) acc[c] += a.part[(s * rows + row) * d + lane + 32 * c];
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
+    if (!__all_sync(0xFFFFFFFFu, fine)) {
+        row_dq<T>(p, a.stats, b, hq, i, a.dq);
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] *= p.scale;
+    RowIO<T>::store(RowIO<T>::at(a.dq, p.sq, b, i, hq), acc, d, lane);
+}
+
+// Owns 64 keys; runs over the packed rows that see them, 32 at a time (with 64 the two 16 x HD accumulators and both
+// tiles would not fit a thread's registers).  S and dP are computed transposed, keys as rows, so that P and dS
+// are already in place as left operands of dV += P^T G and dK += dS^T Q.
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) backward_dkv(const __grid_constant__ BackwardArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    pdl_wait();
+    constexpr int QT = 32, KBYTES = TILE * HD * 2, QBYTES = QT * HD * 2;
+    __shared__ float2 s_stat[2][QT];
+    __shared__ int2 s_keys[2][QT];
+    const Problem &p = a.p;
+    int x = blockIdx.x;
+    const int split = x % a.splits;
+    x /= a.splits;
+    const int hk = x % p.kv_heads;
+    x /= p.kv_heads;
+    const int b = x % p.batch, tile = x / p.batch;  // causal: the first keys are seen by the most rows
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Lengths n = lengths(p, b);
+    const RowMap rm{p.group, hk * p.group};
+    const int j0 = tile * TILE, j1 = min(j0 + TILE, n.nk);
+    int lo = 0, hi = 0;  // packed rows
+    if (j0 < j1) {
+        lo = col_lo(p, n, j0) * p.group;
+        hi = col_hi(p, n, j1 - 1) * p.group;
+    }
+    int blk0 = lo / QT, blk1 = hi > lo ? (hi + QT - 1) / QT : blk0;
+    const int per = (blk1 - blk0 + a.splits - 1) / a.splits;
+    blk0 += split * per;
+    blk1 = min(blk1, blk0 + per);
+    const uint32_t sk = smem_u32(smem), sv = sk + KBYTES, sq = sv + KBYTES, sg = sq + 2 * QBYTES;
+    const int m_all = p.group * p.q_len;
+    const auto load_q = [&](int blk, int st) {
+        load_rows<HD, QT>(sq + st * QBYTES, p.head_dim, p.q, [&](int r) {
+            const int m = blk * QT + r;
+            return m < m_all && rm.token(m) < n.nq
+                       ? reinterpret_cast<const uint16_t *>(p.q) + b * p.sq.b + rm.token(m) * p.sq.t + rm.head(m) * p.sq.h
+                       : nullptr;
+        });
+        load_rows<HD, QT>(sg + st * QBYTES, p.head_dim, p.d_o, [&](int r) {
+            const int m = blk * QT + r;
+            return m < m_all && rm.token(m) < n.nq
+                       ? reinterpret_cast<const uint16_t *>(p.d_o) + b * p.sg.b + rm.token(m) * p.sg.t + rm.head(m) * p.sg.h
+                       : nullptr;
+        });
+        if (threadIdx.x < QT) {
+            const int m = blk * QT + threadIdx.x;
+            const bool ok = m < m_all;
+            s_stat[st][threadIdx.x] =
+                ok ? a.stats[((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m)] : make_float2(CUDART_INF_F, 0.f);
+            s_keys[st][threadIdx.x] = ok ? make_int2(row_lo(p, n, rm.token(m)), row_hi(p, n, rm.token(m))) : make_int2(0, 0);
+        }
+        copy_commit();
+    };
+    if (blk0 < blk1) {
+        load_rows<HD, TILE>(sk, p.head_dim, p.k, [&](int r) {
+            return j0 + r < j1 ? reinterpret_cast<const uint16_t *>(p.k) + b * p.sk.b + (j0 + r) * p.sk.t + hk * p.sk.h : nullptr;
+        });
+        load_rows<HD, TILE>(sv, p.head_dim, p.v, [&](int r) {
+            return j0 + r < j1 ? reinterpret_cast<const uint16_t *>(p.v) + b * p.sv.b + (j0 + r) * p.sv.t + hk * p.sv.h : nullptr;
+        });
+        load_q(blk0, 0);
+    }
+    float ak[HD / 8][4] = {}, av[HD / 8][4] = {};
+    for (int blk = blk0; blk < blk1; ++blk) {
+        const int st = (blk - blk0) & 1;
+        copy_wait<0>();
+        __syncthreads();
+        if (blk + 1 < blk1) load_q(blk + 1, st ^ 1);
+        float s[QT / 8][4] = {}, dp[QT / 8][4] = {};
+        product_nt<T, HD, QT / 8>(s, sk, warp * 16, sq + st * QBYTES);
+        product_nt<T, HD, QT / 8>(dp, sv, warp * 16, sg + st * QBYTES);
+        to_p_ds<QT / 8>(s, dp, p.scale_log2,
+                        [&](int c, int e) {
+                            const int j = j0 + warp * 16 + (lane >> 2) + 8 * (e >> 1);
+                            const int2 k = s_keys[st][c * 8 + (lane & 3) * 2 + (e & 1)];
+                            return j >= k.x && j < k.y;
+                        },
+                        [&](int c, int e) { return s_stat[st][c * 8 + (lane & 3) * 2 + (e & 1)]; });
+        product_nn<T, HD, QT / 8>(av, s, sg + st * QBYTES);
+        product_nn<T, HD, QT / 8>(ak, dp, sq + st * QBYTES);
+    }
+    uint32_t redo = 0;
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int j = j0 + warp * 16 + (lane >> 2) + 8 * r;
+        const bool mine = j < p.kv_len;
+        if (a.splits > 1) {
+            const int64_t keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
+            if (mine) {
+                const int64_t row = ((int64_t)b * p.kv_heads + hk) * p.kv_len + j;
+                float *dk = a.part + ((2 * split) * keys + row) * p.head_dim, *dv = dk + keys * p.head_dim;
+#pragma unroll
+                for (int c = 0; c < HD / 8; ++c) {
+                    const int col = c * 8 + (lane & 3) * 2;
+                    if (col < p.head_dim) {
+                        *reinterpret_cast<float2 *>(dk + col) = make_float2(ak[c][2 * r], ak[c][2 * r + 1]);
+                        *reinterpret_cast<float2 *>(dv + col) = make_float2(av[c][2 * r], av[c][2 * r + 1]);
+                    }
+                }
+            }
+            continue;
+        }
+        bool fine = true;
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c)
+            fine = fine && finite(ak[c][2 * r]) && finite(ak[c][2 * r + 1]) && finite(av[c][2 * r]) && finite(av[c][2 * r + 1]);
+        const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
+        if (mine && !((bad >> (lane & ~3)) & 0xF)) {
+            T *dk = RowIO<T>::at(a.dk, p.sk, b, j, hk), *dv = RowIO<T>::at(a.dv, p.sv, b, j, hk);
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) {
+                const int col = c * 8 + (lane & 3) * 2;
+                if (col < p.head_dim) {
+                    *reinterpret_cast<uint32_t *>(dk + col) = Half<T>::pack(ak[c][2 * r] * p.scale, ak[c][2 * r + 1] * p.scale);
+                    *reinterpret_cast<uint32_t *>(dv + col) = Half<T>::pack(av[c][2 * r], av[c][2 * r + 1]);
+                }
+            }
+        }
+#pragma unroll
+        for (int g = 0; g < 8; ++g)
+            if ((bad >> (4 * g)) & 0xF) redo |= 1u << (g + 8 * r);
+    }
+    while (redo) {
+        const int j = j0 + warp * 16 + __ffs(redo) - 1;
+        redo &= redo - 1;
+        row_dkv<T>(p, a.stats, b, hk, j, a.dk, a.dv);
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(THREADS) join_dkv(const __grid_constant__ BackwardArgs a) {
+    pdl_wait();
+    const Problem &p = a.p;
+    const int64_t keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
+    const int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
+    if (row >= keys) return;
+    const int lane = threadIdx.x & 31, d = p.head_dim;
+    const int j = row % p.kv_len, hk = row / p.kv_len % p.kv_heads, b = row / p.kv_len / p.kv_heads;
+    float ak[4] = {0.f, 0.f, 0.f, 0.f}, av[4] = {0.f, 0.f, 0.f, 0.f};
+    for (int s = 0; s < a.splits; ++s)
+#pragma unroll
+        for (int c = 0; c < 4; ++c)
+            if (lane + 32 * c < d) {
+                const float *x = a.part + ((2 * s) * keys + row) * d + lane + 32 * c;
+                ak[c] += x[0];
+                av[c] += x[keys * d];
+            }
+    bool fine = true;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) fine = fine && finite(ak[c]) && finite(av[c]);
+    if (!__all_sync(0xFFFFFFFFu, fine)) {
+        row_dkv<T>(p, a.stats, b, hk, j, a.dk, a.dv);
+        return;
+    }
+#pragma unroll
+    for (int c = 0; c < 4; ++c) ak[c] *= p.scale;
+    RowIO<T>::store(RowIO<T>::at(a.dk, p.sk, b, j, hk), ak, d, lane);
+    RowIO<T>::store(RowIO<T>::at(a.dv, p.sv, b, j, hk), av, d, lane);
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+constexpr uint64_t up256(uint64_t x) { return (x + 255) & ~255ull; }
+
+int check(const scout_attn_t *a) {
+    if (!a) return SCOUT_ERR_INVALID;
+    if (a->dtype != SCOUT_DT_BF16 && a->dtype != SCOUT_DT_F16)
+        return a->dtype <= SCOUT_DT_I32 ? SCOUT_ERR_UNSUPPORTED : SCOUT_ERR_INVALID;
+    if (!a->batch || !a->q_heads || !a->kv_heads || a->q_heads % a->kv_heads || !a->head_dim) return SCOUT_ERR_INVALID;
+    if (a->head_dim % 8 || a->head_dim > 128) return SCOUT_ERR_UNSUPPORTED;
+    if (a->causal > 1 || (a->window && !a->causal) || !(a->scale > 0.f) || !(a->scale <= 3.402823466e38f)) return SCOUT_ERR_INVALID;
+    // row and key numbers, and packed rows, are 32-bit; grids are one-dimensional
+    const uint64_t group = a->q_heads / a->kv_heads;
+    if (a->q_len > (1u << 30) || a->kv_len > (1u << 30) || a->window > (1u << 30) || group * a->q_len > (1ull << 30) ||
+        (uint64_t)a->batch * a->q_heads > (1u << 24))
+        return SCOUT_ERR_UNSUPPORTED;
+    const uint32_t t[2] = {a->q_len, a->kv_len}, h[2] = {a->q_heads, a->kv_heads};
+    const uint64_t *s[5] = {a->q_stride, a->o_stride, a->do_stride, a->k_stride, a->v_stride};
+    for (int x = 0; x < 5; ++x) {
+        const uint32_t extent[3] = {a->batch, t[x > 2], h[x > 2]};
+        for (int d = 0; d < 3; ++d) {
+            if (extent[d] <= 1) continue;
+            if (s[x][d] == 0 || s[x][d] > (1ull << 40)) return SCOUT_ERR_INVALID;
+            if (s[x][d] % 8) return SCOUT_ERR_ALIGN;
+        }
+    }
+    return SCOUT_OK;
+}
+
+Strides strides(const uint64_t s[3], uint32_t b, uint32_t t, uint32_t h) {
+    return {b > 1 ? (int64_t)s[0] : 0, t > 1 ? (int64_t)s[1] : 0, h > 1 ? (int64_t)s[2] : 0};
+}
+
+Problem problem(const scout_attn_t &a) {
+    Problem p = {};
+    p.sq = strides(a.q_stride, a.batch, a.q_len, a.q_heads);
+    p.so = strides(a.o_stride, a.batch, a.q_len, a.q_heads);
+    p.sg = strides(a.do_stride, a.batch, a.q_len, a.q_heads);
+    p.sk = strides(a.k_stride, a.batch, a.kv_len, a.kv_heads);
+    p.sv = strides(a.v_stride, a.batch, a.kv_len, a.kv_heads);
+    p.batch = a.batch, p.q_len = a.q_len, p.kv_len = a.kv_len, p.q_heads = a.q_heads, p.kv_heads = a.kv_heads;
+    p.group = a.q_heads / a.kv_heads, p.head_dim = a.head_dim, p.causal = a.causal, p.window = a.window;
+    p.scale = a.scale, p.scale_log2 = a.scale * LOG2E;
+    return p;
+}
+
+// Parts along the long axis: as many as it takes to give every SM two blocks, each part at least `least` blocks long.
+int parts(uint64_t blocks, uint64_t along, uint64_t least) {
+    const uint64_t want = 2 * 148;
+    if (blocks >= want || along < 2 * least) return 1;
+    return (int)std::min<uint64_t>({(want + blocks - 1) / blocks, along / least, 64});
+}
+
+struct Shape {
+    uint64_t rows, keys, q_tiles, k_tiles;
+    int f_splits, q_splits, k_splits;
+    uint64_t forward_bytes, stats_bytes, backward_bytes;
+};
+Shape shape(const scout_attn_t &a) {
+    Shape s = {};
+    const uint64_t group = a.q_heads / a.kv_heads, bh = (uint64_t)a.batch * a.kv_heads;
+    s.rows = (uint64_t)a.batch * a.q_heads * a.q_len;
+    s.keys = bh * a.kv_len;
+    s.q_tiles = (group * a.q_len + TILE - 1) / TILE;
+    s.k_tiles = (a.kv_len + TILE - 1) / TILE;
+    const uint64_t seen = a.window ? std::min<uint64_t>(a.kv_len, a.window + TILE) : a.kv_len;
+    s.f_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 4);
+    s.q_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 4);
+    const uint64_t seen_by = group * (a.window ? std::min<uint64_t>(a.q_len, a.window + TILE) : a.q_len);
+    s.k_splits = parts(s.k_tiles * bh, (seen_by + 31) / 32, 8);
+    s.forward_bytes = s.f_splits > 1 ? up256(s.f_splits * s.rows * a.head_dim * 4) + up256(s.f_splits * s.rows * 8) : 0;
+    s.stats_bytes = up256(s.rows * 8);
+    const uint64_t pq = s.q_splits > 1 ? s.q_splits * s.rows * a.head_dim * 4 : 0;
+    const uint64_t pk = s.k_splits > 1 ? 2 * s.k_splits * s.keys * a.head_dim * 4 : 0;
+    s.backward_bytes = s.stats_bytes + up256(std::max(pq, pk));  // the two kernels follow one another
+    return s;
+}
+
+template <typename K> int big_smem(K kernel, int bytes) {
+    SCOUT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    return SCOUT_OK;
+}
+
+template <typename Args>
+cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t stream, const Args &args, bool dependent) {
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)grid);
+    cfg.blockDim = dim3(THREADS);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = dependent ? 1 : 0;
+    return cudaLaunchKernelEx(&cfg, kernel, args);
+}
+
+template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaStream_t stream) {
+    constexpr int smem = 5 * TILE * HD * 2;
+    if (int rc = big_smem(forward_tiles<T, HD>, smem)) return rc;
+    f.tiles = (int)s.q_tiles;
+    f.splits = s.f_splits;
+    SCOUT_CUDA(launch(forward_tiles<T, HD>, s.q_tiles * f.p.batch * f.p.kv_heads * f.splits, smem, stream, f, false));
+    if (f.splits > 1) SCOUT_CUDA(launch(forward_join<T>, (s.rows + 3) / 4, 0, stream, f, true));
+    return SCOUT_OK;
+}
+
+template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cudaStream_t stream) {
+    constexpr int smem_q = 6 * TILE * HD * 2, smem_k = 2 * TILE * HD * 2 + 4 * 32 * HD * 2;
+    if (int rc = big_smem(backward_dq<T, HD>, smem_q)) return rc;
+    if (int rc = big_smem(backward_dkv<T, HD>, smem_k)) return rc;
+    const uint64_t bh = (uint64_t)a.p.batch * a.p.kv_heads;
+    if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + 3) / 4, 0, stream, a, false));
+    // every kernel that follows waits for the whole of the one before it (griddepcontrol.wait), so the
+    // statistics are there for all of them and the shared parts are free
+    if (s.rows) {
+        a.tiles = (int)s.q_tiles, a.splits = s.q_splits;
+        SCOUT_CUDA(launch(backward_dq<T, HD>, s.q_tiles * bh * a.splits, smem_q, stream, a, true));
+        if (a.splits > 1) SCOUT_CUDA(launch(join_dq<T>, (s.rows + 3) / 4, 0, stream, a, true));
+    }
+    if (s.keys) {
+        a.tiles = (int)s.k_tiles, a.splits = s.k_splits;
+        SCOUT_CUDA(launch(backward_dkv<T, HD>, s.k_tiles * bh * a.splits, smem_k, stream, a, s.rows > 0));
+        if (a.splits > 1) SCOUT_CUDA(launch(join_dkv<T>, (s.keys + 3) / 4, 0, stream, a, true));
+    }
+    return SCOUT_OK;
+}
+
+bool aligned(const void *x, uintptr_t to) { return (reinterpret_cast<uintptr_t>(x) & (to - 1)) == 0; }
+
+}  // namespace
+}  // namespace attn
+}  // namespace scout
+
+extern "C" int scout_attn_workspace(const scout_attn_t *a, uint64_t *forward_bytes, uint64_t *backward_bytes) {
+    using namespace scout::attn;
+    if (int rc = check(a)) return rc;
+    if (!forward_bytes || !backward_bytes) return SCOUT_ERR_INVALID;
+    const Shape s = shape(*a);
+    *forward_bytes = s.forward_bytes;
+    *backward_bytes = s.backward_bytes;
+    return SCOUT_OK;
+}
+
+extern "C" int scout_attn_forward(const scout_attn_t *a, const void *q, const void *k, const void *v, const int32_t *q_lens,
+                                  const int32_t *kv_lens, void *o, float *lse, void *workspace, uint64_t workspace_bytes,
+                                  void *stream) {
+    using namespace scout;
+    using namespace scout::attn;
+    if (int rc = check(a)) return rc;
+    const Shape s = shape(*a);
+    if (s.rows == 0) return SCOUT_OK;
+    if (!q || !o || !lse || (s.keys && (!k || !v))) return SCOUT_ERR_INVALID;
+    if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(lse, 4) || !aligned(q_lens, 4) ||
+        !aligned(kv_lens, 4) || !aligned(workspace, 256))
+        return SCOUT_ERR_ALIGN;
+    if (workspace_bytes < s.forward_bytes || (s.forward_bytes && !workspace)) return SCOUT_ERR_INVALID;
+    ForwardArgs f = {};
+    f.p = problem(*a);
+    f.p.q = q, f.p.k = k, f.p.v = v, f.p.q_lens = q_lens, f.p.kv_lens = kv_lens;
+    f.o = o, f.lse = lse;
+    f.part_o = (float *)workspace;
+    f.part_ml = (float2 *)((uint8_t *)workspace + up256(s.f_splits * s.rows * a->head_dim * 4));
+    const bool wide = a->head_dim > 64;
+    if (a->dtype == SCOUT_DT_BF16)
+        return wide ? forward<__nv_bfloat16, 128>(s, f, (cudaStream_t)stream) : forward<__nv_bfloat16, 64>(s, f, (cudaStream_t)stream);
+    return wide ? forward<__half, 128>(s, f, (cudaStream_t)stream) : forward<__half, 64>(s, f, (cudaStream_t)stream);
+}
+
+extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const void *k, const void *v, const void *o,
+                                   const float *lse, const void *d_o, const int32_t *q_lens, const int32_t *kv_lens, void *dq,
+                                   void *dk, void *dv, void *workspace, uint64_t workspace_bytes, void *stream) {
+    using namespace scout;
+    using namespace scout::attn;
+    if (int rc = check(a)) return rc;
+    const Shape s = shape(*a);
+    if (s.rows == 0 && s.keys == 0) return SCOUT_OK;
+    if ((s.rows && (!q || !o || !lse || !d_o || !dq)) || (s.keys && (!k || !v || !dk || !dv))) return SCOUT_ERR_INVALID;
+    const void *all[9] = {q, k, v, o, d_o, dq, dk, dv, nullptr};
+    for (const void *x : all)
+        if (!aligned(x, 16)) return SCOUT_ERR_ALIGN;
+    if (!aligned(lse, 4) || !aligned(q_lens, 4) || !aligned(kv_lens, 4) || !aligned(workspace, 256)) return SCOUT_ERR_ALIGN;
+    if (workspace_bytes < s.backward_bytes || (s.backward_bytes && !workspace)) return SCOUT_ERR_INVALID;
+    BackwardArgs b = {};
+    b.p = problem(*a);
+    b.p.q = q, b.p.k = k, b.p.v = v, b.p.o = o, b.p.d_o = d_o, b.p.q_lens = q_lens, b.p.kv_lens = kv_lens;
+    b.lse = lse, b.dq = dq, b.dk = dk, b.dv = dv;
+    b.stats = (float2 *)workspace;
+    b.part = (float *)((uint8_t *)workspace + s.stats_bytes);
+    const bool wide = a->head_dim > 64;
+    if (a->dtype == SCOUT_DT_BF16)
+        return wide ? backward<__nv_bfloat16, 128>(s, b, (cudaStream_t)stream) : backward<__nv_bfloat16, 64>(s, b, (cudaStream_t)stream);
+    return wide ? backward<__half, 128>(s, b, (cudaStream_t)stream) : backward<__half, 64>(s, b, (cudaStream_t)stream);
+}

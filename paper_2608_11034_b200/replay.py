@@ -1,0 +1,203 @@
+"""Operators of one replayed transformer layer, on torch tensors.
+
+In-situ replay (Sec. 6 of the paper) runs a layer again on every peer from the
+same captured inputs; exact consensus then compares the output and the gradients
+bit by bit.  The operators here give the same bits on every healthy GPU: no
+floating-point atomics, every sum in an order that the sizes alone fix.
+
+    attention_forward, attention_backward   softmax attention and its gradient
+    checkpoint_pack, checkpoint_unpack      captured activations held in 8 bits
+    checkpoint_wgrad                        a projection's weight gradient, straight
+                                            from such a checkpoint
+
+Each call checks its arguments, allocates outputs and scratch from torch's
+allocator on the current stream and enqueues the library's kernels there
+(``include/scout_replay.h`` has the definitions).  Tensors are used where they
+lie: as usual in torch, one made on another stream needs that stream's work
+waited for, and ``record_stream`` if it is freed early.
+"""
+from __future__ import annotations
+
+import functools
+import math
+from typing import Optional
+
+import numpy as np
+import torch
+
+from . import binding
+
+_CODE = {torch.float32: binding.DT_F32, torch.bfloat16: binding.DT_BF16, torch.float16: binding.DT_F16}
+_SIXTEEN = (torch.bfloat16, torch.float16)
+
+
+def _fail(what: str):
+    raise ValueError(what)
+
+
+@functools.lru_cache(maxsize=256)
+def _attention(dtype, batch, q_len, kv_len, q_heads, kv_heads, head_dim, causal, window, scale, strides):
+    """-> (record, its address, scratch bytes of the forward and of the backward pass); sizes only, no data"""
+    a = np.zeros(1, dtype=binding.ATTN_DTYPE)
+    a[0] = (_CODE[dtype], batch, q_len, kv_len, q_heads, kv_heads, head_dim, causal, window, scale) + strides
+    return (a, a.ctypes.data) + binding.scout_attn_workspace(a.ctypes.data)
+
+
+def _lens(x, batch, device, name) -> int:
+    if x is None:
+        return 0
+    if x.dtype != torch.int32 or x.shape != (batch,) or x.device != device or not x.is_contiguous():
+        _fail(f"{name}: a contiguous int32 tensor [batch] on the queries' device is wanted")
+    return x.data_ptr()
+
+
+def _strided(x, name):
+    if x.shape[-1] > 1 and x.stride(-1) != 1:
+        _fail(f"{name}: a head's elements must be adjacent (last stride 1)")
+    s = x.stride()
+    return s[0], s[1], s[2]
+
+
+def _problem(q, k, v, o, d_o, causal, window, scale):
+    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
+        _fail("q is [batch, q_len, q_heads, head_dim], k and v are [batch, kv_len, kv_heads, head_dim]")
+    b, tq, hq, d = q.shape
+    if k.shape[0] != b or k.shape[3] != d:
+        _fail("q and k differ in batch or head_dim")
+    if q.dtype not in _SIXTEEN:
+        _fail("attention takes bfloat16 or float16")
+    for x in (k, v, o, d_o):
+        if x.dtype != q.dtype or x.device != q.device:
+            _fail("q, k, v, o and do must share one dtype and device")
+    if not q.is_cuda:
+        _fail("tensors must be on a CUDA device")
+    for x, name in ((o, "o"), (d_o, "do")):
+        if x.shape != q.shape:
+            _fail(f"{name} must have the shape of q")
+    strides = tuple(_strided(x, n) for x, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o"), (d_o, "do")))
+    return _attention(q.dtype, b, tq, k.shape[1], hq, k.shape[2], d, int(bool(causal)), int(window),
+                      1.0 / math.sqrt(d) if scale is None else float(scale), strides)
+
+
+def _scratch(nbytes, device):
+    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
+
+
+def _stream(x) -> int:
+    return torch.cuda.current_stream(x.device).cuda_stream
+
+
+def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, window: int = 0,
+                      scale: Optional[float] = None, q_lens: Optional[torch.Tensor] = None,
+                      kv_lens: Optional[torch.Tensor] = None):
+    """Softmax attention.  q: [batch, q_len, q_heads, head_dim], k, v: [batch, kv_len, kv_heads, head_dim]
+    (bfloat16 or float16; any strides that are multiples of 8 elements, last axis adjacent); query head h
+    reads key head h // (q_heads // kv_heads).
+
+    causal: a row sees the keys up to its own position, the last row standing at the last key.
+    window: with causal, only its own position and the window - 1 before it (0: all).
+    q_lens, kv_lens: int32 [batch], the tokens in use of padded sequences.
+    -> (o like q, lse float32 [batch, q_heads, q_len]); rows that see nothing give 0 and -inf."""
+    o = torch.empty_like(q)
+    _, at, nbytes, _ = _problem(q, k, v, o, o, causal, window, scale)
+    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
+    ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
+    ws = _scratch(nbytes, q.device)
+    with torch.cuda.device(q.device):
+        binding.scout_attn_forward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
+                                   ws.data_ptr() if ws is not None else 0, nbytes, _stream(q))
+    return o, lse
+
+
+def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
+                       do: torch.Tensor, *, causal: bool = False, window: int = 0, scale: Optional[float] = None,
+                       q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None):
+    """Gradients of attention_forward's o with respect to q, k and v, from the gradient `do` of o and what the
+    forward pass returned; the other arguments as there.  Gradients of key heads that several query heads share are
+    summed over those.  -> (dq, dk, dv), laid out like q, k, v."""
+    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    for x, y, name in ((q, dq, "q"), (k, dk, "k"), (v, dv, "v")):
+        if x.stride() != y.stride():
+            _fail(f"{name}: overlapping or gapped memory has no gradient laid out like it; pass {name}.contiguous()")
+    _, at, _, nbytes = _problem(q, k, v, o, do, causal, window, scale)
+    if lse.dtype != torch.float32 or lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous() or \
+            lse.device != q.device:
+        _fail("lse: the forward pass's, a contiguous float32 tensor [batch, q_heads, q_len]")
+    ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
+    ws = _scratch(nbytes, q.device)
+    with torch.cuda.device(q.device):
+        binding.scout_attn_backward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
+                                    ql, kl, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
+                                    ws.data_ptr() if ws is not None else 0, nbytes, _stream(q))
+    return dq, dk, dv
+
+
+def _matrix(x, name):
+    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+        _fail(f"{name}: a matrix with adjacent row elements is wanted")
+    if not x.is_cuda:
+        _fail("tensors must be on a CUDA device")
+    return max(x.stride(0), x.shape[1], 1)
+
+
+def _checkpoint(codes, exps):
+    stride = _matrix(codes, "codes")
+    rows, cols = codes.shape
+    if codes.dtype != torch.int8 or exps.dtype != torch.int8 or not exps.is_contiguous() or exps.device != codes.device or \
+            exps.shape != (rows, -(-cols // binding.CKPT_BLOCK)):
+        _fail("codes: int8 [rows, cols], exps: contiguous int8 [rows, ceil(cols / 32)]")
+    return rows, cols, stride
+
+
+def checkpoint_pack(x: torch.Tensor):
+    """Hold the activation x [rows, cols] (float32, bfloat16 or float16) in 8 bits.
+    -> (codes int8 [rows, cols], exps int8 [rows, ceil(cols / 32)]): x is about codes * 2**exps, exps per block of 32 columns."""
+    stride = _matrix(x, "x")
+    if x.dtype not in _CODE:
+        _fail("activations are float32, bfloat16 or float16")
+    rows, cols = x.shape
+    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
+    exps = torch.empty((rows, -(-cols // binding.CKPT_BLOCK)), dtype=torch.int8, device=x.device)
+    with torch.cuda.device(x.device):
+        binding.scout_ckpt_pack(_CODE[x.dtype], rows, cols, x.data_ptr(), stride, codes.data_ptr(), max(cols, 1),
+                                exps.data_ptr(), _stream(x))
+    return codes, exps
+
+
+def checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
+    """The activation a checkpoint stands for, in `dtype`."""
+    rows, cols, stride = _checkpoint(codes, exps)
+    if dtype not in _CODE:
+        _fail("activations are float32, bfloat16 or float16")
+    x = torch.empty((rows, cols), dtype=dtype, device=codes.device)
+    with torch.cuda.device(codes.device):
+        binding.scout_ckpt_unpack(_CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(), x.data_ptr(),
+                                  max(cols, 1), _stream(codes))
+    return x
+
+
+@functools.lru_cache(maxsize=256)
+def _wgrad_scratch(code, rows, outs, ins):
+    return binding.scout_ckpt_wgrad_workspace(code, rows, outs, ins)
+
+
+def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, *, out_dtype: torch.dtype = torch.float32,
+                     grad: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Weight gradient dW = dy^T x of y = x W^T, x taken from its checkpoint.  dy: [rows, outs], bfloat16 or float16.
+    -> dW [outs, ins] in out_dtype (float32 or dy's); with `grad` (of those dtypes) dW is added to it in place."""
+    rows, ins, code_stride = _checkpoint(codes, exps)
+    dy_stride = _matrix(dy, "dy")
+    if dy.dtype not in _SIXTEEN or dy.shape[0] != rows or dy.device != codes.device:
+        _fail("dy: a bfloat16 or float16 matrix with the checkpoint's rows, on its device")
+    outs = dy.shape[1]
+    dw = torch.empty((outs, ins), dtype=out_dtype, device=dy.device) if grad is None else grad
+    dw_stride = _matrix(dw, "grad")
+    if dw.dtype not in (torch.float32, dy.dtype) or dw.shape != (outs, ins) or dw.device != dy.device:
+        _fail("the gradient is [outs, ins], float32 or of dy's dtype, on dy's device")
+    nbytes = _wgrad_scratch(_CODE[dy.dtype], rows, outs, ins)
+    ws = _scratch(nbytes, dy.device)
+    with torch.cuda.device(dy.device):
+        binding.scout_ckpt_wgrad(_CODE[dy.dtype], _CODE[dw.dtype], rows, outs, ins, dy.data_ptr(), dy_stride, codes.data_ptr(),
+                                 code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
+                                 ws.data_ptr() if ws is not None else 0, nbytes, _stream(dy))
+    return dw
