@@ -121,6 +121,11 @@ SCOUT_API int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t rows
                                const int8_t *exps, void *dw, uint64_t dw_stride, uint32_t accumulate,
                                void *workspace, uint64_t workspace_bytes, void *stream);
 
+/* The kernels' waits on their own copies and products are bounded (2 s).  *count becomes the number that gave up on the
+ * current device since the last call (0 on healthy hardware; results of a call with one are not valid) and is reset.
+ * Synchronises the device. */
+SCOUT_API int scout_replay_error(uint32_t *count /*host*/);
+
 #ifdef __cplusplus
 }
 #endif

@@ -108,6 +108,7 @@ def lib():
             "scout_ckpt_unpack": (C.c_int, [u32, u64, u64, vp, u64, vp, vp, u64, vp]),
             "scout_ckpt_wgrad_workspace": (C.c_int, [u32, u64, u64, u64, C.POINTER(u64)]),
             "scout_ckpt_wgrad": (C.c_int, [u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, u64, u32, vp, u64, vp]),
+            "scout_replay_error": (C.c_int, [C.POINTER(u32)]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
             "scout_last_cuda_error": (C.c_char_p, []),
@@ -428,6 +429,13 @@ def scout_ckpt_wgrad(dtype: int, out_dtype: int, rows: int, outs: int, ins: int,
                      workspace_bytes: int, stream: int) -> None:
     _check(lib().scout_ckpt_wgrad(dtype, out_dtype, rows, outs, ins, dy, dy_stride, codes, code_stride, exps, dw, dw_stride,
                                   accumulate, workspace, workspace_bytes, stream), "scout_ckpt_wgrad")
+
+
+def scout_replay_error() -> int:
+    """Waits of the replay kernels that gave up on the current device since the last call (synchronises)."""
+    n = C.c_uint32()
+    _check(lib().scout_replay_error(C.byref(n)), "scout_replay_error")
+    return n.value
 
 
 def scout_selftest_bounded_wait(limit_ns: int, d_out: int, stream: int) -> None:

@@ -40,62 +40,212 @@ __device__ __forceinline__ int step_of(uint32_t amax_bits) {
     return amax_bits == 0 ? -126 : max(x - 6, -126);
 }
 
-template <typename T> __device__ __forceinline__ int code_of(float x, int e) {
-    // 2^-e may be 2^126 (finite) down to 2^-122 (normal): one exact product
-    const float c = rintf(x * __uint_as_float((uint32_t)(127 - e) << 23));
+// The code's byte.  x 2^-e + 1.5 2^23 in one fused operation rounds to an integer once, ties to even, and leaves it in the low
+// bits (|x 2^-e| <= 127 by the choice of e); the conversion instruction runs at a quarter of the rate.
+template <typename T> __device__ __forceinline__ uint32_t code_of(float x, int e) {
+    constexpr float MAGIC = 12582912.f;
+    // 2^-e lies between 2^126 (finite) and 2^-122 (normal)
+    const float c = fmaf(x, __uint_as_float((uint32_t)(127 - e) << 23), MAGIC);
     const float top = e == TOP_STEP<T> ? 63.f : 127.f;
-    return is_finite_bits(__float_as_uint(x) & 0x7FFFFFFFu) ? (int)fminf(fmaxf(c, -top), top) : -128;
+    const uint32_t byte = __float_as_uint(fminf(fmaxf(c, MAGIC - top), MAGIC + top)) & 0xFFu;
+    return is_finite_bits(__float_as_uint(x) & 0x7FFFFFFFu) ? byte : 0x80u;
 }
+
+// n / d for n < 2^31: one high product and a shift, with the constants of the divisor made on the host
+struct Divisor {
+    uint32_t d, mul, shift;
+    Divisor(uint32_t n = 1) : d(n), mul(0), shift(0) {
+        while ((1ull << shift) < n) ++shift;                                      // 2^shift >= d
+        mul = (uint32_t)((((1ull << shift) - n) << 32) / n + 1);                  // 2^(32 + shift) / d rounded up, less 2^32
+    }
+    __device__ __forceinline__ uint32_t quotient(uint32_t n) const { return (__umulhi(n, mul) + n) >> shift; }
+};
 
 struct Args {
     const void *x;
     void *out;
     int8_t *codes, *exps;
     int64_t x_stride, code_stride;
-    int64_t rows, cols, blocks;  // blocks of 32 in a row
+    int64_t cols, blocks;  // blocks of 32 in a row
+    uint32_t groups;       // groups of 8 blocks, of all rows
+    Divisor per_row;       // groups of a row
 };
 
-// One warp per block of 32, a lane per element: every alignment, every length.
-template <typename T> __global__ void __launch_bounds__(THREADS) pack_elements(const Args a) {
+// A warp's unit of work is a group: eight blocks, 256 elements of a row.
+constexpr int GROUP = 256;
+struct Place {
+    int64_t row, col;
+    bool ok;
+};
+__device__ __forceinline__ Place place(const Args &a, uint32_t g) {
+    const uint32_t row = a.per_row.quotient(g);
+    return {(int64_t)row, (int64_t)(g - row * a.per_row.d) * GROUP, g < a.groups};
+}
+
+// ---- rows on 16-byte boundaries whose length is a multiple of 8 -----------------------------------
+// A lane holds eight elements, four lanes a block; UNROLL groups of a warp are in flight together.  16384 x 14336 bf16:
+// see the launch comment below for what it reaches.
+constexpr int UNROLL = 4;
+template <typename T> struct Eight {
+    static constexpr int N = sizeof(T) / 2;  // 16-byte loads
+    uint4 w[N];
+    __device__ __forceinline__ void load(const T *p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = __ldcs(reinterpret_cast<const uint4 *>(p) + i);
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ float get(int i) const { return up<T>(reinterpret_cast<const T *>(w)[i]); }
+    __device__ __forceinline__ void set(int i, float x) { reinterpret_cast<T *>(w)[i] = down<T>(x); }
+    __device__ __forceinline__ void store(T *p) const {
+#pragma unroll
+        for (int i = 0; i < N; ++i) __stcs(reinterpret_cast<uint4 *>(p) + i, w[i]);
+    }
+};
+
+template <typename T> __global__ void __launch_bounds__(THREADS) pack_vectors(const __grid_constant__ Args a) {
     const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (THREADS / 32);
-    for (int64_t i = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); i < a.rows * a.blocks; i += warps) {
-        const int64_t row = i / a.blocks, blk = i % a.blocks, col = blk * SCOUT_CKPT_BLOCK + lane;
-        const float x = col < a.cols ? up<T>(reinterpret_cast<const T *>(a.x)[row * a.x_stride + col]) : 0.f;
-        const uint32_t bits = __float_as_uint(x) & 0x7FFFFFFFu;
+    const uint32_t g0 = (blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * UNROLL;
+    Eight<T> x[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const Place p = place(a, g0 + u);
+        if (p.ok && p.col + lane * 8 < a.cols) x[u].load(reinterpret_cast<const T *>(a.x) + p.row * a.x_stride + p.col + lane * 8);
+        else x[u].zero();
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const Place p = place(a, g0 + u);
+        uint32_t top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t bits = __float_as_uint(x[u].get(i)) & 0x7FFFFFFFu;
+            top = max(top, is_finite_bits(bits) ? bits : 0u);
+        }
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
+        top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
+        const int e = step_of(top);
+        uint32_t c[2] = {0, 0};
+#pragma unroll
+        for (int i = 0; i < 8; ++i) c[i >> 2] |= code_of<T>(x[u].get(i), e) << (8 * (i & 3));
+        const int64_t col = p.col + lane * 8;
+        if (p.ok && col < a.cols) {
+            __stcs(reinterpret_cast<uint2 *>(a.codes + p.row * a.code_stride + col), make_uint2(c[0], c[1]));
+            if ((lane & 3) == 0) a.exps[p.row * a.blocks + (col >> 5)] = (int8_t)e;
+        }
+    }
+}
+
+template <typename T> __global__ void __launch_bounds__(THREADS) unpack_vectors(const __grid_constant__ Args a) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t g0 = (blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5)) * UNROLL;
+    uint2 c[UNROLL];
+    int e[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const Place p = place(a, g0 + u);
+        const int64_t col = p.col + lane * 8;
+        c[u] = make_uint2(0, 0);
+        e[u] = 0;
+        if (p.ok && col < a.cols) {
+            c[u] = __ldcs(reinterpret_cast<const uint2 *>(a.codes + p.row * a.code_stride + col));
+            e[u] = a.exps[p.row * a.blocks + (col >> 5)];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+        const Place p = place(a, g0 + u);
+        const int64_t col = p.col + lane * 8;
+        if (!p.ok || col >= a.cols) continue;
+        Eight<T> x;
+        float f[8];
+        restore4(f, c[u].x, step_value(e[u]));
+        restore4(f + 4, c[u].y, step_value(e[u]));
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x.set(i, f[i]);
+        x.store(reinterpret_cast<T *>(a.out) + p.row * a.x_stride + col);
+    }
+}
+
+// ---- every other alignment and length ---------------------------------------------------------------
+// A lane per element, a warp instruction per block of 32: accesses stay coalesced wherever a row starts.
+constexpr int BLOCKS = GROUP / SCOUT_CKPT_BLOCK;
+template <typename T> __global__ void __launch_bounds__(THREADS) pack_elements(const __grid_constant__ Args a) {
+    const int lane = threadIdx.x & 31;
+    const Place p = place(a, blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5));
+    if (!p.ok) return;
+    const T *src = reinterpret_cast<const T *>(a.x) + p.row * a.x_stride + p.col + lane;
+    int8_t *dst = a.codes + p.row * a.code_stride + p.col + lane;
+    const int left = (int)min((int64_t)GROUP, a.cols - p.col) - lane;  // elements from this lane's first on
+    float x[BLOCKS];
+#pragma unroll
+    for (int u = 0; u < BLOCKS; ++u) x[u] = 32 * u < left ? up<T>(src[32 * u]) : 0.f;
+    int mine = 0;
+#pragma unroll
+    for (int u = 0; u < BLOCKS; ++u) {
+        const uint32_t bits = __float_as_uint(x[u]) & 0x7FFFFFFFu;
         const int e = step_of(__reduce_max_sync(0xFFFFFFFFu, is_finite_bits(bits) ? bits : 0u));
-        if (col < a.cols) a.codes[row * a.code_stride + col] = (int8_t)code_of<T>(x, e);
-        if (lane == 0) a.exps[i] = (int8_t)e;
+        if (32 * u < left) dst[32 * u] = (int8_t)code_of<T>(x[u], e);
+        mine = lane == u ? e : mine;
     }
+    if (lane < BLOCKS && p.col + lane * SCOUT_CKPT_BLOCK < a.cols)
+        a.exps[p.row * a.blocks + p.col / SCOUT_CKPT_BLOCK + lane] = (int8_t)mine;
 }
-template <typename T> __global__ void __launch_bounds__(THREADS) unpack_elements(const Args a) {
+template <typename T> __global__ void __launch_bounds__(THREADS) unpack_elements(const __grid_constant__ Args a) {
     const int lane = threadIdx.x & 31;
-    const int64_t warps = (int64_t)gridDim.x * (THREADS / 32);
-    for (int64_t i = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5); i < a.rows * a.blocks; i += warps) {
-        const int64_t row = i / a.blocks, blk = i % a.blocks, col = blk * SCOUT_CKPT_BLOCK + lane;
-        if (col < a.cols)
-            reinterpret_cast<T *>(a.out)[row * a.x_stride + col] = down<T>(restore(a.codes[row * a.code_stride + col], a.exps[i]));
+    const Place p = place(a, blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5));
+    if (!p.ok) return;
+    const int8_t *src = a.codes + p.row * a.code_stride + p.col + lane, *exps = a.exps + p.row * a.blocks + p.col / SCOUT_CKPT_BLOCK;
+    T *dst = reinterpret_cast<T *>(a.out) + p.row * a.x_stride + p.col + lane;
+    const int left = (int)min((int64_t)GROUP, a.cols - p.col) - lane;
+    int c[BLOCKS], e[BLOCKS];
+#pragma unroll
+    for (int u = 0; u < BLOCKS; ++u) {
+        c[u] = 32 * u < left ? src[32 * u] : 0;
+        e[u] = 32 * u < left ? exps[u] : 0;
     }
+#pragma unroll
+    for (int u = 0; u < BLOCKS; ++u)
+        if (32 * u < left) dst[32 * u] = down<T>(restore(c[u], e[u]));
 }
 
-unsigned grid_for(int64_t warps) { return (unsigned)std::min<int64_t>((warps + THREADS / 32 - 1) / (THREADS / 32), 148 * 8 * 8); }
-
-template <typename T> int pack(const Args &a, cudaStream_t s) {
-    pack_elements<T><<<grid_for(a.rows * a.blocks), THREADS, 0, s>>>(a);
-    SCOUT_CUDA(cudaGetLastError());
+// Rows in slices of fewer than 2^31 groups; per_block groups to a block of threads.
+template <typename T, typename K> int launch(K kernel, Args a, uint64_t rows, uint32_t per_block, cudaStream_t stream) {
+    const uint64_t per_row = ((uint64_t)a.cols + GROUP - 1) / GROUP, slice = std::max<uint64_t>(1, (1ull << 30) / per_row);
+    a.per_row = Divisor((uint32_t)per_row);
+    for (uint64_t r = 0; r < rows; r += slice) {
+        const uint64_t n = std::min(slice, rows - r);
+        Args b = a;
+        b.groups = (uint32_t)(n * per_row);
+        if (a.x) b.x = reinterpret_cast<const T *>(a.x) + r * a.x_stride;
+        if (a.out) b.out = reinterpret_cast<T *>(a.out) + r * a.x_stride;
+        b.codes = a.codes + r * a.code_stride, b.exps = a.exps + r * a.blocks;
+        kernel<<<(b.groups + per_block - 1) / per_block, THREADS, 0, stream>>>(b);
+        SCOUT_CUDA(cudaGetLastError());
+    }
     return SCOUT_OK;
 }
-template <typename T> int unpack(const Args &a, cudaStream_t s) {
-    unpack_elements<T><<<grid_for(a.rows * a.blocks), THREADS, 0, s>>>(a);
-    SCOUT_CUDA(cudaGetLastError());
-    return SCOUT_OK;
+
+template <typename T> bool vectors(const Args &a, const void *x) {
+    return a.cols % 8 == 0 && a.x_stride % (16 / sizeof(T)) == 0 && (reinterpret_cast<uintptr_t>(x) & 15) == 0 &&
+           a.code_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(a.codes) & 7) == 0;
+}
+template <typename T> int pack(const Args &a, uint64_t rows, cudaStream_t s) {
+    return vectors<T>(a, a.x) ? launch<T>(pack_vectors<T>, a, rows, THREADS / 32 * UNROLL, s)
+                              : launch<T>(pack_elements<T>, a, rows, THREADS / 32, s);
+}
+template <typename T> int unpack(const Args &a, uint64_t rows, cudaStream_t s) {
+    return vectors<T>(a, a.out) ? launch<T>(unpack_vectors<T>, a, rows, THREADS / 32 * UNROLL, s)
+                                : launch<T>(unpack_elements<T>, a, rows, THREADS / 32, s);
 }
 
 int check(uint32_t dtype, uint64_t rows, uint64_t cols, const void *x, uint64_t x_stride, const int8_t *codes, uint64_t code_stride,
           const int8_t *exps) {
     if (dtype > SCOUT_DT_I32) return SCOUT_ERR_INVALID;
     if (dtype != SCOUT_DT_F32 && dtype != SCOUT_DT_BF16 && dtype != SCOUT_DT_F16) return SCOUT_ERR_UNSUPPORTED;
-    if (rows > (1ull << 40) || cols > (1ull << 40) || (rows && cols && rows > (1ull << 48) / cols)) return SCOUT_ERR_UNSUPPORTED;
+    if (rows > (1ull << 40) || cols > (1ull << 36) || (rows && cols && rows > (1ull << 48) / cols)) return SCOUT_ERR_UNSUPPORTED;
     if (rows == 0 || cols == 0) return SCOUT_OK;
     if (!x || !codes || !exps || x_stride < cols || code_stride < cols || x_stride > (1ull << 44) || code_stride > (1ull << 44))
         return SCOUT_ERR_INVALID;
@@ -103,11 +253,11 @@ int check(uint32_t dtype, uint64_t rows, uint64_t cols, const void *x, uint64_t 
     return SCOUT_OK;
 }
 
-Args args(uint64_t rows, uint64_t cols, uint64_t x_stride, int8_t *codes, uint64_t code_stride, int8_t *exps) {
+Args args(uint64_t cols, uint64_t x_stride, int8_t *codes, uint64_t code_stride, int8_t *exps) {
     Args a = {};
     a.codes = codes, a.exps = exps;
     a.x_stride = (int64_t)x_stride, a.code_stride = (int64_t)code_stride;
-    a.rows = (int64_t)rows, a.cols = (int64_t)cols, a.blocks = (int64_t)((cols + SCOUT_CKPT_BLOCK - 1) / SCOUT_CKPT_BLOCK);
+    a.cols = (int64_t)cols, a.blocks = (int64_t)((cols + SCOUT_CKPT_BLOCK - 1) / SCOUT_CKPT_BLOCK);
     return a;
 }
 
@@ -120,11 +270,11 @@ extern "C" int scout_ckpt_pack(uint32_t dtype, uint64_t rows, uint64_t cols, con
     using namespace scout::ckpt;
     if (int rc = check(dtype, rows, cols, x, x_stride, codes, code_stride, exps)) return rc;
     if (rows == 0 || cols == 0) return SCOUT_OK;
-    Args a = args(rows, cols, x_stride, codes, code_stride, exps);
+    Args a = args(cols, x_stride, codes, code_stride, exps);
     a.x = x;
-    if (dtype == SCOUT_DT_F32) return pack<float>(a, (cudaStream_t)stream);
-    if (dtype == SCOUT_DT_BF16) return pack<__nv_bfloat16>(a, (cudaStream_t)stream);
-    return pack<__half>(a, (cudaStream_t)stream);
+    if (dtype == SCOUT_DT_F32) return pack<float>(a, rows, (cudaStream_t)stream);
+    if (dtype == SCOUT_DT_BF16) return pack<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
+    return pack<__half>(a, rows, (cudaStream_t)stream);
 }
 
 extern "C" int scout_ckpt_unpack(uint32_t dtype, uint64_t rows, uint64_t cols, const int8_t *codes, uint64_t code_stride,
@@ -132,9 +282,9 @@ extern "C" int scout_ckpt_unpack(uint32_t dtype, uint64_t rows, uint64_t cols, c
     using namespace scout::ckpt;
     if (int rc = check(dtype, rows, cols, x, x_stride, codes, code_stride, exps)) return rc;
     if (rows == 0 || cols == 0) return SCOUT_OK;
-    Args a = args(rows, cols, x_stride, const_cast<int8_t *>(codes), code_stride, const_cast<int8_t *>(exps));
+    Args a = args(cols, x_stride, const_cast<int8_t *>(codes), code_stride, const_cast<int8_t *>(exps));
     a.out = x;
-    if (dtype == SCOUT_DT_F32) return unpack<float>(a, (cudaStream_t)stream);
-    if (dtype == SCOUT_DT_BF16) return unpack<__nv_bfloat16>(a, (cudaStream_t)stream);
-    return unpack<__half>(a, (cudaStream_t)stream);
+    if (dtype == SCOUT_DT_F32) return unpack<float>(a, rows, (cudaStream_t)stream);
+    if (dtype == SCOUT_DT_BF16) return unpack<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
+    return unpack<__half>(a, rows, (cudaStream_t)stream);
 }

@@ -4,12 +4,19 @@
 // the checkpoint holds; only the fp32 sums round.  Tokens are the contraction, so both operands lie in memory with the
 // contraction as their slow axis and are transposed on their way into the matrix instructions.
 //
-// 128 x 128 outputs per block, 32 tokens per step, eight warps of 64 x 32.  Where the outputs give too few blocks for the
-// SMs, the tokens are split into parts that go to scratch in fp32 and are added in order.
+// Two kernels.  wgrad_tc: the checkpoint is restored to scratch in dy's type (one memory pass, small next to the product) and
+// both operands go by TMA to tcgen05.  wgrad_tiles: restores on the way into shared memory and uses the warp-level matrix
+// instructions; for few outputs, few tokens, and rows of dy that TMA cannot address.
+// Where the outputs give too few blocks for the SMs, the tokens are split into parts that go to scratch in fp32 and are
+// added in order.
+//
+// The tensor cores truncate when they add to an accumulator: a chain of 4096 tokens ends 2.2e-6 off (relative), where fp32
+// additions give 3e-7.  wgrad_tc therefore cuts its chains at CHAIN tokens and adds them in registers, rounding to nearest.
 #include <algorithm>
 
 #include "scout_attention.cuh"
 #include "scout_checkpoint.cuh"
+#include "scout_tc.cuh"
 
 namespace scout {
 namespace wgrad {
@@ -27,11 +34,13 @@ struct Args {
     const void *dy;
     const int8_t *codes, *exps;
     void *dw;
-    float *part;  // [splits][outs][ins] or null
-    int64_t dy_stride, code_stride, dw_stride, rows, outs, ins, blocks;
+    float *part;  // [splits][outs][part_stride] or null
+    int64_t dy_stride, code_stride, dw_stride, part_stride, rows, outs, ins, blocks;
     int64_t per;  // tokens of a part, a multiple of BK
-    int splits, tiles_i;
+    int splits, tiles_i, tiles;
     int out_f32, accumulate;
+    int wide;  // rows of dw start on 32-byte boundaries
+    uint32_t *gave_up;
 };
 
 __device__ __forceinline__ uint32_t at(int r, int c) { return r * ROW + ((c ^ (r & 7)) << 4); }
@@ -145,47 +154,250 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(con
             for (int e = 0; e < 4; ++e) {
                 const int64_t o = o0 + wm + m * 16 + (lane >> 2) + 8 * (e >> 1), i = i0 + wn + n * 8 + (lane & 3) * 2 + (e & 1);
                 if (o >= a.outs || i >= a.ins) continue;
-                if (a.splits > 1) a.part[((int64_t)split * a.outs + o) * a.ins + i] = acc[m][n][e];
+                if (a.splits > 1) a.part[((int64_t)split * a.outs + o) * a.part_stride + i] = acc[m][n][e];
                 else put<T>(a, o, i, acc[m][n][e]);
             }
 }
 
+// ---- tcgen05 -------------------------------------------------------------------------------------------
+// A persistent block takes 128 x 256 outputs (the widest product of one SM) after another.  Per 64 tokens: 128 of dy's and 256 of
+// the activation's features by TMA, 64 tokens x 64 features to a box, each landing as tcgen05 wants an operand whose
+// M or N axis is contiguous.  Warps 0-7 add up the chains, warp 8 loads, warp 9 issues.  Two accumulators of 256 columns each
+// fill tensor memory: one is read while the other is written.
+constexpr int TM = 128, TN = 256, TK = 64, STAGES = 4, CHAIN = 1024 / TK;  // in steps of TK tokens
+constexpr int TC_THREADS = 320, BOX = 64 * TK * 2, STAGE = (TM + TN) / 64 * BOX;
+constexpr int TC_SMEM = STAGES * STAGE + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
+
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
+    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                 "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+}
+__device__ __forceinline__ void load32(uint32_t (&w)[8], const void *p) {
+    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
+                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
+                 : "l"(p) : "memory");
+}
+
+template <typename T>
+__global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map_y,
+                                                          const __grid_constant__ CUtensorMap map_x) {
+    extern __shared__ uint8_t smem_raw[];
+    __shared__ uint64_t bars[2 * STAGES + 4];
+    __shared__ uint32_t tmem_slot, dead;
+    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, sum_full = empty + 8 * STAGES, sum_empty = sum_full + 16;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const tc::Patience patience{&dead, a.gave_up};
+    if (threadIdx.x == 0) {
+        dead = 0;
+        for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
+        for (int s = 0; s < 2; ++s) tc::bar_init(sum_full + 8 * s, 1), tc::bar_init(sum_empty + 8 * s, 8);
+        tc::bar_init_done();
+    }
+    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    pdl_wait();  // the restored activation
+
+    const int items = a.tiles * a.splits;
+    const auto steps_of = [&](int item) {  // first token and number of steps
+        const int64_t t0 = (int64_t)(item % a.splits) * a.per, t1 = min(t0 + a.per, a.rows);
+        return make_int2((int)t0, (int)((t1 - t0 + TK - 1) / TK));
+    };
+    if (warp == 8) {
+        if (lane == 0) {
+            tc::prefetch_map(&map_y);
+            tc::prefetch_map(&map_x);
+            uint32_t n = 0;
+            for (int item = blockIdx.x; item < items; item += gridDim.x) {
+                const int tile = item / a.splits, o0 = tile / a.tiles_i * TM, i0 = tile % a.tiles_i * TN;
+                const int2 st = steps_of(item);
+                for (int k = 0; k < st.y; ++k, ++n) {
+                    const uint32_t s = n % STAGES, to = base + s * STAGE;
+                    if (!patience.wait(empty + 8 * s, ((n / STAGES) & 1) ^ 1)) goto done;
+                    tc::bar_expect(full + 8 * s, STAGE);
+#pragma unroll
+                    for (int c = 0; c < TM / 64; ++c) tc::tma_2d(to + c * BOX, &map_y, full + 8 * s, o0 + c * 64, st.x + k * TK);
+#pragma unroll
+                    for (int c = 0; c < TN / 64; ++c) tc::tma_2d(to + (TM / 64 + c) * BOX, &map_x, full + 8 * s, i0 + c * 64, st.x + k * TK);
+                }
+            }
+        }
+    } else if (warp == 9) {
+        if (lane == 0) {
+            constexpr uint32_t idesc = tc::instr(Half<T>::is_bf16, TM, TN, true, true);
+            uint32_t n = 0, chain = 0;
+            for (int item = blockIdx.x; item < items; item += gridDim.x) {
+                const int2 st = steps_of(item);
+                for (int k = 0; k < st.y; ++chain) {
+                    const uint32_t buf = chain & 1;
+                    if (!patience.wait(sum_empty + 8 * buf, ((chain >> 1) & 1) ^ 1)) goto done;
+                    tc::tc_fence_after();
+                    for (int c = 0; c < CHAIN && k < st.y; ++c, ++k, ++n) {
+                        const uint32_t s = n % STAGES, from = base + s * STAGE;
+                        if (!patience.wait(full + 8 * s, (n / STAGES) & 1)) goto done;
+                        tc::tc_fence_after();
+#pragma unroll
+                        for (int kk = 0; kk < TK / 16; ++kk)
+                            tc::mma(tmem + buf * TN, tc::smem_desc(from + kk * 2048, BOX, 1024),
+                                    tc::smem_desc(from + TM / 64 * BOX + kk * 2048, BOX, 1024), idesc, c > 0 || kk > 0);
+                        tc::mma_commit(empty + 8 * s);
+                    }
+                    tc::mma_commit(sum_full + 8 * buf);
+                }
+            }
+        }
+    } else {
+        uint32_t chain = 0;
+        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 128;
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const int tile = item / a.splits, split = item % a.splits;
+            const int2 st = steps_of(item);
+            float sum[128];
+#pragma unroll
+            for (int c = 0; c < 128; ++c) sum[c] = 0.f;
+            for (int k = 0; k < st.y; k += CHAIN, ++chain) {
+                const uint32_t buf = chain & 1;
+                if (!patience.wait(sum_full + 8 * buf, (chain >> 1) & 1)) goto done;
+                tc::tc_fence_after();
+#pragma unroll
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t r[32];
+                    tc::tmem_load32(r, mine + buf * TN + c * 32);
+                    tc::tmem_load_wait(r);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) sum[c * 32 + e] += __uint_as_float(r[e]);
+                }
+                tc::tc_fence_before();
+                __syncwarp();
+                if (lane == 0) tc::bar_arrive(sum_empty + 8 * buf);
+            }
+            const int64_t o = (int64_t)(tile / a.tiles_i) * TM + row, i0 = (int64_t)(tile % a.tiles_i) * TN + half * 128;
+            if (o >= a.outs) continue;
+            if (a.splits > 1) {
+                float *dst = a.part + ((int64_t)split * a.outs + o) * a.part_stride + i0;
+#pragma unroll
+                for (int c = 0; c < 128; c += 8) {
+                    uint32_t w[8];
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(sum[c + e]);
+                    if (i0 + c < a.ins) store32(dst + c, w);  // rows of parts are padded to eight columns
+                }
+                continue;
+            }
+#pragma unroll
+            for (int c = 0; c < 128; c += 16) {
+                const int64_t i = i0 + c;
+                if (a.wide && i + 16 <= a.ins) {
+                    uint32_t w[8];
+                    if (a.out_f32) {
+                        float *dst = reinterpret_cast<float *>(a.dw) + o * a.dw_stride + i;
+#pragma unroll
+                        for (int h = 0; h < 16; h += 8) {
+                            if (a.accumulate) load32(w, dst + h);
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(a.accumulate ? __uint_as_float(w[e]) + sum[c + h + e] : sum[c + h + e]);
+                            store32(dst + h, w);
+                        }
+                    } else {
+                        T *dst = reinterpret_cast<T *>(a.dw) + o * a.dw_stride + i;
+                        if (a.accumulate) load32(w, dst);
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) {
+                            const float2 was = a.accumulate ? Half<T>::unpack(w[e]) : make_float2(0.f, 0.f);
+                            w[e] = Half<T>::pack(was.x + sum[c + 2 * e], was.y + sum[c + 2 * e + 1]);
+                        }
+                        store32(dst, w);
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 16; ++e)
+                        if (i + e < a.ins) put<T>(a, o, i + e, sum[c + e]);
+                }
+            }
+        }
+    }
+done:
+    __syncwarp();
+    if (dead) tc::let_flights_end();
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    if (warp == 9) tc::tmem_free(tmem, 512);
+}
+
 template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_join(const __grid_constant__ Args a) {
     pdl_wait();
-    const int64_t n = a.outs * a.ins;
+    const int64_t n = a.outs * a.part_stride;
     for (int64_t x = (int64_t)blockIdx.x * THREADS + threadIdx.x; x < n; x += (int64_t)gridDim.x * THREADS) {
+        const int64_t o = x / a.part_stride, i = x % a.part_stride;
+        if (i >= a.ins) continue;
         float v = 0.f;
         for (int s = 0; s < a.splits; ++s) v += a.part[s * n + x];
-        put<T>(a, x / a.ins, x % a.ins, v);
+        put<T>(a, o, i, v);
     }
 }
 
-// dW = 0, or left alone, when there is no token
+// How a product is cut; the scratch holds the parts, then the restored activation.
 struct Tiling {
+    bool tensor;  // wgrad_tc
     uint64_t tiles_o, tiles_i;
-    int64_t per;
+    int64_t per, part_stride, x_stride;
     int splits;
-    uint64_t bytes;
+    uint64_t part_bytes, bytes;
 };
-Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins) {
+Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
     Tiling t = {};
-    t.tiles_o = (outs + BM - 1) / BM, t.tiles_i = (ins + BN - 1) / BN;
-    const uint64_t tiles = t.tiles_o * t.tiles_i, steps = (rows + BK - 1) / BK;
-    uint64_t want = tiles >= 148 ? 1 : std::min<uint64_t>((2 * 148 + tiles - 1) / tiles, steps / 4);
+    t.tensor = tensor;
+    const uint64_t bm = tensor ? TM : BM, bn = tensor ? TN : BN, bk = tensor ? TK : BK, least = tensor ? 8 : 4;
+    t.tiles_o = (outs + bm - 1) / bm, t.tiles_i = (ins + bn - 1) / bn;
+    const uint64_t tiles = t.tiles_o * t.tiles_i, steps = (rows + bk - 1) / bk;
+    uint64_t want = tiles >= 148 ? 1 : std::min<uint64_t>((tensor ? 148 : 2 * 148 + tiles - 1) / tiles, steps / least);
     want = std::max<uint64_t>(1, std::min<uint64_t>(want, 64));
     const uint64_t per = (steps + want - 1) / want;
-    t.per = (int64_t)std::max<uint64_t>(per, 1) * BK;
+    t.per = (int64_t)(std::max<uint64_t>(per, 1) * bk);
     t.splits = (int)std::max<uint64_t>(1, (rows + t.per - 1) / t.per);
-    t.bytes = t.splits > 1 ? (t.splits * outs * ins * 4 + 255) & ~255ull : 0;
+    t.part_stride = (int64_t)((ins + 7) & ~7ull);
+    t.part_bytes = t.splits > 1 ? (t.splits * outs * t.part_stride * 4 + 255) & ~255ull : 0;
+    t.x_stride = t.part_stride;
+    t.bytes = t.part_bytes + (tensor ? (rows * t.x_stride * 2 + 255) & ~255ull : 0);
     return t;
 }
+// The restored copy costs a pass over memory and a launch: worth it from these sizes on.
+bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) { return rows >= TK && outs >= TM && ins >= 64; }
 
-template <typename T> int run(Args &a, const Tiling &t, cudaStream_t stream) {
-    wgrad_tiles<T><<<(unsigned)(t.tiles_o * t.tiles_i * t.splits), THREADS, 0, stream>>>(a);
-    SCOUT_CUDA(cudaGetLastError());
-    if (t.splits > 1)
-        SCOUT_CUDA(launch_dependent(wgrad_join<T>, dim3((unsigned)std::min<int64_t>((a.outs * a.ins + THREADS - 1) / THREADS, 148 * 8)),
-                                    dim3(THREADS), stream, a));
+template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStream_t stream) {
+    const int64_t join_grid = std::min<int64_t>((a.outs * a.part_stride + THREADS - 1) / THREADS, 148 * 8);
+    if (t.tensor) {
+        constexpr bool bf16 = Half<T>::is_bf16;
+        CUtensorMap my, mx;
+        const uint64_t dy_dims[2] = {(uint64_t)a.outs, (uint64_t)a.rows}, x_dims[2] = {(uint64_t)a.ins, (uint64_t)a.rows};
+        const uint64_t dy_strides[1] = {(uint64_t)a.dy_stride * 2}, x_strides[1] = {(uint64_t)t.x_stride * 2};
+        if (int rc = tc::tensor_map(&my, bf16, a.dy, 2, dy_dims, dy_strides, TK)) return rc;
+        if (int rc = tc::tensor_map(&mx, bf16, restored, 2, x_dims, x_strides, TK)) return rc;
+        if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
+        SCOUT_CUDA(cudaFuncSetAttribute(wgrad_tc<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
+        if (int rc = scout_ckpt_unpack(bf16 ? SCOUT_DT_BF16 : SCOUT_DT_F16, a.rows, a.ins, a.codes, a.code_stride, a.exps, restored, t.x_stride, stream))
+            return rc;
+        cudaLaunchConfig_t cfg = {};
+        cfg.gridDim = dim3((unsigned)std::min(a.tiles * a.splits, 148));
+        cfg.blockDim = dim3(TC_THREADS);
+        cfg.dynamicSmemBytes = TC_SMEM;
+        cfg.stream = stream;
+        cudaLaunchAttribute attr[1];
+        attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[0].val.programmaticStreamSerializationAllowed = 1;
+        cfg.attrs = attr;
+        cfg.numAttrs = 1;
+        SCOUT_CUDA(cudaLaunchKernelEx(&cfg, wgrad_tc<T>, a, my, mx));
+    } else {
+        wgrad_tiles<T><<<(unsigned)(a.tiles * a.splits), THREADS, 0, stream>>>(a);
+        SCOUT_CUDA(cudaGetLastError());
+    }
+    if (t.splits > 1) SCOUT_CUDA(launch_dependent(wgrad_join<T>, dim3((unsigned)join_grid), dim3(THREADS), stream, a));
     return SCOUT_OK;
 }
 
@@ -204,7 +416,8 @@ extern "C" int scout_ckpt_wgrad_workspace(uint32_t dtype, uint64_t rows, uint64_
     using namespace scout::wgrad;
     if (int rc = check(dtype, rows, outs, ins)) return rc;
     if (!bytes) return SCOUT_ERR_INVALID;
-    *bytes = tiling(rows, outs, ins).bytes;
+    *bytes = tiling(rows, outs, ins, false).bytes;
+    if (worth_tensor(rows, outs, ins)) *bytes = std::max(*bytes, tiling(rows, outs, ins, true).bytes);
     return SCOUT_OK;
 }
 
@@ -221,14 +434,20 @@ extern "C" int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t row
     if (reinterpret_cast<uintptr_t>(dw) & (out_dtype == SCOUT_DT_F32 ? 3 : 1) || reinterpret_cast<uintptr_t>(dy) & 1 ||
         reinterpret_cast<uintptr_t>(workspace) & 255)
         return SCOUT_ERR_ALIGN;
-    const Tiling t = tiling(rows, outs, ins);
-    if (workspace_bytes < t.bytes || (t.bytes && !workspace)) return SCOUT_ERR_INVALID;
+    uint64_t bytes = 0;
+    if (int rc = scout_ckpt_wgrad_workspace(dtype, rows, outs, ins, &bytes)) return rc;
+    if (workspace_bytes < bytes || (bytes && !workspace)) return SCOUT_ERR_INVALID;
+    const bool tma = dy_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(dy) & 15) == 0;
+    const Tiling t = tiling(rows, outs, ins, tma && worth_tensor(rows, outs, ins));
     if (t.tiles_o * t.tiles_i * t.splits > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
     Args a = {};
     a.dy = dy, a.codes = codes, a.exps = exps, a.dw = dw, a.part = (float *)workspace;
     a.dy_stride = (int64_t)dy_stride, a.code_stride = (int64_t)code_stride, a.dw_stride = (int64_t)dw_stride;
     a.rows = (int64_t)rows, a.outs = (int64_t)outs, a.ins = (int64_t)ins, a.blocks = (int64_t)((ins + SCOUT_CKPT_BLOCK - 1) / SCOUT_CKPT_BLOCK);
-    a.per = t.per, a.splits = t.splits, a.tiles_i = (int)t.tiles_i;
+    a.per = t.per, a.part_stride = t.part_stride, a.splits = t.splits, a.tiles_i = (int)t.tiles_i, a.tiles = (int)(t.tiles_o * t.tiles_i);
+    const uint64_t size = out_dtype == SCOUT_DT_F32 ? 4 : 2;
+    a.wide = dw_stride * size % 32 == 0 && (reinterpret_cast<uintptr_t>(dw) & 31) == 0;
+    void *restored = (uint8_t *)workspace + t.part_bytes;
     a.out_f32 = out_dtype == SCOUT_DT_F32, a.accumulate = (int)accumulate;
-    return dtype == SCOUT_DT_BF16 ? run<__nv_bfloat16>(a, t, (cudaStream_t)stream) : run<__half>(a, t, (cudaStream_t)stream);
+    return dtype == SCOUT_DT_BF16 ? run<__nv_bfloat16>(a, t, restored, (cudaStream_t)stream) : run<__half>(a, t, restored, (cudaStream_t)stream);
 }

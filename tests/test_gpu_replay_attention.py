@@ -11,6 +11,13 @@ pytestmark = pytest.mark.gpu
 BF, HF = torch.bfloat16, torch.float16
 
 
+@pytest.fixture(autouse=True)
+def no_wait_gives_up():
+    yield
+    from paper_2608_11034_b200 import binding
+    assert binding.scout_replay_error() == 0
+
+
 def make(seed, dtype, B, Tq, Tk, Hq, Hk, D, scale_do=1.0):
     g = torch.Generator(device="cuda").manual_seed(seed)
     n = lambda *s: torch.randn(*s, generator=g, device="cuda").to(dtype)          # noqa: E731
