@@ -705,11 +705,6 @@ Shape shape(const scout_attn_t &a) {
     return s;
 }
 
-template <typename K> int big_smem(K kernel, int bytes) {
-    SCOUT_CUDA(cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
-    return SCOUT_OK;
-}
-
 template <typename Args>
 cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t stream, const Args &args, bool dependent) {
     cudaLaunchConfig_t cfg = {};
@@ -727,7 +722,7 @@ cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t s
 
 template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaStream_t stream) {
     constexpr int smem = 5 * TILE * HD * 2;
-    if (int rc = big_smem(forward_tiles<T, HD>, smem)) return rc;
+    if (int rc = allow_smem<forward_tiles<T, HD>>(smem)) return rc;
     f.tiles = (int)s.q_tiles;
     f.splits = s.f_splits;
     SCOUT_CUDA(launch(forward_tiles<T, HD>, s.q_tiles * f.p.batch * f.p.kv_heads * f.splits, smem, stream, f, false));
@@ -737,8 +732,8 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
 
 template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cudaStream_t stream) {
     constexpr int smem_q = 6 * TILE * HD * 2, smem_k = 2 * TILE * HD * 2 + 4 * 32 * HD * 2;
-    if (int rc = big_smem(backward_dq<T, HD>, smem_q)) return rc;
-    if (int rc = big_smem(backward_dkv<T, HD>, smem_k)) return rc;
+    if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
+    if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
     const uint64_t bh = (uint64_t)a.p.batch * a.p.kv_heads;
     if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + 3) / 4, 0, stream, a, false));
     // every kernel that follows waits for the whole of the one before it (griddepcontrol.wait), so the
@@ -792,6 +787,11 @@ extern "C" int scout_attn_forward(const scout_attn_t *a, const void *q, const vo
     f.part_o = (float *)workspace;
     f.part_ml = (float2 *)((uint8_t *)workspace + up256(s.f_splits * s.rows * a->head_dim * 4));
     const bool wide = a->head_dim > 64;
+    if (s.keys && s.f_splits == 1 && a->q_len >= 96) {
+        bool taken = false;
+        const int rc = forward_tensor(f.p, a->dtype == SCOUT_DT_BF16, o, lse, (cudaStream_t)stream, &taken);
+        if (rc || taken) return rc;
+    }
     if (a->dtype == SCOUT_DT_BF16)
         return wide ? forward<__nv_bfloat16, 128>(s, f, (cudaStream_t)stream) : forward<__nv_bfloat16, 64>(s, f, (cudaStream_t)stream);
     return wide ? forward<__half, 128>(s, f, (cudaStream_t)stream) : forward<__half, 64>(s, f, (cudaStream_t)stream);

@@ -248,5 +248,8 @@ __device__ __noinline__ void row_dkv(const Problem &p, const float2 *stats, int 
     RowIO<T>::store(RowIO<T>::at(dv, p.sv, b, j, hk), av, d, lane);
 }
 
+// The tcgen05 forward pass (scout_attention_tc.cu); *taken is false where TMA cannot address a tensor and nothing was enqueued.
+int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken);
+
 }  // namespace attn
 }  // namespace scout

@@ -4,6 +4,7 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
 #include <vector>
 
 #include "scout.h"
@@ -140,6 +141,18 @@ void set_cuda_error(cudaError_t e, const char *what);
             return SCOUT_ERR_CUDA;                        \
         }                                                 \
     } while (0)
+
+// Allows a kernel `bytes` of dynamic shared memory, once per kernel and device.
+template <auto KERNEL> inline int allow_smem(int bytes) {
+    static std::atomic<uint64_t> done{0};
+    int dev = 0;
+    SCOUT_CUDA(cudaGetDevice(&dev));
+    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
+    if (done.load(std::memory_order_relaxed) & bit) return SCOUT_OK;
+    SCOUT_CUDA(cudaFuncSetAttribute(KERNEL, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes));
+    done.fetch_or(bit, std::memory_order_relaxed);
+    return SCOUT_OK;
+}
 
 // ---- programmatic dependent launch ------------------------------------------------
 // The small kernels that follow the scan (finalise, vote, certificate) are launched

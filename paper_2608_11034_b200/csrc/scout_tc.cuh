@@ -59,6 +59,8 @@ struct Patience {
             if (bar_try(bar, parity)) return true;
         return wait_long(bar, parity);
     }
+    // the same for a whole warp whose next steps need all of its lanes
+    __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
     __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity) const {
         const uint64_t until = now_ns() + WAIT_LIMIT_NS;
         while (!bar_try(bar, parity)) {

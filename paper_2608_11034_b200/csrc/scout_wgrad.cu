@@ -166,7 +166,8 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(con
 // fill tensor memory: one is read while the other is written.
 constexpr int TM = 128, TN = 256, TK = 64, STAGES = 4, CHAIN = 1024 / TK;  // in steps of TK tokens
 constexpr int TC_THREADS = 320, BOX = 64 * TK * 2, STAGE = (TM + TN) / 64 * BOX;
-constexpr int TC_SMEM = STAGES * STAGE + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
+constexpr int TURN = 32 * 33 * 4;  // a warp's 32 x 32 results on their way to rows of dw that start anywhere
+constexpr int TC_SMEM = STAGES * STAGE + 8 * TURN + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
 
 __device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
     asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
@@ -261,7 +262,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
             for (int c = 0; c < 128; ++c) sum[c] = 0.f;
             for (int k = 0; k < st.y; k += CHAIN, ++chain) {
                 const uint32_t buf = chain & 1;
-                if (!patience.wait(sum_full + 8 * buf, (chain >> 1) & 1)) goto done;
+                if (!patience.wait_warp(sum_full + 8 * buf, (chain >> 1) & 1)) goto done;
                 tc::tc_fence_after();
 #pragma unroll
                 for (int c = 0; c < 4; ++c) {
@@ -276,7 +277,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                 if (lane == 0) tc::bar_arrive(sum_empty + 8 * buf);
             }
             const int64_t o = (int64_t)(tile / a.tiles_i) * TM + row, i0 = (int64_t)(tile % a.tiles_i) * TN + half * 128;
-            if (o >= a.outs) continue;
             if (a.splits > 1) {
                 float *dst = a.part + ((int64_t)split * a.outs + o) * a.part_stride + i0;
 #pragma unroll
@@ -284,17 +284,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                     uint32_t w[8];
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(sum[c + e]);
-                    if (i0 + c < a.ins) store32(dst + c, w);  // rows of parts are padded to eight columns
+                    if (o < a.outs && i0 + c < a.ins) store32(dst + c, w);  // rows of parts are padded to eight columns
                 }
-                continue;
-            }
+            } else if (a.wide && i0 + 128 <= a.ins) {
+                // a thread's row in 32-byte pieces
 #pragma unroll
-            for (int c = 0; c < 128; c += 16) {
-                const int64_t i = i0 + c;
-                if (a.wide && i + 16 <= a.ins) {
+                for (int c = 0; c < 128; c += 16) {
                     uint32_t w[8];
+                    if (o >= a.outs) break;
                     if (a.out_f32) {
-                        float *dst = reinterpret_cast<float *>(a.dw) + o * a.dw_stride + i;
+                        float *dst = reinterpret_cast<float *>(a.dw) + o * a.dw_stride + i0 + c;
 #pragma unroll
                         for (int h = 0; h < 16; h += 8) {
                             if (a.accumulate) load32(w, dst + h);
@@ -303,7 +302,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                             store32(dst + h, w);
                         }
                     } else {
-                        T *dst = reinterpret_cast<T *>(a.dw) + o * a.dw_stride + i;
+                        T *dst = reinterpret_cast<T *>(a.dw) + o * a.dw_stride + i0 + c;
                         if (a.accumulate) load32(w, dst);
 #pragma unroll
                         for (int e = 0; e < 8; ++e) {
@@ -312,10 +311,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                         }
                         store32(dst, w);
                     }
-                } else {
+                }
+            } else {
+                // rows of dw on any boundary, and ragged ends: 32 x 32 results are turned in shared memory, a lane per column
+                float *turn = reinterpret_cast<float *>(smem_raw + (base - smem_u32(smem_raw)) + STAGES * STAGE + warp * TURN);
+                const int64_t row0 = o - lane;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e)
-                        if (i + e < a.ins) put<T>(a, o, i + e, sum[c + e]);
+                for (int c = 0; c < 4; ++c) {
+                    __syncwarp();
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) turn[lane * 33 + e] = sum[c * 32 + e];
+                    __syncwarp();
+                    const int64_t i = i0 + c * 32 + lane;
+                    if (i < a.ins)
+                        for (int r = 0; r < 32 && row0 + r < a.outs; ++r) put<T>(a, row0 + r, i, turn[r * 33 + lane]);
                 }
             }
         }
@@ -379,7 +388,7 @@ template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStre
         if (int rc = tc::tensor_map(&my, bf16, a.dy, 2, dy_dims, dy_strides, TK)) return rc;
         if (int rc = tc::tensor_map(&mx, bf16, restored, 2, x_dims, x_strides, TK)) return rc;
         if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-        SCOUT_CUDA(cudaFuncSetAttribute(wgrad_tc<T>, cudaFuncAttributeMaxDynamicSharedMemorySize, TC_SMEM));
+        if (int rc = allow_smem<wgrad_tc<T>>(TC_SMEM)) return rc;
         if (int rc = scout_ckpt_unpack(bf16 ? SCOUT_DT_BF16 : SCOUT_DT_F16, a.rows, a.ins, a.codes, a.code_stride, a.exps, restored, t.x_stride, stream))
             return rc;
         cudaLaunchConfig_t cfg = {};

@@ -83,8 +83,22 @@ def _scratch(nbytes, device):
     return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
 
 
-def _stream(x) -> int:
-    return torch.cuda.current_stream(x.device).cuda_stream
+class _On:
+    """The tensors' device made current, and its current stream's handle; costs nothing when it is current already."""
+
+    def __init__(self, x):
+        self.index = x.device.index
+
+    def __enter__(self) -> int:
+        now = torch.cuda.current_device()
+        self.back = None if now == self.index else now
+        if self.back is not None:
+            torch.cuda.set_device(self.index)
+        return torch._C._cuda_getCurrentRawStream(self.index)
+
+    def __exit__(self, *_):
+        if self.back is not None:
+            torch.cuda.set_device(self.back)
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, window: int = 0,
@@ -103,9 +117,9 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
     ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
     ws = _scratch(nbytes, q.device)
-    with torch.cuda.device(q.device):
+    with _On(q) as stream:
         binding.scout_attn_forward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
-                                   ws.data_ptr() if ws is not None else 0, nbytes, _stream(q))
+                                   ws.data_ptr() if ws is not None else 0, nbytes, stream)
     return o, lse
 
 
@@ -125,10 +139,10 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
         _fail("lse: the forward pass's, a contiguous float32 tensor [batch, q_heads, q_len]")
     ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
     ws = _scratch(nbytes, q.device)
-    with torch.cuda.device(q.device):
+    with _On(q) as stream:
         binding.scout_attn_backward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
                                     ql, kl, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                    ws.data_ptr() if ws is not None else 0, nbytes, _stream(q))
+                                    ws.data_ptr() if ws is not None else 0, nbytes, stream)
     return dq, dk, dv
 
 
@@ -158,9 +172,9 @@ def checkpoint_pack(x: torch.Tensor):
     rows, cols = x.shape
     codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
     exps = torch.empty((rows, -(-cols // binding.CKPT_BLOCK)), dtype=torch.int8, device=x.device)
-    with torch.cuda.device(x.device):
+    with _On(x) as stream:
         binding.scout_ckpt_pack(_CODE[x.dtype], rows, cols, x.data_ptr(), stride, codes.data_ptr(), max(cols, 1),
-                                exps.data_ptr(), _stream(x))
+                                exps.data_ptr(), stream)
     return codes, exps
 
 
@@ -170,9 +184,9 @@ def checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, dtype: torch.dtyp
     if dtype not in _CODE:
         _fail("activations are float32, bfloat16 or float16")
     x = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-    with torch.cuda.device(codes.device):
+    with _On(codes) as stream:
         binding.scout_ckpt_unpack(_CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(), x.data_ptr(),
-                                  max(cols, 1), _stream(codes))
+                                  max(cols, 1), stream)
     return x
 
 
@@ -196,8 +210,8 @@ def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, 
         _fail("the gradient is [outs, ins], float32 or of dy's dtype, on dy's device")
     nbytes = _wgrad_scratch(_CODE[dy.dtype], rows, outs, ins)
     ws = _scratch(nbytes, dy.device)
-    with torch.cuda.device(dy.device):
+    with _On(dy) as stream:
         binding.scout_ckpt_wgrad(_CODE[dy.dtype], _CODE[dw.dtype], rows, outs, ins, dy.data_ptr(), dy_stride, codes.data_ptr(),
                                  code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
-                                 ws.data_ptr() if ws is not None else 0, nbytes, _stream(dy))
+                                 ws.data_ptr() if ws is not None else 0, nbytes, stream)
     return dw
