@@ -10,7 +10,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libscout_b200.so")
 SOURCES = ["scout_api.cu", "scout_sign.cu", "scout_one_launch.cu", "scout_noalloc.cu", "scout_vote.cu", "scout_timing.cu",
-           "scout_attention.cu", "scout_attention_tc.cu", "scout_checkpoint.cu", "scout_wgrad.cu", "scout_tc.cu", "scout_ledger.cpp"]
+           "scout_attention.cu", "scout_attention_tc.cu", "scout_attention_bwd_tc.cu", "scout_checkpoint.cu", "scout_wgrad.cu", "scout_tc.cu", "scout_ledger.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-Xcompiler", "-fvisibility=hidden", "-Xlinker", "--exclude-libs,ALL"]
 

@@ -673,9 +673,8 @@ Problem problem(const scout_attn_t &a) {
     return p;
 }
 
-// Parts along the long axis: as many as it takes to give every SM two blocks, each part at least `least` blocks long.
-int parts(uint64_t blocks, uint64_t along, uint64_t least) {
-    const uint64_t want = 2 * 148;
+// Parts along the long axis: as many as it takes to have `want` blocks, each part at least `least` blocks long.
+int parts(uint64_t blocks, uint64_t along, uint64_t want, uint64_t least) {
     if (blocks >= want || along < 2 * least) return 1;
     return (int)std::min<uint64_t>({(want + blocks - 1) / blocks, along / least, 64});
 }
@@ -685,18 +684,24 @@ struct Shape {
     int f_splits, q_splits, k_splits;
     uint64_t forward_bytes, stats_bytes, backward_bytes;
 };
-Shape shape(const scout_attn_t &a) {
+// tensor: the backward pass runs on tcgen05 (tiles of 128, one block an SM)
+Shape shape(const scout_attn_t &a, bool tensor) {
     Shape s = {};
     const uint64_t group = a.q_heads / a.kv_heads, bh = (uint64_t)a.batch * a.kv_heads;
     s.rows = (uint64_t)a.batch * a.q_heads * a.q_len;
     s.keys = bh * a.kv_len;
     s.q_tiles = (group * a.q_len + TILE - 1) / TILE;
     s.k_tiles = (a.kv_len + TILE - 1) / TILE;
-    const uint64_t seen = a.window ? std::min<uint64_t>(a.kv_len, a.window + TILE) : a.kv_len;
-    s.f_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 4);
-    s.q_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 4);
-    const uint64_t seen_by = group * (a.window ? std::min<uint64_t>(a.q_len, a.window + TILE) : a.q_len);
-    s.k_splits = parts(s.k_tiles * bh, (seen_by + 31) / 32, 8);
+    const uint64_t seen = a.window ? std::min<uint64_t>(a.kv_len, (uint64_t)a.window + TILE) : a.kv_len;
+    s.f_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
+    const uint64_t seen_by = a.window ? std::min<uint64_t>(a.q_len, (uint64_t)a.window + TILE) : a.q_len;
+    if (tensor) {
+        s.q_splits = parts((a.q_len + 127) / 128 * bh * group, (seen + 127) / 128, 148, 3);
+        s.k_splits = parts((a.kv_len + 127) / 128 * bh, group * ((seen_by + 127) / 128), 148, 3);
+    } else {
+        s.q_splits = s.f_splits;
+        s.k_splits = parts(s.k_tiles * bh, (group * seen_by + 31) / 32, 2 * 148, 8);
+    }
     s.forward_bytes = s.f_splits > 1 ? up256(s.f_splits * s.rows * a.head_dim * 4) + up256(s.f_splits * s.rows * 8) : 0;
     s.stats_bytes = up256(s.rows * 8);
     const uint64_t pq = s.q_splits > 1 ? s.q_splits * s.rows * a.head_dim * 4 : 0;
@@ -704,6 +709,7 @@ Shape shape(const scout_attn_t &a) {
     s.backward_bytes = s.stats_bytes + up256(std::max(pq, pk));  // the two kernels follow one another
     return s;
 }
+bool worth_tensor(const scout_attn_t &a) { return a.q_len >= 96 && a.kv_len >= 96; }
 
 template <typename Args>
 cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t stream, const Args &args, bool dependent) {
@@ -730,7 +736,7 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
     return SCOUT_OK;
 }
 
-template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cudaStream_t stream) {
+template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, const CUtensorMap (*maps)[4], cudaStream_t stream) {
     constexpr int smem_q = 6 * TILE * HD * 2, smem_k = 2 * TILE * HD * 2 + 4 * 32 * HD * 2;
     if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
     if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
@@ -740,12 +746,20 @@ template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cuda
     // statistics are there for all of them and the shared parts are free
     if (s.rows) {
         a.tiles = (int)s.q_tiles, a.splits = s.q_splits;
-        SCOUT_CUDA(launch(backward_dq<T, HD>, s.q_tiles * bh * a.splits, smem_q, stream, a, true));
+        if (maps) {
+            if (int rc = dq_tensor(a.p, Half<T>::is_bf16, a.stats, a.dq, a.part, a.splits, *maps, stream)) return rc;
+        } else {
+            SCOUT_CUDA(launch(backward_dq<T, HD>, s.q_tiles * bh * a.splits, smem_q, stream, a, true));
+        }
         if (a.splits > 1) SCOUT_CUDA(launch(join_dq<T>, (s.rows + 3) / 4, 0, stream, a, true));
     }
     if (s.keys) {
         a.tiles = (int)s.k_tiles, a.splits = s.k_splits;
-        SCOUT_CUDA(launch(backward_dkv<T, HD>, s.k_tiles * bh * a.splits, smem_k, stream, a, s.rows > 0));
+        if (maps) {
+            if (int rc = dkv_tensor(a.p, Half<T>::is_bf16, a.stats, a.dk, a.dv, a.part, a.splits, *maps, stream)) return rc;
+        } else {
+            SCOUT_CUDA(launch(backward_dkv<T, HD>, s.k_tiles * bh * a.splits, smem_k, stream, a, s.rows > 0));
+        }
         if (a.splits > 1) SCOUT_CUDA(launch(join_dkv<T>, (s.keys + 3) / 4, 0, stream, a, true));
     }
     return SCOUT_OK;
@@ -761,9 +775,10 @@ extern "C" int scout_attn_workspace(const scout_attn_t *a, uint64_t *forward_byt
     using namespace scout::attn;
     if (int rc = check(a)) return rc;
     if (!forward_bytes || !backward_bytes) return SCOUT_ERR_INVALID;
-    const Shape s = shape(*a);
+    const Shape s = shape(*a, false);
     *forward_bytes = s.forward_bytes;
-    *backward_bytes = s.backward_bytes;
+    // enough for either kernel, so that the size does not depend on the pointers
+    *backward_bytes = std::max(s.backward_bytes, worth_tensor(*a) ? shape(*a, true).backward_bytes : 0);
     return SCOUT_OK;
 }
 
@@ -773,7 +788,7 @@ extern "C" int scout_attn_forward(const scout_attn_t *a, const void *q, const vo
     using namespace scout;
     using namespace scout::attn;
     if (int rc = check(a)) return rc;
-    const Shape s = shape(*a);
+    const Shape s = shape(*a, false);
     if (s.rows == 0) return SCOUT_OK;
     if (!q || !o || !lse || (s.keys && (!k || !v))) return SCOUT_ERR_INVALID;
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(lse, 4) || !aligned(q_lens, 4) ||
@@ -803,22 +818,27 @@ extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const v
     using namespace scout;
     using namespace scout::attn;
     if (int rc = check(a)) return rc;
-    const Shape s = shape(*a);
+    Shape s = shape(*a, false);
     if (s.rows == 0 && s.keys == 0) return SCOUT_OK;
     if ((s.rows && (!q || !o || !lse || !d_o || !dq)) || (s.keys && (!k || !v || !dk || !dv))) return SCOUT_ERR_INVALID;
     const void *all[9] = {q, k, v, o, d_o, dq, dk, dv, nullptr};
     for (const void *x : all)
         if (!aligned(x, 16)) return SCOUT_ERR_ALIGN;
     if (!aligned(lse, 4) || !aligned(q_lens, 4) || !aligned(kv_lens, 4) || !aligned(workspace, 256)) return SCOUT_ERR_ALIGN;
-    if (workspace_bytes < s.backward_bytes || (s.backward_bytes && !workspace)) return SCOUT_ERR_INVALID;
+    uint64_t forward_bytes = 0, backward_bytes = 0;
+    if (int rc = scout_attn_workspace(a, &forward_bytes, &backward_bytes)) return rc;
+    if (workspace_bytes < backward_bytes || (backward_bytes && !workspace)) return SCOUT_ERR_INVALID;
     BackwardArgs b = {};
     b.p = problem(*a);
     b.p.q = q, b.p.k = k, b.p.v = v, b.p.o = o, b.p.d_o = d_o, b.p.q_lens = q_lens, b.p.kv_lens = kv_lens;
     b.lse = lse, b.dq = dq, b.dk = dk, b.dv = dv;
     b.stats = (float2 *)workspace;
     b.part = (float *)((uint8_t *)workspace + s.stats_bytes);
-    const bool wide = a->head_dim > 64;
-    if (a->dtype == SCOUT_DT_BF16)
-        return wide ? backward<__nv_bfloat16, 128>(s, b, (cudaStream_t)stream) : backward<__nv_bfloat16, 64>(s, b, (cudaStream_t)stream);
-    return wide ? backward<__half, 128>(s, b, (cudaStream_t)stream) : backward<__half, 64>(s, b, (cudaStream_t)stream);
+    const bool wide = a->head_dim > 64, bf16 = a->dtype == SCOUT_DT_BF16;
+    CUtensorMap views[4];
+    const CUtensorMap(*maps)[4] = worth_tensor(*a) && backward_views(b.p, bf16, views) ? &views : nullptr;
+    if (maps) s = shape(*a, true);
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (bf16) return wide ? backward<__nv_bfloat16, 128>(s, b, maps, st) : backward<__nv_bfloat16, 64>(s, b, maps, st);
+    return wide ? backward<__half, 128>(s, b, maps, st) : backward<__half, 64>(s, b, maps, st);
 }

@@ -2,6 +2,7 @@
 // types, warp-level matrix instructions, and the row-by-row evaluation of the definition.
 #pragma once
 
+#include <cuda.h>  // CUtensorMap
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <math_constants.h>
@@ -248,8 +249,16 @@ __device__ __noinline__ void row_dkv(const Problem &p, const float2 *stats, int 
     RowIO<T>::store(RowIO<T>::at(dv, p.sv, b, j, hk), av, d, lane);
 }
 
-// The tcgen05 forward pass (scout_attention_tc.cu); *taken is false where TMA cannot address a tensor and nothing was enqueued.
+// ---- the tcgen05 kernels (scout_attention_tc.cu, scout_attention_bwd_tc.cu) ---------------------------
+// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch); false where TMA cannot address it.
+bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box);
+// *taken is false where TMA cannot address a tensor and nothing was enqueued
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken);
+// views of q, k, v, d_o for the two calls below, which write the results or, with splits > 1, fp32 parts of them
+bool backward_views(const Problem &p, bool bf16, CUtensorMap (&m)[4]);
+int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const CUtensorMap (&m)[4], cudaStream_t stream);
+int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const CUtensorMap (&m)[4],
+               cudaStream_t stream);
 
 }  // namespace attn
 }  // namespace scout

@@ -305,17 +305,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch); false where TMA cannot address it.
-bool view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box) {
-    const uint64_t dims[4] = {(uint64_t)p.head_dim, (uint64_t)tokens, (uint64_t)heads, (uint64_t)p.batch};
-    uint64_t strides[3] = {(uint64_t)s.t * 2, (uint64_t)s.h * 2, (uint64_t)s.b * 2};
-    for (uint64_t &y : strides) {
-        if (y == 0) y = (uint64_t)p.head_dim * 2;  // an axis of one element
-        if (y >= 1ull << 40) return false;
-    }
-    return tc::tensor_map(m, bf16, x, 4, dims, strides, box) == SCOUT_OK;
-}
-
 template <typename T, int HD> int run_forward(const Problem &p, void *o, float *lse, const CUtensorMap (&m)[3], cudaStream_t stream) {
     TcForwardArgs a = {p, o, lse, nullptr, 0, 0};
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
@@ -331,10 +320,21 @@ template <typename T, int HD> int run_forward(const Problem &p, void *o, float *
 
 }  // namespace
 
+// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch); false where TMA cannot address it.
+bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box) {
+    const uint64_t dims[4] = {(uint64_t)p.head_dim, (uint64_t)tokens, (uint64_t)heads, (uint64_t)p.batch};
+    uint64_t strides[3] = {(uint64_t)s.t * 2, (uint64_t)s.h * 2, (uint64_t)s.b * 2};
+    for (uint64_t &y : strides) {
+        if (y == 0) y = (uint64_t)p.head_dim * 2;  // an axis of one element
+        if (y >= 1ull << 40) return false;
+    }
+    return tc::tensor_map(m, bf16, x, 4, dims, strides, box) == SCOUT_OK;
+}
+
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken) {
     CUtensorMap m[3];
-    *taken = view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
-             view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS);
+    *taken = tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
+             tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS);
     if (!*taken) return SCOUT_OK;
     if (p.head_dim > 64)
         return bf16 ? run_forward<__nv_bfloat16, 128>(p, o, lse, m, stream) : run_forward<__half, 128>(p, o, lse, m, stream);
