@@ -162,7 +162,7 @@ __device__ __forceinline__ bool all_nan(const float (&x)[4], int d, int lane) {
 }
 
 template <typename T>
-__device__ __noinline__ void row_forward(const Problem &p, int b, int hq, int i, void *o, float *lse) {
+__device__ __forceinline__ void row_forward(const Problem &p, int b, int hq, int i, void *o, float *lse) {
     const int lane = threadIdx.x & 31, d = p.head_dim, hk = hq / p.group;
     const Lengths n = lengths(p, b);
     const int lo = row_lo(p, n, i), hi = row_hi(p, n, i);
@@ -199,7 +199,7 @@ __device__ __forceinline__ void pair_terms(const Problem &p, const float (&q)[4]
 }
 // stats: {lse * log2 e (+inf for a row that sees nothing), g . o}, [batch][q_heads][q_len]
 template <typename T>
-__device__ __noinline__ void row_dq(const Problem &p, const float2 *stats, int b, int hq, int i, void *dq) {
+__device__ __forceinline__ void row_dq(const Problem &p, const float2 *stats, int b, int hq, int i, void *dq) {
     const int lane = threadIdx.x & 31, d = p.head_dim, hk = hq / p.group;
     const Lengths n = lengths(p, b);
     const int lo = row_lo(p, n, i), hi = row_hi(p, n, i);
@@ -221,7 +221,7 @@ __device__ __noinline__ void row_dq(const Problem &p, const float2 *stats, int b
     RowIO<T>::store(RowIO<T>::at(dq, p.sq, b, i, hq), acc, d, lane);
 }
 template <typename T>
-__device__ __noinline__ void row_dkv(const Problem &p, const float2 *stats, int b, int hk, int j, void *dk, void *dv) {
+__device__ __forceinline__ void row_dkv(const Problem &p, const float2 *stats, int b, int hk, int j, void *dk, void *dv) {
     const int lane = threadIdx.x & 31, d = p.head_dim;
     const Lengths n = lengths(p, b);
     const int lo = col_lo(p, n, j), hi = col_hi(p, n, j);

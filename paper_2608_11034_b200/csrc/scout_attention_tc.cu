@@ -66,19 +66,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                                                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using L = Layout<HD>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * L::STAGES + 7];
+    __shared__ uint64_t bars[2 * L::STAGES + 9];
     __shared__ uint32_t tmem_slot, dead;
     const Problem &p = a.p;
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u, ring = base + 2 * L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * L::STAGES, q_full = empty + 8 * L::STAGES, s_full = q_full + 8, p_full = s_full + 16,
-                   pv_done = p_full + 16;
+                   pv_done = p_full + 32;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     if (threadIdx.x == 0) {
         dead = 0;
         for (int s = 0; s < L::STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
         tc::bar_init(q_full, 1);
-        for (int s = 0; s < 2; ++s) tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 8 * s, 4), tc::bar_init(pv_done + 8 * s, 1);
+        for (int s = 0; s < 2; ++s) tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 16 * s, 4), tc::bar_init(p_full + 16 * s + 8, 4), tc::bar_init(pv_done + 8 * s, 1);
         tc::bar_init_done();
     }
     if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -99,7 +99,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     const int u0 = any0 && any1 ? min(slots[0].blk0, slots[1].blk0) : any0 ? slots[0].blk0 : slots[1].blk0;
     const int u1 = max(slots[0].blk1, slots[1].blk1);
 
+    // launched with 384 x 168 registers, of which the softmax, which holds a row of 128 scores, gets 256 x 224
     if (warp == 8) {
+        tc::registers_down<56>();
         if (lane == 0 && u0 < u1) {
             tc::bar_expect(q_full, 2 * L::TILE);
             for (int s = 0; s < 2; ++s)
@@ -116,6 +118,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             }
         }
     } else if (warp == 9) {
+        tc::registers_down<56>();
         // the whole warp walks the schedule, one lane issues
         constexpr uint32_t qk = tc::instr(Half<T>::is_bf16, ROWS, KEYS, false, false), pv = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
         const auto stage = [&](int r) { return ring + (r % L::STAGES) * L::TILE; };
@@ -156,16 +159,19 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             if (next) ok = landed(rk);
             for (int s = 0; ok && s < 2; ++s) {
                 if (slots[s].blk0 <= u && u < slots[s].blk1) {
-                    ok = patience.wait_warp(p_full + 8 * s, done[s] & 1);
-                    if (!ok) break;
-                    tc::tc_fence_after();
-                    if (lane == 0) {
+                    for (int half = 0; ok && half < 2; ++half) {
+                        ok = patience.wait_warp(p_full + 16 * s + 8 * half, done[s] & 1);
+                        if (!ok) break;
+                        tc::tc_fence_after();
+                        if (lane == 0) {
 #pragma unroll
-                        for (int k = 0; k < KEYS / 16; ++k)
-                            tc::mma_ts(tmem + L::O + s * HD, tmem + L::S + s * KEYS + k * 8, tc::smem_desc(stage(rv) + k * 2048, L::SUB, 1024), pv,
-                                       done[s] > 0 || k > 0);
-                        tc::mma_commit(pv_done + 8 * s);
+                            for (int k = 0; k < KEYS / 32; ++k)
+                                tc::mma_ts(tmem + L::O + s * HD, tmem + L::S + s * KEYS + half * 32 + k * 8,
+                                           tc::smem_desc(stage(rv) + half * (KEYS / 2 * 128) + k * 2048, L::SUB, 1024), pv, done[s] > 0 || half > 0 || k > 0);
+                            if (half) tc::mma_commit(pv_done + 8 * s);
+                        }
                     }
+                    if (!ok) break;
                     __syncwarp();
                     ++done[s];
                 }
@@ -177,7 +183,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             }
             __syncwarp();
         }
-    } else if (warp < 8) {
+    } else if (warp >= 10) {
+        tc::registers_down<56>();
+    } else {
+        tc::registers_up<224>();
         const int s = warp >> 2;
         const Slot sl = slots[s];
         const int i = sl.row0 + (warp & 3) * 32 + lane;
@@ -193,21 +202,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             tc::tc_fence_after();
             const bool whole = blk >= sl.full0 && blk < sl.full1;
             const int first = lo - blk * KEYS, end = hi - blk * KEYS;  // the row's columns
-            uint32_t r[32];
-            float high = -CUDART_INF_F;
+            uint32_t r[4][32];
 #pragma unroll
-            for (int c = 0; c < KEYS / 32; ++c) {
-                tc::tmem_load32(r, at_s + c * 32);
-                tc::tmem_load_wait(r);
-                if (whole) {
+            for (int c = 0; c < 4; ++c) tc::tmem_load32(r[c], at_s + c * 32);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) high = fmaxf(high, __uint_as_float(r[e]));
-                } else {
+            for (int c = 0; c < 4; ++c) tc::tmem_load_wait(r[c]);
+            if (!whole) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) high = c * 32 + e >= first && c * 32 + e < end ? fmaxf(high, __uint_as_float(r[e])) : high;
-                }
+                for (int c = 0; c < 4; ++c)
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) r[c][e] = c * 32 + e >= first && c * 32 + e < end ? r[c][e] : 0xFF800000u;  // -inf
             }
-            high *= p.scale_log2;
+            float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
+#pragma unroll
+            for (int c = 0; c < 4; ++c)
+#pragma unroll
+                for (int e = 0; e < 32; e += 2) m4[(e >> 1) & 3] = fmaxf(fmaxf(m4[(e >> 1) & 3], __uint_as_float(r[c][e])), __uint_as_float(r[c][e + 1]));
+            const float high = fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])) * p.scale_log2;
             const bool move = high > top + LAZY;  // also from -inf
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float fade = move ? exp2_fast(top - high) : 1.f;
@@ -217,42 +228,41 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                     tc::tc_fence_after();
 #pragma unroll
                     for (int c = 0; c < HD / 32; ++c) {
-                        tc::tmem_load32(r, at_o + c * 32);
-                        tc::tmem_load_wait(r);
+                        uint32_t w[32];
+                        tc::tmem_load32(w, at_o + c * 32);
+                        tc::tmem_load_wait(w);
 #pragma unroll
-                        for (int e = 0; e < 32; ++e) r[e] = __float_as_uint(__uint_as_float(r[e]) * fade);
-                        tc::tmem_store16(at_o + c * 32, r);
-                        tc::tmem_store16(at_o + c * 32 + 16, r + 16);
+                        for (int e = 0; e < 32; ++e) w[e] = __float_as_uint(__uint_as_float(w[e]) * fade);
+                        tc::tmem_store16(at_o + c * 32, w);
+                        tc::tmem_store16(at_o + c * 32 + 16, w + 16);
                     }
                 }
                 sum *= fade;
                 top = move ? high : top;
             }
             const float minus = top == -CUDART_INF_F ? 0.f : -top;
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            const tc::F2 scale2 = tc::f2(p.scale_log2, p.scale_log2), minus2 = tc::f2(minus, minus);
+            tc::F2 part[2] = {tc::f2(0.f, 0.f), tc::f2(0.f, 0.f)};
 #pragma unroll
-            for (int c = 0; c < KEYS / 32; ++c) {
-                tc::tmem_load32(r, at_s + c * 32);
-                tc::tmem_load_wait(r);
+            for (int c = 0; c < 4; ++c) {
                 uint32_t w[16];
 #pragma unroll
                 for (int e = 0; e < 32; e += 2) {
-                    float v[2];
-#pragma unroll
-                    for (int g = 0; g < 2; ++g) {
-                        v[g] = exp2_fast(fmaf(__uint_as_float(r[e + g]), p.scale_log2, minus));
-                        if (!whole) v[g] = c * 32 + e + g >= first && c * 32 + e + g < end ? v[g] : 0.f;
-                        part[(e + g) & 3] += v[g];
-                    }
-                    w[e / 2] = Half<T>::pack(v[0], v[1]);
+                    const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1])), scale2, minus2));
+                    const float2 v = make_float2(exp2_fast(y.x), exp2_fast(y.y));
+                    part[(e >> 1) & 1] = tc::add2(part[(e >> 1) & 1], tc::f2(v.x, v.y));
+                    w[e / 2] = Half<T>::pack(v.x, v.y);
                 }
                 tc::tmem_store16(at_s + c * 16, w);  // over columns that have been read
+                if (c & 1) {  // half of the keys: their product can start
+                    tc::tmem_store_wait();
+                    tc::tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) tc::bar_arrive(p_full + 16 * s + 8 * (c >> 1));
+                }
             }
-            sum += (part[0] + part[1]) + (part[2] + part[3]);
-            tc::tmem_store_wait();
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(p_full + 8 * s);
+            const float2 all = tc::split(tc::add2(part[0], part[1]));
+            sum += all.x + all.y;
         }
         if (ok && it > 0) ok = patience.wait_warp(pv_done + 8 * s, (it - 1) & 1);
         tc::tc_fence_after();

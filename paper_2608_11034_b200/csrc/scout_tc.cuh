@@ -61,7 +61,7 @@ struct Patience {
     }
     // the same for a whole warp whose next steps need all of its lanes
     __device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity) const { return __all_sync(0xFFFFFFFFu, wait(bar, parity)); }
-    __device__ __noinline__ bool wait_long(uint32_t bar, uint32_t parity) const {
+    __device__ __forceinline__ bool wait_long(uint32_t bar, uint32_t parity) const {
         const uint64_t until = now_ns() + WAIT_LIMIT_NS;
         while (!bar_try(bar, parity)) {
             if (*dead) return false;
@@ -93,6 +93,40 @@ __device__ __forceinline__ void tma_4d(uint32_t dst, const CUtensorMap *m, uint3
 }
 // what this thread wrote to shared memory becomes visible to TMA and tcgen05
 __device__ __forceinline__ void fence_async() { asm volatile("fence.proxy.async.shared::cta;" ::: "memory"); }
+
+// Registers move between the warpgroups of a block: the sum over its warpgroups must stay within what it was launched with.
+template <int N> __device__ __forceinline__ void registers_up() { asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(N)); }
+template <int N> __device__ __forceinline__ void registers_down() { asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(N)); }
+
+// Two fp32 operations in one instruction.
+struct F2 {
+    uint64_t v;
+};
+__device__ __forceinline__ F2 f2(float lo, float hi) {
+    F2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r.v) : "f"(lo), "f"(hi));
+    return r;
+}
+__device__ __forceinline__ float2 split(F2 x) {
+    float2 r;
+    asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(x.v));
+    return r;
+}
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) {
+    F2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.v) : "l"(a.v), "l"(b.v), "l"(c.v));
+    return r;
+}
+__device__ __forceinline__ F2 add2(F2 a, F2 b) {
+    F2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
+__device__ __forceinline__ F2 mul2(F2 a, F2 b) {
+    F2 r;
+    asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r.v) : "l"(a.v), "l"(b.v));
+    return r;
+}
 
 // Tensor memory: `cols` (a power of two, 32..512) columns of 128 lanes x 32 bits; one warp allocates and frees.
 __device__ __forceinline__ void tmem_alloc(uint32_t slot, uint32_t cols) {

@@ -35,12 +35,40 @@ def _fail(what: str):
     raise ValueError(what)
 
 
-@functools.lru_cache(maxsize=256)
-def _attention(dtype, batch, q_len, kv_len, q_heads, kv_heads, head_dim, causal, window, scale, strides):
-    """-> (record, its address, scratch bytes of the forward and of the backward pass); sizes only, no data"""
-    a = np.zeros(1, dtype=binding.ATTN_DTYPE)
-    a[0] = (_CODE[dtype], batch, q_len, kv_len, q_heads, kv_heads, head_dim, causal, window, scale) + strides
-    return (a, a.ctypes.data) + binding.scout_attn_workspace(a.ctypes.data)
+class _Attention:
+    """What a call needs to know of its arguments' sizes: the library's record and the scratch of both passes."""
+    __slots__ = ("record", "at", "forward_bytes", "backward_bytes", "batch", "rows", "index")
+
+
+@functools.lru_cache(maxsize=1024)
+def _attention(dtypes, devices, qs, ks, vs, os, gs, q_stride, k_stride, v_stride, o_stride, g_stride, causal, window, scale):
+    """Checks a description of q, k, v, o, do (sizes only, no data) -> _Attention."""
+    if len(qs) != 4 or len(ks) != 4 or ks != vs:
+        _fail("q is [batch, q_len, q_heads, head_dim], k and v are [batch, kv_len, kv_heads, head_dim]")
+    b, tq, hq, d = qs
+    if ks[0] != b or ks[3] != d:
+        _fail("q and k differ in batch or head_dim")
+    if os != qs or gs != qs:
+        _fail("o and do must have the shape of q")
+    if dtypes[0] not in _SIXTEEN:
+        _fail("attention takes bfloat16 or float16")
+    if len(set(dtypes)) != 1 or len(set(devices)) != 1:
+        _fail("q, k, v, o and do must share one dtype and device")
+    if devices[0].type != "cuda":
+        _fail("tensors must be on a CUDA device")
+    if window < 0:
+        _fail("window: 0 (all) or a number of tokens")
+    strides = (q_stride, k_stride, v_stride, o_stride, g_stride)
+    if d > 1 and any(st[3] != 1 for st in strides):
+        _fail("a head's elements must be adjacent (last stride 1)")
+    r = _Attention()
+    r.record = np.zeros(1, dtype=binding.ATTN_DTYPE)
+    r.record[0] = (_CODE[dtypes[0]], b, tq, ks[1], hq, ks[2], d, int(bool(causal)), int(window),
+                   1.0 / math.sqrt(d) if scale is None and d else float(scale or 0.0)) + tuple(st[:3] for st in strides)
+    r.at = r.record.ctypes.data
+    r.forward_bytes, r.backward_bytes = binding.scout_attn_workspace(r.at)
+    r.batch, r.rows, r.index = b, (b, hq, tq), devices[0].index
+    return r
 
 
 def _lens(x, batch, device, name) -> int:
@@ -51,54 +79,21 @@ def _lens(x, batch, device, name) -> int:
     return x.data_ptr()
 
 
-def _strided(x, name):
-    if x.shape[-1] > 1 and x.stride(-1) != 1:
-        _fail(f"{name}: a head's elements must be adjacent (last stride 1)")
-    s = x.stride()
-    return s[0], s[1], s[2]
+def _scratch(nbytes, x):
+    return x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
 
 
-def _problem(q, k, v, o, d_o, causal, window, scale):
-    if q.dim() != 4 or k.dim() != 4 or k.shape != v.shape:
-        _fail("q is [batch, q_len, q_heads, head_dim], k and v are [batch, kv_len, kv_heads, head_dim]")
-    b, tq, hq, d = q.shape
-    if k.shape[0] != b or k.shape[3] != d:
-        _fail("q and k differ in batch or head_dim")
-    if q.dtype not in _SIXTEEN:
-        _fail("attention takes bfloat16 or float16")
-    for x in (k, v, o, d_o):
-        if x.dtype != q.dtype or x.device != q.device:
-            _fail("q, k, v, o and do must share one dtype and device")
-    if not q.is_cuda:
-        _fail("tensors must be on a CUDA device")
-    for x, name in ((o, "o"), (d_o, "do")):
-        if x.shape != q.shape:
-            _fail(f"{name} must have the shape of q")
-    strides = tuple(_strided(x, n) for x, n in ((q, "q"), (k, "k"), (v, "v"), (o, "o"), (d_o, "do")))
-    return _attention(q.dtype, b, tq, k.shape[1], hq, k.shape[2], d, int(bool(causal)), int(window),
-                      1.0 / math.sqrt(d) if scale is None else float(scale), strides)
-
-
-def _scratch(nbytes, device):
-    return torch.empty(nbytes, dtype=torch.uint8, device=device) if nbytes else None
-
-
-class _On:
-    """The tensors' device made current, and its current stream's handle; costs nothing when it is current already."""
-
-    def __init__(self, x):
-        self.index = x.device.index
-
-    def __enter__(self) -> int:
-        now = torch.cuda.current_device()
-        self.back = None if now == self.index else now
-        if self.back is not None:
-            torch.cuda.set_device(self.index)
-        return torch._C._cuda_getCurrentRawStream(self.index)
-
-    def __exit__(self, *_):
-        if self.back is not None:
-            torch.cuda.set_device(self.back)
+def _enqueue(index: int, call, *args) -> None:
+    """call(*args, stream) with the tensors' device current, on its current stream"""
+    now = torch.cuda.current_device()
+    if now == index:
+        call(*args, torch._C._cuda_getCurrentRawStream(index))
+        return
+    torch.cuda.set_device(index)
+    try:
+        call(*args, torch._C._cuda_getCurrentRawStream(index))
+    finally:
+        torch.cuda.set_device(now)
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, window: int = 0,
@@ -113,13 +108,13 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     q_lens, kv_lens: int32 [batch], the tokens in use of padded sequences.
     -> (o like q, lse float32 [batch, q_heads, q_len]); rows that see nothing give 0 and -inf."""
     o = torch.empty_like(q)
-    _, at, nbytes, _ = _problem(q, k, v, o, o, causal, window, scale)
-    lse = torch.empty((q.shape[0], q.shape[2], q.shape[1]), dtype=torch.float32, device=q.device)
-    ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
-    ws = _scratch(nbytes, q.device)
-    with _On(q) as stream:
-        binding.scout_attn_forward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
-                                   ws.data_ptr() if ws is not None else 0, nbytes, stream)
+    t = _attention((q.dtype, k.dtype, v.dtype), (q.device, k.device, v.device), q.shape, k.shape, v.shape, q.shape, q.shape,
+                   q.stride(), k.stride(), v.stride(), o.stride(), o.stride(), causal, window, scale)
+    lse = q.new_empty(t.rows, dtype=torch.float32)
+    ql, kl = _lens(q_lens, t.batch, q.device, "q_lens"), _lens(kv_lens, t.batch, q.device, "kv_lens")
+    ws = _scratch(t.forward_bytes, q)
+    _enqueue(t.index, binding.scout_attn_forward, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(),
+             lse.data_ptr(), ws.data_ptr() if ws is not None else 0, t.forward_bytes)
     return o, lse
 
 
@@ -129,20 +124,20 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     """Gradients of attention_forward's o with respect to q, k and v, from the gradient `do` of o and what the
     forward pass returned; the other arguments as there.  Gradients of key heads that several query heads share are
     summed over those.  -> (dq, dk, dv), laid out like q, k, v."""
+    t = _attention((q.dtype, k.dtype, v.dtype, o.dtype, do.dtype), (q.device, k.device, v.device, o.device, do.device), q.shape,
+                   k.shape, v.shape, o.shape, do.shape, q.stride(), k.stride(), v.stride(), o.stride(), do.stride(), causal, window,
+                   scale)
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     for x, y, name in ((q, dq, "q"), (k, dk, "k"), (v, dv, "v")):
         if x.stride() != y.stride():
             _fail(f"{name}: overlapping or gapped memory has no gradient laid out like it; pass {name}.contiguous()")
-    _, at, _, nbytes = _problem(q, k, v, o, do, causal, window, scale)
-    if lse.dtype != torch.float32 or lse.shape != (q.shape[0], q.shape[2], q.shape[1]) or not lse.is_contiguous() or \
-            lse.device != q.device:
+    if lse.dtype != torch.float32 or lse.shape != t.rows or not lse.is_contiguous() or lse.device != q.device:
         _fail("lse: the forward pass's, a contiguous float32 tensor [batch, q_heads, q_len]")
-    ql, kl = _lens(q_lens, q.shape[0], q.device, "q_lens"), _lens(kv_lens, q.shape[0], q.device, "kv_lens")
-    ws = _scratch(nbytes, q.device)
-    with _On(q) as stream:
-        binding.scout_attn_backward(at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(), do.data_ptr(),
-                                    ql, kl, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
-                                    ws.data_ptr() if ws is not None else 0, nbytes, stream)
+    ql, kl = _lens(q_lens, t.batch, q.device, "q_lens"), _lens(kv_lens, t.batch, q.device, "kv_lens")
+    ws = _scratch(t.backward_bytes, q)
+    _enqueue(t.index, binding.scout_attn_backward, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+             do.data_ptr(), ql, kl, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr() if ws is not None else 0,
+             t.backward_bytes)
     return dq, dk, dv
 
 
@@ -170,11 +165,10 @@ def checkpoint_pack(x: torch.Tensor):
     if x.dtype not in _CODE:
         _fail("activations are float32, bfloat16 or float16")
     rows, cols = x.shape
-    codes = torch.empty((rows, cols), dtype=torch.int8, device=x.device)
-    exps = torch.empty((rows, -(-cols // binding.CKPT_BLOCK)), dtype=torch.int8, device=x.device)
-    with _On(x) as stream:
-        binding.scout_ckpt_pack(_CODE[x.dtype], rows, cols, x.data_ptr(), stride, codes.data_ptr(), max(cols, 1),
-                                exps.data_ptr(), stream)
+    codes = x.new_empty((rows, cols), dtype=torch.int8)
+    exps = x.new_empty((rows, -(-cols // binding.CKPT_BLOCK)), dtype=torch.int8)
+    _enqueue(x.device.index, binding.scout_ckpt_pack, _CODE[x.dtype], rows, cols, x.data_ptr(), stride, codes.data_ptr(),
+             max(cols, 1), exps.data_ptr())
     return codes, exps
 
 
@@ -183,10 +177,9 @@ def checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, dtype: torch.dtyp
     rows, cols, stride = _checkpoint(codes, exps)
     if dtype not in _CODE:
         _fail("activations are float32, bfloat16 or float16")
-    x = torch.empty((rows, cols), dtype=dtype, device=codes.device)
-    with _On(codes) as stream:
-        binding.scout_ckpt_unpack(_CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(), x.data_ptr(),
-                                  max(cols, 1), stream)
+    x = codes.new_empty((rows, cols), dtype=dtype)
+    _enqueue(codes.device.index, binding.scout_ckpt_unpack, _CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(),
+             x.data_ptr(), max(cols, 1))
     return x
 
 
@@ -204,14 +197,13 @@ def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, 
     if dy.dtype not in _SIXTEEN or dy.shape[0] != rows or dy.device != codes.device:
         _fail("dy: a bfloat16 or float16 matrix with the checkpoint's rows, on its device")
     outs = dy.shape[1]
-    dw = torch.empty((outs, ins), dtype=out_dtype, device=dy.device) if grad is None else grad
+    dw = dy.new_empty((outs, ins), dtype=out_dtype) if grad is None else grad
     dw_stride = _matrix(dw, "grad")
     if dw.dtype not in (torch.float32, dy.dtype) or dw.shape != (outs, ins) or dw.device != dy.device:
         _fail("the gradient is [outs, ins], float32 or of dy's dtype, on dy's device")
     nbytes = _wgrad_scratch(_CODE[dy.dtype], rows, outs, ins)
-    ws = _scratch(nbytes, dy.device)
-    with _On(dy) as stream:
-        binding.scout_ckpt_wgrad(_CODE[dy.dtype], _CODE[dw.dtype], rows, outs, ins, dy.data_ptr(), dy_stride, codes.data_ptr(),
-                                 code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
-                                 ws.data_ptr() if ws is not None else 0, nbytes, stream)
+    ws = _scratch(nbytes, dy)
+    _enqueue(dy.device.index, binding.scout_ckpt_wgrad, _CODE[dy.dtype], _CODE[dw.dtype], rows, outs, ins, dy.data_ptr(), dy_stride,
+             codes.data_ptr(), code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
+             ws.data_ptr() if ws is not None else 0, nbytes)
     return dw
