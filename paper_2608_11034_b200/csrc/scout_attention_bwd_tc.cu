@@ -47,7 +47,7 @@ template <int HD> __device__ __forceinline__ void clear_rows(uint32_t tile, int 
     tc::fence_async();
     __syncwarp();
 }
-// D = A B^T of two tiles, both [128 rows][HD]; one lane
+// D = A B^T of two tiles, both [128 rows][HD]
 template <typename T, int HD> __device__ __forceinline__ void product_tiles(uint32_t d, uint32_t x, uint32_t y) {
     constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, ROWS, false, false);
 #pragma unroll
@@ -56,7 +56,7 @@ template <typename T, int HD> __device__ __forceinline__ void product_tiles(uint
         tc::mma(d, tc::smem_desc(x + off, 16, 1024), tc::smem_desc(y + off, 16, 1024), id, k > 0);
     }
 }
-// D += W X: W [128 lanes][128 k] in 16 bits in tensor memory, the second 64 k at w + gap; X a tile [128 k][HD]; one lane
+// D += W X: W [128 lanes][128 k] in 16 bits in tensor memory, the second 64 k at w + gap; X a tile [128 k][HD]
 template <typename T, int HD> __device__ __forceinline__ void product_sum(uint32_t d, uint32_t w, uint32_t gap, uint32_t x, bool add) {
     constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
 #pragma unroll
@@ -167,7 +167,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
     const uint32_t sq = (smem_u32(smem_raw) + 1023) & ~1023u, sg = sq + L::TILE, ring = sg + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 8, dp_full = s_full + 8,
                    s_read = dp_full + 8, ds_full = s_read + 8, dq_done = ds_full + 8;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     if (threadIdx.x == 0) {
         dead = 0;
@@ -180,7 +180,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = tc::uniform(tmem_slot);
     pdl_wait();  // the statistics
 
     int x = blockIdx.x;
@@ -219,19 +219,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         const auto issue_s = [&](int j) {
             // keys past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dQ
             if (n.nk < p.kv_len && (blk0 + j + 1) * ROWS > n.nk) clear_rows<HD>(stage(2 * j), max(n.nk - (blk0 + j) * ROWS, 0), lane);
-            if (lane == 0) {
-                product_tiles<T, HD>(tmem + S, sq, stage(2 * j));
-                tc::mma_commit(s_full);
-            }
-            __syncwarp();
+            product_tiles<T, HD>(tmem + S, sq, stage(2 * j));
+            tc::mma_commit(s_full);
         };
         const auto issue_dp = [&](int j) {
-            if (lane == 0) {
-                product_tiles<T, HD>(tmem + DP, sg, stage(2 * j + 1));
-                tc::mma_commit(dp_full);
-                tc::mma_commit(empty + 8 * ((2 * j + 1) % STAGES));
-            }
-            __syncwarp();
+            product_tiles<T, HD>(tmem + DP, sg, stage(2 * j + 1));
+            tc::mma_commit(dp_full);
+            tc::mma_commit(empty + 8 * ((2 * j + 1) % STAGES));
         };
         bool ok = steps > 0 && patience.wait_warp(q_full, 0) && landed(0);
         if (ok) issue_s(0);
@@ -248,12 +242,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
             ok = patience.wait_warp(ds_full, j & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            if (lane == 0) {
-                product_sum<T, HD>(tmem + DQ, tmem + DS, 32, stage(2 * j), j > 0);
-                tc::mma_commit(empty + 8 * ((2 * j) % STAGES));
-                if (!next) tc::mma_commit(dq_done);
-            }
-            __syncwarp();
+            product_sum<T, HD>(tmem + DQ, tmem + DS, 32, stage(2 * j), j > 0);
+            tc::mma_commit(empty + 8 * ((2 * j) % STAGES));
+            if (!next) tc::mma_commit(dq_done);
             if (next) {
                 ok = landed(2 * j + 3);
                 if (ok) issue_dp(j + 1);
@@ -328,7 +319,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     const uint32_t sk = (smem_u32(smem_raw) + 1023) & ~1023u, sv = sk + L::TILE, ring = sv + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 8, dp_full = s_full + 8,
                    p_full = dp_full + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     if (threadIdx.x == 0) {
         dead = 0;
@@ -342,7 +333,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = tc::uniform(tmem_slot);
     pdl_wait();  // the statistics, and the parts that dQ's join has read
 
     int x = blockIdx.x;
@@ -387,18 +378,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             return true;
         };
         const auto issue_s = [&](int s) {
-            if (lane == 0) {
-                product_tiles<T, HD>(tmem + S, sk, stage(2 * s));
-                tc::mma_commit(s_full);
-            }
-            __syncwarp();
+            product_tiles<T, HD>(tmem + S, sk, stage(2 * s));
+            tc::mma_commit(s_full);
         };
         const auto issue_dp = [&](int s) {
-            if (lane == 0) {
-                product_tiles<T, HD>(tmem + DP, sv, stage(2 * s + 1));
-                tc::mma_commit(dp_full);
-            }
-            __syncwarp();
+            product_tiles<T, HD>(tmem + DP, sv, stage(2 * s + 1));
+            tc::mma_commit(dp_full);
         };
         bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0);
         if (ok) issue_s(0);
@@ -409,11 +394,8 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             ok = patience.wait_warp(p_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            if (lane == 0) {
-                product_sum<T, HD>(tmem + DV, tmem + S, 64, stage(2 * s + 1), s > 0);
-                tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));
-            }
-            __syncwarp();
+            product_sum<T, HD>(tmem + DV, tmem + S, 64, stage(2 * s + 1), s > 0);
+            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));
             if (next) {
                 ok = landed(2 * s + 2);
                 if (!ok) break;
@@ -422,12 +404,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             ok = patience.wait_warp(ds_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            if (lane == 0) {
-                product_sum<T, HD>(tmem + DK, tmem + DP, 64, stage(2 * s), s > 0);
-                tc::mma_commit(empty + 8 * ((2 * s) % STAGES));
-                if (!next) tc::mma_commit(all_done);
-            }
-            __syncwarp();
+            product_sum<T, HD>(tmem + DK, tmem + DP, 64, stage(2 * s), s > 0);
+            tc::mma_commit(empty + 8 * ((2 * s) % STAGES));
+            if (!next) tc::mma_commit(all_done);
             if (next) {
                 ok = landed(2 * s + 3);
                 if (ok) issue_dp(s + 1);

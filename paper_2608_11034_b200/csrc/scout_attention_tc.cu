@@ -36,8 +36,8 @@ struct TcForwardArgs {
 template <int HD> struct Layout {
     static constexpr int SUB = ROWS * 128;           // 128 rows x 64 elements
     static constexpr int TILE = SUB * (HD / 64);
-    static constexpr int STAGES = HD == 128 ? 5 : 8;  // of K or V tiles
-    static constexpr int SMEM = (2 + STAGES) * TILE + 1024;
+    static constexpr int STAGES = HD == 128 ? 2 : 4;  // of pairs (V of a block, K of the next)
+    static constexpr int SMEM = (3 + 2 * STAGES) * TILE + 1024;  // Q of two slots, the first K, the pairs
     static constexpr int S = 0, O = 256;             // tensor memory columns: S (and P) of two slots, O of two slots
 };
 
@@ -66,26 +66,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                                                             const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
     using L = Layout<HD>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * L::STAGES + 9];
+    __shared__ uint64_t bars[2 * L::STAGES + 11];
     __shared__ uint32_t tmem_slot, dead;
     const Problem &p = a.p;
-    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u, ring = base + 2 * L::TILE;
+    const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u, first_k = base + 2 * L::TILE, ring = first_k + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * L::STAGES, q_full = empty + 8 * L::STAGES, s_full = q_full + 8, p_full = s_full + 16,
-                   pv_done = p_full + 32;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+                   o_done = p_full + 32, clean = o_done + 16;
+    const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     if (threadIdx.x == 0) {
         dead = 0;
         for (int s = 0; s < L::STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        tc::bar_init(q_full, 1);
-        for (int s = 0; s < 2; ++s) tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 16 * s, 4), tc::bar_init(p_full + 16 * s + 8, 4), tc::bar_init(pv_done + 8 * s, 1);
+        tc::bar_init(q_full, 1), tc::bar_init(clean, 1), tc::bar_init(clean + 8, 1);
+        for (int s = 0; s < 2; ++s) tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 16 * s, 4), tc::bar_init(p_full + 16 * s + 8, 4), tc::bar_init(o_done + 8 * s, 1);
         tc::bar_init_done();
     }
     if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = tc::uniform(tmem_slot);
 
     int x = blockIdx.x;
     const int hs = a.pair_heads ? p.q_heads / 2 : p.q_heads;
@@ -98,92 +98,98 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     const bool any0 = slots[0].blk0 < slots[0].blk1, any1 = slots[1].blk0 < slots[1].blk1;
     const int u0 = any0 && any1 ? min(slots[0].blk0, slots[1].blk0) : any0 ? slots[0].blk0 : slots[1].blk0;
     const int u1 = max(slots[0].blk1, slots[1].blk1);
+    const int dirty = n.nk < p.kv_len && n.nk % KEYS ? n.nk / KEYS : -1;  // the block that a sequence ends inside of
 
     // launched with 384 x 168 registers, of which the softmax, which holds a row of 128 scores, gets 256 x 224
     if (warp == 8) {
         tc::registers_down<56>();
         if (lane == 0 && u0 < u1) {
-            tc::bar_expect(q_full, 2 * L::TILE);
-            for (int s = 0; s < 2; ++s)
+            const auto load = [&](uint32_t to, const CUtensorMap *m, uint32_t bar, int row, int head) {
 #pragma unroll
-                for (int c = 0; c < HD / 64; ++c)
-                    tc::tma_4d(base + s * L::TILE + c * L::SUB, &map_q, q_full, c * 64, slots[s].row0, slots[s].head, b);
-            for (int r = 0; r < 2 * (u1 - u0); ++r) {
-                const int st = r % L::STAGES;
-                if (!patience.wait(empty + 8 * st, ((r / L::STAGES) & 1) ^ 1)) break;
-                tc::bar_expect(full + 8 * st, L::TILE);
-#pragma unroll
-                for (int c = 0; c < HD / 64; ++c)
-                    tc::tma_4d(ring + st * L::TILE + c * L::SUB, r & 1 ? &map_v : &map_k, full + 8 * st, c * 64, (u0 + (r >> 1)) * KEYS, hk, b);
+                for (int c = 0; c < HD / 64; ++c) tc::tma_4d(to + c * L::SUB, m, bar, c * 64, row, head, b);
+            };
+            tc::bar_expect(q_full, 3 * L::TILE);
+            load(base, &map_q, q_full, slots[0].row0, slots[0].head);
+            load(first_k, &map_k, q_full, u0 * KEYS, hk);
+            load(base + L::TILE, &map_q, q_full, slots[1].row0, slots[1].head);
+            for (int u = u0; u < u1; ++u) {
+                const int st = (u - u0) % L::STAGES;
+                const bool next = u + 1 < u1;
+                if (!patience.wait(empty + 8 * st, (((u - u0) / L::STAGES) & 1) ^ 1)) break;
+                tc::bar_expect(full + 8 * st, next ? 2 * L::TILE : L::TILE);
+                load(ring + st * 2 * L::TILE, &map_v, full + 8 * st, u * KEYS, hk);
+                if (next) load(ring + st * 2 * L::TILE + L::TILE, &map_k, full + 8 * st, (u + 1) * KEYS, hk);
             }
         }
     } else if (warp == 9) {
         tc::registers_down<56>();
-        // the whole warp walks the schedule, one lane issues
-        constexpr uint32_t qk = tc::instr(Half<T>::is_bf16, ROWS, KEYS, false, false), pv = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
-        const auto stage = [&](int r) { return ring + (r % L::STAGES) * L::TILE; };
-        const auto landed = [&](int r) { return patience.wait_warp(full + 8 * (r % L::STAGES), (r / L::STAGES) & 1); };
-        const auto product_s = [&](int s, int r) {
-            if (lane == 0) {
+        // The pipe takes few instructions in advance and issuing waits for it, so what stands between two products
+        // (waits, commits) is kept short: it is hidden only as long as the products already taken last.
+        if (u0 < u1 && patience.wait_warp(q_full, 0)) {
+            constexpr uint32_t qk = tc::instr(Half<T>::is_bf16, ROWS, KEYS, false, false), pv = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
+            const uint64_t dq = tc::smem_desc(base, 16, 1024), dk = tc::smem_desc(first_k, 16, 1024), dv = tc::smem_desc(ring, L::SUB, 1024);
+            const auto seen = [&](int s, int u) { return slots[s].blk0 <= u && u < slots[s].blk1; };
+            const auto product_s = [&](int s, uint64_t k) {
 #pragma unroll
-                for (int k = 0; k < HD / 16; ++k)
-                    tc::mma(tmem + L::S + s * KEYS, tc::smem_desc(base + s * L::TILE + (k >> 2) * L::SUB + (k & 3) * 32, 16, 1024),
-                            tc::smem_desc(stage(r) + (k >> 2) * L::SUB + (k & 3) * 32, 16, 1024), qk, k > 0);
+                for (int i = 0; i < HD / 16; ++i)
+                    tc::mma(tmem + L::S + s * KEYS, tc::desc_at(dq, s * L::TILE + (i >> 2) * L::SUB + (i & 3) * 32),
+                            tc::desc_at(k, (i >> 2) * L::SUB + (i & 3) * 32), qk, i > 0);
                 tc::mma_commit(s_full + 8 * s);
-            }
-            __syncwarp();
-        };
-        int done[2] = {0, 0};
-        bool ok = u0 >= u1 || (patience.wait_warp(q_full, 0) && landed(0));
-        if (ok && u0 < u1) {
-            tc::tc_fence_after();
+            };
+#pragma unroll
             for (int s = 0; s < 2; ++s)
-                if (slots[s].blk0 <= u0 && u0 < slots[s].blk1) product_s(s, 0);
-            if (lane == 0) tc::mma_commit(empty);
-            __syncwarp();
+                if (seen(s, u0)) product_s(s, dk);
+            bool ok = true;
+            int done[2] = {0, 0};
+            for (int u = u0; ok && u < u1; ++u) {
+                const int st = (u - u0) % L::STAGES;
+                const uint64_t v = tc::desc_at(dv, st * 2 * L::TILE), k = tc::desc_at(tc::smem_desc(ring + L::TILE, 16, 1024), st * 2 * L::TILE);
+                ok = patience.wait_warp(full + 8 * st, ((u - u0) / L::STAGES) & 1);
+                if (ok && u == dirty) {
+                    if (lane == 0) tc::bar_arrive(clean);
+                    ok = patience.wait_warp(clean + 8, 0);
+                }
+#pragma unroll
+                for (int s = 0; s < 2; ++s) {
+                    if (!ok) break;
+                    if (seen(s, u)) {
+#pragma unroll
+                        for (int half = 0; half < 2; ++half) {
+                            ok = ok && patience.wait_warp(p_full + 16 * s + 8 * half, done[s] & 1);
+                            if (!ok) break;
+                            tc::tc_fence_after();
+#pragma unroll
+                            for (int i = 0; i < KEYS / 32; ++i)
+                                tc::mma_ts(tmem + L::O + s * HD, tmem + L::S + s * KEYS + half * 32 + i * 8,
+                                           tc::desc_at(v, half * (KEYS / 2 * 128) + i * 2048), pv, done[s] > 0 || half > 0 || i > 0);
+                        }
+                        if (!ok) break;
+                        ++done[s];
+                        if (u + 1 == slots[s].blk1) tc::mma_commit(o_done + 8 * s);
+                    }
+                    // reaching s_full also says that the product with V before it is done
+                    if (seen(s, u + 1)) product_s(s, k);
+                }
+                tc::mma_commit(empty + 8 * st);
+            }
         }
-        for (int u = u0; ok && u < u1; ++u) {
-            const int rv = 2 * (u - u0) + 1, rk = rv + 1;
-            ok = landed(rv);
-            if (!ok) break;
-            // padding between a sequence's length and the tensor's end may hold anything, and 0 * NaN is NaN
-            if (n.nk < p.kv_len && (u + 1) * KEYS > n.nk) {
-                for (int i = lane; i < ((u + 1) * KEYS - max(n.nk, u * KEYS)) * (HD / 8); i += 32) {
+    } else if (warp == 10) {
+        tc::registers_down<56>();
+        // padding between a sequence's length and the tensor's end may hold anything, and 0 * NaN is NaN: V's rows there become zeros
+        if (dirty >= u0 && dirty < u1) {
+            const int st = (dirty - u0) % L::STAGES;
+            if (patience.wait_warp(clean, 0)) {  // it has landed
+                for (int i = lane; i < ((dirty + 1) * KEYS - n.nk) * (HD / 8); i += 32) {
                     const int row = KEYS - 1 - i / (HD / 8), chunk = i % (HD / 8);
-                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(stage(rv) + (chunk >> 3) * L::SUB + row * 128 + (chunk & 7) * 16), "r"(0) : "memory");
+                    asm volatile("st.shared.v4.b32 [%0], {%1,%1,%1,%1};" ::"r"(ring + st * 2 * L::TILE + (chunk >> 3) * L::SUB + row * 128 + (chunk & 7) * 16),
+                                 "r"(0) : "memory");
                 }
                 tc::fence_async();
                 __syncwarp();
+                if (lane == 0) tc::bar_arrive(clean + 8);
             }
-            bool next = u + 1 < u1;
-            if (next) ok = landed(rk);
-            for (int s = 0; ok && s < 2; ++s) {
-                if (slots[s].blk0 <= u && u < slots[s].blk1) {
-                    for (int half = 0; ok && half < 2; ++half) {
-                        ok = patience.wait_warp(p_full + 16 * s + 8 * half, done[s] & 1);
-                        if (!ok) break;
-                        tc::tc_fence_after();
-                        if (lane == 0) {
-#pragma unroll
-                            for (int k = 0; k < KEYS / 32; ++k)
-                                tc::mma_ts(tmem + L::O + s * HD, tmem + L::S + s * KEYS + half * 32 + k * 8,
-                                           tc::smem_desc(stage(rv) + half * (KEYS / 2 * 128) + k * 2048, L::SUB, 1024), pv, done[s] > 0 || half > 0 || k > 0);
-                            if (half) tc::mma_commit(pv_done + 8 * s);
-                        }
-                    }
-                    if (!ok) break;
-                    __syncwarp();
-                    ++done[s];
-                }
-                if (next && slots[s].blk0 <= u + 1 && u + 1 < slots[s].blk1) product_s(s, rk);
-            }
-            if (lane == 0) {
-                tc::mma_commit(empty + 8 * (rv % L::STAGES));
-                if (next) tc::mma_commit(empty + 8 * (rk % L::STAGES));
-            }
-            __syncwarp();
         }
-    } else if (warp >= 10) {
+    } else if (warp == 11) {
         tc::registers_down<56>();
     } else {
         tc::registers_up<224>();
@@ -223,9 +229,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             if (__any_sync(0xFFFFFFFFu, move)) {
                 const float fade = move ? exp2_fast(top - high) : 1.f;
                 if (it > 0) {
-                    ok = patience.wait_warp(pv_done + 8 * s, (it - 1) & 1);
-                    if (!ok) break;
-                    tc::tc_fence_after();
 #pragma unroll
                     for (int c = 0; c < HD / 32; ++c) {
                         uint32_t w[32];
@@ -264,7 +267,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             const float2 all = tc::split(tc::add2(part[0], part[1]));
             sum += all.x + all.y;
         }
-        if (ok && it > 0) ok = patience.wait_warp(pv_done + 8 * s, (it - 1) & 1);
+        if (ok && it > 0) ok = patience.wait_warp(o_done + 8 * s, 0);
         tc::tc_fence_after();
         if (ok) {
             const bool sees = hi > lo;  // rows past their sequence went along with the tile

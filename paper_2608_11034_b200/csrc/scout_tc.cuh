@@ -22,11 +22,8 @@ int gave_up_counter(uint32_t **counter);
 // ---- device --------------------------------------------------------------------------------------
 constexpr uint64_t WAIT_LIMIT_NS = 2000000000ull;
 
-__device__ __forceinline__ uint32_t elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.b32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p;
-}
+// a value that is the same in all lanes, as one that the compiler knows to be
+__device__ __forceinline__ uint32_t uniform(uint32_t x) { return __shfl_sync(0xFFFFFFFFu, x, 0); }
 __device__ __forceinline__ uint64_t now_ns() {
     uint64_t t;
     asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
@@ -152,19 +149,24 @@ __device__ __forceinline__ uint64_t smem_desc(uint32_t addr, uint32_t lead, uint
     return (uint64_t)((addr >> 4) & 0x3FFF) | ((uint64_t)((lead >> 4) & 0x3FFF) << 16) | ((uint64_t)((stride >> 4) & 0x3FFF) << 32) |
            (1ull << 46) | (2ull << 61);
 }
-// D (tensor memory) = A B, or += with add
+// The same operand `bytes` further on: only the address field changes (it counts 16 bytes and never carries out).
+__device__ __forceinline__ uint64_t desc_at(uint64_t desc, uint32_t bytes) { return desc + (bytes >> 4); }
+// D (tensor memory) = A B, or += with add.  A whole warp calls these, and one lane issues: the descriptors then live in
+// uniform registers, where the instruction wants them; from a branch that one lane takes they would be moved there one by one.
 __device__ __forceinline__ void mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a),
-                 "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred e, p;\n\telect.sync _|e, 0xFFFFFFFF;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n\t}" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
 // the same with A in tensor memory: 128 lanes, two 16-bit elements of K to a column
 __device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, bool add) {
-    asm volatile("{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\ttcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a),
-                 "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
+    asm volatile(
+        "{\n\t.reg .pred e, p;\n\telect.sync _|e, 0xFFFFFFFF;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "@e tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n\t}" ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"((uint32_t)add) : "memory");
 }
-// arrives on the barrier when every product this thread has issued so far is done
+// arrives on the barrier when every product this warp has issued so far is done (the elected lane is always the same)
 __device__ __forceinline__ void mma_commit(uint32_t bar) {
-    asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+    asm volatile("{\n\t.reg .pred e;\n\telect.sync _|e, 0xFFFFFFFF;\n\t@e tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];\n\t}" ::"r"(bar) : "memory");
 }
 
 // 32 lanes (those of this warp's quarter) x 32 columns to / from registers, lane by thread

@@ -187,7 +187,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
     __shared__ uint32_t tmem_slot, dead;
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, sum_full = empty + 8 * STAGES, sum_empty = sum_full + 16;
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     if (threadIdx.x == 0) {
         dead = 0;
@@ -199,7 +199,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
     tc::tc_fence_before();
     __syncthreads();
     tc::tc_fence_after();
-    const uint32_t tmem = tmem_slot;
+    const uint32_t tmem = tc::uniform(tmem_slot);
     pdl_wait();  // the restored activation
 
     const int items = a.tiles * a.splits;
@@ -227,27 +227,25 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
             }
         }
     } else if (warp == 9) {
-        if (lane == 0) {
-            constexpr uint32_t idesc = tc::instr(Half<T>::is_bf16, TM, TN, true, true);
-            uint32_t n = 0, chain = 0;
-            for (int item = blockIdx.x; item < items; item += gridDim.x) {
-                const int2 st = steps_of(item);
-                for (int k = 0; k < st.y; ++chain) {
-                    const uint32_t buf = chain & 1;
-                    if (!patience.wait(sum_empty + 8 * buf, ((chain >> 1) & 1) ^ 1)) goto done;
+        constexpr uint32_t idesc = tc::instr(Half<T>::is_bf16, TM, TN, true, true);
+        uint32_t n = 0, chain = 0;
+        for (int item = blockIdx.x; item < items; item += gridDim.x) {
+            const int2 st = steps_of(item);
+            for (int k = 0; k < st.y; ++chain) {
+                const uint32_t buf = chain & 1;
+                if (!patience.wait_warp(sum_empty + 8 * buf, ((chain >> 1) & 1) ^ 1)) goto done;
+                tc::tc_fence_after();
+                for (int c = 0; c < CHAIN && k < st.y; ++c, ++k, ++n) {
+                    const uint32_t s = n % STAGES, from = base + s * STAGE;
+                    if (!patience.wait_warp(full + 8 * s, (n / STAGES) & 1)) goto done;
                     tc::tc_fence_after();
-                    for (int c = 0; c < CHAIN && k < st.y; ++c, ++k, ++n) {
-                        const uint32_t s = n % STAGES, from = base + s * STAGE;
-                        if (!patience.wait(full + 8 * s, (n / STAGES) & 1)) goto done;
-                        tc::tc_fence_after();
 #pragma unroll
-                        for (int kk = 0; kk < TK / 16; ++kk)
-                            tc::mma(tmem + buf * TN, tc::smem_desc(from + kk * 2048, BOX, 1024),
-                                    tc::smem_desc(from + TM / 64 * BOX + kk * 2048, BOX, 1024), idesc, c > 0 || kk > 0);
-                        tc::mma_commit(empty + 8 * s);
-                    }
-                    tc::mma_commit(sum_full + 8 * buf);
+                    for (int kk = 0; kk < TK / 16; ++kk)
+                        tc::mma(tmem + buf * TN, tc::smem_desc(from + kk * 2048, BOX, 1024),
+                                tc::smem_desc(from + TM / 64 * BOX + kk * 2048, BOX, 1024), idesc, c > 0 || kk > 0);
+                    tc::mma_commit(empty + 8 * s);
                 }
+                tc::mma_commit(sum_full + 8 * buf);
             }
         }
     } else {
