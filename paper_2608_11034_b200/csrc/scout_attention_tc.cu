@@ -63,35 +63,19 @@ __device__ __forceinline__ Slot slot_of(const TcForwardArgs &a, const Lengths &n
 
 template <typename T, int HD>
 __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constant__ TcForwardArgs a, const __grid_constant__ CUtensorMap map_q,
-                                                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v) {
+                                                            const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
+                                                            const __grid_constant__ CUtensorMap map_o) {
     using L = Layout<HD>;
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * L::STAGES + 11];
+    __shared__ uint64_t bars[2 * L::STAGES + 12];
     __shared__ uint32_t tmem_slot, dead;
     const Problem &p = a.p;
     const uint32_t base = (smem_u32(smem_raw) + 1023) & ~1023u, first_k = base + 2 * L::TILE, ring = first_k + L::TILE;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * L::STAGES, q_full = empty + 8 * L::STAGES, s_full = q_full + 8, p_full = s_full + 16,
+    const uint32_t full = smem_u32(bars), empty = full + 8 * L::STAGES, q_full = empty + 8 * L::STAGES, s_full = q_full + 16, p_full = s_full + 16,
                    o_done = p_full + 32, clean = o_done + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    if (threadIdx.x == 0) {
-        dead = 0;
-        for (int s = 0; s < L::STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        tc::bar_init(q_full, 1), tc::bar_init(clean, 1), tc::bar_init(clean + 8, 1);
-        for (int s = 0; s < 2; ++s) tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 16 * s, 4), tc::bar_init(p_full + 16 * s + 8, 4), tc::bar_init(o_done + 8 * s, 1);
-        tc::bar_init_done();
-    }
-    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
-    tc::tc_fence_before();
-    __syncthreads();
-    tc::tc_fence_after();
-    const uint32_t tmem = tc::uniform(tmem_slot);
-
-    int x = blockIdx.x;
-    const int hs = a.pair_heads ? p.q_heads / 2 : p.q_heads;
-    const int h = x % hs;
-    x /= hs;
-    const int b = x % p.batch, tile = a.tiles - 1 - x / p.batch;  // the longest rows of a causal problem first
+    const int h = blockIdx.x, b = blockIdx.y, tile = a.tiles - 1 - (int)blockIdx.z;  // the longest rows of a causal problem first
     const Lengths n = lengths(p, b);
     const Slot slots[2] = {slot_of(a, n, tile, h, 0), slot_of(a, n, tile, h, 1)};
     const int hk = slots[0].head / p.group;
@@ -100,18 +84,35 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     const int u1 = max(slots[0].blk1, slots[1].blk1);
     const int dirty = n.nk < p.kv_len && n.nk % KEYS ? n.nk / KEYS : -1;  // the block that a sequence ends inside of
 
+    const auto load = [&](uint32_t to, const CUtensorMap *m, uint32_t bar, int row, int head) {
+#pragma unroll
+        for (int c = 0; c < HD / 64; ++c) tc::tma_4d(to + c * L::SUB, m, bar, c * 64, row, head, b);
+    };
+    if (warp == 8 && lane == 0) {
+        dead = 0;
+        for (int s = 0; s < L::STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
+        tc::bar_init(q_full, 1), tc::bar_init(q_full + 8, 1), tc::bar_init(clean, 1), tc::bar_init(clean + 8, 1);
+        for (int s = 0; s < 2; ++s)
+            tc::bar_init(s_full + 8 * s, 1), tc::bar_init(p_full + 16 * s, 4), tc::bar_init(p_full + 16 * s + 8, 4), tc::bar_init(o_done + 8 * s, 1);
+        tc::bar_init_done();
+        if (u0 < u1) {  // on their way before the block is set up; the first product needs the first two
+            tc::bar_expect(q_full, 2 * L::TILE);
+            load(first_k, &map_k, q_full, u0 * KEYS, hk);
+            load(base, &map_q, q_full, slots[0].row0, slots[0].head);
+            tc::bar_expect(q_full + 8, L::TILE);
+            load(base + L::TILE, &map_q, q_full + 8, slots[1].row0, slots[1].head);
+        }
+    }
+    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = tc::uniform(tmem_slot);
+
     // launched with 384 x 168 registers, of which the softmax, which holds a row of 128 scores, gets 256 x 224
     if (warp == 8) {
         tc::registers_down<56>();
-        if (lane == 0 && u0 < u1) {
-            const auto load = [&](uint32_t to, const CUtensorMap *m, uint32_t bar, int row, int head) {
-#pragma unroll
-                for (int c = 0; c < HD / 64; ++c) tc::tma_4d(to + c * L::SUB, m, bar, c * 64, row, head, b);
-            };
-            tc::bar_expect(q_full, 3 * L::TILE);
-            load(base, &map_q, q_full, slots[0].row0, slots[0].head);
-            load(first_k, &map_k, q_full, u0 * KEYS, hk);
-            load(base + L::TILE, &map_q, q_full, slots[1].row0, slots[1].head);
+        if (lane == 0) {
             for (int u = u0; u < u1; ++u) {
                 const int st = (u - u0) % L::STAGES;
                 const bool next = u + 1 < u1;
@@ -137,8 +138,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                 tc::mma_commit(s_full + 8 * s);
             };
 #pragma unroll
-            for (int s = 0; s < 2; ++s)
+            for (int s = 0; s < 2; ++s) {
+                if (s && !patience.wait_warp(q_full + 8, 0)) break;
                 if (seen(s, u0)) product_s(s, dk);
+            }
             bool ok = true;
             int done[2] = {0, 0};
             for (int u = u0; ok && u < u1; ++u) {
@@ -217,7 +220,13 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
 #pragma unroll
                 for (int c = 0; c < 4; ++c)
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) r[c][e] = c * 32 + e >= first && c * 32 + e < end ? r[c][e] : 0xFF800000u;  // -inf
+                    for (int e = 0; e < 32; ++e) r[c][e] = c * 32 + e < end ? r[c][e] : 0xFF800000u;  // -inf
+                if (blk < sl.full0) {
+#pragma unroll
+                    for (int c = 0; c < 4; ++c)
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) r[c][e] = c * 32 + e >= first ? r[c][e] : 0xFF800000u;
+                }
             }
             float m4[4] = {-CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F, -CUDART_INF_F};
 #pragma unroll
@@ -274,35 +283,49 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             if (!sees) top = -CUDART_INF_F, sum = 0.f;
             const float inv = sum == 0.f ? 1.f : 1.f / sum;
             bool fine = finite(sum) && top != CUDART_INF_F;
-            T *dst = RowIO<T>::at(a.o, p.so, b, mine ? i : 0, sl.head);
+            // O leaves through the slot's Q tile, which the last product has read (32 rows of this warp, 64 elements wide each)
+            if (it == 0 && u0 < u1) ok = patience.wait_warp(q_full + 8 * s, 0);
+            const uint32_t out = base + s * L::TILE + (warp & 3) * 32 * 128;
+            const bool all_see = __all_sync(0xFFFFFFFFu, sees && it > 0);
+            const tc::F2 inv2 = tc::f2(inv, inv), zero2 = tc::f2(0.f, 0.f);
+            tc::F2 odd = zero2;  // stays 0 while every element is finite: 0 x is NaN otherwise
 #pragma unroll
             for (int c = 0; c < HD / 32; ++c) {
-                uint32_t r[32];
-                if (it > 0) {
-                    tc::tmem_load32(r, at_o + c * 32);
-                    tc::tmem_load_wait(r);
-                } else {
+                uint32_t r[32], w[16];
+                tc::tmem_load32(r, at_o + c * 32);
+                tc::tmem_load_wait(r);
+                if (!all_see) {
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) r[e] = 0;
+                    for (int e = 0; e < 32; ++e) r[e] = sees && it > 0 ? r[e] : 0u;
                 }
 #pragma unroll
-                for (int e = 0; e < 32; ++e) {
-                    r[e] = sees ? r[e] : 0u;
-                    fine = fine && finite(__uint_as_float(r[e]));
+                for (int e = 0; e < 16; ++e) {
+                    const tc::F2 x = tc::f2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
+                    odd = tc::fma2(x, zero2, odd);
+                    const float2 y = tc::split(tc::mul2(x, inv2));
+                    w[e] = Half<T>::pack(y.x, y.y);
                 }
 #pragma unroll
-                for (int e = 0; e < 32; e += 8) {
-                    uint4 w;
-                    w.x = Half<T>::pack(__uint_as_float(r[e]) * inv, __uint_as_float(r[e + 1]) * inv);
-                    w.y = Half<T>::pack(__uint_as_float(r[e + 2]) * inv, __uint_as_float(r[e + 3]) * inv);
-                    w.z = Half<T>::pack(__uint_as_float(r[e + 4]) * inv, __uint_as_float(r[e + 5]) * inv);
-                    w.w = Half<T>::pack(__uint_as_float(r[e + 6]) * inv, __uint_as_float(r[e + 7]) * inv);
-                    if (mine && c * 32 + e < p.head_dim) *reinterpret_cast<uint4 *>(dst + c * 32 + e) = w;
-                }
+                for (int e = 0; e < 16; e += 4)
+                    tc::store_shared16(tc::swizzled(out + (c >> 1) * L::SUB, lane, (c & 1) * 4 + e / 4), w[e], w[e + 1], w[e + 2], w[e + 3]);
+            }
+            fine = fine && tc::split(odd).x == 0.f && tc::split(odd).y == 0.f;
+            tc::fence_async();
+            __syncwarp();
+            if (lane == 0) {
+#pragma unroll
+                for (int c = 0; c < HD / 64; ++c)
+                    if (i < p.q_len && c * 64 < p.head_dim) tc::tma_store_4d(&map_o, out + c * L::SUB, c * 64, i, sl.head, b);
+                tc::tma_store_commit();
             }
             if (mine)
                 a.lse[((int64_t)b * p.q_heads + sl.head) * p.q_len + i] = top == -CUDART_INF_F ? -CUDART_INF_F : (top + log2f(sum)) * LN2;
             uint32_t redo = __ballot_sync(0xFFFFFFFFu, mine && !fine);
+            if (lane == 0) {
+                if (redo) tc::tma_stored();
+                else tc::tma_store_read();
+            }
+            __syncwarp();
             while (redo) {
                 const int r = __ffs(redo) - 1;
                 redo &= redo - 1;
@@ -318,15 +341,15 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-template <typename T, int HD> int run_forward(const Problem &p, void *o, float *lse, const CUtensorMap (&m)[3], cudaStream_t stream) {
+template <typename T, int HD> int run_forward(const Problem &p, void *o, float *lse, const CUtensorMap (&m)[4], cudaStream_t stream) {
     TcForwardArgs a = {p, o, lse, nullptr, 0, 0};
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     a.pair_heads = p.group % 2 == 0;
     const int rows = a.pair_heads ? ROWS : 2 * ROWS;
     a.tiles = (p.q_len + rows - 1) / rows;
-    const int64_t blocks = (int64_t)a.tiles * p.batch * (a.pair_heads ? p.q_heads / 2 : p.q_heads);
+    const dim3 blocks(a.pair_heads ? p.q_heads / 2 : p.q_heads, p.batch, a.tiles);
     if (int rc = allow_smem<forward_tc<T, HD>>(Layout<HD>::SMEM)) return rc;
-    forward_tc<T, HD><<<(unsigned)blocks, TC_THREADS, Layout<HD>::SMEM, stream>>>(a, m[0], m[1], m[2]);
+    forward_tc<T, HD><<<blocks, TC_THREADS, Layout<HD>::SMEM, stream>>>(a, m[0], m[1], m[2], m[3]);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
@@ -345,9 +368,9 @@ bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, con
 }
 
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken) {
-    CUtensorMap m[3];
-    *taken = tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
-             tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS);
+    CUtensorMap m[4];
+    *taken = p.batch < 65536 && p.q_len < 65536 * ROWS && tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
+             tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS) && tensor_view(&m[3], bf16, o, p.so, p, p.q_len, p.q_heads, 32);
     if (!*taken) return SCOUT_OK;
     if (p.head_dim > 64)
         return bf16 ? run_forward<__nv_bfloat16, 128>(p, o, lse, m, stream) : run_forward<__half, 128>(p, o, lse, m, stream);
