@@ -736,7 +736,7 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
     return SCOUT_OK;
 }
 
-template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, const CUtensorMap (*maps)[4], cudaStream_t stream) {
+template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, const BackwardViews *maps, cudaStream_t stream) {
     constexpr int smem_q = 6 * TILE * HD * 2, smem_k = 2 * TILE * HD * 2 + 4 * 32 * HD * 2;
     if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
     if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
@@ -835,8 +835,8 @@ extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const v
     b.stats = (float2 *)workspace;
     b.part = (float *)((uint8_t *)workspace + s.stats_bytes);
     const bool wide = a->head_dim > 64, bf16 = a->dtype == SCOUT_DT_BF16;
-    CUtensorMap views[4];
-    const CUtensorMap(*maps)[4] = worth_tensor(*a) && backward_views(b.p, bf16, views) ? &views : nullptr;
+    BackwardViews views;
+    const BackwardViews *maps = worth_tensor(*a) && backward_views(b.p, bf16, dq, dk, dv, &views) ? &views : nullptr;
     if (maps) s = shape(*a, true);
     const cudaStream_t st = (cudaStream_t)stream;
     if (bf16) return wide ? backward<__nv_bfloat16, 128>(s, b, maps, st) : backward<__nv_bfloat16, 64>(s, b, maps, st);

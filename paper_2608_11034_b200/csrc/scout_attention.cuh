@@ -254,11 +254,14 @@ __device__ __forceinline__ void row_dkv(const Problem &p, const float2 *stats, i
 bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box);
 // *taken is false where TMA cannot address a tensor and nothing was enqueued
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken);
-// views of q, k, v, d_o for the two calls below, which write the results or, with splits > 1, fp32 parts of them
-bool backward_views(const Problem &p, bool bf16, CUtensorMap (&m)[4]);
-int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const CUtensorMap (&m)[4], cudaStream_t stream);
-int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const CUtensorMap (&m)[4],
-               cudaStream_t stream);
+// The backward pass's views; false where TMA cannot address a tensor.  The two calls write the results or, with splits > 1,
+// fp32 parts of them.
+struct BackwardViews {
+    CUtensorMap q, k, v, d_o, dq, dk, dv;
+};
+bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v);
+int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const BackwardViews &v, cudaStream_t stream);
+int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const BackwardViews &v, cudaStream_t stream);
 
 }  // namespace attn
 }  // namespace scout

@@ -3,13 +3,12 @@
 //
 //   dkv_tc  owns 128 keys and runs over the 128-row query tiles that see them, all heads of the group:
 //               S^T = K Q^T    dP^T = V G^T    dV += P^T G    dK += dS^T Q
-//           Keys are the rows, so P^T and dS^T are left operands as they come out of the softmax; they replace S^T and dP^T in
-//           tensor memory (4 x 128 columns in all).
+//           Keys are the rows, so P^T and dS^T are left operands as they come out of the softmax.
 //   dq_tc   owns 128 rows of a head and runs over their keys:   S = Q K^T    dP = G V^T    dQ += dS K
 //
-// Eight warps make P = 2^(s' - lse') and dS = P (dP - delta), two warpgroups of 64 columns each, a thread per row; while
-// they work on one of the two, the tensor cores have the other: per tile [dV S][dK dP] against [P][dS], and
-// [S] [dQ dP] against [dS] [P].
+// Eight warps make P = 2^(s' - lse') and dS = P (dP - delta), two warpgroups of 64 columns each, a thread per row. They
+// take the scores into registers first, so that the next product of scores runs while they work.  dkv_tc has no
+// tensor memory left for P beside the scores (4 x 128 columns are S, dP, dV, dK), so its P goes through shared memory.
 //
 // One kernel that added dQ from blocks of keys would need 5 products instead of 4 + 3, but its sums would cross blocks:
 // float atomics give other bits on every run, and these gradients are compared bit by bit.
@@ -29,7 +28,8 @@ template <int HD> struct Layout {
     static constexpr int TILE = SUB * (HD / 64);
     static constexpr int DQ_STAGES = HD == 128 ? 5 : 8;  // of K or V tiles
     static constexpr int DKV_STAGES = HD == 128 ? 4 : 8; // of Q or G tiles
-    static constexpr int DQ_SMEM = (2 + DQ_STAGES) * TILE + 1024, DKV_SMEM = (2 + DKV_STAGES) * TILE + 1024;
+    static constexpr int DKV_SIDE = 3072;  // barriers and the rows' statistics; with HD = 128 the block's shared memory is full to the last byte
+    static constexpr int DQ_SMEM = (2 + DQ_STAGES) * TILE + 1024, DKV_SMEM = (2 + DKV_STAGES) * TILE + 2 * SUB + DKV_SIDE;
 };
 
 __device__ __forceinline__ void both_warpgroups() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -50,18 +50,28 @@ template <int HD> __device__ __forceinline__ void clear_rows(uint32_t tile, int 
 // D = A B^T of two tiles, both [128 rows][HD]
 template <typename T, int HD> __device__ __forceinline__ void product_tiles(uint32_t d, uint32_t x, uint32_t y) {
     constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, ROWS, false, false);
+    const uint64_t dx = tc::smem_desc(x, 16, 1024), dy = tc::smem_desc(y, 16, 1024);
 #pragma unroll
     for (int k = 0; k < HD / 16; ++k) {
         const uint32_t off = (k >> 2) * Layout<HD>::SUB + (k & 3) * 32;
-        tc::mma(d, tc::smem_desc(x + off, 16, 1024), tc::smem_desc(y + off, 16, 1024), id, k > 0);
+        tc::mma(d, tc::desc_at(dx, off), tc::desc_at(dy, off), id, k > 0);
     }
 }
 // D += W X: W [128 lanes][128 k] in 16 bits in tensor memory, the second 64 k at w + gap; X a tile [128 k][HD]
 template <typename T, int HD> __device__ __forceinline__ void product_sum(uint32_t d, uint32_t w, uint32_t gap, uint32_t x, bool add) {
     constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
+    const uint64_t dx = tc::smem_desc(x, Layout<HD>::SUB, 1024);
+#pragma unroll
+    for (int k = 0; k < ROWS / 16; ++k) tc::mma_ts(d, w + (k >> 2) * gap + (k & 3) * 8, tc::desc_at(dx, k * 2048), id, add || k > 0);
+}
+
+// D += W X: W [128 rows][128 k] in shared memory in two pieces of 64 k, X as above
+template <typename T, int HD> __device__ __forceinline__ void product_rows(uint32_t d, uint32_t w, uint32_t x, bool add) {
+    constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
+    const uint64_t dw = tc::smem_desc(w, 16, 1024), dx = tc::smem_desc(x, Layout<HD>::SUB, 1024);
 #pragma unroll
     for (int k = 0; k < ROWS / 16; ++k)
-        tc::mma_ts(d, w + (k >> 2) * gap + (k & 3) * 8, tc::smem_desc(x + k * 2048, Layout<HD>::SUB, 1024), id, add || k > 0);
+        tc::mma(d, tc::desc_at(dw, (k >> 2) * Layout<HD>::SUB + (k & 3) * 32), tc::desc_at(dx, k * 2048), id, add || k > 0);
 }
 
 struct TcBackwardArgs {
@@ -73,48 +83,55 @@ struct TcBackwardArgs {
     int tiles, splits;
 };
 
-// P of 64 columns from S at `at`, kept in w and stored in 16 bits at `to` (columns already read, or of their own).
-// minus(c): -lse' of column c.  first, end: the columns the row sees (not looked at with whole).
-template <typename T, bool STORE, typename F>
-__device__ __forceinline__ void make_p(float (&w)[64], uint32_t at, uint32_t to, float scale_log2, bool whole, int first, int end, F minus) {
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t r[32];
-        tc::tmem_load32(r, at + c * 32);
-        tc::tmem_load_wait(r);
-#pragma unroll
-        for (int e = 0; e < 32; ++e) w[c * 32 + e] = exp2_fast(fmaf(__uint_as_float(r[e]), scale_log2, minus(c * 32 + e)));
-        if (!whole) {
-#pragma unroll
-            for (int e = 0; e < 32; ++e) w[c * 32 + e] = c * 32 + e >= first && c * 32 + e < end ? w[c * 32 + e] : 0.f;
-        }
-        if constexpr (STORE) {
-            uint32_t x[16];
-#pragma unroll
-            for (int e = 0; e < 16; ++e) x[e] = Half<T>::pack(w[c * 32 + 2 * e], w[c * 32 + 2 * e + 1]);
-            tc::tmem_store16(to + c * 16, x);
-        }
-    }
+// 64 columns of this thread's row to registers
+__device__ __forceinline__ void take(uint32_t (&r)[2][32], uint32_t at) {
+    tc::tmem_load32(r[0], at);
+    tc::tmem_load32(r[1], at + 32);
+    tc::tmem_load_wait(r[0]);
+    tc::tmem_load_wait(r[1]);
 }
-// dS of the same columns, from dP at `at`
-template <typename T, typename F>
-__device__ __forceinline__ void make_ds(const float (&w)[64], uint32_t at, uint32_t to, bool whole, int first, int end, F delta) {
+// The columns of a row that are seen: those in [first, end), where a bound that no row of the tile meets is not looked at.
+struct Seen {
+    int first, end;
+    bool low, high;
+    __device__ __forceinline__ void hide(uint32_t (&r)[2][32]) const {  // hidden places become 0
+        if (high) {
 #pragma unroll
-    for (int c = 0; c < 2; ++c) {
-        uint32_t r[32], x[16];
-        tc::tmem_load32(r, at + c * 32);
-        tc::tmem_load_wait(r);
-        float d[32];
-#pragma unroll
-        for (int e = 0; e < 32; ++e) d[e] = w[c * 32 + e] * (__uint_as_float(r[e]) - delta(c * 32 + e));
-        if (!whole) {  // a hidden place's dP may be anything
-#pragma unroll
-            for (int e = 0; e < 32; ++e) d[e] = c * 32 + e >= first && c * 32 + e < end ? d[e] : 0.f;
+            for (int e = 0; e < 64; ++e) r[e >> 5][e & 31] = e < end ? r[e >> 5][e & 31] : 0u;
         }
+        if (low) {
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[e] = Half<T>::pack(d[2 * e], d[2 * e + 1]);
-        tc::tmem_store16(to + c * 16, x);
+            for (int e = 0; e < 64; ++e) r[e >> 5][e & 31] = e >= first ? r[e >> 5][e & 31] : 0u;
+        }
     }
+};
+// scores -> P; minus(c): -lse' of columns c, c + 1
+template <typename F> __device__ __forceinline__ void to_p(uint32_t (&r)[2][32], float scale_log2, const Seen &seen, F minus) {
+    const tc::F2 scale2 = tc::f2(scale_log2, scale_log2);
+#pragma unroll
+    for (int c = 0; c < 64; c += 2) {
+        uint32_t &lo = r[c >> 5][c & 31], &hi = r[c >> 5][(c & 31) + 1];
+        const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(lo), __uint_as_float(hi)), scale2, minus(c)));
+        lo = __float_as_uint(exp2_fast(y.x)), hi = __float_as_uint(exp2_fast(y.y));
+    }
+    seen.hide(r);
+}
+// dP -> dS = P (dP - delta); minus(c): -delta of columns c, c + 1.  A hidden place's dP may be anything.
+template <typename F> __device__ __forceinline__ void to_ds(uint32_t (&r)[2][32], const uint32_t (&w)[2][32], const Seen &seen, F minus) {
+#pragma unroll
+    for (int c = 0; c < 64; c += 2) {
+        uint32_t &lo = r[c >> 5][c & 31], &hi = r[c >> 5][(c & 31) + 1];
+        const tc::F2 d = tc::add2(tc::f2(__uint_as_float(lo), __uint_as_float(hi)), minus(c));
+        const float2 y = tc::split(tc::mul2(d, tc::f2(__uint_as_float(w[c >> 5][c & 31]), __uint_as_float(w[c >> 5][(c & 31) + 1]))));
+        lo = __float_as_uint(y.x), hi = __float_as_uint(y.y);
+    }
+    seen.hide(r);
+}
+// the 16-bit words of 64 columns
+template <typename T> __device__ __forceinline__ void round16(uint32_t (&x)[32], const uint32_t (&r)[2][32]) {
+#pragma unroll
+    for (int e = 0; e < 32; ++e)
+        x[e] = Half<T>::pack(__uint_as_float(r[e >> 4][2 * (e & 15)]), __uint_as_float(r[e >> 4][2 * (e & 15) + 1]));
 }
 __device__ __forceinline__ void stored(uint32_t bar, int lane) {
     tc::tmem_store_wait();
@@ -125,27 +142,40 @@ __device__ __forceinline__ void stored(uint32_t bar, int lane) {
 
 // COLS columns of this thread's row to registers (zeros where nothing was summed), and whether all are finite
 template <int COLS> __device__ __forceinline__ bool read_row(float (&x)[COLS], uint32_t at, bool any) {
-    bool fine = true;
+    const bool all = __all_sync(0xFFFFFFFFu, any);
+    const tc::F2 zero2 = tc::f2(0.f, 0.f);
+    tc::F2 odd = zero2;  // stays 0 while every element is finite: 0 x is NaN otherwise
 #pragma unroll
     for (int c = 0; c < COLS; c += 32) {
         uint32_t r[32];
         tc::tmem_load32(r, at + c);
         tc::tmem_load_wait(r);
+        if (!all) {
 #pragma unroll
-        for (int e = 0; e < 32; ++e) {
-            x[c + e] = any ? __uint_as_float(r[e]) : 0.f;
-            fine = fine && finite(x[c + e]);
+            for (int e = 0; e < 32; ++e) r[e] = any ? r[e] : 0u;
+        }
+#pragma unroll
+        for (int e = 0; e < 32; e += 2) {
+            x[c + e] = __uint_as_float(r[e]), x[c + e + 1] = __uint_as_float(r[e + 1]);
+            odd = tc::fma2(tc::f2(x[c + e], x[c + e + 1]), zero2, odd);
         }
     }
-    return fine;
+    const float2 o = tc::split(odd);
+    return o.x == 0.f && o.y == 0.f;
 }
-// columns [col, col + COLS) of a row of head_dim, times f
-template <typename T, int COLS> __device__ __forceinline__ void write_row(T *row, const float (&x)[COLS], int col, int head_dim, float f) {
+// The row, times f and in 16 bits, to columns [col, col + COLS) of row r of a tile in shared memory (64-element wide pieces).
+template <typename T, int COLS> __device__ __forceinline__ void stage_row(uint32_t tile, int r, const float (&x)[COLS], int col, float f) {
 #pragma unroll
     for (int e = 0; e < COLS; e += 8)
-        if (col + e < head_dim)
-            *reinterpret_cast<uint4 *>(row + col + e) = make_uint4(Half<T>::pack(x[e] * f, x[e + 1] * f), Half<T>::pack(x[e + 2] * f, x[e + 3] * f),
-                                                                   Half<T>::pack(x[e + 4] * f, x[e + 5] * f), Half<T>::pack(x[e + 6] * f, x[e + 7] * f));
+        tc::store_shared16(tc::swizzled(tile + ((col + e) >> 6) * (ROWS * 128), r, ((col + e) & 63) >> 3), Half<T>::pack(x[e] * f, x[e + 1] * f),
+                           Half<T>::pack(x[e + 2] * f, x[e + 3] * f), Half<T>::pack(x[e + 4] * f, x[e + 5] * f), Half<T>::pack(x[e + 6] * f, x[e + 7] * f));
+}
+// 32 rows of a staged tile to memory, from row r0 of the tile; one lane
+template <int HD> __device__ __forceinline__ void store_rows(const CUtensorMap *m, uint32_t tile, int r0, int row, int rows, int head_dim, int head, int b) {
+#pragma unroll
+    for (int c = 0; c < HD / 64; ++c)
+        if (row < rows && c * 64 < head_dim) tc::tma_store_4d(m, tile + c * (ROWS * 128) + r0 * 128, c * 64, row, head, b);
+    tc::tma_store_commit();
 }
 template <int COLS> __device__ __forceinline__ void write_part(float *row, const float (&x)[COLS], int col, int head_dim) {
 #pragma unroll
@@ -157,38 +187,19 @@ template <int COLS> __device__ __forceinline__ void write_part(float *row, const
 template <typename T, int HD>
 __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ TcBackwardArgs a, const __grid_constant__ CUtensorMap map_q,
                                                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                       const __grid_constant__ CUtensorMap map_g) {
+                                                       const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dq) {
     using L = Layout<HD>;
     constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 128, DQ = 256, DS = 384;  // tensor memory columns
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * STAGES + 6];
+    __shared__ uint64_t bars[2 * STAGES + 7];
     __shared__ uint32_t tmem_slot, dead, s_bad[2][4];
     const Problem &p = a.p;
     const uint32_t sq = (smem_u32(smem_raw) + 1023) & ~1023u, sg = sq + L::TILE, ring = sg + L::TILE;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 8, dp_full = s_full + 8,
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 8,
                    s_read = dp_full + 8, ds_full = s_read + 8, dq_done = ds_full + 8;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    if (threadIdx.x == 0) {
-        dead = 0;
-        for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        tc::bar_init(q_full, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(dq_done, 1);
-        tc::bar_init(s_read, 8), tc::bar_init(ds_full, 8);
-        tc::bar_init_done();
-    }
-    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
-    tc::tc_fence_before();
-    __syncthreads();
-    tc::tc_fence_after();
-    const uint32_t tmem = tc::uniform(tmem_slot);
-    pdl_wait();  // the statistics
-
-    int x = blockIdx.x;
-    const int split = x % a.splits;
-    x /= a.splits;
-    const int head = x % p.q_heads;
-    x /= p.q_heads;
-    const int b = x % p.batch, row0 = (a.tiles - 1 - x / p.batch) * ROWS;
+    const int head = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits, row0 = (a.tiles - 1 - (int)blockIdx.z / a.splits) * ROWS;
     const Lengths n = lengths(p, b);
     const int hk = head / p.group, last = min(row0 + ROWS, n.nq) - 1;
     int blk0 = 0, blk1 = 0, full0 = 0, full1 = 0;
@@ -201,12 +212,30 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
     }
     const int steps = max(blk1 - blk0, 0);
 
-    if (warp == 8) {
-        if (lane == 0 && steps) {
-            tc::bar_expect(q_full, 2 * L::TILE);
+    if (warp == 8 && lane == 0) {
+        dead = 0;
+        for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
+        tc::bar_init(q_full, 1), tc::bar_init(q_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(dq_done, 1);
+        tc::bar_init(s_read, 8), tc::bar_init(ds_full, 8);
+        tc::bar_init_done();
+        if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
+            tc::bar_expect(q_full, L::TILE);
             load_tile<HD>(sq, &map_q, q_full, row0, head, b);
-            load_tile<HD>(sg, &map_g, q_full, row0, head, b);
-            for (int r = 0; r < 2 * steps; ++r) {
+            tc::bar_expect(full, L::TILE);
+            load_tile<HD>(ring, &map_k, full, blk0 * ROWS, hk, b);
+            tc::bar_expect(q_full + 8, L::TILE);
+            load_tile<HD>(sg, &map_g, q_full + 8, row0, head, b);
+        }
+    }
+    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = tc::uniform(tmem_slot);
+
+    if (warp == 8) {
+        if (lane == 0) {
+            for (int r = 1; r < 2 * steps; ++r) {
                 const int st = r % STAGES;
                 if (!patience.wait(empty + 8 * st, ((r / STAGES) & 1) ^ 1)) break;
                 tc::bar_expect(full + 8 * st, L::TILE);
@@ -229,7 +258,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         };
         bool ok = steps > 0 && patience.wait_warp(q_full, 0) && landed(0);
         if (ok) issue_s(0);
-        ok = ok && landed(1);
+        ok = ok && patience.wait_warp(q_full + 8, 0) && landed(1);
         if (ok) issue_dp(0);
         for (int j = 0; ok && j < steps; ++j) {
             const bool next = j + 1 < steps;
@@ -255,24 +284,31 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         const bool mine = i < p.q_len;
         const int lo = row_lo(p, n, i), hi = row_hi(p, n, i);
         const uint32_t quarter = tmem + ((uint32_t)((warp & 3) * 32) << 16);
+        pdl_wait();  // the statistics
         const float2 st = mine ? a.stats[((int64_t)b * p.q_heads + head) * p.q_len + i] : make_float2(CUDART_INF_F, 0.f);
+        const tc::F2 lse2 = tc::f2(-st.x, -st.x), delta2 = tc::f2(-st.y, -st.y);
         bool ok = true;
         for (int j = 0; j < steps; ++j) {
-            const int blk = blk0 + j, first = lo - blk * ROWS - wg * 64, end = hi - blk * ROWS - wg * 64;
-            const bool whole = blk >= full0 && blk < full1;
+            const int blk = blk0 + j, c0 = blk * ROWS + wg * 64;
+            const Seen seen = {lo - c0, hi - c0, blk < full0, blk >= full1};
             ok = patience.wait_warp(s_full, j & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            float w[64];
-            make_p<T, false>(w, quarter + S + wg * 64, 0, p.scale_log2, whole, first, end, [&](int) { return -st.x; });
+            uint32_t w[2][32], r[2][32], x[32];
+            take(w, quarter + S + wg * 64);
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::bar_arrive(s_read);
+            to_p(w, p.scale_log2, seen, [&](int) { return lse2; });
             // dP of this step was issued after dQ of the step before: dS's columns are free by then
             ok = patience.wait_warp(dp_full, j & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            make_ds<T>(w, quarter + DP + wg * 64, quarter + DS + wg * 32, whole, first, end, [&](int) { return st.y; });
+            take(r, quarter + DP + wg * 64);
+            to_ds(r, w, seen, [&](int) { return delta2; });
+            round16<T>(x, r);
+            tc::tmem_store16(quarter + DS + wg * 32, x);
+            tc::tmem_store16(quarter + DS + wg * 32 + 16, x + 16);
             stored(ds_full, lane);
         }
         if (ok && steps) ok = patience.wait_warp(dq_done, 0);
@@ -285,12 +321,23 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
                 const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
                 if (mine) write_part<COLS>(a.part + (split * rows + ((int64_t)b * p.q_heads + head) * p.q_len + i) * p.head_dim, g, wg * COLS, p.head_dim);
             } else {
+                // through Q's tile, which the last product has read
+                stage_row<T, COLS>(sq, (warp & 3) * 32 + lane, g, wg * COLS, p.scale);
+                tc::fence_async();
                 const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
                 if (lane == 0) s_bad[wg][warp & 3] = bad;
                 both_warpgroups();
                 uint32_t redo = s_bad[0][warp & 3] | s_bad[1][warp & 3];
-                if (mine && !((redo >> lane) & 1)) write_row<T, COLS>(RowIO<T>::at(a.dq, p.sq, b, i, head), g, wg * COLS, p.head_dim, p.scale);
-                for (; wg == 0 && redo; redo &= redo - 1) row_dq<T>(p, a.stats, b, head, row0 + (warp & 3) * 32 + __ffs(redo) - 1, a.dq);
+                if (wg == 0) {
+                    const int r0 = (warp & 3) * 32;
+                    if (lane == 0) {
+                        store_rows<HD>(&map_dq, sq, r0, row0 + r0, p.q_len, p.head_dim, head, b);
+                        if (redo) tc::tma_stored();
+                        else tc::tma_store_read();
+                    }
+                    __syncwarp();
+                    for (; redo; redo &= redo - 1) row_dq<T>(p, a.stats, b, head, row0 + r0 + __ffs(redo) - 1, a.dq);
+                }
             }
         } else if (a.splits == 1) {
             both_warpgroups();
@@ -308,40 +355,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
 template <typename T, int HD>
 __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ TcBackwardArgs a, const __grid_constant__ CUtensorMap map_q,
                                                         const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                        const __grid_constant__ CUtensorMap map_g) {
+                                                        const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dk,
+                                                        const __grid_constant__ CUtensorMap map_dv) {
     using L = Layout<HD>;
     constexpr int STAGES = L::DKV_STAGES, S = 0, DP = 128, DV = 256, DK = 256 + HD;  // tensor memory columns
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * STAGES + 10];
-    __shared__ uint32_t tmem_slot, dead, s_bad[2][4];
-    __shared__ __align__(16) float s_lse[2][ROWS], s_delta[2][ROWS];  // -lse', delta of a step's rows
+    struct Side {
+        float lse[2][ROWS], delta[2][ROWS];  // -lse', -delta of a step's rows
+        uint64_t bars[2 * STAGES + 12];
+        uint32_t tmem_slot, dead, bad[2][4];
+    };
+    static_assert(sizeof(Side) <= L::DKV_SIDE, "");
+    extern __shared__ __align__(1024) uint8_t smem_tiles[];  // nothing static beside it: it starts on a swizzle's boundary
+    Side &side = *reinterpret_cast<Side *>(smem_tiles + L::DKV_SMEM - L::DKV_SIDE);
+    uint64_t *const bars = side.bars;
+    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
+    float (&s_lse)[2][ROWS] = side.lse, (&s_delta)[2][ROWS] = side.delta;
     const Problem &p = a.p;
-    const uint32_t sk = (smem_u32(smem_raw) + 1023) & ~1023u, sv = sk + L::TILE, ring = sv + L::TILE;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 8, dp_full = s_full + 8,
-                   p_full = dp_full + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
+    const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, sp = sv + L::TILE, ring = sp + 2 * L::SUB;  // K, V, P, pairs (Q, G)
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 16, dp_full = s_full + 8,
+                   s_read = dp_full + 8, p_full = s_read + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    if (threadIdx.x == 0) {
-        dead = 0;
-        for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        tc::bar_init(k_full, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(all_done, 1);
-        tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
-        for (int s = 0; s < 2; ++s) tc::bar_init(st_full + 8 * s, 1), tc::bar_init(st_empty + 8 * s, 8);
-        tc::bar_init_done();
-    }
-    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
-    tc::tc_fence_before();
-    __syncthreads();
-    tc::tc_fence_after();
-    const uint32_t tmem = tc::uniform(tmem_slot);
-    pdl_wait();  // the statistics, and the parts that dQ's join has read
-
-    int x = blockIdx.x;
-    const int split = x % a.splits;
-    x /= a.splits;
-    const int hk = x % p.kv_heads;
-    x /= p.kv_heads;
-    const int b = x % p.batch, j0 = x / p.batch * ROWS;  // causal: the first keys are seen by the most rows
+    // causal: the first keys are seen by the most rows
+    const int hk = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits, j0 = (int)blockIdx.z / a.splits * ROWS;
     const Lengths n = lengths(p, b);
     const int j1 = min(j0 + ROWS, n.nk);
     int qt0 = 0, tiles = 0, full0 = 0, full1 = 0;
@@ -356,12 +392,32 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     const auto tile_of = [&](int s) { return qt0 + (step0 + s) % tiles; };
     const auto head_of = [&](int s) { return hk * p.group + (step0 + s) / tiles; };
 
-    if (warp == 8) {
-        if (lane == 0 && steps) {
-            tc::bar_expect(k_full, 2 * L::TILE);
+    if (warp == 8 && lane == 0) {
+        dead = 0;
+        for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
+        tc::bar_init(k_full, 1), tc::bar_init(k_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(all_done, 1);
+        tc::bar_init(s_read, 8), tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
+        for (int s = 0; s < 2; ++s) tc::bar_init(st_full + 8 * s, 1), tc::bar_init(st_empty + 8 * s, 8);
+        tc::bar_init_done();
+        if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
+            tc::bar_expect(k_full, L::TILE);
             load_tile<HD>(sk, &map_k, k_full, j0, hk, b);
-            load_tile<HD>(sv, &map_v, k_full, j0, hk, b);
-            for (int r = 0; r < 2 * steps; ++r) {
+            tc::bar_expect(full, L::TILE);
+            load_tile<HD>(ring, &map_q, full, tile_of(0) * ROWS, head_of(0), b);
+            tc::bar_expect(k_full + 8, L::TILE);
+            load_tile<HD>(sv, &map_v, k_full + 8, j0, hk, b);
+        }
+    }
+    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
+    tc::tc_fence_before();
+    __syncthreads();
+    tc::tc_fence_after();
+    const uint32_t tmem = tc::uniform(tmem_slot);
+    pdl_wait();  // the statistics, and the parts that dQ's join has read
+
+    if (warp == 8) {
+        if (lane == 0) {
+            for (int r = 1; r < 2 * steps; ++r) {
                 const int st = r % STAGES;
                 if (!patience.wait(empty + 8 * st, ((r / STAGES) & 1) ^ 1)) break;
                 tc::bar_expect(full + 8 * st, L::TILE);
@@ -387,20 +443,20 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         };
         bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0);
         if (ok) issue_s(0);
-        ok = ok && landed(1);
+        ok = ok && patience.wait_warp(k_full + 8, 0) && landed(1);
         if (ok) issue_dp(0);
         for (int s = 0; ok && s < steps; ++s) {
             const bool next = s + 1 < steps;
-            ok = patience.wait_warp(p_full, s & 1);
-            if (!ok) break;
-            tc::tc_fence_after();
-            product_sum<T, HD>(tmem + DV, tmem + S, 64, stage(2 * s + 1), s > 0);
-            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));
             if (next) {
-                ok = landed(2 * s + 2);
+                ok = landed(2 * s + 2) && patience.wait_warp(s_read, s & 1);
                 if (!ok) break;
+                tc::tc_fence_after();
                 issue_s(s + 1);
             }
+            ok = patience.wait_warp(p_full, s & 1);
+            if (!ok) break;
+            product_rows<T, HD>(tmem + DV, sp, stage(2 * s + 1), s > 0);
+            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));  // also: P's tile is free
             ok = patience.wait_warp(ds_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
@@ -421,7 +477,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             for (int c = 0; c < 4; ++c) v[c] = row0 + lane + 32 * c < p.q_len ? src[row0 + lane + 32 * c] : make_float2(CUDART_INF_F, 0.f);
             if (!patience.wait_warp(st_empty + 8 * st, ((s >> 1) & 1) ^ 1)) break;
 #pragma unroll
-            for (int c = 0; c < 4; ++c) s_lse[st][lane + 32 * c] = -v[c].x, s_delta[st][lane + 32 * c] = v[c].y;
+            for (int c = 0; c < 4; ++c) s_lse[st][lane + 32 * c] = -v[c].x, s_delta[st][lane + 32 * c] = -v[c].y;
             __syncwarp();
             if (lane == 0) tc::bar_arrive(st_full + 8 * st);
         }
@@ -432,19 +488,45 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         const uint32_t quarter = tmem + ((uint32_t)((warp & 3) * 32) << 16);
         bool ok = true;
         for (int s = 0; s < steps; ++s) {
-            const int st = s & 1, qt = tile_of(s), first = lo - qt * ROWS - wg * 64, end = hi - qt * ROWS - wg * 64;
-            const bool whole = qt >= full0 && qt < full1;
-            ok = patience.wait_warp(st_full + 8 * st, (s >> 1) & 1) && patience.wait_warp(s_full, s & 1);
+            const int st = s & 1, qt = tile_of(s), c0 = qt * ROWS + wg * 64;
+            const Seen seen = {lo - c0, hi - c0, qt < full0, qt >= full1};
+            ok = patience.wait_warp(s_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            float w[64];
-            make_p<T, true>(w, quarter + S + wg * 64, quarter + S + wg * 64, p.scale_log2, whole, first, end,
-                            [&](int c) { return s_lse[st][wg * 64 + c]; });
-            stored(p_full, lane);
+            uint32_t w[2][32], r[2][32], x[32];
+            take(w, quarter + S + wg * 64);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(s_read);
+            ok = patience.wait_warp(st_full + 8 * st, (s >> 1) & 1);
+            if (!ok) break;
+            const auto pairs = [&](const float *v) {
+                return [=](int c) {
+                    const float2 y = *reinterpret_cast<const float2 *>(v + c);
+                    return tc::f2(y.x, y.y);
+                };
+            };
+            to_p(w, p.scale_log2, seen, pairs(s_lse[st] + wg * 64));
+            round16<T>(x, w);
+            if (s > 0) {  // the product that read P's tile a step ago
+                const int was = 2 * s - 1;
+                ok = patience.wait_warp(empty + 8 * (was % STAGES), (was / STAGES) & 1);
+                if (!ok) break;
+            }
+#pragma unroll
+            for (int c = 0; c < 8; ++c)
+                tc::store_shared16(tc::swizzled(sp + wg * L::SUB, (warp & 3) * 32 + lane, c), x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
+            tc::fence_async();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(p_full);
             ok = patience.wait_warp(dp_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            make_ds<T>(w, quarter + DP + wg * 64, quarter + DP + wg * 64, whole, first, end, [&](int c) { return s_delta[st][wg * 64 + c]; });
+            take(r, quarter + DP + wg * 64);
+            to_ds(r, w, seen, pairs(s_delta[st] + wg * 64));
+            round16<T>(x, r);
+            tc::tmem_store16(quarter + DP + wg * 64, x);  // over columns that have been read
+            tc::tmem_store16(quarter + DP + wg * 64 + 16, x + 16);
             stored(ds_full, lane);
             if (lane == 0) tc::bar_arrive(st_empty + 8 * st);
         }
@@ -459,15 +541,27 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
                     write_part<HD>(a.part + ((2 * split + (wg ? 0 : 1)) * keys + ((int64_t)b * p.kv_heads + hk) * p.kv_len + j) * p.head_dim, g, 0,
                                    p.head_dim);
             } else {
+                // through the tiles of V and K, which the last products have read
+                const int r0 = (warp & 3) * 32;
+                const uint32_t tile = wg ? sk : sv;
+                stage_row<T, HD>(tile, r0 + lane, g, 0, wg ? p.scale : 1.f);
+                tc::fence_async();
                 const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
                 if (lane == 0) s_bad[wg][warp & 3] = bad;
                 both_warpgroups();
-                uint32_t redo = s_bad[0][warp & 3] | s_bad[1][warp & 3];
-                if (mine && !((redo >> lane) & 1)) {
-                    if (wg) write_row<T, HD>(RowIO<T>::at(a.dk, p.sk, b, j, hk), g, 0, p.head_dim, p.scale);
-                    else write_row<T, HD>(RowIO<T>::at(a.dv, p.sv, b, j, hk), g, 0, p.head_dim, 1.f);
+                uint32_t any = 0;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) any |= s_bad[c >> 2][c & 3];
+                if (lane == 0) {
+                    store_rows<HD>(wg ? &map_dk : &map_dv, tile, r0, j0 + r0, p.kv_len, p.head_dim, hk, b);
+                    if (any) tc::tma_stored();
+                    else tc::tma_store_read();
                 }
-                for (; wg == 0 && redo; redo &= redo - 1) row_dkv<T>(p, a.stats, b, hk, j0 + (warp & 3) * 32 + __ffs(redo) - 1, a.dk, a.dv);
+                if (any) {
+                    both_warpgroups();
+                    uint32_t redo = s_bad[0][warp & 3] | s_bad[1][warp & 3];
+                    for (; wg == 0 && redo; redo &= redo - 1) row_dkv<T>(p, a.stats, b, hk, j0 + r0 + __ffs(redo) - 1, a.dk, a.dv);
+                }
             }
         } else if (a.splits == 1) {
             both_warpgroups();
@@ -481,9 +575,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-template <typename K> cudaError_t launch(K kernel, int64_t grid, int smem, cudaStream_t stream, const TcBackwardArgs &a, const CUtensorMap (&m)[4]) {
+template <typename K, typename... M> cudaError_t launch(K kernel, dim3 grid, int smem, cudaStream_t stream, const TcBackwardArgs &a, const M &...maps) {
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)grid);
+    cfg.gridDim = grid;
     cfg.blockDim = dim3(TC_THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
@@ -492,40 +586,43 @@ template <typename K> cudaError_t launch(K kernel, int64_t grid, int smem, cudaS
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, m[0], m[1], m[2], m[3]);
+    return cudaLaunchKernelEx(&cfg, kernel, a, maps...);
 }
 
-template <typename T, int HD> int run_dq(TcBackwardArgs &a, const CUtensorMap (&m)[4], cudaStream_t stream) {
+template <typename T, int HD> int run_dq(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
     if (int rc = allow_smem<dq_tc<T, HD>>(Layout<HD>::DQ_SMEM)) return rc;
     a.tiles = (a.p.q_len + ROWS - 1) / ROWS;
-    SCOUT_CUDA(launch(dq_tc<T, HD>, (int64_t)a.tiles * a.p.batch * a.p.q_heads * a.splits, Layout<HD>::DQ_SMEM, stream, a, m));
+    SCOUT_CUDA(launch(dq_tc<T, HD>, dim3(a.p.q_heads, a.p.batch, a.tiles * a.splits), Layout<HD>::DQ_SMEM, stream, a, v.q, v.k, v.v, v.d_o, v.dq));
     return SCOUT_OK;
 }
-template <typename T, int HD> int run_dkv(TcBackwardArgs &a, const CUtensorMap (&m)[4], cudaStream_t stream) {
+template <typename T, int HD> int run_dkv(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
     if (int rc = allow_smem<dkv_tc<T, HD>>(Layout<HD>::DKV_SMEM)) return rc;
     a.tiles = (a.p.kv_len + ROWS - 1) / ROWS;
-    SCOUT_CUDA(launch(dkv_tc<T, HD>, (int64_t)a.tiles * a.p.batch * a.p.kv_heads * a.splits, Layout<HD>::DKV_SMEM, stream, a, m));
+    SCOUT_CUDA(launch(dkv_tc<T, HD>, dim3(a.p.kv_heads, a.p.batch, a.tiles * a.splits), Layout<HD>::DKV_SMEM, stream, a, v.q, v.k, v.v, v.d_o, v.dk, v.dv));
     return SCOUT_OK;
 }
 
 }  // namespace
 
-bool backward_views(const Problem &p, bool bf16, CUtensorMap (&m)[4]) {
-    return tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, ROWS) &&
-           tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, ROWS) && tensor_view(&m[3], bf16, p.d_o, p.sg, p, p.q_len, p.q_heads, ROWS);
+bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v) {
+    // the grid's second and third axes (tiles are split only where there are fewer than 148)
+    if (p.batch > 65535 || p.q_len > 65535 * ROWS || p.kv_len > 65535 * ROWS) return false;
+    return tensor_view(&v->q, bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&v->k, bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, ROWS) &&
+           tensor_view(&v->v, bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, ROWS) && tensor_view(&v->d_o, bf16, p.d_o, p.sg, p, p.q_len, p.q_heads, ROWS) &&
+           tensor_view(&v->dq, bf16, dq, p.sq, p, p.q_len, p.q_heads, 32) && tensor_view(&v->dk, bf16, dk, p.sk, p, p.kv_len, p.kv_heads, 32) &&
+           tensor_view(&v->dv, bf16, dv, p.sv, p, p.kv_len, p.kv_heads, 32);
 }
-int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const CUtensorMap (&m)[4], cudaStream_t stream) {
+int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const BackwardViews &v, cudaStream_t stream) {
     TcBackwardArgs a = {p, stats, dq, nullptr, nullptr, part, nullptr, 0, splits};
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-    if (p.head_dim > 64) return bf16 ? run_dq<__nv_bfloat16, 128>(a, m, stream) : run_dq<__half, 128>(a, m, stream);
-    return bf16 ? run_dq<__nv_bfloat16, 64>(a, m, stream) : run_dq<__half, 64>(a, m, stream);
+    if (p.head_dim > 64) return bf16 ? run_dq<__nv_bfloat16, 128>(a, v, stream) : run_dq<__half, 128>(a, v, stream);
+    return bf16 ? run_dq<__nv_bfloat16, 64>(a, v, stream) : run_dq<__half, 64>(a, v, stream);
 }
-int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const CUtensorMap (&m)[4],
-               cudaStream_t stream) {
+int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const BackwardViews &v, cudaStream_t stream) {
     TcBackwardArgs a = {p, stats, nullptr, dk, dv, part, nullptr, 0, splits};
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-    if (p.head_dim > 64) return bf16 ? run_dkv<__nv_bfloat16, 128>(a, m, stream) : run_dkv<__half, 128>(a, m, stream);
-    return bf16 ? run_dkv<__nv_bfloat16, 64>(a, m, stream) : run_dkv<__half, 64>(a, m, stream);
+    if (p.head_dim > 64) return bf16 ? run_dkv<__nv_bfloat16, 128>(a, v, stream) : run_dkv<__half, 128>(a, v, stream);
+    return bf16 ? run_dkv<__nv_bfloat16, 64>(a, v, stream) : run_dkv<__half, 64>(a, v, stream);
 }
 
 }  // namespace attn
