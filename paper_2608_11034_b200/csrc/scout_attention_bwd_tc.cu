@@ -189,14 +189,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
                                                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
                                                        const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dq) {
     using L = Layout<HD>;
-    constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 128, DQ = 256, DS = 384;  // tensor memory columns
+    constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 256, DQ = 384;  // tensor memory columns: two tiles of scores, dP (then dS), dQ
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * STAGES + 7];
+    __shared__ uint64_t bars[2 * STAGES + 6];
     __shared__ uint32_t tmem_slot, dead, s_bad[2][4];
     const Problem &p = a.p;
     const uint32_t sq = (smem_u32(smem_raw) + 1023) & ~1023u, sg = sq + L::TILE, ring = sg + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 8,
-                   s_read = dp_full + 8, ds_full = s_read + 8, dq_done = ds_full + 8;
+                   ds_full = dp_full + 8, dq_done = ds_full + 8;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     const int head = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits, row0 = (a.tiles - 1 - (int)blockIdx.z / a.splits) * ROWS;
@@ -216,7 +216,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
         tc::bar_init(q_full, 1), tc::bar_init(q_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(dq_done, 1);
-        tc::bar_init(s_read, 8), tc::bar_init(ds_full, 8);
+        tc::bar_init(ds_full, 8);
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
             tc::bar_expect(q_full, L::TILE);
@@ -248,7 +248,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         const auto issue_s = [&](int j) {
             // keys past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dQ
             if (n.nk < p.kv_len && (blk0 + j + 1) * ROWS > n.nk) clear_rows<HD>(stage(2 * j), max(n.nk - (blk0 + j) * ROWS, 0), lane);
-            product_tiles<T, HD>(tmem + S, sq, stage(2 * j));
+            product_tiles<T, HD>(tmem + S + (j & 1) * ROWS, sq, stage(2 * j));
             tc::mma_commit(s_full);
         };
         const auto issue_dp = [&](int j) {
@@ -260,23 +260,24 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         if (ok) issue_s(0);
         ok = ok && patience.wait_warp(q_full + 8, 0) && landed(1);
         if (ok) issue_dp(0);
+        if (ok && steps > 1) {
+            ok = landed(2);
+            if (ok) issue_s(1);
+        }
         for (int j = 0; ok && j < steps; ++j) {
-            const bool next = j + 1 < steps;
-            if (next) {
-                ok = landed(2 * j + 2) && patience.wait_warp(s_read, j & 1);
-                if (!ok) break;
-                tc::tc_fence_after();
-                issue_s(j + 1);
-            }
-            ok = patience.wait_warp(ds_full, j & 1);
+            ok = patience.wait_warp(ds_full, j & 1);  // also: these scores have been taken
             if (!ok) break;
             tc::tc_fence_after();
-            product_sum<T, HD>(tmem + DQ, tmem + DS, 32, stage(2 * j), j > 0);
+            product_sum<T, HD>(tmem + DQ, tmem + DP, 64, stage(2 * j), j > 0);
             tc::mma_commit(empty + 8 * ((2 * j) % STAGES));
-            if (!next) tc::mma_commit(dq_done);
-            if (next) {
+            if (j + 1 == steps) tc::mma_commit(dq_done);
+            if (j + 1 < steps) {
                 ok = landed(2 * j + 3);
                 if (ok) issue_dp(j + 1);
+            }
+            if (ok && j + 2 < steps) {
+                ok = landed(2 * j + 4);
+                if (ok) issue_s(j + 2);
             }
         }
     } else if (warp < 8) {
@@ -295,20 +296,16 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
             if (!ok) break;
             tc::tc_fence_after();
             uint32_t w[2][32], r[2][32], x[32];
-            take(w, quarter + S + wg * 64);
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(s_read);
+            take(w, quarter + S + (j & 1) * ROWS + wg * 64);
             to_p(w, p.scale_log2, seen, [&](int) { return lse2; });
-            // dP of this step was issued after dQ of the step before: dS's columns are free by then
             ok = patience.wait_warp(dp_full, j & 1);
             if (!ok) break;
             tc::tc_fence_after();
             take(r, quarter + DP + wg * 64);
             to_ds(r, w, seen, [&](int) { return delta2; });
             round16<T>(x, r);
-            tc::tmem_store16(quarter + DS + wg * 32, x);
-            tc::tmem_store16(quarter + DS + wg * 32 + 16, x + 16);
+            tc::tmem_store16(quarter + DP + wg * 64, x);  // over columns that have been read
+            tc::tmem_store16(quarter + DP + wg * 64 + 16, x + 16);
             stored(ds_full, lane);
         }
         if (ok && steps) ok = patience.wait_warp(dq_done, 0);
@@ -361,7 +358,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     constexpr int STAGES = L::DKV_STAGES, S = 0, DP = 128, DV = 256, DK = 256 + HD;  // tensor memory columns
     struct Side {
         float lse[2][ROWS], delta[2][ROWS];  // -lse', -delta of a step's rows
-        uint64_t bars[2 * STAGES + 12];
+        uint64_t bars[2 * STAGES + 11];
         uint32_t tmem_slot, dead, bad[2][4];
     };
     static_assert(sizeof(Side) <= L::DKV_SIDE, "");
@@ -373,7 +370,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     const Problem &p = a.p;
     const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, sp = sv + L::TILE, ring = sp + 2 * L::SUB;  // K, V, P, pairs (Q, G)
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 16, dp_full = s_full + 8,
-                   s_read = dp_full + 8, p_full = s_read + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
+                   p_full = dp_full + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     // causal: the first keys are seen by the most rows
@@ -389,6 +386,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         }
     }
     const int all = tiles * p.group, per = (all + a.splits - 1) / a.splits, step0 = split * per, steps = max(min(all, step0 + per) - step0, 0);
+    // Where Q (g = 0) and G (1) of a step land: PAIRS pairs of slots in turn.  A pair's slots change roles every time: G is done with
+    // first (dV before dK), and its slot takes the Q that is needed first.
+    constexpr int PAIRS = STAGES / 2;
+    const auto slot = [&](int s, int g) { return s % PAIRS * 2 + (g ^ (s / PAIRS & 1)); };
+    const auto turn = [&](int s) { return (uint32_t)(s / PAIRS & 1); };
     const auto tile_of = [&](int s) { return qt0 + (step0 + s) % tiles; };
     const auto head_of = [&](int s) { return hk * p.group + (step0 + s) / tiles; };
 
@@ -396,7 +398,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
         tc::bar_init(k_full, 1), tc::bar_init(k_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(all_done, 1);
-        tc::bar_init(s_read, 8), tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
+        tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
         for (int s = 0; s < 2; ++s) tc::bar_init(st_full + 8 * s, 1), tc::bar_init(st_empty + 8 * s, 8);
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
@@ -418,53 +420,49 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     if (warp == 8) {
         if (lane == 0) {
             for (int r = 1; r < 2 * steps; ++r) {
-                const int st = r % STAGES;
-                if (!patience.wait(empty + 8 * st, ((r / STAGES) & 1) ^ 1)) break;
-                tc::bar_expect(full + 8 * st, L::TILE);
-                load_tile<HD>(ring + st * L::TILE, r & 1 ? &map_g : &map_q, full + 8 * st, tile_of(r >> 1) * ROWS, head_of(r >> 1), b);
+                const int s = r >> 1, g = r & 1, at = slot(s, g);
+                if (!patience.wait(empty + 8 * at, turn(s) ^ 1)) break;
+                tc::bar_expect(full + 8 * at, L::TILE);
+                load_tile<HD>(ring + at * L::TILE, g ? &map_g : &map_q, full + 8 * at, tile_of(s) * ROWS, head_of(s), b);
             }
         }
     } else if (warp == 9) {
-        const auto stage = [&](int r) { return ring + (r % STAGES) * L::TILE; };
-        const auto landed = [&](int r) {
-            if (!patience.wait_warp(full + 8 * (r % STAGES), (r / STAGES) & 1)) return false;
+        const auto stage = [&](int s, int g) { return ring + slot(s, g) * L::TILE; };
+        const auto landed = [&](int s, int g) {
+            if (!patience.wait_warp(full + 8 * slot(s, g), turn(s))) return false;
             // rows past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dK and dV
-            const int row0 = tile_of(r >> 1) * ROWS;
-            if (n.nq < p.q_len && row0 + ROWS > n.nq) clear_rows<HD>(stage(r), max(n.nq - row0, 0), lane);
+            const int row0 = tile_of(s) * ROWS;
+            if (n.nq < p.q_len && row0 + ROWS > n.nq) clear_rows<HD>(stage(s, g), max(n.nq - row0, 0), lane);
             return true;
         };
         const auto issue_s = [&](int s) {
-            product_tiles<T, HD>(tmem + S, sk, stage(2 * s));
+            product_tiles<T, HD>(tmem + S, sk, stage(s, 0));
             tc::mma_commit(s_full);
         };
         const auto issue_dp = [&](int s) {
-            product_tiles<T, HD>(tmem + DP, sv, stage(2 * s + 1));
+            product_tiles<T, HD>(tmem + DP, sv, stage(s, 1));
             tc::mma_commit(dp_full);
         };
-        bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0);
+        bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0, 0);
         if (ok) issue_s(0);
-        ok = ok && patience.wait_warp(k_full + 8, 0) && landed(1);
+        ok = ok && patience.wait_warp(k_full + 8, 0) && landed(0, 1);
         if (ok) issue_dp(0);
         for (int s = 0; ok && s < steps; ++s) {
             const bool next = s + 1 < steps;
-            if (next) {
-                ok = landed(2 * s + 2) && patience.wait_warp(s_read, s & 1);
-                if (!ok) break;
-                tc::tc_fence_after();
-                issue_s(s + 1);
-            }
-            ok = patience.wait_warp(p_full, s & 1);
+            ok = (!next || landed(s + 1, 0)) && patience.wait_warp(p_full, s & 1);  // also: the scores have been taken
             if (!ok) break;
-            product_rows<T, HD>(tmem + DV, sp, stage(2 * s + 1), s > 0);
-            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));  // also: P's tile is free
+            tc::tc_fence_after();
+            if (next) issue_s(s + 1);
+            product_rows<T, HD>(tmem + DV, sp, stage(s, 1), s > 0);
+            tc::mma_commit(empty + 8 * slot(s, 1));  // also: P's tile is free
             ok = patience.wait_warp(ds_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            product_sum<T, HD>(tmem + DK, tmem + DP, 64, stage(2 * s), s > 0);
-            tc::mma_commit(empty + 8 * ((2 * s) % STAGES));
+            product_sum<T, HD>(tmem + DK, tmem + DP, 64, stage(s, 0), s > 0);
+            tc::mma_commit(empty + 8 * slot(s, 0));
             if (!next) tc::mma_commit(all_done);
             if (next) {
-                ok = landed(2 * s + 3);
+                ok = landed(s + 1, 1);
                 if (ok) issue_dp(s + 1);
             }
         }
@@ -495,9 +493,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             tc::tc_fence_after();
             uint32_t w[2][32], r[2][32], x[32];
             take(w, quarter + S + wg * 64);
-            tc::tc_fence_before();
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(s_read);
             ok = patience.wait_warp(st_full + 8 * st, (s >> 1) & 1);
             if (!ok) break;
             const auto pairs = [&](const float *v) {
@@ -509,14 +504,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             to_p(w, p.scale_log2, seen, pairs(s_lse[st] + wg * 64));
             round16<T>(x, w);
             if (s > 0) {  // the product that read P's tile a step ago
-                const int was = 2 * s - 1;
-                ok = patience.wait_warp(empty + 8 * (was % STAGES), (was / STAGES) & 1);
+                ok = patience.wait_warp(empty + 8 * slot(s - 1, 1), turn(s - 1));
                 if (!ok) break;
             }
 #pragma unroll
             for (int c = 0; c < 8; ++c)
                 tc::store_shared16(tc::swizzled(sp + wg * L::SUB, (warp & 3) * 32 + lane, c), x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
             tc::fence_async();
+            tc::tc_fence_before();  // the scores' loads
             __syncwarp();
             if (lane == 0) tc::bar_arrive(p_full);
             ok = patience.wait_warp(dp_full, s & 1);
