@@ -237,6 +237,172 @@ __global__ void __launch_bounds__(THREADS) forward_tiles(const __grid_constant__
     }
 }
 
+// O and LSE of a row from its maximum, sum and weighted values, four elements a lane
+template <typename T>
+__device__ __forceinline__ void finish_row(const ForwardArgs &a, int b, int hq, int i, float top, float sum, float (&acc)[4]) {
+    const Problem &p = a.p;
+    const int lane = threadIdx.x & 31;
+    bool fine = finite(sum) && top != CUDART_INF_F;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
+    if (!__all_sync(0xFFFFFFFFu, fine)) {
+        row_forward<T>(p, b, hq, i, a.o, a.lse);
+        return;
+    }
+    const float inv = sum == 0.f ? 1.f : 1.f / sum;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) acc[c] *= inv;
+    RowIO<T>::store(RowIO<T>::at(a.o, p.so, b, i, hq), acc, p.head_dim, lane);
+    if (lane == 0) a.lse[((int64_t)b * p.q_heads + hq) * p.q_len + i] = top == -CUDART_INF_F ? -CUDART_INF_F : (top + log2f(sum)) * LN2;
+}
+
+// At most 16 packed rows (a token or a few, with the group's heads): every warp of a block has all the rows and a share of the
+// keys, 16 at a time through a ring of its own, and the warps' results are merged in shared memory.  What bounds it is the
+// pass over the keys: 4 warps x FEW_STAGES x 8 KiB are in flight for a block (HD = 128).
+constexpr int FEW_KEYS = 16, FEW_STAGES = 3;
+template <int HD> constexpr int few_smem() { return 4 * FEW_STAGES * 2 * FEW_KEYS * HD * 2; }
+template <typename T, int HD>
+__global__ void __launch_bounds__(THREADS) forward_few(const __grid_constant__ ForwardArgs a) {
+    extern __shared__ __align__(1024) uint8_t smem[];
+    __shared__ float s_top[4][16], s_sum[4][16];
+    pdl_launch_dependents();
+    const Problem &p = a.p;
+    int x = blockIdx.x;
+    const int split = x % a.splits;
+    x /= a.splits;
+    const int hk = x % p.kv_heads, b = x / p.kv_heads;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const Lengths n = lengths(p, b);
+    const RowMap rm{p.group, hk * p.group};
+    const int m1 = p.group * p.q_len;
+    int lo, hi;
+    tile_keys(p, n, rm, 0, m1, lo, hi);
+    // whole blocks of 64 keys to a part, 16 of each to a warp
+    int blk0 = lo / 64, blk1 = hi > lo ? (hi + 63) / 64 : blk0;
+    const int per = (blk1 - blk0 + a.splits - 1) / a.splits;
+    blk0 += split * per;
+    blk1 = min(blk1, blk0 + per);
+    constexpr int BYTES = FEW_KEYS * HD * 2, CH = HD / 8;
+    const uint32_t ring = smem_u32(smem) + warp * FEW_STAGES * 2 * BYTES;
+    const uint16_t *kp = reinterpret_cast<const uint16_t *>(p.k) + b * p.sk.b + hk * p.sk.h, *vp = reinterpret_cast<const uint16_t *>(p.v) + b * p.sv.b + hk * p.sv.h;
+    const auto load = [&](int blk, int st) {  // this warp's 16 keys
+        const int j0 = blk * 64 + warp * FEW_KEYS;
+#pragma unroll
+        for (int c = 0; c < FEW_KEYS * CH / 32; ++c) {
+            const int r = (c * 32 + lane) / CH, ch = (c * 32 + lane) % CH, j = j0 + r;
+            const bool ok = j < n.nk && ch * 8 < p.head_dim;
+            copy16(ring + st * 2 * BYTES + at16<HD>(r, ch), ok ? kp + j * p.sk.t + ch * 8 : kp, ok);
+            copy16(ring + st * 2 * BYTES + BYTES + at16<HD>(r, ch), ok ? vp + j * p.sv.t + ch * 8 : vp, ok);
+        }
+    };
+#pragma unroll
+    for (int s = 0; s < FEW_STAGES - 1; ++s) {
+        if (blk0 + s < blk1) load(blk0 + s, s);
+        copy_commit();
+    }
+    // Q in matrix-instruction layout, straight from memory; rows past the end are zeros
+    uint32_t fq[HD / 16][4];
+    int rlo[2], rhi[2];
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        const int m = (lane >> 2) + 8 * r;
+        const bool ok = m < m1;
+        rlo[r] = ok ? row_lo(p, n, rm.token(m)) : 0;
+        rhi[r] = ok ? row_hi(p, n, rm.token(m)) : 0;
+        const uint16_t *q = reinterpret_cast<const uint16_t *>(p.q) + b * p.sq.b + (ok ? rm.token(m) * p.sq.t + rm.head(m) * p.sq.h : 0);
+#pragma unroll
+        for (int c = 0; c < HD / 16; ++c)
+#pragma unroll
+            for (int e = 0; e < 2; ++e) {
+                const int d = c * 16 + e * 8 + (lane & 3) * 2;
+                fq[c][r + 2 * e] = ok && d < p.head_dim ? *reinterpret_cast<const uint32_t *>(q + d) : 0u;
+            }
+    }
+    float acc[HD / 8][4] = {}, top[2] = {-CUDART_INF_F, -CUDART_INF_F}, sum[2] = {0.f, 0.f};
+    for (int blk = blk0, it = 0; blk < blk1; ++blk, ++it) {
+        if (blk + FEW_STAGES - 1 < blk1) load(blk + FEW_STAGES - 1, (it + FEW_STAGES - 1) % FEW_STAGES);
+        copy_commit();
+        copy_wait<FEW_STAGES - 1>();
+        __syncwarp();
+        const uint32_t sk = ring + it % FEW_STAGES * 2 * BYTES, sv = sk + BYTES;
+        float s[2][4] = {};
+#pragma unroll
+        for (int kk = 0; kk < HD / 16; ++kk) {
+            uint32_t fb[4];
+            ldsm(fb, sk + at16<HD>((lane & 7) + ((lane >> 4) << 3), kk * 2 + ((lane >> 3) & 1)));
+            mma16816<T>(s[0], fq[kk], fb[0], fb[1]);
+            mma16816<T>(s[1], fq[kk], fb[2], fb[3]);
+        }
+        float up[2] = {top[0], top[1]};
+#pragma unroll
+        for (int c = 0; c < 2; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int j = blk * 64 + warp * FEW_KEYS + c * 8 + (lane & 3) * 2 + (e & 1);
+                s[c][e] = j >= rlo[e >> 1] && j < rhi[e >> 1] ? s[c][e] * p.scale_log2 : -CUDART_INF_F;
+                up[e >> 1] = fmaxf(up[e >> 1], s[c][e]);
+            }
+#pragma unroll
+        for (int r = 0; r < 2; ++r) {
+            up[r] = fmaxf(up[r], __shfl_xor_sync(0xFFFFFFFFu, up[r], 1));
+            up[r] = fmaxf(up[r], __shfl_xor_sync(0xFFFFFFFFu, up[r], 2));
+            const float base = up[r] == -CUDART_INF_F ? 0.f : up[r];
+            const float fade = exp2_fast(top[r] - base);
+            top[r] = up[r];
+            sum[r] *= fade;
+#pragma unroll
+            for (int c = 0; c < HD / 8; ++c) acc[c][2 * r] *= fade, acc[c][2 * r + 1] *= fade;
+#pragma unroll
+            for (int c = 0; c < 2; ++c)
+#pragma unroll
+                for (int e = 2 * r; e < 2 * r + 2; ++e) {
+                    s[c][e] = exp2_fast(s[c][e] - base);
+                    sum[r] += s[c][e];
+                }
+        }
+        product_nn<T, HD, 2>(acc, s, sv);
+        __syncwarp();  // the slot is free for the copies issued next
+    }
+    copy_wait<0>();
+    __syncthreads();
+    // merge: the rings are free, each warp puts its O (16 x HD) there
+    float *all = reinterpret_cast<float *>(smem);
+#pragma unroll
+    for (int r = 0; r < 2; ++r) {
+        sum[r] += __shfl_xor_sync(0xFFFFFFFFu, sum[r], 1);
+        sum[r] += __shfl_xor_sync(0xFFFFFFFFu, sum[r], 2);
+        const int m = (lane >> 2) + 8 * r;
+        if ((lane & 3) == 0) s_top[warp][m] = top[r], s_sum[warp][m] = sum[r];
+#pragma unroll
+        for (int c = 0; c < HD / 8; ++c)
+            *reinterpret_cast<float2 *>(all + (warp * 16 + m) * HD + c * 8 + (lane & 3) * 2) = make_float2(acc[c][2 * r], acc[c][2 * r + 1]);
+    }
+    __syncthreads();
+    for (int m = warp; m < m1; m += 4) {
+        float t = -CUDART_INF_F, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) t = fmaxf(t, s_top[w][m]);
+        const float base = t == -CUDART_INF_F ? 0.f : t;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const float f = exp2f(s_top[w][m] - base);
+            l = fmaf(s_sum[w][m], f, l);
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) o[c] = fmaf(all[(w * 16 + m) * HD + lane + 32 * c], f, o[c]);
+        }
+        const int64_t row = ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m);
+        if (a.splits > 1) {
+            const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c)
+                if (lane + 32 * c < p.head_dim) a.part_o[(split * rows + row) * p.head_dim + lane + 32 * c] = o[c];
+            if (lane == 0) a.part_ml[split * rows + row] = make_float2(t, l);
+        } else {
+            finish_row<T>(a, b, rm.head(m), rm.token(m), t, l, o);
+        }
+    }
+}
+
 // One warp joins a row's parts in order.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) forward_join(const __grid_constant__ ForwardArgs a) {
@@ -248,12 +414,14 @@ __global__ void __launch_bounds__(THREADS) forward_join(const __grid_constant__ 
     const int lane = threadIdx.x & 31, d = p.head_dim;
     const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
     float top = -CUDART_INF_F;
+#pragma unroll 8
     for (int s = 0; s < a.splits; ++s) {
         const float m = a.part_ml[s * rows + row].x;
         top = fmaxf(top, m);
     }
     const float base = top == -CUDART_INF_F ? 0.f : top;
     float sum = 0.f, acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s) {
         const float2 ml = a.part_ml[s * rows + row];
         const float w = exp2f(ml.x - base);
@@ -262,18 +430,7 @@ __global__ void __launch_bounds__(THREADS) forward_join(const __grid_constant__ 
         for (int c = 0; c < 4; ++c)
             if (lane + 32 * c < d) acc[c] = fmaf(a.part_o[(s * rows + row) * d + lane + 32 * c], w, acc[c]);
     }
-    bool fine = finite(sum) && top != CUDART_INF_F;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
-    if (!__all_sync(0xFFFFFFFFu, fine)) {
-        row_forward<T>(p, b, hq, i, a.o, a.lse);
-        return;
-    }
-    const float inv = sum == 0.f ? 1.f : 1.f / sum;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] *= inv;
-    RowIO<T>::store(RowIO<T>::at(a.o, p.so, b, i, hq), acc, d, lane);
-    if (lane == 0) a.lse[row] = top == -CUDART_INF_F ? -CUDART_INF_F : (base + log2f(sum)) * LN2;
+    finish_row<T>(a, b, hq, i, top, sum, acc);
 }
 
 // ---- backward ----------------------------------------------------------------------------------------
@@ -286,28 +443,55 @@ struct BackwardArgs {
     int tiles, splits;
 };
 
-// One warp per row: delta = g . o, and the row statistic on powers of two.  A row that sees nothing gets +inf:
-// its probabilities come out 0.
+// delta = g . o, and the row statistic on powers of two.  A row that sees nothing gets +inf: its probabilities come out 0.
+// One pass over o and g, 16 bytes a lane, half a warp to a row, four rows of a half warp in flight.
+constexpr int STAT_ROWS = 4 * THREADS / 16;
 template <typename T>
 __global__ void __launch_bounds__(THREADS) backward_stats(const __grid_constant__ BackwardArgs a) {
     const Problem &p = a.p;
-    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
-    const int64_t x = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
     pdl_launch_dependents();
-    if (x >= rows) return;
-    const int lane = threadIdx.x & 31;
-    const int hq = x % p.q_heads, i = x / p.q_heads % p.q_len, b = x / p.q_heads / p.q_len;  // heads adjacent in memory
-    const Lengths n = lengths(p, b);
-    const int64_t row = ((int64_t)b * p.q_heads + hq) * p.q_len + i;
-    float2 st = make_float2(CUDART_INF_F, 0.f);
-    if (row_hi(p, n, i) > row_lo(p, n, i)) {
-        const float l = a.lse[row];
-        float o[4], g[4];
-        RowIO<T>::load(o, RowIO<T>::at(p.o, p.so, b, i, hq), p.head_dim, lane);
-        RowIO<T>::load(g, RowIO<T>::at(p.d_o, p.sg, b, i, hq), p.head_dim, lane);
-        st = make_float2(l == -CUDART_INF_F ? CUDART_INF_F : l * LOG2E, warp_dot(o, g, p.head_dim, lane));
+    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
+    const int lane = threadIdx.x & 15, d = lane * 8;
+    float4 o[4], g[4];
+    int64_t at[4];
+    bool ok[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const int64_t x = (int64_t)blockIdx.x * STAT_ROWS + u * (THREADS / 16) + (threadIdx.x >> 4);  // heads adjacent in memory
+        int hq, i, b;
+        if (rows <= 0x7FFFFFFF) {
+            const uint32_t y = (uint32_t)x, t = y / (uint32_t)p.q_heads;
+            hq = y - t * p.q_heads, b = t / (uint32_t)p.q_len, i = t - b * p.q_len;
+        } else {
+            hq = x % p.q_heads, i = x / p.q_heads % p.q_len, b = (int)(x / p.q_heads / p.q_len);
+        }
+        at[u] = x < rows ? ((int64_t)b * p.q_heads + hq) * p.q_len + i : -1;
+        ok[u] = false;
+        o[u] = g[u] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (x >= rows) continue;
+        const Lengths n = lengths(p, b);
+        ok[u] = row_hi(p, n, i) > row_lo(p, n, i);
+        if (ok[u] && d < p.head_dim) {
+            o[u] = *reinterpret_cast<const float4 *>(RowIO<T>::at(p.o, p.so, b, i, hq) + d);
+            g[u] = *reinterpret_cast<const float4 *>(RowIO<T>::at(p.d_o, p.sg, b, i, hq) + d);
+        }
     }
-    if (lane == 0) a.stats[row] = st;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        const uint32_t *x = reinterpret_cast<const uint32_t *>(&o[u]), *y = reinterpret_cast<const uint32_t *>(&g[u]);
+        float dot = 0.f;
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+            const float2 v = Half<T>::unpack(x[c]), w = Half<T>::unpack(y[c]);
+            dot = fmaf(v.x, w.x, fmaf(v.y, w.y, dot));
+        }
+#pragma unroll
+        for (int m = 8; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
+        if (lane == 0 && at[u] >= 0) {
+            const float l = ok[u] ? a.lse[at[u]] : -CUDART_INF_F;
+            a.stats[at[u]] = l == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(l * LOG2E, dot);
+        }
+    }
 }
 
 // P and dS of a tile in accumulator layout.  s, dp: 16 rows x 8 NT columns
@@ -451,6 +635,7 @@ __global__ void __launch_bounds__(THREADS) join_dq(const __grid_constant__ Backw
     const int lane = threadIdx.x & 31, d = p.head_dim;
     const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
     float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -607,6 +792,7 @@ __global__ void __launch_bounds__(THREADS) join_dkv(const __grid_constant__ Back
     const int lane = threadIdx.x & 31, d = p.head_dim;
     const int j = row % p.kv_len, hk = row / p.kv_len % p.kv_heads, b = row / p.kv_len / p.kv_heads;
     float ak[4] = {0.f, 0.f, 0.f, 0.f}, av[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
     for (int s = 0; s < a.splits; ++s)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
@@ -682,6 +868,7 @@ int parts(uint64_t blocks, uint64_t along, uint64_t want, uint64_t least) {
 struct Shape {
     uint64_t rows, keys, q_tiles, k_tiles;
     int f_splits, q_splits, k_splits;
+    bool few;
     uint64_t forward_bytes, stats_bytes, backward_bytes;
 };
 // tensor: the backward pass runs on tcgen05 (tiles of 128, one block an SM)
@@ -693,13 +880,15 @@ Shape shape(const scout_attn_t &a, bool tensor) {
     s.q_tiles = (group * a.q_len + TILE - 1) / TILE;
     s.k_tiles = (a.kv_len + TILE - 1) / TILE;
     const uint64_t seen = a.window ? std::min<uint64_t>(a.kv_len, (uint64_t)a.window + TILE) : a.kv_len;
-    s.f_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
+    // few rows: about four blocks to an SM, of which two run at a time, evens out sequences of different lengths
+    s.few = group * a.q_len <= 16;
+    s.f_splits = s.few ? parts(bh, (seen + TILE - 1) / TILE, 4 * 148, 2) : parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
     const uint64_t seen_by = a.window ? std::min<uint64_t>(a.q_len, (uint64_t)a.window + TILE) : a.q_len;
     if (tensor) {
         s.q_splits = parts((a.q_len + 127) / 128 * bh * group, (seen + 127) / 128, 148, 3);
         s.k_splits = parts((a.kv_len + 127) / 128 * bh, group * ((seen_by + 127) / 128), 148, 3);
     } else {
-        s.q_splits = s.f_splits;
+        s.q_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
         s.k_splits = parts(s.k_tiles * bh, (group * seen_by + 31) / 32, 2 * 148, 8);
     }
     s.forward_bytes = s.f_splits > 1 ? up256(s.f_splits * s.rows * a.head_dim * 4) + up256(s.f_splits * s.rows * 8) : 0;
@@ -727,11 +916,17 @@ cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t s
 }
 
 template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaStream_t stream) {
-    constexpr int smem = 5 * TILE * HD * 2;
-    if (int rc = allow_smem<forward_tiles<T, HD>>(smem)) return rc;
     f.tiles = (int)s.q_tiles;
     f.splits = s.f_splits;
-    SCOUT_CUDA(launch(forward_tiles<T, HD>, s.q_tiles * f.p.batch * f.p.kv_heads * f.splits, smem, stream, f, false));
+    const uint64_t blocks = s.q_tiles * f.p.batch * f.p.kv_heads * f.splits;
+    if (s.few) {
+        if (int rc = allow_smem<forward_few<T, HD>>(few_smem<HD>())) return rc;
+        SCOUT_CUDA(launch(forward_few<T, HD>, blocks, few_smem<HD>(), stream, f, false));
+    } else {
+        constexpr int smem = 5 * TILE * HD * 2;
+        if (int rc = allow_smem<forward_tiles<T, HD>>(smem)) return rc;
+        SCOUT_CUDA(launch(forward_tiles<T, HD>, blocks, smem, stream, f, false));
+    }
     if (f.splits > 1) SCOUT_CUDA(launch(forward_join<T>, (s.rows + 3) / 4, 0, stream, f, true));
     return SCOUT_OK;
 }
@@ -741,7 +936,7 @@ template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cons
     if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
     if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
     const uint64_t bh = (uint64_t)a.p.batch * a.p.kv_heads;
-    if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + 3) / 4, 0, stream, a, false));
+    if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + STAT_ROWS - 1) / STAT_ROWS, 0, stream, a, false));
     // every kernel that follows waits for the whole of the one before it (griddepcontrol.wait), so the
     // statistics are there for all of them and the shared parts are free
     if (s.rows) {

@@ -191,11 +191,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
     using L = Layout<HD>;
     constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 256, DQ = 384;  // tensor memory columns: two tiles of scores, dP (then dS), dQ
     extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * STAGES + 6];
+    __shared__ uint64_t bars[2 * STAGES + 7];
     __shared__ uint32_t tmem_slot, dead, s_bad[2][4];
     const Problem &p = a.p;
     const uint32_t sq = (smem_u32(smem_raw) + 1023) & ~1023u, sg = sq + L::TILE, ring = sg + L::TILE;
-    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 8,
+    const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 16,
                    ds_full = dp_full + 8, dq_done = ds_full + 8;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
@@ -215,7 +215,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
     if (warp == 8 && lane == 0) {
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        tc::bar_init(q_full, 1), tc::bar_init(q_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(dq_done, 1);
+        tc::bar_init(q_full, 1), tc::bar_init(q_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(s_full + 8, 1), tc::bar_init(dp_full, 1), tc::bar_init(dq_done, 1);
         tc::bar_init(ds_full, 8);
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
@@ -249,7 +249,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
             // keys past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dQ
             if (n.nk < p.kv_len && (blk0 + j + 1) * ROWS > n.nk) clear_rows<HD>(stage(2 * j), max(n.nk - (blk0 + j) * ROWS, 0), lane);
             product_tiles<T, HD>(tmem + S + (j & 1) * ROWS, sq, stage(2 * j));
-            tc::mma_commit(s_full);
+            tc::mma_commit(s_full + 8 * (j & 1));  // a barrier to a tile: one of them may be two products ahead of its readers
         };
         const auto issue_dp = [&](int j) {
             product_tiles<T, HD>(tmem + DP, sg, stage(2 * j + 1));
@@ -292,7 +292,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         for (int j = 0; j < steps; ++j) {
             const int blk = blk0 + j, c0 = blk * ROWS + wg * 64;
             const Seen seen = {lo - c0, hi - c0, blk < full0, blk >= full1};
-            ok = patience.wait_warp(s_full, j & 1);
+            ok = patience.wait_warp(s_full + 8 * (j & 1), (j >> 1) & 1);
             if (!ok) break;
             tc::tc_fence_after();
             uint32_t w[2][32], r[2][32], x[32];

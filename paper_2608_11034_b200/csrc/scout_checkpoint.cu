@@ -40,15 +40,16 @@ __device__ __forceinline__ int step_of(uint32_t amax_bits) {
     return amax_bits == 0 ? -126 : max(x - 6, -126);
 }
 
-// The code's byte.  x 2^-e + 1.5 2^23 in one fused operation rounds to an integer once, ties to even, and leaves it in the low
-// bits (|x 2^-e| <= 127 by the choice of e); the conversion instruction runs at a quarter of the rate.
-template <typename T> __device__ __forceinline__ uint32_t code_of(float x, int e) {
-    constexpr float MAGIC = 12582912.f;
-    // 2^-e lies between 2^126 (finite) and 2^-122 (normal)
-    const float c = fmaf(x, __uint_as_float((uint32_t)(127 - e) << 23), MAGIC);
-    const float top = e == TOP_STEP<T> ? 63.f : 127.f;
-    const uint32_t byte = __float_as_uint(fminf(fmaxf(c, MAGIC - top), MAGIC + top)) & 0xFFu;
-    return is_finite_bits(__float_as_uint(x) & 0x7FFFFFFFu) ? byte : 0x80u;
+// Where 2^-e lies: between 2^126 (finite) and 2^-122 (normal).
+__device__ __forceinline__ float inverse_step(int e) { return __uint_as_float((uint32_t)(127 - e) << 23); }
+// x 2^-e + 1.5 2^23 in one fused operation rounds to an integer once, ties to even, and leaves it in the low byte (the
+// conversion instruction runs at a quarter of the rate); |x 2^-e| <= 127 by the choice of e.
+constexpr float MAGIC = 12582912.f;
+__device__ __forceinline__ uint32_t code_of(float x, float inverse) { return __float_as_uint(fmaf(x, inverse, MAGIC)); }
+// the same in the type's topmost binade, and where the block holds non-finite elements
+template <typename T> __device__ __forceinline__ uint32_t code_careful(float x, int e) {
+    const float top = e == TOP_STEP<T> ? 63.f : 127.f, c = fmaf(x, inverse_step(e), MAGIC);
+    return is_finite_bits(__float_as_uint(x) & 0x7FFFFFFFu) ? __float_as_uint(fminf(fmaxf(c, MAGIC - top), MAGIC + top)) : 0x80u;
 }
 
 // n / d for n < 2^31: one high product and a shift, with the constants of the divisor made on the host
@@ -97,6 +98,22 @@ template <typename T> struct Eight {
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i] = make_uint4(0, 0, 0, 0);
     }
+    // the largest magnitude, as bits of a float (magnitudes order as their bits do; NaN and Inf come out largest)
+    __device__ __forceinline__ uint32_t top() const {
+        const uint32_t *v = reinterpret_cast<const uint32_t *>(w);
+        if constexpr (sizeof(T) == 4) {
+            uint32_t m = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) m = max(m, v[i] & 0x7FFFFFFFu);
+            return m;
+        } else {
+            uint32_t m = v[0] & 0x7FFF7FFFu;
+#pragma unroll
+            for (int i = 1; i < 4; ++i) m = __vmaxu2(m, v[i] & 0x7FFF7FFFu);
+            const uint16_t h = (uint16_t)max(m & 0xFFFFu, m >> 16);
+            return __float_as_uint(up<T>(*reinterpret_cast<const T *>(&h)));
+        }
+    }
     __device__ __forceinline__ float get(int i) const { return up<T>(reinterpret_cast<const T *>(w)[i]); }
     __device__ __forceinline__ void set(int i, float x) { reinterpret_cast<T *>(w)[i] = down<T>(x); }
     __device__ __forceinline__ void store(T *p) const {
@@ -118,21 +135,37 @@ template <typename T> __global__ void __launch_bounds__(THREADS) pack_vectors(co
 #pragma unroll
     for (int u = 0; u < UNROLL; ++u) {
         const Place p = place(a, g0 + u);
-        uint32_t top = 0;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const uint32_t bits = __float_as_uint(x[u].get(i)) & 0x7FFFFFFFu;
-            top = max(top, is_finite_bits(bits) ? bits : 0u);
-        }
+        // ordinary blocks take no look at single elements: NaN and Inf show in the largest magnitude
+        uint32_t top = x[u].top();
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
         top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-        const int e = step_of(top);
-        uint32_t c[2] = {0, 0};
+        int e = step_of(top);
+        uint32_t c[8];
+        if (e < TOP_STEP<T>) {
+            const float inverse = inverse_step(e);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) c[i >> 2] |= code_of<T>(x[u].get(i), e) << (8 * (i & 3));
+            for (int i = 0; i < 8; ++i) c[i] = code_of(x[u].get(i), inverse);
+        } else {  // the same way for the four lanes of a block
+            top = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const uint32_t bits = __float_as_uint(x[u].get(i)) & 0x7FFFFFFFu;
+                top = max(top, is_finite_bits(bits) ? bits : 0u);
+            }
+            const uint32_t four = 0xFu << (lane & 28);
+            top = max(top, __shfl_xor_sync(four, top, 1));
+            top = max(top, __shfl_xor_sync(four, top, 2));
+            e = step_of(top);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) c[i] = code_careful<T>(x[u].get(i), e);
+        }
+        uint32_t w[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+            w[i] = __byte_perm(__byte_perm(c[4 * i], c[4 * i + 1], 0x0040), __byte_perm(c[4 * i + 2], c[4 * i + 3], 0x0040), 0x5410);
         const int64_t col = p.col + lane * 8;
         if (p.ok && col < a.cols) {
-            __stcs(reinterpret_cast<uint2 *>(a.codes + p.row * a.code_stride + col), make_uint2(c[0], c[1]));
+            __stcs(reinterpret_cast<uint2 *>(a.codes + p.row * a.code_stride + col), make_uint2(w[0], w[1]));
             if ((lane & 3) == 0) a.exps[p.row * a.blocks + (col >> 5)] = (int8_t)e;
         }
     }
@@ -186,8 +219,15 @@ template <typename T> __global__ void __launch_bounds__(THREADS) pack_elements(c
 #pragma unroll
     for (int u = 0; u < BLOCKS; ++u) {
         const uint32_t bits = __float_as_uint(x[u]) & 0x7FFFFFFFu;
-        const int e = step_of(__reduce_max_sync(0xFFFFFFFFu, is_finite_bits(bits) ? bits : 0u));
-        if (32 * u < left) dst[32 * u] = (int8_t)code_of<T>(x[u], e);
+        int e = step_of(__reduce_max_sync(0xFFFFFFFFu, bits));
+        uint32_t c;
+        if (e < TOP_STEP<T>) {
+            c = code_of(x[u], inverse_step(e));
+        } else {
+            e = step_of(__reduce_max_sync(0xFFFFFFFFu, is_finite_bits(bits) ? bits : 0u));
+            c = code_careful<T>(x[u], e);
+        }
+        if (32 * u < left) dst[32 * u] = (int8_t)c;
         mine = lane == u ? e : mine;
     }
     if (lane < BLOCKS && p.col + lane * SCOUT_CKPT_BLOCK < a.cols)
