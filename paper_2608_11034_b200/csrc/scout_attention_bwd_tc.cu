@@ -7,8 +7,10 @@
 //   dq_tc   owns 128 rows of a head and runs over their keys:   S = Q K^T    dP = G V^T    dQ += dS K
 //
 // Eight warps make P = 2^(s' - lse') and dS = P (dP - delta), two warpgroups of 64 columns each, a thread per row. They
-// take the scores into registers first, so that the next product of scores runs while they work.  dkv_tc has no
-// tensor memory left for P beside the scores (4 x 128 columns are S, dP, dV, dK), so its P goes through shared memory.
+// take scores and dP into registers before they work on them, so that the next products run meanwhile.  dkv_tc has four
+// times 128 columns of tensor memory for S, dP, dV and dK: P and dS take the place of the scores, the next scores that of dP, and the
+// two change places every step.  (P through shared memory instead: 3418 cycles a step instead of the 2048 of its
+// products; 384 KiB a step pass through shared memory then, at 128 bytes a cycle.)
 //
 // One kernel that added dQ from blocks of keys would need 5 products instead of 4 + 3, but its sums would cross blocks:
 // float atomics give other bits on every run, and these gradients are compared bit by bit.
@@ -27,9 +29,9 @@ template <int HD> struct Layout {
     static constexpr int SUB = ROWS * 128;             // 128 rows x 64 elements
     static constexpr int TILE = SUB * (HD / 64);
     static constexpr int DQ_STAGES = HD == 128 ? 5 : 8;  // of K or V tiles
-    static constexpr int DKV_STAGES = HD == 128 ? 4 : 8; // of Q or G tiles
+    static constexpr int DKV_STAGES = HD == 128 ? 5 : 8; // of Q or G tiles
     static constexpr int DKV_SIDE = 3072;  // barriers and the rows' statistics; with HD = 128 the block's shared memory is full to the last byte
-    static constexpr int DQ_SMEM = (2 + DQ_STAGES) * TILE + 1024, DKV_SMEM = (2 + DKV_STAGES) * TILE + 2 * SUB + DKV_SIDE;
+    static constexpr int DQ_SMEM = (2 + DQ_STAGES) * TILE + 1024, DKV_SMEM = (2 + DKV_STAGES) * TILE + DKV_SIDE;
 };
 
 __device__ __forceinline__ void both_warpgroups() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -65,15 +67,6 @@ template <typename T, int HD> __device__ __forceinline__ void product_sum(uint32
     for (int k = 0; k < ROWS / 16; ++k) tc::mma_ts(d, w + (k >> 2) * gap + (k & 3) * 8, tc::desc_at(dx, k * 2048), id, add || k > 0);
 }
 
-// D += W X: W [128 rows][128 k] in shared memory in two pieces of 64 k, X as above
-template <typename T, int HD> __device__ __forceinline__ void product_rows(uint32_t d, uint32_t w, uint32_t x, bool add) {
-    constexpr uint32_t id = tc::instr(Half<T>::is_bf16, ROWS, HD, false, true);
-    const uint64_t dw = tc::smem_desc(w, 16, 1024), dx = tc::smem_desc(x, Layout<HD>::SUB, 1024);
-#pragma unroll
-    for (int k = 0; k < ROWS / 16; ++k)
-        tc::mma(d, tc::desc_at(dw, (k >> 2) * Layout<HD>::SUB + (k & 3) * 32), tc::desc_at(dx, k * 2048), id, add || k > 0);
-}
-
 struct TcBackwardArgs {
     Problem p;
     const float2 *stats;
@@ -105,25 +98,41 @@ struct Seen {
         }
     }
 };
-// scores -> P; minus(c): -lse' of columns c, c + 1
+// what is added to columns c .. c + 3: one number for the row, or four of a table in shared memory (16-byte loads: all lanes read
+// the same, and a load of 4 bytes occupies shared memory as long)
+struct Four {
+    tc::F2 lo, hi;
+};
+__device__ __forceinline__ auto four(const float *table) {
+    return [table](int c) {
+        const float4 v = *reinterpret_cast<const float4 *>(table + c);
+        return Four{tc::f2(v.x, v.y), tc::f2(v.z, v.w)};
+    };
+}
+// scores -> P; minus(c): -lse' of columns c .. c + 3
 template <typename F> __device__ __forceinline__ void to_p(uint32_t (&r)[2][32], float scale_log2, const Seen &seen, F minus) {
     const tc::F2 scale2 = tc::f2(scale_log2, scale_log2);
 #pragma unroll
-    for (int c = 0; c < 64; c += 2) {
-        uint32_t &lo = r[c >> 5][c & 31], &hi = r[c >> 5][(c & 31) + 1];
-        const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(lo), __uint_as_float(hi)), scale2, minus(c)));
-        lo = __float_as_uint(exp2_fast(y.x)), hi = __float_as_uint(exp2_fast(y.y));
+    for (int c = 0; c < 64; c += 4) {
+        uint32_t *v = &r[c >> 5][c & 31];
+        const Four m = minus(c);
+        const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, m.lo));
+        const float2 z = tc::split(tc::fma2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, m.hi));
+        v[0] = __float_as_uint(exp2_fast(y.x)), v[1] = __float_as_uint(exp2_fast(y.y));
+        v[2] = __float_as_uint(exp2_fast(z.x)), v[3] = __float_as_uint(exp2_fast(z.y));
     }
     seen.hide(r);
 }
-// dP -> dS = P (dP - delta); minus(c): -delta of columns c, c + 1.  A hidden place's dP may be anything.
+// dP -> dS = P (dP - delta); minus(c): -delta of columns c .. c + 3.  A hidden place's dP may be anything.
 template <typename F> __device__ __forceinline__ void to_ds(uint32_t (&r)[2][32], const uint32_t (&w)[2][32], const Seen &seen, F minus) {
 #pragma unroll
-    for (int c = 0; c < 64; c += 2) {
-        uint32_t &lo = r[c >> 5][c & 31], &hi = r[c >> 5][(c & 31) + 1];
-        const tc::F2 d = tc::add2(tc::f2(__uint_as_float(lo), __uint_as_float(hi)), minus(c));
-        const float2 y = tc::split(tc::mul2(d, tc::f2(__uint_as_float(w[c >> 5][c & 31]), __uint_as_float(w[c >> 5][(c & 31) + 1]))));
-        lo = __float_as_uint(y.x), hi = __float_as_uint(y.y);
+    for (int c = 0; c < 64; c += 4) {
+        uint32_t *v = &r[c >> 5][c & 31];
+        const uint32_t *q = &w[c >> 5][c & 31];
+        const Four m = minus(c);
+        const float2 y = tc::split(tc::mul2(tc::add2(tc::f2(__uint_as_float(v[0]), __uint_as_float(v[1])), m.lo), tc::f2(__uint_as_float(q[0]), __uint_as_float(q[1]))));
+        const float2 z = tc::split(tc::mul2(tc::add2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), m.hi), tc::f2(__uint_as_float(q[2]), __uint_as_float(q[3]))));
+        v[0] = __float_as_uint(y.x), v[1] = __float_as_uint(y.y), v[2] = __float_as_uint(z.x), v[3] = __float_as_uint(z.y);
     }
     seen.hide(r);
 }
@@ -297,12 +306,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
             tc::tc_fence_after();
             uint32_t w[2][32], r[2][32], x[32];
             take(w, quarter + S + (j & 1) * ROWS + wg * 64);
-            to_p(w, p.scale_log2, seen, [&](int) { return lse2; });
+            to_p(w, p.scale_log2, seen, [&](int) { return Four{lse2, lse2}; });
             ok = patience.wait_warp(dp_full, j & 1);
             if (!ok) break;
             tc::tc_fence_after();
             take(r, quarter + DP + wg * 64);
-            to_ds(r, w, seen, [&](int) { return delta2; });
+            to_ds(r, w, seen, [&](int) { return Four{delta2, delta2}; });
             round16<T>(x, r);
             tc::tmem_store16(quarter + DP + wg * 64, x);  // over columns that have been read
             tc::tmem_store16(quarter + DP + wg * 64 + 16, x + 16);
@@ -355,10 +364,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
                                                         const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dk,
                                                         const __grid_constant__ CUtensorMap map_dv) {
     using L = Layout<HD>;
-    constexpr int STAGES = L::DKV_STAGES, S = 0, DP = 128, DV = 256, DK = 256 + HD;  // tensor memory columns
+    constexpr int STAGES = L::DKV_STAGES, SIDES = 0, DV = 256, DK = 256 + HD;  // tensor memory columns; two sides of 128 for S and dP
     struct Side {
         float lse[2][ROWS], delta[2][ROWS];  // -lse', -delta of a step's rows
-        uint64_t bars[2 * STAGES + 11];
+        uint64_t bars[2 * STAGES + 12];
         uint32_t tmem_slot, dead, bad[2][4];
     };
     static_assert(sizeof(Side) <= L::DKV_SIDE, "");
@@ -368,9 +377,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
     float (&s_lse)[2][ROWS] = side.lse, (&s_delta)[2][ROWS] = side.delta;
     const Problem &p = a.p;
-    const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, sp = sv + L::TILE, ring = sp + 2 * L::SUB;  // K, V, P, pairs (Q, G)
+    const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, ring = sv + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 16, dp_full = s_full + 8,
-                   p_full = dp_full + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
+                   dp_taken = dp_full + 8, p_full = dp_taken + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     // causal: the first keys are seen by the most rows
@@ -386,11 +395,6 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         }
     }
     const int all = tiles * p.group, per = (all + a.splits - 1) / a.splits, step0 = split * per, steps = max(min(all, step0 + per) - step0, 0);
-    // Where Q (g = 0) and G (1) of a step land: PAIRS pairs of slots in turn.  A pair's slots change roles every time: G is done with
-    // first (dV before dK), and its slot takes the Q that is needed first.
-    constexpr int PAIRS = STAGES / 2;
-    const auto slot = [&](int s, int g) { return s % PAIRS * 2 + (g ^ (s / PAIRS & 1)); };
-    const auto turn = [&](int s) { return (uint32_t)(s / PAIRS & 1); };
     const auto tile_of = [&](int s) { return qt0 + (step0 + s) % tiles; };
     const auto head_of = [&](int s) { return hk * p.group + (step0 + s) / tiles; };
 
@@ -398,7 +402,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
         tc::bar_init(k_full, 1), tc::bar_init(k_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(all_done, 1);
-        tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
+        tc::bar_init(dp_taken, 8), tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
         for (int s = 0; s < 2; ++s) tc::bar_init(st_full + 8 * s, 1), tc::bar_init(st_empty + 8 * s, 8);
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
@@ -420,51 +424,55 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     if (warp == 8) {
         if (lane == 0) {
             for (int r = 1; r < 2 * steps; ++r) {
-                const int s = r >> 1, g = r & 1, at = slot(s, g);
-                if (!patience.wait(empty + 8 * at, turn(s) ^ 1)) break;
+                const int at = r % STAGES;
+                if (!patience.wait(empty + 8 * at, ((r / STAGES) & 1) ^ 1)) break;
                 tc::bar_expect(full + 8 * at, L::TILE);
-                load_tile<HD>(ring + at * L::TILE, g ? &map_g : &map_q, full + 8 * at, tile_of(s) * ROWS, head_of(s), b);
+                load_tile<HD>(ring + at * L::TILE, r & 1 ? &map_g : &map_q, full + 8 * at, tile_of(r >> 1) * ROWS, head_of(r >> 1), b);
             }
         }
     } else if (warp == 9) {
-        const auto stage = [&](int s, int g) { return ring + slot(s, g) * L::TILE; };
-        const auto landed = [&](int s, int g) {
-            if (!patience.wait_warp(full + 8 * slot(s, g), turn(s))) return false;
+        const auto stage = [&](int r) { return ring + (r % STAGES) * L::TILE; };
+        const auto landed = [&](int r) {
+            if (!patience.wait_warp(full + 8 * (r % STAGES), (r / STAGES) & 1)) return false;
             // rows past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dK and dV
-            const int row0 = tile_of(s) * ROWS;
-            if (n.nq < p.q_len && row0 + ROWS > n.nq) clear_rows<HD>(stage(s, g), max(n.nq - row0, 0), lane);
+            const int row0 = tile_of(r >> 1) * ROWS;
+            if (n.nq < p.q_len && row0 + ROWS > n.nq) clear_rows<HD>(stage(r), max(n.nq - row0, 0), lane);
             return true;
         };
+        const auto side_s = [&](int s) { return tmem + SIDES + (s & 1) * ROWS; };
+        const auto side_dp = [&](int s) { return tmem + SIDES + ((s & 1) ^ 1) * ROWS; };
         const auto issue_s = [&](int s) {
-            product_tiles<T, HD>(tmem + S, sk, stage(s, 0));
+            product_tiles<T, HD>(side_s(s), sk, stage(2 * s));
             tc::mma_commit(s_full);
         };
         const auto issue_dp = [&](int s) {
-            product_tiles<T, HD>(tmem + DP, sv, stage(s, 1));
+            product_tiles<T, HD>(side_dp(s), sv, stage(2 * s + 1));
             tc::mma_commit(dp_full);
         };
-        bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0, 0);
+        bool ok = steps > 0 && patience.wait_warp(k_full, 0) && landed(0);
         if (ok) issue_s(0);
-        ok = ok && patience.wait_warp(k_full + 8, 0) && landed(0, 1);
+        ok = ok && patience.wait_warp(k_full + 8, 0) && landed(1);
         if (ok) issue_dp(0);
         for (int s = 0; ok && s < steps; ++s) {
             const bool next = s + 1 < steps;
-            ok = (!next || landed(s + 1, 0)) && patience.wait_warp(p_full, s & 1);  // also: the scores have been taken
-            if (!ok) break;
-            tc::tc_fence_after();
-            if (next) issue_s(s + 1);
-            product_rows<T, HD>(tmem + DV, sp, stage(s, 1), s > 0);
-            tc::mma_commit(empty + 8 * slot(s, 1));  // also: P's tile is free
-            ok = patience.wait_warp(ds_full, s & 1);
-            if (!ok) break;
-            tc::tc_fence_after();
-            product_sum<T, HD>(tmem + DK, tmem + DP, 64, stage(s, 0), s > 0);
-            tc::mma_commit(empty + 8 * slot(s, 0));
-            if (!next) tc::mma_commit(all_done);
             if (next) {
-                ok = landed(s + 1, 1);
-                if (ok) issue_dp(s + 1);
+                ok = landed(2 * s + 2) && patience.wait_warp(dp_taken, s & 1);
+                if (!ok) break;
+                tc::tc_fence_after();
+                issue_s(s + 1);  // over dP
             }
+            ok = patience.wait_warp(p_full, s & 1);
+            if (!ok) break;
+            tc::tc_fence_after();
+            product_sum<T, HD>(tmem + DV, side_s(s), 64, stage(2 * s + 1), s > 0);
+            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));
+            ok = (!next || landed(2 * s + 3)) && patience.wait_warp(ds_full, s & 1);
+            if (!ok) break;
+            tc::tc_fence_after();
+            product_sum<T, HD>(tmem + DK, side_s(s) + 32, 64, stage(2 * s), s > 0);
+            tc::mma_commit(empty + 8 * ((2 * s) % STAGES));
+            if (next) issue_dp(s + 1);  // over P and dS
+            else tc::mma_commit(all_done);
         }
     } else if (warp == 10) {
         for (int s = 0; s < steps; ++s) {
@@ -492,36 +500,26 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             if (!ok) break;
             tc::tc_fence_after();
             uint32_t w[2][32], r[2][32], x[32];
-            take(w, quarter + S + wg * 64);
+            const uint32_t at = quarter + SIDES + wg * 64, at_s = at + (s & 1) * ROWS, at_dp = at + ((s & 1) ^ 1) * ROWS;
+            take(w, at_s);
             ok = patience.wait_warp(st_full + 8 * st, (s >> 1) & 1);
             if (!ok) break;
-            const auto pairs = [&](const float *v) {
-                return [=](int c) {
-                    const float2 y = *reinterpret_cast<const float2 *>(v + c);
-                    return tc::f2(y.x, y.y);
-                };
-            };
-            to_p(w, p.scale_log2, seen, pairs(s_lse[st] + wg * 64));
+            to_p(w, p.scale_log2, seen, four(s_lse[st] + wg * 64));
             round16<T>(x, w);
-            if (s > 0) {  // the product that read P's tile a step ago
-                ok = patience.wait_warp(empty + 8 * slot(s - 1, 1), turn(s - 1));
-                if (!ok) break;
-            }
-#pragma unroll
-            for (int c = 0; c < 8; ++c)
-                tc::store_shared16(tc::swizzled(sp + wg * L::SUB, (warp & 3) * 32 + lane, c), x[4 * c], x[4 * c + 1], x[4 * c + 2], x[4 * c + 3]);
-            tc::fence_async();
-            tc::tc_fence_before();  // the scores' loads
-            __syncwarp();
-            if (lane == 0) tc::bar_arrive(p_full);
+            tc::tmem_store16(at_s, x);  // over columns that this warp has read
+            tc::tmem_store16(at_s + 16, x + 16);
+            stored(p_full, lane);
             ok = patience.wait_warp(dp_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
-            take(r, quarter + DP + wg * 64);
-            to_ds(r, w, seen, pairs(s_delta[st] + wg * 64));
+            take(r, at_dp);
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::bar_arrive(dp_taken);
+            to_ds(r, w, seen, four(s_delta[st] + wg * 64));
             round16<T>(x, r);
-            tc::tmem_store16(quarter + DP + wg * 64, x);  // over columns that have been read
-            tc::tmem_store16(quarter + DP + wg * 64 + 16, x + 16);
+            tc::tmem_store16(at_s + 32, x);
+            tc::tmem_store16(at_s + 48, x + 16);
             stored(ds_full, lane);
             if (lane == 0) tc::bar_arrive(st_empty + 8 * st);
         }
