@@ -439,8 +439,9 @@ struct BackwardArgs {
     const float *lse;
     float2 *stats;  // [batch][q_heads][q_len] {lse', delta}
     void *dq, *dk, *dv;
-    float *part;    // fp32 parts, or null: [splits][rows][head_dim] (dQ), [splits][2][keys][head_dim] (dK, dV)
-    int tiles, splits;
+    float *part_q, *part_kv;  // fp32 parts: [q_splits][rows][head_dim] of dQ, [kv_splits][2][keys][head_dim] of dK, dV
+    int q_splits, kv_splits;
+    int tiles, splits;        // of the kernel that is launched
 };
 
 // delta = g . o, and the row statistic on powers of two.  A row that sees nothing gets +inf: its probabilities come out 0.
@@ -452,29 +453,33 @@ __global__ void __launch_bounds__(THREADS) backward_stats(const __grid_constant_
     pdl_launch_dependents();
     const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
     const int lane = threadIdx.x & 15, d = lane * 8;
-    float4 o[4], g[4];
+    const T *po[4], *pg[4];
     int64_t at[4];
     bool ok[4];
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-        const int64_t x = (int64_t)blockIdx.x * STAT_ROWS + u * (THREADS / 16) + (threadIdx.x >> 4);  // heads adjacent in memory
+        const int64_t x = min((int64_t)blockIdx.x * STAT_ROWS + u * (THREADS / 16) + (threadIdx.x >> 4), rows);  // heads adjacent in memory
+        const int64_t y = min(x, rows - 1);
         int hq, i, b;
         if (rows <= 0x7FFFFFFF) {
-            const uint32_t y = (uint32_t)x, t = y / (uint32_t)p.q_heads;
-            hq = y - t * p.q_heads, b = t / (uint32_t)p.q_len, i = t - b * p.q_len;
+            const uint32_t z = (uint32_t)y, t = z / (uint32_t)p.q_heads;
+            hq = z - t * p.q_heads, b = t / (uint32_t)p.q_len, i = t - b * p.q_len;
         } else {
-            hq = x % p.q_heads, i = x / p.q_heads % p.q_len, b = (int)(x / p.q_heads / p.q_len);
+            hq = y % p.q_heads, i = y / p.q_heads % p.q_len, b = (int)(y / p.q_heads / p.q_len);
         }
         at[u] = x < rows ? ((int64_t)b * p.q_heads + hq) * p.q_len + i : -1;
-        ok[u] = false;
-        o[u] = g[u] = make_float4(0.f, 0.f, 0.f, 0.f);
-        if (x >= rows) continue;
+        po[u] = RowIO<T>::at(p.o, p.so, b, i, hq) + d, pg[u] = RowIO<T>::at(p.d_o, p.sg, b, i, hq) + d;
         const Lengths n = lengths(p, b);
-        ok[u] = row_hi(p, n, i) > row_lo(p, n, i);
-        if (ok[u] && d < p.head_dim) {
-            o[u] = *reinterpret_cast<const float4 *>(RowIO<T>::at(p.o, p.so, b, i, hq) + d);
-            g[u] = *reinterpret_cast<const float4 *>(RowIO<T>::at(p.d_o, p.sg, b, i, hq) + d);
-        }
+        ok[u] = x < rows && row_hi(p, n, i) > row_lo(p, n, i);
+    }
+    float4 o[4], g[4];
+    float lse[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {  // nothing between the loads
+        const bool in = ok[u] && d < p.head_dim;
+        o[u] = in ? __ldg(reinterpret_cast<const float4 *>(po[u])) : make_float4(0.f, 0.f, 0.f, 0.f);
+        g[u] = in ? __ldg(reinterpret_cast<const float4 *>(pg[u])) : make_float4(0.f, 0.f, 0.f, 0.f);
+        lse[u] = ok[u] ? a.lse[at[u]] : -CUDART_INF_F;
     }
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
@@ -488,8 +493,7 @@ __global__ void __launch_bounds__(THREADS) backward_stats(const __grid_constant_
 #pragma unroll
         for (int m = 8; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
         if (lane == 0 && at[u] >= 0) {
-            const float l = ok[u] ? a.lse[at[u]] : -CUDART_INF_F;
-            a.stats[at[u]] = l == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(l * LOG2E, dot);
+            a.stats[at[u]] = lse[u] == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(lse[u] * LOG2E, dot);
         }
     }
 }
@@ -592,7 +596,7 @@ __global__ void __launch_bounds__(THREADS) backward_dq(const __grid_constant__ B
         if (a.splits > 1) {
             const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
             if (mine) {
-                float *dst = a.part + (split * rows + ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m)) * p.head_dim;
+                float *dst = a.part_q + (split * rows + ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m)) * p.head_dim;
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c) {
                     const int col = c * 8 + (lane & 3) * 2;
@@ -623,33 +627,6 @@ __global__ void __launch_bounds__(THREADS) backward_dq(const __grid_constant__ B
         redo &= redo - 1;
         row_dq<T>(p, a.stats, b, rm.head(m), rm.token(m), a.dq);
     }
-}
-
-template <typename T>
-__global__ void __launch_bounds__(THREADS) join_dq(const __grid_constant__ BackwardArgs a) {
-    pdl_wait();
-    const Problem &p = a.p;
-    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
-    const int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
-    if (row >= rows) return;
-    const int lane = threadIdx.x & 31, d = p.head_dim;
-    const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
-    float acc[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int s = 0; s < a.splits; ++s)
-#pragma unroll
-        for (int c = 0; c < 4; ++c)
-            if (lane + 32 * c < d) acc[c] += a.part[(s * rows + row) * d + lane + 32 * c];
-    bool fine = true;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
-    if (!__all_sync(0xFFFFFFFFu, fine)) {
-        row_dq<T>(p, a.stats, b, hq, i, a.dq);
-        return;
-    }
-#pragma unroll
-    for (int c = 0; c < 4; ++c) acc[c] *= p.scale;
-    RowIO<T>::store(RowIO<T>::at(a.dq, p.sq, b, i, hq), acc, d, lane);
 }
 
 // Owns 64 keys; runs over the packed rows that see them, 32 at a time (with 64 the two 16 x HD accumulators and both
@@ -743,7 +720,7 @@ __global__ void __launch_bounds__(THREADS) backward_dkv(const __grid_constant__ 
             const int64_t keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
             if (mine) {
                 const int64_t row = ((int64_t)b * p.kv_heads + hk) * p.kv_len + j;
-                float *dk = a.part + ((2 * split) * keys + row) * p.head_dim, *dv = dk + keys * p.head_dim;
+                float *dk = a.part_kv + ((2 * split) * keys + row) * p.head_dim, *dv = dk + keys * p.head_dim;
 #pragma unroll
                 for (int c = 0; c < HD / 8; ++c) {
                     const int col = c * 8 + (lane & 3) * 2;
@@ -782,22 +759,46 @@ __global__ void __launch_bounds__(THREADS) backward_dkv(const __grid_constant__ 
     }
 }
 
+// One warp adds up a row's parts in order: rows of dQ first (where it has parts), then keys.
 template <typename T>
-__global__ void __launch_bounds__(THREADS) join_dkv(const __grid_constant__ BackwardArgs a) {
+__global__ void __launch_bounds__(THREADS) backward_join(const __grid_constant__ BackwardArgs a) {
     pdl_wait();
     const Problem &p = a.p;
-    const int64_t keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
-    const int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
-    if (row >= keys) return;
+    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len, keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
+    int64_t row = (int64_t)blockIdx.x * (THREADS / 32) + (threadIdx.x >> 5);
     const int lane = threadIdx.x & 31, d = p.head_dim;
+    if (a.q_splits > 1) {
+        if (row < rows) {
+            const int i = row % p.q_len, hq = row / p.q_len % p.q_heads, b = row / p.q_len / p.q_heads;
+            float acc[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+            for (int s = 0; s < a.q_splits; ++s)
+#pragma unroll
+                for (int c = 0; c < 4; ++c)
+                    if (lane + 32 * c < d) acc[c] += a.part_q[(s * rows + row) * d + lane + 32 * c];
+            bool fine = true;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) fine = fine && finite(acc[c]);
+            if (!__all_sync(0xFFFFFFFFu, fine)) {
+                row_dq<T>(p, a.stats, b, hq, i, a.dq);
+                return;
+            }
+#pragma unroll
+            for (int c = 0; c < 4; ++c) acc[c] *= p.scale;
+            RowIO<T>::store(RowIO<T>::at(a.dq, p.sq, b, i, hq), acc, d, lane);
+            return;
+        }
+        row -= rows;
+    }
+    if (a.kv_splits < 2 || row >= keys) return;
     const int j = row % p.kv_len, hk = row / p.kv_len % p.kv_heads, b = row / p.kv_len / p.kv_heads;
     float ak[4] = {0.f, 0.f, 0.f, 0.f}, av[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-    for (int s = 0; s < a.splits; ++s)
+    for (int s = 0; s < a.kv_splits; ++s)
 #pragma unroll
         for (int c = 0; c < 4; ++c)
             if (lane + 32 * c < d) {
-                const float *x = a.part + ((2 * s) * keys + row) * d + lane + 32 * c;
+                const float *x = a.part_kv + ((2 * s) * keys + row) * d + lane + 32 * c;
                 ak[c] += x[0];
                 av[c] += x[keys * d];
             }
@@ -869,7 +870,7 @@ struct Shape {
     uint64_t rows, keys, q_tiles, k_tiles;
     int f_splits, q_splits, k_splits;
     bool few;
-    uint64_t forward_bytes, stats_bytes, backward_bytes;
+    uint64_t forward_bytes, stats_bytes, part_q_bytes, backward_bytes;
 };
 // tensor: the backward pass runs on tcgen05 (tiles of 128, one block an SM)
 Shape shape(const scout_attn_t &a, bool tensor) {
@@ -895,7 +896,8 @@ Shape shape(const scout_attn_t &a, bool tensor) {
     s.stats_bytes = up256(s.rows * 8);
     const uint64_t pq = s.q_splits > 1 ? s.q_splits * s.rows * a.head_dim * 4 : 0;
     const uint64_t pk = s.k_splits > 1 ? 2 * s.k_splits * s.keys * a.head_dim * 4 : 0;
-    s.backward_bytes = s.stats_bytes + up256(std::max(pq, pk));  // the two kernels follow one another
+    s.part_q_bytes = up256(pq);
+    s.backward_bytes = s.stats_bytes + s.part_q_bytes + up256(pk);
     return s;
 }
 bool worth_tensor(const scout_attn_t &a) { return a.q_len >= 96 && a.kv_len >= 96; }
@@ -933,30 +935,26 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
 
 template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, const BackwardViews *maps, cudaStream_t stream) {
     constexpr int smem_q = 6 * TILE * HD * 2, smem_k = 2 * TILE * HD * 2 + 4 * 32 * HD * 2;
-    if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
-    if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
     const uint64_t bh = (uint64_t)a.p.batch * a.p.kv_heads;
+    a.q_splits = s.rows ? s.q_splits : 1, a.kv_splits = s.keys ? s.k_splits : 1;
+    // every kernel waits for the whole of the one before it (griddepcontrol.wait), which has waited for its own predecessor
     if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + STAT_ROWS - 1) / STAT_ROWS, 0, stream, a, false));
-    // every kernel that follows waits for the whole of the one before it (griddepcontrol.wait), so the
-    // statistics are there for all of them and the shared parts are free
-    if (s.rows) {
-        a.tiles = (int)s.q_tiles, a.splits = s.q_splits;
-        if (maps) {
-            if (int rc = dq_tensor(a.p, Half<T>::is_bf16, a.stats, a.dq, a.part, a.splits, *maps, stream)) return rc;
-        } else {
+    if (maps) {
+        if (int rc = backward_tensor(a.p, Half<T>::is_bf16, a.stats, a.dq, a.dk, a.dv, a.part_q, a.q_splits, a.part_kv, a.kv_splits, *maps, stream)) return rc;
+    } else {
+        if (int rc = allow_smem<backward_dq<T, HD>>(smem_q)) return rc;
+        if (int rc = allow_smem<backward_dkv<T, HD>>(smem_k)) return rc;
+        if (s.rows) {
+            a.tiles = (int)s.q_tiles, a.splits = a.q_splits;
             SCOUT_CUDA(launch(backward_dq<T, HD>, s.q_tiles * bh * a.splits, smem_q, stream, a, true));
         }
-        if (a.splits > 1) SCOUT_CUDA(launch(join_dq<T>, (s.rows + 3) / 4, 0, stream, a, true));
-    }
-    if (s.keys) {
-        a.tiles = (int)s.k_tiles, a.splits = s.k_splits;
-        if (maps) {
-            if (int rc = dkv_tensor(a.p, Half<T>::is_bf16, a.stats, a.dk, a.dv, a.part, a.splits, *maps, stream)) return rc;
-        } else {
+        if (s.keys) {
+            a.tiles = (int)s.k_tiles, a.splits = a.kv_splits;
             SCOUT_CUDA(launch(backward_dkv<T, HD>, s.k_tiles * bh * a.splits, smem_k, stream, a, s.rows > 0));
         }
-        if (a.splits > 1) SCOUT_CUDA(launch(join_dkv<T>, (s.keys + 3) / 4, 0, stream, a, true));
     }
+    const uint64_t joined = (a.q_splits > 1 ? s.rows : 0) + (a.kv_splits > 1 ? s.keys : 0);
+    if (joined) SCOUT_CUDA(launch(backward_join<T>, (joined + 3) / 4, 0, stream, a, true));
     return SCOUT_OK;
 }
 
@@ -1028,11 +1026,11 @@ extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const v
     b.p.q = q, b.p.k = k, b.p.v = v, b.p.o = o, b.p.d_o = d_o, b.p.q_lens = q_lens, b.p.kv_lens = kv_lens;
     b.lse = lse, b.dq = dq, b.dk = dk, b.dv = dv;
     b.stats = (float2 *)workspace;
-    b.part = (float *)((uint8_t *)workspace + s.stats_bytes);
     const bool wide = a->head_dim > 64, bf16 = a->dtype == SCOUT_DT_BF16;
     BackwardViews views;
     const BackwardViews *maps = worth_tensor(*a) && backward_views(b.p, bf16, dq, dk, dv, &views) ? &views : nullptr;
     if (maps) s = shape(*a, true);
+    b.part_q = (float *)((uint8_t *)workspace + s.stats_bytes), b.part_kv = (float *)((uint8_t *)b.part_q + s.part_q_bytes);
     const cudaStream_t st = (cudaStream_t)stream;
     if (bf16) return wide ? backward<__nv_bfloat16, 128>(s, b, maps, st) : backward<__nv_bfloat16, 64>(s, b, maps, st);
     return wide ? backward<__half, 128>(s, b, maps, st) : backward<__half, 64>(s, b, maps, st);

@@ -254,14 +254,14 @@ __device__ __forceinline__ void row_dkv(const Problem &p, const float2 *stats, i
 bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box);
 // *taken is false where TMA cannot address a tensor and nothing was enqueued
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken);
-// The backward pass's views; false where TMA cannot address a tensor.  The two calls write the results or, with splits > 1,
-// fp32 parts of them.
+// The backward pass's views; false where TMA cannot address a tensor.  The call writes the results or, with splits > 1, fp32 parts
+// of them: [q_splits][rows][head_dim] for dQ, [kv_splits][2][keys][head_dim] for dK and dV.
 struct BackwardViews {
     CUtensorMap q, k, v, d_o, dq, dk, dv;
 };
 bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v);
-int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const BackwardViews &v, cudaStream_t stream);
-int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const BackwardViews &v, cudaStream_t stream);
+int backward_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, void *dk, void *dv, float *part_q, int q_splits, float *part_kv, int kv_splits,
+                    const BackwardViews &v, cudaStream_t stream);
 
 }  // namespace attn
 }  // namespace scout

@@ -1,13 +1,13 @@
-// Attention's backward pass on tcgen05: two kernels of the same shape, both with everything but the inputs in
+// Attention's backward pass on tcgen05: two parts of one launch, both with everything but the inputs in
 // tensor memory.
 //
-//   dkv_tc  owns 128 keys and runs over the 128-row query tiles that see them, all heads of the group:
+//   dkv_block  owns 128 keys and runs over the 128-row query tiles that see them, all heads of the group:
 //               S^T = K Q^T    dP^T = V G^T    dV += P^T G    dK += dS^T Q
 //           Keys are the rows, so P^T and dS^T are left operands as they come out of the softmax.
-//   dq_tc   owns 128 rows of a head and runs over their keys:   S = Q K^T    dP = G V^T    dQ += dS K
+//   dq_block   owns 128 rows of a head and runs over their keys:   S = Q K^T    dP = G V^T    dQ += dS K
 //
 // Eight warps make P = 2^(s' - lse') and dS = P (dP - delta), two warpgroups of 64 columns each, a thread per row. They
-// take scores and dP into registers before they work on them, so that the next products run meanwhile.  dkv_tc has four
+// take scores and dP into registers before they work on them, so that the next products run meanwhile.  dkv_block has four
 // times 128 columns of tensor memory for S, dP, dV and dK: P and dS take the place of the scores, the next scores that of dP, and the
 // two change places every step.  (P through shared memory instead: 3418 cycles a step instead of the 2048 of its
 // products; 384 KiB a step pass through shared memory then, at 128 bytes a cycle.)
@@ -29,9 +29,10 @@ template <int HD> struct Layout {
     static constexpr int SUB = ROWS * 128;             // 128 rows x 64 elements
     static constexpr int TILE = SUB * (HD / 64);
     static constexpr int DQ_STAGES = HD == 128 ? 5 : 8;  // of K or V tiles
-    static constexpr int DKV_STAGES = HD == 128 ? 5 : 8; // of Q or G tiles
-    static constexpr int DKV_SIDE = 3072;  // barriers and the rows' statistics; with HD = 128 the block's shared memory is full to the last byte
-    static constexpr int DQ_SMEM = (2 + DQ_STAGES) * TILE + 1024, DKV_SMEM = (2 + DKV_STAGES) * TILE + DKV_SIDE;
+    static constexpr int DKV_Q = HD == 128 ? 3 : 4, DKV_G = HD == 128 ? 2 : 4;  // Q is used to the end of a step, G until dV
+    static constexpr int TILES = 7 + (HD == 64 ? 3 : 0), SIDE = 3072;  // with HD = 128 the block's shared memory is full to the last byte
+    static constexpr int SMEM = TILES * TILE + SIDE;
+    static_assert(2 + DQ_STAGES <= TILES && 2 + DKV_Q + DKV_G <= TILES, "");
 };
 
 __device__ __forceinline__ void both_warpgroups() { asm volatile("bar.sync 1, 256;" ::: "memory"); }
@@ -71,9 +72,14 @@ struct TcBackwardArgs {
     Problem p;
     const float2 *stats;
     void *dq, *dk, *dv;
-    float *part;
+    float *part_q, *part_kv;  // fp32 parts where q_splits, kv_splits exceed 1
     uint32_t *gave_up;
-    int tiles, splits;
+    int q_tiles, q_splits, kv_tiles, kv_splits, kv_blocks;  // blocks [0, kv_blocks) make dK and dV, the others dQ
+};
+struct Side {  // what a block keeps in shared memory beside its tiles
+    float lse[2][ROWS], delta[2][ROWS];  // dK, dV: -lse', -delta of a step's rows
+    uint64_t bars[32];
+    uint32_t tmem_slot, dead, bad[2][4];
 };
 
 // 64 columns of this thread's row to registers
@@ -98,6 +104,24 @@ struct Seen {
         }
     }
 };
+// 2^x of two numbers by multiply-adds, beside the special function unit (four lanes a cycle): of a row's 32 pairs of exponentials SHARE
+// are made this way (0: 244, 4: 240, 6: 238.5, 8: 239, 12: 252 us for 2 x 2048 tokens, 32/8 heads of 128, causal).  Cody-Waite: x = n + f with n the nearest integer, which adding 1.5 2^23 leaves in the low
+// bits, and 2^f on [-1/2, 1/2] by the polynomial of degree 4 of least maximal relative error (Remez exchange; 2.7e-6, far
+// below the 2^-9 or 2^-12 that P is rounded to).  What lies below 2^-126 comes out as 2^-126.
+constexpr int SHARE = 6;
+__device__ __forceinline__ float2 exp2_fma(tc::F2 x) {
+    const float2 lim = tc::split(x);
+    const tc::F2 y = tc::f2(fmaxf(lim.x, -126.f), fmaxf(lim.y, -126.f)), magic = tc::f2(12582912.f, 12582912.f);
+    const tc::F2 t = tc::add2(y, magic), n = tc::add2(t, tc::f2(-12582912.f, -12582912.f)), f = tc::fma2(n, tc::f2(-1.f, -1.f), y);
+    tc::F2 p = tc::f2(0.009570102207362652f, 0.009570102207362652f);
+    p = tc::fma2(p, f, tc::f2(0.05591785907745361f, 0.05591785907745361f));
+    p = tc::fma2(p, f, tc::f2(0.240247443318367f, 0.240247443318367f));
+    p = tc::fma2(p, f, tc::f2(0.6931217908859253f, 0.6931217908859253f));
+    p = tc::fma2(p, f, tc::f2(0.9999992847442627f, 0.9999992847442627f));
+    const float2 m = tc::split(p), e = tc::split(t);
+    return make_float2(__uint_as_float(__float_as_uint(m.x) + (__float_as_uint(e.x) << 23)),
+                       __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
+}
 // what is added to columns c .. c + 3: one number for the row, or four of a table in shared memory (16-byte loads: all lanes read
 // the same, and a load of 4 bytes occupies shared memory as long)
 struct Four {
@@ -117,9 +141,11 @@ template <typename F> __device__ __forceinline__ void to_p(uint32_t (&r)[2][32],
         uint32_t *v = &r[c >> 5][c & 31];
         const Four m = minus(c);
         const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, m.lo));
-        const float2 z = tc::split(tc::fma2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, m.hi));
+        const tc::F2 z = tc::fma2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, m.hi);
         v[0] = __float_as_uint(exp2_fast(y.x)), v[1] = __float_as_uint(exp2_fast(y.y));
-        v[2] = __float_as_uint(exp2_fast(z.x)), v[3] = __float_as_uint(exp2_fast(z.y));
+        const bool fma = (c >> 2) * SHARE % 16 + SHARE >= 16;  // SHARE of the 16 second pairs, spread evenly
+        const float2 u = fma ? exp2_fma(z) : make_float2(exp2_fast(tc::split(z).x), exp2_fast(tc::split(z).y));
+        v[2] = __float_as_uint(u.x), v[3] = __float_as_uint(u.y);
     }
     seen.hide(r);
 }
@@ -194,28 +220,30 @@ template <int COLS> __device__ __forceinline__ void write_part(float *row, const
 
 // ---- dQ ------------------------------------------------------------------------------------------------------
 template <typename T, int HD>
-__global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ TcBackwardArgs a, const __grid_constant__ CUtensorMap map_q,
-                                                       const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                       const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dq) {
+__device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const BackwardViews &views, uint8_t *smem_tiles, Side &side, int block) {
     using L = Layout<HD>;
     constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 256, DQ = 384;  // tensor memory columns: two tiles of scores, dP (then dS), dQ
-    extern __shared__ uint8_t smem_raw[];
-    __shared__ uint64_t bars[2 * STAGES + 7];
-    __shared__ uint32_t tmem_slot, dead, s_bad[2][4];
+    uint64_t *const bars = side.bars;
+    static_assert(2 * STAGES + 7 <= 32, "");
+    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
     const Problem &p = a.p;
-    const uint32_t sq = (smem_u32(smem_raw) + 1023) & ~1023u, sg = sq + L::TILE, ring = sg + L::TILE;
+    const uint32_t sq = smem_u32(smem_tiles), sg = sq + L::TILE, ring = sg + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 16,
                    ds_full = dp_full + 8, dq_done = ds_full + 8;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    const int head = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits, row0 = (a.tiles - 1 - (int)blockIdx.z / a.splits) * ROWS;
+    const int split = block % a.q_splits;
+    block /= a.q_splits;
+    const int head = block % p.q_heads;
+    block /= p.q_heads;
+    const int b = block % p.batch, row0 = (a.q_tiles - 1 - block / p.batch) * ROWS;  // causal: the last rows see the most keys
     const Lengths n = lengths(p, b);
     const int hk = head / p.group, last = min(row0 + ROWS, n.nq) - 1;
     int blk0 = 0, blk1 = 0, full0 = 0, full1 = 0;
     if (last >= row0 && row_hi(p, n, last) > row_lo(p, n, row0)) {
         blk0 = row_lo(p, n, row0) / ROWS, blk1 = (row_hi(p, n, last) + ROWS - 1) / ROWS;
         full0 = (row_lo(p, n, last) + ROWS - 1) / ROWS, full1 = row_hi(p, n, row0) / ROWS;
-        const int per = (blk1 - blk0 + a.splits - 1) / a.splits;
+        const int per = (blk1 - blk0 + a.q_splits - 1) / a.q_splits;
         blk0 += split * per;
         blk1 = min(blk1, blk0 + per);
     }
@@ -229,11 +257,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
             tc::bar_expect(q_full, L::TILE);
-            load_tile<HD>(sq, &map_q, q_full, row0, head, b);
+            load_tile<HD>(sq, &views.q, q_full, row0, head, b);
             tc::bar_expect(full, L::TILE);
-            load_tile<HD>(ring, &map_k, full, blk0 * ROWS, hk, b);
+            load_tile<HD>(ring, &views.k, full, blk0 * ROWS, hk, b);
             tc::bar_expect(q_full + 8, L::TILE);
-            load_tile<HD>(sg, &map_g, q_full + 8, row0, head, b);
+            load_tile<HD>(sg, &views.d_o, q_full + 8, row0, head, b);
         }
     }
     if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -248,7 +276,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
                 const int st = r % STAGES;
                 if (!patience.wait(empty + 8 * st, ((r / STAGES) & 1) ^ 1)) break;
                 tc::bar_expect(full + 8 * st, L::TILE);
-                load_tile<HD>(ring + st * L::TILE, r & 1 ? &map_v : &map_k, full + 8 * st, (blk0 + (r >> 1)) * ROWS, hk, b);
+                load_tile<HD>(ring + st * L::TILE, r & 1 ? &views.v : &views.k, full + 8 * st, (blk0 + (r >> 1)) * ROWS, hk, b);
             }
         }
     } else if (warp == 9) {
@@ -323,9 +351,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
             constexpr int COLS = HD / 2;
             float g[COLS];
             const bool fine = read_row<COLS>(g, quarter + DQ + wg * COLS, steps > 0 && hi > lo);
-            if (a.splits > 1) {
+            if (a.q_splits > 1) {
                 const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
-                if (mine) write_part<COLS>(a.part + (split * rows + ((int64_t)b * p.q_heads + head) * p.q_len + i) * p.head_dim, g, wg * COLS, p.head_dim);
+                if (mine) write_part<COLS>(a.part_q + (split * rows + ((int64_t)b * p.q_heads + head) * p.q_len + i) * p.head_dim, g, wg * COLS, p.head_dim);
             } else {
                 // through Q's tile, which the last product has read
                 stage_row<T, COLS>(sq, (warp & 3) * 32 + lane, g, wg * COLS, p.scale);
@@ -337,7 +365,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
                 if (wg == 0) {
                     const int r0 = (warp & 3) * 32;
                     if (lane == 0) {
-                        store_rows<HD>(&map_dq, sq, r0, row0 + r0, p.q_len, p.head_dim, head, b);
+                        store_rows<HD>(&views.dq, sq, r0, row0 + r0, p.q_len, p.head_dim, head, b);
                         if (redo) tc::tma_stored();
                         else tc::tma_store_read();
                     }
@@ -345,7 +373,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
                     for (; redo; redo &= redo - 1) row_dq<T>(p, a.stats, b, head, row0 + r0 + __ffs(redo) - 1, a.dq);
                 }
             }
-        } else if (a.splits == 1) {
+        } else if (a.q_splits == 1) {
             both_warpgroups();
         }
     }
@@ -359,21 +387,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dq_tc(const __grid_constant__ T
 
 // ---- dK, dV ----------------------------------------------------------------------------------------------------
 template <typename T, int HD>
-__global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ TcBackwardArgs a, const __grid_constant__ CUtensorMap map_q,
-                                                        const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                                                        const __grid_constant__ CUtensorMap map_g, const __grid_constant__ CUtensorMap map_dk,
-                                                        const __grid_constant__ CUtensorMap map_dv) {
+__device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const BackwardViews &views, uint8_t *smem_tiles, Side &side, int block) {
     using L = Layout<HD>;
-    constexpr int STAGES = L::DKV_STAGES, SIDES = 0, DV = 256, DK = 256 + HD;  // tensor memory columns; two sides of 128 for S and dP
-    struct Side {
-        float lse[2][ROWS], delta[2][ROWS];  // -lse', -delta of a step's rows
-        uint64_t bars[2 * STAGES + 12];
-        uint32_t tmem_slot, dead, bad[2][4];
-    };
-    static_assert(sizeof(Side) <= L::DKV_SIDE, "");
-    extern __shared__ __align__(1024) uint8_t smem_tiles[];  // nothing static beside it: it starts on a swizzle's boundary
-    Side &side = *reinterpret_cast<Side *>(smem_tiles + L::DKV_SMEM - L::DKV_SIDE);
+    constexpr int NQ = L::DKV_Q, NG = L::DKV_G, STAGES = NQ + NG, SIDES = 0, DV = 256, DK = 256 + HD;  // tensor memory columns; two sides of 128 for S and dP
     uint64_t *const bars = side.bars;
+    static_assert(2 * STAGES + 12 <= 32, "");
     uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
     float (&s_lse)[2][ROWS] = side.lse, (&s_delta)[2][ROWS] = side.delta;
     const Problem &p = a.p;
@@ -382,8 +400,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
                    dp_taken = dp_full + 8, p_full = dp_taken + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    // causal: the first keys are seen by the most rows
-    const int hk = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits, j0 = (int)blockIdx.z / a.splits * ROWS;
+    const int split = block % a.kv_splits;
+    block /= a.kv_splits;
+    const int hk = block % p.kv_heads;
+    block /= p.kv_heads;
+    const int b = block % p.batch, j0 = block / p.batch * ROWS;  // causal: the first keys are seen by the most rows
     const Lengths n = lengths(p, b);
     const int j1 = min(j0 + ROWS, n.nk);
     int qt0 = 0, tiles = 0, full0 = 0, full1 = 0;
@@ -394,7 +415,10 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             full0 = (col_lo(p, n, j1 - 1) + ROWS - 1) / ROWS, full1 = col_hi(p, n, j0) / ROWS;
         }
     }
-    const int all = tiles * p.group, per = (all + a.splits - 1) / a.splits, step0 = split * per, steps = max(min(all, step0 + per) - step0, 0);
+    const int all = tiles * p.group, per = (all + a.kv_splits - 1) / a.kv_splits, step0 = split * per, steps = max(min(all, step0 + per) - step0, 0);
+    // load r is Q (even) or G (odd) of step r / 2: its slot, and how often that slot has been filled before
+    const auto slot = [&](int r) { return r & 1 ? NQ + (r >> 1) % NG : (r >> 1) % NQ; };
+    const auto turn = [&](int r) { return (uint32_t)(r & 1 ? (r >> 1) / NG : (r >> 1) / NQ) & 1u; };
     const auto tile_of = [&](int s) { return qt0 + (step0 + s) % tiles; };
     const auto head_of = [&](int s) { return hk * p.group + (step0 + s) / tiles; };
 
@@ -407,11 +431,11 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
             tc::bar_expect(k_full, L::TILE);
-            load_tile<HD>(sk, &map_k, k_full, j0, hk, b);
+            load_tile<HD>(sk, &views.k, k_full, j0, hk, b);
             tc::bar_expect(full, L::TILE);
-            load_tile<HD>(ring, &map_q, full, tile_of(0) * ROWS, head_of(0), b);
+            load_tile<HD>(ring, &views.q, full, tile_of(0) * ROWS, head_of(0), b);  // slot 0
             tc::bar_expect(k_full + 8, L::TILE);
-            load_tile<HD>(sv, &map_v, k_full + 8, j0, hk, b);
+            load_tile<HD>(sv, &views.v, k_full + 8, j0, hk, b);
         }
     }
     if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
@@ -419,21 +443,21 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     __syncthreads();
     tc::tc_fence_after();
     const uint32_t tmem = tc::uniform(tmem_slot);
-    pdl_wait();  // the statistics, and the parts that dQ's join has read
+    pdl_wait();  // the statistics
 
     if (warp == 8) {
         if (lane == 0) {
             for (int r = 1; r < 2 * steps; ++r) {
-                const int at = r % STAGES;
-                if (!patience.wait(empty + 8 * at, ((r / STAGES) & 1) ^ 1)) break;
+                const int at = slot(r);
+                if (!patience.wait(empty + 8 * at, turn(r) ^ 1)) break;
                 tc::bar_expect(full + 8 * at, L::TILE);
-                load_tile<HD>(ring + at * L::TILE, r & 1 ? &map_g : &map_q, full + 8 * at, tile_of(r >> 1) * ROWS, head_of(r >> 1), b);
+                load_tile<HD>(ring + at * L::TILE, r & 1 ? &views.d_o : &views.q, full + 8 * at, tile_of(r >> 1) * ROWS, head_of(r >> 1), b);
             }
         }
     } else if (warp == 9) {
-        const auto stage = [&](int r) { return ring + (r % STAGES) * L::TILE; };
+        const auto stage = [&](int r) { return ring + slot(r) * L::TILE; };
         const auto landed = [&](int r) {
-            if (!patience.wait_warp(full + 8 * (r % STAGES), (r / STAGES) & 1)) return false;
+            if (!patience.wait_warp(full + 8 * slot(r), turn(r))) return false;
             // rows past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dK and dV
             const int row0 = tile_of(r >> 1) * ROWS;
             if (n.nq < p.q_len && row0 + ROWS > n.nq) clear_rows<HD>(stage(r), max(n.nq - row0, 0), lane);
@@ -465,12 +489,12 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             if (!ok) break;
             tc::tc_fence_after();
             product_sum<T, HD>(tmem + DV, side_s(s), 64, stage(2 * s + 1), s > 0);
-            tc::mma_commit(empty + 8 * ((2 * s + 1) % STAGES));
+            tc::mma_commit(empty + 8 * slot(2 * s + 1));
             ok = (!next || landed(2 * s + 3)) && patience.wait_warp(ds_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();
             product_sum<T, HD>(tmem + DK, side_s(s) + 32, 64, stage(2 * s), s > 0);
-            tc::mma_commit(empty + 8 * ((2 * s) % STAGES));
+            tc::mma_commit(empty + 8 * slot(2 * s));
             if (next) issue_dp(s + 1);  // over P and dS
             else tc::mma_commit(all_done);
         }
@@ -529,9 +553,9 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
             float g[HD];
             const bool fine = read_row<HD>(g, quarter + (wg ? DK : DV), steps > 0 && hi > lo);
             const int64_t keys = (int64_t)p.batch * p.kv_heads * p.kv_len;
-            if (a.splits > 1) {
+            if (a.kv_splits > 1) {
                 if (mine)
-                    write_part<HD>(a.part + ((2 * split + (wg ? 0 : 1)) * keys + ((int64_t)b * p.kv_heads + hk) * p.kv_len + j) * p.head_dim, g, 0,
+                    write_part<HD>(a.part_kv + ((2 * split + (wg ? 0 : 1)) * keys + ((int64_t)b * p.kv_heads + hk) * p.kv_len + j) * p.head_dim, g, 0,
                                    p.head_dim);
             } else {
                 // through the tiles of V and K, which the last products have read
@@ -546,7 +570,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
 #pragma unroll
                 for (int c = 0; c < 8; ++c) any |= s_bad[c >> 2][c & 3];
                 if (lane == 0) {
-                    store_rows<HD>(wg ? &map_dk : &map_dv, tile, r0, j0 + r0, p.kv_len, p.head_dim, hk, b);
+                    store_rows<HD>(wg ? &views.dk : &views.dv, tile, r0, j0 + r0, p.kv_len, p.head_dim, hk, b);
                     if (any) tc::tma_stored();
                     else tc::tma_store_read();
                 }
@@ -556,7 +580,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
                     for (; wg == 0 && redo; redo &= redo - 1) row_dkv<T>(p, a.stats, b, hk, j0 + r0 + __ffs(redo) - 1, a.dk, a.dv);
                 }
             }
-        } else if (a.splits == 1) {
+        } else if (a.kv_splits == 1) {
             both_warpgroups();
         }
     }
@@ -568,54 +592,51 @@ __global__ void __launch_bounds__(TC_THREADS, 1) dkv_tc(const __grid_constant__ 
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-template <typename K, typename... M> cudaError_t launch(K kernel, dim3 grid, int smem, cudaStream_t stream, const TcBackwardArgs &a, const M &...maps) {
+// One launch for both, the larger blocks first: each fills what the other's last round of blocks leaves idle.
+template <typename T, int HD>
+__global__ void __launch_bounds__(TC_THREADS, 1) backward_tc(const __grid_constant__ TcBackwardArgs a, const __grid_constant__ BackwardViews views) {
+    using L = Layout<HD>;
+    extern __shared__ __align__(1024) uint8_t smem_tiles[];  // nothing static beside it: it starts on a swizzle's boundary
+    Side &side = *reinterpret_cast<Side *>(smem_tiles + L::TILES * L::TILE);
+    static_assert(sizeof(Side) <= L::SIDE, "");
+    if ((int)blockIdx.x < a.kv_blocks) dkv_block<T, HD>(a, views, smem_tiles, side, blockIdx.x);
+    else dq_block<T, HD>(a, views, smem_tiles, side, blockIdx.x - a.kv_blocks);
+}
+
+template <typename T, int HD> int run_backward(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
+    if (int rc = allow_smem<backward_tc<T, HD>>(Layout<HD>::SMEM)) return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = grid;
+    cfg.gridDim = dim3((unsigned)(a.kv_blocks + (int64_t)a.q_tiles * a.p.batch * a.p.q_heads * a.q_splits));
     cfg.blockDim = dim3(TC_THREADS);
-    cfg.dynamicSmemBytes = smem;
+    cfg.dynamicSmemBytes = Layout<HD>::SMEM;
     cfg.stream = stream;
     cudaLaunchAttribute attr[1];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    return cudaLaunchKernelEx(&cfg, kernel, a, maps...);
-}
-
-template <typename T, int HD> int run_dq(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
-    if (int rc = allow_smem<dq_tc<T, HD>>(Layout<HD>::DQ_SMEM)) return rc;
-    a.tiles = (a.p.q_len + ROWS - 1) / ROWS;
-    SCOUT_CUDA(launch(dq_tc<T, HD>, dim3(a.p.q_heads, a.p.batch, a.tiles * a.splits), Layout<HD>::DQ_SMEM, stream, a, v.q, v.k, v.v, v.d_o, v.dq));
-    return SCOUT_OK;
-}
-template <typename T, int HD> int run_dkv(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
-    if (int rc = allow_smem<dkv_tc<T, HD>>(Layout<HD>::DKV_SMEM)) return rc;
-    a.tiles = (a.p.kv_len + ROWS - 1) / ROWS;
-    SCOUT_CUDA(launch(dkv_tc<T, HD>, dim3(a.p.kv_heads, a.p.batch, a.tiles * a.splits), Layout<HD>::DKV_SMEM, stream, a, v.q, v.k, v.v, v.d_o, v.dk, v.dv));
+    SCOUT_CUDA(cudaLaunchKernelEx(&cfg, backward_tc<T, HD>, a, v));
     return SCOUT_OK;
 }
 
 }  // namespace
 
 bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v) {
-    // the grid's second and third axes (tiles are split only where there are fewer than 148)
-    if (p.batch > 65535 || p.q_len > 65535 * ROWS || p.kv_len > 65535 * ROWS) return false;
+    // blocks are numbered in 31 bits
+    const int64_t most = (int64_t)p.batch * ((p.q_len / ROWS + 1ll) * p.q_heads + (p.kv_len / ROWS + 1ll) * p.kv_heads);
+    if (most > 0x7FFFFFFF / 64) return false;
     return tensor_view(&v->q, bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&v->k, bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, ROWS) &&
            tensor_view(&v->v, bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, ROWS) && tensor_view(&v->d_o, bf16, p.d_o, p.sg, p, p.q_len, p.q_heads, ROWS) &&
            tensor_view(&v->dq, bf16, dq, p.sq, p, p.q_len, p.q_heads, 32) && tensor_view(&v->dk, bf16, dk, p.sk, p, p.kv_len, p.kv_heads, 32) &&
            tensor_view(&v->dv, bf16, dv, p.sv, p, p.kv_len, p.kv_heads, 32);
 }
-int dq_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, float *part, int splits, const BackwardViews &v, cudaStream_t stream) {
-    TcBackwardArgs a = {p, stats, dq, nullptr, nullptr, part, nullptr, 0, splits};
+int backward_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, void *dk, void *dv, float *part_q, int q_splits, float *part_kv, int kv_splits,
+                    const BackwardViews &v, cudaStream_t stream) {
+    TcBackwardArgs a = {p, stats, dq, dk, dv, part_q, part_kv, nullptr, (p.q_len + ROWS - 1) / ROWS, q_splits, (p.kv_len + ROWS - 1) / ROWS, kv_splits, 0};
+    a.kv_blocks = a.kv_tiles * p.batch * p.kv_heads * kv_splits;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-    if (p.head_dim > 64) return bf16 ? run_dq<__nv_bfloat16, 128>(a, v, stream) : run_dq<__half, 128>(a, v, stream);
-    return bf16 ? run_dq<__nv_bfloat16, 64>(a, v, stream) : run_dq<__half, 64>(a, v, stream);
-}
-int dkv_tensor(const Problem &p, bool bf16, const float2 *stats, void *dk, void *dv, float *part, int splits, const BackwardViews &v, cudaStream_t stream) {
-    TcBackwardArgs a = {p, stats, nullptr, dk, dv, part, nullptr, 0, splits};
-    if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-    if (p.head_dim > 64) return bf16 ? run_dkv<__nv_bfloat16, 128>(a, v, stream) : run_dkv<__half, 128>(a, v, stream);
-    return bf16 ? run_dkv<__nv_bfloat16, 64>(a, v, stream) : run_dkv<__half, 64>(a, v, stream);
+    if (p.head_dim > 64) return bf16 ? run_backward<__nv_bfloat16, 128>(a, v, stream) : run_backward<__half, 128>(a, v, stream);
+    return bf16 ? run_backward<__nv_bfloat16, 64>(a, v, stream) : run_backward<__half, 64>(a, v, stream);
 }
 
 }  // namespace attn
