@@ -257,10 +257,21 @@ __device__ __forceinline__ void finish_row(const ForwardArgs &a, int b, int hq, 
 }
 
 // At most 16 packed rows (a token or a few, with the group's heads): every warp of a block has all the rows and a share of the
-// keys, 16 at a time through a ring of its own, and the warps' results are merged in shared memory.  What bounds it is the
-// pass over the keys: 4 warps x FEW_STAGES x 8 KiB are in flight for a block (HD = 128).
-constexpr int FEW_KEYS = 16, FEW_STAGES = 3;
-template <int HD> constexpr int few_smem() { return 4 * FEW_STAGES * 2 * FEW_KEYS * HD * 2; }
+// keys, 16 at a time through a ring of its own, and the warps' results are merged in shared memory.  Up to eight parts
+// of a key head are one cluster, whose blocks read each other's results through distributed shared memory: no scratch and no second
+// launch.  What bounds it is the pass over the keys.  8 sequences of 2048..4096 keys, 8 key heads of 128: three blocks of
+// two stages an SM 27 us (with a join), two of three 30, one of four 39: warps count for more than bytes in flight.
+constexpr int FEW_KEYS = 16, FEW_STAGES = 2, FEW_CLUSTER = 8;
+__device__ __forceinline__ void cluster_sync() {
+    asm volatile("barrier.cluster.arrive.release.aligned;\n\tbarrier.cluster.wait.acquire.aligned;" ::: "memory");
+}
+__device__ __forceinline__ float from_block(const float *mine, uint32_t rank) {  // the same place in another block of the cluster
+    float v;
+    asm volatile("{\n\t.reg .b32 a;\n\tmapa.shared::cluster.u32 a, %1, %2;\n\tld.shared::cluster.f32 %0, [a];\n\t}" : "=f"(v) : "r"(smem_u32(mine)), "r"(rank) : "memory");
+    return v;
+}
+template <int HD> constexpr int few_smem() { return 4 * FEW_STAGES * 2 * FEW_KEYS * HD * 2; }  // at least the 5 x 16 x HD floats of the merge
+static_assert(4 * FEW_STAGES * 2 * FEW_KEYS * 2 >= 5 * 16 * 4, "");
 template <typename T, int HD>
 __global__ void __launch_bounds__(THREADS) forward_few(const __grid_constant__ ForwardArgs a) {
     extern __shared__ __align__(1024) uint8_t smem[];
@@ -378,6 +389,9 @@ __global__ void __launch_bounds__(THREADS) forward_few(const __grid_constant__ F
             *reinterpret_cast<float2 *>(all + (warp * 16 + m) * HD + c * 8 + (lane & 3) * 2) = make_float2(acc[c][2 * r], acc[c][2 * r + 1]);
     }
     __syncthreads();
+    __shared__ float c_top[16], c_sum[16];
+    float *joined = all + 4 * 16 * HD;  // [16][HD]: this block's part, for the cluster
+    const bool cluster = a.splits > 1 && a.splits <= FEW_CLUSTER;
     for (int m = warp; m < m1; m += 4) {
         float t = -CUDART_INF_F, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
@@ -391,7 +405,11 @@ __global__ void __launch_bounds__(THREADS) forward_few(const __grid_constant__ F
             for (int c = 0; c < HD / 32; ++c) o[c] = fmaf(all[(w * 16 + m) * HD + lane + 32 * c], f, o[c]);
         }
         const int64_t row = ((int64_t)b * p.q_heads + rm.head(m)) * p.q_len + rm.token(m);
-        if (a.splits > 1) {
+        if (cluster) {
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) joined[m * HD + lane + 32 * c] = o[c];
+            if (lane == 0) c_top[m] = t, c_sum[m] = l;
+        } else if (a.splits > 1) {
             const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
 #pragma unroll
             for (int c = 0; c < HD / 32; ++c)
@@ -401,6 +419,30 @@ __global__ void __launch_bounds__(THREADS) forward_few(const __grid_constant__ F
             finish_row<T>(a, b, rm.head(m), rm.token(m), t, l, o);
         }
     }
+    if (!cluster) return;
+    __syncwarp();
+    cluster_sync();
+    // a warp of the cluster to a row, parts in order
+    for (int m = split * 4 + warp; m < m1; m += a.splits * 4) {
+        float top_of[FEW_CLUSTER], t = -CUDART_INF_F, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int r = 0; r < FEW_CLUSTER; ++r) {
+            top_of[r] = r < a.splits ? from_block(&c_top[m], r) : -CUDART_INF_F;
+            t = fmaxf(t, top_of[r]);
+        }
+        const float base = t == -CUDART_INF_F ? 0.f : t;
+#pragma unroll
+        for (int r = 0; r < FEW_CLUSTER; ++r) {
+            if (r >= a.splits) break;
+            const float f = exp2f(top_of[r] - base);
+            l = fmaf(from_block(&c_sum[m], r), f, l);
+#pragma unroll
+            for (int c = 0; c < HD / 32; ++c) o[c] = fmaf(from_block(&joined[m * HD + lane + 32 * c], r), f, o[c]);
+        }
+        finish_row<T>(a, b, rm.head(m), rm.token(m), t, l, o);
+    }
+    __syncwarp();
+    cluster_sync();  // no block leaves while another reads its shared memory
 }
 
 // One warp joins a row's parts in order.
@@ -881,9 +923,14 @@ Shape shape(const scout_attn_t &a, bool tensor) {
     s.q_tiles = (group * a.q_len + TILE - 1) / TILE;
     s.k_tiles = (a.kv_len + TILE - 1) / TILE;
     const uint64_t seen = a.window ? std::min<uint64_t>(a.kv_len, (uint64_t)a.window + TILE) : a.kv_len;
-    // few rows: about four blocks to an SM, of which two run at a time, evens out sequences of different lengths
+    const uint64_t key_tiles = (seen + TILE - 1) / TILE;
     s.few = group * a.q_len <= 16;
-    s.f_splits = s.few ? parts(bh, (seen + TILE - 1) / TILE, 4 * 148, 2) : parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
+    if (s.few) {  // three blocks run on an SM; one round of them, as parts of a cluster if that fills half of it, else more parts and a join
+        const uint64_t want = std::max<uint64_t>(3 * 148 / bh, 1), most = std::max<uint64_t>(key_tiles / 2, 1);
+        s.f_splits = (int)std::min<uint64_t>(std::min(want, most), bh * FEW_CLUSTER >= 148 ? FEW_CLUSTER : 64);
+    } else {
+        s.f_splits = parts(s.q_tiles * bh, key_tiles, 2 * 148, 4);
+    }
     const uint64_t seen_by = a.window ? std::min<uint64_t>(a.q_len, (uint64_t)a.window + TILE) : a.q_len;
     if (tensor) {
         s.q_splits = parts((a.q_len + 127) / 128 * bh * group, (seen + 127) / 128, 148, 3);
@@ -892,7 +939,7 @@ Shape shape(const scout_attn_t &a, bool tensor) {
         s.q_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
         s.k_splits = parts(s.k_tiles * bh, (group * seen_by + 31) / 32, 2 * 148, 8);
     }
-    s.forward_bytes = s.f_splits > 1 ? up256(s.f_splits * s.rows * a.head_dim * 4) + up256(s.f_splits * s.rows * 8) : 0;
+    s.forward_bytes = s.f_splits > (s.few ? FEW_CLUSTER : 1) ? up256(s.f_splits * s.rows * a.head_dim * 4) + up256(s.f_splits * s.rows * 8) : 0;
     s.stats_bytes = up256(s.rows * 8);
     const uint64_t pq = s.q_splits > 1 ? s.q_splits * s.rows * a.head_dim * 4 : 0;
     const uint64_t pk = s.k_splits > 1 ? 2 * s.k_splits * s.keys * a.head_dim * 4 : 0;
@@ -903,17 +950,25 @@ Shape shape(const scout_attn_t &a, bool tensor) {
 bool worth_tensor(const scout_attn_t &a) { return a.q_len >= 96 && a.kv_len >= 96; }
 
 template <typename Args>
-cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t stream, const Args &args, bool dependent) {
+cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t stream, const Args &args, bool dependent, int cluster = 1) {
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)grid);
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
-    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cudaLaunchAttribute attr[2];
+    int n = 0;
+    if (dependent) {
+        attr[n].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+        attr[n++].val.programmaticStreamSerializationAllowed = 1;
+    }
+    if (cluster > 1) {
+        attr[n].id = cudaLaunchAttributeClusterDimension;
+        attr[n].val.clusterDim.x = cluster, attr[n].val.clusterDim.y = attr[n].val.clusterDim.z = 1;
+        ++n;
+    }
     cfg.attrs = attr;
-    cfg.numAttrs = dependent ? 1 : 0;
+    cfg.numAttrs = n;
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
@@ -923,7 +978,8 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
     const uint64_t blocks = s.q_tiles * f.p.batch * f.p.kv_heads * f.splits;
     if (s.few) {
         if (int rc = allow_smem<forward_few<T, HD>>(few_smem<HD>())) return rc;
-        SCOUT_CUDA(launch(forward_few<T, HD>, blocks, few_smem<HD>(), stream, f, false));
+        SCOUT_CUDA(launch(forward_few<T, HD>, blocks, few_smem<HD>(), stream, f, false, f.splits <= FEW_CLUSTER ? f.splits : 1));
+        if (f.splits <= FEW_CLUSTER) return SCOUT_OK;
     } else {
         constexpr int smem = 5 * TILE * HD * 2;
         if (int rc = allow_smem<forward_tiles<T, HD>>(smem)) return rc;
