@@ -933,8 +933,13 @@ Shape shape(const scout_attn_t &a, bool tensor) {
     }
     const uint64_t seen_by = a.window ? std::min<uint64_t>(a.q_len, (uint64_t)a.window + TILE) : a.q_len;
     if (tensor) {
-        s.q_splits = parts((a.q_len + 127) / 128 * bh * group, (seen + 127) / 128, 148, 3);
-        s.k_splits = parts((a.kv_len + 127) / 128 * bh, group * ((seen_by + 127) / 128), 148, 3);
+        // One launch for both: a block's chain of 128 x 128 steps is cut only where it is longer than an SM's share of all steps, and
+        // than 12 steps (below that the join costs more: 5 x 318 tokens, 32/8 heads of 128, 81 us with two parts, 65 with one)
+        const uint64_t qt = (a.q_len + 127) / 128, kt = (a.kv_len + 127) / 128;
+        const uint64_t q_chain = std::min(kt, (seen + 255) / 128), k_chain = group * std::min(qt, (seen_by + 255) / 128);
+        const uint64_t steps = bh * group * qt * q_chain * 2 / (a.causal && !a.window ? 2 : 1), share = std::max<uint64_t>(steps / 148, 12);
+        s.q_splits = (int)std::min<uint64_t>((q_chain + share - 1) / share, 64);
+        s.k_splits = (int)std::min<uint64_t>((k_chain + share - 1) / share, 64);
     } else {
         s.q_splits = parts(s.q_tiles * bh, (seen + TILE - 1) / TILE, 2 * 148, 4);
         s.k_splits = parts(s.k_tiles * bh, (group * seen_by + 31) / 32, 2 * 148, 8);

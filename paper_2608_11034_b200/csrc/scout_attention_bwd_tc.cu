@@ -149,8 +149,9 @@ template <typename F> __device__ __forceinline__ void to_p(uint32_t (&r)[2][32],
     }
     seen.hide(r);
 }
-// dP -> dS = P (dP - delta); minus(c): -delta of columns c .. c + 3.  A hidden place's dP may be anything.
-template <typename F> __device__ __forceinline__ void to_ds(uint32_t (&r)[2][32], const uint32_t (&w)[2][32], const Seen &seen, F minus) {
+// dP -> dS = P (dP - delta); minus(c): -delta of columns c .. c + 3.  At a hidden place P is 0, and so is dS unless its dP is NaN or
+// Inf, which shows in the row's result: such a row is made again from the definition.
+template <typename F> __device__ __forceinline__ void to_ds(uint32_t (&r)[2][32], const uint32_t (&w)[2][32], F minus) {
 #pragma unroll
     for (int c = 0; c < 64; c += 4) {
         uint32_t *v = &r[c >> 5][c & 31];
@@ -160,7 +161,6 @@ template <typename F> __device__ __forceinline__ void to_ds(uint32_t (&r)[2][32]
         const float2 z = tc::split(tc::mul2(tc::add2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), m.hi), tc::f2(__uint_as_float(q[2]), __uint_as_float(q[3]))));
         v[0] = __float_as_uint(y.x), v[1] = __float_as_uint(y.y), v[2] = __float_as_uint(z.x), v[3] = __float_as_uint(z.y);
     }
-    seen.hide(r);
 }
 // the 16-bit words of 64 columns
 template <typename T> __device__ __forceinline__ void round16(uint32_t (&x)[32], const uint32_t (&r)[2][32]) {
@@ -282,13 +282,18 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
     } else if (warp == 9) {
         const auto stage = [&](int r) { return ring + (r % STAGES) * L::TILE; };
         const auto landed = [&](int r) { return patience.wait_warp(full + 8 * (r % STAGES), (r / STAGES) & 1); };
+        // keys and values past the sequence, up to the tensor's end, may hold anything: they meet zeros in dQ and in dS
+        const auto clean = [&](int r) {
+            const int j0 = (blk0 + (r >> 1)) * ROWS;
+            if (n.nk < p.kv_len && j0 + ROWS > n.nk) clear_rows<HD>(stage(r), max(n.nk - j0, 0), lane);
+        };
         const auto issue_s = [&](int j) {
-            // keys past the sequence, up to the tensor's end, may hold anything: they are multiplied by zeros in dQ
-            if (n.nk < p.kv_len && (blk0 + j + 1) * ROWS > n.nk) clear_rows<HD>(stage(2 * j), max(n.nk - (blk0 + j) * ROWS, 0), lane);
+            clean(2 * j);
             product_tiles<T, HD>(tmem + S + (j & 1) * ROWS, sq, stage(2 * j));
             tc::mma_commit(s_full + 8 * (j & 1));  // a barrier to a tile: one of them may be two products ahead of its readers
         };
         const auto issue_dp = [&](int j) {
+            clean(2 * j + 1);
             product_tiles<T, HD>(tmem + DP, sg, stage(2 * j + 1));
             tc::mma_commit(dp_full);
             tc::mma_commit(empty + 8 * ((2 * j + 1) % STAGES));
@@ -339,7 +344,7 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
             if (!ok) break;
             tc::tc_fence_after();
             take(r, quarter + DP + wg * 64);
-            to_ds(r, w, seen, [&](int) { return Four{delta2, delta2}; });
+            to_ds(r, w, [&](int) { return Four{delta2, delta2}; });
             round16<T>(x, r);
             tc::tmem_store16(quarter + DP + wg * 64, x);  // over columns that have been read
             tc::tmem_store16(quarter + DP + wg * 64 + 16, x + 16);
@@ -540,7 +545,7 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::bar_arrive(dp_taken);
-            to_ds(r, w, seen, four(s_delta[st] + wg * 64));
+            to_ds(r, w, four(s_delta[st] + wg * 64));
             round16<T>(x, r);
             tc::tmem_store16(at_s + 32, x);
             tc::tmem_store16(at_s + 48, x + 16);

@@ -39,7 +39,8 @@ struct Args {
     int64_t per;  // tokens of a part, a multiple of BK
     int splits, tiles_i, tiles;
     int out_f32, accumulate;
-    int wide;  // rows of dw start on 32-byte boundaries
+    int wide;   // rows of dw start on 32-byte boundaries
+    int pairs;  // and on those of two elements
     uint32_t *gave_up;
 };
 
@@ -151,11 +152,18 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(con
 #pragma unroll
         for (int n = 0; n < 4; ++n)
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const int64_t o = o0 + wm + m * 16 + (lane >> 2) + 8 * (e >> 1), i = i0 + wn + n * 8 + (lane & 3) * 2 + (e & 1);
+            for (int e = 0; e < 4; e += 2) {
+                const int64_t o = o0 + wm + m * 16 + (lane >> 2) + 4 * e, i = i0 + wn + n * 8 + (lane & 3) * 2;
                 if (o >= a.outs || i >= a.ins) continue;
-                if (a.splits > 1) a.part[((int64_t)split * a.outs + o) * a.part_stride + i] = acc[m][n][e];
-                else put<T>(a, o, i, acc[m][n][e]);
+                if (a.splits > 1) {  // rows of parts are padded to eight columns
+                    *reinterpret_cast<float2 *>(&a.part[((int64_t)split * a.outs + o) * a.part_stride + i]) = make_float2(acc[m][n][e], acc[m][n][e + 1]);
+                } else if (a.pairs && !a.accumulate && i + 1 < a.ins) {
+                    if (a.out_f32) *reinterpret_cast<float2 *>(reinterpret_cast<float *>(a.dw) + o * a.dw_stride + i) = make_float2(acc[m][n][e], acc[m][n][e + 1]);
+                    else *reinterpret_cast<uint32_t *>(reinterpret_cast<T *>(a.dw) + o * a.dw_stride + i) = Half<T>::pack(acc[m][n][e], acc[m][n][e + 1]);
+                } else {
+                    put<T>(a, o, i, acc[m][n][e]);
+                    if (i + 1 < a.ins) put<T>(a, o, i + 1, acc[m][n][e + 1]);
+                }
             }
 }
 
@@ -373,8 +381,11 @@ Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
     t.bytes = t.part_bytes + (tensor ? (rows * t.x_stride * 2 + 255) & ~255ull : 0);
     return t;
 }
-// The restored copy costs a pass over memory and a launch: worth it from these sizes on.
-bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) { return rows >= TK && outs >= TM && ins >= 64; }
+// The restored copy costs a pass over memory and a launch: worth it from a step of tokens on, or where the outputs are many (56
+// tokens, 9456 x 2568: what is written bounds it, and wgrad_tiles writes 84 us).
+bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) {
+    return outs >= TM && ins >= 64 && (rows >= TK || (rows > 0 && outs * ins >= 1u << 20));
+}
 
 template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStream_t stream) {
     const int64_t join_grid = std::min<int64_t>((a.outs * a.part_stride + THREADS - 1) / THREADS, 148 * 8);
@@ -454,6 +465,7 @@ extern "C" int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t row
     a.per = t.per, a.part_stride = t.part_stride, a.splits = t.splits, a.tiles_i = (int)t.tiles_i, a.tiles = (int)(t.tiles_o * t.tiles_i);
     const uint64_t size = out_dtype == SCOUT_DT_F32 ? 4 : 2;
     a.wide = dw_stride * size % 32 == 0 && (reinterpret_cast<uintptr_t>(dw) & 31) == 0;
+    a.pairs = dw_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(dw) & (2 * size - 1)) == 0;
     void *restored = (uint8_t *)workspace + t.part_bytes;
     a.out_f32 = out_dtype == SCOUT_DT_F32, a.accumulate = (int)accumulate;
     return dtype == SCOUT_DT_BF16 ? run<__nv_bfloat16>(a, t, restored, (cudaStream_t)stream) : run<__half>(a, t, restored, (cudaStream_t)stream);

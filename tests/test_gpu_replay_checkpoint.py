@@ -129,7 +129,7 @@ def grad_bound(dy, x, want, out_dtype):
 @pytest.mark.parametrize("dtype,out", [(BF, F32), (BF, BF), (HF, F32), (HF, HF)])
 @pytest.mark.parametrize("rows,outs,ins", [(1, 1, 1), (1, 64, 64), (33, 40, 72), (64, 128, 256), (100, 130, 257), (259, 96, 520),
                                            (500, 257, 128), (1000, 8, 8), (3000, 136, 48), (31, 999, 33), (129, 384, 512),
-                                           (64, 128, 64), (65, 136, 67), (1030, 200, 264), (2500, 128, 300), (2049, 520, 1000), (5000, 1000, 72)])
+                                           (64, 128, 64), (65, 136, 67), (1030, 200, 264), (2500, 128, 300), (2049, 520, 1000), (5000, 1000, 72), (20, 1100, 1000), (1, 2048, 520)])
 def test_weight_gradient(dtype, out, rows, outs, ins):
     from paper_2608_11034_b200 import replay
     x = activation(rows + outs, rows, ins, dtype)
