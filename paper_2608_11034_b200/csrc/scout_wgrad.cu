@@ -39,7 +39,7 @@ struct Args {
     int64_t per;  // tokens of a part, a multiple of BK
     int splits, tiles_i, tiles;
     int out_f32, accumulate;
-    int wide;   // rows of dw start on 32-byte boundaries
+    int wide;   // rows of dw start on 16-byte (1) or 32-byte (2) boundaries
     int pairs;  // and on those of two elements
     uint32_t *gave_up;
 };
@@ -177,14 +177,19 @@ constexpr int TC_THREADS = 320, BOX = 64 * TK * 2, STAGE = (TM + TN) / 64 * BOX;
 constexpr int TURN = 32 * 33 * 4;  // a warp's 32 x 32 results on their way to rows of dw that start anywhere
 constexpr int TC_SMEM = STAGES * STAGE + 8 * TURN + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
 
-__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8]) {
-    asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
-                 "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+// 32 bytes of a thread, in one piece where they start on a 32-byte boundary (whole), else in two of 16
+__device__ __forceinline__ void store32(void *p, const uint32_t (&w)[8], bool whole = true) {
+    if (whole) {
+        asm volatile("st.global.v8.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8};" ::"l"(p), "r"(w[0]), "r"(w[1]), "r"(w[2]), "r"(w[3]), "r"(w[4]),
+                     "r"(w[5]), "r"(w[6]), "r"(w[7]) : "memory");
+    } else {
+        reinterpret_cast<uint4 *>(p)[0] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4 *>(p)[1] = make_uint4(w[4], w[5], w[6], w[7]);
+    }
 }
 __device__ __forceinline__ void load32(uint32_t (&w)[8], const void *p) {
-    asm volatile("ld.global.v8.b32 {%0,%1,%2,%3,%4,%5,%6,%7}, [%8];"
-                 : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]), "=r"(w[4]), "=r"(w[5]), "=r"(w[6]), "=r"(w[7])
-                 : "l"(p) : "memory");
+    const uint4 x = reinterpret_cast<const uint4 *>(p)[0], y = reinterpret_cast<const uint4 *>(p)[1];
+    w[0] = x.x, w[1] = x.y, w[2] = x.z, w[3] = x.w, w[4] = y.x, w[5] = y.y, w[6] = y.z, w[7] = y.w;
 }
 
 template <typename T>
@@ -305,7 +310,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                             if (a.accumulate) load32(w, dst + h);
 #pragma unroll
                             for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(a.accumulate ? __uint_as_float(w[e]) + sum[c + h + e] : sum[c + h + e]);
-                            store32(dst + h, w);
+                            store32(dst + h, w, a.wide == 2);
                         }
                     } else {
                         T *dst = reinterpret_cast<T *>(a.dw) + o * a.dw_stride + i0 + c;
@@ -315,7 +320,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) wgrad_tc(const __grid_constant_
                             const float2 was = a.accumulate ? Half<T>::unpack(w[e]) : make_float2(0.f, 0.f);
                             w[e] = Half<T>::pack(was.x + sum[c + 2 * e], was.y + sum[c + 2 * e + 1]);
                         }
-                        store32(dst, w);
+                        store32(dst, w, a.wide == 2);
                     }
                 }
             } else {
@@ -464,7 +469,8 @@ extern "C" int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t row
     a.rows = (int64_t)rows, a.outs = (int64_t)outs, a.ins = (int64_t)ins, a.blocks = (int64_t)((ins + SCOUT_CKPT_BLOCK - 1) / SCOUT_CKPT_BLOCK);
     a.per = t.per, a.part_stride = t.part_stride, a.splits = t.splits, a.tiles_i = (int)t.tiles_i, a.tiles = (int)(t.tiles_o * t.tiles_i);
     const uint64_t size = out_dtype == SCOUT_DT_F32 ? 4 : 2;
-    a.wide = dw_stride * size % 32 == 0 && (reinterpret_cast<uintptr_t>(dw) & 31) == 0;
+    const uintptr_t start = dw_stride * size | reinterpret_cast<uintptr_t>(dw);
+    a.wide = start % 32 == 0 ? 2 : start % 16 == 0 ? 1 : 0;
     a.pairs = dw_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(dw) & (2 * size - 1)) == 0;
     void *restored = (uint8_t *)workspace + t.part_bytes;
     a.out_f32 = out_dtype == SCOUT_DT_F32, a.accumulate = (int)accumulate;
