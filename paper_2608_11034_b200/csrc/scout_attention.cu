@@ -14,6 +14,7 @@
 // Where the grid would leave SMs idle (few rows, long keys) the long axis is split into parts of
 // fixed size; parts go to scratch in fp32 and a join kernel adds them in order.
 #include <algorithm>
+#include <cmath>
 
 #include "scout_attention.cuh"
 
@@ -914,7 +915,25 @@ struct Shape {
     bool few;
     uint64_t forward_bytes, stats_bytes, part_q_bytes, backward_bytes;
 };
-// tensor: the backward pass runs on tcgen05 (tiles of 128, one block an SM)
+// Parts of the tcgen05 forward pass's keys: the number that leaves the least estimated time, counted in steps (two slots, 128 keys; about
+// 1.7 us).  A block costs two steps beside its own; a join one and its traffic.  With equal blocks rounds of 148 count, with causal
+// ones, which go longest first, the mean and half of the longest.
+int forward_parts(const scout_attn_t &a, uint64_t seen) {
+    const bool pairs = a.q_heads / a.kv_heads % 2 == 0;
+    const uint64_t tiles = (a.q_len + (pairs ? 127 : 255)) / (pairs ? 128 : 256);
+    const double blocks = (double)tiles * a.batch * (pairs ? a.q_heads / 2 : a.q_heads), chain = (double)std::min<uint64_t>((a.kv_len + 127) / 128, (seen + 255) / 128);
+    const bool uneven = a.causal && !a.window && a.q_len > 256;
+    const double mean = uneven ? chain - 0.5 * std::min((double)(a.q_len / 128), chain) : chain, out = (double)a.batch * a.q_heads * a.q_len * a.head_dim * 4 / 11e6;
+    int best = 1;
+    double least = 0;
+    for (int s = 1; s <= 8 && s <= chain / 4 + 1; ++s) {
+        const double rounds = std::ceil(blocks * s / 148);
+        const double time = (uneven ? std::max(chain / s + 2, blocks * (mean + 2.0 * s) / 148 + 0.5 * chain / s) : rounds * (chain / s + 2)) + (s > 1 ? 1 + (s + 1) * out : 0);
+        if (s == 1 || time < 0.95 * least) best = s, least = time;
+    }
+    return best;
+}
+// tensor: on tcgen05 (tiles of 128, one block an SM)
 Shape shape(const scout_attn_t &a, bool tensor) {
     Shape s = {};
     const uint64_t group = a.q_heads / a.kv_heads, bh = (uint64_t)a.batch * a.kv_heads;
@@ -929,7 +948,7 @@ Shape shape(const scout_attn_t &a, bool tensor) {
         const uint64_t want = std::max<uint64_t>(3 * 148 / bh, 1), most = std::max<uint64_t>(key_tiles / 2, 1);
         s.f_splits = (int)std::min<uint64_t>(std::min(want, most), bh * FEW_CLUSTER >= 148 ? FEW_CLUSTER : 64);
     } else {
-        s.f_splits = parts(s.q_tiles * bh, key_tiles, 2 * 148, 4);
+        s.f_splits = tensor ? forward_parts(a, seen) : parts(s.q_tiles * bh, key_tiles, 2 * 148, 4);
     }
     const uint64_t seen_by = a.window ? std::min<uint64_t>(a.q_len, (uint64_t)a.window + TILE) : a.q_len;
     if (tensor) {
@@ -977,6 +996,11 @@ cudaError_t launch(void (*kernel)(Args), uint64_t grid, int smem, cudaStream_t s
     return cudaLaunchKernelEx(&cfg, kernel, args);
 }
 
+int join(const Shape &s, const ForwardArgs &f, bool bf16, cudaStream_t stream) {
+    SCOUT_CUDA(launch(bf16 ? forward_join<__nv_bfloat16> : forward_join<__half>, (s.rows + 3) / 4, 0, stream, f, true));
+    return SCOUT_OK;
+}
+
 template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaStream_t stream) {
     f.tiles = (int)s.q_tiles;
     f.splits = s.f_splits;
@@ -990,8 +1014,7 @@ template <typename T, int HD> int forward(const Shape &s, ForwardArgs &f, cudaSt
         if (int rc = allow_smem<forward_tiles<T, HD>>(smem)) return rc;
         SCOUT_CUDA(launch(forward_tiles<T, HD>, blocks, smem, stream, f, false));
     }
-    if (f.splits > 1) SCOUT_CUDA(launch(forward_join<T>, (s.rows + 3) / 4, 0, stream, f, true));
-    return SCOUT_OK;
+    return f.splits > 1 ? join(s, f, Half<T>::is_bf16, stream) : SCOUT_OK;
 }
 
 template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, const BackwardViews *maps, cudaStream_t stream) {
@@ -1030,9 +1053,11 @@ extern "C" int scout_attn_workspace(const scout_attn_t *a, uint64_t *forward_byt
     if (int rc = check(a)) return rc;
     if (!forward_bytes || !backward_bytes) return SCOUT_ERR_INVALID;
     const Shape s = shape(*a, false);
-    *forward_bytes = s.forward_bytes;
-    // enough for either kernel, so that the size does not depend on the pointers
-    *backward_bytes = std::max(s.backward_bytes, worth_tensor(*a) ? shape(*a, true).backward_bytes : 0);
+    *forward_bytes = s.forward_bytes, *backward_bytes = s.backward_bytes;
+    if (worth_tensor(*a)) {  // enough for either kernel, so that the size does not depend on the pointers
+        const Shape t = shape(*a, true);
+        *forward_bytes = std::max(*forward_bytes, t.forward_bytes), *backward_bytes = std::max(*backward_bytes, t.backward_bytes);
+    }
     return SCOUT_OK;
 }
 
@@ -1048,22 +1073,27 @@ extern "C" int scout_attn_forward(const scout_attn_t *a, const void *q, const vo
     if (!aligned(q, 16) || !aligned(k, 16) || !aligned(v, 16) || !aligned(o, 16) || !aligned(lse, 4) || !aligned(q_lens, 4) ||
         !aligned(kv_lens, 4) || !aligned(workspace, 256))
         return SCOUT_ERR_ALIGN;
-    if (workspace_bytes < s.forward_bytes || (s.forward_bytes && !workspace)) return SCOUT_ERR_INVALID;
+    uint64_t forward_bytes = 0, backward_bytes = 0;
+    if (int rc = scout_attn_workspace(a, &forward_bytes, &backward_bytes)) return rc;
+    if (workspace_bytes < forward_bytes || (forward_bytes && !workspace)) return SCOUT_ERR_INVALID;
     ForwardArgs f = {};
     f.p = problem(*a);
     f.p.q = q, f.p.k = k, f.p.v = v, f.p.q_lens = q_lens, f.p.kv_lens = kv_lens;
     f.o = o, f.lse = lse;
     f.part_o = (float *)workspace;
-    f.part_ml = (float2 *)((uint8_t *)workspace + up256(s.f_splits * s.rows * a->head_dim * 4));
-    const bool wide = a->head_dim > 64;
-    if (s.keys && s.f_splits == 1 && a->q_len >= 96) {
+    const auto ml = [&](int splits) { return (float2 *)((uint8_t *)workspace + up256(splits * s.rows * a->head_dim * 4)); };
+    const bool wide = a->head_dim > 64, bf16 = a->dtype == SCOUT_DT_BF16;
+    const cudaStream_t st = (cudaStream_t)stream;
+    if (worth_tensor(*a)) {
+        f.splits = shape(*a, true).f_splits;
+        f.part_ml = ml(f.splits);
         bool taken = false;
-        const int rc = forward_tensor(f.p, a->dtype == SCOUT_DT_BF16, o, lse, (cudaStream_t)stream, &taken);
-        if (rc || taken) return rc;
+        if (int rc = forward_tensor(f.p, bf16, o, lse, f.splits, f.part_o, f.part_ml, st, &taken)) return rc;
+        if (taken) return f.splits > 1 ? join(s, f, bf16, st) : SCOUT_OK;
     }
-    if (a->dtype == SCOUT_DT_BF16)
-        return wide ? forward<__nv_bfloat16, 128>(s, f, (cudaStream_t)stream) : forward<__nv_bfloat16, 64>(s, f, (cudaStream_t)stream);
-    return wide ? forward<__half, 128>(s, f, (cudaStream_t)stream) : forward<__half, 64>(s, f, (cudaStream_t)stream);
+    f.part_ml = ml(s.f_splits);
+    if (bf16) return wide ? forward<__nv_bfloat16, 128>(s, f, st) : forward<__nv_bfloat16, 64>(s, f, st);
+    return wide ? forward<__half, 128>(s, f, st) : forward<__half, 64>(s, f, st);
 }
 
 extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const void *k, const void *v, const void *o,

@@ -31,6 +31,9 @@ struct TcForwardArgs {
     uint32_t *gave_up;
     int tiles;       // row tiles (pairs of them without pair_heads) of a head
     int pair_heads;
+    int splits;      // parts of every item's keys; with more than one O and LSE leave as fp32 parts:
+    float *part_o;   // [splits][rows][head_dim], rows = batch * q_heads * q_len
+    float2 *part_ml; // [splits][rows] {m, l}
 };
 
 template <int HD> struct Layout {
@@ -75,9 +78,18 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                    o_done = p_full + 32, clean = o_done + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
-    const int h = blockIdx.x, b = blockIdx.y, tile = a.tiles - 1 - (int)blockIdx.z;  // the longest rows of a causal problem first
+    const int h = blockIdx.x, b = blockIdx.y, split = blockIdx.z % a.splits;
+    const int tile = a.tiles - 1 - (int)blockIdx.z / a.splits;  // the longest rows of a causal problem first
     const Lengths n = lengths(p, b);
-    const Slot slots[2] = {slot_of(a, n, tile, h, 0), slot_of(a, n, tile, h, 1)};
+    Slot slots[2] = {slot_of(a, n, tile, h, 0), slot_of(a, n, tile, h, 1)};
+    if (a.splits > 1) {
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int per = (slots[s].blk1 - slots[s].blk0 + a.splits - 1) / a.splits;
+            slots[s].blk0 = min(slots[s].blk0 + split * per, slots[s].blk1);
+            slots[s].blk1 = min(slots[s].blk0 + per, slots[s].blk1);
+        }
+    }
     const int hk = slots[0].head / p.group;
     const bool any0 = slots[0].blk0 < slots[0].blk1, any1 = slots[1].blk0 < slots[1].blk1;
     const int u0 = any0 && any1 ? min(slots[0].blk0, slots[1].blk0) : any0 ? slots[0].blk0 : slots[1].blk0;
@@ -283,53 +295,70 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             if (!sees) top = -CUDART_INF_F, sum = 0.f;
             const float inv = sum == 0.f ? 1.f : 1.f / sum;
             bool fine = finite(sum) && top != CUDART_INF_F;
-            // O leaves through the slot's Q tile, which the last product has read (32 rows of this warp, 64 elements wide each)
-            if (it == 0 && u0 < u1) ok = patience.wait_warp(q_full + 8 * s, 0);
-            const uint32_t out = base + s * L::TILE + (warp & 3) * 32 * 128;
-            const bool all_see = __all_sync(0xFFFFFFFFu, sees && it > 0);
-            const tc::F2 inv2 = tc::f2(inv, inv), zero2 = tc::f2(0.f, 0.f);
-            tc::F2 odd = zero2;  // stays 0 while every element is finite: 0 x is NaN otherwise
+            if (a.splits > 1) {
+                const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len, row = split * rows + ((int64_t)b * p.q_heads + sl.head) * p.q_len + i;
 #pragma unroll
-            for (int c = 0; c < HD / 32; ++c) {
-                uint32_t r[32], w[16];
-                tc::tmem_load32(r, at_o + c * 32);
-                tc::tmem_load_wait(r);
-                if (!all_see) {
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t r[32];
+                    tc::tmem_load32(r, at_o + c * 32);
+                    tc::tmem_load_wait(r);
 #pragma unroll
                     for (int e = 0; e < 32; ++e) r[e] = sees && it > 0 ? r[e] : 0u;
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4)
+                        if (mine && c * 32 + e < p.head_dim)
+                            *reinterpret_cast<uint4 *>(a.part_o + row * p.head_dim + c * 32 + e) = make_uint4(r[e], r[e + 1], r[e + 2], r[e + 3]);
                 }
+                if (mine) a.part_ml[row] = make_float2(top, sum);
+            } else {
+                // O leaves through the slot's Q tile, which the last product has read (32 rows of this warp, 64 elements wide each)
+                if (it == 0 && u0 < u1) ok = patience.wait_warp(q_full + 8 * s, 0);
+                const uint32_t out = base + s * L::TILE + (warp & 3) * 32 * 128;
+                const bool all_see = __all_sync(0xFFFFFFFFu, sees && it > 0);
+                const tc::F2 inv2 = tc::f2(inv, inv), zero2 = tc::f2(0.f, 0.f);
+                tc::F2 odd = zero2;  // stays 0 while every element is finite: 0 x is NaN otherwise
 #pragma unroll
-                for (int e = 0; e < 16; ++e) {
-                    const tc::F2 x = tc::f2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
-                    odd = tc::fma2(x, zero2, odd);
-                    const float2 y = tc::split(tc::mul2(x, inv2));
-                    w[e] = Half<T>::pack(y.x, y.y);
+                for (int c = 0; c < HD / 32; ++c) {
+                    uint32_t r[32], w[16];
+                    tc::tmem_load32(r, at_o + c * 32);
+                    tc::tmem_load_wait(r);
+                    if (!all_see) {
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) r[e] = sees && it > 0 ? r[e] : 0u;
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const tc::F2 x = tc::f2(__uint_as_float(r[2 * e]), __uint_as_float(r[2 * e + 1]));
+                        odd = tc::fma2(x, zero2, odd);
+                        const float2 y = tc::split(tc::mul2(x, inv2));
+                        w[e] = Half<T>::pack(y.x, y.y);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; e += 4)
+                        tc::store_shared16(tc::swizzled(out + (c >> 1) * L::SUB, lane, (c & 1) * 4 + e / 4), w[e], w[e + 1], w[e + 2], w[e + 3]);
                 }
+                fine = fine && tc::split(odd).x == 0.f && tc::split(odd).y == 0.f;
+                tc::fence_async();
+                __syncwarp();
+                if (lane == 0) {
 #pragma unroll
-                for (int e = 0; e < 16; e += 4)
-                    tc::store_shared16(tc::swizzled(out + (c >> 1) * L::SUB, lane, (c & 1) * 4 + e / 4), w[e], w[e + 1], w[e + 2], w[e + 3]);
-            }
-            fine = fine && tc::split(odd).x == 0.f && tc::split(odd).y == 0.f;
-            tc::fence_async();
-            __syncwarp();
-            if (lane == 0) {
-#pragma unroll
-                for (int c = 0; c < HD / 64; ++c)
-                    if (i < p.q_len && c * 64 < p.head_dim) tc::tma_store_4d(&map_o, out + c * L::SUB, c * 64, i, sl.head, b);
-                tc::tma_store_commit();
-            }
-            if (mine)
-                a.lse[((int64_t)b * p.q_heads + sl.head) * p.q_len + i] = top == -CUDART_INF_F ? -CUDART_INF_F : (top + log2f(sum)) * LN2;
-            uint32_t redo = __ballot_sync(0xFFFFFFFFu, mine && !fine);
-            if (lane == 0) {
-                if (redo) tc::tma_stored();
-                else tc::tma_store_read();
-            }
-            __syncwarp();
-            while (redo) {
-                const int r = __ffs(redo) - 1;
-                redo &= redo - 1;
-                row_forward<T>(p, b, sl.head, sl.row0 + (warp & 3) * 32 + r, a.o, a.lse);
+                    for (int c = 0; c < HD / 64; ++c)
+                        if (i < p.q_len && c * 64 < p.head_dim) tc::tma_store_4d(&map_o, out + c * L::SUB, c * 64, i, sl.head, b);
+                    tc::tma_store_commit();
+                }
+                if (mine)
+                    a.lse[((int64_t)b * p.q_heads + sl.head) * p.q_len + i] = top == -CUDART_INF_F ? -CUDART_INF_F : (top + log2f(sum)) * LN2;
+                uint32_t redo = __ballot_sync(0xFFFFFFFFu, mine && !fine);
+                if (lane == 0) {
+                    if (redo) tc::tma_stored();
+                    else tc::tma_store_read();
+                }
+                __syncwarp();
+                while (redo) {
+                    const int r = __ffs(redo) - 1;
+                    redo &= redo - 1;
+                    row_forward<T>(p, b, sl.head, sl.row0 + (warp & 3) * 32 + r, a.o, a.lse);
+                }
             }
         }
     }
@@ -341,13 +370,14 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-template <typename T, int HD> int run_forward(const Problem &p, void *o, float *lse, const CUtensorMap (&m)[4], cudaStream_t stream) {
-    TcForwardArgs a = {p, o, lse, nullptr, 0, 0};
+template <typename T, int HD>
+int run_forward(const Problem &p, void *o, float *lse, int splits, float *part_o, float2 *part_ml, const CUtensorMap (&m)[4], cudaStream_t stream) {
+    TcForwardArgs a = {p, o, lse, nullptr, 0, 0, splits, part_o, part_ml};
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     a.pair_heads = p.group % 2 == 0;
     const int rows = a.pair_heads ? ROWS : 2 * ROWS;
     a.tiles = (p.q_len + rows - 1) / rows;
-    const dim3 blocks(a.pair_heads ? p.q_heads / 2 : p.q_heads, p.batch, a.tiles);
+    const dim3 blocks(a.pair_heads ? p.q_heads / 2 : p.q_heads, p.batch, a.tiles * splits);
     if (int rc = allow_smem<forward_tc<T, HD>>(Layout<HD>::SMEM)) return rc;
     forward_tc<T, HD><<<blocks, TC_THREADS, Layout<HD>::SMEM, stream>>>(a, m[0], m[1], m[2], m[3]);
     SCOUT_CUDA(cudaGetLastError());
@@ -367,14 +397,14 @@ bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, con
     return tc::tensor_map(m, bf16, x, 4, dims, strides, box) == SCOUT_OK;
 }
 
-int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, cudaStream_t stream, bool *taken) {
+int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, int splits, float *part_o, float2 *part_ml, cudaStream_t stream, bool *taken) {
     CUtensorMap m[4];
-    *taken = p.batch < 65536 && p.q_len < 65536 * ROWS && tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
+    *taken = p.batch < 65536 && p.q_len < 65535 / splits * ROWS && tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
              tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS) && tensor_view(&m[3], bf16, o, p.so, p, p.q_len, p.q_heads, 32);
     if (!*taken) return SCOUT_OK;
     if (p.head_dim > 64)
-        return bf16 ? run_forward<__nv_bfloat16, 128>(p, o, lse, m, stream) : run_forward<__half, 128>(p, o, lse, m, stream);
-    return bf16 ? run_forward<__nv_bfloat16, 64>(p, o, lse, m, stream) : run_forward<__half, 64>(p, o, lse, m, stream);
+        return bf16 ? run_forward<__nv_bfloat16, 128>(p, o, lse, splits, part_o, part_ml, m, stream) : run_forward<__half, 128>(p, o, lse, splits, part_o, part_ml, m, stream);
+    return bf16 ? run_forward<__nv_bfloat16, 64>(p, o, lse, splits, part_o, part_ml, m, stream) : run_forward<__half, 64>(p, o, lse, splits, part_o, part_ml, m, stream);
 }
 
 }  // namespace attn

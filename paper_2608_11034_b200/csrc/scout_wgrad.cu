@@ -389,7 +389,7 @@ Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
 // The restored copy costs a pass over memory and a launch: worth it from a step of tokens on, or where the outputs are many (56
 // tokens, 9456 x 2568: what is written bounds it, and wgrad_tiles writes 84 us).
 bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) {
-    return outs >= TM && ins >= 64 && (rows >= TK || (rows > 0 && outs * ins >= 1u << 20));
+    return outs >= 64 && ins >= 64 && (rows >= TK || (rows > 0 && outs * ins >= 1u << 20));
 }
 
 template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStream_t stream) {

@@ -67,6 +67,8 @@ SIZES = [  # B, Tq, Tk, Hq, Hk, D, causal, window
     (1, 7, 4000, 4, 1, 96, True, 0),
     (1, 2000, 9, 2, 2, 64, False, 0),       # few keys, many rows
     (1, 1100, 1100, 2, 1, 128, False, 0),
+    (1, 3000, 3000, 1, 1, 64, True, 0),     # one head: its keys go in parts
+    (2, 130, 2600, 1, 1, 128, False, 0),
 ]
 
 
