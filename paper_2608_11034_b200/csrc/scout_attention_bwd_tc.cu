@@ -104,24 +104,6 @@ struct Seen {
         }
     }
 };
-// 2^x of two numbers by multiply-adds, beside the special function unit (four lanes a cycle): of a row's 32 pairs of exponentials SHARE
-// are made this way (0: 244, 4: 240, 6: 238.5, 8: 239, 12: 252 us for 2 x 2048 tokens, 32/8 heads of 128, causal).  Cody-Waite: x = n + f with n the nearest integer, which adding 1.5 2^23 leaves in the low
-// bits, and 2^f on [-1/2, 1/2] by the polynomial of degree 4 of least maximal relative error (Remez exchange; 2.7e-6, far
-// below the 2^-9 or 2^-12 that P is rounded to).  What lies below 2^-126 comes out as 2^-126.
-constexpr int SHARE = 6;
-__device__ __forceinline__ float2 exp2_fma(tc::F2 x) {
-    const float2 lim = tc::split(x);
-    const tc::F2 y = tc::f2(fmaxf(lim.x, -126.f), fmaxf(lim.y, -126.f)), magic = tc::f2(12582912.f, 12582912.f);
-    const tc::F2 t = tc::add2(y, magic), n = tc::add2(t, tc::f2(-12582912.f, -12582912.f)), f = tc::fma2(n, tc::f2(-1.f, -1.f), y);
-    tc::F2 p = tc::f2(0.009570102207362652f, 0.009570102207362652f);
-    p = tc::fma2(p, f, tc::f2(0.05591785907745361f, 0.05591785907745361f));
-    p = tc::fma2(p, f, tc::f2(0.240247443318367f, 0.240247443318367f));
-    p = tc::fma2(p, f, tc::f2(0.6931217908859253f, 0.6931217908859253f));
-    p = tc::fma2(p, f, tc::f2(0.9999992847442627f, 0.9999992847442627f));
-    const float2 m = tc::split(p), e = tc::split(t);
-    return make_float2(__uint_as_float(__float_as_uint(m.x) + (__float_as_uint(e.x) << 23)),
-                       __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
-}
 // what is added to columns c .. c + 3: one number for the row, or four of a table in shared memory (16-byte loads: all lanes read
 // the same, and a load of 4 bytes occupies shared memory as long)
 struct Four {

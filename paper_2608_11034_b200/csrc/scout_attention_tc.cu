@@ -13,6 +13,7 @@
 // Bounds: per 128 keys and two slots the products take 2048 cycles (HD = 128), the 32768 exponentials 2048 cycles of the
 // special function units.
 #include <algorithm>
+#include <type_traits>
 
 #include "scout_attention.cuh"
 #include "scout_tc.cuh"
@@ -267,24 +268,29 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
             const float minus = top == -CUDART_INF_F ? 0.f : -top;
             const tc::F2 scale2 = tc::f2(p.scale_log2, p.scale_log2), minus2 = tc::f2(minus, minus);
             tc::F2 part[2] = {tc::f2(0.f, 0.f), tc::f2(0.f, 0.f)};
+            const auto weights = [&](auto every) {  // every: no hidden place among the 128 (those have to come out as 0)
 #pragma unroll
-            for (int c = 0; c < 4; ++c) {
-                uint32_t w[16];
+                for (int c = 0; c < 4; ++c) {
+                    uint32_t w[16];
 #pragma unroll
-                for (int e = 0; e < 32; e += 2) {
-                    const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(r[c][e]), __uint_as_float(r[c][e + 1])), scale2, minus2));
-                    const float2 v = make_float2(exp2_fast(y.x), exp2_fast(y.y));
-                    part[(e >> 1) & 1] = tc::add2(part[(e >> 1) & 1], tc::f2(v.x, v.y));
-                    w[e / 2] = Half<T>::pack(v.x, v.y);
+                    for (int e = 0; e < 16; ++e) {
+                        const tc::F2 y = tc::fma2(tc::f2(__uint_as_float(r[c][2 * e]), __uint_as_float(r[c][2 * e + 1])), scale2, minus2);
+                        const bool fma = decltype(every)::value && e * SHARE % 16 + SHARE >= 16;  // spread evenly
+                        const float2 v = fma ? exp2_fma(y) : make_float2(exp2_fast(tc::split(y).x), exp2_fast(tc::split(y).y));
+                        part[e & 1] = tc::add2(part[e & 1], tc::f2(v.x, v.y));
+                        w[e] = Half<T>::pack(v.x, v.y);
+                    }
+                    tc::tmem_store16(at_s + c * 16, w);  // over columns that have been read
+                    if (c & 1) {  // half of the keys: their product can start
+                        tc::tmem_store_wait();
+                        tc::tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) tc::bar_arrive(p_full + 16 * s + 8 * (c >> 1));
+                    }
                 }
-                tc::tmem_store16(at_s + c * 16, w);  // over columns that have been read
-                if (c & 1) {  // half of the keys: their product can start
-                    tc::tmem_store_wait();
-                    tc::tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) tc::bar_arrive(p_full + 16 * s + 8 * (c >> 1));
-                }
-            }
+            };
+            if (whole) weights(std::true_type{});
+            else weights(std::false_type{});
             const float2 all = tc::split(tc::add2(part[0], part[1]));
             sum += all.x + all.y;
         }
