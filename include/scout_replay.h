@@ -40,6 +40,10 @@ extern "C" {
  * lse = -inf, and contributes nothing to any gradient.  What stands in keys, values,
  * queries or gradients that a row does not see never reaches it, NaN and Inf included.
  *
+ * Sizes: batch * q_heads * q_len and batch * kv_heads * kv_len up to 2^30, batch * q_heads
+ * up to 2^24, head_dim up to 128; beyond that SCOUT_ERR_UNSUPPORTED.  Element offsets are
+ * 64-bit.
+ *
  * Products are taken of the 16-bit inputs with fp32 sums; the probabilities (and in the
  * backward pass dS) are rounded to the inputs' type for their products; the softmax
  * statistics stay in fp32.  fp16 gradients should be loss-scaled as usual: dS below

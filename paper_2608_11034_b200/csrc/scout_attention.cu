@@ -488,55 +488,41 @@ struct BackwardArgs {
 };
 
 // delta = g . o, and the row statistic on powers of two.  A row that sees nothing gets +inf: its probabilities come out 0.
-// One pass over o and g, 16 bytes a lane, half a warp to a row, four rows of a half warp in flight.
-constexpr int STAT_ROWS = 4 * THREADS / 16;
+// One pass over o and g, 16 bytes a lane, half a warp to a row, a token's heads to a block (32 of them in flight together): what is
+// the same for all heads is worked out once.
 template <typename T>
 __global__ void __launch_bounds__(THREADS) backward_stats(const __grid_constant__ BackwardArgs a) {
     const Problem &p = a.p;
     pdl_launch_dependents();
-    const int64_t rows = (int64_t)p.batch * p.q_heads * p.q_len;
-    const int lane = threadIdx.x & 15, d = lane * 8;
-    const T *po[4], *pg[4];
-    int64_t at[4];
-    bool ok[4];
+    const int b = blockIdx.x / p.q_len, i = blockIdx.x - b * p.q_len, lane = threadIdx.x & 15, d = lane * 8, h0 = threadIdx.x >> 4;
+    const Lengths n = lengths(p, b);
+    const bool sees = row_hi(p, n, i) > row_lo(p, n, i), in = sees && d < p.head_dim;
+    const T *po = RowIO<T>::at(p.o, p.so, b, i, 0) + d, *pg = RowIO<T>::at(p.d_o, p.sg, b, i, 0) + d;
+    for (int h = h0; h < p.q_heads; h += 4 * THREADS / 16) {
+        float4 o[4], g[4];
+        float lse[4];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const int64_t x = min((int64_t)blockIdx.x * STAT_ROWS + u * (THREADS / 16) + (threadIdx.x >> 4), rows);  // heads adjacent in memory
-        const int64_t y = min(x, rows - 1);
-        int hq, i, b;
-        if (rows <= 0x7FFFFFFF) {
-            const uint32_t z = (uint32_t)y, t = z / (uint32_t)p.q_heads;
-            hq = z - t * p.q_heads, b = t / (uint32_t)p.q_len, i = t - b * p.q_len;
-        } else {
-            hq = y % p.q_heads, i = y / p.q_heads % p.q_len, b = (int)(y / p.q_heads / p.q_len);
-        }
-        at[u] = x < rows ? ((int64_t)b * p.q_heads + hq) * p.q_len + i : -1;
-        po[u] = RowIO<T>::at(p.o, p.so, b, i, hq) + d, pg[u] = RowIO<T>::at(p.d_o, p.sg, b, i, hq) + d;
-        const Lengths n = lengths(p, b);
-        ok[u] = x < rows && row_hi(p, n, i) > row_lo(p, n, i);
-    }
-    float4 o[4], g[4];
-    float lse[4];
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {  // nothing between the loads
-        const bool in = ok[u] && d < p.head_dim;
-        o[u] = in ? __ldg(reinterpret_cast<const float4 *>(po[u])) : make_float4(0.f, 0.f, 0.f, 0.f);
-        g[u] = in ? __ldg(reinterpret_cast<const float4 *>(pg[u])) : make_float4(0.f, 0.f, 0.f, 0.f);
-        lse[u] = ok[u] ? a.lse[at[u]] : -CUDART_INF_F;
-    }
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        const uint32_t *x = reinterpret_cast<const uint32_t *>(&o[u]), *y = reinterpret_cast<const uint32_t *>(&g[u]);
-        float dot = 0.f;
-#pragma unroll
-        for (int c = 0; c < 4; ++c) {
-            const float2 v = Half<T>::unpack(x[c]), w = Half<T>::unpack(y[c]);
-            dot = fmaf(v.x, w.x, fmaf(v.y, w.y, dot));
+        for (int u = 0; u < 4; ++u) {  // nothing between the loads
+            const int hq = h + u * (THREADS / 16);
+            const bool ok = in && hq < p.q_heads;
+            o[u] = ok ? __ldg(reinterpret_cast<const float4 *>(po + hq * p.so.h)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            g[u] = ok ? __ldg(reinterpret_cast<const float4 *>(pg + hq * p.sg.h)) : make_float4(0.f, 0.f, 0.f, 0.f);
+            lse[u] = sees && hq < p.q_heads ? a.lse[((int64_t)b * p.q_heads + hq) * p.q_len + i] : -CUDART_INF_F;
         }
 #pragma unroll
-        for (int m = 8; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m);
-        if (lane == 0 && at[u] >= 0) {
-            a.stats[at[u]] = lse[u] == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(lse[u] * LOG2E, dot);
+        for (int u = 0; u < 4; ++u) {
+            const uint32_t *x = reinterpret_cast<const uint32_t *>(&o[u]), *y = reinterpret_cast<const uint32_t *>(&g[u]);
+            float dot = 0.f;
+#pragma unroll
+            for (int c = 0; c < 4; ++c) {
+                const float2 v = Half<T>::unpack(x[c]), w = Half<T>::unpack(y[c]);
+                dot = fmaf(v.x, w.x, fmaf(v.y, w.y, dot));
+            }
+#pragma unroll
+            for (int m = 8; m; m >>= 1) dot += __shfl_xor_sync(0xFFFFFFFFu, dot, m, 16);
+            const int hq = h + u * (THREADS / 16);
+            if (lane == 0 && hq < p.q_heads)
+                a.stats[((int64_t)b * p.q_heads + hq) * p.q_len + i] = lse[u] == -CUDART_INF_F ? make_float2(CUDART_INF_F, 0.f) : make_float2(lse[u] * LOG2E, dot);
         }
     }
 }
@@ -868,10 +854,9 @@ int check(const scout_attn_t *a) {
     if (!a->batch || !a->q_heads || !a->kv_heads || a->q_heads % a->kv_heads || !a->head_dim) return SCOUT_ERR_INVALID;
     if (a->head_dim % 8 || a->head_dim > 128) return SCOUT_ERR_UNSUPPORTED;
     if (a->causal > 1 || (a->window && !a->causal) || !(a->scale > 0.f) || !(a->scale <= 3.402823466e38f)) return SCOUT_ERR_INVALID;
-    // row and key numbers, and packed rows, are 32-bit; grids are one-dimensional
-    const uint64_t group = a->q_heads / a->kv_heads;
-    if (a->q_len > (1u << 30) || a->kv_len > (1u << 30) || a->window > (1u << 30) || group * a->q_len > (1ull << 30) ||
-        (uint64_t)a->batch * a->q_heads > (1u << 24))
+    // rows and keys are numbered in 31 bits (their elements in 64), and so are blocks
+    if (a->q_len > (1u << 30) || a->kv_len > (1u << 30) || a->window > (1u << 30) || (uint64_t)a->batch * a->q_heads > (1u << 24) ||
+        (uint64_t)a->batch * a->q_heads * a->q_len > (1ull << 30) || (uint64_t)a->batch * a->kv_heads * a->kv_len > (1ull << 30))
         return SCOUT_ERR_UNSUPPORTED;
     const uint32_t t[2] = {a->q_len, a->kv_len}, h[2] = {a->q_heads, a->kv_heads};
     const uint64_t *s[5] = {a->q_stride, a->o_stride, a->do_stride, a->k_stride, a->v_stride};
@@ -1022,7 +1007,7 @@ template <typename T, int HD> int backward(const Shape &s, BackwardArgs &a, cons
     const uint64_t bh = (uint64_t)a.p.batch * a.p.kv_heads;
     a.q_splits = s.rows ? s.q_splits : 1, a.kv_splits = s.keys ? s.k_splits : 1;
     // every kernel waits for the whole of the one before it (griddepcontrol.wait), which has waited for its own predecessor
-    if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (s.rows + STAT_ROWS - 1) / STAT_ROWS, 0, stream, a, false));
+    if (s.rows) SCOUT_CUDA(launch(backward_stats<T>, (uint64_t)a.p.batch * a.p.q_len, 0, stream, a, false));
     if (maps) {
         if (int rc = backward_tensor(a.p, Half<T>::is_bf16, a.stats, a.dq, a.dk, a.dv, a.part_q, a.q_splits, a.part_kv, a.kv_splits, *maps, stream)) return rc;
     } else {

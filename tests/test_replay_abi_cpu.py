@@ -28,7 +28,7 @@ def attn(**kw):
     (dict(head_dim=0), binding.ERR_INVALID), (dict(head_dim=136), binding.ERR_UNSUPPORTED), (dict(head_dim=20), binding.ERR_UNSUPPORTED),
     (dict(causal=2), binding.ERR_INVALID), (dict(causal=0, window=5), binding.ERR_INVALID), (dict(scale=0.0), binding.ERR_INVALID),
     (dict(scale=-1.0), binding.ERR_INVALID), (dict(scale=float("nan")), binding.ERR_INVALID), (dict(scale=float("inf")), binding.ERR_INVALID),
-    (dict(q_len=2 ** 31), binding.ERR_UNSUPPORTED), (dict(kv_len=2 ** 31), binding.ERR_UNSUPPORTED),
+    (dict(q_len=2 ** 31), binding.ERR_UNSUPPORTED), (dict(q_len=2 ** 28), binding.ERR_UNSUPPORTED), (dict(kv_len=2 ** 31), binding.ERR_UNSUPPORTED),
     (dict(k_stride=(6144, 0, 64)), binding.ERR_INVALID), (dict(v_stride=(6144, 132, 64)), binding.ERR_ALIGN),
     (dict(do_stride=(8192, 256, 65)), binding.ERR_ALIGN)])
 def test_attention_descriptions_are_checked(kw, code):
