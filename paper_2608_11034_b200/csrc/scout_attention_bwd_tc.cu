@@ -14,6 +14,10 @@
 //
 // One kernel that added dQ from blocks of keys would need 5 products instead of 4 + 3, but its sums would cross blocks:
 // float atomics give other bits on every run, and these gradients are compared bit by bit.
+//
+// What bounds it (HD = 128): dK, dV 2048 cycles of products a step, 288 KiB through shared memory (2250 cycles); dQ 1536 and 224 KiB (1750), 1927
+// measured.  2 x 2048 tokens, 32/8 heads, causal: 221 us with the statistics, 0.78 PFLOP/s of the five products that are asked for, 1.09
+// of the seven that are made.
 #include <algorithm>
 
 #include "scout_attention.cuh"

@@ -84,8 +84,8 @@ __device__ __forceinline__ Place place(const Args &a, uint32_t g) {
 }
 
 // ---- rows on 16-byte boundaries whose length is a multiple of 8 -----------------------------------
-// A lane holds eight elements, four lanes a block; UNROLL groups of a warp are in flight together.  16384 x 14336 bf16:
-// see the launch comment below for what it reaches.
+// A lane holds eight elements, four lanes a block; UNROLL groups of a warp are in flight together.  16384 x 14336 bf16 packed
+// and restored: 232 us, 6.1 TB/s (a warp instruction per block, a lane per element: 1578).
 constexpr int UNROLL = 4;
 template <typename T> struct Eight {
     static constexpr int N = sizeof(T) / 2;  // 16-byte loads
