@@ -79,21 +79,19 @@ def _lens(x, batch, device, name) -> int:
     return x.data_ptr()
 
 
-def _scratch(nbytes, x):
-    return x.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
-
-
-def _enqueue(index: int, call, *args) -> None:
-    """call(*args, stream) with the tensors' device current, on its current stream"""
-    now = torch.cuda.current_device()
+def _enqueue(name: str, index: int, *args) -> None:
+    """The library's call `name` with args and the current stream of the tensors' device, which is made current for it."""
+    now = torch._C._cuda_getDevice()
     if now == index:
-        call(*args, torch._C._cuda_getCurrentRawStream(index))
-        return
-    torch.cuda.set_device(index)
-    try:
-        call(*args, torch._C._cuda_getCurrentRawStream(index))
-    finally:
-        torch.cuda.set_device(now)
+        rc = getattr(binding.lib(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+    else:
+        torch.cuda.set_device(index)
+        try:
+            rc = getattr(binding.lib(), name)(*args, torch._C._cuda_getCurrentRawStream(index))
+        finally:
+            torch.cuda.set_device(now)
+    if rc:
+        raise binding.ScoutError(rc, name)
 
 
 def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, causal: bool = False, window: int = 0,
@@ -108,13 +106,14 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     q_lens, kv_lens: int32 [batch], the tokens in use of padded sequences.
     -> (o like q, lse float32 [batch, q_heads, q_len]); rows that see nothing give 0 and -inf."""
     o = torch.empty_like(q)
-    t = _attention((q.dtype, k.dtype, v.dtype), (q.device, k.device, v.device), q.shape, k.shape, v.shape, q.shape, q.shape,
-                   q.stride(), k.stride(), v.stride(), o.stride(), o.stride(), causal, window, scale)
+    shape = q.shape
+    t = _attention((q.dtype, k.dtype, v.dtype), (q.device, k.device, v.device), shape, k.shape, v.shape, shape, shape,
+                   q.stride(), k.stride(), v.stride(), o.stride(), o.stride(), causal, window, scale if scale is None else float(scale))
     lse = q.new_empty(t.rows, dtype=torch.float32)
     ql, kl = _lens(q_lens, t.batch, q.device, "q_lens"), _lens(kv_lens, t.batch, q.device, "kv_lens")
-    ws = _scratch(t.forward_bytes, q)
-    _enqueue(t.index, binding.scout_attn_forward, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(),
-             lse.data_ptr(), ws.data_ptr() if ws is not None else 0, t.forward_bytes)
+    ws = q.new_empty(t.forward_bytes, dtype=torch.uint8) if t.forward_bytes else None
+    _enqueue("scout_attn_forward", t.index, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), ql, kl, o.data_ptr(), lse.data_ptr(),
+             ws.data_ptr() if ws is not None else 0, t.forward_bytes)
     return o, lse
 
 
@@ -126,7 +125,7 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     summed over those.  -> (dq, dk, dv), laid out like q, k, v."""
     t = _attention((q.dtype, k.dtype, v.dtype, o.dtype, do.dtype), (q.device, k.device, v.device, o.device, do.device), q.shape,
                    k.shape, v.shape, o.shape, do.shape, q.stride(), k.stride(), v.stride(), o.stride(), do.stride(), causal, window,
-                   scale)
+                   scale if scale is None else float(scale))
     dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
     for x, y, name in ((q, dq, "q"), (k, dk, "k"), (v, dv, "v")):
         if x.stride() != y.stride():
@@ -134,76 +133,89 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     if lse.dtype != torch.float32 or lse.shape != t.rows or not lse.is_contiguous() or lse.device != q.device:
         _fail("lse: the forward pass's, a contiguous float32 tensor [batch, q_heads, q_len]")
     ql, kl = _lens(q_lens, t.batch, q.device, "q_lens"), _lens(kv_lens, t.batch, q.device, "kv_lens")
-    ws = _scratch(t.backward_bytes, q)
-    _enqueue(t.index, binding.scout_attn_backward, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
+    ws = q.new_empty(t.backward_bytes, dtype=torch.uint8) if t.backward_bytes else None
+    _enqueue("scout_attn_backward", t.index, t.at, q.data_ptr(), k.data_ptr(), v.data_ptr(), o.data_ptr(), lse.data_ptr(),
              do.data_ptr(), ql, kl, dq.data_ptr(), dk.data_ptr(), dv.data_ptr(), ws.data_ptr() if ws is not None else 0,
              t.backward_bytes)
     return dq, dk, dv
 
 
-def _matrix(x, name):
-    if x.dim() != 2 or (x.shape[1] > 1 and x.stride(1) != 1) or (x.shape[0] > 1 and x.stride(0) < x.shape[1]):
+def _row_stride(shape, stride, device, name) -> int:
+    if len(shape) != 2 or (shape[1] > 1 and stride[1] != 1) or (shape[0] > 1 and stride[0] < shape[1]):
         _fail(f"{name}: a matrix with adjacent row elements is wanted")
-    if not x.is_cuda:
+    if device.type != "cuda":
         _fail("tensors must be on a CUDA device")
-    return max(x.stride(0), x.shape[1], 1)
+    return max(stride[0], shape[1], 1)
 
 
-def _checkpoint(codes, exps):
-    stride = _matrix(codes, "codes")
-    rows, cols = codes.shape
-    if codes.dtype != torch.int8 or exps.dtype != torch.int8 or not exps.is_contiguous() or exps.device != codes.device or \
-            exps.shape != (rows, -(-cols // binding.CKPT_BLOCK)):
+@functools.lru_cache(maxsize=1024)
+def _activation(shape, stride, dtype, device):
+    """Checks a description of x (sizes only) -> its type's code, rows, columns, row stride, shape of the exponents."""
+    if dtype not in _CODE:
+        _fail("activations are float32, bfloat16 or float16")
+    row = _row_stride(shape, stride, device, "x")
+    return _CODE[dtype], shape[0], shape[1], row, (shape[0], -(-shape[1] // binding.CKPT_BLOCK))
+
+
+@functools.lru_cache(maxsize=1024)
+def _checkpoint(shape, stride, dtype, device, exps_shape, exps_stride, exps_dtype, exps_device):
+    """Checks a description of a checkpoint -> rows, columns, row stride of the codes."""
+    row = _row_stride(shape, stride, device, "codes")
+    blocks = -(-shape[1] // binding.CKPT_BLOCK)
+    if dtype != torch.int8 or exps_dtype != torch.int8 or exps_device != device or exps_shape != (shape[0], blocks) or \
+            (shape[0] > 1 and blocks > 0 and exps_stride[0] != blocks) or (blocks > 1 and exps_stride[1] != 1):
         _fail("codes: int8 [rows, cols], exps: contiguous int8 [rows, ceil(cols / 32)]")
-    return rows, cols, stride
+    return shape[0], shape[1], row
 
 
 def checkpoint_pack(x: torch.Tensor):
     """Hold the activation x [rows, cols] (float32, bfloat16 or float16) in 8 bits.
     -> (codes int8 [rows, cols], exps int8 [rows, ceil(cols / 32)]): x is about codes * 2**exps, exps per block of 32 columns."""
-    stride = _matrix(x, "x")
-    if x.dtype not in _CODE:
-        _fail("activations are float32, bfloat16 or float16")
-    rows, cols = x.shape
-    codes = x.new_empty((rows, cols), dtype=torch.int8)
-    exps = x.new_empty((rows, -(-cols // binding.CKPT_BLOCK)), dtype=torch.int8)
-    _enqueue(x.device.index, binding.scout_ckpt_pack, _CODE[x.dtype], rows, cols, x.data_ptr(), stride, codes.data_ptr(),
-             max(cols, 1), exps.data_ptr())
+    code, rows, cols, stride, exps_shape = _activation(x.shape, x.stride(), x.dtype, x.device)
+    codes, exps = x.new_empty((rows, cols), dtype=torch.int8), x.new_empty(exps_shape, dtype=torch.int8)
+    _enqueue("scout_ckpt_pack", x.device.index, code, rows, cols, x.data_ptr(), stride, codes.data_ptr(), max(cols, 1),
+             exps.data_ptr())
     return codes, exps
 
 
 def checkpoint_unpack(codes: torch.Tensor, exps: torch.Tensor, dtype: torch.dtype = torch.bfloat16) -> torch.Tensor:
     """The activation a checkpoint stands for, in `dtype`."""
-    rows, cols, stride = _checkpoint(codes, exps)
+    rows, cols, stride = _checkpoint(codes.shape, codes.stride(), codes.dtype, codes.device, exps.shape, exps.stride(), exps.dtype,
+                                     exps.device)
     if dtype not in _CODE:
         _fail("activations are float32, bfloat16 or float16")
     x = codes.new_empty((rows, cols), dtype=dtype)
-    _enqueue(codes.device.index, binding.scout_ckpt_unpack, _CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(),
+    _enqueue("scout_ckpt_unpack", codes.device.index, _CODE[dtype], rows, cols, codes.data_ptr(), stride, exps.data_ptr(),
              x.data_ptr(), max(cols, 1))
     return x
 
 
-@functools.lru_cache(maxsize=256)
-def _wgrad_scratch(code, rows, outs, ins):
-    return binding.scout_ckpt_wgrad_workspace(code, rows, outs, ins)
+@functools.lru_cache(maxsize=1024)
+def _product(shape, stride, dtype, device, rows, codes_device, ins, dw_shape, dw_stride, dw_dtype, dw_device):
+    """Checks a description of dy and the gradient -> their codes, outputs, row strides, scratch bytes."""
+    row = _row_stride(shape, stride, device, "dy")
+    if dtype not in _SIXTEEN or shape[0] != rows or device != codes_device:
+        _fail("dy: a bfloat16 or float16 matrix with the checkpoint's rows, on its device")
+    outs = shape[1]
+    if dw_dtype not in (torch.float32, dtype) or dw_shape != (outs, ins) or dw_device != device:
+        _fail("the gradient is [outs, ins], float32 or of dy's dtype, on dy's device")
+    dw_row = _row_stride(dw_shape, dw_stride, dw_device, "grad")
+    return _CODE[dtype], _CODE[dw_dtype], outs, row, dw_row, binding.scout_ckpt_wgrad_workspace(_CODE[dtype], rows, outs, ins)
 
 
 def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, *, out_dtype: torch.dtype = torch.float32,
                      grad: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Weight gradient dW = dy^T x of y = x W^T, x taken from its checkpoint.  dy: [rows, outs], bfloat16 or float16.
     -> dW [outs, ins] in out_dtype (float32 or dy's); with `grad` (of those dtypes) dW is added to it in place."""
-    rows, ins, code_stride = _checkpoint(codes, exps)
-    dy_stride = _matrix(dy, "dy")
-    if dy.dtype not in _SIXTEEN or dy.shape[0] != rows or dy.device != codes.device:
-        _fail("dy: a bfloat16 or float16 matrix with the checkpoint's rows, on its device")
-    outs = dy.shape[1]
-    dw = dy.new_empty((outs, ins), dtype=out_dtype) if grad is None else grad
-    dw_stride = _matrix(dw, "grad")
-    if dw.dtype not in (torch.float32, dy.dtype) or dw.shape != (outs, ins) or dw.device != dy.device:
-        _fail("the gradient is [outs, ins], float32 or of dy's dtype, on dy's device")
-    nbytes = _wgrad_scratch(_CODE[dy.dtype], rows, outs, ins)
-    ws = _scratch(nbytes, dy)
-    _enqueue(dy.device.index, binding.scout_ckpt_wgrad, _CODE[dy.dtype], _CODE[dw.dtype], rows, outs, ins, dy.data_ptr(), dy_stride,
-             codes.data_ptr(), code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
+    rows, ins, code_stride = _checkpoint(codes.shape, codes.stride(), codes.dtype, codes.device, exps.shape, exps.stride(),
+                                         exps.dtype, exps.device)
+    if dy.dim() != 2:
+        _fail("dy: a matrix with adjacent row elements is wanted")
+    dw = dy.new_empty((dy.shape[1], ins), dtype=out_dtype) if grad is None else grad
+    code, dw_code, outs, dy_stride, dw_stride, nbytes = _product(dy.shape, dy.stride(), dy.dtype, dy.device, rows, codes.device, ins,
+                                                                 dw.shape, dw.stride(), dw.dtype, dw.device)
+    ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
+    _enqueue("scout_ckpt_wgrad", dy.device.index, code, dw_code, rows, outs, ins, dy.data_ptr(), dy_stride, codes.data_ptr(),
+             code_stride, exps.data_ptr(), dw.data_ptr(), dw_stride, int(grad is not None),
              ws.data_ptr() if ws is not None else 0, nbytes)
     return dw
