@@ -390,10 +390,11 @@ Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
     t.bytes = t.part_bytes + (tensor ? (rows * t.x_stride * 2 + 255) & ~255ull : 0);
     return t;
 }
-// The restored copy costs a pass over memory and a launch: worth it from a step of tokens on, or where the outputs are many (56
-// tokens, 9456 x 2568: what is written bounds it, and wgrad_tiles writes 84 us).
+// The restored copy costs a pass over memory and a launch (a call of 128 tokens, 512 x 512: 21.8 us with it, 12.3 without; 512
+// tokens: the same; 512 tokens, 1024 x 1024: 15.2 against 18.5).  Few tokens of many outputs: what is written bounds it (56 tokens,
+// 9456 x 2568: 32 us against 84).
 bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) {
-    return outs >= 64 && ins >= 64 && (rows >= TK || (rows > 0 && outs * ins >= 1u << 20));
+    return outs >= 64 && ins >= 64 && (rows >= 4 * TK || (rows > 0 && outs * ins >= 1u << 20));
 }
 
 template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStream_t stream) {
