@@ -382,13 +382,13 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
     using L = Layout<HD>;
     constexpr int NQ = L::DKV_Q, NG = L::DKV_G, STAGES = NQ + NG, SIDES = 0, DV = 256, DK = 256 + HD;  // tensor memory columns; two sides of 128 for S and dP
     uint64_t *const bars = side.bars;
-    static_assert(2 * STAGES + 12 <= 32, "");
+    static_assert(2 * STAGES + 13 <= 32, "");
     uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
     float (&s_lse)[2][ROWS] = side.lse, (&s_delta)[2][ROWS] = side.delta;
     const Problem &p = a.p;
     const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, ring = sv + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, k_full = empty + 8 * STAGES, s_full = k_full + 16, dp_full = s_full + 8,
-                   dp_taken = dp_full + 8, p_full = dp_taken + 8, ds_full = p_full + 8, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
+                   dp_taken = dp_full + 8, p_full = dp_taken + 8, ds_full = p_full + 16, all_done = ds_full + 8, st_full = all_done + 8, st_empty = st_full + 16;
     const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
     const tc::Patience patience{&dead, a.gave_up};
     const int split = block % a.kv_splits;
@@ -417,7 +417,7 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
         tc::bar_init(k_full, 1), tc::bar_init(k_full + 8, 1), tc::bar_init(s_full, 1), tc::bar_init(dp_full, 1), tc::bar_init(all_done, 1);
-        tc::bar_init(dp_taken, 8), tc::bar_init(p_full, 8), tc::bar_init(ds_full, 8);
+        tc::bar_init(dp_taken, 8), tc::bar_init(p_full, 8), tc::bar_init(p_full + 8, 8), tc::bar_init(ds_full, 8);
         for (int s = 0; s < 2; ++s) tc::bar_init(st_full + 8 * s, 1), tc::bar_init(st_empty + 8 * s, 8);
         tc::bar_init_done();
         if (steps) {  // inputs of the call: on their way before the block is set up, in the order the products need them
@@ -476,7 +476,8 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
                 tc::tc_fence_after();
                 issue_s(s + 1);  // over dP
             }
-            ok = patience.wait_warp(p_full, s & 1);
+            // two barriers in turn: the next scores are on their way by now, so P of the next step may be complete before this look
+            ok = patience.wait_warp(p_full + 8 * (s & 1), (s >> 1) & 1);
             if (!ok) break;
             tc::tc_fence_after();
             product_sum<T, HD>(tmem + DV, side_s(s), 64, stage(2 * s + 1), s > 0);
@@ -523,7 +524,7 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
             round16<T>(x, w);
             tc::tmem_store16(at_s, x);  // over columns that this warp has read
             tc::tmem_store16(at_s + 16, x + 16);
-            stored(p_full, lane);
+            stored(p_full + 8 * (s & 1), lane);
             ok = patience.wait_warp(dp_full, s & 1);
             if (!ok) break;
             tc::tc_fence_after();

@@ -203,6 +203,28 @@ def test_same_bits_every_time_and_in_every_batch(size):
         assert all(torch.equal(a, b) for a, b in zip(got, first))
 
 
+def test_what_else_runs_does_not_show():
+    """The same bits while another stream keeps memory and SMs busy: loads come late, blocks start late, warps fall behind."""
+    import random
+    from paper_2608_11034_b200 import replay
+    rng, side, noise = random.Random(5), torch.cuda.Stream(), torch.empty(1 << 27, device="cuda")
+
+    def run(q, k, v, do, causal):
+        o, lse = replay.attention_forward(q, k, v, causal=causal)
+        return (o, lse) + replay.attention_backward(q, k, v, o, lse, do, causal=causal)
+
+    for _ in range(60):
+        Hk, G, D, T = rng.choice([1, 2, 8]), rng.choice([1, 2, 4]), rng.choice([64, 128]), rng.randint(100, 1500)
+        case = make(rng.randrange(1 << 16), BF, rng.randint(1, 3), T, T, Hk * G, Hk, D) + (rng.random() < 0.7,)
+        want = run(*case)
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            for _ in range(rng.randint(1, 6)):
+                noise[:rng.randint(1 << 16, 1 << 27)].add_(1.0)
+        for _ in range(3):
+            assert all(torch.equal(a, b) for a, b in zip(run(*case), want))
+
+
 def test_gradients_against_differences():
     """Directional derivatives of the definition's loss, by central differences in 64 bits."""
     from paper_2608_11034_b200 import replay
