@@ -37,8 +37,9 @@ extern "C" {
  * keys it sees:
  *     lse_i = ln sum_j exp s_ij,   o_i = sum_j exp(s_ij - lse_i) v_j
  * A row that sees nothing (past its length, or all its keys masked) has o = 0 and
- * lse = -inf, and contributes nothing to any gradient.  What stands in keys, values,
- * queries or gradients that a row does not see never reaches it, NaN and Inf included.
+ * lse = -inf, and contributes nothing to any gradient; one whose scores are all -Inf has
+ * the same o and lse.  What stands in keys, values, queries or gradients that a row does
+ * not see never reaches it, NaN and Inf included; a NaN that it sees always does.
  *
  * Sizes: batch * q_heads * q_len and batch * kv_heads * kv_len up to 2^30, batch * q_heads
  * up to 2^24, head_dim up to 128; beyond that SCOUT_ERR_UNSUPPORTED.  Element offsets are

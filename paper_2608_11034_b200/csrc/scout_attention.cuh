@@ -91,23 +91,37 @@ __device__ __forceinline__ float exp2_fast(float x) {
 // 2^x of two numbers by multiply-adds, for a share of the exponentials beside the special function unit (four lanes a cycle).
 // Cody-Waite: x = n + f with n the nearest integer, which adding 1.5 2^23 leaves in the low bits, and 2^f on [-1/2, 1/2] by the
 // polynomial of degree 4 of least maximal relative error (Remez exchange; 2.7e-6, far below the 2^-9 or 2^-12 that
-// probabilities are rounded to; mean 4e-8, which is what their sum sees).  What lies below 2^-126 comes out as 2^-126.
-// SHARE pairs of every 16 go this way in the forward kernel, of every 32 in the backward one.  Forward, 2 x 4096 tokens, 16 heads of 64:
-// 0: 237, 4: 222, 6: 213, 8: 236 us; 2 x 2048 tokens, 32/8 heads of 128, causal: 79.0, 76.3, 75.2, 78.7; backward of the
-// latter: 244, 240, 238.5, 239.
-constexpr int SHARE = 6;
-__device__ __forceinline__ float2 exp2_fma(tc::F2 x) {
-    const float2 lim = tc::split(x);
-    const tc::F2 y = tc::f2(fmaxf(lim.x, -126.f), fmaxf(lim.y, -126.f)), magic = tc::f2(12582912.f, 12582912.f);
+// probabilities are rounded to; mean 4e-8, which is what their sum sees).  2^n is a factor, so that what is no number stays none
+// (a NaN score shows in the row's sum, from which the row is made again), and n is held to [-127, 128], where the factor is 0 or Inf:
+// below 2^-126.5 the result is 0, as the unit's, and from 2^127.5 on it is Inf.  With ABOVE = false x is known to stay below 127.
+// SHARE pairs of every 16 go this way in the forward kernel, BACKWARD_SHARE of every 32 in the backward one (whose scores may lie
+// anywhere above a row statistic that is not theirs).  Forward, 2 x 4096 tokens, 16 heads of 64, of 16 pairs 0: 243, 4: 222, 6: 216,
+// 8: 235 us; 2 x 2048 tokens, 32/8 heads of 128, causal: 77.9, 74.4, 73.2, 78.0; backward of the latter, of 32 pairs 2: 221, 4: 220,
+// 5: 221, 6: 224, 7: 225.
+constexpr int SHARE = 6, BACKWARD_SHARE = 4;
+__device__ __forceinline__ float keep_nan_max(float x, float y) {
+    float z;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+__device__ __forceinline__ float keep_nan_min(float x, float y) {
+    float z;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(z) : "f"(x), "f"(y));
+    return z;
+}
+template <bool ABOVE> __device__ __forceinline__ float2 exp2_fma(tc::F2 x) {
+    float2 lim = tc::split(x);
+    lim.x = keep_nan_max(lim.x, -127.f), lim.y = keep_nan_max(lim.y, -127.f);
+    if constexpr (ABOVE) lim.x = keep_nan_min(lim.x, 128.f), lim.y = keep_nan_min(lim.y, 128.f);
+    const tc::F2 y = tc::f2(lim.x, lim.y), magic = tc::f2(12582912.f, 12582912.f);
     const tc::F2 t = tc::add2(y, magic), n = tc::add2(t, tc::f2(-12582912.f, -12582912.f)), f = tc::fma2(n, tc::f2(-1.f, -1.f), y);
     tc::F2 p = tc::f2(0.009570102207362652f, 0.009570102207362652f);
     p = tc::fma2(p, f, tc::f2(0.05591785907745361f, 0.05591785907745361f));
     p = tc::fma2(p, f, tc::f2(0.240247443318367f, 0.240247443318367f));
     p = tc::fma2(p, f, tc::f2(0.6931217908859253f, 0.6931217908859253f));
     p = tc::fma2(p, f, tc::f2(0.9999992847442627f, 0.9999992847442627f));
-    const float2 m = tc::split(p), e = tc::split(t);
-    return make_float2(__uint_as_float(__float_as_uint(m.x) + (__float_as_uint(e.x) << 23)),
-                       __uint_as_float(__float_as_uint(m.y) + (__float_as_uint(e.y) << 23)));
+    const float2 e = tc::split(t);
+    return tc::split(tc::mul2(p, tc::f2(__uint_as_float((__float_as_uint(e.x) << 23) + 0x3F800000u), __uint_as_float((__float_as_uint(e.y) << 23) + 0x3F800000u))));
 }
 
 // ---- warp-level pieces ---------------------------------------------------------------------------

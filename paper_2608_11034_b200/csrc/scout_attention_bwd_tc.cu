@@ -129,8 +129,8 @@ template <typename F> __device__ __forceinline__ void to_p(uint32_t (&r)[2][32],
         const float2 y = tc::split(tc::fma2(tc::f2(__uint_as_float(v[0]), __uint_as_float(v[1])), scale2, m.lo));
         const tc::F2 z = tc::fma2(tc::f2(__uint_as_float(v[2]), __uint_as_float(v[3])), scale2, m.hi);
         v[0] = __float_as_uint(exp2_fast(y.x)), v[1] = __float_as_uint(exp2_fast(y.y));
-        const bool fma = (c >> 2) * SHARE % 16 + SHARE >= 16;  // SHARE of the 16 second pairs, spread evenly
-        const float2 u = fma ? exp2_fma(z) : make_float2(exp2_fast(tc::split(z).x), exp2_fast(tc::split(z).y));
+        const bool fma = (c >> 2) * BACKWARD_SHARE % 16 + BACKWARD_SHARE >= 16;  // so many of the 16 second pairs, spread evenly
+        const float2 u = fma ? exp2_fma<true>(z) : make_float2(exp2_fast(tc::split(z).x), exp2_fast(tc::split(z).y));
         v[2] = __float_as_uint(u.x), v[3] = __float_as_uint(u.y);
     }
     seen.hide(r);

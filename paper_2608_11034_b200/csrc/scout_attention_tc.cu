@@ -278,7 +278,7 @@ __global__ void __launch_bounds__(TC_THREADS, 1) forward_tc(const __grid_constan
                     for (int e = 0; e < 16; ++e) {
                         const tc::F2 y = tc::fma2(tc::f2(__uint_as_float(r[c][2 * e]), __uint_as_float(r[c][2 * e + 1])), scale2, minus2);
                         const bool fma = decltype(every)::value && e * SHARE % 16 + SHARE >= 16;  // spread evenly
-                        const float2 v = fma ? exp2_fma(y) : make_float2(exp2_fast(tc::split(y).x), exp2_fast(tc::split(y).y));
+                        const float2 v = fma ? exp2_fma<false>(y) : make_float2(exp2_fast(tc::split(y).x), exp2_fast(tc::split(y).y));
                         part[e & 1] = tc::add2(part[e & 1], tc::f2(v.x, v.y));
                         w[e] = Half<T>::pack(v.x, v.y);
                     }
