@@ -119,7 +119,9 @@ SCOUT_API int scout_ckpt_unpack(uint32_t dtype, uint64_t rows, uint64_t cols, co
  *   dy           device [rows][outs], row stride dy_stride
  *   codes, exps  the checkpoint: [rows][ins] and [rows][ceil(ins / 32)]
  *   dw           device [outs][ins], row stride dw_stride
- * dy and dw are aligned to their element sizes. */
+ * dy and dw are aligned to their element sizes.  The result's bits depend on the values and
+ * sizes alone: rows of dy that do not start on 16-byte boundaries are copied to scratch
+ * first (the scratch has room for that). */
 SCOUT_API int scout_ckpt_wgrad_workspace(uint32_t dtype, uint64_t rows, uint64_t outs, uint64_t ins, uint64_t *bytes);
 SCOUT_API int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t rows, uint64_t outs, uint64_t ins,
                                const void *dy, uint64_t dy_stride, const int8_t *codes, uint64_t code_stride,

@@ -6,7 +6,9 @@
 //
 // Two kernels.  wgrad_tc: the checkpoint is restored to scratch in dy's type (one memory pass, small next to the product) and
 // both operands go by TMA to tcgen05.  wgrad_tiles: restores on the way into shared memory and uses the warp-level matrix
-// instructions; for few outputs, few tokens, and rows of dy that TMA cannot address.
+// instructions; for few outputs and few tokens.  Which of them runs, its parts and its chains follow from the sizes alone, so that equal
+// values give equal bits wherever they lie: rows of dy that TMA cannot address (not on 16-byte boundaries) are copied to
+// scratch first.  8192 x 14335 x 4096 into fp32: 890 us a call, 717 with 14336 outputs; 300 x 65 x 64: 27.4, 24 with 64.
 // Where the outputs give too few blocks for the SMs, the tokens are split into parts that go to scratch in fp32 and are
 // added in order.
 //
@@ -365,13 +367,45 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_join(cons
     }
 }
 
-// How a product is cut; the scratch holds the parts, then the restored activation.
+// ---- rows of dy on any boundary -----------------------------------------------------------------------------
+// To rows on 16-byte boundaries.  A lane holds a word of two elements and takes the next one from its neighbour; a warp has COPY_WORDS
+// of them a lane in flight, along a row.
+constexpr int COPY_WORDS = 8;
+__global__ void __launch_bounds__(THREADS) copy_rows(const uint16_t *src, int64_t stride, int64_t rows, int64_t cols, uint16_t *dst, int64_t dst_stride) {
+    const int lane = threadIdx.x;
+    const int64_t c0 = (int64_t)blockIdx.x * (64 * COPY_WORDS);
+    for (int64_t r = (int64_t)blockIdx.y * (THREADS / 32) + threadIdx.y; r < rows; r += (int64_t)gridDim.y * (THREADS / 32)) {  // the same for a warp
+        const uint16_t *row = src + r * stride, *end = row + cols;
+        const int odd = (int)(reinterpret_cast<uintptr_t>(row + c0) >> 1) & 1;  // the row's words lie one element past boundaries
+        // the word that holds element c - odd; an element outside the row is not read
+        const auto load = [&](int64_t c) {
+            const uint16_t *at = row + c - odd;
+            if (at >= row && at + 2 <= end) return __ldg(reinterpret_cast<const uint32_t *>(at));
+            return (at >= row && at < end ? (uint32_t)at[0] : 0u) | (at + 1 >= row && at + 1 < end ? (uint32_t)at[1] << 16 : 0u);
+        };
+        uint32_t w[COPY_WORDS];
+#pragma unroll
+        for (int u = 0; u < COPY_WORDS; ++u) w[u] = load(c0 + 64 * u + 2 * lane);
+        const uint32_t last = odd && lane == 31 ? load(c0 + 64 * COPY_WORDS) : 0u;
+        uint32_t *out = reinterpret_cast<uint32_t *>(dst + r * dst_stride + c0) + lane;
+#pragma unroll
+        for (int u = 0; u < COPY_WORDS; ++u) {
+            // lane 31 takes lane 0's word of the next 64 elements
+            const uint32_t next = __shfl_sync(0xFFFFFFFFu, lane == 0 && u + 1 < COPY_WORDS ? w[u + 1] : w[u], (lane + 1) & 31);
+            const uint32_t x = odd ? __funnelshift_r(w[u], lane == 31 && u + 1 == COPY_WORDS ? last : next, 16) : w[u];
+            if (c0 + 64 * u + 2 * lane < cols) out[32 * u] = x;  // rows of the copy are padded to eight elements
+        }
+    }
+}
+
+// How a product is cut; the scratch holds the parts, then the restored activation, then room for a copy of dy.
 struct Tiling {
     bool tensor;  // wgrad_tc
     uint64_t tiles_o, tiles_i;
     int64_t per, part_stride, x_stride;
     int splits;
-    uint64_t part_bytes, bytes;
+    int64_t y_stride;
+    uint64_t part_bytes, x_bytes, bytes;
 };
 Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
     Tiling t = {};
@@ -387,7 +421,9 @@ Tiling tiling(uint64_t rows, uint64_t outs, uint64_t ins, bool tensor) {
     t.part_stride = (int64_t)((ins + 7) & ~7ull);
     t.part_bytes = t.splits > 1 ? (t.splits * outs * t.part_stride * 4 + 255) & ~255ull : 0;
     t.x_stride = t.part_stride;
-    t.bytes = t.part_bytes + (tensor ? (rows * t.x_stride * 2 + 255) & ~255ull : 0);
+    t.y_stride = (int64_t)((outs + 7) & ~7ull);
+    t.x_bytes = tensor ? (rows * t.x_stride * 2 + 255) & ~255ull : 0;
+    t.bytes = t.part_bytes + t.x_bytes + (tensor ? (rows * t.y_stride * 2 + 255) & ~255ull : 0);
     return t;
 }
 // The restored copy costs a pass over memory and a launch (a call of 128 tokens, 512 x 512: 21.8 us with it, 12.3 without; 512
@@ -397,10 +433,19 @@ bool worth_tensor(uint64_t rows, uint64_t outs, uint64_t ins) {
     return outs >= 64 && ins >= 64 && (rows >= 4 * TK || (rows > 0 && outs * ins >= 1u << 20));
 }
 
-template <typename T> int run(Args &a, const Tiling &t, void *restored, cudaStream_t stream) {
+template <typename T> int run(Args &a, const Tiling &t, void *workspace, cudaStream_t stream) {
+    void *const restored = (uint8_t *)workspace + t.part_bytes;
     const int64_t join_grid = std::min<int64_t>((a.outs * a.part_stride + THREADS - 1) / THREADS, 148 * 8);
     if (t.tensor) {
         constexpr bool bf16 = Half<T>::is_bf16;
+        if (a.dy_stride % 8 || a.dy_stride >= 1ll << 39 || reinterpret_cast<uintptr_t>(a.dy) & 15) {
+            uint16_t *const copy = reinterpret_cast<uint16_t *>((uint8_t *)restored + t.x_bytes);
+            const int64_t across = (a.outs + 64 * COPY_WORDS - 1) / (64 * COPY_WORDS), down = (a.rows + THREADS / 32 - 1) / (THREADS / 32);
+            copy_rows<<<dim3((unsigned)across, (unsigned)std::min<int64_t>(down, 65535)), dim3(32, THREADS / 32), 0, stream>>>(
+                reinterpret_cast<const uint16_t *>(a.dy), a.dy_stride, a.rows, a.outs, copy, t.y_stride);
+            SCOUT_CUDA(cudaGetLastError());
+            a.dy = copy, a.dy_stride = t.y_stride;
+        }
         CUtensorMap my, mx;
         const uint64_t dy_dims[2] = {(uint64_t)a.outs, (uint64_t)a.rows}, x_dims[2] = {(uint64_t)a.ins, (uint64_t)a.rows};
         const uint64_t dy_strides[1] = {(uint64_t)a.dy_stride * 2}, x_strides[1] = {(uint64_t)t.x_stride * 2};
@@ -444,8 +489,7 @@ extern "C" int scout_ckpt_wgrad_workspace(uint32_t dtype, uint64_t rows, uint64_
     using namespace scout::wgrad;
     if (int rc = check(dtype, rows, outs, ins)) return rc;
     if (!bytes) return SCOUT_ERR_INVALID;
-    *bytes = tiling(rows, outs, ins, false).bytes;
-    if (worth_tensor(rows, outs, ins)) *bytes = std::max(*bytes, tiling(rows, outs, ins, true).bytes);
+    *bytes = tiling(rows, outs, ins, worth_tensor(rows, outs, ins)).bytes;
     return SCOUT_OK;
 }
 
@@ -465,8 +509,7 @@ extern "C" int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t row
     uint64_t bytes = 0;
     if (int rc = scout_ckpt_wgrad_workspace(dtype, rows, outs, ins, &bytes)) return rc;
     if (workspace_bytes < bytes || (bytes && !workspace)) return SCOUT_ERR_INVALID;
-    const bool tma = dy_stride % 8 == 0 && (reinterpret_cast<uintptr_t>(dy) & 15) == 0;
-    const Tiling t = tiling(rows, outs, ins, tma && worth_tensor(rows, outs, ins));
+    const Tiling t = tiling(rows, outs, ins, worth_tensor(rows, outs, ins));
     if (t.tiles_o * t.tiles_i * t.splits > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
     Args a = {};
     a.dy = dy, a.codes = codes, a.exps = exps, a.dw = dw, a.part = (float *)workspace;
@@ -477,7 +520,6 @@ extern "C" int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t row
     const uintptr_t start = dw_stride * size | reinterpret_cast<uintptr_t>(dw);
     a.wide = start % 32 == 0 ? 2 : start % 16 == 0 ? 1 : 0;
     a.pairs = dw_stride % 2 == 0 && (reinterpret_cast<uintptr_t>(dw) & (2 * size - 1)) == 0;
-    void *restored = (uint8_t *)workspace + t.part_bytes;
     a.out_f32 = out_dtype == SCOUT_DT_F32, a.accumulate = (int)accumulate;
-    return dtype == SCOUT_DT_BF16 ? run<__nv_bfloat16>(a, t, restored, (cudaStream_t)stream) : run<__half>(a, t, restored, (cudaStream_t)stream);
+    return dtype == SCOUT_DT_BF16 ? run<__nv_bfloat16>(a, t, workspace, (cudaStream_t)stream) : run<__half>(a, t, workspace, (cudaStream_t)stream);
 }
