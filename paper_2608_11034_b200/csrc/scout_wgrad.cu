@@ -13,8 +13,9 @@
 // added in order.
 //
 // The tensor cores truncate when they add to an accumulator: a chain of 4096 tokens ends 2.2e-6 off (relative), where fp32
-// additions give 3e-7.  wgrad_tc therefore cuts its chains at CHAIN tokens and adds them in registers, rounding to
-// nearest (3.8e-7).
+// additions give 3e-7; with tokens of one sign the loss is a bias that grows with the chain (16384 tokens: 4.6e-5, with either kind
+// of instruction).  Both kernels therefore cut their chains at 1024 tokens and add them in fp32, rounding to nearest (3.8e-7;
+// tokens of one sign: a bias of 1.9e-7).
 //
 // What bounds wgrad_tc: the products.  8192 x 14336 x 4096: 700 to 850 us (1.13 to 1.37 PFLOP/s; the power limit decides, the measured
 // sustained rate being 1.40); 4096^3 into fp32: 109 us with the restore, 512 tiles being 3.46 rounds of 148 blocks.
@@ -63,7 +64,10 @@ __device__ __forceinline__ void put(const Args &a, int64_t o, int64_t i, float v
     }
 }
 
-template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(const __grid_constant__ Args a) {
+// CUT: more tokens than a chain has.  The sums of chains stand in shared memory, [64][THREADS]: beside the accumulators in registers
+// they would leave one block an SM instead of two (16384 x 40 x 19000: 1143 us, 879 this way, 806 as one chain).
+constexpr int TILES_CHAIN = 1024 / BK, TILES_SUMS = 64 * THREADS * 4;  // steps of BK tokens; bytes
+template <typename T, bool CUT> __global__ void __launch_bounds__(THREADS, 2) wgrad_tiles(const __grid_constant__ Args a) {
     __shared__ __align__(1024) uint8_t sy[2][BK * ROW], sx[2][BK * ROW];
     int64_t x = blockIdx.x;
     const int split = x % a.splits;
@@ -127,6 +131,20 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(con
         }
     };
     float acc[4][4][4] = {};
+    extern __shared__ float sums[];  // CUT alone
+    const auto end_chain = [&](bool first, bool last) {  // the chain so far moves to its sum, or with `last` the sum to the accumulators
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+            for (int n = 0; n < 4; ++n)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    float &s = sums[((m * 4 + n) * 4 + e) * THREADS + threadIdx.x];
+                    const float v = first ? acc[m][n][e] : s + acc[m][n][e];
+                    if (last) acc[m][n][e] = v;
+                    else s = v, acc[m][n][e] = 0.f;
+                }
+    };
     if (t0 < t1) {
         fetch(t0);
         stash(0);
@@ -151,8 +169,10 @@ template <typename T> __global__ void __launch_bounds__(THREADS) wgrad_tiles(con
                 for (int n = 0; n < 4; ++n) mma16816<T>(acc[m][n], fa[m], fb[n >> 1][2 * (n & 1)], fb[n >> 1][2 * (n & 1) + 1]);
         }
         if (t + BK < t1) stash(st ^ 1);
+        if (CUT && (it + 1) % TILES_CHAIN == 0) end_chain(it + 1 == TILES_CHAIN, false);
         __syncthreads();
     }
+    if (CUT && t1 - t0 > (TILES_CHAIN - 1) * BK) end_chain(false, true);  // a chain has ended
 #pragma unroll
     for (int m = 0; m < 4; ++m)
 #pragma unroll
@@ -467,7 +487,10 @@ template <typename T> int run(Args &a, const Tiling &t, void *workspace, cudaStr
         cfg.numAttrs = 1;
         SCOUT_CUDA(cudaLaunchKernelEx(&cfg, wgrad_tc<T>, a, my, mx));
     } else {
-        wgrad_tiles<T><<<(unsigned)(a.tiles * a.splits), THREADS, 0, stream>>>(a);
+        const bool cut = a.per > TILES_CHAIN * BK;
+        if (cut)
+            if (int rc = allow_smem<wgrad_tiles<T, true>>(TILES_SUMS)) return rc;
+        (cut ? wgrad_tiles<T, true> : wgrad_tiles<T, false>)<<<(unsigned)(a.tiles * a.splits), THREADS, cut ? TILES_SUMS : 0, stream>>>(a);
         SCOUT_CUDA(cudaGetLastError());
     }
     if (t.splits > 1) SCOUT_CUDA(launch_dependent(wgrad_join<T>, dim3((unsigned)join_grid), dim3(THREADS), stream, a));

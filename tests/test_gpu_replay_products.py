@@ -1,5 +1,5 @@
 """The weight gradient where it is cut: many output tiles, many tokens, rows of dy on any boundary.  Sums of small integers
-are exact in fp32, so that a lost or doubled token shows."""
+are exact in fp32, so that a lost or doubled token shows; sums of one sign over many tokens show how chains round."""
 import pytest
 import torch
 
@@ -30,7 +30,7 @@ def off_boundary(x, by):
 
 SIZES = [  # rows, outs, ins
     (1, 1, 1), (1, 8, 8), (31, 40, 33), (33, 63, 129), (64, 128, 256), (255, 64, 64), (256, 64, 64), (257, 72, 67), (259, 1000, 520), (1025, 130, 257),
-    (4100, 20, 40), (70000, 9, 17),          # few outputs: parts of more than 1024 tokens
+    (4100, 20, 40), (70000, 9, 17), (67528, 9, 17),   # few outputs: parts of 1120 and of 1056 tokens, the last of 1000
     (2100, 1700, 2900), (3001, 2050, 2570),  # more than 148 tiles: several to a block, three chains each
     (700, 1281, 5121), (2049, 60, 19000),    # the same with few outputs a token
     (8, 1031, 1024),
@@ -76,3 +76,23 @@ def test_the_bits_do_not_depend_on_where_dy_lies(dtype, out, rows, outs, ins):
     replay.checkpoint_wgrad(dy, codes, exps, grad=grad)
     replay.checkpoint_wgrad(off_boundary(dy, 5), codes, exps, grad=room[:, 1:])
     assert torch.equal(grad, room[:, 1:])
+
+
+@pytest.mark.parametrize("rows,outs,ins", [(16384, 1700, 2900), (16384, 40, 19000), (16384, 1701, 2900), (131072, 60, 129)])
+def test_chains_are_cut(rows, outs, ins):
+    """Tokens of one sign and similar size.  A matrix instruction of 16 tokens drops, on average, at most half a unit in the last place
+    (2^-24) of the sum that it adds to; over a chain of 1024 tokens that sum is on average half of the chain's, and additions in
+    fp32 round to nearest: no bias beyond 64 * 2^-24 / 2.  One chain over all tokens would have rows / 1024 times that."""
+    from paper_2608_11034_b200 import replay
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = (1.0 + torch.rand(rows, ins, generator=g, device="cuda")).to(BF)
+    dy = (1.0 + torch.rand(rows, outs, generator=g, device="cuda")).to(BF)
+    if outs % 2:
+        dy = off_boundary(dy, 1)
+    codes, exps = replay.checkpoint_pack(x)
+    xd = defn.restore(codes, exps)
+    want = dy.double().t() @ xd
+    got = replay.checkpoint_wgrad(dy, codes, exps).double()
+    off = (got - want) / want
+    assert off.mean().abs() <= 64 * 2.0 ** -24 / 2
+    assert off.abs().max() <= 64 * 2.0 ** -23 + (rows // 1024) * 2.0 ** -24
