@@ -133,6 +133,11 @@ SCOUT_API int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t rows
  * Synchronises the device. */
 SCOUT_API int scout_replay_error(uint32_t *count /*host*/);
 
+/* Runs the end of a block of the backward pass in which the warps whose bits are set in `stuck` (0..255) wait on a barrier that
+ * nothing arrives at, give up after 2 s (counted as above) and then agree with the others.  d_out: device uint32 [8][2], for every
+ * warp the rows that it would make again and flags: 1 = some warp has such rows, 2 = no warp gave up. */
+SCOUT_API int scout_selftest_give_up(uint32_t stuck, uint32_t *d_out /*device*/, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -109,6 +109,7 @@ def lib():
             "scout_ckpt_wgrad_workspace": (C.c_int, [u32, u64, u64, u64, C.POINTER(u64)]),
             "scout_ckpt_wgrad": (C.c_int, [u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, u64, u32, vp, u64, vp]),
             "scout_replay_error": (C.c_int, [C.POINTER(u32)]),
+            "scout_selftest_give_up": (C.c_int, [u32, vp, vp]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
             "scout_last_cuda_error": (C.c_char_p, []),
@@ -436,6 +437,10 @@ def scout_replay_error() -> int:
     n = C.c_uint32()
     _check(lib().scout_replay_error(C.byref(n)), "scout_replay_error")
     return n.value
+
+
+def scout_selftest_give_up(stuck: int, d_out: int, stream: int) -> None:
+    _check(lib().scout_selftest_give_up(stuck, d_out, stream), "scout_selftest_give_up")
 
 
 def scout_selftest_bounded_wait(limit_ns: int, d_out: int, stream: int) -> None:

@@ -83,8 +83,24 @@ struct TcBackwardArgs {
 struct Side {  // what a block keeps in shared memory beside its tiles
     float lse[2][ROWS], delta[2][ROWS];  // dK, dV: -lse', -delta of a step's rows
     uint64_t bars[32];
-    uint32_t tmem_slot, dead, bad[2][4];
+    uint32_t tmem_slot, dead, bad[8], gave_up[8];  // the last two by warp
 };
+
+// Before rows leave, the eight warps that hold them agree which are made again: a warp's own 32 (of either warpgroup) and whether there
+// are any.  All eight come here once, also those whose wait gave up (ok = false).  With one of them there are no rows to make again
+// for anybody, as the results of such a call are not valid: every warp takes the same way through the barriers that follow.
+struct Again {
+    uint32_t mine;
+    bool any, ok;
+};
+__device__ __forceinline__ Again agree(Side &side, int warp, int lane, bool ok, uint32_t bad) {
+    if (lane == 0) side.bad[warp] = bad, side.gave_up[warp] = !ok;
+    both_warpgroups();
+    uint32_t any = 0, gave_up = 0;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) any |= side.bad[w], gave_up |= side.gave_up[w];
+    return {gave_up ? 0u : side.bad[warp & 3] | side.bad[4 + (warp & 3)], !gave_up && any, !gave_up};
+}
 
 // 64 columns of this thread's row to registers
 __device__ __forceinline__ void take(uint32_t (&r)[2][32], uint32_t at) {
@@ -211,7 +227,7 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
     constexpr int STAGES = L::DQ_STAGES, S = 0, DP = 256, DQ = 384;  // tensor memory columns: two tiles of scores, dP (then dS), dQ
     uint64_t *const bars = side.bars;
     static_assert(2 * STAGES + 7 <= 32, "");
-    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
+    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead;
     const Problem &p = a.p;
     const uint32_t sq = smem_u32(smem_tiles), sg = sq + L::TILE, ring = sg + L::TILE;
     const uint32_t full = smem_u32(bars), empty = full + 8 * STAGES, q_full = empty + 8 * STAGES, s_full = q_full + 16, dp_full = s_full + 16,
@@ -338,7 +354,7 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
         }
         if (ok && steps) ok = patience.wait_warp(dq_done, 0);
         tc::tc_fence_after();
-        if (ok) {  // the same for all warps: one that gave up has made the others give up, or come here with all of its work done
+        if (ok) {
             constexpr int COLS = HD / 2;
             float g[COLS];
             const bool fine = read_row<COLS>(g, quarter + DQ + wg * COLS, steps > 0 && hi > lo);
@@ -349,12 +365,10 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
                 // through Q's tile, which the last product has read
                 stage_row<T, COLS>(sq, (warp & 3) * 32 + lane, g, wg * COLS, p.scale);
                 tc::fence_async();
-                const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
-                if (lane == 0) s_bad[wg][warp & 3] = bad;
-                both_warpgroups();
-                uint32_t redo = s_bad[0][warp & 3] | s_bad[1][warp & 3];
-                if (wg == 0) {
+                const Again again = agree(side, warp, lane, true, __ballot_sync(0xFFFFFFFFu, mine && !fine));
+                if (again.ok && wg == 0) {
                     const int r0 = (warp & 3) * 32;
+                    uint32_t redo = again.mine;
                     if (lane == 0) {
                         store_rows<HD>(&views.dq, sq, r0, row0 + r0, p.q_len, p.head_dim, head, b);
                         if (redo) tc::tma_stored();
@@ -365,7 +379,7 @@ __device__ __forceinline__ void dq_block(const TcBackwardArgs &a, const Backward
                 }
             }
         } else if (a.q_splits == 1) {
-            both_warpgroups();
+            agree(side, warp, lane, false, 0);
         }
     }
     __syncwarp();
@@ -383,7 +397,7 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
     constexpr int NQ = L::DKV_Q, NG = L::DKV_G, STAGES = NQ + NG, SIDES = 0, DV = 256, DK = 256 + HD;  // tensor memory columns; two sides of 128 for S and dP
     uint64_t *const bars = side.bars;
     static_assert(2 * STAGES + 13 <= 32, "");
-    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead, (&s_bad)[2][4] = side.bad;
+    uint32_t &tmem_slot = side.tmem_slot, &dead = side.dead;
     float (&s_lse)[2][ROWS] = side.lse, (&s_delta)[2][ROWS] = side.delta;
     const Problem &p = a.p;
     const uint32_t sk = smem_u32(smem_tiles), sv = sk + L::TILE, ring = sv + L::TILE;
@@ -555,25 +569,20 @@ __device__ __forceinline__ void dkv_block(const TcBackwardArgs &a, const Backwar
                 const uint32_t tile = wg ? sk : sv;
                 stage_row<T, HD>(tile, r0 + lane, g, 0, wg ? p.scale : 1.f);
                 tc::fence_async();
-                const uint32_t bad = __ballot_sync(0xFFFFFFFFu, mine && !fine);
-                if (lane == 0) s_bad[wg][warp & 3] = bad;
-                both_warpgroups();
-                uint32_t any = 0;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) any |= s_bad[c >> 2][c & 3];
-                if (lane == 0) {
+                const Again again = agree(side, warp, lane, true, __ballot_sync(0xFFFFFFFFu, mine && !fine));
+                if (again.ok && lane == 0) {
                     store_rows<HD>(wg ? &views.dk : &views.dv, tile, r0, j0 + r0, p.kv_len, p.head_dim, hk, b);
-                    if (any) tc::tma_stored();
+                    if (again.any) tc::tma_stored();
                     else tc::tma_store_read();
                 }
-                if (any) {
+                if (again.any) {  // dK and dV of a key are made again together, when both have been stored
                     both_warpgroups();
-                    uint32_t redo = s_bad[0][warp & 3] | s_bad[1][warp & 3];
+                    uint32_t redo = again.mine;
                     for (; wg == 0 && redo; redo &= redo - 1) row_dkv<T>(p, a.stats, b, hk, j0 + r0 + __ffs(redo) - 1, a.dk, a.dv);
                 }
             }
         } else if (a.kv_splits == 1) {
-            both_warpgroups();
+            agree(side, warp, lane, false, 0);  // no rows to make again: no second barrier for anybody
         }
     }
     __syncwarp();
@@ -593,6 +602,25 @@ __global__ void __launch_bounds__(TC_THREADS, 1) backward_tc(const __grid_consta
     static_assert(sizeof(Side) <= L::SIDE, "");
     if ((int)blockIdx.x < a.kv_blocks) dkv_block<T, HD>(a, views, smem_tiles, side, blockIdx.x);
     else dq_block<T, HD>(a, views, smem_tiles, side, blockIdx.x - a.kv_blocks);
+}
+
+// The end of a block some of whose eight warps (a bit each in `stuck`) wait on a barrier that nothing arrives at.
+__global__ void __launch_bounds__(256) give_up_selftest(uint32_t stuck, uint32_t *gave_up, uint32_t *out) {
+    __shared__ Side side;
+    const int warp = tc::uniform(threadIdx.x >> 5), lane = threadIdx.x & 31;
+    const uint32_t bar = smem_u32(side.bars);
+    if (threadIdx.x < 8) side.bad[threadIdx.x] = side.gave_up[threadIdx.x] = 0xFFFFFFFFu;  // as memory may be found
+    if (threadIdx.x == 0) {
+        side.dead = 0;
+        tc::bar_init(bar, 1);
+        tc::bar_init_done();
+    }
+    __syncthreads();
+    const tc::Patience patience{&side.dead, gave_up};
+    const bool ok = !(stuck >> warp & 1) || patience.wait_warp(bar, 0);
+    const Again again = agree(side, warp, lane, ok, ok ? 1u << warp : 0u);
+    if (again.any) both_warpgroups();
+    if (lane == 0) out[2 * warp] = again.mine, out[2 * warp + 1] = again.any + 2 * again.ok;
 }
 
 template <typename T, int HD> int run_backward(TcBackwardArgs &a, const BackwardViews &v, cudaStream_t stream) {
@@ -633,3 +661,13 @@ int backward_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, 
 
 }  // namespace attn
 }  // namespace scout
+
+extern "C" int scout_selftest_give_up(uint32_t stuck, uint32_t *d_out, void *stream) {
+    using namespace scout;
+    if (!d_out || stuck > 0xFF) return SCOUT_ERR_INVALID;
+    uint32_t *counter = nullptr;
+    if (int rc = tc::gave_up_counter(&counter)) return rc;
+    attn::give_up_selftest<<<1, 256, 0, (cudaStream_t)stream>>>(stuck, counter, d_out);
+    SCOUT_CUDA(cudaGetLastError());
+    return SCOUT_OK;
+}
