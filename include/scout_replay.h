@@ -128,9 +128,12 @@ SCOUT_API int scout_ckpt_wgrad(uint32_t dtype, uint32_t out_dtype, uint64_t rows
                                const int8_t *exps, void *dw, uint64_t dw_stride, uint32_t accumulate,
                                void *workspace, uint64_t workspace_bytes, void *stream);
 
-/* The kernels' waits on their own copies and products are bounded (2 s).  *count becomes the number that gave up on the
- * current device since the last call (0 on healthy hardware; results of a call with one are not valid) and is reset.
- * Synchronises the device. */
+/* The kernels' waits on their own copies and products are bounded (2 s).  Results of a call in which one gave up are not
+ * valid and must not be voted on; on healthy hardware none does.  *total becomes the number that gave up on the current
+ * device since the library was loaded.  It is never reset: two readings that differ say that one of the calls between them (on
+ * whatever stream of the device) is not valid, whoever else reads.  Synchronises the device. */
+SCOUT_API int scout_replay_waits(uint32_t *total /*host*/);
+/* The same, counted since this function was last called in the process. */
 SCOUT_API int scout_replay_error(uint32_t *count /*host*/);
 
 /* Runs the end of a block of the backward pass in which the warps whose bits are set in `stuck` (0..255) wait on a barrier that

@@ -109,6 +109,7 @@ def lib():
             "scout_ckpt_wgrad_workspace": (C.c_int, [u32, u64, u64, u64, C.POINTER(u64)]),
             "scout_ckpt_wgrad": (C.c_int, [u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, u64, u32, vp, u64, vp]),
             "scout_replay_error": (C.c_int, [C.POINTER(u32)]),
+            "scout_replay_waits": (C.c_int, [C.POINTER(u32)]),
             "scout_selftest_give_up": (C.c_int, [u32, vp, vp]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
@@ -432,8 +433,15 @@ def scout_ckpt_wgrad(dtype: int, out_dtype: int, rows: int, outs: int, ins: int,
                                   accumulate, workspace, workspace_bytes, stream), "scout_ckpt_wgrad")
 
 
+def scout_replay_waits() -> int:
+    """Waits of the replay kernels that gave up on the current device since the library was loaded (synchronises)."""
+    n = C.c_uint32()
+    _check(lib().scout_replay_waits(C.byref(n)), "scout_replay_waits")
+    return n.value
+
+
 def scout_replay_error() -> int:
-    """Waits of the replay kernels that gave up on the current device since the last call (synchronises)."""
+    """The same since the last call (synchronises)."""
     n = C.c_uint32()
     _check(lib().scout_replay_error(C.byref(n)), "scout_replay_error")
     return n.value

@@ -1,4 +1,4 @@
-// Host side of scout_tc.cuh: tensor maps, and the counter of waits that gave up.
+// Host side of scout_tc.cuh: tensor maps, and the counter of waits that gave up, which is never reset.
 #include <cuda.h>
 
 #include <mutex>
@@ -70,13 +70,28 @@ int gave_up_counter(uint32_t **counter) {
 }  // namespace tc
 }  // namespace scout
 
-extern "C" int scout_replay_error(uint32_t *count) {
+extern "C" int scout_replay_waits(uint32_t *total) {
     using namespace scout;
-    if (!count) return SCOUT_ERR_INVALID;
+    if (!total) return SCOUT_ERR_INVALID;
     uint32_t *p = nullptr;
     if (int rc = tc::gave_up_counter(&p)) return rc;
     SCOUT_CUDA(cudaDeviceSynchronize());
-    SCOUT_CUDA(cudaMemcpy(count, p, sizeof *count, cudaMemcpyDeviceToHost));
-    if (*count) SCOUT_CUDA(cudaMemset(p, 0, sizeof *count));
+    SCOUT_CUDA(cudaMemcpy(total, p, sizeof *total, cudaMemcpyDeviceToHost));
+    return SCOUT_OK;
+}
+
+extern "C" int scout_replay_error(uint32_t *count) {
+    using namespace scout;
+    static std::mutex lock;
+    static uint32_t reported[64] = {};  // by device
+    if (!count) return SCOUT_ERR_INVALID;
+    int dev = 0;
+    uint32_t total = 0;
+    SCOUT_CUDA(cudaGetDevice(&dev));
+    if (dev >= 64) return SCOUT_ERR_UNSUPPORTED;
+    if (int rc = scout_replay_waits(&total)) return rc;
+    std::lock_guard<std::mutex> hold(lock);
+    *count = total - reported[dev];
+    reported[dev] = total;
     return SCOUT_OK;
 }

@@ -34,16 +34,18 @@ def make_layer(tokens: int, hidden: int, q_heads: int, kv_heads: int, head_dim: 
 
 
 def replay_layer(layer, codes: torch.Tensor, exps: torch.Tensor):
-    """One replay from the checkpoint (codes, exps) of the layer's input: the surfaces that peers compare."""
-    x = replay.checkpoint_unpack(codes, exps, layer.dtype)
-    t = x.shape[0]
-    q, k, v = ((x @ layer.w[n].t()).view(1, t, layer.heads[n], layer.head_dim) for n in "qkv")
-    o, lse = replay.attention_forward(q, k, v, causal=True)
-    grads = replay.attention_backward(q, k, v, o, lse, layer.grad, causal=True)
-    surfaces = dict(o=o, lse=lse)
-    for n, g in zip("qkv", grads):
-        surfaces["d" + n] = g
-        surfaces["dw" + n] = replay.checkpoint_wgrad(g.view(t, -1), codes, exps)
+    """One replay from the checkpoint (codes, exps) of the layer's input: the surfaces that peers compare.  Raises
+    replay.WaitGaveUp where they are not valid: a replica that has not computed them does not take part in the vote."""
+    with replay.waits_checked(codes.device):
+        x = replay.checkpoint_unpack(codes, exps, layer.dtype)
+        t = x.shape[0]
+        q, k, v = ((x @ layer.w[n].t()).view(1, t, layer.heads[n], layer.head_dim) for n in "qkv")
+        o, lse = replay.attention_forward(q, k, v, causal=True)
+        grads = replay.attention_backward(q, k, v, o, lse, layer.grad, causal=True)
+        surfaces = dict(o=o, lse=lse)
+        for n, g in zip("qkv", grads):
+            surfaces["d" + n] = g
+            surfaces["dw" + n] = replay.checkpoint_wgrad(g.view(t, -1), codes, exps)
     return surfaces
 
 

@@ -15,9 +15,14 @@ allocator on the current stream and enqueues the library's kernels there
 (``include/scout_replay.h`` has the definitions).  Tensors are used where they
 lie: as usual in torch, one made on another stream needs that stream's work
 waited for, and ``record_stream`` if it is freed early.
+
+The kernels' waits are bounded.  A call in which one gave up has no valid results, and
+cannot say so itself, since it only enqueues: ``with waits_checked(device):`` around
+the calls raises WaitGaveUp before anybody signs or votes on what they left.
 """
 from __future__ import annotations
 
+import contextlib
 import functools
 import math
 from typing import Optional
@@ -29,6 +34,23 @@ from . import binding
 
 _CODE = {torch.float32: binding.DT_F32, torch.bfloat16: binding.DT_BF16, torch.float16: binding.DT_F16}
 _SIXTEEN = (torch.bfloat16, torch.float16)
+
+
+class WaitGaveUp(RuntimeError):
+    """A wait of a replay kernel ran into its limit: what the calls since the last check left is not valid."""
+
+
+@contextlib.contextmanager
+def waits_checked(device: torch.device):
+    """Raises WaitGaveUp if a wait of the replay kernels gave up on `device` between entry and exit, on any of its streams
+    (synchronises the device at both)."""
+    with torch.cuda.device(device):
+        before = binding.scout_replay_waits()
+    yield
+    with torch.cuda.device(device):
+        n = (binding.scout_replay_waits() - before) % (1 << 32)
+    if n:
+        raise WaitGaveUp(f"{n} waits of the replay kernels gave up on {device}: the results are not valid")
 
 
 def _fail(what: str):

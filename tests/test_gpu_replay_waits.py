@@ -21,6 +21,26 @@ def test_warps_that_gave_up_and_warps_that_did_not_leave_together(stuck):
     assert (binding.scout_replay_error() > 0) == (stuck != 0) and binding.scout_replay_error() == 0
 
 
+def test_a_wait_that_gave_up_is_seen_by_everybody_who_looks():
+    """One reader does not take the count from another, and results of such a call are refused before anybody votes on them."""
+    from paper_2608_11034_b200 import binding, layer_replay, replay
+    layer = layer_replay.make_layer(130, 264, 2, 1, 64)
+    before = binding.scout_replay_waits()
+    layer_replay.replay_layer(layer, layer.codes, layer.exps)
+    assert binding.scout_replay_waits() == before
+    out = torch.empty(16, dtype=torch.int32, device="cuda")
+    with pytest.raises(replay.WaitGaveUp):
+        with replay.waits_checked(torch.device("cuda")):
+            binding.scout_selftest_give_up(1, out.data_ptr(), torch.cuda.current_stream().cuda_stream)
+            with replay.waits_checked(torch.device("cuda")):
+                pass
+    now = binding.scout_replay_waits()
+    assert now > before and binding.scout_replay_error() == now - before
+    assert binding.scout_replay_waits() == now and binding.scout_replay_error() == 0
+    with replay.waits_checked(torch.device("cuda")):          # and the next call is judged by itself
+        layer_replay.replay_layer(layer, layer.codes, layer.exps)
+
+
 def test_refusals_of_the_selftest():
     from paper_2608_11034_b200 import binding
     for stuck, out in ((256, 256), (0, 0)):
