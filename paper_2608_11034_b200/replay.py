@@ -225,15 +225,21 @@ def _product(shape, stride, dtype, device, rows, codes_device, ins, dw_shape, dw
     return _CODE[dtype], _CODE[dw_dtype], outs, row, dw_row, binding.scout_ckpt_wgrad_workspace(_CODE[dtype], rows, outs, ins)
 
 
-def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, *, out_dtype: torch.dtype = torch.float32,
+def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, *, out_dtype: Optional[torch.dtype] = None,
                      grad: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Weight gradient dW = dy^T x of y = x W^T, x taken from its checkpoint.  dy: [rows, outs], bfloat16 or float16.
-    -> dW [outs, ins] in out_dtype (float32 or dy's); with `grad` (of those dtypes) dW is added to it in place."""
+    -> dW [outs, ins] in out_dtype (float32, which is the default, or dy's); with `grad` (of those dtypes) dW is added to it in
+    place, and out_dtype may only repeat its dtype."""
     rows, ins, code_stride = _checkpoint(codes.shape, codes.stride(), codes.dtype, codes.device, exps.shape, exps.stride(),
                                          exps.dtype, exps.device)
     if dy.dim() != 2:
         _fail("dy: a matrix with adjacent row elements is wanted")
-    dw = dy.new_empty((dy.shape[1], ins), dtype=out_dtype) if grad is None else grad
+    if grad is None:
+        dw = dy.new_empty((dy.shape[1], ins), dtype=out_dtype or torch.float32)
+    else:
+        if out_dtype not in (None, grad.dtype):
+            _fail("grad is added to in its own dtype; out_dtype names another")
+        dw = grad
     code, dw_code, outs, dy_stride, dw_stride, nbytes = _product(dy.shape, dy.stride(), dy.dtype, dy.device, rows, codes.device, ins,
                                                                  dw.shape, dw.stride(), dw.dtype, dw.device)
     ws = dy.new_empty(nbytes, dtype=torch.uint8) if nbytes else None
