@@ -1104,7 +1104,10 @@ extern "C" int scout_attn_backward(const scout_attn_t *a, const void *q, const v
     b.stats = (float2 *)workspace;
     const bool wide = a->head_dim > 64, bf16 = a->dtype == SCOUT_DT_BF16;
     BackwardViews views;
-    const BackwardViews *maps = worth_tensor(*a) && backward_views(b.p, bf16, dq, dk, dv, &views) ? &views : nullptr;
+    bool fits = false;
+    if (worth_tensor(*a))
+        if (int rc = backward_views(b.p, bf16, dq, dk, dv, &views, &fits)) return rc;
+    const BackwardViews *maps = fits ? &views : nullptr;
     if (maps) s = shape(*a, true);
     b.part_q = (float *)((uint8_t *)workspace + s.stats_bytes), b.part_kv = (float *)((uint8_t *)b.part_q + s.part_q_bytes);
     const cudaStream_t st = (cudaStream_t)stream;

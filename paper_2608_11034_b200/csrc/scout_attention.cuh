@@ -287,17 +287,20 @@ __device__ __forceinline__ void row_dkv(const Problem &p, const float2 *stats, i
 }
 
 // ---- the tcgen05 kernels (scout_attention_tc.cu, scout_attention_bwd_tc.cu) ---------------------------
-// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch); false where TMA cannot address it.
-bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box);
+// Whether TMA can address tensors of these strides (in bytes they have 40 bits): a matter of the description alone, so that equal
+// calls always take the same kernel.  What fails later is an error.
+bool addressable(const Strides &s);
+// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch).
+int tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box);
 // *taken is false where TMA cannot address a tensor and nothing was enqueued; with splits > 1 it writes fp32 parts:
 // part_o [splits][rows][head_dim], not divided by the sums, and part_ml [splits][rows] {m, l}
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, int splits, float *part_o, float2 *part_ml, cudaStream_t stream, bool *taken);
-// The backward pass's views; false where TMA cannot address a tensor.  The call writes the results or, with splits > 1, fp32 parts
+// The backward pass's views; *fits is false where TMA cannot address a tensor.  The call writes the results or, with splits > 1, fp32 parts
 // of them: [q_splits][rows][head_dim] for dQ, [kv_splits][2][keys][head_dim] for dK and dV.
 struct BackwardViews {
     CUtensorMap q, k, v, d_o, dq, dk, dv;
 };
-bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v);
+int backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v, bool *fits);
 int backward_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, void *dk, void *dv, float *part_q, int q_splits, float *part_kv, int kv_splits,
                     const BackwardViews &v, cudaStream_t stream);
 

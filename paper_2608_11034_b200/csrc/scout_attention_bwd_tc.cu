@@ -641,14 +641,18 @@ template <typename T, int HD> int run_backward(TcBackwardArgs &a, const Backward
 
 }  // namespace
 
-bool backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v) {
+int backward_views(const Problem &p, bool bf16, void *dq, void *dk, void *dv, BackwardViews *v, bool *fits) {
     // blocks are numbered in 31 bits
     const int64_t most = (int64_t)p.batch * ((p.q_len / ROWS + 1ll) * p.q_heads + (p.kv_len / ROWS + 1ll) * p.kv_heads);
-    if (most > 0x7FFFFFFF / 64) return false;
-    return tensor_view(&v->q, bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&v->k, bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, ROWS) &&
-           tensor_view(&v->v, bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, ROWS) && tensor_view(&v->d_o, bf16, p.d_o, p.sg, p, p.q_len, p.q_heads, ROWS) &&
-           tensor_view(&v->dq, bf16, dq, p.sq, p, p.q_len, p.q_heads, 32) && tensor_view(&v->dk, bf16, dk, p.sk, p, p.kv_len, p.kv_heads, 32) &&
-           tensor_view(&v->dv, bf16, dv, p.sv, p, p.kv_len, p.kv_heads, 32);
+    *fits = most <= 0x7FFFFFFF / 64 && addressable(p.sq) && addressable(p.sk) && addressable(p.sv) && addressable(p.sg);
+    if (!*fits) return SCOUT_OK;
+    if (int rc = tensor_view(&v->q, bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS)) return rc;
+    if (int rc = tensor_view(&v->k, bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, ROWS)) return rc;
+    if (int rc = tensor_view(&v->v, bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, ROWS)) return rc;
+    if (int rc = tensor_view(&v->d_o, bf16, p.d_o, p.sg, p, p.q_len, p.q_heads, ROWS)) return rc;
+    if (int rc = tensor_view(&v->dq, bf16, dq, p.sq, p, p.q_len, p.q_heads, 32)) return rc;
+    if (int rc = tensor_view(&v->dk, bf16, dk, p.sk, p, p.kv_len, p.kv_heads, 32)) return rc;
+    return tensor_view(&v->dv, bf16, dv, p.sv, p, p.kv_len, p.kv_heads, 32);
 }
 int backward_tensor(const Problem &p, bool bf16, const float2 *stats, void *dq, void *dk, void *dv, float *part_q, int q_splits, float *part_kv, int kv_splits,
                     const BackwardViews &v, cudaStream_t stream) {

@@ -394,22 +394,25 @@ int run_forward(const Problem &p, void *o, float *lse, int splits, float *part_o
 
 }  // namespace
 
-// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch); false where TMA cannot address it.
-bool tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box) {
+bool addressable(const Strides &s) { return s.t < 1ll << 39 && s.h < 1ll << 39 && s.b < 1ll << 39; }
+
+// The [batch, tokens, heads, head_dim] tensor as (d, token, head, batch).
+int tensor_view(CUtensorMap *m, bool bf16, const void *x, const Strides &s, const Problem &p, int tokens, int heads, uint32_t box) {
     const uint64_t dims[4] = {(uint64_t)p.head_dim, (uint64_t)tokens, (uint64_t)heads, (uint64_t)p.batch};
     uint64_t strides[3] = {(uint64_t)s.t * 2, (uint64_t)s.h * 2, (uint64_t)s.b * 2};
-    for (uint64_t &y : strides) {
+    for (uint64_t &y : strides)
         if (y == 0) y = (uint64_t)p.head_dim * 2;  // an axis of one element
-        if (y >= 1ull << 40) return false;
-    }
-    return tc::tensor_map(m, bf16, x, 4, dims, strides, box) == SCOUT_OK;
+    return tc::tensor_map(m, bf16, x, 4, dims, strides, box);
 }
 
 int forward_tensor(const Problem &p, bool bf16, void *o, float *lse, int splits, float *part_o, float2 *part_ml, cudaStream_t stream, bool *taken) {
     CUtensorMap m[4];
-    *taken = p.batch < 65536 && p.q_len < 65535 / splits * ROWS && tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS) && tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS) &&
-             tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS) && tensor_view(&m[3], bf16, o, p.so, p, p.q_len, p.q_heads, 32);
+    *taken = p.batch < 65536 && p.q_len < 65535 / splits * ROWS && addressable(p.sq) && addressable(p.sk) && addressable(p.sv) && addressable(p.so);
     if (!*taken) return SCOUT_OK;
+    if (int rc = tensor_view(&m[0], bf16, p.q, p.sq, p, p.q_len, p.q_heads, ROWS)) return rc;
+    if (int rc = tensor_view(&m[1], bf16, p.k, p.sk, p, p.kv_len, p.kv_heads, KEYS)) return rc;
+    if (int rc = tensor_view(&m[2], bf16, p.v, p.sv, p, p.kv_len, p.kv_heads, KEYS)) return rc;
+    if (int rc = tensor_view(&m[3], bf16, o, p.so, p, p.q_len, p.q_heads, 32)) return rc;
     if (p.head_dim > 64)
         return bf16 ? run_forward<__nv_bfloat16, 128>(p, o, lse, splits, part_o, part_ml, m, stream) : run_forward<__half, 128>(p, o, lse, splits, part_o, part_ml, m, stream);
     return bf16 ? run_forward<__nv_bfloat16, 64>(p, o, lse, splits, part_o, part_ml, m, stream) : run_forward<__half, 64>(p, o, lse, splits, part_o, part_ml, m, stream);

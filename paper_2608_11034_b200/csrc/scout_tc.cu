@@ -40,9 +40,19 @@ int tensor_map(CUtensorMap *map, bool bf16, const void *base, int rank, const ui
     cuuint32_t box[5] = {64, box_rows, 1, 1, 1}, one[5] = {1, 1, 1, 1, 1};
     for (int i = 0; i < rank; ++i) d[i] = dims[i];
     for (int i = 0; i + 1 < rank; ++i) s[i] = strides[i];
-    const CUresult r = f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void *>(base),
-                         d, s, box, one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
-                         CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    const auto encode = [&] {
+        return f(map, bf16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16 : CU_TENSOR_MAP_DATA_TYPE_FLOAT16, (cuuint32_t)rank, const_cast<void *>(base), d, s, box,
+                 one, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+    };
+    CUresult r = encode();
+    if (r != CUDA_SUCCESS) {
+        // The driver's calls want a context on the calling thread, which the runtime puts there with the thread's first call of its own
+        // that needs one: in a new thread (autograd's, say) that may still be to come.
+        int dev = 0;
+        SCOUT_CUDA(cudaGetDevice(&dev));
+        SCOUT_CUDA(cudaSetDevice(dev));
+        r = encode();
+    }
     if (r != CUDA_SUCCESS) {
         set_cuda_error(cudaErrorInvalidValue, "cuTensorMapEncodeTiled");
         return SCOUT_ERR_CUDA;
