@@ -16,6 +16,11 @@ allocator on the current stream and enqueues the library's kernels there
 lie: as usual in torch, one made on another stream needs that stream's work
 waited for, and ``record_stream`` if it is freed early.
 
+None of the calls is recorded by autograd.  Where it would be asked to (grad mode on,
+an input of attention or of the weight gradient that requires a gradient), they raise
+instead of dropping the gradient: call them under torch.no_grad(), or from the
+forward and backward of a torch.autograd.Function, where grad mode is off.
+
 The kernels' waits are bounded.  A call in which one gave up has no valid results, and
 cannot say so itself, since it only enqueues: ``with waits_checked(device):`` around
 the calls raises WaitGaveUp before anybody signs or votes on what they left.
@@ -55,6 +60,11 @@ def waits_checked(device: torch.device):
 
 def _fail(what: str):
     raise ValueError(what)
+
+
+def _no_autograd(*tensors) -> None:
+    if torch.is_grad_enabled() and any(x.requires_grad for x in tensors):
+        _fail("autograd does not record this call: use torch.no_grad() or a torch.autograd.Function")
 
 
 class _Attention:
@@ -127,6 +137,7 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
     window: with causal, only its own position and the window - 1 before it (0: all).
     q_lens, kv_lens: int32 [batch], the tokens in use of padded sequences.
     -> (o like q, lse float32 [batch, q_heads, q_len]); rows that see nothing give 0 and -inf."""
+    _no_autograd(q, k, v)
     o = torch.empty_like(q)
     shape = q.shape
     t = _attention((q.dtype, k.dtype, v.dtype), (q.device, k.device, v.device), shape, k.shape, v.shape, shape, shape,
@@ -145,6 +156,7 @@ def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: tor
     """Gradients of attention_forward's o with respect to q, k and v, from the gradient `do` of o and what the
     forward pass returned; the other arguments as there.  Gradients of key heads that several query heads share are
     summed over those.  -> (dq, dk, dv), laid out like q, k, v."""
+    _no_autograd(q, k, v, o, do)
     t = _attention((q.dtype, k.dtype, v.dtype, o.dtype, do.dtype), (q.device, k.device, v.device, o.device, do.device), q.shape,
                    k.shape, v.shape, o.shape, do.shape, q.stride(), k.stride(), v.stride(), o.stride(), do.stride(), causal, window,
                    scale if scale is None else float(scale))
@@ -232,6 +244,7 @@ def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, 
     place, and out_dtype may only repeat its dtype."""
     rows, ins, code_stride = _checkpoint(codes.shape, codes.stride(), codes.dtype, codes.device, exps.shape, exps.stride(),
                                          exps.dtype, exps.device)
+    _no_autograd(dy) if grad is None else _no_autograd(dy, grad)
     if dy.dim() != 2:
         _fail("dy: a matrix with adjacent row elements is wanted")
     if grad is None:

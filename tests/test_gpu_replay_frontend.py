@@ -18,3 +18,39 @@ def test_a_type_for_the_result_that_is_not_the_accumulated_gradients():
         assert (grad == 0).all()
         assert replay.checkpoint_wgrad(dy, codes, exps, grad=grad, out_dtype=have) is grad
         assert torch.equal(grad, replay.checkpoint_wgrad(dy, codes, exps, out_dtype=have))
+
+
+def test_a_gradient_is_not_dropped_without_a_word():
+    """Grad mode on and an input that requires a gradient: an error.  Off, or inside an autograd.Function, the calls run, and the
+    function's gradients are the formula's."""
+    from paper_2608_11034_b200 import replay
+
+    class Attention(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, q, k, v):
+            o, lse = replay.attention_forward(q, k, v, causal=True)
+            ctx.save_for_backward(q, k, v, o, lse)
+            return o
+
+        @staticmethod
+        def backward(ctx, do):
+            return replay.attention_backward(*ctx.saved_tensors, do.contiguous(), causal=True)
+
+    g = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v = (torch.randn(1, 130, 2, 64, generator=g, device="cuda").to(BF).requires_grad_() for _ in range(3))
+    do = torch.randn(1, 130, 2, 64, generator=g, device="cuda").to(BF)
+    for x in ((q, k.detach(), v.detach()), (q.detach(), k.detach(), v)):
+        with pytest.raises(ValueError):
+            replay.attention_forward(*x)
+    with torch.no_grad():
+        o, lse = replay.attention_forward(q, k, v, causal=True)
+        want = replay.attention_backward(q, k, v, o, lse, do, causal=True)
+    with pytest.raises(ValueError):
+        replay.attention_backward(q, k, v, o, lse, do, causal=True)
+    Attention.apply(q, k, v).backward(do)
+    assert all(torch.equal(x.grad, y) for x, y in zip((q, k, v), want))
+    codes, exps = replay.checkpoint_pack(q.view(130, 128))          # whole numbers: nothing to record
+    dy = torch.randn(130, 8, device="cuda").to(BF)
+    replay.checkpoint_wgrad(dy, codes, exps)
+    with pytest.raises(ValueError):
+        replay.checkpoint_wgrad(dy.requires_grad_(), codes, exps)
