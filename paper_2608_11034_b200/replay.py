@@ -152,18 +152,23 @@ def attention_forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, caus
 
 def attention_backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, o: torch.Tensor, lse: torch.Tensor,
                        do: torch.Tensor, *, causal: bool = False, window: int = 0, scale: Optional[float] = None,
-                       q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None):
+                       q_lens: Optional[torch.Tensor] = None, kv_lens: Optional[torch.Tensor] = None, grads=None):
     """Gradients of attention_forward's o with respect to q, k and v, from the gradient `do` of o and what the
     forward pass returned; the other arguments as there.  Gradients of key heads that several query heads share are
-    summed over those.  -> (dq, dk, dv), laid out like q, k, v."""
-    _no_autograd(q, k, v, o, do)
+    summed over those.  -> (dq, dk, dv), laid out like q, k, v.
+
+    grads: the three tensors to write, which q, k and v that are parts of one projection's output need: the same parts of a
+    gradient laid out like that output.  They do not overlap."""
+    _no_autograd(q, k, v, o, do, *(grads or ()))
     t = _attention((q.dtype, k.dtype, v.dtype, o.dtype, do.dtype), (q.device, k.device, v.device, o.device, do.device), q.shape,
                    k.shape, v.shape, o.shape, do.shape, q.stride(), k.stride(), v.stride(), o.stride(), do.stride(), causal, window,
                    scale if scale is None else float(scale))
-    dq, dk, dv = torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)
+    dq, dk, dv = (torch.empty_like(q), torch.empty_like(k), torch.empty_like(v)) if grads is None else grads
     for x, y, name in ((q, dq, "q"), (k, dk, "k"), (v, dv, "v")):
+        if grads is not None and (y.shape != x.shape or y.dtype != x.dtype or y.device != x.device):
+            _fail(f"grads: d{name} has the shape, dtype and device of {name}")
         if x.stride() != y.stride():
-            _fail(f"{name}: overlapping or gapped memory has no gradient laid out like it; pass {name}.contiguous()")
+            _fail(f"{name}: overlapping or gapped memory has no gradient laid out like it; pass {name}.contiguous(), or grads")
     if lse.dtype != torch.float32 or lse.shape != t.rows or not lse.is_contiguous() or lse.device != q.device:
         _fail("lse: the forward pass's, a contiguous float32 tensor [batch, q_heads, q_len]")
     ql, kl = _lens(q_lens, t.batch, q.device, "q_lens"), _lens(kv_lens, t.batch, q.device, "kv_lens")

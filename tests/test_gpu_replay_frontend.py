@@ -1,4 +1,6 @@
 """What the torch front end of the replay operators refuses rather than doing something other than was asked for."""
+import math
+
 import pytest
 import torch
 
@@ -54,3 +56,36 @@ def test_a_gradient_is_not_dropped_without_a_word():
     replay.checkpoint_wgrad(dy, codes, exps)
     with pytest.raises(ValueError):
         replay.checkpoint_wgrad(dy.requires_grad_(), codes, exps)
+
+
+@pytest.mark.parametrize("B,T,Hq,Hk,D,bad", [(2, 131, 4, 2, 64, False), (2, 131, 4, 2, 64, True), (1, 300, 6, 3, 128, True), (2, 70, 4, 1, 80, True),
+                                             (1, 2600, 1, 1, 64, False), (1, 2600, 1, 1, 64, True)])
+def test_queries_keys_and_values_of_one_projection(B, T, Hq, Hk, D, bad):
+    """Parts of one output, and their gradients into the same parts of one gradient: the bits of separate tensors, and nothing beside
+    them is written; rows that are made again for a NaN included."""
+    from paper_2608_11034_b200 import replay
+    g = torch.Generator(device="cuda").manual_seed(3)
+    width, gap = (Hq + 2 * Hk) * D, 24
+    room = torch.randn(B, T, width + gap, generator=g, device="cuda").to(BF)
+    do = torch.randn(B, T, Hq, D, generator=g, device="cuda").to(BF)
+    if bad:
+        room[0, T // 2, (Hq + Hk) * D + 3] = math.nan      # in the values of one token
+
+    def parts(x):
+        cut = [0, Hq * D, (Hq + Hk) * D, width]
+        return [x[..., a:b].unflatten(-1, (-1, D)) for a, b in zip(cut, cut[1:])]
+
+    q, k, v = parts(room)
+    flat = [x.contiguous() for x in (q, k, v)]
+    o, lse = replay.attention_forward(*flat, causal=True)
+    want = replay.attention_backward(*flat, o, lse, do, causal=True)
+    with pytest.raises(ValueError):
+        replay.attention_backward(q, k, v, o, lse, do, causal=True)
+    grad = torch.full_like(room, 7.0)
+    got = replay.attention_backward(q, k, v, o, lse, do, causal=True, grads=parts(grad))
+    same = lambda a, b: torch.equal(a.view(torch.int16), b.view(torch.int16))          # noqa: E731  - NaN included
+    assert all(same(a.contiguous(), b) for a, b in zip(got, want)) and (grad[..., width:] == 7.0).all()
+    assert any(x.isnan().any() for x in want) == bad
+    for wrong in (parts(grad.half()), parts(grad[:, :-1]), [x.contiguous() for x in parts(grad)], parts(grad.cpu())):
+        with pytest.raises(ValueError):
+            replay.attention_backward(q, k, v, o, lse, do, causal=True, grads=wrong)
