@@ -142,3 +142,58 @@ def test_powers_of_two_by_multiply_adds():
     want = torch.log(1.0 + (Tk - 1) * torch.exp(-depth))
     bound = 2.7e-6 + 2.0 ** -24 * (16 * math.log(2) * 2 + 8 + 2 * 6)
     assert ((lse[0, 0].double() - want).abs() <= bound).all()
+
+
+def where_nan_belongs(q, k, v, do, see, group):
+    """Truth values in [batch, heads, tokens, head_dim]: which elements of o, dq, dk, dv (and of lse) the formulas make NaN, from
+    where the inputs are.  see: [batch, 1, q_len, kv_len]."""
+    up = lambda x: x.isnan().permute(0, 2, 1, 3)                                      # noqa: E731
+    Q, G = up(q), up(do)
+    K, V = (up(x).repeat_interleave(group, 1) for x in (k, v))
+    see = see.expand(-1, Q.shape[1], -1, -1)
+    reach = lambda a, b: (a.float() @ b.float()) > 0                                  # noqa: E731
+    score = see & (Q.any(-1)[..., :, None] | K.any(-1)[..., None, :])
+    lse = score.any(-1)
+    o = lse[..., None] | reach(see, V)
+    p = see & (score | lse[..., None])
+    delta = see.any(-1) & (o | G).any(-1)
+    ds = see & (p | G.any(-1)[..., :, None] | V.any(-1)[..., None, :] | delta[..., None])
+    dq = ds.any(-1)[..., None] | reach(see, K)
+    back = lambda x: x.view(x.shape[0], -1, group, *x.shape[2:]).any(2)               # noqa: E731
+    dk = back(ds.any(-2)[..., None] | reach(see.transpose(-1, -2), Q))
+    dv = back(p.any(-2)[..., None] | reach(see.transpose(-1, -2), G))
+    return lse, o, dq, dk, dv
+
+
+@pytest.mark.parametrize("seed", range(1150, 1310))
+def test_nan_is_where_the_formulas_put_it_and_nowhere_else(seed):
+    """A few NaN anywhere in the inputs, single elements and whole tokens, under every mask and in every kernel."""
+    import random
+    from paper_2608_11034_b200 import replay
+    r = random.Random(seed)
+    dtype, B, Hk, group, D = r.choice([BF, HF]), r.randint(1, 2), r.choice([1, 2]), r.choice([1, 2, 3]), r.choice([8, 64, 72, 128])
+    Tk = r.choice([r.randint(1, 40), r.randint(90, 500)])
+    Tq = r.choice([Tk, Tk, r.randint(1, 500), r.randint(1, 20)])
+    causal = r.random() < 0.65
+    window = r.choice([0, 0, 1, r.randint(2, 300)]) if causal else 0
+    q, k, v, do = make(seed, dtype, B, Tq, Tk, Hk * group, Hk, D)
+    for x in (q, k, v, do):
+        for _ in range(r.choice([0, 1, 1, 3])):
+            at = tuple(r.randrange(s) for s in x.shape)
+            x[at if r.random() < 0.7 else at[:3]] = math.nan
+    ql = kl = None
+    if r.random() < 0.4:
+        ql, kl = (torch.tensor([r.randint(0, t) for _ in range(B)], dtype=torch.int32, device="cuda") for t in (Tq, Tk))
+    see = torch.zeros(B, 1, Tq, Tk, dtype=torch.bool, device="cuda")
+    for b in range(B):
+        nq, nk = Tq if ql is None else int(ql[b]), Tk if kl is None else int(kl[b])
+        for i in range(nq):
+            keys = defn.seen_by_row(i, nq, nk, causal, window)
+            see[b, 0, i, keys.start:keys.stop] = True
+    kw = dict(causal=causal, window=window, q_lens=ql, kv_lens=kl)
+    o, lse = replay.attention_forward(q, k, v, **kw)
+    got = (o,) + replay.attention_backward(q, k, v, o, lse, do, **kw)
+    want = where_nan_belongs(q, k, v, do, see, group)
+    assert torch.equal(lse.isnan(), want[0])
+    for name, x, w in zip(("o", "dq", "dk", "dv"), got, want[1:]):
+        assert torch.equal(x.permute(0, 2, 1, 3).isnan(), w), name
