@@ -12,12 +12,19 @@
 // two change places every step.  (P through shared memory instead: 3418 cycles a step instead of the 2048 of its
 // products; 384 KiB a step pass through shared memory then, at 128 bytes a cycle.)
 //
-// One kernel that added dQ from blocks of keys would need 5 products instead of 4 + 3, but its sums would cross blocks:
-// float atomics give other bits on every run, and these gradients are compared bit by bit.
+// One kernel that added dQ from blocks of keys would need 5 products instead of 4 + 3.  Its sums would cross blocks: float
+// atomics give other bits on every run, and these gradients are compared bit by bit.  Blocks that add in a fixed order, each
+// waiting for the one before, would give the same bits too; that form is not built.
+//
+// P and dS are rounded to the inputs' type, as in the forward pass, since the matrix instructions take 16-bit operands.  Against 64
+// bits the gradients are 40 % further off than those of an fp32 form rounded once (2 x 2048 tokens, bf16: 2.5e-3, 1.8e-3).
+// dP of the next step is written over P and dS (dQ: over dS) right behind the products that read them: matrix instructions of
+// one block are taken to execute in the order of issue, also where they have different accumulators (the ISA's list of ordered
+// pairs names those with the same accumulator and shape).
 //
 // What bounds it (HD = 128): dK, dV 2048 cycles of products a step, 288 KiB through shared memory (2250 cycles); dQ 1536 and 224 KiB (1750), 1927
-// measured.  2 x 2048 tokens, 32/8 heads, causal: 221 us with the statistics, 0.78 PFLOP/s of the five products that are asked for, 1.09
-// of the seven that are made.
+// measured.  2 x 2048 tokens, 32/8 heads, causal: 220 us with the statistics (device time on warm data; a call 260), 0.78 PFLOP/s of the
+// five products that are asked for, 1.09 of the seven that are made.
 #include <algorithm>
 
 #include "scout_attention.cuh"

@@ -10,10 +10,18 @@
 // then the accumulated O is rescaled in tensor memory, which after the first blocks hardly ever happens.  Any
 // reference point gives the same quotient O / l; the sums stay far inside fp32 and the 16-bit range.
 //
+// P is rounded to the inputs' type, since the matrix instructions take two 16-bit operands of one type.  Against 64 bits the
+// results are a quarter further off than those of an fp32 softmax that is rounded once (2 x 2048 tokens, bf16: 2.0e-3 of the
+// result's size, 1.6e-3).  The sum l is of the unrounded P.
+//
+// S of the next keys is written over P right behind the product that reads P: matrix instructions of one block are taken to
+// execute in the order of issue, also where they have different accumulators (the ISA's list of ordered pairs names those with
+// the same accumulator and shape).
+//
 // What bounds it (HD = 128): a step of two slots and 128 keys is 2048 cycles of products and as many of shared-memory reads; it takes
 // 2785 where every key is visible, because a slot's softmax (1780 cycles, of which 128 exponentials a row) and its hand-over to the
 // next product do not quite fit behind the other slot's products.  8191 tokens, 32/8 heads, causal: 1.15 to 1.31 PFLOP/s at the power limit;
-// 2 x 2048 tokens: 72 us, of which about 5 us for the start and end of each of 3.5 blocks an SM.
+// 2 x 2048 tokens: 71 us (device time on warm data; a call 83), of which about 5 us for the start and end of each of 3.5 blocks an SM.
 #include <algorithm>
 #include <type_traits>
 

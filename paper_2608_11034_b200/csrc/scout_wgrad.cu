@@ -17,8 +17,9 @@
 // of instruction).  Both kernels therefore cut their chains at 1024 tokens and add them in fp32, rounding to nearest (3.8e-7;
 // tokens of one sign: a bias of 1.9e-7).
 //
-// What bounds wgrad_tc: the products.  8192 x 14336 x 4096: 700 to 850 us (1.13 to 1.37 PFLOP/s; the power limit decides, the measured
-// sustained rate being 1.40); 4096^3 into fp32: 109 us with the restore, 512 tiles being 3.46 rounds of 148 blocks.
+// What bounds wgrad_tc: the products.  8192 x 14336 x 4096: 690 to 850 us (1.13 to 1.39 PFLOP/s; the power limit decides, the measured
+// sustained rate being 1.40); 4096^3 into fp32: 108 us with the restore (device time on warm data; a call 131), 512 tiles being 3.46
+// rounds of 148 blocks.  Its 128 sums beside what a step needs do not fit 168 registers: 160 bytes a thread are spilled.
 #include <algorithm>
 
 #include "scout_attention.cuh"
