@@ -48,7 +48,11 @@ class WaitGaveUp(RuntimeError):
 @contextlib.contextmanager
 def waits_checked(device: torch.device):
     """Raises WaitGaveUp if a wait of the replay kernels gave up on `device` between entry and exit, on any of its streams
-    (synchronises the device at both)."""
+    (synchronises the device at both).  While a CUDA graph is captured nothing runs and nothing is checked: that is for
+    whoever replays the graph."""
+    if torch.cuda.is_initialized() and torch.cuda.is_current_stream_capturing():
+        yield
+        return
     with torch.cuda.device(device):
         before = binding.scout_replay_waits()
     yield

@@ -41,6 +41,19 @@ def test_a_wait_that_gave_up_is_seen_by_everybody_who_looks():
         layer_replay.replay_layer(layer, layer.codes, layer.exps)
 
 
+def test_a_captured_replay_is_checked_where_the_graph_runs():
+    from paper_2608_11034_b200 import layer_replay, replay
+    layer = layer_replay.make_layer(130, 264, 2, 1, 64)
+    want = layer_replay.replay_layer(layer, layer.codes, layer.exps)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = layer_replay.replay_layer(layer, layer.codes, layer.exps)
+    with replay.waits_checked(torch.device("cuda")):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert all(torch.equal(got[n], want[n]) for n in want)
+
+
 def test_refusals_of_the_selftest():
     from paper_2608_11034_b200 import binding
     for stuck, out in ((256, 256), (0, 0)):
