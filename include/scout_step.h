@@ -1,0 +1,125 @@
+/*
+ * scout_step.h - operators of a replayed training step around its layers, on the device.
+ *
+ * A replay that starts from the step's tokens and ends at its loss (Sec. 6) leaves more
+ * surfaces than a layer's: the embedding table's gradient, the activations and norms
+ * between blocks, the loss of every token and the gradients of the output projection.
+ * Exact consensus (Sec. 5.3) compares their bits, so these operators too give the same
+ * bits wherever the hardware is healthy: no floating-point atomics, every sum in an order
+ * that the sizes and the token ids fix, and random numbers from a counter.
+ *
+ *   scout_embed_forward / scout_embed_backward   rows of a table, and the table's gradient
+ *   scout_dropout                                and its gradient, which is the same call
+ *   scout_join_forward / scout_join_backward     a block's output joins the residual stream:
+ *        norm, dropout, gate and scale, sum, the next block's norm
+ *
+ * Conventions are those of scout_replay.h: plain C, error codes, caller-owned memory, work
+ * enqueued on `stream`, scratch of the size the *_workspace calls return (256-byte aligned,
+ * no initialisation, one for each of two calls that may run at the same time).  Matrices
+ * have a row stride in elements, at least their columns, and adjacent columns; they are
+ * aligned to their element size, and rows that lie on 16-byte boundaries are faster.
+ * Types are SCOUT_DT_F32, SCOUT_DT_BF16 and SCOUT_DT_F16; sums, statistics and products of
+ * elements are fp32, rounded to the result's type once.  Inputs and outputs of a call do
+ * not overlap, save where it says so.
+ */
+#ifndef SCOUT_STEP_H
+#define SCOUT_STEP_H
+
+#include "scout.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/* ---- token embedding ----------------------------------------------------------------
+ * y[t] = scale * table[ids[t]], and zeros where ids[t] is outside 0..vocab-1 (padding, or
+ * a token of another part of the vocabulary).
+ *   id_dtype     SCOUT_DT_I32 or SCOUT_DT_I64
+ *   dtype        of table;  out_dtype  of y: dtype or SCOUT_DT_F32
+ *   ids          device [rows]
+ *   table        device [vocab][dim], row stride table_stride
+ *   y            device [rows][dim], row stride y_stride
+ *   scale        finite */
+SCOUT_API int scout_embed_forward(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows,
+                                  uint64_t dim, uint64_t vocab, const void *ids, const void *table,
+                                  uint64_t table_stride, float scale, void *y, uint64_t y_stride, void *stream);
+
+/* d_table[v] = (accumulate ? d_table[v] : 0) + scale * sum over t with ids[t] = v of dy[t]
+ * Tokens are sorted by id; the sum over a token's places runs in their order, in pieces
+ * whose borders follow from the sizes and the ids.  With accumulate, rows without a token
+ * are neither read nor written; without it every row is written.  What stands in dy where
+ * the id is outside 0..vocab-1 is not read.
+ *   dtype        of dy;  out_dtype  of d_table: dtype or SCOUT_DT_F32
+ * rows up to 2^30, vocab up to 2^31 - 1; beyond that SCOUT_ERR_UNSUPPORTED. */
+SCOUT_API int scout_embed_backward_workspace(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t *bytes);
+SCOUT_API int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows,
+                                   uint64_t dim, uint64_t vocab, const void *ids, const void *dy,
+                                   uint64_t dy_stride, float scale, void *d_table, uint64_t d_table_stride,
+                                   uint32_t accumulate, void *workspace, uint64_t workspace_bytes, void *stream);
+
+/* ---- dropout from a counter ------------------------------------------------------------
+ * Place (r, c) of a matrix has the 16-bit number h_{c mod 8} of the eight that
+ *     Philox4x32-10(counter = (c / 8, r, offset low, offset high), key = (seed low, seed high))
+ * returns (low half of a word before its high half), with offset = `offset` + (d_offset ?
+ * *d_offset : 0) modulo 2^64.  With cut = min(65535, floor(65536 p + 1/2)) it is kept where
+ * h >= cut:
+ *     y = x * (65536 / (65536 - cut))    where kept, else 0 (whatever x is)
+ * The mask depends on the place, seed and offset alone: it is made again wherever it is
+ * needed and never stored.  The gradient of x is the same call on the gradient of y.
+ *   p            0 <= p < 1
+ *   d_offset     device, one number, or NULL; read when the kernel runs, so that a captured
+ *                call can drop other places each time it is replayed
+ * rows up to 2^32, cols up to 2^33.  y may be x. */
+SCOUT_API int scout_dropout(uint32_t dtype, uint64_t rows, uint64_t cols, const void *x, uint64_t x_stride, void *y,
+                            uint64_t y_stride, double p, uint64_t seed, uint64_t offset, const uint64_t *d_offset,
+                            void *stream);
+
+/* ---- a block joins the residual stream ---------------------------------------------------
+ * With x the residual stream, b the block's output, all per row of `dim` elements, and
+ *     rms(z) = (mean of z^2 + eps)^(-1/2):
+ *     u = post ? b * rms(b) * post : b            norm behind the block
+ *     u = dropout(u)                              as scout_dropout, with p, seed, offset
+ *     y = x + scale * gate * u                    (x NULL: 0; gate NULL: 1)
+ *     n = y * rms(y) * norm                       norm before the next block (norm NULL: none)
+ * y is rounded to the stream's type where it is stored; n is made from what it was before.
+ * gate has one row for every rows / groups rows in turn: one of learned scales (groups = 1),
+ * one per sequence, one per token (groups = rows).
+ *   stats        device [2][rows] fp32: rms(b), rms(y); 0 where there is no such norm */
+typedef struct {
+    uint32_t dtype;            /* of b, n, dn, db                                       */
+    uint32_t stream_dtype;     /* of x, y, dy, dx: dtype or SCOUT_DT_F32                */
+    uint32_t weight_dtype;     /* of gate, post, norm and their gradients: the same two */
+    float scale;               /* finite                                                */
+    float eps;                 /* finite, >= 0                                          */
+    uint32_t reserved;         /* 0                                                     */
+    uint64_t rows;             /* up to 2^32                                            */
+    uint64_t dim;              /* 1..16384                                              */
+    uint64_t groups;           /* divides rows; gate is [groups][dim], dense            */
+    /* row strides of forward (x, b, y, n) and backward (dy, dn, b, y, dx, db) */
+    uint64_t x_stride, b_stride, y_stride, n_stride, dy_stride, dn_stride, dx_stride, db_stride;
+} scout_join_t;
+
+SCOUT_API int scout_join_forward(const scout_join_t *j, const void *x, const void *b, const void *gate,
+                                 const void *post, const void *norm, double p, uint64_t seed, uint64_t offset,
+                                 const uint64_t *d_offset, void *y, void *n, float *stats, void *stream);
+
+/* From dy and dn, the gradients of y and n (NULL: zero), over a row:
+ *     t = dn * norm,   z = y * rms(y)
+ *     g = dy + rms(y) (t - z mean(t z))            dx = g
+ *     h = scale * g,   du = dropout(h * gate)      db = du without post, else with
+ *     c = b * rms(b),  s = du * post               db = rms(b) (s - c mean(s c))
+ * and over rows, fp32 sums in an order that the sizes fix:
+ *     d_gate = sum over its rows of h * u,  d_post = sum of du * c,  d_norm = sum of dn * z
+ * y and stats are the forward pass's.  dx, d_gate, d_post, d_norm: NULL where not wanted;
+ * d_gate needs gate, d_post post, d_norm norm and dn. */
+SCOUT_API int scout_join_backward_workspace(const scout_join_t *j, uint64_t *bytes);
+SCOUT_API int scout_join_backward(const scout_join_t *j, const void *dy, const void *dn, const void *b, const void *y,
+                                  const float *stats, const void *gate, const void *post, const void *norm, double p,
+                                  uint64_t seed, uint64_t offset, const uint64_t *d_offset, void *dx, void *db,
+                                  void *d_gate, void *d_post, void *d_norm, void *workspace, uint64_t workspace_bytes,
+                                  void *stream);
+
+#ifdef __cplusplus
+}
+#endif
+#endif /* SCOUT_STEP_H */

@@ -111,6 +111,13 @@ def lib():
             "scout_replay_error": (C.c_int, [C.POINTER(u32)]),
             "scout_replay_waits": (C.c_int, [C.POINTER(u32)]),
             "scout_selftest_give_up": (C.c_int, [u32, vp, vp]),
+            "scout_embed_forward": (C.c_int, [u32, u32, u32, u64, u64, u64, vp, vp, u64, C.c_float, vp, u64, vp]),
+            "scout_embed_backward_workspace": (C.c_int, [u64, u64, u64, C.POINTER(u64)]),
+            "scout_embed_backward": (C.c_int, [u32, u32, u32, u64, u64, u64, vp, vp, u64, C.c_float, vp, u64, u32, vp, u64, vp]),
+            "scout_dropout": (C.c_int, [u32, u64, u64, vp, u64, vp, u64, C.c_double, u64, u64, vp, vp]),
+            "scout_join_forward": (C.c_int, [vp] * 6 + [C.c_double, u64, u64] + [vp] * 5),
+            "scout_join_backward_workspace": (C.c_int, [vp, C.POINTER(u64)]),
+            "scout_join_backward": (C.c_int, [vp] * 9 + [C.c_double, u64, u64] + [vp] * 7 + [u64, vp]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
             "scout_last_cuda_error": (C.c_char_p, []),
@@ -449,6 +456,58 @@ def scout_replay_error() -> int:
 
 def scout_selftest_give_up(stuck: int, d_out: int, stream: int) -> None:
     _check(lib().scout_selftest_give_up(stuck, d_out, stream), "scout_selftest_give_up")
+
+
+# ---- operators of a replayed step around its layers (include/scout_step.h) ------------
+
+JOIN_DTYPE = np.dtype([("dtype", "<u4"), ("stream_dtype", "<u4"), ("weight_dtype", "<u4"), ("scale", "<f4"), ("eps", "<f4"),
+                       ("reserved", "<u4"), ("rows", "<u8"), ("dim", "<u8"), ("groups", "<u8"), ("x_stride", "<u8"),
+                       ("b_stride", "<u8"), ("y_stride", "<u8"), ("n_stride", "<u8"), ("dy_stride", "<u8"), ("dn_stride", "<u8"),
+                       ("dx_stride", "<u8"), ("db_stride", "<u8")])
+
+
+def scout_embed_forward(id_dtype: int, dtype: int, out_dtype: int, rows: int, dim: int, vocab: int, ids: int, table: int,
+                        table_stride: int, scale: float, y: int, y_stride: int, stream: int) -> None:
+    _check(lib().scout_embed_forward(id_dtype, dtype, out_dtype, rows, dim, vocab, ids, table, table_stride, scale, y, y_stride,
+                                     stream), "scout_embed_forward")
+
+
+def scout_embed_backward_workspace(rows: int, dim: int, vocab: int) -> int:
+    n = C.c_uint64()
+    _check(lib().scout_embed_backward_workspace(rows, dim, vocab, C.byref(n)), "scout_embed_backward_workspace")
+    return n.value
+
+
+def scout_embed_backward(id_dtype: int, dtype: int, out_dtype: int, rows: int, dim: int, vocab: int, ids: int, dy: int,
+                         dy_stride: int, scale: float, d_table: int, d_table_stride: int, accumulate: int, workspace: int,
+                         workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_embed_backward(id_dtype, dtype, out_dtype, rows, dim, vocab, ids, dy, dy_stride, scale, d_table,
+                                      d_table_stride, accumulate, workspace, workspace_bytes, stream), "scout_embed_backward")
+
+
+def scout_dropout(dtype: int, rows: int, cols: int, x: int, x_stride: int, y: int, y_stride: int, p: float, seed: int, offset: int,
+                  d_offset: int, stream: int) -> None:
+    _check(lib().scout_dropout(dtype, rows, cols, x, x_stride, y, y_stride, p, seed, offset, d_offset, stream), "scout_dropout")
+
+
+def scout_join_forward(join: int, x: int, b: int, gate: int, post: int, norm: int, p: float, seed: int, offset: int, d_offset: int,
+                       y: int, n: int, stats: int, stream: int) -> None:
+    """join: address of one JOIN_DTYPE record."""
+    _check(lib().scout_join_forward(join, x, b, gate, post, norm, p, seed, offset, d_offset, y, n, stats, stream),
+           "scout_join_forward")
+
+
+def scout_join_backward_workspace(join: int) -> int:
+    n = C.c_uint64()
+    _check(lib().scout_join_backward_workspace(join, C.byref(n)), "scout_join_backward_workspace")
+    return n.value
+
+
+def scout_join_backward(join: int, dy: int, dn: int, b: int, y: int, stats: int, gate: int, post: int, norm: int, p: float, seed: int,
+                        offset: int, d_offset: int, dx: int, db: int, d_gate: int, d_post: int, d_norm: int, workspace: int,
+                        workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_join_backward(join, dy, dn, b, y, stats, gate, post, norm, p, seed, offset, d_offset, dx, db, d_gate, d_post,
+                                     d_norm, workspace, workspace_bytes, stream), "scout_join_backward")
 
 
 def scout_selftest_bounded_wait(limit_ns: int, d_out: int, stream: int) -> None:

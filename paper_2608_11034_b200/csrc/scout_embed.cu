@@ -1,0 +1,415 @@
+// Token embedding: rows of a table, and the table's gradient by sorted tokens.
+//
+// Forward is a copy of rows, bound by memory.  Backward: every token's gradient goes to its id's row, and the places of an id are
+// added in their order, whatever ran first.  Three launches:
+//   sort_ids     one cluster of eight blocks sorts (id, place) by id, places of an id staying in order (radix sort from the
+//                lowest digit, up to nine bits a pass), and marks the ids that occur;
+//   sum_places   the sorted places in pieces of PIECE: a thread adds up eight columns of a piece, writes what begins and ends
+//                inside, and leaves what crosses a border in scratch; other blocks write zeros to rows of ids that do not occur;
+//   join_pieces  adds the parts of an id that crosses borders, in order.
+// Pieces of equal size keep one frequent id (padding, a line break) from holding up the rest.
+#include <algorithm>
+#include <cmath>
+
+#include <cooperative_groups.h>
+
+#include "scout_step.cuh"
+
+namespace scout {
+namespace step {
+namespace {
+
+namespace cg = cooperative_groups;
+
+constexpr int THREADS = 256, UNROLL = 4;
+
+// id of place t, or `vocab` where it is outside 0..vocab-1
+__device__ __forceinline__ uint32_t id_at(const void *ids, bool wide, int64_t t, uint32_t vocab) {
+    const int64_t id = wide ? reinterpret_cast<const int64_t *>(ids)[t] : (int64_t) reinterpret_cast<const int32_t *>(ids)[t];
+    return id >= 0 && id < (int64_t)vocab ? (uint32_t)id : vocab;
+}
+
+// ---- forward ------------------------------------------------------------------------------------------
+struct Lookup {
+    const void *ids, *table;
+    void *y;
+    int64_t table_stride, y_stride, dim, row0;
+    uint32_t vocab, per_row, groups, mul, shift;  // eights of a row, of all rows; n / per_row
+    float scale;
+    int id64, wide;
+};
+
+template <typename T, typename TO> __global__ void __launch_bounds__(THREADS) lookup(const __grid_constant__ Lookup a) {
+    const uint32_t stride = gridDim.x * THREADS;
+    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 < a.groups; q0 += (uint64_t)stride * UNROLL) {
+        Eight<T> e[UNROLL];
+        uint32_t row[UNROLL], chunk[UNROLL], id[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const uint64_t q = q0 + (uint64_t)u * stride;
+            if (q >= a.groups) continue;
+            row[u] = (__umulhi((uint32_t)q, a.mul) + (uint32_t)q) >> a.shift;
+            chunk[u] = (uint32_t)q - row[u] * a.per_row;
+            id[u] = id_at(a.ids, a.id64, a.row0 + row[u], a.vocab);
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (q0 + (uint64_t)u * stride >= a.groups) continue;
+            e[u].zero();
+            if (id[u] < a.vocab)
+                e[u].template load<false>(reinterpret_cast<const T *>(a.table) + (int64_t)id[u] * a.table_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.dim - 8ll * chunk[u]));
+        }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            if (q0 + (uint64_t)u * stride >= a.groups) continue;
+            float x[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) x[i] = id[u] < a.vocab ? a.scale * e[u].get(i) : 0.f;
+            Eight<TO> o;
+            o.set(x);
+            o.store(reinterpret_cast<TO *>(a.y) + row[u] * a.y_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.dim - 8ll * chunk[u]));
+        }
+    }
+}
+
+template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaStream_t stream) {
+    const uint64_t per_row = ((uint64_t)a.dim + 7) / 8, most = std::max<uint64_t>(1, 0x7FFFFFFFull / per_row);
+    a.per_row = (uint32_t)per_row;
+    while ((1ull << a.shift) < per_row) ++a.shift;
+    a.mul = (uint32_t)((((1ull << a.shift) - per_row) << 32) / per_row + 1);
+    for (uint64_t r = 0; r < rows; r += most) {
+        const uint64_t groups = std::min(most, rows - r) * per_row;
+        a.row0 = (int64_t)r, a.groups = (uint32_t)groups;
+        lookup<T, TO><<<(unsigned)std::min<uint64_t>((groups + THREADS - 1) / THREADS, SMS * 8), THREADS, 0, stream>>>(a);
+        SCOUT_CUDA(cudaGetLastError());
+        a.y = reinterpret_cast<TO *>(a.y) + std::min(most, rows - r) * a.y_stride;
+    }
+    return SCOUT_OK;
+}
+
+// ---- backward -----------------------------------------------------------------------------------------
+constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT;
+constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4;
+constexpr int PIECE = 32, SUM_THREADS = 128, FILL_BYTES = 1 << 16;
+constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
+
+struct Grad {
+    const void *ids, *dy;
+    void *table;
+    uint32_t *key[2], *place[2];  // [rows] each: sorted by the digits so far, passes alternate
+    uint32_t *seen;               // a bit for every id
+    float *part;                  // [pieces][2][dim]: what goes on from the piece before, and what goes on into the next one
+    int64_t dy_stride, table_stride, rows, dim;
+    uint32_t vocab, pieces, across;  // blocks of columns
+    uint32_t fill_rows;              // rows of a block that writes zeros
+    int digit, passes, id64, wide, accumulate;
+    float scale;
+};
+
+__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
+    extern __shared__ uint32_t smem[];
+    uint32_t *const hist = smem, *const total = smem + SORT_WARPS * MAX_BINS, *const scan = total + MAX_BINS;  // [warp][bin], [bin], [bin]
+    __shared__ uint32_t warp_total[SORT_WARPS];
+    cg::cluster_group cluster = cg::this_cluster();
+    const uint32_t rank = cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1u << a.digit;
+    for (uint32_t w = rank * SORT_THREADS + threadIdx.x; w < (a.vocab + 31) / 32; w += CLUSTER * SORT_THREADS) a.seen[w] = 0;
+    // a warp's run of places: whole warps' widths
+    const int64_t run = (a.rows + CLUSTER * SORT_WARPS * 32 - 1) / (CLUSTER * SORT_WARPS * 32) * 32;
+    const int64_t begin = min((int64_t)(rank * SORT_WARPS + warp) * run, a.rows), end = min(begin + run, a.rows);
+    for (int pass = 0; pass < a.passes; ++pass) {
+        const int shift = pass * a.digit, from = (pass + 1) & 1, to = pass & 1;
+        const auto key_of = [&](int64_t t) { return pass == 0 ? id_at(a.ids, a.id64, t, a.vocab) : a.key[from][t]; };
+        for (uint32_t i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_THREADS) hist[i] = 0;
+        __syncthreads();
+        for (int64_t t = begin + lane; t < end; t += 32) atomicAdd(&hist[warp * bins + ((key_of(t) >> shift) & (bins - 1))], 1u);
+        __syncthreads();
+        // counts become places: warps before within the block, then blocks before, then smaller digits
+        if (threadIdx.x < bins) {
+            uint32_t sum = 0;
+            for (int w = 0; w < SORT_WARPS; ++w) {
+                const uint32_t n = hist[w * bins + threadIdx.x];
+                hist[w * bins + threadIdx.x] = sum;
+                sum += n;
+            }
+            total[threadIdx.x] = sum;
+        }
+        cluster.sync();
+        uint32_t all = 0, before = 0;
+        if (threadIdx.x < bins)
+#pragma unroll
+            for (int c = 0; c < CLUSTER; ++c) {
+                const uint32_t n = cluster.map_shared_rank(total, c)[threadIdx.x];
+                if (c < (int)rank) before += n;
+                all += n;
+            }
+        uint32_t sum = all;  // inclusive over a warp's bins
+#pragma unroll
+        for (int d = 1; d < 32; d <<= 1) {
+            const uint32_t n = __shfl_up_sync(0xFFFFFFFFu, sum, d);
+            if ((int)lane >= d) sum += n;
+        }
+        if (lane == 31) warp_total[warp] = sum;
+        __syncthreads();
+        if (threadIdx.x < bins) {
+            for (uint32_t w = 0; w < warp; ++w) sum += warp_total[w];
+            scan[threadIdx.x] = sum - all + before;
+        }
+        __syncthreads();
+        for (int64_t t0 = begin; t0 < end; t0 += 32) {  // the same for a warp
+            const int64_t t = t0 + lane;
+            const bool on = t < end;
+            const uint32_t key = on ? key_of(t) : 0, digit = on ? (key >> shift) & (bins - 1) : bins;
+            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+            if (on) {
+                const uint32_t at = scan[digit] + hist[warp * bins + digit] + __popc(same & ((1u << lane) - 1));
+                a.key[to][at] = key;
+                a.place[to][at] = pass == 0 ? (uint32_t)t : a.place[from][t];
+                if (pass == a.passes - 1 && key < a.vocab) atomicOr(&a.seen[key >> 5], 1u << (key & 31));
+            }
+            __syncwarp();
+            if (on && (same >> lane) == 1u) hist[warp * bins + digit] += __popc(same);  // the last of them
+            __syncwarp();
+        }
+        cluster.sync();  // what the others wrote is read next; nobody's `total` is read any more
+    }
+}
+
+// out = (accumulate ? out : 0) + scale * sum, eight columns
+template <typename TO> __device__ __forceinline__ void put(const Grad &a, uint32_t id, int64_t col, int n, const float (&sum)[8]) {
+    TO *p = reinterpret_cast<TO *>(a.table) + (int64_t)id * a.table_stride + col;
+    Eight<TO> e;
+    float x[8];
+    if (a.accumulate) e.template load<true>(p, a.wide, n);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) x[i] = a.accumulate ? fmaf(a.scale, sum[i], e.get(i)) : a.scale * sum[i];
+    e.set(x);
+    e.store(p, a.wide, n);
+}
+
+template <typename T, typename TO> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
+    pdl_wait();
+    const uint32_t *const keys = a.key[(a.passes + 1) & 1], *const places = a.place[(a.passes + 1) & 1];
+    const uint64_t sums = (uint64_t)a.pieces * a.across;
+    if (blockIdx.x >= sums) {  // zeros
+        const int64_t v0 = (int64_t)(blockIdx.x - sums) * a.fill_rows, v1 = min(v0 + a.fill_rows, (int64_t)a.vocab);
+        Eight<TO> z;
+        z.zero();
+        for (int64_t v = v0; v < v1; ++v) {
+            if ((a.seen[v >> 5] >> (v & 31)) & 1) continue;
+            for (int64_t c = 8 * threadIdx.x; c < a.dim; c += 8 * SUM_THREADS)
+                z.store(reinterpret_cast<TO *>(a.table) + v * a.table_stride + c, a.wide, (int)min(8ll, (long long)a.dim - c));
+        }
+        return;
+    }
+    __shared__ uint32_t key[PIECE + 2], place[PIECE];
+    const uint32_t piece = blockIdx.x / a.across;
+    const int64_t p0 = (int64_t)piece * PIECE;
+    const int count = (int)min((long long)PIECE, (long long)a.rows - p0);
+    // keys of the piece and its neighbours; outside, one that is nobody's
+    if (threadIdx.x < PIECE + 2) {
+        const int64_t p = p0 + (int)threadIdx.x - 1;
+        key[threadIdx.x] = p >= 0 && p < a.rows && p <= p0 + count ? keys[p] : 0xFFFFFFFFu;
+    }
+    if (threadIdx.x < count) place[threadIdx.x] = places[p0 + threadIdx.x];
+    __syncthreads();
+    const int64_t col = ((int64_t)(blockIdx.x % a.across) * SUM_THREADS + threadIdx.x) * 8;
+    const int n = (int)max(0ll, min(8ll, (long long)a.dim - col));
+    if (n == 0) return;
+    float sum[8] = {};
+    bool begun = key[0] != key[1];  // the current id's places begin inside this piece
+    for (int k0 = 0; k0 < count; k0 += UNROLL) {
+        Eight<T> e[UNROLL];
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u)
+            if (k0 + u < count && key[k0 + u + 1] < a.vocab)
+                e[u].template load<true>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride + col, a.wide, n);
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) {
+            const int k = k0 + u;
+            if (k >= count || key[k + 1] >= a.vocab) break;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sum[i] += e[u].get(i);
+            const bool ends = key[k + 2] != key[k + 1];
+            if (ends && begun) {
+                put<TO>(a, key[k + 1], col, n, sum);
+            } else if (ends || k + 1 == count) {
+                float *part = a.part + ((int64_t)piece * 2 + begun) * a.dim + col;
+#pragma unroll
+                for (int i = 0; i < 8; ++i)
+                    if (i < n) part[i] = sum[i];
+            }
+            if (ends) {
+                begun = true;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) sum[i] = 0.f;
+            }
+        }
+    }
+}
+
+// Ids that begin in one piece and go on into the next.  A block looks at JOIN_THREADS pieces at once (every gridDim.y-th) and then
+// takes those that such an id begins in, one after the other: eight warps take every eighth part each, a lane four columns.
+template <typename TO> __global__ void __launch_bounds__(JOIN_THREADS) join_pieces(const __grid_constant__ Grad a) {
+    pdl_wait();
+    __shared__ float part[JOIN_WAYS][JOIN_COLS];
+    __shared__ uint32_t found[JOIN_THREADS], counts[JOIN_WAYS];
+    const uint32_t *const keys = a.key[(a.passes + 1) & 1];
+    const int lane = threadIdx.x & 31, way = threadIdx.x >> 5;
+    const int64_t col = (int64_t)blockIdx.x * JOIN_COLS + lane;
+    for (int64_t first = blockIdx.y; first + 1 < a.pieces; first += (int64_t)gridDim.y * JOIN_THREADS) {
+        const int64_t mine = first + (int64_t)gridDim.y * threadIdx.x, after = mine * PIECE + PIECE;
+        bool begins = false;
+        if (mine + 1 < a.pieces) {
+            const uint32_t key = keys[after - 1];
+            begins = key < a.vocab && keys[after] == key && (mine == 0 || keys[mine * PIECE - 1] != key);
+        }
+        const uint32_t who = __ballot_sync(0xFFFFFFFFu, begins);
+        __syncthreads();
+        if (lane == 0) counts[way] = __popc(who);
+        __syncthreads();
+        int at = 0, all = 0;
+#pragma unroll
+        for (int w = 0; w < JOIN_WAYS; ++w) at += w < way ? counts[w] : 0, all += counts[w];
+        if (begins) found[at + __popc(who & ((1u << lane) - 1))] = (uint32_t)mine;
+        __syncthreads();
+        for (int k = 0; k < all; ++k) {
+            const int64_t piece = found[k];
+            const uint32_t key = keys[piece * PIECE + PIECE - 1];
+            int64_t end = piece + 1;  // the piece that it ends in: the last whose first key is still this one
+            for (;; end += 32) {      // the same for every warp
+                const int64_t next = end + 1 + lane;
+                const uint32_t go = __ballot_sync(0xFFFFFFFFu, next < a.pieces && keys[next * PIECE] == key);
+                if (go != 0xFFFFFFFFu) {
+                    end += __ffs(~go) - 1;
+                    break;
+                }
+            }
+            float sum[4] = {};
+#pragma unroll 2
+            for (int64_t p = piece + way; p <= end; p += JOIN_WAYS)
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (col + 32 * i < a.dim) sum[i] += a.part[(p * 2 + (p == piece)) * a.dim + col + 32 * i];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 4; ++i) part[way][lane + 32 * i] = sum[i];
+            __syncthreads();
+            const int64_t c = (int64_t)blockIdx.x * JOIN_COLS + threadIdx.x;
+            if (threadIdx.x < JOIN_COLS && c < a.dim) {
+                float s = part[0][threadIdx.x];
+#pragma unroll
+                for (int w = 1; w < JOIN_WAYS; ++w) s += part[w][threadIdx.x];
+                TO *p = reinterpret_cast<TO *>(a.table) + (int64_t)key * a.table_stride + c;
+                *p = down<TO>(a.accumulate ? fmaf(a.scale, s, up<TO>(*p)) : a.scale * s);
+            }
+        }
+    }
+}
+
+template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream) {
+    if (int rc = allow_smem<sort_ids>(SORT_SMEM)) return rc;
+    sort_ids<<<CLUSTER, SORT_THREADS, SORT_SMEM, stream>>>(a);
+    SCOUT_CUDA(cudaGetLastError());
+    a.fill_rows = (uint32_t)std::max<uint64_t>(1, FILL_BYTES / (a.dim * sizeof(TO)));
+    const uint64_t fill = a.accumulate ? 0 : (a.vocab + a.fill_rows - 1) / a.fill_rows, grid = (uint64_t)a.pieces * a.across + fill;
+    if (grid > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
+    if (grid) SCOUT_CUDA(launch_dependent(sum_places<T, TO>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
+    if (a.pieces > 1) {
+        const uint32_t wide = (uint32_t)((a.dim + JOIN_COLS - 1) / JOIN_COLS);
+        const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 4 * SMS / wide)));
+        SCOUT_CUDA(launch_dependent(join_pieces<TO>, jg, dim3(JOIN_THREADS), stream, a));
+    }
+    return SCOUT_OK;
+}
+
+int check(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim, uint64_t vocab, float scale) {
+    if (dtype > SCOUT_DT_I32 || out_dtype > SCOUT_DT_I32 || id_dtype > SCOUT_DT_I32 || !std::isfinite(scale)) return SCOUT_ERR_INVALID;
+    if (!known_float(dtype) || (out_dtype != dtype && out_dtype != SCOUT_DT_F32) || (id_dtype != SCOUT_DT_I32 && id_dtype != SCOUT_DT_I64))
+        return SCOUT_ERR_UNSUPPORTED;
+    return rows > 1ull << 30 || dim > 1ull << 24 || vocab > 0x7FFFFFFFull ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;
+}
+
+struct Scratch {
+    uint64_t key[2], place[2], seen, part, bytes;
+};
+Scratch scratch(uint64_t rows, uint64_t dim, uint64_t vocab) {
+    const auto up = [](uint64_t n) { return (n + 255) & ~255ull; };
+    Scratch s = {};
+    const uint64_t each = up(rows * 4);
+    s.key[0] = 0, s.key[1] = each, s.place[0] = 2 * each, s.place[1] = 3 * each, s.seen = 4 * each;
+    s.part = s.seen + up((vocab + 31) / 32 * 4);
+    s.bytes = s.part + up((rows + PIECE - 1) / PIECE * 2 * dim * 4);
+    return s;
+}
+
+}  // namespace
+}  // namespace step
+}  // namespace scout
+
+extern "C" int scout_embed_forward(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
+                                   const void *ids, const void *table, uint64_t table_stride, float scale, void *y, uint64_t y_stride, void *stream) {
+    using namespace scout::step;
+    if (int rc = check(id_dtype, dtype, out_dtype, rows, dim, vocab, scale)) return rc;
+    if (rows == 0 || dim == 0) return SCOUT_OK;
+    if (!ids || (vocab && !table)) return SCOUT_ERR_INVALID;
+    if (!aligned(ids, id_dtype == SCOUT_DT_I64 ? 8 : 4)) return SCOUT_ERR_ALIGN;
+    if (vocab)
+        if (int rc = check_matrix(table, table_stride, dim, dtype)) return rc;
+    if (int rc = check_matrix(y, y_stride, dim, out_dtype)) return rc;
+    Lookup a = {};
+    a.ids = ids, a.table = table, a.y = y, a.table_stride = (int64_t)table_stride, a.y_stride = (int64_t)y_stride, a.dim = (int64_t)dim;
+    a.vocab = (uint32_t)vocab, a.scale = scale, a.id64 = id_dtype == SCOUT_DT_I64;
+    a.wide = wide_rows(table, table_stride, dtype) && wide_rows(y, y_stride, out_dtype);
+    const cudaStream_t s = (cudaStream_t)stream;
+    const bool f32 = out_dtype == SCOUT_DT_F32;
+    switch (dtype) {
+        case SCOUT_DT_F32: return run_lookup<float, float>(a, rows, s);
+        case SCOUT_DT_BF16: return f32 ? run_lookup<__nv_bfloat16, float>(a, rows, s) : run_lookup<__nv_bfloat16, __nv_bfloat16>(a, rows, s);
+        default: return f32 ? run_lookup<__half, float>(a, rows, s) : run_lookup<__half, __half>(a, rows, s);
+    }
+}
+
+extern "C" int scout_embed_backward_workspace(uint64_t rows, uint64_t dim, uint64_t vocab, uint64_t *bytes) {
+    using namespace scout::step;
+    if (!bytes) return SCOUT_ERR_INVALID;
+    if (int rc = check(SCOUT_DT_I64, SCOUT_DT_F32, SCOUT_DT_F32, rows, dim, vocab, 1.f)) return rc;
+    *bytes = scratch(rows, dim, vocab).bytes;
+    return SCOUT_OK;
+}
+
+extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
+                                    const void *ids, const void *dy, uint64_t dy_stride, float scale, void *d_table, uint64_t d_table_stride,
+                                    uint32_t accumulate, void *workspace, uint64_t workspace_bytes, void *stream) {
+    using namespace scout::step;
+    if (int rc = check(id_dtype, dtype, out_dtype, rows, dim, vocab, scale)) return rc;
+    if (accumulate > 1) return SCOUT_ERR_INVALID;
+    if (dim == 0 || vocab == 0 || (rows == 0 && accumulate)) return SCOUT_OK;
+    if (int rc = check_matrix(d_table, d_table_stride, dim, out_dtype)) return rc;
+    if (rows) {
+        if (!ids) return SCOUT_ERR_INVALID;
+        if (!aligned(ids, id_dtype == SCOUT_DT_I64 ? 8 : 4)) return SCOUT_ERR_ALIGN;
+        if (int rc = check_matrix(dy, dy_stride, dim, dtype)) return rc;
+    }
+    const Scratch need = scratch(rows, dim, vocab);
+    if (workspace_bytes < need.bytes || !workspace) return SCOUT_ERR_INVALID;
+    if (!aligned(workspace, 256)) return SCOUT_ERR_ALIGN;
+    Grad a = {};
+    uint8_t *const ws = (uint8_t *)workspace;
+    a.ids = ids, a.dy = dy, a.table = d_table;
+    for (int i = 0; i < 2; ++i) a.key[i] = (uint32_t *)(ws + need.key[i]), a.place[i] = (uint32_t *)(ws + need.place[i]);
+    a.seen = (uint32_t *)(ws + need.seen), a.part = (float *)(ws + need.part);
+    a.dy_stride = (int64_t)dy_stride, a.table_stride = (int64_t)d_table_stride, a.rows = (int64_t)rows, a.dim = (int64_t)dim;
+    a.vocab = (uint32_t)vocab, a.pieces = (uint32_t)((rows + PIECE - 1) / PIECE), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
+    int bits = 1;
+    while (vocab >> bits) ++bits;  // digits of `vocab` itself, which stands for ids outside
+    a.passes = (bits + MAX_DIGIT - 1) / MAX_DIGIT, a.digit = (bits + a.passes - 1) / a.passes;
+    a.id64 = id_dtype == SCOUT_DT_I64, a.accumulate = (int)accumulate, a.scale = scale;
+    a.wide = (!rows || wide_rows(dy, dy_stride, dtype)) && wide_rows(d_table, d_table_stride, out_dtype);
+    const cudaStream_t s = (cudaStream_t)stream;
+    const bool f32 = out_dtype == SCOUT_DT_F32;
+    switch (dtype) {
+        case SCOUT_DT_F32: return run_gradient<float, float>(a, s);
+        case SCOUT_DT_BF16: return f32 ? run_gradient<__nv_bfloat16, float>(a, s) : run_gradient<__nv_bfloat16, __nv_bfloat16>(a, s);
+        default: return f32 ? run_gradient<__half, float>(a, s) : run_gradient<__half, __half>(a, s);
+    }
+}

@@ -1,0 +1,154 @@
+// What the kernels of the step operators share: element types, eight elements of a row at a time, sums over a warp, and the
+// counter-based generator behind dropout.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include "scout_internal.h"
+#include "scout_step.h"
+
+namespace scout {
+namespace step {
+
+constexpr int SMS = 148;
+
+template <typename T> __device__ __forceinline__ float up(T x);
+template <> __device__ __forceinline__ float up<float>(float x) { return x; }
+template <> __device__ __forceinline__ float up<__nv_bfloat16>(__nv_bfloat16 x) { return __bfloat162float(x); }
+template <> __device__ __forceinline__ float up<__half>(__half x) { return __half2float(x); }
+template <typename T> __device__ __forceinline__ T down(float x);
+template <> __device__ __forceinline__ float down<float>(float x) { return x; }
+template <> __device__ __forceinline__ __nv_bfloat16 down<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
+template <> __device__ __forceinline__ __half down<__half>(float x) { return __float2half_rn(x); }
+
+// Eight elements of a row, as they lie in memory.  n: how many of them the row has (8 with wide: one or two 16-byte accesses).
+template <typename T> struct Eight {
+    static constexpr int N = sizeof(T) / 2;
+    uint4 w[N];
+    __device__ __forceinline__ float get(int i) const {
+        const uint32_t *v = reinterpret_cast<const uint32_t *>(w);
+        if constexpr (sizeof(T) == 4) {
+            return __uint_as_float(v[i]);
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+            return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
+        } else {
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i >> 1]));
+            return i & 1 ? f.y : f.x;
+        }
+    }
+    __device__ __forceinline__ void zero() {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = make_uint4(0, 0, 0, 0);
+    }
+    __device__ __forceinline__ void set(const float (&x)[8]) {
+        uint32_t *v = reinterpret_cast<uint32_t *>(w);
+        if constexpr (sizeof(T) == 4) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(x[i]);
+        } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                v[i] = *reinterpret_cast<const uint32_t *>(&p);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __half2 p = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                v[i] = *reinterpret_cast<const uint32_t *>(&p);
+            }
+        }
+    }
+    // STREAM: read once, or written and not read soon
+    template <bool STREAM> __device__ __forceinline__ void load(const T *p, bool wide, int n) {
+        if (wide && n == 8) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) w[i] = STREAM ? __ldcs(reinterpret_cast<const uint4 *>(p) + i) : __ldg(reinterpret_cast<const uint4 *>(p) + i);
+        } else {
+            zero();
+            T *v = reinterpret_cast<T *>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) v[i] = p[i];
+        }
+    }
+    __device__ __forceinline__ void store(T *p, bool wide, int n) const {
+        if (wide && n == 8) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) reinterpret_cast<uint4 *>(p)[i] = w[i];
+        } else {
+            const T *v = reinterpret_cast<const T *>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (i < n) p[i] = v[i];
+        }
+    }
+};
+
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll
+    for (int m = 16; m; m >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, m);
+    return v;
+}
+
+// ---- Philox 4x32 with ten rounds (Salmon, Moraes, Dror, Shaw: "Parallel random numbers: as easy as 1, 2, 3", 2011) -----------
+// Two 32 x 32 -> 64 bit products and four exclusive ors a round; the round keys follow from the seed alone and are made once, on
+// the host.  Eight places share a counter, 16 bits each: with 32 bits a place the generator would take as long as memory does.
+struct Drop {
+    uint32_t k0[10], k1[10];
+    uint32_t cut;  // places below are dropped; 0: no dropout
+    float factor;
+    uint64_t offset;
+    const uint64_t *d_offset;
+    __device__ __forceinline__ uint64_t at() const { return offset + (d_offset ? *d_offset : 0); }
+};
+inline int make_drop(double p, uint64_t seed, uint64_t offset, const uint64_t *d_offset, Drop *d) {
+    if (!(p >= 0.0 && p < 1.0)) return SCOUT_ERR_INVALID;
+    if (reinterpret_cast<uintptr_t>(d_offset) & 7) return SCOUT_ERR_ALIGN;
+    uint32_t a = (uint32_t)seed, b = (uint32_t)(seed >> 32);
+    for (int i = 0; i < 10; ++i, a += 0x9E3779B9u, b += 0xBB67AE85u) d->k0[i] = a, d->k1[i] = b;
+    const uint32_t cut = (uint32_t)(p * 65536.0 + 0.5);
+    d->cut = cut > 65535 ? 65535 : cut;
+    d->factor = (float)(65536.0 / (65536 - d->cut));
+    d->offset = offset, d->d_offset = d_offset;
+    return SCOUT_OK;
+}
+// the eight numbers of places 8 * chunk .. 8 * chunk + 7 of a row, two to a word
+__device__ __forceinline__ uint4 philox(const Drop &d, uint32_t chunk, uint32_t row, uint64_t offset) {
+    uint32_t c0 = chunk, c1 = row, c2 = (uint32_t)offset, c3 = (uint32_t)(offset >> 32);
+#pragma unroll
+    for (int i = 0; i < 10; ++i) {
+        const uint64_t a = (uint64_t)c0 * 0xD2511F53u, b = (uint64_t)c2 * 0xCD9E8D57u;
+        c0 = (uint32_t)(b >> 32) ^ c1 ^ d.k0[i], c1 = (uint32_t)b;
+        c2 = (uint32_t)(a >> 32) ^ c3 ^ d.k1[i], c3 = (uint32_t)a;
+    }
+    return make_uint4(c0, c1, c2, c3);
+}
+// x times the factor where kept, else 0
+__device__ __forceinline__ void drop8(const Drop &d, const uint4 &bits, float (&x)[8]) {
+    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        x[2 * i] = (w[i] & 0xFFFFu) >= d.cut ? x[2 * i] * d.factor : 0.f;
+        x[2 * i + 1] = (w[i] >> 16) >= d.cut ? x[2 * i + 1] * d.factor : 0.f;
+    }
+}
+
+// ---- host ------------------------------------------------------------------------------------------------
+inline bool known_float(uint32_t dtype) { return dtype == SCOUT_DT_F32 || dtype == SCOUT_DT_BF16 || dtype == SCOUT_DT_F16; }
+inline uint64_t size_of(uint32_t dtype) { return dtype == SCOUT_DT_F32 ? 4 : 2; }
+// rows of a matrix lie on 16-byte boundaries
+inline bool wide_rows(const void *p, uint64_t stride, uint32_t dtype) {
+    return ((reinterpret_cast<uintptr_t>(p) | stride * size_of(dtype)) & 15) == 0;
+}
+inline bool aligned(const void *p, uint64_t bytes) { return (reinterpret_cast<uintptr_t>(p) & (bytes - 1)) == 0; }
+constexpr uint64_t MAX_STRIDE = 1ull << 40;
+// a matrix argument: present, with a stride that holds its columns
+inline int check_matrix(const void *p, uint64_t stride, uint64_t cols, uint32_t dtype) {
+    if (!p || stride < cols || stride > MAX_STRIDE) return SCOUT_ERR_INVALID;
+    return aligned(p, size_of(dtype)) ? SCOUT_OK : SCOUT_ERR_ALIGN;
+}
+
+}  // namespace step
+}  // namespace scout
