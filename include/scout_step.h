@@ -12,6 +12,8 @@
  *   scout_dropout                                and its gradient, which is the same call
  *   scout_join_forward / scout_join_backward     a block's output joins the residual stream:
  *        norm, dropout, gate and scale, sum, the next block's norm
+ *   scout_loss_forward / scout_loss_backward     softmax cross entropy over a vocabulary,
+ *        from hidden states and output projection; the scores are never kept
  *
  * Conventions are those of scout_replay.h: plain C, error codes, caller-owned memory, work
  * enqueued on `stream`, scratch of the size the *_workspace calls return (256-byte aligned,
@@ -118,6 +120,40 @@ SCOUT_API int scout_join_backward(const scout_join_t *j, const void *dy, const v
                                   uint64_t seed, uint64_t offset, const uint64_t *d_offset, void *dx, void *db,
                                   void *d_gate, void *d_post, void *d_norm, void *workspace, uint64_t workspace_bytes,
                                   void *stream);
+
+/* ---- cross entropy over a vocabulary -----------------------------------------------------
+ * With s_tv = x_t . w_v, for the rows t whose target is in 0..vocab-1:
+ *     lse_t = ln sum_v exp s_tv,   loss_t = lse_t - s_{t,target}
+ * Other rows do not count: loss and lse are 0 and their gradient is 0, whatever stands in x.
+ *   dtype        of x and w: SCOUT_DT_BF16 or SCOUT_DT_F16
+ *   x            device [rows][dim], row stride x_stride
+ *   w            device [vocab][dim], row stride w_stride; 16-byte aligned, w_stride a multiple of 8
+ *                (else SCOUT_ERR_ALIGN)
+ *   targets      device [rows], SCOUT_DT_I32 or SCOUT_DT_I64
+ *   loss, lse    device [rows] fp32
+ * dim a multiple of 8 up to 65536, rows and vocab up to 2^24 and rows * vocab up to 2^45, else
+ * SCOUT_ERR_UNSUPPORTED.  The scratch of the backward pass holds a copy of x, dx in fp32, and G for a
+ * piece of the vocabulary: half a GiB, more only where 8192 columns take more. */
+SCOUT_API int scout_loss_workspace(uint32_t dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
+                                   uint64_t *forward_bytes, uint64_t *backward_bytes);
+SCOUT_API int scout_loss_forward(uint32_t dtype, uint32_t id_dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
+                                 const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,
+                                 const void *targets, float *loss, float *lse, void *workspace,
+                                 uint64_t workspace_bytes, void *stream);
+
+/* With g_t = d_loss[t * d_loss_stride] (stride 0: one number for all rows):
+ *     G_tv = g_t (exp(s_tv - lse_t) - [v = target_t]),   dx_t = sum_v G_tv w_v
+ *     dw_v = (accumulate ? dw_v : 0) + sum_t G_tv x_t
+ * over the rows that count.  The scores are made again, in pieces of the vocabulary; G is
+ * rounded to 16 bits for its products, which have fp32 sums (a row's entry at its target
+ * enters dx with what that rounding took away).  dx has x's type, dw out_dtype (dtype or
+ * SCOUT_DT_F32).  Every row of dx and dw is written.
+ *   dw           device [vocab][dim], row stride dw_stride */
+SCOUT_API int scout_loss_backward(uint32_t dtype, uint32_t id_dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim,
+                                  uint64_t vocab, const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,
+                                  const void *targets, const float *lse, const float *d_loss, uint64_t d_loss_stride,
+                                  void *dx, uint64_t dx_stride, void *dw, uint64_t dw_stride, uint32_t accumulate,
+                                  void *workspace, uint64_t workspace_bytes, void *stream);
 
 #ifdef __cplusplus
 }

@@ -118,6 +118,10 @@ def lib():
             "scout_join_forward": (C.c_int, [vp] * 6 + [C.c_double, u64, u64] + [vp] * 5),
             "scout_join_backward_workspace": (C.c_int, [vp, C.POINTER(u64)]),
             "scout_join_backward": (C.c_int, [vp] * 9 + [C.c_double, u64, u64] + [vp] * 7 + [u64, vp]),
+            "scout_loss_workspace": (C.c_int, [u32, u64, u64, u64, C.POINTER(u64), C.POINTER(u64)]),
+            "scout_loss_forward": (C.c_int, [u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, vp, vp, u64, vp]),
+            "scout_loss_backward": (C.c_int, [u32, u32, u32, u64, u64, u64, vp, u64, vp, u64, vp, vp, vp, u64, vp, u64, vp, u64, u32, vp,
+                                              u64, vp]),
             "scout_strerror": (C.c_char_p, [C.c_int]),
             "scout_version": (C.c_int, []),
             "scout_last_cuda_error": (C.c_char_p, []),
@@ -508,6 +512,27 @@ def scout_join_backward(join: int, dy: int, dn: int, b: int, y: int, stats: int,
                         workspace_bytes: int, stream: int) -> None:
     _check(lib().scout_join_backward(join, dy, dn, b, y, stats, gate, post, norm, p, seed, offset, d_offset, dx, db, d_gate, d_post,
                                      d_norm, workspace, workspace_bytes, stream), "scout_join_backward")
+
+
+def scout_loss_workspace(dtype: int, rows: int, dim: int, vocab: int):
+    """-> (forward_bytes, backward_bytes)"""
+    f, b = C.c_uint64(), C.c_uint64()
+    _check(lib().scout_loss_workspace(dtype, rows, dim, vocab, C.byref(f), C.byref(b)), "scout_loss_workspace")
+    return f.value, b.value
+
+
+def scout_loss_forward(dtype: int, id_dtype: int, rows: int, dim: int, vocab: int, x: int, x_stride: int, w: int, w_stride: int,
+                       targets: int, loss: int, lse: int, workspace: int, workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_loss_forward(dtype, id_dtype, rows, dim, vocab, x, x_stride, w, w_stride, targets, loss, lse, workspace,
+                                    workspace_bytes, stream), "scout_loss_forward")
+
+
+def scout_loss_backward(dtype: int, id_dtype: int, out_dtype: int, rows: int, dim: int, vocab: int, x: int, x_stride: int, w: int,
+                        w_stride: int, targets: int, lse: int, d_loss: int, d_loss_stride: int, dx: int, dx_stride: int, dw: int,
+                        dw_stride: int, accumulate: int, workspace: int, workspace_bytes: int, stream: int) -> None:
+    _check(lib().scout_loss_backward(dtype, id_dtype, out_dtype, rows, dim, vocab, x, x_stride, w, w_stride, targets, lse, d_loss,
+                                     d_loss_stride, dx, dx_stride, dw, dw_stride, accumulate, workspace, workspace_bytes, stream),
+           "scout_loss_backward")
 
 
 def scout_selftest_bounded_wait(limit_ns: int, d_out: int, stream: int) -> None:

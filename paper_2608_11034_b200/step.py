@@ -269,3 +269,76 @@ def join_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], block:
              _at(post_weight), _at(norm_weight), p, seed, host, dev, dx.data_ptr(), db.data_ptr(), _at(dgate), _at(dpost),
              dnorm.data_ptr() if dnorm is not None and dn is not None else 0, ws.data_ptr(), j.bytes)
     return dx, db, dgate, dpost, dnorm
+
+
+# ---- cross entropy over a vocabulary ------------------------------------------------------------------------
+
+@functools.lru_cache(maxsize=1024)
+def _scores(x_shape, x_stride, w_shape, w_stride, dtype, w_dtype, device, w_device, targets_shape):
+    """Checks a description of x, w and targets -> their type's code, rows, dim, vocab, row strides, scratch of both passes."""
+    if dtype not in (torch.bfloat16, torch.float16) or w_dtype != dtype or w_device != device:
+        _fail("x and w: bfloat16 or float16, of one dtype and on one device")
+    x_row, w_row = _row_stride(x_shape, x_stride, device, "x"), _row_stride(w_shape, w_stride, device, "w")
+    if x_shape[1] != w_shape[1]:
+        _fail("x is [rows, dim], w is [vocab, dim]")
+    if targets_shape != x_shape[:1]:
+        _fail("targets: one for each row of x")
+    code, (rows, dim), vocab = _CODE[dtype], x_shape, w_shape[0]
+    if dim == 0:
+        _fail("x: a row has at least one element")
+    return (code, rows, dim, vocab, x_row, w_row) + binding.scout_loss_workspace(code, rows, dim, vocab)
+
+
+def _describe_scores(x, w, targets):
+    if x.dim() != 2 or w.dim() != 2:
+        _fail("x is [rows, dim], w is [vocab, dim]")
+    return _scores(x.shape, x.stride(), w.shape, w.stride(), x.dtype, w.dtype, x.device, w.device, targets.shape)
+
+
+def loss_forward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor):
+    """Softmax cross entropy of the scores x w^T, which are not kept.  x: [rows, dim] hidden states, w: [vocab, dim] output
+    projection (bfloat16 or float16, dim a multiple of 8, rows of w on 16-byte boundaries); targets: int32 or int64 [rows].
+    Rows whose target is outside 0..vocab-1 (padding) do not count, and nothing is read from them.
+    -> (loss, lse), float32 [rows]: lse is the logarithm of the sum of exponentials, for the backward pass; both are 0 for rows
+    that do not count."""
+    _no_autograd(x, w)
+    code, rows, dim, vocab, x_row, w_row, nbytes, _ = _describe_scores(x, w, targets)
+    targets = _flat_ids(targets, x.device, "targets")
+    loss, lse = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    _enqueue("scout_loss_forward", x.device.index, code, _IDS[targets.dtype], rows, dim, vocab, x.data_ptr(), x_row, w.data_ptr(), w_row,
+             targets.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes)
+    return loss, lse
+
+
+def loss_backward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: torch.Tensor, dloss: torch.Tensor, *,
+                  out_dtype: Optional[torch.dtype] = None, grad: Optional[torch.Tensor] = None):
+    """Gradients of loss_forward's loss with respect to x and w, from its lse and the gradient dloss (float32 [rows], of any stride:
+    a mean over the batch has one number, expanded).
+    -> (dx like x, dw [vocab, dim] in out_dtype: float32, which is the default, or w's); with `grad` (of those dtypes, of a tied
+    embedding, say) dw is added to it in place, and out_dtype may only repeat its dtype.
+    The gradient of the scores is rounded to x's type for its products, so a float32 dw is as exact as its terms are (2^-9 of
+    each in bfloat16, 2^-12 in float16), not as float32 is."""
+    _no_autograd(x, w, lse, dloss) if grad is None else _no_autograd(x, w, lse, dloss, grad)
+    code, rows, dim, vocab, x_row, w_row, _, nbytes = _describe_scores(x, w, targets)
+    targets = _flat_ids(targets, x.device, "targets")
+    for t, name in ((lse, "lse"), (dloss, "dloss")):
+        if t.dtype != torch.float32 or t.shape != (rows,) or t.device != x.device:
+            _fail(f"{name}: float32 [rows], on x's device")
+    if not lse.is_contiguous():
+        lse = lse.contiguous()
+    if grad is None:
+        dw = w.new_empty((vocab, dim), dtype=out_dtype or torch.float32)
+    else:
+        if out_dtype not in (None, grad.dtype):
+            _fail("grad is added to in its own dtype; out_dtype names another")
+        dw = grad
+    if dw.dtype not in (torch.float32, w.dtype) or dw.shape != (vocab, dim) or dw.device != x.device:
+        _fail("the gradient is [vocab, dim], float32 or of w's dtype, on x's device")
+    dw_row = _row_stride(dw.shape, dw.stride(), dw.device, "grad")
+    dx = x.new_empty((rows, dim))
+    ws = x.new_empty(nbytes, dtype=torch.uint8)
+    _enqueue("scout_loss_backward", x.device.index, code, _IDS[targets.dtype], _CODE[dw.dtype], rows, dim, vocab, x.data_ptr(), x_row,
+             w.data_ptr(), w_row, targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(), dloss.stride(0), dx.data_ptr(), dim, dw.data_ptr(),
+             dw_row, int(grad is not None), ws.data_ptr(), nbytes)
+    return dx, dw

@@ -133,3 +133,37 @@ def within(got, want, bound):
     assert torch.equal(torch.isnan(got), nan)
     d = torch.where(nan | (got == want), 0.0, (got - want).abs() / bound.clamp(min=1e-300))
     return float(d.max()) if d.numel() else 0.0
+
+
+def loss(x, w, targets, dloss=None):
+    """-> dict of loss, lse (and dx, dw) and bounds b_*.
+
+    Scores are sums of `dim` exact products: chains of at most 1024 added by the tensor cores, which truncate (2^-23 of the running
+    sum for each 16 products that enter it, taken as 2^-23 * 64 of the sum of magnitudes), then fp32 additions; SCORE covers both.
+    lse moves by no more than the largest error of a score, and its own sum, exponentials (2 ulp) and logarithm by 2^-20; G by its
+    rounding and by exp of what scores and lse are off, and its products as the scores are."""
+    u, tiny = U[x.dtype], TINY[x.dtype]
+    live = (targets >= 0) & (targets < w.shape[0])
+    at = torch.where(live, targets, 0).long()
+    xd, wd = torch.where(live[:, None], x.double(), 0.0), w.double()
+    s = xd @ wd.t()
+    off = 2.0 ** -17 * (xd.abs() @ wd.abs().t()).amax(1)
+    lse = torch.logsumexp(s, 1)
+    st = s.gather(1, at[:, None])[:, 0]
+    r = dict(lse=torch.where(live, lse, 0.0), loss=torch.where(live, lse - st, 0.0))
+    r["b_lse"] = off + 2.0 ** -20 + 2.0 ** -23 * lse.abs()
+    r["b_loss"] = r["b_lse"] + off + 2.0 ** -23 * st.abs()
+    if dloss is None:
+        return r
+    g = torch.where(live, dloss.double(), 0.0)
+    p = torch.exp(s - lse[:, None])
+    e = g.abs()[:, None] * p * (off[:, None] * 2 + 2.0 ** -19)
+    p[torch.arange(len(p), device=p.device), at] -= 1
+    gs = g[:, None] * p
+    # the least that float16 holds is 2^-24 of what is held 2^13 times over, with the largest g as one
+    least = g.abs().max() * (2.0 ** -38 if x.dtype == torch.float16 else 0.0)
+    e = e + (u + 2.0 ** -17) * gs.abs() + least
+    r["dx"], r["dw"] = gs @ wd, gs.t() @ xd
+    r["b_dx"] = torch.where(live[:, None], e @ wd.abs() + u * r["dx"].abs() + tiny, 0.0)
+    r["b_dw"] = e.t() @ xd.abs()            # and the rounding of what is stored
+    return r

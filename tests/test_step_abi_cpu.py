@@ -90,3 +90,28 @@ def test_join_pointers_are_checked(lib):
     assert bwd(dy=258) == bwd(dx=258) == bwd(dg=257) == bwd(ws=128) == ALIGN
     empty = join(rows=0)
     assert lib.scout_join_forward(empty.ctypes.data, 0, 0, 0, 0, 0, 0.0, 0, 0, 0, 0, 0, 0, 0) == binding.OK
+
+
+def test_loss_arguments_are_checked(lib):
+    f, b = binding.scout_loss_workspace(B, 100, 64, 1000)
+    assert f % 256 == 0 and b % 256 == 0 and b >= 128 * 1000 * 2 + 128 * 64 * 6
+    for bad, code in (((F, 4, 8, 4), NOT), ((99, 4, 8, 4), BAD), ((B, 4, 12, 4), NOT), ((B, 4, 0, 4), BAD), ((B, 2 ** 25, 8, 4), NOT),
+                      ((B, 4, 8, 2 ** 25), NOT), ((B, 4, 65544, 4), NOT), ((B, 2 ** 23, 8, 2 ** 24), NOT)):
+        with pytest.raises(binding.ScoutError) as e:
+            binding.scout_loss_workspace(*bad)
+        assert e.value.code == code, bad
+
+    def fwd(t=B, idt=I64, rows=100, dim=64, vocab=1000, x=256, xs=64, w=256, wst=64, tg=256, loss=256, lse=256, ws=256, nb=f):
+        return lib.scout_loss_forward(t, idt, rows, dim, vocab, x, xs, w, wst, tg, loss, lse, ws, nb, 0)
+
+    assert fwd(idt=F) == NOT
+    assert fwd(x=0) == fwd(w=0) == fwd(tg=0) == fwd(loss=0) == fwd(lse=0) == fwd(ws=0) == fwd(nb=f - 1) == fwd(xs=63) == fwd(wst=56) == BAD
+    assert fwd(x=257) == fwd(w=264) == fwd(wst=68) == fwd(tg=260) == fwd(loss=258) == fwd(ws=128) == ALIGN
+    assert fwd(rows=0, x=0, w=0, tg=0, loss=0, lse=0) == binding.OK
+
+    def bwd(out=B, x=256, w=256, tg=256, lse=256, dl=256, dls=0, dx=256, dxs=64, dw=256, dws=64, acc=0, ws=256, nb=b):
+        return lib.scout_loss_backward(B, I64, out, 100, 64, 1000, x, 64, w, 64, tg, lse, dl, dls, dx, dxs, dw, dws, acc, ws, nb, 0)
+
+    assert bwd(out=H) == bwd(acc=2) == bwd(x=0) == bwd(w=0) == bwd(tg=0) == bwd(lse=0) == bwd(dl=0) == bwd(dx=0) == bwd(dw=0) == BAD
+    assert bwd(dxs=63) == bwd(dws=63) == bwd(ws=0) == bwd(nb=b - 1) == BAD
+    assert bwd(dx=257) == bwd(dw=257) == bwd(lse=258) == bwd(dl=258) == bwd(ws=128) == ALIGN and bwd(out=F, dw=258) == ALIGN
