@@ -1,7 +1,7 @@
 // Dropout with a mask that is made again from a counter wherever it is needed.
 //
 // Bound by memory (an element in, an element out); the generator costs 40 instructions for eight elements.  A thread takes eight
-// columns of a row at a time, UNROLL of them in flight.
+// columns of a row at a time, 64 bytes of them in flight.
 #include <algorithm>
 
 #include "scout_step.cuh"
@@ -10,56 +10,59 @@ namespace scout {
 namespace step {
 namespace {
 
-constexpr int THREADS = 256, UNROLL = 4;
+constexpr int THREADS = 256, BLOCKS = 4;  // blocks of an SM
 
 struct Args {
     const void *x;
     void *y;
     int64_t x_stride, y_stride, cols;
-    uint32_t row0, per_row, groups;  // first row of this launch; eights of a row; eights of all its rows (below 2^31)
-    uint32_t mul, shift;             // n / per_row for n < 2^31: a high product and a shift
+    uint32_t row0, per_row, units;  // first row of this launch; eights of a row (whole warps of them unless wide); of all its rows (below 2^31)
+    uint32_t mul, shift;            // n / per_row for n < 2^31: a high product and a shift
     int wide;
     Drop drop;
 };
 
-template <typename T> __global__ void __launch_bounds__(THREADS) dropout(const __grid_constant__ Args a) {
+template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, BLOCKS) dropout(const __grid_constant__ Args a) {
+    constexpr int UNROLL = sizeof(T) == 4 ? 2 : 4;
     const uint64_t offset = a.drop.at();
     const uint32_t stride = gridDim.x * THREADS;
-    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 < a.groups; q0 += (uint64_t)stride * UNROLL) {
+    // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop
+    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 - (threadIdx.x & 31) < a.units; q0 += (uint64_t)stride * UNROLL) {
         Eight<T> e[UNROLL];
-        uint32_t row[UNROLL], chunk[UNROLL];
+        uint32_t row[UNROLL], k[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint64_t q = q0 + (uint64_t)u * stride;
-            if (q >= a.groups) continue;
             row[u] = (__umulhi((uint32_t)q, a.mul) + (uint32_t)q) >> a.shift;
-            chunk[u] = (uint32_t)q - row[u] * a.per_row;
-            e[u].template load<true>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.cols - 8ll * chunk[u]));
+            k[u] = (uint32_t)q - row[u] * a.per_row;
+            if (q < a.units) e[u].template load<true, WIDE>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride, Columns<WIDE>(k[u], a.cols));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            if (q0 + (uint64_t)u * stride >= a.groups) continue;
+            const uint64_t q = q0 + (uint64_t)u * stride;
+            if (q - (threadIdx.x & 31) >= a.units) break;
+            const uint32_t keep = keep8<WIDE>(a.drop, k[u], a.row0 + row[u], offset);
+            if (q >= a.units) continue;
             float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = e[u].get(i);
-            drop8(a.drop, philox(a.drop, chunk[u], a.row0 + row[u], offset), x);
+            for (int i = 0; i < 8; ++i) x[i] = (keep >> i) & 1 ? e[u].get(i) * a.drop.factor : 0.f;
             e[u].set(x);
-            e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.cols - 8ll * chunk[u]));
+            e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.cols));
         }
     }
 }
 
-template <typename T> int run(Args a, uint64_t rows, uint64_t per_row, uint32_t dtype, cudaStream_t stream) {
+template <typename T> int run(Args a, uint64_t rows, cudaStream_t stream) {
+    const uint64_t per_row = a.wide ? (uint64_t)a.cols / 8 : (uint64_t)(a.cols + 255) / 256 * 32;
     const uint64_t most = std::max<uint64_t>(1, 0x7FFFFFFFull / per_row);  // rows of a launch
     a.per_row = (uint32_t)per_row;
-    a.shift = 0;
     while ((1ull << a.shift) < per_row) ++a.shift;
     a.mul = (uint32_t)((((1ull << a.shift) - per_row) << 32) / per_row + 1);
     for (uint64_t r = 0; r < rows; r += most) {
-        const uint64_t n = std::min(most, rows - r), groups = n * per_row;
-        a.row0 = (uint32_t)r, a.groups = (uint32_t)groups;
-        const unsigned grid = (unsigned)std::min<uint64_t>((groups + THREADS - 1) / THREADS, SMS * 8);
-        dropout<T><<<grid, THREADS, 0, stream>>>(a);
+        const uint64_t n = std::min(most, rows - r), units = n * per_row;
+        a.row0 = (uint32_t)r, a.units = (uint32_t)units;
+        const unsigned grid = (unsigned)std::min<uint64_t>((units + THREADS - 1) / THREADS, SMS * BLOCKS);
+        (a.wide ? dropout<T, true> : dropout<T, false>)<<<grid, THREADS, 0, stream>>>(a);
         SCOUT_CUDA(cudaGetLastError());
         a.x = reinterpret_cast<const T *>(a.x) + n * a.x_stride, a.y = reinterpret_cast<T *>(a.y) + n * a.y_stride;
     }
@@ -82,11 +85,10 @@ extern "C" int scout_dropout(uint32_t dtype, uint64_t rows, uint64_t cols, const
     if (int rc = check_matrix(x, x_stride, cols, dtype)) return rc;
     if (int rc = check_matrix(y, y_stride, cols, dtype)) return rc;
     a.x = x, a.y = y, a.x_stride = (int64_t)x_stride, a.y_stride = (int64_t)y_stride, a.cols = (int64_t)cols;
-    a.wide = wide_rows(x, x_stride, dtype) && wide_rows(y, y_stride, dtype);
-    const uint64_t per_row = (cols + 7) / 8;
+    a.wide = cols % 8 == 0 && wide_rows(x, x_stride, dtype) && wide_rows(y, y_stride, dtype);
     switch (dtype) {
-        case SCOUT_DT_F32: return run<float>(a, rows, per_row, dtype, (cudaStream_t)stream);
-        case SCOUT_DT_BF16: return run<__nv_bfloat16>(a, rows, per_row, dtype, (cudaStream_t)stream);
-        default: return run<__half>(a, rows, per_row, dtype, (cudaStream_t)stream);
+        case SCOUT_DT_F32: return run<float>(a, rows, (cudaStream_t)stream);
+        case SCOUT_DT_BF16: return run<__nv_bfloat16>(a, rows, (cudaStream_t)stream);
+        default: return run<__half>(a, rows, (cudaStream_t)stream);
     }
 }

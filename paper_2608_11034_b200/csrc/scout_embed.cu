@@ -21,7 +21,7 @@ namespace {
 
 namespace cg = cooperative_groups;
 
-constexpr int THREADS = 256, UNROLL = 4;
+constexpr int THREADS = 256, BLOCKS = 5;  // blocks of an SM
 
 // id of place t, or `vocab` where it is outside 0..vocab-1
 __device__ __forceinline__ uint32_t id_at(const void *ids, bool wide, int64_t t, uint32_t vocab) {
@@ -34,53 +34,51 @@ struct Lookup {
     const void *ids, *table;
     void *y;
     int64_t table_stride, y_stride, dim, row0;
-    uint32_t vocab, per_row, groups, mul, shift;  // eights of a row, of all rows; n / per_row
+    uint32_t vocab, per_row, units, mul, shift;  // eights of a row (whole warps of them unless wide), of all rows; n / per_row
     float scale;
     int id64, wide;
 };
 
-template <typename T, typename TO> __global__ void __launch_bounds__(THREADS) lookup(const __grid_constant__ Lookup a) {
+template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(THREADS, BLOCKS) lookup(const __grid_constant__ Lookup a) {
+    constexpr int UNROLL = sizeof(T) == 4 ? 2 : 4;
     const uint32_t stride = gridDim.x * THREADS;
-    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 < a.groups; q0 += (uint64_t)stride * UNROLL) {
+    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 < a.units; q0 += (uint64_t)stride * UNROLL) {
         Eight<T> e[UNROLL];
-        uint32_t row[UNROLL], chunk[UNROLL], id[UNROLL];
+        uint32_t row[UNROLL], k[UNROLL], id[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint64_t q = q0 + (uint64_t)u * stride;
-            if (q >= a.groups) continue;
             row[u] = (__umulhi((uint32_t)q, a.mul) + (uint32_t)q) >> a.shift;
-            chunk[u] = (uint32_t)q - row[u] * a.per_row;
-            id[u] = id_at(a.ids, a.id64, a.row0 + row[u], a.vocab);
+            k[u] = (uint32_t)q - row[u] * a.per_row;
+            id[u] = q < a.units ? id_at(a.ids, a.id64, a.row0 + row[u], a.vocab) : a.vocab;
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            if (q0 + (uint64_t)u * stride >= a.groups) continue;
             e[u].zero();
-            if (id[u] < a.vocab)
-                e[u].template load<false>(reinterpret_cast<const T *>(a.table) + (int64_t)id[u] * a.table_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.dim - 8ll * chunk[u]));
+            if (id[u] < a.vocab) e[u].template load<false, WIDE>(reinterpret_cast<const T *>(a.table) + (int64_t)id[u] * a.table_stride, Columns<WIDE>(k[u], a.dim));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            if (q0 + (uint64_t)u * stride >= a.groups) continue;
+            if (q0 + (uint64_t)u * stride >= a.units) break;
             float x[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = id[u] < a.vocab ? a.scale * e[u].get(i) : 0.f;
             Eight<TO> o;
             o.set(x);
-            o.store(reinterpret_cast<TO *>(a.y) + row[u] * a.y_stride + 8ll * chunk[u], a.wide, (int)min(8ll, (long long)a.dim - 8ll * chunk[u]));
+            o.store(reinterpret_cast<TO *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.dim));
         }
     }
 }
 
 template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaStream_t stream) {
-    const uint64_t per_row = ((uint64_t)a.dim + 7) / 8, most = std::max<uint64_t>(1, 0x7FFFFFFFull / per_row);
+    const uint64_t per_row = a.wide ? (uint64_t)a.dim / 8 : (uint64_t)(a.dim + 255) / 256 * 32, most = std::max<uint64_t>(1, 0x7FFFFFFFull / per_row);
     a.per_row = (uint32_t)per_row;
     while ((1ull << a.shift) < per_row) ++a.shift;
     a.mul = (uint32_t)((((1ull << a.shift) - per_row) << 32) / per_row + 1);
     for (uint64_t r = 0; r < rows; r += most) {
-        const uint64_t groups = std::min(most, rows - r) * per_row;
-        a.row0 = (int64_t)r, a.groups = (uint32_t)groups;
-        lookup<T, TO><<<(unsigned)std::min<uint64_t>((groups + THREADS - 1) / THREADS, SMS * 8), THREADS, 0, stream>>>(a);
+        const uint64_t units = std::min(most, rows - r) * per_row;
+        a.row0 = (int64_t)r, a.units = (uint32_t)units;
+        (a.wide ? lookup<T, TO, true> : lookup<T, TO, false>)<<<(unsigned)std::min<uint64_t>((units + THREADS - 1) / THREADS, SMS * BLOCKS), THREADS, 0, stream>>>(a);
         SCOUT_CUDA(cudaGetLastError());
         a.y = reinterpret_cast<TO *>(a.y) + std::min(most, rows - r) * a.y_stride;
     }
@@ -90,7 +88,7 @@ template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaS
 // ---- backward -----------------------------------------------------------------------------------------
 constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT;
 constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4;
-constexpr int PIECE = 32, SUM_THREADS = 128, FILL_BYTES = 1 << 16;
+constexpr int PIECE = 32, AHEAD = 8, SUM_THREADS = 128, FILL_BYTES = 1 << 16;
 constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
 
 struct Grad {
@@ -175,30 +173,35 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) 
 }
 
 // out = (accumulate ? out : 0) + scale * sum, eight columns
-template <typename TO> __device__ __forceinline__ void put(const Grad &a, uint32_t id, int64_t col, int n, const float (&sum)[8]) {
-    TO *p = reinterpret_cast<TO *>(a.table) + (int64_t)id * a.table_stride + col;
+template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad &a, uint32_t id, const Columns<WIDE> &c, const float (&sum)[8]) {
+    TO *row = reinterpret_cast<TO *>(a.table) + (int64_t)id * a.table_stride;
     Eight<TO> e;
     float x[8];
-    if (a.accumulate) e.template load<true>(p, a.wide, n);
+    if (a.accumulate) e.template load<true, WIDE>(row, c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = a.accumulate ? fmaf(a.scale, sum[i], e.get(i)) : a.scale * sum[i];
     e.set(x);
-    e.store(p, a.wide, n);
+    e.store(row, c);
 }
 
-template <typename T, typename TO> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
+// zeros to a row, whatever it starts on: whole 16 bytes, and the elements before and behind them
+template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_t dim) {
+    constexpr int N = 16 / sizeof(TO);
+    const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int64_t)sizeof(TO), dim), body = (dim - head) / N;
+    if (threadIdx.x < head) row[threadIdx.x] = down<TO>(0.f);
+    uint4 *const wide = reinterpret_cast<uint4 *>(row + head);
+    for (int64_t i = threadIdx.x; i < body; i += SUM_THREADS) wide[i] = make_uint4(0, 0, 0, 0);
+    if (head + body * N + threadIdx.x < dim) row[head + body * N + threadIdx.x] = down<TO>(0.f);
+}
+
+template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
     pdl_wait();
     const uint32_t *const keys = a.key[(a.passes + 1) & 1], *const places = a.place[(a.passes + 1) & 1];
     const uint64_t sums = (uint64_t)a.pieces * a.across;
     if (blockIdx.x >= sums) {  // zeros
         const int64_t v0 = (int64_t)(blockIdx.x - sums) * a.fill_rows, v1 = min(v0 + a.fill_rows, (int64_t)a.vocab);
-        Eight<TO> z;
-        z.zero();
-        for (int64_t v = v0; v < v1; ++v) {
-            if ((a.seen[v >> 5] >> (v & 31)) & 1) continue;
-            for (int64_t c = 8 * threadIdx.x; c < a.dim; c += 8 * SUM_THREADS)
-                z.store(reinterpret_cast<TO *>(a.table) + v * a.table_stride + c, a.wide, (int)min(8ll, (long long)a.dim - c));
-        }
+        for (int64_t v = v0; v < v1; ++v)
+            if (!((a.seen[v >> 5] >> (v & 31)) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + v * a.table_stride, a.dim);
         return;
     }
     __shared__ uint32_t key[PIECE + 2], place[PIECE];
@@ -212,31 +215,29 @@ template <typename T, typename TO> __global__ void __launch_bounds__(SUM_THREADS
     }
     if (threadIdx.x < count) place[threadIdx.x] = places[p0 + threadIdx.x];
     __syncthreads();
-    const int64_t col = ((int64_t)(blockIdx.x % a.across) * SUM_THREADS + threadIdx.x) * 8;
-    const int n = (int)max(0ll, min(8ll, (long long)a.dim - col));
-    if (n == 0) return;
+    const Columns<WIDE> c((int64_t)(blockIdx.x % a.across) * SUM_THREADS + threadIdx.x, a.dim);
+    if (!c.any()) return;
     float sum[8] = {};
     bool begun = key[0] != key[1];  // the current id's places begin inside this piece
-    for (int k0 = 0; k0 < count; k0 += UNROLL) {
-        Eight<T> e[UNROLL];
+    for (int k0 = 0; k0 < count; k0 += AHEAD) {
+        Eight<T> e[AHEAD];
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u)
-            if (k0 + u < count && key[k0 + u + 1] < a.vocab)
-                e[u].template load<true>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride + col, a.wide, n);
+        for (int u = 0; u < AHEAD; ++u)
+            if (k0 + u < count && key[k0 + u + 1] < a.vocab) e[u].template load<true, WIDE>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride, c);
 #pragma unroll
-        for (int u = 0; u < UNROLL; ++u) {
+        for (int u = 0; u < AHEAD; ++u) {
             const int k = k0 + u;
             if (k >= count || key[k + 1] >= a.vocab) break;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += e[u].get(i);
             const bool ends = key[k + 2] != key[k + 1];
             if (ends && begun) {
-                put<TO>(a, key[k + 1], col, n, sum);
+                put<TO>(a, key[k + 1], c, sum);
             } else if (ends || k + 1 == count) {
-                float *part = a.part + ((int64_t)piece * 2 + begun) * a.dim + col;
+                float *part = a.part + ((int64_t)piece * 2 + begun) * a.dim;
 #pragma unroll
                 for (int i = 0; i < 8; ++i)
-                    if (i < n) part[i] = sum[i];
+                    if (c.has(i)) part[c.col(i)] = sum[i];
             }
             if (ends) {
                 begun = true;
@@ -313,7 +314,7 @@ template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream
     a.fill_rows = (uint32_t)std::max<uint64_t>(1, FILL_BYTES / (a.dim * sizeof(TO)));
     const uint64_t fill = a.accumulate ? 0 : (a.vocab + a.fill_rows - 1) / a.fill_rows, grid = (uint64_t)a.pieces * a.across + fill;
     if (grid > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
-    if (grid) SCOUT_CUDA(launch_dependent(sum_places<T, TO>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
+    if (grid) SCOUT_CUDA(launch_dependent(a.wide ? sum_places<T, TO, true> : sum_places<T, TO, false>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
     if (a.pieces > 1) {
         const uint32_t wide = (uint32_t)((a.dim + JOIN_COLS - 1) / JOIN_COLS);
         const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 4 * SMS / wide)));
@@ -359,7 +360,7 @@ extern "C" int scout_embed_forward(uint32_t id_dtype, uint32_t dtype, uint32_t o
     Lookup a = {};
     a.ids = ids, a.table = table, a.y = y, a.table_stride = (int64_t)table_stride, a.y_stride = (int64_t)y_stride, a.dim = (int64_t)dim;
     a.vocab = (uint32_t)vocab, a.scale = scale, a.id64 = id_dtype == SCOUT_DT_I64;
-    a.wide = wide_rows(table, table_stride, dtype) && wide_rows(y, y_stride, out_dtype);
+    a.wide = dim % 8 == 0 && wide_rows(table, table_stride, dtype) && wide_rows(y, y_stride, out_dtype);
     const cudaStream_t s = (cudaStream_t)stream;
     const bool f32 = out_dtype == SCOUT_DT_F32;
     switch (dtype) {
@@ -404,7 +405,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     while (vocab >> bits) ++bits;  // digits of `vocab` itself, which stands for ids outside
     a.passes = (bits + MAX_DIGIT - 1) / MAX_DIGIT, a.digit = (bits + a.passes - 1) / a.passes;
     a.id64 = id_dtype == SCOUT_DT_I64, a.accumulate = (int)accumulate, a.scale = scale;
-    a.wide = (!rows || wide_rows(dy, dy_stride, dtype)) && wide_rows(d_table, d_table_stride, out_dtype);
+    a.wide = dim % 8 == 0 && (!rows || wide_rows(dy, dy_stride, dtype)) && wide_rows(d_table, d_table_stride, out_dtype);
     const cudaStream_t s = (cudaStream_t)stream;
     const bool f32 = out_dtype == SCOUT_DT_F32;
     switch (dtype) {

@@ -1,9 +1,9 @@
 // A block's output joins the residual stream: u = dropout(rms norm of b), y = x + scale gate u, n = rms norm of y; and the gradients.
 //
 // Bound by memory: forward reads x, b and writes y, n; backward reads dy, dn, b, y and writes dx, db.  A row is held in registers by
-// one team of warps, eight elements a thread (16 beyond 4096), so that each tensor crosses memory once although a row's sums are
-// needed twice.  Rows are dealt to teams: in turn (forward), in runs (backward, whose column sums stay with the thread that owns
-// the column for a whole run; runs meet in a second kernel, in order).
+// one team of warps, eight elements a thread (32 beyond 4096), so that each tensor crosses memory once although a row's sums are
+// needed twice, and the next rows are fetched before the present ones are worked on.  Rows are dealt to teams: in turn (forward), in
+// runs (backward, whose column sums stay with the thread that owns the column for a whole run; runs meet in a second kernel, in order).
 #include <algorithm>
 #include <cmath>
 
@@ -13,7 +13,7 @@ namespace scout {
 namespace step {
 namespace {
 
-constexpr int MAX_DIM = 16384;
+constexpr int MAX_DIM = 16384, THREADS = 512;  // registers for two blocks' worth of half as many threads
 
 struct Args {
     const void *x, *b, *dy, *dn, *yin, *gate, *post, *norm;
@@ -26,214 +26,301 @@ struct Args {
     int64_t rows, group_rows, per, slabs;
     int32_t dim, team, teams;  // threads of a team, teams of a block
     float scale, eps, inv_dim;
-    int wide, wide_w;
+    bool wide;  // all rows, those of the weights too, on 16-byte boundaries and of whole eights
     Drop drop;
 };
 
-// Sum over a team.  `slots`: [teams][32] in shared memory, not written again before every thread has passed another team_sum.
-__device__ __forceinline__ float team_sum(float v, float *slots, int team_threads, int t) {
-    v = warp_sum(v);
-    if (team_threads == 32) return v;
-    if ((t & 31) == 0) slots[t >> 5] = v;
+// Sums over a team, R at once.  Set k of the slots ([2][R][warps of the block] in shared memory) is not written again before every
+// thread has passed another team_sum.
+template <int R, int N> __device__ __forceinline__ void team_sum(float (&x)[R], float (*slots)[N], int k, int team_threads, int team, int t) {
+#pragma unroll
+    for (int r = 0; r < R; ++r) x[r] = warp_sum(x[r]);
+    if (team_threads == 32) return;
+    const int warps = team_threads / 32, at = team * warps;
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+        if ((t & 31) == 0) slots[k * R + r][at + (t >> 5)] = x[r];
     __syncthreads();
-    return warp_sum((t & 31) < team_threads / 32 ? slots[t & 31] : 0.f);
+#pragma unroll
+    for (int r = 0; r < R; ++r) x[r] = warp_sum((t & 31) < warps ? slots[k * R + r][at + (t & 31)] : 0.f);
 }
-__device__ __forceinline__ int eights(int dim, int chunk) { return max(0, min(8, dim - 8 * chunk)); }
-// A row of weights, or what stands for none.
-template <typename TW> __device__ __forceinline__ void weights(float (&w)[8], const void *row, int chunk, int n, bool wide, float none) {
+// Pairs of weights, or what stands for none.
+template <typename TW, bool WIDE> __device__ __forceinline__ void weights(tc::F2 (&w)[4], const void *row, const Columns<WIDE> &c) {
     if (!row) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = none;
+        for (int i = 0; i < 4; ++i) w[i] = tc::f2(1.f, 1.f);
         return;
     }
     Eight<TW> e;
-    e.template load<false>(reinterpret_cast<const TW *>(row) + 8 * chunk, wide, n);
+    e.template load<false, WIDE>(reinterpret_cast<const TW *>(row), c);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = e.get(i);
+    for (int i = 0; i < 4; ++i) w[i] = e.pair(i);
 }
 template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, int64_t row) {
     return a.gate ? reinterpret_cast<const TW *>(a.gate) + row / a.group_rows * a.dim : nullptr;
 }
+__device__ __forceinline__ tc::F2 both(float x) { return tc::f2(x, x); }
+// pair i of what is kept: the factor where it is, else 0
+__device__ __forceinline__ tc::F2 kept(uint32_t keep, int i, float factor) {
+    return tc::f2((keep >> (2 * i)) & 1 ? factor : 0.f, (keep >> (2 * i + 1)) & 1 ? factor : 0.f);
+}
+__device__ __forceinline__ float add_pairs(const tc::F2 &x) {
+    const float2 f = tc::split(x);
+    return f.x + f.y;
+}
 
-template <typename TB, typename TS, typename TW, int V, int MOST> __global__ void __launch_bounds__(MOST) join_forward(const __grid_constant__ Args a) {
-    __shared__ float slots[2][32];
+// R rows of a team at a time share the waits of their sums and the weights they read; the next R are on their way meanwhile.
+template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ void __launch_bounds__(THREADS) join_forward(const __grid_constant__ Args a) {
+    constexpr int R = V == 1 ? 2 : 1;
+    constexpr bool AHEAD = V == 1;
+    __shared__ float slots[2 * R][THREADS / 32];
     const int t = threadIdx.x % a.team, team = threadIdx.x / a.team;
-    float *const s0 = slots[0] + team * (a.team / 32), *const s1 = slots[1] + team * (a.team / 32);
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
-    for (int64_t base = (int64_t)blockIdx.x * a.teams; base < a.rows; base += (int64_t)gridDim.x * a.teams) {
-        const int64_t row = base + team;
-        const bool on = row < a.rows;
-        Eight<TB> b[V];
-        Eight<TS> x[V];
-        float u[V][8];
-        float sq = 0.f;
+    Eight<TB> b[R][V], b_next[R][V];
+    Eight<TS> x[R][V], x_next[R][V];
+    const int64_t stride = (int64_t)gridDim.x * a.teams;
+    int64_t row = (int64_t)blockIdx.x * a.teams + team;
+    const auto fetch = [&](Eight<TB> (&eb)[R][V], Eight<TS> (&ex)[R][V], int64_t from) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-            b[v].zero(), x[v].zero();
-            if (n) {
-                b[v].template load<true>(reinterpret_cast<const TB *>(a.b) + row * a.b_stride + 8 * chunk, a.wide, n);
-                if (a.x) x[v].template load<true>(reinterpret_cast<const TS *>(a.x) + row * a.x_stride + 8 * chunk, a.wide, n);
-            }
-        }
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) u[v][i] = b[v].get(i), sq += u[v][i] * u[v][i];
-        float rb = 0.f;
-        if (a.post) rb = rsqrtf(team_sum(sq, s0, a.team, t) * a.inv_dim + a.eps);
-        sq = 0.f;
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-            if (n) {
-                float w[8];
-                if (a.post) {
-                    weights<TW>(w, a.post, chunk, n, a.wide_w, 1.f);
-#pragma unroll
-                    for (int i = 0; i < 8; ++i) u[v][i] *= rb * w[i];
-                }
-                if (a.drop.cut) drop8(a.drop, philox(a.drop, chunk, (uint32_t)row, offset), u[v]);
-                weights<TW>(w, gate_row<TW>(a, row), chunk, n, a.wide_w, 1.f);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] = fmaf(a.scale * w[i], u[v][i], x[v].get(i));
-                x[v].set(u[v]);
-                x[v].store(reinterpret_cast<TS *>(a.y) + row * a.y_stride + 8 * chunk, a.wide, n);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sq += i < n ? u[v][i] * u[v][i] : 0.f;
-        }
-        float ry = 0.f;
-        if (a.norm) {
-            ry = rsqrtf(team_sum(sq, s1, a.team, t) * a.inv_dim + a.eps);
+        for (int r = 0; r < R; ++r)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-                if (!n) continue;
-                float w[8];
-                weights<TW>(w, a.norm, chunk, n, a.wide_w, 1.f);
+                const Columns<WIDE> c(t + v * a.team, a.dim);
+                const int64_t at = from + r * stride;
+                eb[r][v].zero(), ex[r][v].zero();
+                if (at >= a.rows) continue;
+                eb[r][v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + at * a.b_stride, c);
+                if (a.x) ex[r][v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.x) + at * a.x_stride, c);
+            }
+    };
+    fetch(b, x, row);
+    for (; row - team < a.rows; row += R * stride) {  // the same for all teams of a block
+        if constexpr (AHEAD) fetch(b_next, x_next, row + R * stride);
+        tc::F2 u[R][V][4];
+        float sum[R];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) w[i] *= u[v][i] * ry;
-                b[v].set(w);
-                b[v].store(reinterpret_cast<TB *>(a.n) + row * a.n_stride + 8 * chunk, a.wide, n);
+        for (int r = 0; r < R; ++r) {
+            tc::F2 sq = both(0.f);
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) u[r][v][i] = b[r][v].pair(i), sq = tc::fma2(u[r][v][i], u[r][v][i], sq);
+            sum[r] = add_pairs(sq);
+        }
+        float rb[R] = {}, ry[R] = {};
+        if (a.post) {
+            team_sum<R>(sum, slots, 0, a.team, team, t);
+#pragma unroll
+            for (int r = 0; r < R; ++r) rb[r] = rsqrtf(sum[r] * a.inv_dim + a.eps);
+        }
+        tc::F2 sq[R];
+#pragma unroll
+        for (int r = 0; r < R; ++r) sq[r] = both(0.f);
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Columns<WIDE> c(t + v * a.team, a.dim);
+            if (a.post) {
+                tc::F2 w[4];
+                weights<TW, WIDE>(w, a.post, c);
+#pragma unroll
+                for (int r = 0; r < R; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) u[r][v][i] = tc::mul2(u[r][v][i], tc::mul2(both(rb[r]), w[i]));
+            }
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const int64_t at = row + r * stride;
+                if (a.drop.cut) {
+                    const uint32_t keep = keep8<WIDE>(a.drop, t + v * a.team, (uint32_t)at, offset);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {  // what is dropped is 0, whatever it was
+                        const float2 f = tc::split(u[r][v][i]);
+                        u[r][v][i] = tc::f2((keep >> (2 * i)) & 1 ? f.x * a.drop.factor : 0.f, (keep >> (2 * i + 1)) & 1 ? f.y * a.drop.factor : 0.f);
+                    }
+                }
+                if (at >= a.rows) continue;
+                tc::F2 w[4];
+                weights<TW, WIDE>(w, gate_row<TW>(a, at), c);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    u[r][v][i] = tc::fma2(tc::mul2(both(a.scale), w[i]), u[r][v][i], x[r][v].pair(i));
+                    sq[r] = tc::fma2(u[r][v][i], u[r][v][i], sq[r]);
+                }
+                x[r][v].set(u[r][v]);
+                x[r][v].store(reinterpret_cast<TS *>(a.y) + at * a.y_stride, c);
             }
         }
-        if (t == 0 && on) a.stats[row] = rb, a.stats[a.rows + row] = ry;
-        if (!(a.post && a.norm) && a.team > 32) __syncthreads();  // the one slot row is written again by the next row
+        if (a.norm) {
+#pragma unroll
+            for (int r = 0; r < R; ++r) sum[r] = add_pairs(sq[r]);
+            team_sum<R>(sum, slots, 1, a.team, team, t);
+#pragma unroll
+            for (int r = 0; r < R; ++r) ry[r] = rsqrtf(sum[r] * a.inv_dim + a.eps);
+#pragma unroll
+            for (int v = 0; v < V; ++v) {
+                const Columns<WIDE> c(t + v * a.team, a.dim);
+                tc::F2 w[4];
+                weights<TW, WIDE>(w, a.norm, c);
+#pragma unroll
+                for (int r = 0; r < R; ++r) {
+                    if (row + r * stride >= a.rows) continue;
+                    tc::F2 n[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) n[i] = tc::mul2(w[i], tc::mul2(u[r][v][i], both(ry[r])));
+                    b[r][v].set(n);
+                    b[r][v].store(reinterpret_cast<TB *>(a.n) + (row + r * stride) * a.n_stride, c);
+                }
+            }
+        }
+        if (t < R && row + t * stride < a.rows) {
+            a.stats[row + t * stride] = t == 0 ? rb[0] : rb[R - 1];
+            a.stats[a.rows + row + t * stride] = t == 0 ? ry[0] : ry[R - 1];
+        }
+        if (!(a.post && a.norm) && a.team > 32) __syncthreads();  // the one set of slots is written again by the next rows
+        if constexpr (AHEAD) {
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+#pragma unroll
+                for (int v = 0; v < V; ++v) b[r][v] = b_next[r][v], x[r][v] = x_next[r][v];
+        } else {
+            fetch(b, x, row + R * stride);
+        }
     }
 }
 
-// The column sums of a run of rows: in registers, or with V = 2 in shared memory ([3][V * 8][threads], a thread's own places).
-template <int V> struct Columns {
-    float r[V == 1 ? 3 : 1][8];
-    float *s;
+// The column sums of a run of rows: in registers, or with V > 1 in shared memory ([3][V * 4][threads], a thread's own places).
+template <int V> struct Sums {
+    tc::F2 r[V == 1 ? 3 : 1][4];
+    float2 *s;
     int threads, t;
-    __device__ __forceinline__ float &at(int which, int v, int i) {
-        if constexpr (V == 1) return r[which][i];
-        else return s[((which * V + v) * 8 + i) * threads + t];
+    __device__ __forceinline__ void clear() {
+#pragma unroll
+        for (int k = 0; k < 3; ++k)
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) set(k, v, i, both(0.f));
     }
+    __device__ __forceinline__ tc::F2 get(int which, int v, int i) const {
+        if constexpr (V == 1) {
+            return r[which][i];
+        } else {
+            const float2 f = s[((which * V + v) * 4 + i) * threads + t];
+            return tc::f2(f.x, f.y);
+        }
+    }
+    __device__ __forceinline__ void set(int which, int v, int i, tc::F2 x) {
+        if constexpr (V == 1) r[which][i] = x;
+        else s[((which * V + v) * 4 + i) * threads + t] = tc::split(x);
+    }
+    __device__ __forceinline__ void add(int which, int v, int i, tc::F2 x, tc::F2 y) { set(which, v, i, tc::fma2(x, y, get(which, v, i))); }
 };
 
-template <typename TB, typename TS, typename TW, int V, int MOST> __global__ void __launch_bounds__(MOST) join_backward(const __grid_constant__ Args a) {
-    __shared__ float slots[2][32];
-    extern __shared__ float sums[];
+template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ void __launch_bounds__(THREADS) join_backward(const __grid_constant__ Args a) {
+    constexpr bool AHEAD = V == 1;
+    __shared__ float slots[2][THREADS / 32];
+    extern __shared__ float2 sums[];
     const int t = threadIdx.x % a.team, team = threadIdx.x / a.team;
-    float *const s0 = slots[0] + team * (a.team / 32), *const s1 = slots[1] + team * (a.team / 32);
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
     const int64_t slab = (int64_t)blockIdx.x * a.teams + team, first = slab * a.per, last = min(first + a.per, a.rows);
-    Columns<V> acc;
+    Sums<V> acc;
     if constexpr (V > 1) acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
+    acc.clear();
+    struct Row {
+        Eight<TS> y[V], g[V];
+        Eight<TB> n[V], b[V];
+        float rb, ry;
+    } cur, next;
+    const auto fetch = [&](Row &e, int64_t row) {
+        e.rb = 1.f, e.ry = 0.f;
 #pragma unroll
-    for (int k = 0; k < 3; ++k)
-#pragma unroll
-        for (int v = 0; v < V; ++v)
-#pragma unroll
-            for (int i = 0; i < 8; ++i) acc.at(k, v, i) = 0.f;
+        for (int v = 0; v < V; ++v) {
+            const Columns<WIDE> c(t + v * a.team, a.dim);
+            e.y[v].zero(), e.g[v].zero(), e.n[v].zero(), e.b[v].zero();
+            if (row >= last) continue;
+            if (a.dn) {
+                e.y[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.yin) + row * a.y_stride, c);
+                e.n[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.dn) + row * a.dn_stride, c);
+            }
+            if (a.dy) e.g[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.dy) + row * a.dy_stride, c);
+            e.b[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + row * a.b_stride, c);
+        }
+        if (row >= last) return;
+        if (a.post) e.rb = a.stats_in[row];
+        if (a.dn) e.ry = a.stats_in[a.rows + row];
+    };
     int64_t begun = first;  // where the gate's current sum began
+    fetch(cur, first);
     for (int64_t it = 0; it < a.per; ++it) {
         const int64_t row = first + it;
         const bool on = row < last;
-        Eight<TS> ey[V], eg[V];
-        Eight<TB> en[V], eb[V];
-#pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-            ey[v].zero(), eg[v].zero(), en[v].zero(), eb[v].zero();
-            if (n) {
-                if (a.dn) ey[v].template load<true>(reinterpret_cast<const TS *>(a.yin) + row * a.y_stride + 8 * chunk, a.wide, n);
-                if (a.dn) en[v].template load<true>(reinterpret_cast<const TB *>(a.dn) + row * a.dn_stride + 8 * chunk, a.wide, n);
-                if (a.dy) eg[v].template load<true>(reinterpret_cast<const TS *>(a.dy) + row * a.dy_stride + 8 * chunk, a.wide, n);
-                eb[v].template load<true>(reinterpret_cast<const TB *>(a.b) + row * a.b_stride + 8 * chunk, a.wide, n);
-            }
-        }
-        const float rb = on && a.post ? a.stats_in[row] : 1.f, ry = on && a.dn ? a.stats_in[a.rows + row] : 0.f;
-        float g[V][8];
-        float dot = 0.f;
+        if constexpr (AHEAD) fetch(next, row + 1 < first + a.per ? row + 1 : last);
+        const float rb = cur.rb, ry = cur.ry;
+        tc::F2 g[V][4];
+        float dot[1] = {0.f};
         if (a.dn) {
+            tc::F2 d = both(0.f);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-                float w[8];
-                if (n) weights<TW>(w, a.norm, chunk, n, a.wide_w, 1.f);
+                tc::F2 w[4];
+                weights<TW, WIDE>(w, a.norm, Columns<WIDE>(t + v * a.team, a.dim));
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    const float z = ey[v].get(i) * ry, d = en[v].get(i);
-                    if (i < n) {
-                        g[v][i] = d * w[i];
-                        acc.at(2, v, i) += d * z;
-                        dot += g[v][i] * z;
-                    }
+                for (int i = 0; i < 4; ++i) {
+                    const tc::F2 z = tc::mul2(cur.y[v].pair(i), both(ry)), dn = cur.n[v].pair(i);
+                    g[v][i] = tc::mul2(dn, w[i]);
+                    acc.add(2, v, i, dn, z);
+                    d = tc::fma2(g[v][i], z, d);
                 }
             }
-            dot = team_sum(dot, s0, a.team, t) * a.inv_dim;
+            dot[0] = add_pairs(d);
+            team_sum<1>(dot, slots, 0, a.team, team, t);
         }
-        float dot2 = 0.f;
+        const float pull = -(dot[0] * a.inv_dim) * ry;
+        tc::F2 d = both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-            if (!n) continue;
-            float u[8], w[8], gw[8];
+            const Columns<WIDE> c(t + v * a.team, a.dim);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) g[v][i] = a.dn ? eg[v].get(i) + ry * (g[v][i] - ey[v].get(i) * ry * dot) : eg[v].get(i);
-            if (a.dx) {
-                eg[v].set(g[v]);
-                eg[v].store(reinterpret_cast<TS *>(a.dx) + row * a.dx_stride + 8 * chunk, a.wide, n);
+            for (int i = 0; i < 4; ++i)
+                g[v][i] = a.dn ? tc::fma2(both(ry), tc::fma2(both(pull), cur.y[v].pair(i), g[v][i]), cur.g[v].pair(i)) : cur.g[v].pair(i);
+            if (a.dx && on) {
+                cur.g[v].set(g[v]);
+                cur.g[v].store(reinterpret_cast<TS *>(a.dx) + row * a.dx_stride, c);
             }
-            weights<TW>(w, a.post, chunk, n, a.wide_w, 1.f);
-            weights<TW>(gw, gate_row<TW>(a, row), chunk, n, a.wide_w, 1.f);
+            tc::F2 w[4], gw[4];
+            weights<TW, WIDE>(w, a.post, c);
+            weights<TW, WIDE>(gw, on ? gate_row<TW>(a, row) : nullptr, c);
+            const uint32_t keep = a.drop.cut ? keep8<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset) : 0xFFu;
+            const float factor = a.scale * (a.drop.cut ? a.drop.factor : 1.f);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float h = a.scale * g[v][i];
-                u[i] = eb[v].get(i) * rb * w[i] * h;   // what the gate's sum takes, but for the mask
-                g[v][i] = h * gw[i];                   // du, but for the mask
-            }
-            if (a.drop.cut) {
-                const uint4 bits = philox(a.drop, chunk, (uint32_t)row, offset);
-                drop8(a.drop, bits, u);
-                drop8(a.drop, bits, g[v]);
-            }
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const float c = eb[v].get(i) * rb;
-                if (i < n) {
-                    acc.at(0, v, i) += u[i];
-                    acc.at(1, v, i) += g[v][i] * c;
-                    g[v][i] *= w[i];
-                    dot2 += g[v][i] * c;
+            for (int i = 0; i < 4; ++i) {
+                const tc::F2 cb = tc::mul2(cur.b[v].pair(i), both(rb)), m = kept(keep, i, factor);
+                tc::F2 u = tc::mul2(cb, w[i]);
+                const tc::F2 h = tc::mul2(g[v][i], m);  // scale g, masked
+                if (a.drop.cut) {                      // what was dropped is 0, whatever it was
+                    const float2 f = tc::split(u);
+                    u = tc::f2((keep >> (2 * i)) & 1 ? f.x : 0.f, (keep >> (2 * i + 1)) & 1 ? f.y : 0.f);
                 }
+                acc.add(0, v, i, u, h);
+                const tc::F2 du = tc::mul2(h, gw[i]);
+                acc.add(1, v, i, du, cb);
+                g[v][i] = tc::mul2(du, w[i]);
+                d = tc::fma2(g[v][i], cb, d);
             }
         }
-        if (a.post) dot2 = team_sum(dot2, s1, a.team, t) * a.inv_dim;
+        float dot2[1] = {add_pairs(d)};
+        if (a.post) team_sum<1>(dot2, slots, 1, a.team, team, t);
+        const float pull2 = -(dot2[0] * a.inv_dim) * rb;
+        if (on) {
 #pragma unroll
-        for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = on ? eights(a.dim, chunk) : 0;
-            if (!n) continue;
-            if (a.post) {
+            for (int v = 0; v < V; ++v) {
+                if (a.post) {
 #pragma unroll
-                for (int i = 0; i < 8; ++i) g[v][i] = rb * (g[v][i] - eb[v].get(i) * rb * dot2);
+                    for (int i = 0; i < 4; ++i) g[v][i] = tc::mul2(both(rb), tc::fma2(both(pull2), cur.b[v].pair(i), g[v][i]));
+                }
+                cur.b[v].set(g[v]);
+                cur.b[v].store(reinterpret_cast<TB *>(a.db) + row * a.db_stride, Columns<WIDE>(t + v * a.team, a.dim));
             }
-            eb[v].set(g[v]);
-            eb[v].store(reinterpret_cast<TB *>(a.db) + row * a.db_stride + 8 * chunk, a.wide, n);
         }
         if (!(a.post && a.dn) && a.team > 32) __syncthreads();
         // the gate's sum ends with its group or with the run
@@ -242,27 +329,33 @@ template <typename TB, typename TS, typename TW, int V, int MOST> __global__ voi
             const bool whole = begun == group * a.group_rows && row + 1 == begun + a.group_rows;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const int chunk = t + v * a.team, n = eights(a.dim, chunk);
+                const Columns<WIDE> c(t + v * a.team, a.dim);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    if (i >= n) continue;
-                    if (whole) reinterpret_cast<TW *>(a.d_gate)[group * a.dim + 8 * chunk + i] = down<TW>(acc.at(0, v, i));
-                    else a.part_gate[(slab * 2 + (begun != first)) * a.dim + 8 * chunk + i] = acc.at(0, v, i);
-                    acc.at(0, v, i) = 0.f;
+                    const float2 f = tc::split(acc.get(0, v, i >> 1));
+                    const float x = i & 1 ? f.y : f.x;
+                    if (!c.has(i)) continue;
+                    if (whole) reinterpret_cast<TW *>(a.d_gate)[group * a.dim + c.col(i)] = down<TW>(x);
+                    else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = x;
                 }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc.set(0, v, i, both(0.f));
             }
             begun = row + 1;
         }
+        if constexpr (AHEAD) cur = next;
+        else fetch(cur, it + 1 < a.per ? row + 1 : last);
     }
     if (first < last) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const int chunk = t + v * a.team, n = eights(a.dim, chunk);
+            const Columns<WIDE> c(t + v * a.team, a.dim);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                if (i >= n) continue;
-                if (a.d_post) a.part[slab * 2 * a.dim + 8 * chunk + i] = acc.at(1, v, i);
-                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + 8 * chunk + i] = acc.at(2, v, i);
+                const float2 p = tc::split(acc.get(1, v, i >> 1)), n = tc::split(acc.get(2, v, i >> 1));
+                if (!c.has(i)) continue;
+                if (a.d_post) a.part[slab * 2 * a.dim + c.col(i)] = i & 1 ? p.y : p.x;
+                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = i & 1 ? n.y : n.x;
             }
         }
     }
@@ -304,41 +397,39 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
 
 // How rows are dealt out.
 struct Shape {
-    int v, team, teams, most;
+    int v, team, teams;
     int64_t slabs, per;
 };
-Shape shape(uint64_t rows, uint64_t dim, bool backward) {
+Shape shape(uint64_t rows, uint64_t dim) {
     Shape s = {};
-    const int chunks = (int)((dim + 7) / 8);
-    s.v = chunks > 512 ? 2 : 1;
-    s.team = ((chunks + s.v - 1) / s.v + 31) / 32 * 32;
+    const int threads = (int)((dim + 255) / 256 * 32);  // whole warps of eight columns a thread
+    s.v = threads > THREADS ? 4 : 1;
+    s.team = ((threads + s.v - 1) / s.v + 31) / 32 * 32;
     s.teams = std::max(1, 128 / s.team);
-    s.most = s.team * s.teams > 512 ? 1024 : 512;
-    const int64_t want = (int64_t)SMS * std::max(1, (backward ? 512 : 2048) / (s.team * s.teams)) * s.teams;
+    const int64_t want = (int64_t)SMS * std::max(1, THREADS / (s.team * s.teams)) * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);
     s.slabs = ((int64_t)rows + s.per - 1) / s.per;
     return s;
 }
 
-template <typename TB, typename TS, typename TW> int run_forward(Args &a, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim, false);
+template <typename TB, typename TS, typename TW, bool WIDE> int run_forward(Args &a, cudaStream_t stream) {
+    const Shape s = shape(a.rows, a.dim);
     a.team = s.team, a.teams = s.teams;
-    const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * std::max(1, 2048 / (s.team * s.teams)));
-    const auto kernel = s.v == 1 ? join_forward<TB, TS, TW, 1, 512> : join_forward<TB, TS, TW, 2, 1024>;
-    kernel<<<grid, s.team * s.teams, 0, stream>>>(a);
+    const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * std::max(1, THREADS / (s.team * s.teams)));
+    (s.v == 1 ? join_forward<TB, TS, TW, 1, WIDE> : join_forward<TB, TS, TW, 4, WIDE>)<<<grid, s.team * s.teams, 0, stream>>>(a);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
 
-template <typename TB, typename TS, typename TW> int run_backward(Args &a, int64_t groups, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim, true);
+template <typename TB, typename TS, typename TW, bool WIDE> int run_backward(Args &a, int64_t groups, cudaStream_t stream) {
+    const Shape s = shape(a.rows, a.dim);
     a.team = s.team, a.teams = s.teams, a.per = s.per, a.slabs = s.slabs;
     const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams);
     if (s.v == 1) {
-        join_backward<TB, TS, TW, 1, 512><<<grid, s.team * s.teams, 0, stream>>>(a);
+        join_backward<TB, TS, TW, 1, WIDE><<<grid, s.team * s.teams, 0, stream>>>(a);
     } else {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 2, 1024>>(3 * 2 * 8 * 1024 * 4)) return rc;
-        join_backward<TB, TS, TW, 2, 1024><<<grid, s.team * s.teams, 3 * 2 * 8 * 4 * s.team * s.teams, stream>>>(a);
+        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE>>(3 * 4 * 4 * 8 * THREADS)) return rc;
+        join_backward<TB, TS, TW, 4, WIDE><<<grid, s.team * s.teams, 3 * 4 * 4 * 8 * s.team * s.teams, stream>>>(a);
     }
     SCOUT_CUDA(cudaGetLastError());
     if (!a.d_post && !a.d_norm && !a.d_gate) return SCOUT_OK;
@@ -373,6 +464,11 @@ int check_weights(const scout_join_t *j, std::initializer_list<const void *> all
         if (!aligned(p, size_of(j->weight_dtype))) return SCOUT_ERR_ALIGN;
     return SCOUT_OK;
 }
+bool wide_weights(const scout_join_t *j, std::initializer_list<const void *> all) {
+    for (const void *p : all)
+        if (!wide_rows(p, j->dim, j->weight_dtype)) return false;
+    return true;
+}
 void describe(const scout_join_t *j, Args *a) {
     a->x_stride = (int64_t)j->x_stride, a->b_stride = (int64_t)j->b_stride, a->y_stride = (int64_t)j->y_stride, a->n_stride = (int64_t)j->n_stride;
     a->dy_stride = (int64_t)j->dy_stride, a->dn_stride = (int64_t)j->dn_stride, a->dx_stride = (int64_t)j->dx_stride, a->db_stride = (int64_t)j->db_stride;
@@ -402,17 +498,19 @@ extern "C" int scout_join_forward(const scout_join_t *j, const void *x, const vo
     if (int rc = check_weights(j, {gate, post, norm})) return rc;
     describe(j, &a);
     a.x = x, a.b = b, a.gate = gate, a.post = post, a.norm = norm, a.y = y, a.n = n, a.stats = stats;
-    a.wide = (!x || wide_rows(x, j->x_stride, j->stream_dtype)) && wide_rows(b, j->b_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype) &&
+    a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!x || wide_rows(x, j->x_stride, j->stream_dtype)) && wide_rows(b, j->b_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype) &&
              (!n || wide_rows(n, j->n_stride, j->dtype));
-    a.wide_w = wide_rows(gate, j->dim, j->weight_dtype) && wide_rows(post, 0, j->weight_dtype) && wide_rows(norm, 0, j->weight_dtype);
-    return by_types(*j, [&](auto tb, auto ts, auto tw) { return run_forward<decltype(tb), decltype(ts), decltype(tw)>(a, (cudaStream_t)stream); });
+    return by_types(*j, [&](auto tb, auto ts, auto tw) { 
+        const cudaStream_t s = (cudaStream_t)stream;
+        return a.wide ? run_forward<decltype(tb), decltype(ts), decltype(tw), true>(a, s) : run_forward<decltype(tb), decltype(ts), decltype(tw), false>(a, s);
+    });
 }
 
 extern "C" int scout_join_backward_workspace(const scout_join_t *j, uint64_t *bytes) {
     using namespace scout::step;
     if (!bytes) return SCOUT_ERR_INVALID;
     if (int rc = check(j)) return rc;
-    *bytes = (uint64_t)(shape(j->rows, j->dim, true).slabs * 4 * j->dim * 4 + 255) & ~255ull;
+    *bytes = (uint64_t)(shape(j->rows, j->dim).slabs * 4 * j->dim * 4 + 255) & ~255ull;
     return SCOUT_OK;
 }
 
@@ -451,11 +549,12 @@ extern "C" int scout_join_backward(const scout_join_t *j, const void *dy, const 
     a.dy = dy, a.dn = dn, a.b = b, a.yin = y, a.stats_in = stats, a.gate = gate, a.post = post, a.norm = norm;
     a.dx = dx, a.db = db, a.d_gate = d_gate, a.d_post = d_post, a.d_norm = d_norm;
     a.part = (float *)workspace;
-    a.part_gate = a.part + shape(j->rows, j->dim, true).slabs * 2 * (int64_t)j->dim;
-    a.wide = (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
+    a.part_gate = a.part + shape(j->rows, j->dim).slabs * 2 * (int64_t)j->dim;
+    a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
              wide_rows(b, j->b_stride, j->dtype) && (!dx || wide_rows(dx, j->dx_stride, j->stream_dtype)) && wide_rows(db, j->db_stride, j->dtype);
-    a.wide_w = wide_rows(gate, j->dim, j->weight_dtype) && wide_rows(post, 0, j->weight_dtype) && wide_rows(norm, 0, j->weight_dtype);
     return by_types(*j, [&](auto tb, auto ts, auto tw) {
-        return run_backward<decltype(tb), decltype(ts), decltype(tw)>(a, (int64_t)j->groups, (cudaStream_t)stream);
+        const cudaStream_t s = (cudaStream_t)stream;
+        const int64_t groups = (int64_t)j->groups;
+        return a.wide ? run_backward<decltype(tb), decltype(ts), decltype(tw), true>(a, groups, s) : run_backward<decltype(tb), decltype(ts), decltype(tw), false>(a, groups, s);
     });
 }

@@ -48,7 +48,8 @@ struct Args {
     int32_t *which;     // [padded]: row of x of a taken row
     int32_t *where;     // [rows]: its place among the taken rows, or -1
     int32_t *target;    // [padded]
-    float *row_lse, *row_g, *row_rest, *row_score;  // [padded]: lse; g / g_ref; what rounding took from G at the target; the target's score
+    float *row_lse, *row_g, *row_rest;  // [padded]: lse; g / g_ref; what rounding took from G at the target
+    float *row_score, *row_rough;       // [padded]: the target's score, in fp32 and as the tensor cores have it
     void *xc, *gs;      // [padded][dim], [padded][piece]
     float2 *part;       // [2 * tiles of the vocabulary][padded]: maximum and sum of 128 columns
     float *dxp;         // [splits][padded][dim]
@@ -63,11 +64,23 @@ __device__ __forceinline__ int target_at(const Args &a, int64_t t) {
     const int64_t v = a.id64 ? reinterpret_cast<const int64_t *>(a.targets)[t] : (int64_t) reinterpret_cast<const int32_t *>(a.targets)[t];
     return v >= 0 && v < a.vocab ? (int)v : -1;
 }
-// Each block takes a run of rows; how many before it count it finds out by itself.
+template <typename T> __device__ __forceinline__ void load_any(Eight<T> &e, const T *p, bool wide) {
+    if (wide) {
+        e.w[0] = __ldcs(reinterpret_cast<const uint4 *>(p));
+    } else {
+        const uint16_t *h = reinterpret_cast<const uint16_t *>(p);
+        uint32_t v[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = h[2 * i] | (uint32_t)h[2 * i + 1] << 16;
+        e.w[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    }
+}
+// Each block takes a run of rows; how many before it count it finds out by itself.  For the forward pass a row's score at its target
+// is made here too, in fp32 (see join_scores).
 template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(const __grid_constant__ Args a, int64_t per) {
     __shared__ int counts[TAKE_THREADS / 32];
     __shared__ float tops[TAKE_THREADS / 32];
-    __shared__ int rows_at[TAKE_THREADS];
+    __shared__ int rows_at[TAKE_THREADS], targets[TAKE_THREADS];
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r0 = blockIdx.x * per, r1 = min(r0 + per, a.rows);
     const bool last = r1 == a.rows;
@@ -102,7 +115,7 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
         for (int w = 0; w < TAKE_THREADS / 32; ++w) at += w < warp ? counts[w] : 0, all += counts[w];
         at += __popc(who & ((1u << lane) - 1));
         if (target >= 0) {
-            rows_at[at] = (int)t;
+            rows_at[at] = (int)t, targets[at] = target;
             a.which[before + at] = (int)t, a.target[before + at] = target;
             if (a.d_loss) {
                 a.where[t] = before + at;
@@ -116,10 +129,20 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
         for (int k = warp; k < all; k += TAKE_THREADS / 32) {
             const T *src = reinterpret_cast<const T *>(a.x) + (int64_t)rows_at[k] * a.x_stride;
             T *dst = reinterpret_cast<T *>(a.xc) + (int64_t)(before + k) * a.dim;
+            float score = 0.f;
+            const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)targets[k] * a.w_stride;
             for (int64_t c = 8 * lane; c < a.dim; c += 256) {
-                Eight<T> e;
-                e.template load<true>(src + c, a.wide_x, 8);
-                e.store(dst + c, true, 8);
+                Eight<T> e, f;
+                load_any(e, src + c, a.wide_x);
+                *reinterpret_cast<uint4 *>(dst + c) = e.w[0];
+                if (a.d_loss) continue;
+                f.w[0] = __ldg(reinterpret_cast<const uint4 *>(w + c));
+#pragma unroll
+                for (int i = 0; i < 8; ++i) score = fmaf(e.get(i), f.get(i), score);
+            }
+            if (!a.d_loss) {
+                score = warp_sum(score);
+                if (lane == 0) a.row_score[before + k] = score;
             }
         }
         before += all;
@@ -132,7 +155,7 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
         const int64_t end = min((before + (int64_t)TM - 1) / TM * TM, a.padded);
         Eight<T> z;
         z.zero();
-        for (int64_t i = before * (a.dim / 8) + threadIdx.x; i < end * (a.dim / 8); i += TAKE_THREADS) z.store(reinterpret_cast<T *>(a.xc) + 8 * i, true, 8);
+        for (int64_t i = before * (a.dim / 8) + threadIdx.x; i < end * (a.dim / 8); i += TAKE_THREADS) *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.xc) + 8 * i) = z.w[0];
         for (int64_t i = before + threadIdx.x; i < end; i += TAKE_THREADS) {
             a.target[i] = -1;
             if (a.d_loss) a.row_lse[i] = 0.f, a.row_g[i] = 0.f;
@@ -317,7 +340,7 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
                 float top = -CUDART_INF_F, score = 0.f, total = 0.f;
 #pragma unroll
                 for (int c = 0; c < 128; ++c) top = fmaxf(top, sum[c]), score = c == at ? sum[c] : score;
-                if (at >= 0 && at < 128) a.row_score[m] = score;
+                if (at >= 0 && at < 128) a.row_rough[m] = score;
                 const float from = fabsf(top) == CUDART_INF_F ? 0.f : top;
 #pragma unroll
                 for (int c = 0; c < 128; ++c) total += exp2_fast((sum[c] - from) * LOG2E);
@@ -432,9 +455,13 @@ __global__ void __launch_bounds__(32 * JOIN_WAYS) join_scores(const __grid_const
     if (threadIdx.y == 0 && m < count) {
 #pragma unroll
         for (int k = 1; k < JOIN_WAYS; ++k) take(part[k][threadIdx.x]);
-        const float lse = (fabsf(top) == CUDART_INF_F ? 0.f : top) + logf(total);
+        float lse = (fabsf(top) == CUDART_INF_F ? 0.f : top) + logf(total);
+        // The tensor cores' sums come out small, the more so the larger they are, and the largest is often the target's.  Its share of lse
+        // is put right with the score that take_rows made, to first order; what the others are off is an average over many.
+        const float score = a.row_score[m], rough = a.row_rough[m], off = expf(rough - lse) * (score - rough);
+        if (fabsf(off) < 1e-2f) lse += off;  // finite, that is
         const int t = a.which[m];
-        a.lse[t] = lse, a.loss[t] = lse - a.row_score[m];
+        a.lse[t] = lse, a.loss[t] = lse - score;
     }
 }
 
@@ -444,25 +471,32 @@ template <typename T> __global__ void __launch_bounds__(256) join_states(const _
     const int64_t per_row = a.dim / 8, all = a.rows * per_row;
     const float ref = *a.g_ref * power2(-a.scale_log2);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
-        const int64_t t = q / per_row, c = (q - t * per_row) * 8;
+        const int64_t t = q / per_row;
+        const Columns<true> at(q - t * per_row, a.dim);
         const int m = a.where[t];
         float x[8] = {};
         if (m >= 0) {
             for (int s = 0; s < a.splits; ++s) {
                 Eight<float> e;
-                e.template load<true>(a.dxp + ((int64_t)s * a.padded + m) * a.dim + c, true, 8);
+                e.template load<true, true>(a.dxp + ((int64_t)s * a.padded + m) * a.dim, at);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] += e.get(i);
             }
             Eight<T> w;
-            w.template load<false>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride + c, true, 8);
+            w.template load<false, true>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride, at);
             const float rest = a.row_rest[m];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = ref * fmaf(rest, w.get(i), x[i]);
         }
         Eight<T> o;
         o.set(x);
-        o.store(reinterpret_cast<T *>(a.dx) + t * a.dx_stride + c, wide, 8);
+        T *const to = reinterpret_cast<T *>(a.dx) + t * a.dx_stride + at.c0;
+        if (wide) {
+            *reinterpret_cast<uint4 *>(to) = o.w[0];
+        } else {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = down<T>(x[i]);
+        }
     }
 }
 
@@ -471,7 +505,7 @@ constexpr uint64_t PIECE_BYTES = 512ull << 20, LEAST_PIECE = 8192;
 struct Layout {
     uint64_t padded, tiles, piece;
     int splits, per;
-    uint64_t count, g_ref, which, where, target, row_lse, row_g, row_rest, row_score, xc, part, gs, dxp, forward, backward;
+    uint64_t count, g_ref, which, where, target, row_lse, row_g, row_rest, row_score, row_rough, xc, part, gs, dxp, forward, backward;
 };
 Layout layout(uint64_t rows, uint64_t dim, uint64_t vocab) {
     Layout l = {};
@@ -497,7 +531,7 @@ Layout layout(uint64_t rows, uint64_t dim, uint64_t vocab) {
     l.which = take(l.padded * 4), l.target = take(l.padded * 4), l.row_score = take(l.padded * 4);
     l.xc = take(l.padded * dim * 2);
     const uint64_t common = at;
-    l.part = take(2 * l.tiles * l.padded * 8);
+    l.row_rough = take(l.padded * 4), l.part = take(2 * l.tiles * l.padded * 8);
     l.forward = at;
     at = common;
     l.where = take(rows * 4), l.row_lse = take(l.padded * 4), l.row_g = take(l.padded * 4), l.row_rest = take(l.padded * 4);
@@ -531,7 +565,7 @@ void place(Args *a, const Layout &l, void *workspace, bool backward) {
         a->where = (int32_t *)(ws + l.where), a->row_lse = (float *)(ws + l.row_lse), a->row_g = (float *)(ws + l.row_g);
         a->row_rest = (float *)(ws + l.row_rest), a->gs = ws + l.gs, a->dxp = (float *)(ws + l.dxp);
     } else {
-        a->part = (float2 *)(ws + l.part);
+        a->row_rough = (float *)(ws + l.row_rough), a->part = (float2 *)(ws + l.part);
     }
 }
 

@@ -7,6 +7,7 @@
 
 #include "scout_internal.h"
 #include "scout_step.h"
+#include "scout_tc.cuh"
 
 namespace scout {
 namespace step {
@@ -22,66 +23,94 @@ template <> __device__ __forceinline__ float down<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 down<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half down<__half>(float x) { return __float2half_rn(x); }
 
-// Eight elements of a row, as they lie in memory.  n: how many of them the row has (8 with wide: one or two 16-byte accesses).
+// Which eight columns of a row a thread has.  Rows on 16-byte boundaries, whose length is a multiple of eight (WIDE): thread k has columns
+// 8 k .. 8 k + 7, in one or two accesses.  Other rows: the threads of a warp have its 256 columns in turn, element i of lane l being
+// column l + 32 i, so that each access of the warp is one piece of memory.  A row's dropout is made in eights either way (keep8).
+template <bool WIDE> struct Columns {
+    int64_t c0, dim;
+    __device__ __forceinline__ Columns(int64_t k, int64_t dim_) : c0(WIDE ? 8 * k : 256 * (k >> 5) + (k & 31)), dim(dim_) {}
+    __device__ __forceinline__ int64_t col(int i) const { return c0 + (WIDE ? i : 32 * i); }
+    __device__ __forceinline__ bool has(int i) const { return (WIDE ? c0 : c0 + 32 * i) < dim; }
+    __device__ __forceinline__ bool any() const { return c0 < dim; }
+};
+
+// Eight elements of a row, as they lie in memory; zeros where the row ends.
 template <typename T> struct Eight {
     static constexpr int N = sizeof(T) / 2;
     uint4 w[N];
-    __device__ __forceinline__ float get(int i) const {
+    __device__ __forceinline__ tc::F2 pair(int i) const {  // elements 2 i and 2 i + 1
         const uint32_t *v = reinterpret_cast<const uint32_t *>(w);
         if constexpr (sizeof(T) == 4) {
-            return __uint_as_float(v[i]);
+            return tc::f2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
         } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-            return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
+            return tc::f2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xFFFF0000u));
         } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i >> 1]));
-            return i & 1 ? f.y : f.x;
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i]));
+            return tc::f2(f.x, f.y);
         }
+    }
+    __device__ __forceinline__ float get(int i) const {
+        const float2 f = tc::split(pair(i >> 1));
+        return i & 1 ? f.y : f.x;
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i] = make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
+    __device__ __forceinline__ void set_pair(int i, float lo, float hi) {
         uint32_t *v = reinterpret_cast<uint32_t *>(w);
         if constexpr (sizeof(T) == 4) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(x[i]);
+            v[2 * i] = __float_as_uint(lo), v[2 * i + 1] = __float_as_uint(hi);
         } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
-                v[i] = *reinterpret_cast<const uint32_t *>(&p);
-            }
+            const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
+            v[i] = *reinterpret_cast<const uint32_t *>(&p);
         } else {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const __half2 p = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
-                v[i] = *reinterpret_cast<const uint32_t *>(&p);
-            }
+            const __half2 p = __floats2half2_rn(lo, hi);
+            v[i] = *reinterpret_cast<const uint32_t *>(&p);
         }
     }
-    // STREAM: read once, or written and not read soon
-    template <bool STREAM> __device__ __forceinline__ void load(const T *p, bool wide, int n) {
-        if (wide && n == 8) {
+    __device__ __forceinline__ void set(const float (&x)[8]) {
 #pragma unroll
-            for (int i = 0; i < N; ++i) w[i] = STREAM ? __ldcs(reinterpret_cast<const uint4 *>(p) + i) : __ldg(reinterpret_cast<const uint4 *>(p) + i);
-        } else {
-            zero();
-            T *v = reinterpret_cast<T *>(w);
+        for (int i = 0; i < 4; ++i) set_pair(i, x[2 * i], x[2 * i + 1]);
+    }
+    __device__ __forceinline__ void set(const tc::F2 (&x)[4]) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (i < n) v[i] = p[i];
+        for (int i = 0; i < 4; ++i) {
+            const float2 f = tc::split(x[i]);
+            set_pair(i, f.x, f.y);
         }
     }
-    __device__ __forceinline__ void store(T *p, bool wide, int n) const {
-        if (wide && n == 8) {
+    // STREAM: read once
+    template <bool STREAM, bool WIDE> __device__ __forceinline__ void load(const T *row, const Columns<WIDE> &c) {
+        zero();
+        if constexpr (WIDE) {
+            if (c.any())
 #pragma unroll
-            for (int i = 0; i < N; ++i) reinterpret_cast<uint4 *>(p)[i] = w[i];
+                for (int i = 0; i < N; ++i)
+                    w[i] = STREAM ? __ldcs(reinterpret_cast<const uint4 *>(row + c.c0) + i) : __ldg(reinterpret_cast<const uint4 *>(row + c.c0) + i);
         } else {
-            const T *v = reinterpret_cast<const T *>(w);
+            uint32_t *v = reinterpret_cast<uint32_t *>(w);
 #pragma unroll
             for (int i = 0; i < 8; ++i)
-                if (i < n) p[i] = v[i];
+                if (c.has(i)) {
+                    if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(row[c.col(i)]);
+                    else v[i >> 1] |= (uint32_t) reinterpret_cast<const uint16_t *>(row)[c.col(i)] << (16 * (i & 1));
+                }
+        }
+    }
+    template <bool WIDE> __device__ __forceinline__ void store(T *row, const Columns<WIDE> &c) const {
+        if constexpr (WIDE) {
+            if (c.any())
+#pragma unroll
+                for (int i = 0; i < N; ++i) reinterpret_cast<uint4 *>(row + c.c0)[i] = w[i];
+        } else {
+            const uint32_t *v = reinterpret_cast<const uint32_t *>(w);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+                if (c.has(i)) {
+                    if constexpr (sizeof(T) == 4) row[c.col(i)] = __uint_as_float(v[i]);
+                    else reinterpret_cast<uint16_t *>(row)[c.col(i)] = (uint16_t)(v[i >> 1] >> (16 * (i & 1)));
+                }
         }
     }
 };
@@ -125,20 +154,32 @@ __device__ __forceinline__ uint4 philox(const Drop &d, uint32_t chunk, uint32_t 
     }
     return make_uint4(c0, c1, c2, c3);
 }
-// x times the factor where kept, else 0
-__device__ __forceinline__ void drop8(const Drop &d, const uint4 &bits, float (&x)[8]) {
-    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w};
+// Bit i: the thread's element i is kept.  k: the thread's number in its row, all threads of a warp in turn, and whole warps call this.
+// Where the lanes' elements are not the eights that share a counter, a lane makes its eight bits and the warp deals them out: lanes
+// 4 i .. 4 i + 3 hold the 32 places that element i of lanes 0 .. 31 are, in order.
+template <bool WIDE> __device__ __forceinline__ uint32_t keep8(const Drop &d, int64_t k, uint32_t row, uint64_t offset) {
+    const uint4 bits = philox(d, (uint32_t)k, row, offset);
+    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w}, cut = d.cut << 16;
+    uint32_t m = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        x[2 * i] = (w[i] & 0xFFFFu) >= d.cut ? x[2 * i] * d.factor : 0.f;
-        x[2 * i + 1] = (w[i] >> 16) >= d.cut ? x[2 * i + 1] * d.factor : 0.f;
+        m |= (w[i] << 16) >= cut ? 1u << (2 * i) : 0u;
+        m |= w[i] >= cut ? 2u << (2 * i) : 0u;
     }
+    if constexpr (WIDE) return m;
+    const uint32_t lane = threadIdx.x & 31;
+    uint32_t word = m << (8 * (lane & 3)), mine = 0;
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 1);
+    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) mine |= ((__shfl_sync(0xFFFFFFFFu, word, 4 * i) >> lane) & 1u) << i;
+    return mine;
 }
 
 // ---- host ------------------------------------------------------------------------------------------------
 inline bool known_float(uint32_t dtype) { return dtype == SCOUT_DT_F32 || dtype == SCOUT_DT_BF16 || dtype == SCOUT_DT_F16; }
 inline uint64_t size_of(uint32_t dtype) { return dtype == SCOUT_DT_F32 ? 4 : 2; }
-// rows of a matrix lie on 16-byte boundaries
+// rows of a matrix start on 16-byte boundaries
 inline bool wide_rows(const void *p, uint64_t stride, uint32_t dtype) {
     return ((reinterpret_cast<uintptr_t>(p) | stride * size_of(dtype)) & 15) == 0;
 }
