@@ -1,7 +1,7 @@
 // Dropout with a mask that is made again from a counter wherever it is needed.
 //
 // Bound by memory (an element in, an element out); the generator costs 40 instructions for eight elements.  A thread takes eight
-// columns of a row at a time, 64 bytes of them in flight.
+// columns of a row at a time, two such units in flight.
 #include <algorithm>
 
 #include "scout_step.cuh"
@@ -10,7 +10,8 @@ namespace scout {
 namespace step {
 namespace {
 
-constexpr int THREADS = 256, BLOCKS = 4;  // blocks of an SM
+constexpr int THREADS = 256;
+constexpr int blocks(bool wide) { return wide ? 6 : 4; }  // of an SM
 
 struct Args {
     const void *x;
@@ -22,30 +23,33 @@ struct Args {
     Drop drop;
 };
 
-template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, BLOCKS) dropout(const __grid_constant__ Args a) {
-    constexpr int UNROLL = sizeof(T) == 4 ? 2 : 4;
+template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, blocks(WIDE)) dropout(const __grid_constant__ Args a) {
+    constexpr int UNROLL = 2;
     const uint64_t offset = a.drop.at();
-    const uint32_t stride = gridDim.x * THREADS;
-    // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop
-    for (uint64_t q0 = (uint64_t)blockIdx.x * THREADS + threadIdx.x; q0 - (threadIdx.x & 31) < a.units; q0 += (uint64_t)stride * UNROLL) {
+    const uint32_t stride = gridDim.x * THREADS, lane = threadIdx.x & 31;
+    const tc::F2 factor = tc::f2(a.drop.factor, a.drop.factor);
+    // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop.
+    // Units are counted to 2^31, so that the sums here stay below 2^32.
+    for (uint32_t q0 = blockIdx.x * THREADS + threadIdx.x; q0 - lane < a.units; q0 += stride * UNROLL) {
         Eight<T> e[UNROLL];
         uint32_t row[UNROLL], k[UNROLL];
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const uint64_t q = q0 + (uint64_t)u * stride;
-            row[u] = (__umulhi((uint32_t)q, a.mul) + (uint32_t)q) >> a.shift;
-            k[u] = (uint32_t)q - row[u] * a.per_row;
+            const uint32_t q = q0 + u * stride;
+            row[u] = (__umulhi(q, a.mul) + q) >> a.shift;
+            k[u] = q - row[u] * a.per_row;
+            e[u].zero();
             if (q < a.units) e[u].template load<true, WIDE>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride, Columns<WIDE>(k[u], a.cols));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
-            const uint64_t q = q0 + (uint64_t)u * stride;
-            if (q - (threadIdx.x & 31) >= a.units) break;
-            const uint32_t keep = keep8<WIDE>(a.drop, k[u], a.row0 + row[u], offset);
+            const uint32_t q = q0 + u * stride;
+            if (q - lane >= a.units) break;
+            const Keep<WIDE> keep(a.drop, k[u], a.row0 + row[u], offset);
             if (q >= a.units) continue;
-            float x[8];
+            tc::F2 x[4];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = (keep >> i) & 1 ? e[u].get(i) * a.drop.factor : 0.f;
+            for (int i = 0; i < 4; ++i) x[i] = keep.of(i, tc::mul2(e[u].pair(i), factor));
             e[u].set(x);
             e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.cols));
         }
@@ -61,7 +65,7 @@ template <typename T> int run(Args a, uint64_t rows, cudaStream_t stream) {
     for (uint64_t r = 0; r < rows; r += most) {
         const uint64_t n = std::min(most, rows - r), units = n * per_row;
         a.row0 = (uint32_t)r, a.units = (uint32_t)units;
-        const unsigned grid = (unsigned)std::min<uint64_t>((units + THREADS - 1) / THREADS, SMS * BLOCKS);
+        const unsigned grid = (unsigned)std::min<uint64_t>((units + THREADS - 1) / THREADS, SMS * blocks(a.wide));
         (a.wide ? dropout<T, true> : dropout<T, false>)<<<grid, THREADS, 0, stream>>>(a);
         SCOUT_CUDA(cudaGetLastError());
         a.x = reinterpret_cast<const T *>(a.x) + n * a.x_stride, a.y = reinterpret_cast<T *>(a.y) + n * a.y_stride;

@@ -1,13 +1,14 @@
 // Token embedding: rows of a table, and the table's gradient by sorted tokens.
 //
 // Forward is a copy of rows, bound by memory.  Backward: every token's gradient goes to its id's row, and the places of an id are
-// added in their order, whatever ran first.  Three launches:
+// added in their order, whatever ran first:
+//   mark_ids     which ids occur (not where the gradient is added to one that is there)
 //   sort_ids     one cluster of eight blocks sorts (id, place) by id, places of an id staying in order (radix sort from the
-//                lowest digit, up to nine bits a pass), and marks the ids that occur;
+//                lowest digit, up to nine bits a pass); the other blocks write zeros to rows of ids that do not occur
 //   sum_places   the sorted places in pieces of PIECE: a thread adds up eight columns of a piece, writes what begins and ends
-//                inside, and leaves what crosses a border in scratch; other blocks write zeros to rows of ids that do not occur;
-//   join_pieces  adds the parts of an id that crosses borders, in order.
-// Pieces of equal size keep one frequent id (padding, a line break) from holding up the rest.
+//                inside, and leaves what crosses a border in scratch
+//   join_pieces  adds the parts of an id that crosses borders, in order
+// Pieces of equal size keep one frequent id (a line break, say) from holding up the rest.
 #include <algorithm>
 #include <cmath>
 
@@ -86,9 +87,10 @@ template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaS
 }
 
 // ---- backward -----------------------------------------------------------------------------------------
-constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT;
-constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4;
-constexpr int PIECE = 32, AHEAD = 8, SUM_THREADS = 128, FILL_BYTES = 1 << 16;
+constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT, HELD = 4;
+constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4, FILL_CLUSTERS = SMS / CLUSTER - 1;
+constexpr int MARKED = 1 << 20, MARK_SMEM = MARKED / 8;  // ids of a block of mark_ids
+constexpr int PIECE = 32, AHEAD = 8, SUM_THREADS = 128;
 constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
 
 struct Grad {
@@ -96,34 +98,88 @@ struct Grad {
     void *table;
     uint32_t *key[2], *place[2];  // [rows] each: sorted by the digits so far, passes alternate
     uint32_t *seen;               // a bit for every id
+    uint2 *across_list;           // [pieces]: the piece that an id begins in and a later one that it ends in
+    uint32_t *across_count;
     float *part;                  // [pieces][2][dim]: what goes on from the piece before, and what goes on into the next one
     int64_t dy_stride, table_stride, rows, dim;
     uint32_t vocab, pieces, across;  // blocks of columns
-    uint32_t fill_rows;              // rows of a block that writes zeros
     int digit, passes, id64, wide, accumulate;
     float scale;
 };
 
-__global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
+// The ids that occur, as bits: a block takes MARKED ids and looks at all places.
+__global__ void __launch_bounds__(SORT_THREADS) mark_ids(const __grid_constant__ Grad a) {
+    pdl_launch_dependents();
     extern __shared__ uint32_t smem[];
+    const uint32_t first = blockIdx.x * MARKED, ids = min((uint32_t)MARKED, a.vocab - first), words = (ids + 31) / 32;
+    for (uint32_t w = threadIdx.x; w < words; w += SORT_THREADS) smem[w] = 0;
+    __syncthreads();
+#pragma unroll 8
+    for (int64_t t = threadIdx.x; t < a.rows; t += SORT_THREADS) {
+        const uint32_t id = id_at(a.ids, a.id64, t, a.vocab) - first;  // `vocab` and ids before wrap or stay outside
+        if (id < ids) atomicOr(&smem[id >> 5], 1u << (id & 31));
+    }
+    __syncthreads();
+    for (uint32_t w = threadIdx.x; w < words; w += SORT_THREADS) a.seen[first / 32 + w] = smem[w];
+}
+
+// zeros to a row by a warp, whatever it starts on: whole 16 bytes, and the elements before and behind them
+template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_t dim) {
+    constexpr int N = 16 / sizeof(TO);
+    const int lane = threadIdx.x & 31;
+    const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int64_t)sizeof(TO), dim), body = (dim - head) / N;
+    if (lane < head) row[lane] = down<TO>(0.f);
+    uint4 *const wide = reinterpret_cast<uint4 *>(row + head);
+#pragma unroll 4
+    for (int64_t i = lane; i < body; i += 32) wide[i] = make_uint4(0, 0, 0, 0);
+    if (head + body * N + lane < dim) row[head + body * N + lane] = down<TO>(0.f);
+}
+
+// Sorts (the first cluster), and meanwhile writes zeros to rows of ids that do not occur (the others).
+template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
+    extern __shared__ uint32_t smem[];
+    if (blockIdx.x >= CLUSTER) {
+        pdl_wait();  // the marks; what the sorting blocks read and write has nothing to do with them
+        const int64_t stride = (int64_t)(gridDim.x - CLUSTER) * SORT_WARPS;
+        for (int64_t v = (int64_t)(blockIdx.x - CLUSTER) * SORT_WARPS + (threadIdx.x >> 5); v < a.vocab; v += stride)
+            if (!((a.seen[v >> 5] >> (v & 31)) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + v * a.table_stride, a.dim);
+        return;
+    }
     uint32_t *const hist = smem, *const total = smem + SORT_WARPS * MAX_BINS, *const scan = total + MAX_BINS;  // [warp][bin], [bin], [bin]
     __shared__ uint32_t warp_total[SORT_WARPS];
     cg::cluster_group cluster = cg::this_cluster();
     const uint32_t rank = cluster.block_rank(), warp = threadIdx.x >> 5, lane = threadIdx.x & 31, bins = 1u << a.digit;
-    for (uint32_t w = rank * SORT_THREADS + threadIdx.x; w < (a.vocab + 31) / 32; w += CLUSTER * SORT_THREADS) a.seen[w] = 0;
-    // a warp's run of places: whole warps' widths
+    if (rank == 0 && threadIdx.x == 0) *a.across_count = 0;
+    // a warp's run of places, in pieces of HELD each lane
     const int64_t run = (a.rows + CLUSTER * SORT_WARPS * 32 - 1) / (CLUSTER * SORT_WARPS * 32) * 32;
     const int64_t begin = min((int64_t)(rank * SORT_WARPS + warp) * run, a.rows), end = min(begin + run, a.rows);
+    const bool held = run <= 32 * HELD;  // the whole run stays in registers between the two looks at it
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * a.digit, from = (pass + 1) & 1, to = pass & 1;
-        const auto key_of = [&](int64_t t) { return pass == 0 ? id_at(a.ids, a.id64, t, a.vocab) : a.key[from][t]; };
+        uint32_t key[HELD], place[HELD];
+        const auto read = [&](int64_t t0) {
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                const int64_t t = t0 + 32 * h + lane;
+                if (t >= end) continue;
+                key[h] = pass == 0 ? id_at(a.ids, a.id64, t, a.vocab) : a.key[from][t];
+                place[h] = pass == 0 ? (uint32_t)t : a.place[from][t];
+            }
+        };
+        if (held) read(begin);
         for (uint32_t i = threadIdx.x; i < SORT_WARPS * bins; i += SORT_THREADS) hist[i] = 0;
         __syncthreads();
-        for (int64_t t = begin + lane; t < end; t += 32) atomicAdd(&hist[warp * bins + ((key_of(t) >> shift) & (bins - 1))], 1u);
+        for (int64_t t0 = begin; t0 < end; t0 += 32 * HELD) {
+            if (!held) read(t0);
+#pragma unroll
+            for (int h = 0; h < HELD; ++h)
+                if (t0 + 32 * h + lane < end) atomicAdd(&hist[warp * bins + ((key[h] >> shift) & (bins - 1))], 1u);
+        }
         __syncthreads();
         // counts become places: warps before within the block, then blocks before, then smaller digits
         if (threadIdx.x < bins) {
             uint32_t sum = 0;
+#pragma unroll 8
             for (int w = 0; w < SORT_WARPS; ++w) {
                 const uint32_t n = hist[w * bins + threadIdx.x];
                 hist[w * bins + threadIdx.x] = sum;
@@ -153,22 +209,41 @@ __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) 
             scan[threadIdx.x] = sum - all + before;
         }
         __syncthreads();
-        for (int64_t t0 = begin; t0 < end; t0 += 32) {  // the same for a warp
-            const int64_t t = t0 + lane;
-            const bool on = t < end;
-            const uint32_t key = on ? key_of(t) : 0, digit = on ? (key >> shift) & (bins - 1) : bins;
-            const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
-            if (on) {
-                const uint32_t at = scan[digit] + hist[warp * bins + digit] + __popc(same & ((1u << lane) - 1));
-                a.key[to][at] = key;
-                a.place[to][at] = pass == 0 ? (uint32_t)t : a.place[from][t];
-                if (pass == a.passes - 1 && key < a.vocab) atomicOr(&a.seen[key >> 5], 1u << (key & 31));
+        for (int64_t t0 = begin; t0 < end; t0 += 32 * HELD) {  // the same for a warp
+            if (!held) read(t0);
+#pragma unroll
+            for (int h = 0; h < HELD; ++h) {
+                if (t0 + 32 * h >= end) break;
+                const bool on = t0 + 32 * h + lane < end;
+                const uint32_t digit = on ? (key[h] >> shift) & (bins - 1) : bins;
+                const uint32_t same = __match_any_sync(0xFFFFFFFFu, digit);
+                if (on) {
+                    const uint32_t at = scan[digit] + hist[warp * bins + digit] + __popc(same & ((1u << lane) - 1));
+                    a.key[to][at] = key[h], a.place[to][at] = place[h];
+                }
+                __syncwarp();
+                if (on && (same >> lane) == 1u) hist[warp * bins + digit] += __popc(same);  // the last of them
+                __syncwarp();
             }
-            __syncwarp();
-            if (on && (same >> lane) == 1u) hist[warp * bins + digit] += __popc(same);  // the last of them
-            __syncwarp();
         }
         cluster.sync();  // what the others wrote is read next; nobody's `total` is read any more
+    }
+    // ids that begin in one piece and go on into the next; the order of the list says nothing
+    const uint32_t *const keys = a.key[(a.passes + 1) & 1];
+    for (int64_t piece = rank * SORT_THREADS + threadIdx.x; piece + 1 < a.pieces; piece += CLUSTER * SORT_THREADS) {
+        const int64_t after = (piece + 1) * PIECE;
+        const uint32_t id = keys[after - 1];
+        if (id >= a.vocab || keys[after] != id || (piece > 0 && keys[piece * PIECE - 1] == id)) continue;
+        // the last piece whose first key is still this one: lo's is, hi's is not
+        int64_t lo = piece + 1, hi = lo + 1;
+        for (; hi < a.pieces && keys[hi * PIECE] == id; hi = lo + 2 * (hi - piece)) lo = hi;
+        hi = min(hi, (int64_t)a.pieces);
+        while (hi - lo > 1) {
+            const int64_t mid = (lo + hi) / 2;
+            if (keys[mid * PIECE] == id) lo = mid;
+            else hi = mid;
+        }
+        a.across_list[atomicAdd(a.across_count, 1u)] = make_uint2((uint32_t)piece, (uint32_t)lo);
     }
 }
 
@@ -177,6 +252,7 @@ template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad
     TO *row = reinterpret_cast<TO *>(a.table) + (int64_t)id * a.table_stride;
     Eight<TO> e;
     float x[8];
+    e.zero();
     if (a.accumulate) e.template load<true, WIDE>(row, c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = a.accumulate ? fmaf(a.scale, sum[i], e.get(i)) : a.scale * sum[i];
@@ -184,26 +260,9 @@ template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad
     e.store(row, c);
 }
 
-// zeros to a row, whatever it starts on: whole 16 bytes, and the elements before and behind them
-template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_t dim) {
-    constexpr int N = 16 / sizeof(TO);
-    const int64_t head = min((int64_t)((16 - (reinterpret_cast<uintptr_t>(row) & 15)) & 15) / (int64_t)sizeof(TO), dim), body = (dim - head) / N;
-    if (threadIdx.x < head) row[threadIdx.x] = down<TO>(0.f);
-    uint4 *const wide = reinterpret_cast<uint4 *>(row + head);
-    for (int64_t i = threadIdx.x; i < body; i += SUM_THREADS) wide[i] = make_uint4(0, 0, 0, 0);
-    if (head + body * N + threadIdx.x < dim) row[head + body * N + threadIdx.x] = down<TO>(0.f);
-}
-
 template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
     pdl_wait();
     const uint32_t *const keys = a.key[(a.passes + 1) & 1], *const places = a.place[(a.passes + 1) & 1];
-    const uint64_t sums = (uint64_t)a.pieces * a.across;
-    if (blockIdx.x >= sums) {  // zeros
-        const int64_t v0 = (int64_t)(blockIdx.x - sums) * a.fill_rows, v1 = min(v0 + a.fill_rows, (int64_t)a.vocab);
-        for (int64_t v = v0; v < v1; ++v)
-            if (!((a.seen[v >> 5] >> (v & 31)) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + v * a.table_stride, a.dim);
-        return;
-    }
     __shared__ uint32_t key[PIECE + 2], place[PIECE];
     const uint32_t piece = blockIdx.x / a.across;
     const int64_t p0 = (int64_t)piece * PIECE;
@@ -248,76 +307,63 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
     }
 }
 
-// Ids that begin in one piece and go on into the next.  A block looks at JOIN_THREADS pieces at once (every gridDim.y-th) and then
-// takes those that such an id begins in, one after the other: eight warps take every eighth part each, a lane four columns.
+// The parts of an id that crosses borders: eight warps take every eighth part each, a lane four columns.
 template <typename TO> __global__ void __launch_bounds__(JOIN_THREADS) join_pieces(const __grid_constant__ Grad a) {
     pdl_wait();
     __shared__ float part[JOIN_WAYS][JOIN_COLS];
-    __shared__ uint32_t found[JOIN_THREADS], counts[JOIN_WAYS];
-    const uint32_t *const keys = a.key[(a.passes + 1) & 1];
     const int lane = threadIdx.x & 31, way = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * JOIN_COLS + lane;
-    for (int64_t first = blockIdx.y; first + 1 < a.pieces; first += (int64_t)gridDim.y * JOIN_THREADS) {
-        const int64_t mine = first + (int64_t)gridDim.y * threadIdx.x, after = mine * PIECE + PIECE;
-        bool begins = false;
-        if (mine + 1 < a.pieces) {
-            const uint32_t key = keys[after - 1];
-            begins = key < a.vocab && keys[after] == key && (mine == 0 || keys[mine * PIECE - 1] != key);
-        }
-        const uint32_t who = __ballot_sync(0xFFFFFFFFu, begins);
-        __syncthreads();
-        if (lane == 0) counts[way] = __popc(who);
-        __syncthreads();
-        int at = 0, all = 0;
-#pragma unroll
-        for (int w = 0; w < JOIN_WAYS; ++w) at += w < way ? counts[w] : 0, all += counts[w];
-        if (begins) found[at + __popc(who & ((1u << lane) - 1))] = (uint32_t)mine;
-        __syncthreads();
-        for (int k = 0; k < all; ++k) {
-            const int64_t piece = found[k];
-            const uint32_t key = keys[piece * PIECE + PIECE - 1];
-            int64_t end = piece + 1;  // the piece that it ends in: the last whose first key is still this one
-            for (;; end += 32) {      // the same for every warp
-                const int64_t next = end + 1 + lane;
-                const uint32_t go = __ballot_sync(0xFFFFFFFFu, next < a.pieces && keys[next * PIECE] == key);
-                if (go != 0xFFFFFFFFu) {
-                    end += __ffs(~go) - 1;
-                    break;
-                }
-            }
-            float sum[4] = {};
+    const int64_t first = (int64_t)blockIdx.x * JOIN_COLS, col = first + lane;
+    const uint32_t count = *a.across_count;
+    for (uint32_t k = blockIdx.y; k < count; k += gridDim.y) {
+        const uint2 range = a.across_list[k];
+        const uint32_t key = a.key[(a.passes + 1) & 1][(int64_t)range.x * PIECE + PIECE - 1];
+        float sum[4] = {};
 #pragma unroll 2
-            for (int64_t p = piece + way; p <= end; p += JOIN_WAYS)
+        for (int64_t p = range.x + way; p <= range.y; p += JOIN_WAYS)
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (col + 32 * i < a.dim) sum[i] += a.part[(p * 2 + (p == piece)) * a.dim + col + 32 * i];
-            __syncthreads();
+            for (int i = 0; i < 4; ++i)
+                if (col + 32 * i < a.dim) sum[i] += a.part[(p * 2 + (p == range.x)) * a.dim + col + 32 * i];
+        __syncthreads();
 #pragma unroll
-            for (int i = 0; i < 4; ++i) part[way][lane + 32 * i] = sum[i];
-            __syncthreads();
-            const int64_t c = (int64_t)blockIdx.x * JOIN_COLS + threadIdx.x;
-            if (threadIdx.x < JOIN_COLS && c < a.dim) {
-                float s = part[0][threadIdx.x];
+        for (int i = 0; i < 4; ++i) part[way][lane + 32 * i] = sum[i];
+        __syncthreads();
+        const int64_t c = first + threadIdx.x;
+        if (threadIdx.x < JOIN_COLS && c < a.dim) {
+            float s = part[0][threadIdx.x];
 #pragma unroll
-                for (int w = 1; w < JOIN_WAYS; ++w) s += part[w][threadIdx.x];
-                TO *p = reinterpret_cast<TO *>(a.table) + (int64_t)key * a.table_stride + c;
-                *p = down<TO>(a.accumulate ? fmaf(a.scale, s, up<TO>(*p)) : a.scale * s);
-            }
+            for (int w = 1; w < JOIN_WAYS; ++w) s += part[w][threadIdx.x];
+            TO *p = reinterpret_cast<TO *>(a.table) + (int64_t)key * a.table_stride + c;
+            *p = down<TO>(a.accumulate ? fmaf(a.scale, s, up<TO>(*p)) : a.scale * s);
         }
     }
 }
 
 template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream) {
-    if (int rc = allow_smem<sort_ids>(SORT_SMEM)) return rc;
-    sort_ids<<<CLUSTER, SORT_THREADS, SORT_SMEM, stream>>>(a);
-    SCOUT_CUDA(cudaGetLastError());
-    a.fill_rows = (uint32_t)std::max<uint64_t>(1, FILL_BYTES / (a.dim * sizeof(TO)));
-    const uint64_t fill = a.accumulate ? 0 : (a.vocab + a.fill_rows - 1) / a.fill_rows, grid = (uint64_t)a.pieces * a.across + fill;
+    if (int rc = allow_smem<mark_ids>(MARK_SMEM)) return rc;
+    if (int rc = allow_smem<sort_ids<TO>>(SORT_SMEM)) return rc;
+    const uint64_t grid = (uint64_t)a.pieces * a.across;
     if (grid > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
+    if (!a.accumulate) {
+        mark_ids<<<(a.vocab + MARKED - 1) / MARKED, SORT_THREADS, (std::min<uint32_t>(a.vocab, MARKED) + 31) / 32 * 4, stream>>>(a);
+        SCOUT_CUDA(cudaGetLastError());
+    }
+    // as many clusters as rows without a token can need, a row to a warp
+    const uint32_t fill = a.accumulate ? 0 : std::min<uint32_t>(FILL_CLUSTERS, (a.vocab + CLUSTER * SORT_WARPS - 1) / (CLUSTER * SORT_WARPS));
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CLUSTER * (1 + fill));
+    cfg.blockDim = dim3(SORT_THREADS);
+    cfg.dynamicSmemBytes = SORT_SMEM;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = a.accumulate ? 0 : 1;
+    SCOUT_CUDA(cudaLaunchKernelEx(&cfg, sort_ids<TO>, a));
     if (grid) SCOUT_CUDA(launch_dependent(a.wide ? sum_places<T, TO, true> : sum_places<T, TO, false>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
     if (a.pieces > 1) {
         const uint32_t wide = (uint32_t)((a.dim + JOIN_COLS - 1) / JOIN_COLS);
-        const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 4 * SMS / wide)));
+        const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 8 * SMS / wide)));
         SCOUT_CUDA(launch_dependent(join_pieces<TO>, jg, dim3(JOIN_THREADS), stream, a));
     }
     return SCOUT_OK;
@@ -331,14 +377,14 @@ int check(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, 
 }
 
 struct Scratch {
-    uint64_t key[2], place[2], seen, part, bytes;
+    uint64_t key[2], place[2], seen, list, count, part, bytes;
 };
 Scratch scratch(uint64_t rows, uint64_t dim, uint64_t vocab) {
     const auto up = [](uint64_t n) { return (n + 255) & ~255ull; };
     Scratch s = {};
     const uint64_t each = up(rows * 4);
     s.key[0] = 0, s.key[1] = each, s.place[0] = 2 * each, s.place[1] = 3 * each, s.seen = 4 * each;
-    s.part = s.seen + up((vocab + 31) / 32 * 4);
+    s.list = s.seen + up((vocab + 31) / 32 * 4), s.count = s.list + up((rows + PIECE - 1) / PIECE * 8), s.part = s.count + 256;
     s.bytes = s.part + up((rows + PIECE - 1) / PIECE * 2 * dim * 4);
     return s;
 }
@@ -398,7 +444,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     uint8_t *const ws = (uint8_t *)workspace;
     a.ids = ids, a.dy = dy, a.table = d_table;
     for (int i = 0; i < 2; ++i) a.key[i] = (uint32_t *)(ws + need.key[i]), a.place[i] = (uint32_t *)(ws + need.place[i]);
-    a.seen = (uint32_t *)(ws + need.seen), a.part = (float *)(ws + need.part);
+    a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.part = (float *)(ws + need.part);
     a.dy_stride = (int64_t)dy_stride, a.table_stride = (int64_t)d_table_stride, a.rows = (int64_t)rows, a.dim = (int64_t)dim;
     a.vocab = (uint32_t)vocab, a.pieces = (uint32_t)((rows + PIECE - 1) / PIECE), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
     int bits = 1;

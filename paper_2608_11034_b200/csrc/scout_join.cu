@@ -52,18 +52,17 @@ template <typename TW, bool WIDE> __device__ __forceinline__ void weights(tc::F2
         return;
     }
     Eight<TW> e;
+    e.zero();
     e.template load<false, WIDE>(reinterpret_cast<const TW *>(row), c);
 #pragma unroll
     for (int i = 0; i < 4; ++i) w[i] = e.pair(i);
 }
-template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, int64_t row) {
-    return a.gate ? reinterpret_cast<const TW *>(a.gate) + row / a.group_rows * a.dim : nullptr;
+template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, uint32_t group) {
+    return a.gate ? reinterpret_cast<const TW *>(a.gate) + (int64_t)group * a.dim : nullptr;
 }
+// rows are below 2^32, and group_rows is that many only in one group
+__device__ __forceinline__ uint32_t group_of(const Args &a, int64_t row) { return a.group_rows == a.rows ? 0 : (uint32_t)row / (uint32_t)a.group_rows; }
 __device__ __forceinline__ tc::F2 both(float x) { return tc::f2(x, x); }
-// pair i of what is kept: the factor where it is, else 0
-__device__ __forceinline__ tc::F2 kept(uint32_t keep, int i, float factor) {
-    return tc::f2((keep >> (2 * i)) & 1 ? factor : 0.f, (keep >> (2 * i + 1)) & 1 ? factor : 0.f);
-}
 __device__ __forceinline__ float add_pairs(const tc::F2 &x) {
     const float2 f = tc::split(x);
     return f.x + f.y;
@@ -86,13 +85,15 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Columns<WIDE> c(t + v * a.team, a.dim);
-                const int64_t at = from + r * stride;
-                eb[r][v].zero(), ex[r][v].zero();
-                if (at >= a.rows) continue;
+                const int64_t at = min(from + r * stride, a.rows - 1);  // past the end the last row again, for nothing
                 eb[r][v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + at * a.b_stride, c);
                 if (a.x) ex[r][v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.x) + at * a.x_stride, c);
             }
     };
+#pragma unroll
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[r][v].zero(), x[r][v].zero(), b_next[r][v].zero(), x_next[r][v].zero();
     fetch(b, x, row);
     for (; row - team < a.rows; row += R * stride) {  // the same for all teams of a block
         if constexpr (AHEAD) fetch(b_next, x_next, row + R * stride);
@@ -131,16 +132,13 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
             for (int r = 0; r < R; ++r) {
                 const int64_t at = row + r * stride;
                 if (a.drop.cut) {
-                    const uint32_t keep = keep8<WIDE>(a.drop, t + v * a.team, (uint32_t)at, offset);
+                    const Keep<WIDE> keep(a.drop, t + v * a.team, (uint32_t)at, offset);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {  // what is dropped is 0, whatever it was
-                        const float2 f = tc::split(u[r][v][i]);
-                        u[r][v][i] = tc::f2((keep >> (2 * i)) & 1 ? f.x * a.drop.factor : 0.f, (keep >> (2 * i + 1)) & 1 ? f.y * a.drop.factor : 0.f);
-                    }
+                    for (int i = 0; i < 4; ++i) u[r][v][i] = keep.of(i, tc::mul2(u[r][v][i], both(a.drop.factor)));
                 }
                 if (at >= a.rows) continue;
                 tc::F2 w[4];
-                weights<TW, WIDE>(w, gate_row<TW>(a, at), c);
+                weights<TW, WIDE>(w, gate_row<TW>(a, group_of(a, at)), c);
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
                     u[r][v][i] = tc::fma2(tc::mul2(both(a.scale), w[i]), u[r][v][i], x[r][v].pair(i));
@@ -231,13 +229,16 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
         Eight<TB> n[V], b[V];
         float rb, ry;
     } cur, next;
-    const auto fetch = [&](Row &e, int64_t row) {
+    const auto clear = [&](Row &e) {
+#pragma unroll
+        for (int v = 0; v < V; ++v) e.y[v].zero(), e.g[v].zero(), e.n[v].zero(), e.b[v].zero();
         e.rb = 1.f, e.ry = 0.f;
+    };
+    const auto fetch = [&](Row &e, int64_t at) {
+        const int64_t row = min(at, a.rows - 1);  // past the end the last row again, for nothing
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Columns<WIDE> c(t + v * a.team, a.dim);
-            e.y[v].zero(), e.g[v].zero(), e.n[v].zero(), e.b[v].zero();
-            if (row >= last) continue;
             if (a.dn) {
                 e.y[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.yin) + row * a.y_stride, c);
                 e.n[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.dn) + row * a.dn_stride, c);
@@ -245,16 +246,18 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
             if (a.dy) e.g[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.dy) + row * a.dy_stride, c);
             e.b[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + row * a.b_stride, c);
         }
-        if (row >= last) return;
         if (a.post) e.rb = a.stats_in[row];
         if (a.dn) e.ry = a.stats_in[a.rows + row];
     };
+    uint32_t group = group_of(a, min(first, a.rows - 1));
+    int64_t group_end = (group + 1ll) * a.group_rows;
+    clear(cur), clear(next);
     int64_t begun = first;  // where the gate's current sum began
     fetch(cur, first);
     for (int64_t it = 0; it < a.per; ++it) {
         const int64_t row = first + it;
         const bool on = row < last;
-        if constexpr (AHEAD) fetch(next, row + 1 < first + a.per ? row + 1 : last);
+        if constexpr (AHEAD) fetch(next, row + 1);
         const float rb = cur.rb, ry = cur.ry;
         tc::F2 g[V][4];
         float dot[1] = {0.f};
@@ -268,7 +271,7 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
                 for (int i = 0; i < 4; ++i) {
                     const tc::F2 z = tc::mul2(cur.y[v].pair(i), both(ry)), dn = cur.n[v].pair(i);
                     g[v][i] = tc::mul2(dn, w[i]);
-                    acc.add(2, v, i, dn, z);
+                    if (on) acc.add(2, v, i, dn, z);
                     d = tc::fma2(g[v][i], z, d);
                 }
             }
@@ -289,19 +292,17 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
             }
             tc::F2 w[4], gw[4];
             weights<TW, WIDE>(w, a.post, c);
-            weights<TW, WIDE>(gw, on ? gate_row<TW>(a, row) : nullptr, c);
-            const uint32_t keep = a.drop.cut ? keep8<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset) : 0xFFu;
-            const float factor = a.scale * (a.drop.cut ? a.drop.factor : 1.f);
+            weights<TW, WIDE>(gw, gate_row<TW>(a, group), c);
+            Keep<WIDE> keep;
+            if (a.drop.cut) keep = Keep<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset);
+            else keep.all();
+            const tc::F2 factor = both(a.scale * (a.drop.cut ? a.drop.factor : 1.f));
+            if (!on) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const tc::F2 cb = tc::mul2(cur.b[v].pair(i), both(rb)), m = kept(keep, i, factor);
-                tc::F2 u = tc::mul2(cb, w[i]);
-                const tc::F2 h = tc::mul2(g[v][i], m);  // scale g, masked
-                if (a.drop.cut) {                      // what was dropped is 0, whatever it was
-                    const float2 f = tc::split(u);
-                    u = tc::f2((keep >> (2 * i)) & 1 ? f.x : 0.f, (keep >> (2 * i + 1)) & 1 ? f.y : 0.f);
-                }
-                acc.add(0, v, i, u, h);
+                // what was dropped is 0 in both, whatever it was
+                const tc::F2 cb = keep.of(i, tc::mul2(cur.b[v].pair(i), both(rb))), h = keep.of(i, tc::mul2(g[v][i], factor));
+                acc.add(0, v, i, tc::mul2(cb, w[i]), h);
                 const tc::F2 du = tc::mul2(h, gw[i]);
                 acc.add(1, v, i, du, cb);
                 g[v][i] = tc::mul2(du, w[i]);
@@ -324,9 +325,8 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
         }
         if (!(a.post && a.dn) && a.team > 32) __syncthreads();
         // the gate's sum ends with its group or with the run
-        if (a.d_gate && on && (row + 1 == last || (row + 1) % a.group_rows == 0)) {
-            const int64_t group = row / a.group_rows;
-            const bool whole = begun == group * a.group_rows && row + 1 == begun + a.group_rows;
+        if (on && (row + 1 == last || row + 1 == group_end)) {
+            const bool whole = begun + a.group_rows == group_end && row + 1 == group_end;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Columns<WIDE> c(t + v * a.team, a.dim);
@@ -334,17 +334,19 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
                 for (int i = 0; i < 8; ++i) {
                     const float2 f = tc::split(acc.get(0, v, i >> 1));
                     const float x = i & 1 ? f.y : f.x;
-                    if (!c.has(i)) continue;
-                    if (whole) reinterpret_cast<TW *>(a.d_gate)[group * a.dim + c.col(i)] = down<TW>(x);
+                    if (!a.d_gate || !c.has(i)) continue;
+                    if (whole) reinterpret_cast<TW *>(a.d_gate)[(int64_t)group * a.dim + c.col(i)] = down<TW>(x);
                     else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = x;
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc.set(0, v, i, both(0.f));
             }
             begun = row + 1;
+            if (begun == group_end) ++group, group_end += a.group_rows;
+            if (begun == a.rows) group = 0;  // for nothing, but inside
         }
         if constexpr (AHEAD) cur = next;
-        else fetch(cur, it + 1 < a.per ? row + 1 : last);
+        else fetch(cur, row + 1);
     }
     if (first < last) {
 #pragma unroll

@@ -59,7 +59,7 @@ struct Args {
 };
 
 // ---- rows that count ----------------------------------------------------------------------------------
-constexpr int TAKE_THREADS = 256;
+constexpr int TAKE_THREADS = 256, TAKE_AHEAD = 4;
 __device__ __forceinline__ int target_at(const Args &a, int64_t t) {
     const int64_t v = a.id64 ? reinterpret_cast<const int64_t *>(a.targets)[t] : (int64_t) reinterpret_cast<const int32_t *>(a.targets)[t];
     return v >= 0 && v < a.vocab ? (int)v : -1;
@@ -131,14 +131,23 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
             T *dst = reinterpret_cast<T *>(a.xc) + (int64_t)(before + k) * a.dim;
             float score = 0.f;
             const T *w = reinterpret_cast<const T *>(a.w) + (int64_t)targets[k] * a.w_stride;
-            for (int64_t c = 8 * lane; c < a.dim; c += 256) {
-                Eight<T> e, f;
-                load_any(e, src + c, a.wide_x);
-                *reinterpret_cast<uint4 *>(dst + c) = e.w[0];
-                if (a.d_loss) continue;
-                f.w[0] = __ldg(reinterpret_cast<const uint4 *>(w + c));
+            for (int64_t c0 = 8 * lane; c0 < a.dim; c0 += 256 * TAKE_AHEAD) {
+                Eight<T> e[TAKE_AHEAD], f[TAKE_AHEAD];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) score = fmaf(e.get(i), f.get(i), score);
+                for (int u = 0; u < TAKE_AHEAD; ++u) {
+                    const int64_t c = c0 + 256 * u;
+                    e[u].zero(), f[u].zero();
+                    if (c >= a.dim) continue;
+                    load_any(e[u], src + c, a.wide_x);
+                    if (!a.d_loss) f[u].w[0] = __ldg(reinterpret_cast<const uint4 *>(w + c));
+                }
+#pragma unroll
+                for (int u = 0; u < TAKE_AHEAD; ++u) {
+                    const int64_t c = c0 + 256 * u;
+                    if (c < a.dim) *reinterpret_cast<uint4 *>(dst + c) = e[u].w[0];
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) score = fmaf(e[u].get(i), f[u].get(i), score);
+                }
             }
             if (!a.d_loss) {
                 score = warp_sum(score);
@@ -433,8 +442,8 @@ done:
     if (warp == 9) tc::tmem_free(tmem, 512);
 }
 
-// ---- lse and loss from the tiles' statistics: 32 rows to a block, eight threads a row ---------------------------------
-constexpr int JOIN_WAYS = 8;
+// ---- lse and loss from the tiles' statistics: 32 rows to a block, 32 threads a row ---------------------------------
+constexpr int JOIN_WAYS = 32, JOIN_AHEAD = 4;
 __global__ void __launch_bounds__(32 * JOIN_WAYS) join_scores(const __grid_constant__ Args a, int tiles) {
     pdl_wait();
     __shared__ float2 part[JOIN_WAYS][32];
@@ -449,11 +458,19 @@ __global__ void __launch_bounds__(32 * JOIN_WAYS) join_scores(const __grid_const
         top = now;
     };
     if (m < count)
-        for (int i = threadIdx.y; i < tiles; i += JOIN_WAYS) take(a.part[(int64_t)i * a.padded + m]);
+        for (int i = threadIdx.y; i < tiles; i += JOIN_WAYS * JOIN_AHEAD) {
+            float2 p[JOIN_AHEAD];
+#pragma unroll
+            for (int u = 0; u < JOIN_AHEAD; ++u) {
+                const int at = i + u * JOIN_WAYS;
+                p[u] = at < tiles ? a.part[(int64_t)at * a.padded + m] : make_float2(-CUDART_INF_F, 0.f);
+            }
+#pragma unroll
+            for (int u = 0; u < JOIN_AHEAD; ++u) take(p[u]);
+        }
     part[threadIdx.y][threadIdx.x] = make_float2(top, total);
     __syncthreads();
     if (threadIdx.y == 0 && m < count) {
-#pragma unroll
         for (int k = 1; k < JOIN_WAYS; ++k) take(part[k][threadIdx.x]);
         float lse = (fabsf(top) == CUDART_INF_F ? 0.f : top) + logf(total);
         // The tensor cores' sums come out small, the more so the larger they are, and the largest is often the target's.  Its share of lse

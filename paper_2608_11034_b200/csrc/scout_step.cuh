@@ -34,7 +34,7 @@ template <bool WIDE> struct Columns {
     __device__ __forceinline__ bool any() const { return c0 < dim; }
 };
 
-// Eight elements of a row, as they lie in memory; zeros where the row ends.
+// Eight elements of a row, as they lie in memory.  Where the row ends load leaves what was there: zeros, once zero() was called.
 template <typename T> struct Eight {
     static constexpr int N = sizeof(T) / 2;
     uint4 w[N];
@@ -82,7 +82,6 @@ template <typename T> struct Eight {
     }
     // STREAM: read once
     template <bool STREAM, bool WIDE> __device__ __forceinline__ void load(const T *row, const Columns<WIDE> &c) {
-        zero();
         if constexpr (WIDE) {
             if (c.any())
 #pragma unroll
@@ -90,12 +89,18 @@ template <typename T> struct Eight {
                     w[i] = STREAM ? __ldcs(reinterpret_cast<const uint4 *>(row + c.c0) + i) : __ldg(reinterpret_cast<const uint4 *>(row + c.c0) + i);
         } else {
             uint32_t *v = reinterpret_cast<uint32_t *>(w);
+            if constexpr (sizeof(T) == 4) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
-                if (c.has(i)) {
-                    if constexpr (sizeof(T) == 4) v[i] = __float_as_uint(row[c.col(i)]);
-                    else v[i >> 1] |= (uint32_t) reinterpret_cast<const uint16_t *>(row)[c.col(i)] << (16 * (i & 1));
-                }
+                for (int i = 0; i < 8; ++i)
+                    if (c.has(i)) v[i] = __float_as_uint(row[c.col(i)]);
+            } else {
+                const uint16_t *h = reinterpret_cast<const uint16_t *>(row);
+                uint32_t x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = c.has(i) ? h[c.col(i)] : 0;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) v[i] = x[2 * i] | x[2 * i + 1] << 16;
+            }
         }
     }
     template <bool WIDE> __device__ __forceinline__ void store(T *row, const Columns<WIDE> &c) const {
@@ -154,27 +159,44 @@ __device__ __forceinline__ uint4 philox(const Drop &d, uint32_t chunk, uint32_t 
     }
     return make_uint4(c0, c1, c2, c3);
 }
-// Bit i: the thread's element i is kept.  k: the thread's number in its row, all threads of a warp in turn, and whole warps call this.
-// Where the lanes' elements are not the eights that share a counter, a lane makes its eight bits and the warp deals them out: lanes
-// 4 i .. 4 i + 3 hold the 32 places that element i of lanes 0 .. 31 are, in order.
-template <bool WIDE> __device__ __forceinline__ uint32_t keep8(const Drop &d, int64_t k, uint32_t row, uint64_t offset) {
-    const uint4 bits = philox(d, (uint32_t)k, row, offset);
-    const uint32_t w[4] = {bits.x, bits.y, bits.z, bits.w}, cut = d.cut << 16;
-    uint32_t m = 0;
+// Which of a thread's eight elements are kept.  Whole warps make these together, k being the thread's number in its row, all
+// threads of a warp in turn.
+// Where the lanes' elements are not the eights that share a counter, a lane makes eight bits of its own and the warp deals them out:
+// lanes 4 i .. 4 i + 3 hold the 32 places that element i of lanes 0 .. 31 are, in order.
+template <bool WIDE> struct Keep {
+    uint32_t w[4];  // WIDE: the numbers; else bits, in w[0]
+    uint32_t cut;
+    __device__ __forceinline__ Keep() {}
+    __device__ __forceinline__ Keep(const Drop &d, uint32_t k, uint32_t row, uint64_t offset) : cut(d.cut << 16) {
+        const uint4 n = philox(d, k, row, offset);
+        w[0] = n.x, w[1] = n.y, w[2] = n.z, w[3] = n.w;
+        if constexpr (!WIDE) {
+            uint32_t m = 0, mine = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        m |= (w[i] << 16) >= cut ? 1u << (2 * i) : 0u;
-        m |= w[i] >= cut ? 2u << (2 * i) : 0u;
+            for (int i = 0; i < 4; ++i) {
+                m |= (w[i] << 16) >= cut ? 1u << (2 * i) : 0u;
+                m |= w[i] >= cut ? 2u << (2 * i) : 0u;
+            }
+            const uint32_t lane = threadIdx.x & 31;
+            uint32_t word = m << (8 * (lane & 3));
+            word |= __shfl_xor_sync(0xFFFFFFFFu, word, 1);
+            word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mine |= ((__shfl_sync(0xFFFFFFFFu, word, 4 * i) >> lane) & 1u) << i;
+            w[0] = mine;
+        }
     }
-    if constexpr (WIDE) return m;
-    const uint32_t lane = threadIdx.x & 31;
-    uint32_t word = m << (8 * (lane & 3)), mine = 0;
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 1);
-    word |= __shfl_xor_sync(0xFFFFFFFFu, word, 2);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) mine |= ((__shfl_sync(0xFFFFFFFFu, word, 4 * i) >> lane) & 1u) << i;
-    return mine;
-}
+    __device__ __forceinline__ void all() { w[0] = w[1] = w[2] = w[3] = 0xFFFFFFFFu, cut = 0; }
+    __device__ __forceinline__ bool operator[](int i) const {
+        if constexpr (WIDE) return (i & 1 ? w[i >> 1] : w[i >> 1] << 16) >= cut;
+        else return (w[0] >> i) & 1u;
+    }
+    // pair i where kept, else 0 whatever it was
+    __device__ __forceinline__ tc::F2 of(int i, tc::F2 x) const {
+        const float2 f = tc::split(x);
+        return tc::f2((*this)[2 * i] ? f.x : 0.f, (*this)[2 * i + 1] ? f.y : 0.f);
+    }
+};
 
 // ---- host ------------------------------------------------------------------------------------------------
 inline bool known_float(uint32_t dtype) { return dtype == SCOUT_DT_F32 || dtype == SCOUT_DT_BF16 || dtype == SCOUT_DT_F16; }
