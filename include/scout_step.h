@@ -94,10 +94,10 @@ typedef struct {
     float scale;               /* finite                                                */
     float eps;                 /* finite, >= 0                                          */
     uint32_t reserved;         /* 0                                                     */
-    uint64_t rows;             /* up to 2^32                                            */
+    uint64_t rows;             /* below 2^32                                            */
     uint64_t dim;              /* 1..16384                                              */
     uint64_t groups;           /* divides rows; gate is [groups][dim], dense            */
-    /* row strides of forward (x, b, y, n) and backward (dy, dn, b, y, dx, db) */
+    /* row strides of forward (x, b, y, n) and backward (dy, dn, b, y, dx, db), below 2^32 */
     uint64_t x_stride, b_stride, y_stride, n_stride, dy_stride, dn_stride, dx_stride, db_stride;
 } scout_join_t;
 

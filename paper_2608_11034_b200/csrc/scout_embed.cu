@@ -90,6 +90,7 @@ template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaS
 constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT, HELD = 4;
 constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4, FILL_CLUSTERS = SMS / CLUSTER - 1;
 constexpr int MARKED = 1 << 20, MARK_SMEM = MARKED / 8;  // ids of a block of mark_ids
+constexpr int CLEARED = 4;
 constexpr int PIECE = 32, AHEAD = 8, SUM_THREADS = 128;
 constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
 
@@ -99,7 +100,7 @@ struct Grad {
     uint32_t *key[2], *place[2];  // [rows] each: sorted by the digits so far, passes alternate
     uint32_t *seen;               // a bit for every id
     uint2 *across_list;           // [pieces]: the piece that an id begins in and a later one that it ends in
-    uint32_t *across_count;
+    uint32_t *across_count, *cleared;
     float *part;                  // [pieces][2][dim]: what goes on from the piece before, and what goes on into the next one
     int64_t dy_stride, table_stride, rows, dim;
     uint32_t vocab, pieces, across;  // blocks of columns
@@ -111,6 +112,7 @@ struct Grad {
 __global__ void __launch_bounds__(SORT_THREADS) mark_ids(const __grid_constant__ Grad a) {
     pdl_launch_dependents();
     extern __shared__ uint32_t smem[];
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.cleared = 0;
     const uint32_t first = blockIdx.x * MARKED, ids = min((uint32_t)MARKED, a.vocab - first), words = (ids + 31) / 32;
     for (uint32_t w = threadIdx.x; w < words; w += SORT_THREADS) smem[w] = 0;
     __syncthreads();
@@ -140,10 +142,16 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
     extern __shared__ uint32_t smem[];
     if (blockIdx.x >= CLUSTER) {
         pdl_wait();  // the marks; what the sorting blocks read and write has nothing to do with them
-        const int64_t stride = (int64_t)(gridDim.x - CLUSTER) * SORT_WARPS;
-        for (int64_t v = (int64_t)(blockIdx.x - CLUSTER) * SORT_WARPS + (threadIdx.x >> 5); v < a.vocab; v += stride)
-            if (!((a.seen[v >> 5] >> (v & 31)) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + v * a.table_stride, a.dim);
-        return;
+        // Rows are taken from a counter, CLEARED at a time: the clusters need not all run at once.
+        for (;;) {
+            uint32_t v0 = 0;
+            if ((threadIdx.x & 31) == 0) v0 = atomicAdd(a.cleared, (uint32_t)CLEARED);
+            v0 = __shfl_sync(0xFFFFFFFFu, v0, 0);
+            if (v0 >= a.vocab) return;
+            const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // CLEARED divides 32
+            for (uint32_t i = 0; i < CLEARED && v0 + i < a.vocab; ++i)
+                if (!((seen >> i) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, a.dim);
+        }
     }
     uint32_t *const hist = smem, *const total = smem + SORT_WARPS * MAX_BINS, *const scan = total + MAX_BINS;  // [warp][bin], [bin], [bin]
     __shared__ uint32_t warp_total[SORT_WARPS];
@@ -363,7 +371,7 @@ template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream
     if (grid) SCOUT_CUDA(launch_dependent(a.wide ? sum_places<T, TO, true> : sum_places<T, TO, false>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
     if (a.pieces > 1) {
         const uint32_t wide = (uint32_t)((a.dim + JOIN_COLS - 1) / JOIN_COLS);
-        const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 8 * SMS / wide)));
+        const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 16 * SMS / wide)));
         SCOUT_CUDA(launch_dependent(join_pieces<TO>, jg, dim3(JOIN_THREADS), stream, a));
     }
     return SCOUT_OK;
@@ -444,7 +452,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     uint8_t *const ws = (uint8_t *)workspace;
     a.ids = ids, a.dy = dy, a.table = d_table;
     for (int i = 0; i < 2; ++i) a.key[i] = (uint32_t *)(ws + need.key[i]), a.place[i] = (uint32_t *)(ws + need.place[i]);
-    a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.part = (float *)(ws + need.part);
+    a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.cleared = a.across_count + 1, a.part = (float *)(ws + need.part);
     a.dy_stride = (int64_t)dy_stride, a.table_stride = (int64_t)d_table_stride, a.rows = (int64_t)rows, a.dim = (int64_t)dim;
     a.vocab = (uint32_t)vocab, a.pieces = (uint32_t)((rows + PIECE - 1) / PIECE), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
     int bits = 1;

@@ -1,8 +1,8 @@
 // A block's output joins the residual stream: u = dropout(rms norm of b), y = x + scale gate u, n = rms norm of y; and the gradients.
 //
 // Bound by memory: forward reads x, b and writes y, n; backward reads dy, dn, b, y and writes dx, db.  A row is held in registers by
-// one team of warps, eight elements a thread (32 beyond 4096), so that each tensor crosses memory once although a row's sums are
-// needed twice, and the next rows are fetched before the present ones are worked on.  Rows are dealt to teams: in turn (forward), in
+// one team of warps, so that each tensor crosses memory once although a row's sums are needed twice, and the next row is fetched while
+// the present one is worked on.  Rows are dealt to teams: in turn (forward), in
 // runs (backward, whose column sums stay with the thread that owns the column for a whole run; runs meet in a second kernel, in order).
 #include <algorithm>
 #include <cmath>
@@ -13,7 +13,9 @@ namespace scout {
 namespace step {
 namespace {
 
-constexpr int MAX_DIM = 16384, THREADS = 512;  // registers for two blocks' worth of half as many threads
+constexpr int MAX_DIM = 16384;
+// A thread has V eights of a row: two up to 4096 columns, four beyond.
+template <int V> constexpr int MOST = V == 2 ? 256 : 512;  // threads of a block
 
 struct Args {
     const void *x, *b, *dy, *dn, *yin, *gate, *post, *norm;
@@ -22,7 +24,7 @@ struct Args {
     float *stats;
     float *part;       // [slabs][2][dim]: d_post, d_norm of a run of rows
     float *part_gate;  // [slabs][2][dim]: d_gate of a group's part at the start of a run, and of one that begins inside it
-    int64_t x_stride, b_stride, y_stride, n_stride, dy_stride, dn_stride, dx_stride, db_stride;
+    uint32_t x_stride, b_stride, y_stride, n_stride, dy_stride, dn_stride, dx_stride, db_stride;
     int64_t rows, group_rows, per, slabs;
     int32_t dim, team, teams;  // threads of a team, teams of a block
     float scale, eps, inv_dim;
@@ -30,19 +32,14 @@ struct Args {
     Drop drop;
 };
 
-// Sums over a team, R at once.  Set k of the slots ([2][R][warps of the block] in shared memory) is not written again before every
-// thread has passed another team_sum.
-template <int R, int N> __device__ __forceinline__ void team_sum(float (&x)[R], float (*slots)[N], int k, int team_threads, int team, int t) {
-#pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = warp_sum(x[r]);
-    if (team_threads == 32) return;
-    const int warps = team_threads / 32, at = team * warps;
-#pragma unroll
-    for (int r = 0; r < R; ++r)
-        if ((t & 31) == 0) slots[k * R + r][at + (t >> 5)] = x[r];
+// Sum over a team.  `slots`: the team's part of [teams][warps of a team] in shared memory, not written again before every thread has
+// passed another team_sum.
+__device__ __forceinline__ float team_sum(float x, float *slots, int warps, int t) {
+    x = warp_sum(x);
+    if (warps == 1) return x;
+    if ((t & 31) == 0) slots[t >> 5] = x;
     __syncthreads();
-#pragma unroll
-    for (int r = 0; r < R; ++r) x[r] = warp_sum((t & 31) < warps ? slots[k * R + r][at + (t & 31)] : 0.f);
+    return warp_sum((t & 31) < warps ? slots[t & 31] : 0.f);
 }
 // Pairs of weights, or what stands for none.
 template <typename TW, bool WIDE> __device__ __forceinline__ void weights(tc::F2 (&w)[4], const void *row, const Columns<WIDE> &c) {
@@ -60,293 +57,263 @@ template <typename TW, bool WIDE> __device__ __forceinline__ void weights(tc::F2
 template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, uint32_t group) {
     return a.gate ? reinterpret_cast<const TW *>(a.gate) + (int64_t)group * a.dim : nullptr;
 }
-// rows are below 2^32, and group_rows is that many only in one group
 __device__ __forceinline__ uint32_t group_of(const Args &a, int64_t row) { return a.group_rows == a.rows ? 0 : (uint32_t)row / (uint32_t)a.group_rows; }
+// rows and strides are below 2^32: one product
+template <typename T> __device__ __forceinline__ const T *row_of(const void *p, uint32_t stride, int64_t row) {
+    return reinterpret_cast<const T *>(p) + (uint64_t)(uint32_t)row * stride;
+}
+template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t stride, int64_t row) { return reinterpret_cast<T *>(p) + (uint64_t)(uint32_t)row * stride; }
 __device__ __forceinline__ tc::F2 both(float x) { return tc::f2(x, x); }
 __device__ __forceinline__ float add_pairs(const tc::F2 &x) {
     const float2 f = tc::split(x);
     return f.x + f.y;
 }
 
-// R rows of a team at a time share the waits of their sums and the weights they read; the next R are on their way meanwhile.
-template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ void __launch_bounds__(THREADS) join_forward(const __grid_constant__ Args a) {
-    constexpr int R = V == 1 ? 2 : 1;
-    constexpr bool AHEAD = V == 1;
-    __shared__ float slots[2 * R][THREADS / 32];
-    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team;
+// The next row's elements are fetched into the registers of the present one's as soon as those are free: b once it is widened, x once y
+// is made.
+template <typename TB, typename TS, typename TW, int V, bool WIDE>
+__global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __grid_constant__ Args a) {
+    __shared__ float slots[2][MOST<V> / 32];
+    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
+    float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
-    Eight<TB> b[R][V], b_next[R][V];
-    Eight<TS> x[R][V], x_next[R][V];
     const int64_t stride = (int64_t)gridDim.x * a.teams;
     int64_t row = (int64_t)blockIdx.x * a.teams + team;
-    const auto fetch = [&](Eight<TB> (&eb)[R][V], Eight<TS> (&ex)[R][V], int64_t from) {
+    Eight<TB> b[V];
+    Eight<TS> x[V];
+    // past the end the last row again, for nothing
+    const auto fetch_b = [&](int64_t at) {
 #pragma unroll
-        for (int r = 0; r < R; ++r)
+        for (int v = 0; v < V; ++v) b[v].template load<true, WIDE>(row_of<TB>(a.b, a.b_stride, min(at, a.rows - 1)), Columns<WIDE>(t + v * a.team, a.dim));
+    };
+    const auto fetch_x = [&](int64_t at) {
+        if (a.x)
 #pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Columns<WIDE> c(t + v * a.team, a.dim);
-                const int64_t at = min(from + r * stride, a.rows - 1);  // past the end the last row again, for nothing
-                eb[r][v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + at * a.b_stride, c);
-                if (a.x) ex[r][v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.x) + at * a.x_stride, c);
-            }
+            for (int v = 0; v < V; ++v) x[v].template load<true, WIDE>(row_of<TS>(a.x, a.x_stride, min(at, a.rows - 1)), Columns<WIDE>(t + v * a.team, a.dim));
     };
 #pragma unroll
-    for (int r = 0; r < R; ++r)
+    for (int v = 0; v < V; ++v) b[v].zero(), x[v].zero();
+    fetch_b(row), fetch_x(row);
+    for (; row - team < a.rows; row += stride) {  // the same for all teams of a block
+        const bool on = row < a.rows;
+        tc::F2 u[V][4], sq = both(0.f);
 #pragma unroll
-        for (int v = 0; v < V; ++v) b[r][v].zero(), x[r][v].zero(), b_next[r][v].zero(), x_next[r][v].zero();
-    fetch(b, x, row);
-    for (; row - team < a.rows; row += R * stride) {  // the same for all teams of a block
-        if constexpr (AHEAD) fetch(b_next, x_next, row + R * stride);
-        tc::F2 u[R][V][4];
-        float sum[R];
+        for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int r = 0; r < R; ++r) {
-            tc::F2 sq = both(0.f);
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) u[r][v][i] = b[r][v].pair(i), sq = tc::fma2(u[r][v][i], u[r][v][i], sq);
-            sum[r] = add_pairs(sq);
-        }
-        float rb[R] = {}, ry[R] = {};
-        if (a.post) {
-            team_sum<R>(sum, slots, 0, a.team, team, t);
-#pragma unroll
-            for (int r = 0; r < R; ++r) rb[r] = rsqrtf(sum[r] * a.inv_dim + a.eps);
-        }
-        tc::F2 sq[R];
-#pragma unroll
-        for (int r = 0; r < R; ++r) sq[r] = both(0.f);
+            for (int i = 0; i < 4; ++i) u[v][i] = b[v].pair(i), sq = tc::fma2(u[v][i], u[v][i], sq);
+        fetch_b(row + stride);
+        float rb = 0.f, ry = 0.f;
+        if (a.post) rb = rsqrtf(team_sum(add_pairs(sq), s0, warps, t) * a.inv_dim + a.eps);
+        sq = both(0.f);
+        const void *const gate = gate_row<TW>(a, group_of(a, min(row, a.rows - 1)));
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Columns<WIDE> c(t + v * a.team, a.dim);
+            tc::F2 w[4];
             if (a.post) {
-                tc::F2 w[4];
                 weights<TW, WIDE>(w, a.post, c);
 #pragma unroll
-                for (int r = 0; r < R; ++r)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) u[r][v][i] = tc::mul2(u[r][v][i], tc::mul2(both(rb[r]), w[i]));
+                for (int i = 0; i < 4; ++i) u[v][i] = tc::mul2(u[v][i], tc::mul2(both(rb), w[i]));
             }
+            if (a.drop.cut) {
+                const Keep<WIDE> keep(a.drop, t + v * a.team, (uint32_t)row, offset);
 #pragma unroll
-            for (int r = 0; r < R; ++r) {
-                const int64_t at = row + r * stride;
-                if (a.drop.cut) {
-                    const Keep<WIDE> keep(a.drop, t + v * a.team, (uint32_t)at, offset);
+                for (int i = 0; i < 4; ++i) u[v][i] = keep.of(i, tc::mul2(u[v][i], both(a.drop.factor)));
+            }
+            weights<TW, WIDE>(w, gate, c);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) u[r][v][i] = keep.of(i, tc::mul2(u[r][v][i], both(a.drop.factor)));
-                }
-                if (at >= a.rows) continue;
-                tc::F2 w[4];
-                weights<TW, WIDE>(w, gate_row<TW>(a, group_of(a, at)), c);
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    u[r][v][i] = tc::fma2(tc::mul2(both(a.scale), w[i]), u[r][v][i], x[r][v].pair(i));
-                    sq[r] = tc::fma2(u[r][v][i], u[r][v][i], sq[r]);
-                }
-                x[r][v].set(u[r][v]);
-                x[r][v].store(reinterpret_cast<TS *>(a.y) + at * a.y_stride, c);
+            for (int i = 0; i < 4; ++i) {
+                u[v][i] = tc::fma2(tc::mul2(both(a.scale), w[i]), u[v][i], x[v].pair(i));
+                sq = tc::fma2(u[v][i], u[v][i], sq);
+            }
+            if (on) {
+                Eight<TS> y;
+                y.set(u[v]);
+                y.store(row_of<TS>(a.y, a.y_stride, row), c);
             }
         }
+        fetch_x(row + stride);
         if (a.norm) {
+            ry = rsqrtf(team_sum(add_pairs(sq), s1, warps, t) * a.inv_dim + a.eps);
+            if (on)
 #pragma unroll
-            for (int r = 0; r < R; ++r) sum[r] = add_pairs(sq[r]);
-            team_sum<R>(sum, slots, 1, a.team, team, t);
+                for (int v = 0; v < V; ++v) {
+                    const Columns<WIDE> c(t + v * a.team, a.dim);
+                    tc::F2 w[4];
+                    weights<TW, WIDE>(w, a.norm, c);
+                    Eight<TB> n;
 #pragma unroll
-            for (int r = 0; r < R; ++r) ry[r] = rsqrtf(sum[r] * a.inv_dim + a.eps);
-#pragma unroll
-            for (int v = 0; v < V; ++v) {
-                const Columns<WIDE> c(t + v * a.team, a.dim);
-                tc::F2 w[4];
-                weights<TW, WIDE>(w, a.norm, c);
-#pragma unroll
-                for (int r = 0; r < R; ++r) {
-                    if (row + r * stride >= a.rows) continue;
-                    tc::F2 n[4];
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) n[i] = tc::mul2(w[i], tc::mul2(u[r][v][i], both(ry[r])));
-                    b[r][v].set(n);
-                    b[r][v].store(reinterpret_cast<TB *>(a.n) + (row + r * stride) * a.n_stride, c);
+                    for (int i = 0; i < 4; ++i) w[i] = tc::mul2(w[i], tc::mul2(u[v][i], both(ry)));
+                    n.set(w);
+                    n.store(row_of<TB>(a.n, a.n_stride, row), c);
                 }
-            }
         }
-        if (t < R && row + t * stride < a.rows) {
-            a.stats[row + t * stride] = t == 0 ? rb[0] : rb[R - 1];
-            a.stats[a.rows + row + t * stride] = t == 0 ? ry[0] : ry[R - 1];
-        }
-        if (!(a.post && a.norm) && a.team > 32) __syncthreads();  // the one set of slots is written again by the next rows
-        if constexpr (AHEAD) {
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-#pragma unroll
-                for (int v = 0; v < V; ++v) b[r][v] = b_next[r][v], x[r][v] = x_next[r][v];
-        } else {
-            fetch(b, x, row + R * stride);
-        }
+        if (t == 0 && on) a.stats[row] = rb, a.stats[a.rows + row] = ry;
+        if (!(a.post && a.norm) && warps > 1) __syncthreads();  // the one set of slots is written again by the next row
     }
 }
 
-// The column sums of a run of rows: in registers, or with V > 1 in shared memory ([3][V * 4][threads], a thread's own places).
+// With h = scale g (masked) and c = b rms(b) (masked), du = h gate, and over the rows of one gate S = sum of h c gives both of
+//     d_gate = post S,   d_post = sum over gates of gate S,
+// so that a row adds to two column sums, S and d_norm: in registers, or beyond 4096 columns in shared memory.  d_post takes its part
+// when a gate's rows (or the run) end, in shared memory.
 template <int V> struct Sums {
-    tc::F2 r[V == 1 ? 3 : 1][4];
-    float2 *s;
+    static constexpr bool REGS = V == 2;
+    tc::F2 r[REGS ? 2 : 1][REGS ? V : 1][4];
+    float2 *s;  // [1 or 3][V * 4][threads], a thread's own places; the first is d_post's
     int threads, t;
-    __device__ __forceinline__ void clear() {
-#pragma unroll
-        for (int k = 0; k < 3; ++k)
-#pragma unroll
-            for (int v = 0; v < V; ++v)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) set(k, v, i, both(0.f));
-    }
+    __device__ __forceinline__ float2 &at(int which, int v, int i) const { return s[((which * V + v) * 4 + i) * threads + t]; }
     __device__ __forceinline__ tc::F2 get(int which, int v, int i) const {
-        if constexpr (V == 1) {
-            return r[which][i];
-        } else {
-            const float2 f = s[((which * V + v) * 4 + i) * threads + t];
-            return tc::f2(f.x, f.y);
-        }
+        if (REGS && which > 0) return r[which - 1][v][i];
+        const float2 f = at(which, v, i);
+        return tc::f2(f.x, f.y);
     }
     __device__ __forceinline__ void set(int which, int v, int i, tc::F2 x) {
-        if constexpr (V == 1) r[which][i] = x;
-        else s[((which * V + v) * 4 + i) * threads + t] = tc::split(x);
+        if (REGS && which > 0) r[which - 1][v][i] = x;
+        else at(which, v, i) = tc::split(x);
     }
     __device__ __forceinline__ void add(int which, int v, int i, tc::F2 x, tc::F2 y) { set(which, v, i, tc::fma2(x, y, get(which, v, i))); }
 };
+enum { D_POST, GATE_SUM, D_NORM };
 
-template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ void __launch_bounds__(THREADS) join_backward(const __grid_constant__ Args a) {
-    constexpr bool AHEAD = V == 1;
-    __shared__ float slots[2][THREADS / 32];
+template <typename TB, typename TS, typename TW, int V, bool WIDE>
+__global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const __grid_constant__ Args a) {
+    __shared__ float slots[2][MOST<V> / 32];
     extern __shared__ float2 sums[];
-    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team;
+    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
+    float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
     const int64_t slab = (int64_t)blockIdx.x * a.teams + team, first = slab * a.per, last = min(first + a.per, a.rows);
     Sums<V> acc;
-    if constexpr (V > 1) acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
-    acc.clear();
-    struct Row {
-        Eight<TS> y[V], g[V];
-        Eight<TB> n[V], b[V];
-        float rb, ry;
-    } cur, next;
-    const auto clear = [&](Row &e) {
+    acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
+    Eight<TS> y[V], g0[V];
+    Eight<TB> n[V], b[V];
 #pragma unroll
-        for (int v = 0; v < V; ++v) e.y[v].zero(), e.g[v].zero(), e.n[v].zero(), e.b[v].zero();
-        e.rb = 1.f, e.ry = 0.f;
-    };
-    const auto fetch = [&](Row &e, int64_t at) {
-        const int64_t row = min(at, a.rows - 1);  // past the end the last row again, for nothing
+    for (int v = 0; v < V; ++v) {
+        y[v].zero(), g0[v].zero(), n[v].zero(), b[v].zero();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc.set(D_POST, v, i, both(0.f)), acc.set(GATE_SUM, v, i, both(0.f)), acc.set(D_NORM, v, i, both(0.f));
+    }
+    float rb = 1.f, ry = 0.f;
+    // past the end the last row again, for nothing
+    const auto fetch = [&](int64_t at) {
+        const int64_t row = min(at, a.rows - 1);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Columns<WIDE> c(t + v * a.team, a.dim);
             if (a.dn) {
-                e.y[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.yin) + row * a.y_stride, c);
-                e.n[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.dn) + row * a.dn_stride, c);
+                y[v].template load<true, WIDE>(row_of<TS>(a.yin, a.y_stride, row), c);
+                n[v].template load<true, WIDE>(row_of<TB>(a.dn, a.dn_stride, row), c);
             }
-            if (a.dy) e.g[v].template load<true, WIDE>(reinterpret_cast<const TS *>(a.dy) + row * a.dy_stride, c);
-            e.b[v].template load<true, WIDE>(reinterpret_cast<const TB *>(a.b) + row * a.b_stride, c);
+            if (a.dy) g0[v].template load<true, WIDE>(row_of<TS>(a.dy, a.dy_stride, row), c);
         }
-        if (a.post) e.rb = a.stats_in[row];
-        if (a.dn) e.ry = a.stats_in[a.rows + row];
+        if (a.dn) ry = a.stats_in[a.rows + row];
+    };
+    const auto fetch_b = [&](int64_t at) {
+        const int64_t row = min(at, a.rows - 1);
+#pragma unroll
+        for (int v = 0; v < V; ++v) b[v].template load<true, WIDE>(row_of<TB>(a.b, a.b_stride, row), Columns<WIDE>(t + v * a.team, a.dim));
+        if (a.post) rb = a.stats_in[row];
     };
     uint32_t group = group_of(a, min(first, a.rows - 1));
-    int64_t group_end = (group + 1ll) * a.group_rows;
-    clear(cur), clear(next);
-    int64_t begun = first;  // where the gate's current sum began
-    fetch(cur, first);
+    int64_t group_end = (group + 1ll) * a.group_rows, begun = first;  // where the gate's current sum began
+    const float factor = a.scale * (a.drop.cut ? a.drop.factor : 1.f);
+    fetch(first), fetch_b(first);
     for (int64_t it = 0; it < a.per; ++it) {
         const int64_t row = first + it;
         const bool on = row < last;
-        if constexpr (AHEAD) fetch(next, row + 1);
-        const float rb = cur.rb, ry = cur.ry;
-        tc::F2 g[V][4];
-        float dot[1] = {0.f};
+        tc::F2 g[V][4], d = both(0.f);
         if (a.dn) {
-            tc::F2 d = both(0.f);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                tc::F2 w[4];
-                weights<TW, WIDE>(w, a.norm, Columns<WIDE>(t + v * a.team, a.dim));
+                weights<TW, WIDE>(g[v], a.norm, Columns<WIDE>(t + v * a.team, a.dim));
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    const tc::F2 z = tc::mul2(cur.y[v].pair(i), both(ry)), dn = cur.n[v].pair(i);
-                    g[v][i] = tc::mul2(dn, w[i]);
-                    if (on) acc.add(2, v, i, dn, z);
+                    const tc::F2 z = tc::mul2(y[v].pair(i), both(ry)), dn = n[v].pair(i);
+                    g[v][i] = tc::mul2(dn, g[v][i]);
+                    if (on) acc.add(D_NORM, v, i, dn, z);
                     d = tc::fma2(g[v][i], z, d);
                 }
             }
-            dot[0] = add_pairs(d);
-            team_sum<1>(dot, slots, 0, a.team, team, t);
+            const float pull = -(team_sum(add_pairs(d), s0, warps, t) * a.inv_dim) * ry;
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[v][i] = tc::fma2(both(ry), tc::fma2(both(pull), y[v].pair(i), g[v][i]), g0[v].pair(i));
+        } else {
+#pragma unroll
+            for (int v = 0; v < V; ++v)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) g[v][i] = g0[v].pair(i);
         }
-        const float pull = -(dot[0] * a.inv_dim) * ry;
-        tc::F2 d = both(0.f);
+        if (it + 1 < a.per) fetch(row + 1);
+        d = both(0.f);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Columns<WIDE> c(t + v * a.team, a.dim);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                g[v][i] = a.dn ? tc::fma2(both(ry), tc::fma2(both(pull), cur.y[v].pair(i), g[v][i]), cur.g[v].pair(i)) : cur.g[v].pair(i);
             if (a.dx && on) {
-                cur.g[v].set(g[v]);
-                cur.g[v].store(reinterpret_cast<TS *>(a.dx) + row * a.dx_stride, c);
+                Eight<TS> e;
+                e.set(g[v]);
+                e.store(row_of<TS>(a.dx, a.dx_stride, row), c);
             }
-            tc::F2 w[4], gw[4];
-            weights<TW, WIDE>(w, a.post, c);
-            weights<TW, WIDE>(gw, gate_row<TW>(a, group), c);
             Keep<WIDE> keep;
             if (a.drop.cut) keep = Keep<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset);
-            else keep.all();
-            const tc::F2 factor = both(a.scale * (a.drop.cut ? a.drop.factor : 1.f));
+            tc::F2 w[4], gate[4];
+            weights<TW, WIDE>(w, a.post, c);
+            weights<TW, WIDE>(gate, gate_row<TW>(a, group), c);
             if (!on) continue;
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                // what was dropped is 0 in both, whatever it was
-                const tc::F2 cb = keep.of(i, tc::mul2(cur.b[v].pair(i), both(rb))), h = keep.of(i, tc::mul2(g[v][i], factor));
-                acc.add(0, v, i, tc::mul2(cb, w[i]), h);
-                const tc::F2 du = tc::mul2(h, gw[i]);
-                acc.add(1, v, i, du, cb);
-                g[v][i] = tc::mul2(du, w[i]);
+                tc::F2 cb = tc::mul2(b[v].pair(i), both(rb)), h = tc::mul2(g[v][i], both(factor));
+                if (a.drop.cut) cb = keep.of(i, cb), h = keep.of(i, h);  // what was dropped is 0 in both, whatever it was
+                acc.add(GATE_SUM, v, i, h, cb);
+                g[v][i] = tc::mul2(h, tc::mul2(gate[i], w[i]));
                 d = tc::fma2(g[v][i], cb, d);
             }
         }
-        float dot2[1] = {add_pairs(d)};
-        if (a.post) team_sum<1>(dot2, slots, 1, a.team, team, t);
-        const float pull2 = -(dot2[0] * a.inv_dim) * rb;
+        float pull = 0.f;
+        if (a.post) pull = -(team_sum(add_pairs(d), s1, warps, t) * a.inv_dim) * rb;
         if (on) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 if (a.post) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) g[v][i] = tc::mul2(both(rb), tc::fma2(both(pull2), cur.b[v].pair(i), g[v][i]));
+                    for (int i = 0; i < 4; ++i) g[v][i] = tc::mul2(both(rb), tc::fma2(both(pull), b[v].pair(i), g[v][i]));
                 }
-                cur.b[v].set(g[v]);
-                cur.b[v].store(reinterpret_cast<TB *>(a.db) + row * a.db_stride, Columns<WIDE>(t + v * a.team, a.dim));
+                Eight<TB> e;
+                e.set(g[v]);
+                e.store(row_of<TB>(a.db, a.db_stride, row), Columns<WIDE>(t + v * a.team, a.dim));
             }
         }
-        if (!(a.post && a.dn) && a.team > 32) __syncthreads();
+        if (it + 1 < a.per) fetch_b(row + 1);
+        if (!(a.post && a.dn) && warps > 1) __syncthreads();
         // the gate's sum ends with its group or with the run
         if (on && (row + 1 == last || row + 1 == group_end)) {
             const bool whole = begun + a.group_rows == group_end && row + 1 == group_end;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Columns<WIDE> c(t + v * a.team, a.dim);
+                tc::F2 w[4], gate[4];
+                weights<TW, WIDE>(w, a.post, c);
+                weights<TW, WIDE>(gate, gate_row<TW>(a, group), c);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float2 f = tc::split(acc.get(0, v, i >> 1));
+                    const float2 f = tc::split(tc::mul2(w[i >> 1], acc.get(GATE_SUM, v, i >> 1)));
                     const float x = i & 1 ? f.y : f.x;
                     if (!a.d_gate || !c.has(i)) continue;
                     if (whole) reinterpret_cast<TW *>(a.d_gate)[(int64_t)group * a.dim + c.col(i)] = down<TW>(x);
                     else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = x;
                 }
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc.set(0, v, i, both(0.f));
+                for (int i = 0; i < 4; ++i) {
+                    acc.add(D_POST, v, i, gate[i], acc.get(GATE_SUM, v, i));
+                    acc.set(GATE_SUM, v, i, both(0.f));
+                }
             }
             begun = row + 1;
             if (begun == group_end) ++group, group_end += a.group_rows;
             if (begun == a.rows) group = 0;  // for nothing, but inside
         }
-        if constexpr (AHEAD) cur = next;
-        else fetch(cur, row + 1);
     }
     if (first < last) {
 #pragma unroll
@@ -354,10 +321,10 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> __global__ vo
             const Columns<WIDE> c(t + v * a.team, a.dim);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float2 p = tc::split(acc.get(1, v, i >> 1)), n = tc::split(acc.get(2, v, i >> 1));
+                const float2 p = tc::split(acc.get(D_POST, v, i >> 1)), q = tc::split(acc.get(D_NORM, v, i >> 1));
                 if (!c.has(i)) continue;
                 if (a.d_post) a.part[slab * 2 * a.dim + c.col(i)] = i & 1 ? p.y : p.x;
-                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = i & 1 ? n.y : n.x;
+                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = i & 1 ? q.y : q.x;
             }
         }
     }
@@ -399,38 +366,39 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
 
 // How rows are dealt out.
 struct Shape {
-    int v, team, teams;
+    int v, team, teams, blocks;  // of an SM
     int64_t slabs, per;
 };
-Shape shape(uint64_t rows, uint64_t dim) {
+Shape shape(uint64_t rows, uint64_t dim, bool backward) {
     Shape s = {};
-    const int threads = (int)((dim + 255) / 256 * 32);  // whole warps of eight columns a thread
-    s.v = threads > THREADS ? 4 : 1;
-    s.team = ((threads + s.v - 1) / s.v + 31) / 32 * 32;
+    const int eights = (int)((dim + 255) / 256 * 32);  // whole warps' worth
+    s.v = eights > 2 * MOST<2> ? 4 : 2;
+    s.team = (eights / s.v + 31) / 32 * 32;
     s.teams = std::max(1, 128 / s.team);
-    const int64_t want = (int64_t)SMS * std::max(1, THREADS / (s.team * s.teams)) * s.teams;
+    s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / (s.team * s.teams)) : 1;
+    const int64_t want = (int64_t)SMS * s.blocks * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);
     s.slabs = ((int64_t)rows + s.per - 1) / s.per;
     return s;
 }
 
 template <typename TB, typename TS, typename TW, bool WIDE> int run_forward(Args &a, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim);
+    const Shape s = shape(a.rows, a.dim, false);
     a.team = s.team, a.teams = s.teams;
-    const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * std::max(1, THREADS / (s.team * s.teams)));
-    (s.v == 1 ? join_forward<TB, TS, TW, 1, WIDE> : join_forward<TB, TS, TW, 4, WIDE>)<<<grid, s.team * s.teams, 0, stream>>>(a);
+    const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks);
+    (s.v == 2 ? join_forward<TB, TS, TW, 2, WIDE> : join_forward<TB, TS, TW, 4, WIDE>)<<<grid, s.team * s.teams, 0, stream>>>(a);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
 
 template <typename TB, typename TS, typename TW, bool WIDE> int run_backward(Args &a, int64_t groups, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim);
+    const Shape s = shape(a.rows, a.dim, true);
     a.team = s.team, a.teams = s.teams, a.per = s.per, a.slabs = s.slabs;
     const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams);
-    if (s.v == 1) {
-        join_backward<TB, TS, TW, 1, WIDE><<<grid, s.team * s.teams, 0, stream>>>(a);
+    if (s.v == 2) {
+        join_backward<TB, TS, TW, 2, WIDE><<<grid, s.team * s.teams, 2 * 4 * 8 * s.team * s.teams, stream>>>(a);
     } else {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE>>(3 * 4 * 4 * 8 * THREADS)) return rc;
+        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE>>(3 * 4 * 4 * 8 * MOST<4>)) return rc;
         join_backward<TB, TS, TW, 4, WIDE><<<grid, s.team * s.teams, 3 * 4 * 4 * 8 * s.team * s.teams, stream>>>(a);
     }
     SCOUT_CUDA(cudaGetLastError());
@@ -459,7 +427,9 @@ int check(const scout_join_t *j) {
         if (t != j->dtype && t != SCOUT_DT_F32) return SCOUT_ERR_UNSUPPORTED;
     if (!std::isfinite(j->scale) || !std::isfinite(j->eps) || j->eps < 0.f) return SCOUT_ERR_INVALID;
     if (j->dim == 0 || j->groups == 0 || j->rows % j->groups) return SCOUT_ERR_INVALID;
-    return j->rows > 1ull << 32 || j->dim > MAX_DIM ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;
+    for (uint64_t s : {j->x_stride, j->b_stride, j->y_stride, j->n_stride, j->dy_stride, j->dn_stride, j->dx_stride, j->db_stride})
+        if (s >> 32) return SCOUT_ERR_UNSUPPORTED;
+    return j->rows >= 1ull << 32 || j->dim > MAX_DIM ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;
 }
 int check_weights(const scout_join_t *j, std::initializer_list<const void *> all) {
     for (const void *p : all)
@@ -472,8 +442,8 @@ bool wide_weights(const scout_join_t *j, std::initializer_list<const void *> all
     return true;
 }
 void describe(const scout_join_t *j, Args *a) {
-    a->x_stride = (int64_t)j->x_stride, a->b_stride = (int64_t)j->b_stride, a->y_stride = (int64_t)j->y_stride, a->n_stride = (int64_t)j->n_stride;
-    a->dy_stride = (int64_t)j->dy_stride, a->dn_stride = (int64_t)j->dn_stride, a->dx_stride = (int64_t)j->dx_stride, a->db_stride = (int64_t)j->db_stride;
+    a->x_stride = (uint32_t)j->x_stride, a->b_stride = (uint32_t)j->b_stride, a->y_stride = (uint32_t)j->y_stride, a->n_stride = (uint32_t)j->n_stride;
+    a->dy_stride = (uint32_t)j->dy_stride, a->dn_stride = (uint32_t)j->dn_stride, a->dx_stride = (uint32_t)j->dx_stride, a->db_stride = (uint32_t)j->db_stride;
     a->rows = (int64_t)j->rows, a->group_rows = (int64_t)(j->rows / j->groups), a->dim = (int32_t)j->dim;
     a->scale = j->scale, a->eps = j->eps, a->inv_dim = 1.f / (float)j->dim;
 }
@@ -512,7 +482,7 @@ extern "C" int scout_join_backward_workspace(const scout_join_t *j, uint64_t *by
     using namespace scout::step;
     if (!bytes) return SCOUT_ERR_INVALID;
     if (int rc = check(j)) return rc;
-    *bytes = (uint64_t)(shape(j->rows, j->dim).slabs * 4 * j->dim * 4 + 255) & ~255ull;
+    *bytes = (uint64_t)(shape(j->rows, j->dim, true).slabs * 4 * j->dim * 4 + 255) & ~255ull;
     return SCOUT_OK;
 }
 
@@ -551,7 +521,7 @@ extern "C" int scout_join_backward(const scout_join_t *j, const void *dy, const 
     a.dy = dy, a.dn = dn, a.b = b, a.yin = y, a.stats_in = stats, a.gate = gate, a.post = post, a.norm = norm;
     a.dx = dx, a.db = db, a.d_gate = d_gate, a.d_post = d_post, a.d_norm = d_norm;
     a.part = (float *)workspace;
-    a.part_gate = a.part + shape(j->rows, j->dim).slabs * 2 * (int64_t)j->dim;
+    a.part_gate = a.part + shape(j->rows, j->dim, true).slabs * 2 * (int64_t)j->dim;
     a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
              wide_rows(b, j->b_stride, j->dtype) && (!dx || wide_rows(dx, j->dx_stride, j->stream_dtype)) && wide_rows(db, j->db_stride, j->dtype);
     return by_types(*j, [&](auto tb, auto ts, auto tw) {

@@ -63,7 +63,7 @@ def join(**kw):
 @pytest.mark.parametrize("kw,code", [
     (dict(dtype=99), BAD), (dict(dtype=I32), NOT), (dict(stream_dtype=H), NOT), (dict(weight_dtype=H), NOT), (dict(scale=float("nan")), BAD),
     (dict(eps=-1.0), BAD), (dict(eps=float("inf")), BAD), (dict(dim=0), BAD), (dict(dim=16385), NOT), (dict(groups=0), BAD),
-    (dict(groups=5), BAD), (dict(rows=3 * 2 ** 32), NOT), (dict(reserved=1), BAD), (dict(dtype=F, weight_dtype=B), NOT)])
+    (dict(groups=5), BAD), (dict(rows=3 * 2 ** 31), NOT), (dict(x_stride=2 ** 32), NOT), (dict(reserved=1), BAD), (dict(dtype=F, weight_dtype=B), NOT)])
 def test_join_descriptions_are_checked(kw, code):
     with pytest.raises(binding.ScoutError) as e:
         binding.scout_join_backward_workspace(join(**kw).ctypes.data)
