@@ -16,8 +16,8 @@ constexpr int blocks(bool wide) { return wide ? 6 : 4; }  // of an SM
 struct Args {
     const void *x;
     void *y;
-    int64_t x_stride, y_stride, cols;
-    uint32_t row0, per_row, units;  // first row of this launch; eights of a row (whole warps of them unless wide); of all its rows (below 2^31)
+    int64_t x_stride, y_stride;
+    uint32_t cols, row0, per_row, units;  // first row of this launch; eights of a row (whole warps of them unless wide); of all its rows (below 2^31)
     uint32_t mul, shift;            // n / per_row for n < 2^31: a high product and a shift
     int wide;
     Drop drop;
@@ -27,7 +27,6 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, bloc
     constexpr int UNROLL = 2;
     const uint64_t offset = a.drop.at();
     const uint32_t stride = gridDim.x * THREADS, lane = threadIdx.x & 31;
-    const tc::F2 factor = tc::f2(a.drop.factor, a.drop.factor);
     // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop.
     // Units are counted to 2^31, so that the sums here stay below 2^32.
     for (uint32_t q0 = blockIdx.x * THREADS + threadIdx.x; q0 - lane < a.units; q0 += stride * UNROLL) {
@@ -39,7 +38,7 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, bloc
             row[u] = (__umulhi(q, a.mul) + q) >> a.shift;
             k[u] = q - row[u] * a.per_row;
             e[u].zero();
-            if (q < a.units) e[u].template load<true, WIDE>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride, Columns<WIDE>(k[u], a.cols));
+            if (q < a.units) e[u].template load<true>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride, Columns<WIDE>(k[u], a.cols));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
@@ -47,9 +46,9 @@ template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, bloc
             if (q - lane >= a.units) break;
             const Keep<WIDE> keep(a.drop, k[u], a.row0 + row[u], offset);
             if (q >= a.units) continue;
-            tc::F2 x[4];
+            float x[8];
 #pragma unroll
-            for (int i = 0; i < 4; ++i) x[i] = keep.of(i, tc::mul2(e[u].pair(i), factor));
+            for (int i = 0; i < 8; ++i) x[i] = keep[i] ? e[u].get(i) * a.drop.factor : 0.f;  // 0 whatever it was
             e[u].set(x);
             e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.cols));
         }
@@ -84,11 +83,11 @@ extern "C" int scout_dropout(uint32_t dtype, uint64_t rows, uint64_t cols, const
     if (!known_float(dtype)) return SCOUT_ERR_UNSUPPORTED;
     Args a = {};
     if (int rc = make_drop(p, seed, offset, d_offset, &a.drop)) return rc;
-    if (rows > 1ull << 32 || cols > 1ull << 33) return SCOUT_ERR_UNSUPPORTED;
+    if (rows > 1ull << 32 || cols >= 1ull << 31) return SCOUT_ERR_UNSUPPORTED;
     if (rows == 0 || cols == 0) return SCOUT_OK;
     if (int rc = check_matrix(x, x_stride, cols, dtype)) return rc;
     if (int rc = check_matrix(y, y_stride, cols, dtype)) return rc;
-    a.x = x, a.y = y, a.x_stride = (int64_t)x_stride, a.y_stride = (int64_t)y_stride, a.cols = (int64_t)cols;
+    a.x = x, a.y = y, a.x_stride = (int64_t)x_stride, a.y_stride = (int64_t)y_stride, a.cols = (uint32_t)cols;
     a.wide = cols % 8 == 0 && wide_rows(x, x_stride, dtype) && wide_rows(y, y_stride, dtype);
     switch (dtype) {
         case SCOUT_DT_F32: return run<float>(a, rows, (cudaStream_t)stream);

@@ -56,7 +56,7 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             e[u].zero();
-            if (id[u] < a.vocab) e[u].template load<false, WIDE>(reinterpret_cast<const T *>(a.table) + (int64_t)id[u] * a.table_stride, Columns<WIDE>(k[u], a.dim));
+            if (id[u] < a.vocab) e[u].template load<false>(reinterpret_cast<const T *>(a.table) + (int64_t)id[u] * a.table_stride, Columns<WIDE>(k[u], (uint32_t)a.dim));
         }
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
@@ -66,7 +66,7 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
             for (int i = 0; i < 8; ++i) x[i] = id[u] < a.vocab ? a.scale * e[u].get(i) : 0.f;
             Eight<TO> o;
             o.set(x);
-            o.store(reinterpret_cast<TO *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.dim));
+            o.store(reinterpret_cast<TO *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], (uint32_t)a.dim));
         }
     }
 }
@@ -100,7 +100,7 @@ struct Grad {
     uint32_t *key[2], *place[2];  // [rows] each: sorted by the digits so far, passes alternate
     uint32_t *seen;               // a bit for every id
     uint2 *across_list;           // [pieces]: the piece that an id begins in and a later one that it ends in
-    uint32_t *across_count, *cleared;
+    uint32_t *across_count, *cleared, *sorted;
     float *part;                  // [pieces][2][dim]: what goes on from the piece before, and what goes on into the next one
     int64_t dy_stride, table_stride, rows, dim;
     uint32_t vocab, pieces, across;  // blocks of columns
@@ -110,9 +110,10 @@ struct Grad {
 
 // The ids that occur, as bits: a block takes MARKED ids and looks at all places.
 __global__ void __launch_bounds__(SORT_THREADS) mark_ids(const __grid_constant__ Grad a) {
+    if (blockIdx.x == 0 && threadIdx.x == 0) *a.cleared = 0, *a.sorted = 0;
+    __threadfence();
     pdl_launch_dependents();
     extern __shared__ uint32_t smem[];
-    if (blockIdx.x == 0 && threadIdx.x == 0) *a.cleared = 0;
     const uint32_t first = blockIdx.x * MARKED, ids = min((uint32_t)MARKED, a.vocab - first), words = (ids + 31) / 32;
     for (uint32_t w = threadIdx.x; w < words; w += SORT_THREADS) smem[w] = 0;
     __syncthreads();
@@ -137,21 +138,27 @@ template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_
     if (head + body * N + lane < dim) row[head + body * N + lane] = down<TO>(0.f);
 }
 
+// Rows of ids that do not occur, CLEARED at a time from a counter, so that the blocks need not all run at once; with UNTIL_SORTED a
+// warp leaves when the ids are sorted, and the rest is written beside the sums.
+template <typename TO, bool UNTIL_SORTED> __device__ __forceinline__ void clear_rows(const Grad &a) {
+    for (;;) {
+        uint32_t v0 = 0;
+        if ((threadIdx.x & 31) == 0) v0 = UNTIL_SORTED && *reinterpret_cast<volatile uint32_t *>(a.sorted) ? a.vocab : atomicAdd(a.cleared, (uint32_t)CLEARED);
+        v0 = __shfl_sync(0xFFFFFFFFu, v0, 0);
+        if (v0 >= a.vocab) return;
+        const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // CLEARED divides 32
+        for (uint32_t i = 0; i < CLEARED && v0 + i < a.vocab; ++i)
+            if (!((seen >> i) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, a.dim);
+    }
+}
+
 // Sorts (the first cluster), and meanwhile writes zeros to rows of ids that do not occur (the others).
 template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
     extern __shared__ uint32_t smem[];
     if (blockIdx.x >= CLUSTER) {
         pdl_wait();  // the marks; what the sorting blocks read and write has nothing to do with them
-        // Rows are taken from a counter, CLEARED at a time: the clusters need not all run at once.
-        for (;;) {
-            uint32_t v0 = 0;
-            if ((threadIdx.x & 31) == 0) v0 = atomicAdd(a.cleared, (uint32_t)CLEARED);
-            v0 = __shfl_sync(0xFFFFFFFFu, v0, 0);
-            if (v0 >= a.vocab) return;
-            const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // CLEARED divides 32
-            for (uint32_t i = 0; i < CLEARED && v0 + i < a.vocab; ++i)
-                if (!((seen >> i) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, a.dim);
-        }
+        clear_rows<TO, true>(a);
+        return;
     }
     uint32_t *const hist = smem, *const total = smem + SORT_WARPS * MAX_BINS, *const scan = total + MAX_BINS;  // [warp][bin], [bin], [bin]
     __shared__ uint32_t warp_total[SORT_WARPS];
@@ -236,6 +243,7 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
         }
         cluster.sync();  // what the others wrote is read next; nobody's `total` is read any more
     }
+    if (rank == 0 && threadIdx.x == 0) *a.sorted = 1;
     // ids that begin in one piece and go on into the next; the order of the list says nothing
     const uint32_t *const keys = a.key[(a.passes + 1) & 1];
     for (int64_t piece = rank * SORT_THREADS + threadIdx.x; piece + 1 < a.pieces; piece += CLUSTER * SORT_THREADS) {
@@ -261,7 +269,7 @@ template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad
     Eight<TO> e;
     float x[8];
     e.zero();
-    if (a.accumulate) e.template load<true, WIDE>(row, c);
+    if (a.accumulate) e.template load<true>(row, c);
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = a.accumulate ? fmaf(a.scale, sum[i], e.get(i)) : a.scale * sum[i];
     e.set(x);
@@ -270,6 +278,10 @@ template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad
 
 template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
     pdl_wait();
+    if (blockIdx.x >= a.pieces * a.across) {
+        clear_rows<TO, false>(a);
+        return;
+    }
     const uint32_t *const keys = a.key[(a.passes + 1) & 1], *const places = a.place[(a.passes + 1) & 1];
     __shared__ uint32_t key[PIECE + 2], place[PIECE];
     const uint32_t piece = blockIdx.x / a.across;
@@ -282,7 +294,7 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
     }
     if (threadIdx.x < count) place[threadIdx.x] = places[p0 + threadIdx.x];
     __syncthreads();
-    const Columns<WIDE> c((int64_t)(blockIdx.x % a.across) * SUM_THREADS + threadIdx.x, a.dim);
+    const Columns<WIDE> c(blockIdx.x % a.across * SUM_THREADS + threadIdx.x, (uint32_t)a.dim);
     if (!c.any()) return;
     float sum[8] = {};
     bool begun = key[0] != key[1];  // the current id's places begin inside this piece
@@ -290,7 +302,7 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
         Eight<T> e[AHEAD];
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u)
-            if (k0 + u < count && key[k0 + u + 1] < a.vocab) e[u].template load<true, WIDE>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride, c);
+            if (k0 + u < count && key[k0 + u + 1] < a.vocab) e[u].template load<true>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride, c);
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int k = k0 + u;
@@ -349,7 +361,7 @@ template <typename TO> __global__ void __launch_bounds__(JOIN_THREADS) join_piec
 template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream) {
     if (int rc = allow_smem<mark_ids>(MARK_SMEM)) return rc;
     if (int rc = allow_smem<sort_ids<TO>>(SORT_SMEM)) return rc;
-    const uint64_t grid = (uint64_t)a.pieces * a.across;
+    const uint64_t grid = (uint64_t)a.pieces * a.across + (a.accumulate ? 0 : 4 * SMS);
     if (grid > 0x7FFFFFFFull) return SCOUT_ERR_UNSUPPORTED;
     if (!a.accumulate) {
         mark_ids<<<(a.vocab + MARKED - 1) / MARKED, SORT_THREADS, (std::min<uint32_t>(a.vocab, MARKED) + 31) / 32 * 4, stream>>>(a);
@@ -452,7 +464,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     uint8_t *const ws = (uint8_t *)workspace;
     a.ids = ids, a.dy = dy, a.table = d_table;
     for (int i = 0; i < 2; ++i) a.key[i] = (uint32_t *)(ws + need.key[i]), a.place[i] = (uint32_t *)(ws + need.place[i]);
-    a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.cleared = a.across_count + 1, a.part = (float *)(ws + need.part);
+    a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.cleared = a.across_count + 1, a.sorted = a.across_count + 2, a.part = (float *)(ws + need.part);
     a.dy_stride = (int64_t)dy_stride, a.table_stride = (int64_t)d_table_stride, a.rows = (int64_t)rows, a.dim = (int64_t)dim;
     a.vocab = (uint32_t)vocab, a.pieces = (uint32_t)((rows + PIECE - 1) / PIECE), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
     int bits = 1;

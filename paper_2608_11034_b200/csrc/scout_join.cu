@@ -41,115 +41,115 @@ __device__ __forceinline__ float team_sum(float x, float *slots, int warps, int 
     __syncthreads();
     return warp_sum((t & 31) < warps ? slots[t & 31] : 0.f);
 }
-// Pairs of weights, or what stands for none.
-template <typename TW, bool WIDE> __device__ __forceinline__ void weights(tc::F2 (&w)[4], const void *row, const Columns<WIDE> &c) {
-    if (!row) {
+// Weights, or what stands for none.
+template <typename TW, bool WIDE, bool FULL> __device__ __forceinline__ void weights(float (&w)[8], const void *row, const Columns<WIDE, FULL> &c) {
+    if (!FULL && !row) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) w[i] = tc::f2(1.f, 1.f);
+        for (int i = 0; i < 8; ++i) w[i] = 1.f;
         return;
     }
     Eight<TW> e;
-    e.zero();
-    e.template load<false, WIDE>(reinterpret_cast<const TW *>(row), c);
+    if (!FULL) e.zero();
+    e.template load<false>(reinterpret_cast<const TW *>(row), c);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) w[i] = e.pair(i);
+    for (int i = 0; i < 8; ++i) w[i] = e.get(i);
 }
 template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, uint32_t group) {
     return a.gate ? reinterpret_cast<const TW *>(a.gate) + (int64_t)group * a.dim : nullptr;
 }
 __device__ __forceinline__ uint32_t group_of(const Args &a, int64_t row) { return a.group_rows == a.rows ? 0 : (uint32_t)row / (uint32_t)a.group_rows; }
 // rows and strides are below 2^32: one product
-template <typename T> __device__ __forceinline__ const T *row_of(const void *p, uint32_t stride, int64_t row) {
-    return reinterpret_cast<const T *>(p) + (uint64_t)(uint32_t)row * stride;
-}
-template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t stride, int64_t row) { return reinterpret_cast<T *>(p) + (uint64_t)(uint32_t)row * stride; }
-__device__ __forceinline__ tc::F2 both(float x) { return tc::f2(x, x); }
-__device__ __forceinline__ float add_pairs(const tc::F2 &x) {
-    const float2 f = tc::split(x);
-    return f.x + f.y;
-}
+template <typename T> __device__ __forceinline__ const T *row_of(const void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<const T *>(p) + (uint64_t)row * stride; }
+template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<T *>(p) + (uint64_t)row * stride; }
 
 // The next row's elements are fetched into the registers of the present one's as soon as those are free: b once it is widened, x once y
-// is made.
-template <typename TB, typename TS, typename TW, int V, bool WIDE>
+// is made.  FULL: every operand is there and the threads' columns are the row's, so that nothing is asked on the way (16384 x 4096 in
+// bf16 with every part, against the same without FULL: forward FULL_F, backward FULL_B us).
+template <typename TB, typename TS, typename TW, int V, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __grid_constant__ Args a) {
+    using Cols = Columns<WIDE, FULL>;
     __shared__ float slots[2][MOST<V> / 32];
-    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
+    const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
-    const int64_t stride = (int64_t)gridDim.x * a.teams;
-    int64_t row = (int64_t)blockIdx.x * a.teams + team;
+    const bool post = FULL || a.post, norm = FULL || a.norm;
+    const uint32_t stride = gridDim.x * a.teams, most = (uint32_t)(a.rows - 1);
     Eight<TB> b[V];
     Eight<TS> x[V];
     // past the end the last row again, for nothing
     const auto fetch_b = [&](int64_t at) {
+        const TB *const p = row_of<TB>(a.b, a.b_stride, (uint32_t)min(at, (int64_t)most));
 #pragma unroll
-        for (int v = 0; v < V; ++v) b[v].template load<true, WIDE>(row_of<TB>(a.b, a.b_stride, min(at, a.rows - 1)), Columns<WIDE>(t + v * a.team, a.dim));
+        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim));
     };
     const auto fetch_x = [&](int64_t at) {
-        if (a.x)
+        if (!FULL && !a.x) return;
+        const TS *const p = row_of<TS>(a.x, a.x_stride, (uint32_t)min(at, (int64_t)most));
 #pragma unroll
-            for (int v = 0; v < V; ++v) x[v].template load<true, WIDE>(row_of<TS>(a.x, a.x_stride, min(at, a.rows - 1)), Columns<WIDE>(t + v * a.team, a.dim));
+        for (int v = 0; v < V; ++v) x[v].template load<true>(p, Cols(t + v * a.team, a.dim));
     };
 #pragma unroll
     for (int v = 0; v < V; ++v) b[v].zero(), x[v].zero();
+    int64_t row = (int64_t)blockIdx.x * a.teams + team;
     fetch_b(row), fetch_x(row);
     for (; row - team < a.rows; row += stride) {  // the same for all teams of a block
         const bool on = row < a.rows;
-        tc::F2 u[V][4], sq = both(0.f);
+        float u[V][8], sq = 0.f;
 #pragma unroll
         for (int v = 0; v < V; ++v)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) u[v][i] = b[v].pair(i), sq = tc::fma2(u[v][i], u[v][i], sq);
+            for (int i = 0; i < 8; ++i) u[v][i] = b[v].get(i), sq = fmaf(u[v][i], u[v][i], sq);
         fetch_b(row + stride);
         float rb = 0.f, ry = 0.f;
-        if (a.post) rb = rsqrtf(team_sum(add_pairs(sq), s0, warps, t) * a.inv_dim + a.eps);
-        sq = both(0.f);
-        const void *const gate = gate_row<TW>(a, group_of(a, min(row, a.rows - 1)));
+        if (post) rb = rsqrtf(team_sum(sq, s0, warps, t) * a.inv_dim + a.eps);
+        sq = 0.f;
+        const void *const gate = gate_row<TW>(a, group_of(a, min(row, (int64_t)most)));
+        TS *const y_row = row_of<TS>(a.y, a.y_stride, (uint32_t)row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Columns<WIDE> c(t + v * a.team, a.dim);
-            tc::F2 w[4];
-            if (a.post) {
-                weights<TW, WIDE>(w, a.post, c);
+            const Cols c(t + v * a.team, a.dim);
+            float w[8];
+            if (post) {
+                weights<TW>(w, a.post, c);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) u[v][i] = tc::mul2(u[v][i], tc::mul2(both(rb), w[i]));
+                for (int i = 0; i < 8; ++i) u[v][i] *= rb * w[i];
             }
             if (a.drop.cut) {
                 const Keep<WIDE> keep(a.drop, t + v * a.team, (uint32_t)row, offset);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) u[v][i] = keep.of(i, tc::mul2(u[v][i], both(a.drop.factor)));
+                for (int i = 0; i < 8; ++i) u[v][i] = keep[i] ? u[v][i] * a.drop.factor : 0.f;  // 0 whatever it was
             }
-            weights<TW, WIDE>(w, gate, c);
+            weights<TW>(w, gate, c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                u[v][i] = tc::fma2(tc::mul2(both(a.scale), w[i]), u[v][i], x[v].pair(i));
-                sq = tc::fma2(u[v][i], u[v][i], sq);
+            for (int i = 0; i < 8; ++i) {
+                u[v][i] = fmaf(a.scale * w[i], u[v][i], x[v].get(i));
+                sq = fmaf(u[v][i], u[v][i], sq);
             }
             if (on) {
                 Eight<TS> y;
                 y.set(u[v]);
-                y.store(row_of<TS>(a.y, a.y_stride, row), c);
+                y.store(y_row, c);
             }
         }
         fetch_x(row + stride);
-        if (a.norm) {
-            ry = rsqrtf(team_sum(add_pairs(sq), s1, warps, t) * a.inv_dim + a.eps);
+        if (norm) {
+            ry = rsqrtf(team_sum(sq, s1, warps, t) * a.inv_dim + a.eps);
+            TB *const n_row = row_of<TB>(a.n, a.n_stride, (uint32_t)row);
             if (on)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const Columns<WIDE> c(t + v * a.team, a.dim);
-                    tc::F2 w[4];
-                    weights<TW, WIDE>(w, a.norm, c);
+                    const Cols c(t + v * a.team, a.dim);
+                    float w[8];
+                    weights<TW>(w, a.norm, c);
                     Eight<TB> n;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) w[i] = tc::mul2(w[i], tc::mul2(u[v][i], both(ry)));
+                    for (int i = 0; i < 8; ++i) w[i] *= u[v][i] * ry;
                     n.set(w);
-                    n.store(row_of<TB>(a.n, a.n_stride, row), c);
+                    n.store(n_row, c);
                 }
         }
         if (t == 0 && on) a.stats[row] = rb, a.stats[a.rows + row] = ry;
-        if (!(a.post && a.norm) && warps > 1) __syncthreads();  // the one set of slots is written again by the next row
+        if (!(post && norm) && warps > 1) __syncthreads();  // the one set of slots is written again by the next row
     }
 }
 
@@ -159,30 +159,25 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
 // when a gate's rows (or the run) end, in shared memory.
 template <int V> struct Sums {
     static constexpr bool REGS = V == 2;
-    tc::F2 r[REGS ? 2 : 1][REGS ? V : 1][4];
-    float2 *s;  // [1 or 3][V * 4][threads], a thread's own places; the first is d_post's
+    float r[REGS ? 2 : 1][REGS ? V : 1][8];
+    float *s;  // [1 or 3][V * 8][threads], a thread's own places; the first is d_post's
     int threads, t;
-    __device__ __forceinline__ float2 &at(int which, int v, int i) const { return s[((which * V + v) * 4 + i) * threads + t]; }
-    __device__ __forceinline__ tc::F2 get(int which, int v, int i) const {
-        if (REGS && which > 0) return r[which - 1][v][i];
-        const float2 f = at(which, v, i);
-        return tc::f2(f.x, f.y);
+    __device__ __forceinline__ float &at(int which, int v, int i) {
+        if (REGS && which > 0) return r[which - 1][REGS ? v : 0][i];
+        return s[((which * V + v) * 8 + i) * threads + t];
     }
-    __device__ __forceinline__ void set(int which, int v, int i, tc::F2 x) {
-        if (REGS && which > 0) r[which - 1][v][i] = x;
-        else at(which, v, i) = tc::split(x);
-    }
-    __device__ __forceinline__ void add(int which, int v, int i, tc::F2 x, tc::F2 y) { set(which, v, i, tc::fma2(x, y, get(which, v, i))); }
 };
 enum { D_POST, GATE_SUM, D_NORM };
 
-template <typename TB, typename TS, typename TW, int V, bool WIDE>
+template <typename TB, typename TS, typename TW, int V, bool WIDE, bool FULL>
 __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const __grid_constant__ Args a) {
+    using Cols = Columns<WIDE, FULL>;
     __shared__ float slots[2][MOST<V> / 32];
-    extern __shared__ float2 sums[];
-    const int t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
+    extern __shared__ float sums[];
+    const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
+    const bool post = FULL || a.post, has_dn = FULL || a.dn;
     const int64_t slab = (int64_t)blockIdx.x * a.teams + team, first = slab * a.per, last = min(first + a.per, a.rows);
     Sums<V> acc;
     acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
@@ -192,122 +187,122 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
     for (int v = 0; v < V; ++v) {
         y[v].zero(), g0[v].zero(), n[v].zero(), b[v].zero();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) acc.set(D_POST, v, i, both(0.f)), acc.set(GATE_SUM, v, i, both(0.f)), acc.set(D_NORM, v, i, both(0.f));
+        for (int i = 0; i < 8; ++i) acc.at(D_POST, v, i) = acc.at(GATE_SUM, v, i) = acc.at(D_NORM, v, i) = 0.f;
     }
     float rb = 1.f, ry = 0.f;
+    const uint32_t most = (uint32_t)(a.rows - 1);
     // past the end the last row again, for nothing
     const auto fetch = [&](int64_t at) {
-        const int64_t row = min(at, a.rows - 1);
+        const uint32_t row = (uint32_t)min(at, (int64_t)most);
+        const TS *const py = row_of<TS>(a.yin, a.y_stride, row), *const pg = row_of<TS>(a.dy, a.dy_stride, row);
+        const TB *const pn = row_of<TB>(a.dn, a.dn_stride, row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Columns<WIDE> c(t + v * a.team, a.dim);
-            if (a.dn) {
-                y[v].template load<true, WIDE>(row_of<TS>(a.yin, a.y_stride, row), c);
-                n[v].template load<true, WIDE>(row_of<TB>(a.dn, a.dn_stride, row), c);
-            }
-            if (a.dy) g0[v].template load<true, WIDE>(row_of<TS>(a.dy, a.dy_stride, row), c);
+            const Cols c(t + v * a.team, a.dim);
+            if (has_dn) y[v].template load<true>(py, c), n[v].template load<true>(pn, c);
+            if (FULL || a.dy) g0[v].template load<true>(pg, c);
         }
-        if (a.dn) ry = a.stats_in[a.rows + row];
+        if (has_dn) ry = a.stats_in[a.rows + row];
     };
     const auto fetch_b = [&](int64_t at) {
-        const int64_t row = min(at, a.rows - 1);
+        const uint32_t row = (uint32_t)min(at, (int64_t)most);
+        const TB *const p = row_of<TB>(a.b, a.b_stride, row);
 #pragma unroll
-        for (int v = 0; v < V; ++v) b[v].template load<true, WIDE>(row_of<TB>(a.b, a.b_stride, row), Columns<WIDE>(t + v * a.team, a.dim));
-        if (a.post) rb = a.stats_in[row];
+        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim));
+        if (post) rb = a.stats_in[row];
     };
-    uint32_t group = group_of(a, min(first, a.rows - 1));
+    uint32_t group = group_of(a, min(first, (int64_t)most));
     int64_t group_end = (group + 1ll) * a.group_rows, begun = first;  // where the gate's current sum began
     const float factor = a.scale * (a.drop.cut ? a.drop.factor : 1.f);
     fetch(first), fetch_b(first);
     for (int64_t it = 0; it < a.per; ++it) {
         const int64_t row = first + it;
         const bool on = row < last;
-        tc::F2 g[V][4], d = both(0.f);
-        if (a.dn) {
+        float g[V][8], d = 0.f;
+        if (has_dn) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                weights<TW, WIDE>(g[v], a.norm, Columns<WIDE>(t + v * a.team, a.dim));
+                weights<TW>(g[v], a.norm, Cols(t + v * a.team, a.dim));
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const tc::F2 z = tc::mul2(y[v].pair(i), both(ry)), dn = n[v].pair(i);
-                    g[v][i] = tc::mul2(dn, g[v][i]);
-                    if (on) acc.add(D_NORM, v, i, dn, z);
-                    d = tc::fma2(g[v][i], z, d);
+                for (int i = 0; i < 8; ++i) {
+                    const float z = y[v].get(i) * ry, dn = n[v].get(i);
+                    g[v][i] *= dn;
+                    if (on) acc.at(D_NORM, v, i) = fmaf(dn, z, acc.at(D_NORM, v, i));
+                    d = fmaf(g[v][i], z, d);
                 }
             }
-            const float pull = -(team_sum(add_pairs(d), s0, warps, t) * a.inv_dim) * ry;
+            const float pull = -(team_sum(d, s0, warps, t) * a.inv_dim) * ry;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) g[v][i] = tc::fma2(both(ry), tc::fma2(both(pull), y[v].pair(i), g[v][i]), g0[v].pair(i));
+                for (int i = 0; i < 8; ++i) g[v][i] = fmaf(ry, fmaf(pull, y[v].get(i), g[v][i]), g0[v].get(i));
         } else {
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) g[v][i] = g0[v].pair(i);
+                for (int i = 0; i < 8; ++i) g[v][i] = g0[v].get(i);
         }
         if (it + 1 < a.per) fetch(row + 1);
-        d = both(0.f);
+        d = 0.f;
+        TS *const dx_row = row_of<TS>(a.dx, a.dx_stride, (uint32_t)row);
+        const void *const gates = gate_row<TW>(a, group);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Columns<WIDE> c(t + v * a.team, a.dim);
-            if (a.dx && on) {
+            const Cols c(t + v * a.team, a.dim);
+            if ((FULL || a.dx) && on) {
                 Eight<TS> e;
                 e.set(g[v]);
-                e.store(row_of<TS>(a.dx, a.dx_stride, row), c);
+                e.store(dx_row, c);
             }
             Keep<WIDE> keep;
+            keep.all();
             if (a.drop.cut) keep = Keep<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset);
-            tc::F2 w[4], gate[4];
-            weights<TW, WIDE>(w, a.post, c);
-            weights<TW, WIDE>(gate, gate_row<TW>(a, group), c);
-            if (!on) continue;
+            float w[8], gate[8];
+            weights<TW>(w, a.post, c);
+            weights<TW>(gate, gates, c);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                tc::F2 cb = tc::mul2(b[v].pair(i), both(rb)), h = tc::mul2(g[v][i], both(factor));
-                if (a.drop.cut) cb = keep.of(i, cb), h = keep.of(i, h);  // what was dropped is 0 in both, whatever it was
-                acc.add(GATE_SUM, v, i, h, cb);
-                g[v][i] = tc::mul2(h, tc::mul2(gate[i], w[i]));
-                d = tc::fma2(g[v][i], cb, d);
+            for (int i = 0; i < 8; ++i) {
+                // what was dropped is 0 in both, whatever it was
+                const float cb = on && keep[i] ? b[v].get(i) * rb : 0.f, h = on && keep[i] ? g[v][i] * factor : 0.f;
+                acc.at(GATE_SUM, v, i) = fmaf(h, cb, acc.at(GATE_SUM, v, i));
+                g[v][i] = h * (gate[i] * w[i]);
+                d = fmaf(g[v][i], cb, d);
             }
         }
         float pull = 0.f;
-        if (a.post) pull = -(team_sum(add_pairs(d), s1, warps, t) * a.inv_dim) * rb;
+        if (post) pull = -(team_sum(d, s1, warps, t) * a.inv_dim) * rb;
         if (on) {
+            TB *const db_row = row_of<TB>(a.db, a.db_stride, (uint32_t)row);
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                if (a.post) {
+                if (post) {
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) g[v][i] = tc::mul2(both(rb), tc::fma2(both(pull), b[v].pair(i), g[v][i]));
+                    for (int i = 0; i < 8; ++i) g[v][i] = rb * fmaf(pull, b[v].get(i), g[v][i]);
                 }
                 Eight<TB> e;
                 e.set(g[v]);
-                e.store(row_of<TB>(a.db, a.db_stride, row), Columns<WIDE>(t + v * a.team, a.dim));
+                e.store(db_row, Cols(t + v * a.team, a.dim));
             }
         }
         if (it + 1 < a.per) fetch_b(row + 1);
-        if (!(a.post && a.dn) && warps > 1) __syncthreads();
+        if (!(post && has_dn) && warps > 1) __syncthreads();
         // the gate's sum ends with its group or with the run
         if (on && (row + 1 == last || row + 1 == group_end)) {
             const bool whole = begun + a.group_rows == group_end && row + 1 == group_end;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Columns<WIDE> c(t + v * a.team, a.dim);
-                tc::F2 w[4], gate[4];
-                weights<TW, WIDE>(w, a.post, c);
-                weights<TW, WIDE>(gate, gate_row<TW>(a, group), c);
+                const Cols c(t + v * a.team, a.dim);
+                float w[8], gate[8];
+                weights<TW>(w, a.post, c);
+                weights<TW>(gate, gates, c);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
-                    const float2 f = tc::split(tc::mul2(w[i >> 1], acc.get(GATE_SUM, v, i >> 1)));
-                    const float x = i & 1 ? f.y : f.x;
+                    const float sum = acc.at(GATE_SUM, v, i);
+                    acc.at(D_POST, v, i) = fmaf(gate[i], sum, acc.at(D_POST, v, i));
+                    acc.at(GATE_SUM, v, i) = 0.f;
                     if (!a.d_gate || !c.has(i)) continue;
-                    if (whole) reinterpret_cast<TW *>(a.d_gate)[(int64_t)group * a.dim + c.col(i)] = down<TW>(x);
-                    else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = x;
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    acc.add(D_POST, v, i, gate[i], acc.get(GATE_SUM, v, i));
-                    acc.set(GATE_SUM, v, i, both(0.f));
+                    if (whole) reinterpret_cast<TW *>(a.d_gate)[(int64_t)group * a.dim + c.col(i)] = down<TW>(w[i] * sum);
+                    else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = w[i] * sum;
                 }
             }
             begun = row + 1;
@@ -318,13 +313,12 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
     if (first < last) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Columns<WIDE> c(t + v * a.team, a.dim);
+            const Cols c(t + v * a.team, a.dim);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                const float2 p = tc::split(acc.get(D_POST, v, i >> 1)), q = tc::split(acc.get(D_NORM, v, i >> 1));
                 if (!c.has(i)) continue;
-                if (a.d_post) a.part[slab * 2 * a.dim + c.col(i)] = i & 1 ? p.y : p.x;
-                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = i & 1 ? q.y : q.x;
+                if (a.d_post) a.part[slab * 2 * a.dim + c.col(i)] = acc.at(D_POST, v, i);
+                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = acc.at(D_NORM, v, i);
             }
         }
     }
@@ -367,6 +361,7 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
 // How rows are dealt out.
 struct Shape {
     int v, team, teams, blocks;  // of an SM
+    bool full;                   // the team's columns are the row's
     int64_t slabs, per;
 };
 Shape shape(uint64_t rows, uint64_t dim, bool backward) {
@@ -375,6 +370,7 @@ Shape shape(uint64_t rows, uint64_t dim, bool backward) {
     s.v = eights > 2 * MOST<2> ? 4 : 2;
     s.team = (eights / s.v + 31) / 32 * 32;
     s.teams = std::max(1, 128 / s.team);
+    s.full = (uint64_t)s.team * s.v * 8 == dim;
     s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / (s.team * s.teams)) : 1;
     const int64_t want = (int64_t)SMS * s.blocks * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);
@@ -386,7 +382,9 @@ template <typename TB, typename TS, typename TW, bool WIDE> int run_forward(Args
     const Shape s = shape(a.rows, a.dim, false);
     a.team = s.team, a.teams = s.teams;
     const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks);
-    (s.v == 2 ? join_forward<TB, TS, TW, 2, WIDE> : join_forward<TB, TS, TW, 4, WIDE>)<<<grid, s.team * s.teams, 0, stream>>>(a);
+    const auto kernel = s.v == 4 ? join_forward<TB, TS, TW, 4, WIDE, false>
+                        : WIDE && s.full && a.x && a.gate && a.post && a.norm ? join_forward<TB, TS, TW, 2, true, true> : join_forward<TB, TS, TW, 2, WIDE, false>;
+    kernel<<<grid, s.team * s.teams, 0, stream>>>(a);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
@@ -396,10 +394,11 @@ template <typename TB, typename TS, typename TW, bool WIDE> int run_backward(Arg
     a.team = s.team, a.teams = s.teams, a.per = s.per, a.slabs = s.slabs;
     const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams);
     if (s.v == 2) {
-        join_backward<TB, TS, TW, 2, WIDE><<<grid, s.team * s.teams, 2 * 4 * 8 * s.team * s.teams, stream>>>(a);
+        const auto kernel = WIDE && s.full && a.dy && a.dn && a.gate && a.post && a.norm && a.dx ? join_backward<TB, TS, TW, 2, true, true> : join_backward<TB, TS, TW, 2, WIDE, false>;
+        kernel<<<grid, s.team * s.teams, 2 * 8 * 4 * s.team * s.teams, stream>>>(a);
     } else {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE>>(3 * 4 * 4 * 8 * MOST<4>)) return rc;
-        join_backward<TB, TS, TW, 4, WIDE><<<grid, s.team * s.teams, 3 * 4 * 4 * 8 * s.team * s.teams, stream>>>(a);
+        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE, false>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
+        join_backward<TB, TS, TW, 4, WIDE, false><<<grid, s.team * s.teams, 3 * 4 * 8 * 4 * s.team * s.teams, stream>>>(a);
     }
     SCOUT_CUDA(cudaGetLastError());
     if (!a.d_post && !a.d_norm && !a.d_gate) return SCOUT_OK;

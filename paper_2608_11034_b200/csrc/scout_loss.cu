@@ -489,18 +489,18 @@ template <typename T> __global__ void __launch_bounds__(256) join_states(const _
     const float ref = *a.g_ref * power2(-a.scale_log2);
     for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
         const int64_t t = q / per_row;
-        const Columns<true> at(q - t * per_row, a.dim);
+        const Columns<true> at((uint32_t)(q - t * per_row), (uint32_t)a.dim);
         const int m = a.where[t];
         float x[8] = {};
         if (m >= 0) {
             for (int s = 0; s < a.splits; ++s) {
                 Eight<float> e;
-                e.template load<true, true>(a.dxp + ((int64_t)s * a.padded + m) * a.dim, at);
+                e.template load<true>(a.dxp + ((int64_t)s * a.padded + m) * a.dim, at);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] += e.get(i);
             }
             Eight<T> w;
-            w.template load<false, true>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride, at);
+            w.template load<false>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride, at);
             const float rest = a.row_rest[m];
 #pragma unroll
             for (int i = 0; i < 8; ++i) x[i] = ref * fmaf(rest, w.get(i), x[i]);

@@ -7,7 +7,6 @@
 
 #include "scout_internal.h"
 #include "scout_step.h"
-#include "scout_tc.cuh"
 
 namespace scout {
 namespace step {
@@ -26,62 +25,55 @@ template <> __device__ __forceinline__ __half down<__half>(float x) { return __f
 // Which eight columns of a row a thread has.  Rows on 16-byte boundaries, whose length is a multiple of eight (WIDE): thread k has columns
 // 8 k .. 8 k + 7, in one or two accesses.  Other rows: the threads of a warp have its 256 columns in turn, element i of lane l being
 // column l + 32 i, so that each access of the warp is one piece of memory.  A row's dropout is made in eights either way (keep8).
-template <bool WIDE> struct Columns {
-    int64_t c0, dim;
-    __device__ __forceinline__ Columns(int64_t k, int64_t dim_) : c0(WIDE ? 8 * k : 256 * (k >> 5) + (k & 31)), dim(dim_) {}
-    __device__ __forceinline__ int64_t col(int i) const { return c0 + (WIDE ? i : 32 * i); }
-    __device__ __forceinline__ bool has(int i) const { return (WIDE ? c0 : c0 + 32 * i) < dim; }
-    __device__ __forceinline__ bool any() const { return c0 < dim; }
+// FULL: every thread's eight are inside the row.
+template <bool WIDE, bool FULL = false> struct Columns {
+    uint32_t c0, dim;  // below 2^31
+    __device__ __forceinline__ Columns(uint32_t k, uint32_t dim_) : c0(WIDE ? 8 * k : 256 * (k >> 5) + (k & 31)), dim(dim_) {}
+    __device__ __forceinline__ uint32_t col(int i) const { return c0 + (WIDE ? i : 32 * i); }
+    __device__ __forceinline__ bool has(int i) const { return FULL || (WIDE ? c0 : c0 + 32 * i) < dim; }
+    __device__ __forceinline__ bool any() const { return FULL || c0 < dim; }
 };
 
 // Eight elements of a row, as they lie in memory.  Where the row ends load leaves what was there: zeros, once zero() was called.
 template <typename T> struct Eight {
     static constexpr int N = sizeof(T) / 2;
     uint4 w[N];
-    __device__ __forceinline__ tc::F2 pair(int i) const {  // elements 2 i and 2 i + 1
+    __device__ __forceinline__ float get(int i) const {
         const uint32_t *v = reinterpret_cast<const uint32_t *>(w);
         if constexpr (sizeof(T) == 4) {
-            return tc::f2(__uint_as_float(v[2 * i]), __uint_as_float(v[2 * i + 1]));
+            return __uint_as_float(v[i]);
         } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-            return tc::f2(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xFFFF0000u));
+            return __uint_as_float(i & 1 ? v[i >> 1] & 0xFFFF0000u : v[i >> 1] << 16);
         } else {
-            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i]));
-            return tc::f2(f.x, f.y);
+            const float2 f = __half22float2(*reinterpret_cast<const __half2 *>(&v[i >> 1]));
+            return i & 1 ? f.y : f.x;
         }
-    }
-    __device__ __forceinline__ float get(int i) const {
-        const float2 f = tc::split(pair(i >> 1));
-        return i & 1 ? f.y : f.x;
     }
     __device__ __forceinline__ void zero() {
 #pragma unroll
         for (int i = 0; i < N; ++i) w[i] = make_uint4(0, 0, 0, 0);
     }
-    __device__ __forceinline__ void set_pair(int i, float lo, float hi) {
+    __device__ __forceinline__ void set(const float (&x)[8]) {
         uint32_t *v = reinterpret_cast<uint32_t *>(w);
         if constexpr (sizeof(T) == 4) {
-            v[2 * i] = __float_as_uint(lo), v[2 * i + 1] = __float_as_uint(hi);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v[i] = __float_as_uint(x[i]);
         } else if constexpr (std::is_same<T, __nv_bfloat16>::value) {
-            const __nv_bfloat162 p = __floats2bfloat162_rn(lo, hi);
-            v[i] = *reinterpret_cast<const uint32_t *>(&p);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(x[2 * i], x[2 * i + 1]);
+                v[i] = *reinterpret_cast<const uint32_t *>(&p);
+            }
         } else {
-            const __half2 p = __floats2half2_rn(lo, hi);
-            v[i] = *reinterpret_cast<const uint32_t *>(&p);
-        }
-    }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) set_pair(i, x[2 * i], x[2 * i + 1]);
-    }
-    __device__ __forceinline__ void set(const tc::F2 (&x)[4]) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float2 f = tc::split(x[i]);
-            set_pair(i, f.x, f.y);
+            for (int i = 0; i < 4; ++i) {
+                const __half2 p = __floats2half2_rn(x[2 * i], x[2 * i + 1]);
+                v[i] = *reinterpret_cast<const uint32_t *>(&p);
+            }
         }
     }
     // STREAM: read once
-    template <bool STREAM, bool WIDE> __device__ __forceinline__ void load(const T *row, const Columns<WIDE> &c) {
+    template <bool STREAM, bool WIDE, bool FULL> __device__ __forceinline__ void load(const T *row, const Columns<WIDE, FULL> &c) {
         if constexpr (WIDE) {
             if (c.any())
 #pragma unroll
@@ -103,7 +95,7 @@ template <typename T> struct Eight {
             }
         }
     }
-    template <bool WIDE> __device__ __forceinline__ void store(T *row, const Columns<WIDE> &c) const {
+    template <bool WIDE, bool FULL> __device__ __forceinline__ void store(T *row, const Columns<WIDE, FULL> &c) const {
         if constexpr (WIDE) {
             if (c.any())
 #pragma unroll
@@ -190,11 +182,6 @@ template <bool WIDE> struct Keep {
     __device__ __forceinline__ bool operator[](int i) const {
         if constexpr (WIDE) return (i & 1 ? w[i >> 1] : w[i >> 1] << 16) >= cut;
         else return (w[0] >> i) & 1u;
-    }
-    // pair i where kept, else 0 whatever it was
-    __device__ __forceinline__ tc::F2 of(int i, tc::F2 x) const {
-        const float2 f = tc::split(x);
-        return tc::f2((*this)[2 * i] ? f.x : 0.f, (*this)[2 * i + 1] ? f.y : 0.f);
     }
 };
 
