@@ -11,7 +11,7 @@ CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libscout_b200.so")
 SOURCES = ["scout_api.cu", "scout_sign.cu", "scout_one_launch.cu", "scout_noalloc.cu", "scout_vote.cu", "scout_timing.cu",
            "scout_attention.cu", "scout_attention_tc.cu", "scout_attention_bwd_tc.cu", "scout_checkpoint.cu", "scout_wgrad.cu", "scout_tc.cu",
-           "scout_embed.cu", "scout_dropout.cu", "scout_join.cu", "scout_loss.cu", "scout_ledger.cpp"]
+           "scout_embed.cu", "scout_dropout.cu", "scout_join.cu", "scout_join_ring.cu", "scout_loss.cu", "scout_ledger.cpp"]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17", "--threads", "0",
               "-Xcompiler", "-fPIC", "-Xcompiler", "-Wall", "-Xcompiler", "-fvisibility=hidden", "-Xlinker", "--exclude-libs,ALL"]
 
@@ -26,7 +26,7 @@ def _nvcc() -> str:
 def sources():
     srcs = [os.path.join(CSRC, s) for s in SOURCES]
     deps = srcs + [os.path.join(CSRC, h) for h in ("scout_internal.h", "scout_vote_device.cuh", "scout_scan.cuh", "scout_combine.cuh",
-                                                        "scout_attention.cuh", "scout_checkpoint.cuh", "scout_tc.cuh", "scout_step.cuh")] + \
+                                                        "scout_attention.cuh", "scout_checkpoint.cuh", "scout_tc.cuh", "scout_step.cuh", "scout_join.cuh")] + \
         [os.path.join(ROOT, "include", h) for h in sorted(os.listdir(os.path.join(ROOT, "include")))]
     return srcs, deps
 

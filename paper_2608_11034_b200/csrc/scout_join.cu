@@ -4,75 +4,28 @@
 // one team of warps, so that each tensor crosses memory once although a row's sums are needed twice, and the next row is fetched while
 // the present one is worked on.  Rows are dealt to teams: in turn (forward), in
 // runs (backward, whose column sums stay with the thread that owns the column for a whole run; runs meet in a second kernel, in order).
-#include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
-#include "scout_step.cuh"
+#include "scout_join.cuh"
+#include "scout_tc.cuh"
 
 namespace scout {
 namespace step {
+namespace join {
 namespace {
 
-constexpr int MAX_DIM = 16384;
-// A thread has V eights of a row: two up to 4096 columns, four beyond.
-template <int V> constexpr int MOST = V == 2 ? 256 : 512;  // threads of a block
-
-struct Args {
-    const void *x, *b, *dy, *dn, *yin, *gate, *post, *norm;
-    const float *stats_in;
-    void *y, *n, *dx, *db, *d_gate, *d_post, *d_norm;
-    float *stats;
-    float *part;       // [slabs][2][dim]: d_post, d_norm of a run of rows
-    float *part_gate;  // [slabs][2][dim]: d_gate of a group's part at the start of a run, and of one that begins inside it
-    uint32_t x_stride, b_stride, y_stride, n_stride, dy_stride, dn_stride, dx_stride, db_stride;
-    int64_t rows, group_rows, per, slabs;
-    int32_t dim, team, teams;  // threads of a team, teams of a block
-    float scale, eps, inv_dim;
-    bool wide;  // all rows, those of the weights too, on 16-byte boundaries and of whole eights
-    Drop drop;
-};
-
-// Sum over a team.  `slots`: the team's part of [teams][warps of a team] in shared memory, not written again before every thread has
-// passed another team_sum.
-__device__ __forceinline__ float team_sum(float x, float *slots, int warps, int t) {
-    x = warp_sum(x);
-    if (warps == 1) return x;
-    if ((t & 31) == 0) slots[t >> 5] = x;
-    __syncthreads();
-    return warp_sum((t & 31) < warps ? slots[t & 31] : 0.f);
-}
-// Weights, or what stands for none.
-template <typename TW, bool WIDE, bool FULL> __device__ __forceinline__ void weights(float (&w)[8], const void *row, const Columns<WIDE, FULL> &c) {
-    if (!FULL && !row) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = 1.f;
-        return;
-    }
-    Eight<TW> e;
-    if (!FULL) e.zero();
-    e.template load<false>(reinterpret_cast<const TW *>(row), c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) w[i] = e.get(i);
-}
-template <typename TW> __device__ __forceinline__ const void *gate_row(const Args &a, uint32_t group) {
-    return a.gate ? reinterpret_cast<const TW *>(a.gate) + (int64_t)group * a.dim : nullptr;
-}
-__device__ __forceinline__ uint32_t group_of(const Args &a, int64_t row) { return a.group_rows == a.rows ? 0 : (uint32_t)row / (uint32_t)a.group_rows; }
-// rows and strides are below 2^32: one product
-template <typename T> __device__ __forceinline__ const T *row_of(const void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<const T *>(p) + (uint64_t)row * stride; }
-template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<T *>(p) + (uint64_t)row * stride; }
-
+// ---- rows in registers: off 16-byte boundaries, or wider than 4096 ----------------------------------------------------
 // The next row's elements are fetched into the registers of the present one's as soon as those are free: b once it is widened, x once y
-// is made.  FULL: every operand is there and the threads' columns are the row's, so that nothing is asked on the way (16384 x 4096 in
-// bf16 with every part, against the same without FULL: forward FULL_F, backward FULL_B us).
-template <typename TB, typename TS, typename TW, int V, bool WIDE, bool FULL>
+// is made.
+template <typename TB, typename TS, typename TW, int V, bool WIDE>
 __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __grid_constant__ Args a) {
-    using Cols = Columns<WIDE, FULL>;
+    using Cols = Columns<WIDE>;
     __shared__ float slots[2][MOST<V> / 32];
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
-    const bool post = FULL || a.post, norm = FULL || a.norm;
+    const bool post = a.post, norm = a.norm;
     const uint32_t stride = gridDim.x * a.teams, most = (uint32_t)(a.rows - 1);
     Eight<TB> b[V];
     Eight<TS> x[V];
@@ -83,7 +36,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
         for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim));
     };
     const auto fetch_x = [&](int64_t at) {
-        if (!FULL && !a.x) return;
+        if (!a.x) return;
         const TS *const p = row_of<TS>(a.x, a.x_stride, (uint32_t)min(at, (int64_t)most));
 #pragma unroll
         for (int v = 0; v < V; ++v) x[v].template load<true>(p, Cols(t + v * a.team, a.dim));
@@ -101,7 +54,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
             for (int i = 0; i < 8; ++i) u[v][i] = b[v].get(i), sq = fmaf(u[v][i], u[v][i], sq);
         fetch_b(row + stride);
         float rb = 0.f, ry = 0.f;
-        if (post) rb = rsqrtf(team_sum(sq, s0, warps, t) * a.inv_dim + a.eps);
+        if (post) rb = rsqrtf(team_sum(sq, s0, warps, t, blockDim.x) * a.inv_dim + a.eps);
         sq = 0.f;
         const void *const gate = gate_row<TW>(a, group_of(a, min(row, (int64_t)most)));
         TS *const y_row = row_of<TS>(a.y, a.y_stride, (uint32_t)row);
@@ -133,7 +86,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
         }
         fetch_x(row + stride);
         if (norm) {
-            ry = rsqrtf(team_sum(sq, s1, warps, t) * a.inv_dim + a.eps);
+            ry = rsqrtf(team_sum(sq, s1, warps, t, blockDim.x) * a.inv_dim + a.eps);
             TB *const n_row = row_of<TB>(a.n, a.n_stride, (uint32_t)row);
             if (on)
 #pragma unroll
@@ -149,35 +102,19 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
                 }
         }
         if (t == 0 && on) a.stats[row] = rb, a.stats[a.rows + row] = ry;
-        if (!(post && norm) && warps > 1) __syncthreads();  // the one set of slots is written again by the next row
+        if (!(post && norm) && warps > 1) sync_some(blockDim.x);  // the one set of slots is written again by the next row
     }
 }
 
-// With h = scale g (masked) and c = b rms(b) (masked), du = h gate, and over the rows of one gate S = sum of h c gives both of
-//     d_gate = post S,   d_post = sum over gates of gate S,
-// so that a row adds to two column sums, S and d_norm: in registers, or beyond 4096 columns in shared memory.  d_post takes its part
-// when a gate's rows (or the run) end, in shared memory.
-template <int V> struct Sums {
-    static constexpr bool REGS = V == 2;
-    float r[REGS ? 2 : 1][REGS ? V : 1][8];
-    float *s;  // [1 or 3][V * 8][threads], a thread's own places; the first is d_post's
-    int threads, t;
-    __device__ __forceinline__ float &at(int which, int v, int i) {
-        if (REGS && which > 0) return r[which - 1][REGS ? v : 0][i];
-        return s[((which * V + v) * 8 + i) * threads + t];
-    }
-};
-enum { D_POST, GATE_SUM, D_NORM };
-
-template <typename TB, typename TS, typename TW, int V, bool WIDE, bool FULL>
+template <typename TB, typename TS, typename TW, int V, bool WIDE>
 __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const __grid_constant__ Args a) {
-    using Cols = Columns<WIDE, FULL>;
+    using Cols = Columns<WIDE>;
     __shared__ float slots[2][MOST<V> / 32];
     extern __shared__ float sums[];
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
-    const bool post = FULL || a.post, has_dn = FULL || a.dn;
+    const bool post = a.post, has_dn = a.dn;
     const int64_t slab = (int64_t)blockIdx.x * a.teams + team, first = slab * a.per, last = min(first + a.per, a.rows);
     Sums<V> acc;
     acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
@@ -200,7 +137,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
             if (has_dn) y[v].template load<true>(py, c), n[v].template load<true>(pn, c);
-            if (FULL || a.dy) g0[v].template load<true>(pg, c);
+            if (a.dy) g0[v].template load<true>(pg, c);
         }
         if (has_dn) ry = a.stats_in[a.rows + row];
     };
@@ -231,7 +168,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
                     d = fmaf(g[v][i], z, d);
                 }
             }
-            const float pull = -(team_sum(d, s0, warps, t) * a.inv_dim) * ry;
+            const float pull = -(team_sum(d, s0, warps, t, blockDim.x) * a.inv_dim) * ry;
 #pragma unroll
             for (int v = 0; v < V; ++v)
 #pragma unroll
@@ -249,7 +186,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
-            if ((FULL || a.dx) && on) {
+            if ((a.dx) && on) {
                 Eight<TS> e;
                 e.set(g[v]);
                 e.store(dx_row, c);
@@ -270,7 +207,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
             }
         }
         float pull = 0.f;
-        if (post) pull = -(team_sum(d, s1, warps, t) * a.inv_dim) * rb;
+        if (post) pull = -(team_sum(d, s1, warps, t, blockDim.x) * a.inv_dim) * rb;
         if (on) {
             TB *const db_row = row_of<TB>(a.db, a.db_stride, (uint32_t)row);
 #pragma unroll
@@ -285,7 +222,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
             }
         }
         if (it + 1 < a.per) fetch_b(row + 1);
-        if (!(post && has_dn) && warps > 1) __syncthreads();
+        if (!(post && has_dn) && warps > 1) sync_some(blockDim.x);
         // the gate's sum ends with its group or with the run
         if (on && (row + 1 == last || row + 1 == group_end)) {
             const bool whole = begun + a.group_rows == group_end && row + 1 == group_end;
@@ -358,53 +295,65 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
     }
 }
 
-// How rows are dealt out.
-struct Shape {
-    int v, team, teams, blocks;  // of an SM
-    bool full;                   // the team's columns are the row's
-    int64_t slabs, per;
-};
-Shape shape(uint64_t rows, uint64_t dim, bool backward) {
+// Bytes of a row in the ring.
+int ring_row(const scout_join_t *j, bool backward) { return (int)(j->dim * ((backward ? 2 : 1) * (size_of(j->stream_dtype) + size_of(j->dtype)))); }
+Shape shape(const scout_join_t *j, bool wide, bool backward) {
     Shape s = {};
+    const uint64_t rows = j->rows, dim = j->dim;
     const int eights = (int)((dim + 255) / 256 * 32);  // whole warps' worth
     s.v = eights > 2 * MOST<2> ? 4 : 2;
     s.team = (eights / s.v + 31) / 32 * 32;
     s.teams = std::max(1, 128 / s.team);
     s.full = (uint64_t)s.team * s.v * 8 == dim;
-    s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / (s.team * s.teams)) : 1;
+    const int threads = s.team * s.teams;
+    s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / threads) : 1;
+    if (wide && s.v == 2) {
+        // as many blocks as registers allow, or fewer, so that two rows of each team fit into shared memory; four at most
+        s.stage_bytes = s.teams * ring_row(j, backward);
+        for (;; --s.blocks) {
+            s.stages = std::min(4, ((227 << 10) / s.blocks - 1024 - 256 - (backward ? threads * 64 : 0)) / s.stage_bytes);
+            if (s.stages >= 2 || s.blocks == 1) break;
+        }
+    }
     const int64_t want = (int64_t)SMS * s.blocks * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);
     s.slabs = ((int64_t)rows + s.per - 1) / s.per;
     return s;
 }
+// the runs of the backward pass are at most these, whatever the operands lie on
+int64_t most_slabs(const scout_join_t *j) { return std::max(shape(j, false, true).slabs, shape(j, true, true).slabs); }
 
-template <typename TB, typename TS, typename TW, bool WIDE> int run_forward(Args &a, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim, false);
-    a.team = s.team, a.teams = s.teams;
+template <typename TB, typename TS, typename TW> int run_forward(Args &a, const Shape &s, cudaStream_t stream) {
     const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks);
-    const auto kernel = s.v == 4 ? join_forward<TB, TS, TW, 4, WIDE, false>
-                        : WIDE && s.full && a.x && a.gate && a.post && a.norm ? join_forward<TB, TS, TW, 2, true, true> : join_forward<TB, TS, TW, 2, WIDE, false>;
+    const auto kernel = s.v == 2 ? join_forward<TB, TS, TW, 2, false> : a.wide ? join_forward<TB, TS, TW, 4, true> : join_forward<TB, TS, TW, 4, false>;
     kernel<<<grid, s.team * s.teams, 0, stream>>>(a);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
-
-template <typename TB, typename TS, typename TW, bool WIDE> int run_backward(Args &a, int64_t groups, cudaStream_t stream) {
-    const Shape s = shape(a.rows, a.dim, true);
-    a.team = s.team, a.teams = s.teams, a.per = s.per, a.slabs = s.slabs;
-    const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams);
+template <typename TB, typename TS, typename TW> int run_backward(Args &a, const Shape &s, cudaStream_t stream) {
+    const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams), threads = s.team * s.teams;
     if (s.v == 2) {
-        const auto kernel = WIDE && s.full && a.dy && a.dn && a.gate && a.post && a.norm && a.dx ? join_backward<TB, TS, TW, 2, true, true> : join_backward<TB, TS, TW, 2, WIDE, false>;
-        kernel<<<grid, s.team * s.teams, 2 * 8 * 4 * s.team * s.teams, stream>>>(a);
+        join_backward<TB, TS, TW, 2, false><<<grid, threads, 2 * 8 * 4 * threads, stream>>>(a);
+    } else if (a.wide) {
+        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, true>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
+        join_backward<TB, TS, TW, 4, true><<<grid, threads, 3 * 4 * 8 * 4 * threads, stream>>>(a);
     } else {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, WIDE, false>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
-        join_backward<TB, TS, TW, 4, WIDE, false><<<grid, s.team * s.teams, 3 * 4 * 8 * 4 * s.team * s.teams, stream>>>(a);
+        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, false>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
+        join_backward<TB, TS, TW, 4, false><<<grid, threads, 3 * 4 * 8 * 4 * threads, stream>>>(a);
     }
     SCOUT_CUDA(cudaGetLastError());
+    return SCOUT_OK;
+}
+template <typename TW> int run_columns(const Args &a, int64_t groups, cudaStream_t stream) {
     if (!a.d_post && !a.d_norm && !a.d_gate) return SCOUT_OK;
     const dim3 jg((unsigned)((a.dim + JOIN_COLS - 1) / JOIN_COLS), 2 + (unsigned)(a.d_gate ? std::min<int64_t>(groups, 1024) : 1));
     SCOUT_CUDA(launch_dependent(join_columns<TW>, jg, dim3(JOIN_COLS, JOIN_WAYS), stream, a, groups));
     return SCOUT_OK;
+}
+Types types_of(const scout_join_t *j) {
+    if (j->dtype == SCOUT_DT_F32) return ALL_F32;
+    const int wider = (j->stream_dtype == SCOUT_DT_F32 ? 2 : 0) + (j->weight_dtype == SCOUT_DT_F32 ? 1 : 0);
+    return (Types)((j->dtype == SCOUT_DT_BF16 ? BF16 : F16) + wider);
 }
 
 // calls f.template operator()<TB, TS, TW>() for the types of j
@@ -448,12 +397,14 @@ void describe(const scout_join_t *j, Args *a) {
 }
 
 }  // namespace
+}  // namespace join
 }  // namespace step
 }  // namespace scout
 
 extern "C" int scout_join_forward(const scout_join_t *j, const void *x, const void *b, const void *gate, const void *post, const void *norm,
                                   double p, uint64_t seed, uint64_t offset, const uint64_t *d_offset, void *y, void *n, float *stats, void *stream) {
     using namespace scout::step;
+    using namespace scout::step::join;
     if (int rc = check(j)) return rc;
     Args a = {};
     if (int rc = make_drop(p, seed, offset, d_offset, &a.drop)) return rc;
@@ -471,17 +422,22 @@ extern "C" int scout_join_forward(const scout_join_t *j, const void *x, const vo
     a.x = x, a.b = b, a.gate = gate, a.post = post, a.norm = norm, a.y = y, a.n = n, a.stats = stats;
     a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!x || wide_rows(x, j->x_stride, j->stream_dtype)) && wide_rows(b, j->b_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype) &&
              (!n || wide_rows(n, j->n_stride, j->dtype));
-    return by_types(*j, [&](auto tb, auto ts, auto tw) { 
-        const cudaStream_t s = (cudaStream_t)stream;
-        return a.wide ? run_forward<decltype(tb), decltype(ts), decltype(tw), true>(a, s) : run_forward<decltype(tb), decltype(ts), decltype(tw), false>(a, s);
-    });
+    const cudaStream_t on = (cudaStream_t)stream;
+    const Shape s = shape(j, a.wide, false);
+    a.team = s.team, a.teams = s.teams, a.stages = s.stages;
+    if (s.stages) {
+        if (int rc = scout::tc::gave_up_counter(&a.gave_up)) return rc;
+        return ring_forward(types_of(j), a, s, s.full && x && gate && post && norm, on);
+    }
+    return by_types(*j, [&](auto tb, auto ts, auto tw) { return run_forward<decltype(tb), decltype(ts), decltype(tw)>(a, s, on); });
 }
 
 extern "C" int scout_join_backward_workspace(const scout_join_t *j, uint64_t *bytes) {
     using namespace scout::step;
+    using namespace scout::step::join;
     if (!bytes) return SCOUT_ERR_INVALID;
     if (int rc = check(j)) return rc;
-    *bytes = (uint64_t)(shape(j->rows, j->dim, true).slabs * 4 * j->dim * 4 + 255) & ~255ull;
+    *bytes = (uint64_t)(most_slabs(j) * 4 * j->dim * 4 + 255) & ~255ull;
     return SCOUT_OK;
 }
 
@@ -490,6 +446,7 @@ extern "C" int scout_join_backward(const scout_join_t *j, const void *dy, const 
                                    const uint64_t *d_offset, void *dx, void *db, void *d_gate, void *d_post, void *d_norm, void *workspace,
                                    uint64_t workspace_bytes, void *stream) {
     using namespace scout::step;
+    using namespace scout::step::join;
     uint64_t bytes = 0;
     if (int rc = scout_join_backward_workspace(j, &bytes)) return rc;
     Args a = {};
@@ -520,12 +477,19 @@ extern "C" int scout_join_backward(const scout_join_t *j, const void *dy, const 
     a.dy = dy, a.dn = dn, a.b = b, a.yin = y, a.stats_in = stats, a.gate = gate, a.post = post, a.norm = norm;
     a.dx = dx, a.db = db, a.d_gate = d_gate, a.d_post = d_post, a.d_norm = d_norm;
     a.part = (float *)workspace;
-    a.part_gate = a.part + shape(j->rows, j->dim, true).slabs * 2 * (int64_t)j->dim;
+    a.part_gate = a.part + most_slabs(j) * 2 * (int64_t)j->dim;
     a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
              wide_rows(b, j->b_stride, j->dtype) && (!dx || wide_rows(dx, j->dx_stride, j->stream_dtype)) && wide_rows(db, j->db_stride, j->dtype);
-    return by_types(*j, [&](auto tb, auto ts, auto tw) {
-        const cudaStream_t s = (cudaStream_t)stream;
-        const int64_t groups = (int64_t)j->groups;
-        return a.wide ? run_backward<decltype(tb), decltype(ts), decltype(tw), true>(a, groups, s) : run_backward<decltype(tb), decltype(ts), decltype(tw), false>(a, groups, s);
-    });
+    const cudaStream_t on = (cudaStream_t)stream;
+    const Shape s = shape(j, a.wide, true);
+    a.team = s.team, a.teams = s.teams, a.stages = s.stages, a.per = s.per, a.slabs = s.slabs;
+    if (s.stages) {
+        if (int rc = scout::tc::gave_up_counter(&a.gave_up)) return rc;
+        if (int rc = ring_backward(types_of(j), a, s, s.full && dy && dn && gate && post && norm && dx, on)) return rc;
+    } else if (int rc = by_types(*j, [&](auto tb, auto ts, auto tw) { return run_backward<decltype(tb), decltype(ts), decltype(tw)>(a, s, on); })) {
+        return rc;
+    }
+    const int64_t groups = (int64_t)j->groups;
+    if (j->weight_dtype == SCOUT_DT_F32) return run_columns<float>(a, groups, on);
+    return j->weight_dtype == SCOUT_DT_BF16 ? run_columns<__nv_bfloat16>(a, groups, on) : run_columns<__half>(a, groups, on);
 }
