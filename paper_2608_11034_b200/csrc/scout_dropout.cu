@@ -1,7 +1,7 @@
 // Dropout with a mask that is made again from a counter wherever it is needed.
 //
 // Bound by memory (an element in, an element out); the generator costs 40 instructions for eight elements.  A thread takes eight
-// columns of a row at a time, two such units in flight.
+// columns of a row at a time, and the next ones are on their way while it makes their bits.
 #include <algorithm>
 
 #include "scout_step.cuh"
@@ -11,7 +11,7 @@ namespace step {
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int blocks(bool wide) { return wide ? 6 : 4; }  // of an SM
+constexpr int blocks(bool wide) { return wide ? 5 : 4; }  // of an SM
 
 struct Args {
     const void *x;
@@ -24,34 +24,42 @@ struct Args {
 };
 
 template <typename T, bool WIDE> __global__ void __launch_bounds__(THREADS, blocks(WIDE)) dropout(const __grid_constant__ Args a) {
-    constexpr int UNROLL = 2;
+    constexpr int UNROLL = sizeof(T) == 4 ? 1 : 2;
     const uint64_t offset = a.drop.at();
     const uint32_t stride = gridDim.x * THREADS, lane = threadIdx.x & 31;
-    // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop.
-    // Units are counted to 2^31, so that the sums here stay below 2^32.
-    for (uint32_t q0 = blockIdx.x * THREADS + threadIdx.x; q0 - lane < a.units; q0 += stride * UNROLL) {
-        Eight<T> e[UNROLL];
-        uint32_t row[UNROLL], k[UNROLL];
+    Eight<T> e[UNROLL], ahead[UNROLL];
+    uint32_t row[UNROLL], k[UNROLL], row_ahead[UNROLL], k_ahead[UNROLL];
+    const auto fetch = [&](Eight<T> (&to)[UNROLL], uint32_t (&r)[UNROLL], uint32_t (&c)[UNROLL], uint32_t q0) {
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint32_t q = q0 + u * stride;
-            row[u] = (__umulhi(q, a.mul) + q) >> a.shift;
-            k[u] = q - row[u] * a.per_row;
-            e[u].zero();
-            if (q < a.units) e[u].template load<true>(reinterpret_cast<const T *>(a.x) + row[u] * a.x_stride, Columns<WIDE>(k[u], a.cols));
+            r[u] = (__umulhi(q, a.mul) + q) >> a.shift;
+            c[u] = q - r[u] * a.per_row;
+            to[u].zero();
+            if (q < a.units) to[u].template load<true>(reinterpret_cast<const T *>(a.x) + r[u] * a.x_stride, Columns<WIDE>(c[u], a.cols));
         }
+    };
+    // a warp's units are 32 in turn, and per_row is a multiple of 32 where they have to be of one row: whole warps go on or stop.
+    // Units are counted to 2^31, so that the sums here stay below 2^32.
+    uint32_t q0 = blockIdx.x * THREADS + threadIdx.x;
+    fetch(e, row, k, q0);
+    for (; q0 - lane < a.units; q0 += stride * UNROLL) {
+        fetch(ahead, row_ahead, k_ahead, q0 + stride * UNROLL);
 #pragma unroll
         for (int u = 0; u < UNROLL; ++u) {
             const uint32_t q = q0 + u * stride;
             if (q - lane >= a.units) break;
             const Keep<WIDE> keep(a.drop, k[u], a.row0 + row[u], offset);
-            if (q >= a.units) continue;
-            float x[8];
+            if (q < a.units) {
+                float x[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = keep[i] ? e[u].get(i) * a.drop.factor : 0.f;  // 0 whatever it was
-            e[u].set(x);
-            e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.cols));
+                for (int i = 0; i < 8; ++i) x[i] = keep[i] ? e[u].get(i) * a.drop.factor : 0.f;  // 0 whatever it was
+                e[u].set(x);
+                e[u].store(reinterpret_cast<T *>(a.y) + row[u] * a.y_stride, Columns<WIDE>(k[u], a.cols));
+            }
         }
+#pragma unroll
+        for (int u = 0; u < UNROLL; ++u) e[u] = ahead[u], row[u] = row_ahead[u], k[u] = k_ahead[u];
     }
 }
 

@@ -5,7 +5,7 @@
 //   mark_ids     which ids occur (not where the gradient is added to one that is there)
 //   sort_ids     one cluster of eight blocks sorts (id, place) by id, places of an id staying in order (radix sort from the
 //                lowest digit, up to nine bits a pass); the other blocks write zeros to rows of ids that do not occur
-//   sum_places   the sorted places in pieces of PIECE: a thread adds up eight columns of a piece, writes what begins and ends
+//   sum_places   the sorted places in pieces of 32 or 64: a thread adds up eight columns of a piece, writes what begins and ends
 //                inside, and leaves what crosses a border in scratch
 //   join_pieces  adds the parts of an id that crosses borders, in order
 // Pieces of equal size keep one frequent id (a line break, say) from holding up the rest.
@@ -90,8 +90,7 @@ template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaS
 constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT, HELD = 4;
 constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4, FILL_CLUSTERS = SMS / CLUSTER - 1;
 constexpr int MARKED = 1 << 20, MARK_SMEM = MARKED / 8;  // ids of a block of mark_ids
-constexpr int CLEARED = 4;
-constexpr int PIECE = 32, AHEAD = 8, SUM_THREADS = 128;
+constexpr int LONG_PIECE = 64, AHEAD = 8, SUM_THREADS = 128;
 constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
 
 struct Grad {
@@ -104,6 +103,8 @@ struct Grad {
     float *part;                  // [pieces][2][dim]: what goes on from the piece before, and what goes on into the next one
     int64_t dy_stride, table_stride, rows, dim;
     uint32_t vocab, pieces, across;  // blocks of columns
+    uint32_t at_once;  // rows without a token that a warp takes
+    int piece;         // places of a piece
     int digit, passes, id64, wide, accumulate;
     float scale;
 };
@@ -138,16 +139,15 @@ template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_
     if (head + body * N + lane < dim) row[head + body * N + lane] = down<TO>(0.f);
 }
 
-// Rows of ids that do not occur, CLEARED at a time from a counter, so that the blocks need not all run at once; with UNTIL_SORTED a
-// warp leaves when the ids are sorted, and the rest is written beside the sums.
+// Rows of ids that do not occur, about 16 KiB at a time from a counter, so that the blocks need not all run at once; with UNTIL_SORTED a warp leaves when the ids are sorted, and the rest is written beside the sums.
 template <typename TO, bool UNTIL_SORTED> __device__ __forceinline__ void clear_rows(const Grad &a) {
     for (;;) {
         uint32_t v0 = 0;
-        if ((threadIdx.x & 31) == 0) v0 = UNTIL_SORTED && *reinterpret_cast<volatile uint32_t *>(a.sorted) ? a.vocab : atomicAdd(a.cleared, (uint32_t)CLEARED);
+        if ((threadIdx.x & 31) == 0) v0 = UNTIL_SORTED && *reinterpret_cast<volatile uint32_t *>(a.sorted) ? a.vocab : atomicAdd(a.cleared, a.at_once);
         v0 = __shfl_sync(0xFFFFFFFFu, v0, 0);
         if (v0 >= a.vocab) return;
-        const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // CLEARED divides 32
-        for (uint32_t i = 0; i < CLEARED && v0 + i < a.vocab; ++i)
+        const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // at_once divides 32
+        for (uint32_t i = 0; i < a.at_once && v0 + i < a.vocab; ++i)
             if (!((seen >> i) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, a.dim);
     }
 }
@@ -247,16 +247,16 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
     // ids that begin in one piece and go on into the next; the order of the list says nothing
     const uint32_t *const keys = a.key[(a.passes + 1) & 1];
     for (int64_t piece = rank * SORT_THREADS + threadIdx.x; piece + 1 < a.pieces; piece += CLUSTER * SORT_THREADS) {
-        const int64_t after = (piece + 1) * PIECE;
+        const int64_t after = (piece + 1) * a.piece;
         const uint32_t id = keys[after - 1];
-        if (id >= a.vocab || keys[after] != id || (piece > 0 && keys[piece * PIECE - 1] == id)) continue;
+        if (id >= a.vocab || keys[after] != id || (piece > 0 && keys[piece * a.piece - 1] == id)) continue;
         // the last piece whose first key is still this one: lo's is, hi's is not
         int64_t lo = piece + 1, hi = lo + 1;
-        for (; hi < a.pieces && keys[hi * PIECE] == id; hi = lo + 2 * (hi - piece)) lo = hi;
+        for (; hi < a.pieces && keys[hi * a.piece] == id; hi = lo + 2 * (hi - piece)) lo = hi;
         hi = min(hi, (int64_t)a.pieces);
         while (hi - lo > 1) {
             const int64_t mid = (lo + hi) / 2;
-            if (keys[mid * PIECE] == id) lo = mid;
+            if (keys[mid * a.piece] == id) lo = mid;
             else hi = mid;
         }
         a.across_list[atomicAdd(a.across_count, 1u)] = make_uint2((uint32_t)piece, (uint32_t)lo);
@@ -283,12 +283,12 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
         return;
     }
     const uint32_t *const keys = a.key[(a.passes + 1) & 1], *const places = a.place[(a.passes + 1) & 1];
-    __shared__ uint32_t key[PIECE + 2], place[PIECE];
+    __shared__ uint32_t key[LONG_PIECE + 2], place[LONG_PIECE];
     const uint32_t piece = blockIdx.x / a.across;
-    const int64_t p0 = (int64_t)piece * PIECE;
-    const int count = (int)min((long long)PIECE, (long long)a.rows - p0);
+    const int64_t p0 = (int64_t)piece * a.piece;
+    const int count = (int)min((long long)a.piece, (long long)a.rows - p0);
     // keys of the piece and its neighbours; outside, one that is nobody's
-    if (threadIdx.x < PIECE + 2) {
+    if (threadIdx.x < a.piece + 2) {
         const int64_t p = p0 + (int)threadIdx.x - 1;
         key[threadIdx.x] = p >= 0 && p < a.rows && p <= p0 + count ? keys[p] : 0xFFFFFFFFu;
     }
@@ -336,7 +336,7 @@ template <typename TO> __global__ void __launch_bounds__(JOIN_THREADS) join_piec
     const uint32_t count = *a.across_count;
     for (uint32_t k = blockIdx.y; k < count; k += gridDim.y) {
         const uint2 range = a.across_list[k];
-        const uint32_t key = a.key[(a.passes + 1) & 1][(int64_t)range.x * PIECE + PIECE - 1];
+        const uint32_t key = a.key[(a.passes + 1) & 1][((int64_t)range.x + 1) * a.piece - 1];
         float sum[4] = {};
 #pragma unroll 2
         for (int64_t p = range.x + way; p <= range.y; p += JOIN_WAYS)
@@ -367,6 +367,8 @@ template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream
         mark_ids<<<(a.vocab + MARKED - 1) / MARKED, SORT_THREADS, (std::min<uint32_t>(a.vocab, MARKED) + 31) / 32 * 4, stream>>>(a);
         SCOUT_CUDA(cudaGetLastError());
     }
+    a.at_once = 1;
+    while (a.at_once < 32 && 2 * a.at_once * a.dim * sizeof(TO) <= 16384) a.at_once *= 2;
     // as many clusters as rows without a token can need, a row to a warp
     const uint32_t fill = a.accumulate ? 0 : std::min<uint32_t>(FILL_CLUSTERS, (a.vocab + CLUSTER * SORT_WARPS - 1) / (CLUSTER * SORT_WARPS));
     cudaLaunchConfig_t cfg = {};
@@ -396,6 +398,8 @@ int check(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, 
     return rows > 1ull << 30 || dim > 1ull << 24 || vocab > 0x7FFFFFFFull ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;
 }
 
+// Short pieces where there are few places: a piece's places follow one another.
+int piece_of(uint64_t rows) { return rows >= 8192 ? LONG_PIECE : 32; }
 struct Scratch {
     uint64_t key[2], place[2], seen, list, count, part, bytes;
 };
@@ -404,8 +408,8 @@ Scratch scratch(uint64_t rows, uint64_t dim, uint64_t vocab) {
     Scratch s = {};
     const uint64_t each = up(rows * 4);
     s.key[0] = 0, s.key[1] = each, s.place[0] = 2 * each, s.place[1] = 3 * each, s.seen = 4 * each;
-    s.list = s.seen + up((vocab + 31) / 32 * 4), s.count = s.list + up((rows + PIECE - 1) / PIECE * 8), s.part = s.count + 256;
-    s.bytes = s.part + up((rows + PIECE - 1) / PIECE * 2 * dim * 4);
+    s.list = s.seen + up((vocab + 31) / 32 * 4), s.count = s.list + up((rows + piece_of(rows) - 1) / piece_of(rows) * 8), s.part = s.count + 256;
+    s.bytes = s.part + up((rows + piece_of(rows) - 1) / piece_of(rows) * 2 * dim * 4);
     return s;
 }
 
@@ -466,7 +470,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     for (int i = 0; i < 2; ++i) a.key[i] = (uint32_t *)(ws + need.key[i]), a.place[i] = (uint32_t *)(ws + need.place[i]);
     a.seen = (uint32_t *)(ws + need.seen), a.across_list = (uint2 *)(ws + need.list), a.across_count = (uint32_t *)(ws + need.count), a.cleared = a.across_count + 1, a.sorted = a.across_count + 2, a.part = (float *)(ws + need.part);
     a.dy_stride = (int64_t)dy_stride, a.table_stride = (int64_t)d_table_stride, a.rows = (int64_t)rows, a.dim = (int64_t)dim;
-    a.vocab = (uint32_t)vocab, a.pieces = (uint32_t)((rows + PIECE - 1) / PIECE), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
+    a.vocab = (uint32_t)vocab, a.piece = piece_of(rows), a.pieces = (uint32_t)((rows + piece_of(rows) - 1) / piece_of(rows)), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
     int bits = 1;
     while (vocab >> bits) ++bits;  // digits of `vocab` itself, which stands for ids outside
     a.passes = (bits + MAX_DIGIT - 1) / MAX_DIGIT, a.digit = (bits + a.passes - 1) / a.passes;

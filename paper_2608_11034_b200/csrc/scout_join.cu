@@ -308,12 +308,13 @@ Shape shape(const scout_join_t *j, bool wide, bool backward) {
     const int threads = s.team * s.teams;
     s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / threads) : 1;
     if (wide && s.v == 2) {
-        // as many blocks as registers allow, or fewer, so that two rows of each team fit into shared memory; four at most
+        // Two to four rows of each team, of as many blocks as registers allow, in 160 KiB of an SM, so that the weights stay in the rest;
+        // where two do not fit, all of shared memory, and fewer blocks.
         s.stage_bytes = s.teams * ring_row(j, backward);
-        for (;; --s.blocks) {
-            s.stages = std::min(4, ((227 << 10) / s.blocks - 1024 - 256 - (backward ? threads * 64 : 0)) / s.stage_bytes);
-            if (s.stages >= 2 || s.blocks == 1) break;
-        }
+        const auto fit = [&](int bytes) { return std::min(4, (bytes / s.blocks - 1024 - 256 - (backward ? threads * 64 : 0)) / s.stage_bytes); };
+        s.stages = fit(160 << 10);
+        for (; s.stages < 2; --s.blocks)
+            if ((s.stages = fit(227 << 10)) >= 2 || s.blocks == 1) break;
     }
     const int64_t want = (int64_t)SMS * s.blocks * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);

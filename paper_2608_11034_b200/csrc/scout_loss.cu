@@ -28,11 +28,12 @@ using attn::Half;
 using attn::LOG2E;
 using attn::smem_u32;
 
-constexpr int TM = 128, TN = 256, TK = 64, STAGES = 4, CHAIN = 1024 / TK;  // in steps of TK terms
-constexpr int THREADS = 384, BOX = 64 * TK * 2, STAGE = (TM + TN) / 64 * BOX;
+// A tile is a pair of SMs': 256 x 256, of which each block holds 128 rows and brings 128 of the columns' operand.
+constexpr int TM = 256, TN = 256, TK = 64, STAGES = 6, CHAIN = 1024 / TK;  // in steps of TK terms
+constexpr int HALF = 128, THREADS = 384, BOX = 64 * TK * 2, STAGE = 2 * HALF / 64 * BOX, PAIRS = SMS / 2;
 constexpr int TURN = 32 * 33 * 4;  // a warp's 32 x 32 results on their way to rows that start anywhere
 constexpr int SMEM = STAGES * STAGE + 8 * TURN + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
-constexpr int GROUP = 64;  // row tiles that share a tile of w while it is in L2: 8192 rows, 64 MiB with 4096 columns
+constexpr int GROUP = 32;  // row tiles that share a tile of w while it is in L2: 8192 rows, 64 MiB with 4096 columns
 enum { SCORES, GRADS, TABLE, STATES };
 
 struct Args {
@@ -234,7 +235,7 @@ template <int KIND> struct Work {
 };
 
 template <typename T, int KIND>
-__global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
+__global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b) {
     // operands with their contraction contiguous (K) or their rows (MN)
     constexpr bool mn_a = KIND == TABLE, mn_b = KIND == TABLE || KIND == STATES;
     extern __shared__ uint8_t smem_raw[];
@@ -247,14 +248,15 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
     if (threadIdx.x == 0) {
         dead = 0;
         for (int s = 0; s < STAGES; ++s) tc::bar_init(full + 8 * s, 1), tc::bar_init(empty + 8 * s, 1);
-        for (int s = 0; s < 2; ++s) tc::bar_init(sum_full + 8 * s, 1), tc::bar_init(sum_empty + 8 * s, 8);
+        for (int s = 0; s < 2; ++s) tc::bar_init(sum_full + 8 * s, 1), tc::bar_init(sum_empty + 8 * s, 16);
         tc::bar_init_done();
     }
-    if (warp == 9) tc::tmem_alloc(smem_u32(&tmem_slot), 512);
+    if (warp == 9) tc::pair_tmem_alloc(smem_u32(&tmem_slot), 512);
     tc::tc_fence_before();
     __syncthreads();
+    tc::cluster_sync();  // the other block's barriers too
     tc::tc_fence_after();
-    const uint32_t tmem = tc::uniform(tmem_slot);
+    const uint32_t tmem = tc::uniform(tmem_slot), rank = tc::uniform(tc::cluster_rank()), pair = blockIdx.x >> 1, pairs = gridDim.x >> 1;
     pdl_wait();  // the rows taken, G
     const Work<KIND> work(a);
 
@@ -265,24 +267,25 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
             tc::prefetch_map(&map_a);
             tc::prefetch_map(&map_b);
             uint32_t n = 0;
-            for (int i = blockIdx.x; i < work.items; i += gridDim.x) {
+            for (int i = pair; i < work.items; i += pairs) {
                 const Item it = work.at(i);
                 for (int k = 0; k < it.steps; ++k, ++n) {
-                    const uint32_t s = n % STAGES, to = base + s * STAGE, bar = full + 8 * s;
-                    const int at = (it.k0 + k) * TK;
+                    const uint32_t s = n % STAGES, to = base + s * STAGE;
+                    const int at = (it.k0 + k) * TK, m0 = it.m * TM + (int)rank * HALF, n0 = it.n * TN + (int)rank * HALF;
                     if (!patience.wait(empty + 8 * s, ((n / STAGES) & 1) ^ 1)) goto done;
-                    tc::bar_expect(bar, STAGE);
+                    if (rank == 0) tc::bar_expect(full + 8 * s, 2 * STAGE);
+                    const uint32_t bar = tc::in_block(full + 8 * s, 0);
                     if constexpr (mn_a) {
 #pragma unroll
-                        for (int c = 0; c < TM / 64; ++c) tc::tma_2d(to + c * BOX, &map_a, bar, it.m * TM + c * 64, at);
+                        for (int c = 0; c < HALF / 64; ++c) tc::pair_tma_2d(to + c * BOX, &map_a, bar, m0 + c * 64, at);
                     } else {
-                        tc::tma_2d(to, &map_a, bar, at, it.m * TM);
+                        tc::pair_tma_2d(to, &map_a, bar, at, m0);
                     }
                     if constexpr (mn_b) {
 #pragma unroll
-                        for (int c = 0; c < TN / 64; ++c) tc::tma_2d(to + (TM / 64 + c) * BOX, &map_b, bar, it.n * TN + c * 64, at);
+                        for (int c = 0; c < HALF / 64; ++c) tc::pair_tma_2d(to + (HALF / 64 + c) * BOX, &map_b, bar, n0 + c * 64, at);
                     } else {
-                        tc::tma_2d(to + TM / 64 * BOX, &map_b, bar, at, it.n * TN);
+                        tc::pair_tma_2d(to + HALF / 64 * BOX, &map_b, bar, at, n0);
                     }
                 }
             }
@@ -292,7 +295,7 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
         constexpr uint32_t idesc = tc::instr(Half<T>::is_bf16, TM, TN, mn_a, mn_b);
         constexpr uint32_t next_a = mn_a ? 2048 : 32, next_b = mn_b ? 2048 : 32;  // bytes to the next 16 terms
         uint32_t n = 0, chain = 0;
-        for (int i = blockIdx.x; i < work.items; i += gridDim.x) {
+        for (int i = rank == 0 ? pair : work.items; i < work.items; i += pairs) {
             const Item it = work.at(i);
             for (int k = 0; k < it.steps; ++chain) {
                 const uint32_t buf = chain & 1;
@@ -304,11 +307,11 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
                     tc::tc_fence_after();
 #pragma unroll
                     for (int kk = 0; kk < TK / 16; ++kk)
-                        tc::mma(tmem + buf * TN, tc::smem_desc(from + kk * next_a, mn_a ? BOX : 16, 1024),
-                                tc::smem_desc(from + TM / 64 * BOX + kk * next_b, mn_b ? BOX : 16, 1024), idesc, c > 0 || kk > 0);
-                    tc::mma_commit(empty + 8 * s);
+                        tc::pair_mma(tmem + buf * TN, tc::smem_desc(from + kk * next_a, mn_a ? BOX : 16, 1024),
+                                     tc::smem_desc(from + HALF / 64 * BOX + kk * next_b, mn_b ? BOX : 16, 1024), idesc, c > 0 || kk > 0);
+                    tc::pair_commit(empty + 8 * s);
                 }
-                tc::mma_commit(sum_full + 8 * buf);
+                tc::pair_commit(sum_full + 8 * buf);
             }
         }
     } else if (warp >= 10) {
@@ -316,9 +319,9 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
     } else {
         tc::registers_up<224>();
         uint32_t chain = 0;
-        const int half = warp >> 2, row = (warp & 3) * 32 + lane;
+        const int half = warp >> 2, row = (int)rank * HALF + (warp & 3) * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 128;
-        for (int i = blockIdx.x; i < work.items; i += gridDim.x) {
+        for (int i = pair; i < work.items; i += pairs) {
             const Item it = work.at(i);
             float sum[128];
 #pragma unroll
@@ -337,7 +340,7 @@ __global__ void __launch_bounds__(THREADS, 1) product(const __grid_constant__ Ar
                 }
                 tc::tc_fence_before();
                 __syncwarp();
-                if (lane == 0) tc::bar_arrive(sum_empty + 8 * buf);
+                if (lane == 0) tc::bar_arrive_cluster(tc::in_block(sum_empty + 8 * buf, 0));
             }
             const int64_t m = (int64_t)it.m * TM + row, n0 = (int64_t)it.n * TN + half * 128;
             if constexpr (KIND == SCORES) {
@@ -438,8 +441,9 @@ done:
     if (dead) tc::let_flights_end();
     tc::tc_fence_before();
     __syncthreads();
+    tc::cluster_sync();  // nobody reads or signals the other block any more
     tc::tc_fence_after();
-    if (warp == 9) tc::tmem_free(tmem, 512);
+    if (warp == 9) tc::pair_tmem_free(tmem, 512);
 }
 
 // ---- lse and loss from the tiles' statistics: 32 rows to a block, 32 threads a row ---------------------------------
@@ -534,7 +538,7 @@ Layout layout(uint64_t rows, uint64_t dim, uint64_t vocab) {
     l.piece = ((vocab + pieces - 1) / pieces + TN - 1) / TN * TN;
     // dx has few tiles where rows are few: then the vocabulary is cut into parts, of eight steps at least
     const uint64_t tiles = std::max<uint64_t>(1, l.padded / TM * ((dim + TN - 1) / TN)), steps = (l.piece + TK - 1) / TK;
-    uint64_t want = tiles >= SMS ? 1 : std::min<uint64_t>(SMS / tiles, steps / 8);
+    uint64_t want = tiles >= PAIRS ? 1 : std::min<uint64_t>(PAIRS / tiles, steps / 8);
     want = std::max<uint64_t>(1, want);
     l.per = (int)std::max<uint64_t>(1, (steps + want - 1) / want);
     l.splits = (int)std::max<uint64_t>(1, (steps + l.per - 1) / l.per);
@@ -595,7 +599,7 @@ template <typename T> int take(const Args &a, cudaStream_t stream) {
 template <typename T, int KIND> int run_product(const Args &a, int64_t items, const CUtensorMap &ma, const CUtensorMap &mb, cudaStream_t stream) {
     if (int rc = allow_smem<product<T, KIND>>(SMEM)) return rc;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::max<int64_t>(1, std::min<int64_t>(items, SMS)));
+    cfg.gridDim = dim3(2 * (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, PAIRS)));
     cfg.blockDim = dim3(THREADS);
     cfg.dynamicSmemBytes = SMEM;
     cfg.stream = stream;
@@ -615,8 +619,8 @@ template <typename T> int map_of(CUtensorMap *m, const void *p, uint64_t rows, u
 
 template <typename T> int run_forward(Args &a, const Layout &l, cudaStream_t stream) {
     CUtensorMap mx, mw;
-    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, TM)) return rc;
-    if (int rc = map_of<T>(&mw, a.w, a.vocab, a.dim, a.w_stride, TN)) return rc;
+    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, HALF)) return rc;
+    if (int rc = map_of<T>(&mw, a.w, a.vocab, a.dim, a.w_stride, HALF)) return rc;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     a.pv = a.vocab;
@@ -629,16 +633,16 @@ template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t st
     a.scale_log2 = Half<T>::is_bf16 ? 0 : 13;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     CUtensorMap mx, mw, mg, mg_t, mx_t, mw_n;
-    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, TM)) return rc;
+    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, HALF)) return rc;
     if (int rc = map_of<T>(&mx_t, a.xc, l.padded, a.dim, a.dim, TK)) return rc;
-    if (int rc = map_of<T>(&mg, a.gs, l.padded, l.piece, l.piece, TM)) return rc;
+    if (int rc = map_of<T>(&mg, a.gs, l.padded, l.piece, l.piece, HALF)) return rc;
     if (int rc = map_of<T>(&mg_t, a.gs, l.padded, l.piece, l.piece, TK)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     const int64_t row_tiles = (int64_t)(l.padded / TM), dim_tiles = (a.dim + TN - 1) / TN;
     for (int64_t v0 = 0; v0 < a.vocab; v0 += a.piece) {
         a.v0 = v0, a.pv = std::min<int64_t>(a.piece, a.vocab - v0), a.first = v0 == 0;
         const T *w = reinterpret_cast<const T *>(a.w) + v0 * a.w_stride;
-        if (int rc = map_of<T>(&mw, w, a.pv, a.dim, a.w_stride, TN)) return rc;
+        if (int rc = map_of<T>(&mw, w, a.pv, a.dim, a.w_stride, HALF)) return rc;
         if (int rc = map_of<T>(&mw_n, w, a.pv, a.dim, a.w_stride, TK)) return rc;
         if (int rc = run_product<T, GRADS>(a, row_tiles * ((a.pv + TN - 1) / TN), mx, mw, stream)) return rc;
         if (int rc = run_product<T, TABLE>(a, (a.pv + TM - 1) / TM * dim_tiles, mg_t, mx_t, stream)) return rc;
