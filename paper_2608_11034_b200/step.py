@@ -25,10 +25,17 @@ import numpy as np
 import torch
 
 from . import binding
-from .replay import _CODE, _enqueue, _fail, _no_autograd, _row_stride
+from .replay import _CODE, _enqueue, _fail, _row_stride
 
 _IDS = {torch.int32: binding.DT_I32, torch.int64: binding.DT_I64}
 _MASK64 = (1 << 64) - 1
+
+
+def _no_autograd(*tensors) -> None:
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if x is not None and x.requires_grad:
+                _fail("autograd does not record this call: use torch.no_grad() or a torch.autograd.Function")
 
 
 def _flat_ids(ids: torch.Tensor, device, name: str) -> torch.Tensor:
@@ -91,7 +98,7 @@ def embedding_backward(dy: torch.Tensor, ids: torch.Tensor, vocab: int, *, scale
     -> [vocab, dim] in out_dtype (float32, which is the default, or dy's), zeros for ids that do not occur; with `grad` (of those
     dtypes, of a tied output projection, say) it is added to that in place, rows of ids that do not occur are left alone, and
     out_dtype may only repeat its dtype."""
-    _no_autograd(dy) if grad is None else _no_autograd(dy, grad)
+    _no_autograd(dy, grad)
     ids = _flat_ids(ids, dy.device, "ids")
     if dy.dim() == 0 or vocab < 0:
         _fail("dy: [*ids.shape, dim]; vocab: the table's rows")
@@ -144,7 +151,7 @@ def dropout(x: torch.Tensor, p: float, *, seed: int, offset=0) -> torch.Tensor:
     code, stride = _matrix(x.shape, x.stride(), x.dtype, x.device)
     p, seed, host, dev = _counter(p, seed, offset, x.device)
     rows, cols = x.shape
-    y = x.new_empty((rows, cols))
+    y = torch.empty_like(x)             # rows one behind the other
     _enqueue("scout_dropout", x.device.index, code, rows, cols, x.data_ptr(), stride, y.data_ptr(), max(cols, 1), p, seed, host, dev)
     return y
 
@@ -232,13 +239,12 @@ def join_forward(x: Optional[torch.Tensor], block: torch.Tensor, *, gate: Option
     one row for every rows / groups rows in turn (one per sequence, one per token).  Without post_weight the block is not normed,
     without norm_weight n is None.  p, seed, offset: as in dropout.  dim: up to 16384.
     -> (y, n, stats); stats [2, rows] float32 are the two norms' factors, for the backward pass."""
-    _no_autograd(*(w for w in (x, block, gate, post_weight, norm_weight) if w is not None))
+    _no_autograd(x, block, gate, post_weight, norm_weight)
     j = _join(_say(block), (_say(x),), None, (_say_weight(gate), _say_weight(post_weight), _say_weight(norm_weight)), float(scale),
               float(eps), False)
     p, seed, host, dev = _counter(p, seed, offset, block.device)
-    shape = (j.rows, j.dim)
-    y = block.new_empty(shape, dtype=block.dtype if x is None else x.dtype)
-    n = None if norm_weight is None else block.new_empty(shape)
+    y = torch.empty_like(block if x is None else x)             # rows one behind the other
+    n = None if norm_weight is None else torch.empty_like(block)
     stats = block.new_empty((2, j.rows), dtype=torch.float32)
     _enqueue("scout_join_forward", j.index, j.at, _at(x), block.data_ptr(), _at(gate), _at(post_weight), _at(norm_weight), p, seed, host, dev,
              y.data_ptr(), _at(n), stats.data_ptr())
@@ -252,7 +258,7 @@ def join_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], block:
     pass returned; the other arguments as there.
     -> (dx, dblock, dgate, dpost_weight, dnorm_weight): dx of the stream's dtype, the weights' gradients like the weights, None
     where there is no such weight."""
-    _no_autograd(*(w for w in (dy, dn, block, y, gate, post_weight, norm_weight) if w is not None))
+    _no_autograd(dy, dn, block, y, gate, post_weight, norm_weight)
     if dn is not None and norm_weight is None:
         _fail("dn: without norm_weight there was no n")
     j = _join(_say(block), (_say(y), _say(dy)), _say(dn), (_say_weight(gate), _say_weight(post_weight), _say_weight(norm_weight)),
@@ -260,9 +266,9 @@ def join_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], block:
     if stats.dtype != torch.float32 or stats.shape != (2, j.rows) or not stats.is_contiguous() or stats.device != block.device:
         _fail("stats: the forward pass's, a contiguous float32 tensor [2, rows]")
     p, seed, host, dev = _counter(p, seed, offset, block.device)
-    shape = (j.rows, j.dim)
-    dx, db = y.new_empty(shape), block.new_empty(shape)
-    dgate, dpost = (None if w is None else torch.empty_like(w) for w in (gate, post_weight))
+    dx, db = torch.empty_like(y), torch.empty_like(block)             # rows one behind the other
+    dgate = None if gate is None else torch.empty_like(gate)
+    dpost = None if post_weight is None else torch.empty_like(post_weight)
     dnorm = None if norm_weight is None else torch.empty_like(norm_weight) if dn is not None else torch.zeros_like(norm_weight)
     ws = block.new_empty(j.bytes, dtype=torch.uint8)
     _enqueue("scout_join_backward", j.index, j.at, _at(dy), _at(dn), block.data_ptr(), y.data_ptr(), stats.data_ptr(), _at(gate),
@@ -304,7 +310,8 @@ def loss_forward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor):
     _no_autograd(x, w)
     code, rows, dim, vocab, x_row, w_row, nbytes, _ = _describe_scores(x, w, targets)
     targets = _flat_ids(targets, x.device, "targets")
-    loss, lse = x.new_empty(rows, dtype=torch.float32), x.new_empty(rows, dtype=torch.float32)
+    loss = x.new_empty(rows, dtype=torch.float32)
+    lse = torch.empty_like(loss)
     ws = x.new_empty(nbytes, dtype=torch.uint8)
     _enqueue("scout_loss_forward", x.device.index, code, _IDS[targets.dtype], rows, dim, vocab, x.data_ptr(), x_row, w.data_ptr(), w_row,
              targets.data_ptr(), loss.data_ptr(), lse.data_ptr(), ws.data_ptr(), nbytes)
@@ -319,7 +326,7 @@ def loss_backward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: 
     embedding, say) dw is added to it in place, and out_dtype may only repeat its dtype.
     The gradient of the scores is rounded to x's type for its products, so a float32 dw is as exact as its terms are (2^-9 of
     each in bfloat16, 2^-12 in float16), not as float32 is."""
-    _no_autograd(x, w, lse, dloss) if grad is None else _no_autograd(x, w, lse, dloss, grad)
+    _no_autograd(x, w, lse, dloss, grad)
     code, rows, dim, vocab, x_row, w_row, _, nbytes = _describe_scores(x, w, targets)
     targets = _flat_ids(targets, x.device, "targets")
     for t, name in ((lse, "lse"), (dloss, "dloss")):
@@ -336,7 +343,7 @@ def loss_backward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: 
     if dw.dtype not in (torch.float32, w.dtype) or dw.shape != (vocab, dim) or dw.device != x.device:
         _fail("the gradient is [vocab, dim], float32 or of w's dtype, on x's device")
     dw_row = _row_stride(dw.shape, dw.stride(), dw.device, "grad")
-    dx = x.new_empty((rows, dim))
+    dx = torch.empty_like(x)             # rows one behind the other
     ws = x.new_empty(nbytes, dtype=torch.uint8)
     _enqueue("scout_loss_backward", x.device.index, code, _IDS[targets.dtype], _CODE[dw.dtype], rows, dim, vocab, x.data_ptr(), x_row,
              w.data_ptr(), w_row, targets.data_ptr(), lse.data_ptr(), dloss.data_ptr(), dloss.stride(0), dx.data_ptr(), dim, dw.data_ptr(),
