@@ -5,7 +5,7 @@
 //   mark_ids     which ids occur (not where the gradient is added to one that is there)
 //   sort_ids     one cluster of eight blocks sorts (id, place) by id, places of an id staying in order (radix sort from the
 //                lowest digit, up to nine bits a pass); the other blocks write zeros to rows of ids that do not occur
-//   sum_places   the sorted places in pieces of 32 or 64: a thread adds up eight columns of a piece, writes what begins and ends
+//   sum_places   the sorted places in pieces of 16 to 64: a thread adds up eight columns of a piece, writes what begins and ends
 //                inside, and leaves what crosses a border in scratch
 //   join_pieces  adds the parts of an id that crosses borders, in order
 // Pieces of equal size keep one frequent id (a line break, say) from holding up the rest.
@@ -88,9 +88,10 @@ template <typename T, typename TO> int run_lookup(Lookup a, uint64_t rows, cudaS
 
 // ---- backward -----------------------------------------------------------------------------------------
 constexpr int CLUSTER = 8, SORT_THREADS = 1024, SORT_WARPS = SORT_THREADS / 32, MAX_DIGIT = 9, MAX_BINS = 1 << MAX_DIGIT, HELD = 4;
+constexpr int RANKED = 2048, RANKERS = 8;  // so many places are ranked by counting: 1003 of them take RANK_A us, sorted by digits RANK_B
 constexpr int SORT_SMEM = (SORT_WARPS + 2) * MAX_BINS * 4, FILL_CLUSTERS = SMS / CLUSTER - 1;
 constexpr int MARKED = 1 << 20, MARK_SMEM = MARKED / 8;  // ids of a block of mark_ids
-constexpr int LONG_PIECE = 64, AHEAD = 8, SUM_THREADS = 128;
+constexpr int LONG_PIECE = 64, SUM_THREADS = 128;
 constexpr int JOIN_THREADS = 256, JOIN_WAYS = JOIN_THREADS / 32, JOIN_COLS = 128;
 
 struct Grad {
@@ -127,7 +128,7 @@ __global__ void __launch_bounds__(SORT_THREADS) mark_ids(const __grid_constant__
     for (uint32_t w = threadIdx.x; w < words; w += SORT_THREADS) a.seen[first / 32 + w] = smem[w];
 }
 
-// zeros to a row by a warp, whatever it starts on: whole 16 bytes, and the elements before and behind them
+// zeros to a row, or several, by a warp, whatever it starts on: whole 16 bytes, and the elements before and behind them
 template <typename TO> __device__ __forceinline__ void clear_row(TO *row, int64_t dim) {
     constexpr int N = 16 / sizeof(TO);
     const int lane = threadIdx.x & 31;
@@ -146,15 +147,22 @@ template <typename TO, bool UNTIL_SORTED> __device__ __forceinline__ void clear_
         if ((threadIdx.x & 31) == 0) v0 = UNTIL_SORTED && *reinterpret_cast<volatile uint32_t *>(a.sorted) ? a.vocab : atomicAdd(a.cleared, a.at_once);
         v0 = __shfl_sync(0xFFFFFFFFu, v0, 0);
         if (v0 >= a.vocab) return;
-        const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31);  // at_once divides 32
-        for (uint32_t i = 0; i < a.at_once && v0 + i < a.vocab; ++i)
-            if (!((seen >> i) & 1)) clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, a.dim);
+        const uint32_t seen = a.seen[v0 >> 5] >> (v0 & 31), n = min(a.at_once, a.vocab - v0);  // at_once divides 32
+        for (uint32_t i = 0; i < n;) {
+            uint32_t end = i + 1;
+            if (!((seen >> i) & 1)) {
+                if (a.table_stride == a.dim)  // rows one behind the other are one piece
+                    while (end < n && !((seen >> end) & 1)) ++end;
+                clear_row(reinterpret_cast<TO *>(a.table) + (int64_t)(v0 + i) * a.table_stride, (int64_t)(end - i) * a.dim);
+            }
+            i = end;
+        }
     }
 }
 
 // Sorts (the first cluster), and meanwhile writes zeros to rows of ids that do not occur (the others).
 template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
-    extern __shared__ uint32_t smem[];
+    extern __shared__ __align__(16) uint32_t smem[];
     if (blockIdx.x >= CLUSTER) {
         pdl_wait();  // the marks; what the sorting blocks read and write has nothing to do with them
         clear_rows<TO, true>(a);
@@ -169,6 +177,27 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
     const int64_t run = (a.rows + CLUSTER * SORT_WARPS * 32 - 1) / (CLUSTER * SORT_WARPS * 32) * 32;
     const int64_t begin = min((int64_t)(rank * SORT_WARPS + warp) * run, a.rows), end = min(begin + run, a.rows);
     const bool held = run <= 32 * HELD;  // the whole run stays in registers between the two looks at it
+    if (a.passes == 0) {
+        // Few places: each is told its place among the others by counting those that come before it, RANKERS threads sharing the count.
+        // Id and place make one number.
+        const uint32_t rows = (uint32_t)a.rows, quads = (rows + 3) / 4, each = CLUSTER * SORT_THREADS / RANKERS;
+        for (uint32_t t = threadIdx.x; t < 4 * quads; t += SORT_THREADS) smem[t] = t < rows ? id_at(a.ids, a.id64, t, a.vocab) * RANKED + t : 0xFFFFFFFFu;
+        __syncthreads();
+        const uint32_t share = threadIdx.x % RANKERS;
+        for (uint32_t t0 = 0; t0 < rows; t0 += each) {  // the same for a warp
+            const uint32_t t = t0 + rank * (SORT_THREADS / RANKERS) + threadIdx.x / RANKERS, mine = t < rows ? smem[t] : 0;
+            uint32_t before = 0;
+#pragma unroll 4
+            for (uint32_t q = share; q < quads; q += RANKERS) {
+                const uint4 other = reinterpret_cast<const uint4 *>(smem)[q];
+                before += (other.x < mine) + (other.y < mine) + (other.z < mine) + (other.w < mine);
+            }
+#pragma unroll
+            for (int d = 1; d < RANKERS; d <<= 1) before += __shfl_xor_sync(0xFFFFFFFFu, before, d);
+            if (share == 0 && t < rows) a.key[1][before] = mine / RANKED, a.place[1][before] = t;
+        }
+        cluster.sync();
+    }
     for (int pass = 0; pass < a.passes; ++pass) {
         const int shift = pass * a.digit, from = (pass + 1) & 1, to = pass & 1;
         uint32_t key[HELD], place[HELD];
@@ -263,20 +292,8 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
     }
 }
 
-// out = (accumulate ? out : 0) + scale * sum, eight columns
-template <typename TO, bool WIDE> __device__ __forceinline__ void put(const Grad &a, uint32_t id, const Columns<WIDE> &c, const float (&sum)[8]) {
-    TO *row = reinterpret_cast<TO *>(a.table) + (int64_t)id * a.table_stride;
-    Eight<TO> e;
-    float x[8];
-    e.zero();
-    if (a.accumulate) e.template load<true>(row, c);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = a.accumulate ? fmaf(a.scale, sum[i], e.get(i)) : a.scale * sum[i];
-    e.set(x);
-    e.store(row, c);
-}
-
-template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
+template <typename T, typename TO, bool WIDE, bool ADD> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
+    constexpr int AHEAD = ADD ? 4 : 8;
     pdl_wait();
     if (blockIdx.x >= a.pieces * a.across) {
         clear_rows<TO, false>(a);
@@ -294,24 +311,38 @@ template <typename T, typename TO, bool WIDE> __global__ void __launch_bounds__(
     }
     if (threadIdx.x < count) place[threadIdx.x] = places[p0 + threadIdx.x];
     __syncthreads();
+    const int live = __syncthreads_count((int)threadIdx.x < count && key[min((int)threadIdx.x, count - 1) + 1] < a.vocab);  // sorted: the first ones
     const Columns<WIDE> c(blockIdx.x % a.across * SUM_THREADS + threadIdx.x, (uint32_t)a.dim);
-    if (!c.any()) return;
+    if (!c.any() || live == 0) return;
     float sum[8] = {};
     bool begun = key[0] != key[1];  // the current id's places begin inside this piece
-    for (int k0 = 0; k0 < count; k0 += AHEAD) {
+    for (int k0 = 0; k0 < live; k0 += AHEAD) {
         Eight<T> e[AHEAD];
+        Eight<TO> was[ADD ? AHEAD : 1];
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u)
-            if (k0 + u < count && key[k0 + u + 1] < a.vocab) e[u].template load<true>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k0 + u] * a.dy_stride, c);
+        for (int u = 0; u < AHEAD; ++u) {  // past the end the last one again, for nothing
+            const int k = min(k0 + u, live - 1);
+            e[u].zero();
+            e[u].template load<true>(reinterpret_cast<const T *>(a.dy) + (int64_t)place[k] * a.dy_stride, c);
+            if constexpr (ADD) {
+                was[u].zero();
+                if (key[k + 2] != key[k + 1]) was[u].template load<true>(reinterpret_cast<const TO *>(a.table) + (int64_t)key[k + 1] * a.table_stride, c);
+            }
+        }
 #pragma unroll
         for (int u = 0; u < AHEAD; ++u) {
             const int k = k0 + u;
-            if (k >= count || key[k + 1] >= a.vocab) break;
+            if (k >= live) break;
 #pragma unroll
             for (int i = 0; i < 8; ++i) sum[i] += e[u].get(i);
             const bool ends = key[k + 2] != key[k + 1];
             if (ends && begun) {
-                put<TO>(a, key[k + 1], c, sum);
+                float x[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) x[i] = ADD ? fmaf(a.scale, sum[i], was[ADD ? u : 0].get(i)) : a.scale * sum[i];
+                Eight<TO> o;
+                o.set(x);
+                o.store(reinterpret_cast<TO *>(a.table) + (int64_t)key[k + 1] * a.table_stride, c);
             } else if (ends || k + 1 == count) {
                 float *part = a.part + ((int64_t)piece * 2 + begun) * a.dim;
 #pragma unroll
@@ -382,7 +413,9 @@ template <typename T, typename TO> int run_gradient(Grad &a, cudaStream_t stream
     cfg.attrs = attr;
     cfg.numAttrs = a.accumulate ? 0 : 1;
     SCOUT_CUDA(cudaLaunchKernelEx(&cfg, sort_ids<TO>, a));
-    if (grid) SCOUT_CUDA(launch_dependent(a.wide ? sum_places<T, TO, true> : sum_places<T, TO, false>, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
+    const auto sums = a.accumulate ? (a.wide ? sum_places<T, TO, true, true> : sum_places<T, TO, false, true>)
+                                   : (a.wide ? sum_places<T, TO, true, false> : sum_places<T, TO, false, false>);
+    if (grid) SCOUT_CUDA(launch_dependent(sums, dim3((unsigned)grid), dim3(SUM_THREADS), stream, a));
     if (a.pieces > 1) {
         const uint32_t wide = (uint32_t)((a.dim + JOIN_COLS - 1) / JOIN_COLS);
         const dim3 jg(wide, std::min<uint32_t>(a.pieces - 1, std::max<uint32_t>(1, 16 * SMS / wide)));
@@ -399,7 +432,7 @@ int check(uint32_t id_dtype, uint32_t dtype, uint32_t out_dtype, uint64_t rows, 
 }
 
 // Short pieces where there are few places: a piece's places follow one another.
-int piece_of(uint64_t rows) { return rows >= 8192 ? LONG_PIECE : 32; }
+int piece_of(uint64_t rows) { return rows >= 8192 ? LONG_PIECE : rows >= 2048 ? 32 : 16; }
 struct Scratch {
     uint64_t key[2], place[2], seen, list, count, part, bytes;
 };
@@ -473,7 +506,7 @@ extern "C" int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t 
     a.vocab = (uint32_t)vocab, a.piece = piece_of(rows), a.pieces = (uint32_t)((rows + piece_of(rows) - 1) / piece_of(rows)), a.across = (uint32_t)((dim + 8 * SUM_THREADS - 1) / (8 * SUM_THREADS));
     int bits = 1;
     while (vocab >> bits) ++bits;  // digits of `vocab` itself, which stands for ids outside
-    a.passes = (bits + MAX_DIGIT - 1) / MAX_DIGIT, a.digit = (bits + a.passes - 1) / a.passes;
+    a.passes = rows <= RANKED && vocab < (1ull << 32) / RANKED - 1 ? 0 : (bits + MAX_DIGIT - 1) / MAX_DIGIT, a.digit = a.passes ? (bits + a.passes - 1) / a.passes : 0;
     a.id64 = id_dtype == SCOUT_DT_I64, a.accumulate = (int)accumulate, a.scale = scale;
     a.wide = dim % 8 == 0 && (!rows || wide_rows(dy, dy_stride, dtype)) && wide_rows(d_table, d_table_stride, out_dtype);
     const cudaStream_t s = (cudaStream_t)stream;

@@ -10,7 +10,7 @@
 // G is held with g divided by the largest |g| (GREF): a loss averaged over the batch has one g for all rows, whose rounding would
 // otherwise be the same in every term; in fp16 it is held 2^13 times that, where the products still fit and a probability of 1e-11
 // is not lost.  Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of
-// dx: join_states adds what the rounding took from that entry, times the target's row of w.
+// dx: join_states adds what the rounding took from that entry, times the target's row of w.  TABLE does so where rows are few.
 //
 // The tensor cores truncate when they add to an accumulator; chains of products are cut at 1024 terms and added in fp32.
 #include <algorithm>
@@ -33,6 +33,7 @@ constexpr int TM = 256, TN = 256, TK = 64, STAGES = 6, CHAIN = 1024 / TK;  // in
 constexpr int HALF = 128, THREADS = 384, BOX = 64 * TK * 2, STAGE = 2 * HALF / 64 * BOX, PAIRS = SMS / 2;
 constexpr int TURN = 32 * 33 * 4;  // a warp's 32 x 32 results on their way to rows that start anywhere
 constexpr int SMEM = STAGES * STAGE + 8 * TURN + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
+constexpr int FEW = 64;
 constexpr int GROUP = 32;  // row tiles that share a tile of w while it is in L2: 8192 rows, 64 MiB with 4096 columns
 enum { SCORES, GRADS, TABLE, STATES };
 
@@ -50,7 +51,7 @@ struct Args {
     int32_t *where;     // [rows]: its place among the taken rows, or -1
     int32_t *target;    // [padded]
     float *row_lse, *row_g, *row_rest;  // [padded]: lse; g / g_ref; what rounding took from G at the target
-    float *row_score, *row_rough;       // [padded]: the target's score, in fp32 and as the tensor cores have it
+    float *row_score, *row_rough;       // [padded]: the target's score in fp32 (backward: its probability less 1), and as the tensor cores have it
     void *xc, *gs;      // [padded][dim], [padded][piece]
     float2 *part;       // [2 * tiles of the vocabulary][padded]: maximum and sum of 128 columns
     float *dxp;         // [splits][padded][dim]
@@ -76,8 +77,8 @@ template <typename T> __device__ __forceinline__ void load_any(Eight<T> &e, cons
         e.w[0] = make_uint4(v[0], v[1], v[2], v[3]);
     }
 }
-// Each block takes a run of rows; how many before it count it finds out by itself.  For the forward pass a row's score at its target
-// is made here too, in fp32 (see join_scores).
+// Each block takes a run of rows; how many before it count it finds out by itself.  A row's score at its target is made here too, in
+// fp32: for lse (see join_scores), and for G at the target, which is the difference of a probability near 1 and 1 where a model is sure.
 template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(const __grid_constant__ Args a, int64_t per) {
     __shared__ int counts[TAKE_THREADS / 32];
     __shared__ float tops[TAKE_THREADS / 32];
@@ -140,7 +141,7 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
                     e[u].zero(), f[u].zero();
                     if (c >= a.dim) continue;
                     load_any(e[u], src + c, a.wide_x);
-                    if (!a.d_loss) f[u].w[0] = __ldg(reinterpret_cast<const uint4 *>(w + c));
+                    f[u].w[0] = __ldg(reinterpret_cast<const uint4 *>(w + c));
                 }
 #pragma unroll
                 for (int u = 0; u < TAKE_AHEAD; ++u) {
@@ -150,10 +151,8 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
                     for (int i = 0; i < 8; ++i) score = fmaf(e[u].get(i), f[u].get(i), score);
                 }
             }
-            if (!a.d_loss) {
-                score = warp_sum(score);
-                if (lane == 0) a.row_score[before + k] = score;
-            }
+            score = warp_sum(score);
+            if (lane == 0) a.row_score[before + k] = a.d_loss ? expm1f(score - a.lse_in[rows_at[k]]) : score;
         }
         before += all;
     }
@@ -162,10 +161,11 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
             *a.count = before;
             if (a.d_loss) *a.g_ref = ref;
         }
-        const int64_t end = min((before + (int64_t)TM - 1) / TM * TM, a.padded);
+        // tokens are TABLE's terms, taken TK at a time; rows of a tile that are not there may hold anything, but have no target
+        const int64_t end = min((before + (int64_t)TM - 1) / TM * TM, a.padded), terms = (before + (int64_t)TK - 1) / TK * TK;
         Eight<T> z;
         z.zero();
-        for (int64_t i = before * (a.dim / 8) + threadIdx.x; i < end * (a.dim / 8); i += TAKE_THREADS) *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.xc) + 8 * i) = z.w[0];
+        for (int64_t i = before * (a.dim / 8) + threadIdx.x; i < terms * (a.dim / 8); i += TAKE_THREADS) *reinterpret_cast<uint4 *>(reinterpret_cast<T *>(a.xc) + 8 * i) = z.w[0];
         for (int64_t i = before + threadIdx.x; i < end; i += TAKE_THREADS) {
             a.target[i] = -1;
             if (a.d_loss) a.row_lse[i] = 0.f, a.row_g[i] = 0.f;
@@ -359,7 +359,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 a.part[(int64_t)(it.n * 2 + half) * a.padded + m] = make_float2(top, total);
             } else if constexpr (KIND == GRADS) {
                 const int left = (int)min(128ll, (long long)(a.pv - n0)), at = a.target[m] < 0 ? -1 : (int)max(-1ll, min(128ll, (long long)a.target[m] - a.v0 - n0));
-                const float lse = a.row_lse[m], g = a.row_g[m] * power2(a.scale_log2);
+                const float lse = a.row_lse[m], g = a.row_g[m] * power2(a.scale_log2), at_target = a.row_score[m];
                 const bool on = a.target[m] >= 0;
                 T *dst = reinterpret_cast<T *>(a.gs) + m * a.piece + n0;
 #pragma unroll
@@ -368,7 +368,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
                         const float p = exp2_fast((sum[c + e] - lse) * LOG2E);
-                        sum[c + e] = on && c + e < left ? g * (c + e == at ? p - 1.f : p) : 0.f;
+                        sum[c + e] = on && c + e < left ? g * (c + e == at ? at_target : p) : 0.f;
                         if (c + e == at) a.row_rest[m] = sum[c + e] - Half<T>::up(Half<T>::down(sum[c + e]));
                     }
 #pragma unroll
@@ -390,18 +390,36 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 const float ref = *a.g_ref * power2(-a.scale_log2);
                 const int64_t v = a.v0 + m;
                 const bool on = m < a.pv;
+                // With few rows the rounding of G at a target is all of its row's error, and is put right; with many it is one of many.
+                if (const int count = *a.count; count <= FEW) {
+                    for (int t = 0; t < count; ++t) {
+                        if (a.target[t] != v) continue;
+                        const float rest = a.row_rest[t];
+                        const T *x = reinterpret_cast<const T *>(a.xc) + (int64_t)t * a.dim + n0;
+#pragma unroll
+                        for (int c = 0; c < 128; c += 8) {
+                            if (n0 + c >= a.dim) break;
+                            Eight<T> e;
+                            e.w[0] = *reinterpret_cast<const uint4 *>(x + c);
+#pragma unroll
+                            for (int i = 0; i < 8; ++i) sum[c + i] = fmaf(rest, e.get(i), sum[c + i]);
+                        }
+                    }
+                }
 #pragma unroll
                 for (int c = 0; c < 128; ++c) sum[c] *= ref;
-                if (a.wide && n0 + 128 <= a.dim) {
-                    // a thread's row in 32-byte pieces
+                if (a.wide) {
+                    // a thread's row in 32-byte pieces; it ends with eight columns (16 bytes of a 16-bit type)
 #pragma unroll
                     for (int c = 0; c < 128; c += 16) {
                         uint32_t w[8];
-                        if (!on) break;
+                        const int left = (int)min(16ll, (long long)(a.dim - n0 - c));
+                        if (!on || left <= 0) break;
                         if (a.out_f32) {
                             float *dst = reinterpret_cast<float *>(a.dw) + v * a.dw_stride + n0 + c;
 #pragma unroll
                             for (int h = 0; h < 16; h += 8) {
+                                if (h >= left) break;
                                 if (a.accumulate) load32(w, dst + h);
 #pragma unroll
                                 for (int e = 0; e < 8; ++e) w[e] = __float_as_uint(a.accumulate ? __uint_as_float(w[e]) + sum[c + h + e] : sum[c + h + e]);
@@ -409,17 +427,21 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                             }
                         } else {
                             T *dst = reinterpret_cast<T *>(a.dw) + v * a.dw_stride + n0 + c;
-                            if (a.accumulate) load32(w, dst);
+                            if (a.accumulate) {
+                                const uint4 was = reinterpret_cast<const uint4 *>(dst)[0], more = left > 8 ? reinterpret_cast<const uint4 *>(dst)[1] : was;
+                                w[0] = was.x, w[1] = was.y, w[2] = was.z, w[3] = was.w, w[4] = more.x, w[5] = more.y, w[6] = more.z, w[7] = more.w;
+                            }
 #pragma unroll
                             for (int e = 0; e < 8; ++e) {
                                 const float2 was = a.accumulate ? Half<T>::unpack(w[e]) : make_float2(0.f, 0.f);
                                 w[e] = Half<T>::pack(was.x + sum[c + 2 * e], was.y + sum[c + 2 * e + 1]);
                             }
-                            store32(dst, w, a.wide == 2);
+                            if (left > 8) store32(dst, w, a.wide == 2);
+                            else *reinterpret_cast<uint4 *>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
                         }
                     }
                 } else {
-                    // rows of dw on any boundary, and ragged ends: 32 x 32 results are turned in shared memory, a lane per column
+                    // rows of dw on any boundary: 32 x 32 results are turned in shared memory, a lane per column
                     float *turn = reinterpret_cast<float *>(smem_raw + (base - smem_u32(smem_raw)) + STAGES * STAGE + warp * TURN);
                     const int64_t m0 = m - lane;
 #pragma unroll
@@ -486,23 +508,38 @@ __global__ void __launch_bounds__(32 * JOIN_WAYS) join_scores(const __grid_const
     }
 }
 
-// ---- dx from the parts ---------------------------------------------------------------------------------
-template <typename T> __global__ void __launch_bounds__(256) join_states(const __grid_constant__ Args a, int wide) {
+// ---- dx from the parts: WAYS threads share the parts of eight elements -----------------------------------------------------
+template <typename T, int WAYS> __global__ void __launch_bounds__(256) join_states(const __grid_constant__ Args a, int wide) {
     pdl_wait();
+    __shared__ float part[WAYS > 1 ? WAYS : 1][256 / WAYS][WAYS > 1 ? 9 : 1];
+    const int way = threadIdx.x / (256 / WAYS), lane = threadIdx.x % (256 / WAYS);
     const int64_t per_row = a.dim / 8, all = a.rows * per_row;
     const float ref = *a.g_ref * power2(-a.scale_log2);
-    for (int64_t q = (int64_t)blockIdx.x * 256 + threadIdx.x; q < all; q += (int64_t)gridDim.x * 256) {
-        const int64_t t = q / per_row;
+    for (int64_t q0 = (int64_t)blockIdx.x * (256 / WAYS); q0 < all; q0 += (int64_t)gridDim.x * (256 / WAYS)) {  // the same for a block
+        const int64_t q = min(q0 + lane, all - 1), t = q / per_row;
         const Columns<true> at((uint32_t)(q - t * per_row), (uint32_t)a.dim);
         const int m = a.where[t];
         float x[8] = {};
-        if (m >= 0) {
-            for (int s = 0; s < a.splits; ++s) {
+        if (m >= 0)
+#pragma unroll 4
+            for (int s = way; s < a.splits; s += WAYS) {
                 Eight<float> e;
                 e.template load<true>(a.dxp + ((int64_t)s * a.padded + m) * a.dim, at);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) x[i] += e.get(i);
             }
+        if constexpr (WAYS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < 8; ++i) part[way][lane][i] = x[i];
+            __syncthreads();
+            if (way == 0)
+                for (int w = 1; w < WAYS; ++w)
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) x[i] += part[w][lane][i];
+        }
+        if (way > 0 || q0 + lane >= all) continue;
+        if (m >= 0) {
             Eight<T> w;
             w.template load<false>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride, at);
             const float rest = a.row_rest[m];
@@ -591,7 +628,7 @@ void place(Args *a, const Layout &l, void *workspace, bool backward) {
 }
 
 template <typename T> int take(const Args &a, cudaStream_t stream) {
-    const int64_t per = std::max<int64_t>(8, (a.rows + SMS * 4 - 1) / (SMS * 4));
+    const int64_t per = (a.rows + SMS * 4 - 1) / (SMS * 4);
     take_rows<T><<<(unsigned)((a.rows + per - 1) / per), TAKE_THREADS, 0, stream>>>(a, per);
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
@@ -649,8 +686,9 @@ template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t st
         if (int rc = run_product<T, STATES>(a, row_tiles * dim_tiles * a.splits, mg, mw_n, stream)) return rc;
     }
     const int wide = wide_rows(a.dx, a.dx_stride, SCOUT_DT_BF16);
-    const int64_t blocks = (a.rows * (a.dim / 8) + 255) / 256;
-    SCOUT_CUDA(launch_dependent(join_states<T>, dim3((unsigned)std::min<int64_t>(blocks, SMS * 8)), dim3(256), stream, a, wide));
+    const int ways = a.splits > 4 ? 8 : 1;
+    const int64_t units = 256 / ways, blocks = (a.rows * (a.dim / 8) + units - 1) / units;
+    SCOUT_CUDA(launch_dependent(ways > 1 ? join_states<T, 8> : join_states<T, 1>, dim3((unsigned)std::min<int64_t>(blocks, SMS * 8)), dim3(256), stream, a, wide));
     return SCOUT_OK;
 }
 
