@@ -163,6 +163,7 @@ template <typename TO, bool UNTIL_SORTED> __device__ __forceinline__ void clear_
 // Sorts (the first cluster), and meanwhile writes zeros to rows of ids that do not occur (the others).
 template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_bounds__(SORT_THREADS) sort_ids(const __grid_constant__ Grad a) {
     extern __shared__ __align__(16) uint32_t smem[];
+    pdl_launch_dependents();
     if (blockIdx.x >= CLUSTER) {
         pdl_wait();  // the marks; what the sorting blocks read and write has nothing to do with them
         clear_rows<TO, true>(a);
@@ -295,6 +296,7 @@ template <typename TO> __global__ void __cluster_dims__(CLUSTER, 1, 1) __launch_
 template <typename T, typename TO, bool WIDE, bool ADD> __global__ void __launch_bounds__(SUM_THREADS) sum_places(const __grid_constant__ Grad a) {
     constexpr int AHEAD = ADD ? 4 : 8;
     pdl_wait();
+    pdl_launch_dependents();
     if (blockIdx.x >= a.pieces * a.across) {
         clear_rows<TO, false>(a);
         return;

@@ -118,6 +118,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
     const int64_t slab = (int64_t)blockIdx.x * a.teams + team, first = slab * a.per, last = min(first + a.per, a.rows);
     Sums<V> acc;
     acc.s = sums, acc.threads = blockDim.x, acc.t = threadIdx.x;
+    pdl_launch_dependents();
     Eight<TS> y[V], g0[V];
     Eight<TB> n[V], b[V];
 #pragma unroll

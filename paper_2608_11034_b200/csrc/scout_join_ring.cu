@@ -184,6 +184,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
     Sums<V> acc;
+    pdl_launch_dependents();
     acc.s = reinterpret_cast<float *>(ring + a.stages * stage_bytes), acc.threads = blockDim.x, acc.t = threadIdx.x;
 #pragma unroll
     for (int v = 0; v < V; ++v)

@@ -83,6 +83,7 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
     __shared__ int counts[TAKE_THREADS / 32];
     __shared__ float tops[TAKE_THREADS / 32];
     __shared__ int rows_at[TAKE_THREADS], targets[TAKE_THREADS];
+    pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r0 = blockIdx.x * per, r1 = min(r0 + per, a.rows);
     const bool last = r1 == a.rows;
@@ -392,17 +393,23 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 const bool on = m < a.pv;
                 // With few rows the rounding of G at a target is all of its row's error, and is put right; with many it is one of many.
                 if (const int count = *a.count; count <= FEW) {
-                    for (int t = 0; t < count; ++t) {
-                        if (a.target[t] != v) continue;
-                        const float rest = a.row_rest[t];
-                        const T *x = reinterpret_cast<const T *>(a.xc) + (int64_t)t * a.dim + n0;
 #pragma unroll
-                        for (int c = 0; c < 128; c += 8) {
-                            if (n0 + c >= a.dim) break;
-                            Eight<T> e;
-                            e.w[0] = *reinterpret_cast<const uint4 *>(x + c);
+                    for (int t0 = 0; t0 < FEW; t0 += 32) {
+                        const int64_t mine = t0 + lane < count ? a.target[t0 + lane] : -1, first = v - lane;
+                        uint32_t here = __ballot_sync(0xFFFFFFFFu, mine >= first && mine < first + 32);  // targets among the warp's rows
+                        for (; here; here &= here - 1) {
+                            const int t = __ffs(here) - 1;
+                            if (__shfl_sync(0xFFFFFFFFu, mine, t) != v) continue;
+                            const float rest = a.row_rest[t0 + t];
+                            const T *x = reinterpret_cast<const T *>(a.xc) + (int64_t)(t0 + t) * a.dim + n0;
 #pragma unroll
-                            for (int i = 0; i < 8; ++i) sum[c + i] = fmaf(rest, e.get(i), sum[c + i]);
+                            for (int c = 0; c < 128; c += 8) {
+                                if (n0 + c >= a.dim) break;
+                                Eight<T> e;
+                                e.w[0] = *reinterpret_cast<const uint4 *>(x + c);
+#pragma unroll
+                                for (int i = 0; i < 8; ++i) sum[c + i] = fmaf(rest, e.get(i), sum[c + i]);
+                            }
                         }
                     }
                 }
