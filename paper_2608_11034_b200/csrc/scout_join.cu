@@ -268,16 +268,19 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
     pdl_wait();
     __shared__ float part[JOIN_WAYS][JOIN_COLS];
     const int64_t col = (int64_t)blockIdx.x * JOIN_COLS + threadIdx.x;
-    const int64_t which = blockIdx.y;  // 0: d_post, 1: d_norm, from 2 on a group of the gate
+    const int64_t which = blockIdx.y;  // 0: d_post, 1: d_norm, from 2 on the gate's groups, or where they are more than the runs, the runs' borders
     void *out = which == 0 ? a.d_post : which == 1 ? a.d_norm : a.d_gate;
     if (!out) return;  // the whole block
-    for (int64_t w = which; w < (which < 2 ? which + 1 : groups + 2); w += gridDim.y - 2) {
+    const bool by_group = groups < a.slabs;
+    for (int64_t w = which; w < (which < 2 ? which + 1 : (by_group ? groups : a.slabs - 1) + 2); w += gridDim.y - 2) {
         float sum = 0.f;
-        int64_t s0 = 0, s1 = a.slabs, begin = 0;
-        if (w >= 2) {
-            begin = (w - 2) * a.group_rows;
+        int64_t s0 = 0, s1 = a.slabs, begin = 0, group = 0;
+        if (w >= 2) {  // continues are the same for the whole block
+            const int64_t border = (w - 1) * a.per;
+            group = by_group ? w - 2 : border / a.group_rows, begin = group * a.group_rows;
+            if (!by_group && (begin >= border || begin < border - a.per)) continue;  // no group crosses here, or it has crossed one before
             s0 = begin / a.per, s1 = (begin + a.group_rows - 1) / a.per + 1;
-            if (s1 - s0 == 1) continue;  // written where it was summed; the same for the whole block
+            if (s1 - s0 == 1) continue;  // written where it was summed
         }
         if (col < a.dim)
 #pragma unroll 4
@@ -291,7 +294,7 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
         if (threadIdx.y == 0 && col < a.dim) {
 #pragma unroll
             for (int k = 1; k < JOIN_WAYS; ++k) sum += part[k][threadIdx.x];
-            reinterpret_cast<TW *>(out)[(w < 2 ? 0 : (w - 2) * a.dim) + col] = down<TW>(sum);
+            reinterpret_cast<TW *>(out)[(w < 2 ? 0 : group * a.dim) + col] = down<TW>(sum);
         }
     }
 }
@@ -348,7 +351,7 @@ template <typename TB, typename TS, typename TW> int run_backward(Args &a, const
 }
 template <typename TW> int run_columns(const Args &a, int64_t groups, cudaStream_t stream) {
     if (!a.d_post && !a.d_norm && !a.d_gate) return SCOUT_OK;
-    const dim3 jg((unsigned)((a.dim + JOIN_COLS - 1) / JOIN_COLS), 2 + (unsigned)(a.d_gate ? std::min<int64_t>(groups, 1024) : 1));
+    const dim3 jg((unsigned)((a.dim + JOIN_COLS - 1) / JOIN_COLS), 2 + (unsigned)(a.d_gate ? std::max<int64_t>(1, std::min(groups, a.slabs - 1)) : 1));
     SCOUT_CUDA(launch_dependent(join_columns<TW>, jg, dim3(JOIN_COLS, JOIN_WAYS), stream, a, groups));
     return SCOUT_OK;
 }
