@@ -262,8 +262,8 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
     }
 }
 
-// The runs' sums, added in the order of the rows: eight threads of a column take every eighth run each.
-constexpr int JOIN_COLS = 32, JOIN_WAYS = 8;
+// The runs' sums, added in the order of the rows: 32 threads of a column take every 32nd run each.
+constexpr int JOIN_COLS = 32, JOIN_WAYS = 32;
 template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) join_columns(const __grid_constant__ Args a, int64_t groups) {
     pdl_wait();
     __shared__ float part[JOIN_WAYS][JOIN_COLS];
@@ -292,7 +292,7 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
         part[threadIdx.y][threadIdx.x] = sum;
         __syncthreads();
         if (threadIdx.y == 0 && col < a.dim) {
-#pragma unroll
+#pragma unroll 8
             for (int k = 1; k < JOIN_WAYS; ++k) sum += part[k][threadIdx.x];
             reinterpret_cast<TW *>(out)[(w < 2 ? 0 : group * a.dim) + col] = down<TW>(sum);
         }

@@ -185,14 +185,27 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
     Sums<V> acc;
     pdl_launch_dependents();
-    acc.s = reinterpret_cast<float *>(ring + a.stages * stage_bytes), acc.threads = blockDim.x, acc.t = threadIdx.x;
 #pragma unroll
     for (int v = 0; v < V; ++v)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) acc.at(D_POST, v, i) = acc.at(GATE_SUM, v, i) = acc.at(D_NORM, v, i) = 0.f;
+        for (int i = 0; i < 8; ++i) acc.at(GATE_SUM, v, i) = acc.at(D_NORM, v, i) = 0.f;
     uint32_t group = group_of(a, min(first, a.rows - 1));
     int64_t group_end = (group + 1ll) * a.group_rows, begun = first;  // where the gate's current sum began
     const float factor = a.scale * (a.drop.cut ? a.drop.factor : 1.f);
+    // gate times post of the thread's columns, where only the thread itself reads them
+    float4 *const products = reinterpret_cast<float4 *>(ring + a.stages * stage_bytes) + threadIdx.x;
+    const auto multiply = [&] {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Cols c(t + v * a.team, a.dim);
+            float w[8], gate[8];
+            weights<TW>(w, a.post, c);
+            weights<TW>(gate, gate_row<TW>(a, group), c);
+            products[(2 * v) * blockDim.x] = make_float4(w[0] * gate[0], w[1] * gate[1], w[2] * gate[2], w[3] * gate[3]);
+            products[(2 * v + 1) * blockDim.x] = make_float4(w[4] * gate[4], w[5] * gate[5], w[6] * gate[6], w[7] * gate[7]);
+        }
+    };
+    multiply();
     float rb_next = 1.f, ry_next = 0.f;
     const auto fetch_stats = [&](int64_t row) {
         if (row >= last) return;
@@ -209,6 +222,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
         const uint8_t *const in = ring + at.stage * stage_bytes + team * row_bytes;
         float g[V][8], d = 0.f, pull = 0.f;
         if (has_dn) {
+            if (on)
 #pragma unroll
             for (int v = 0; v < V; ++v) {
                 const Cols c(t + v * a.team, a.dim);
@@ -221,7 +235,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
                 for (int i = 0; i < 8; ++i) {
                     const float z = y.get(i) * ry, dn = n.get(i);
                     g[v][i] *= dn;
-                    if (on) acc.at(D_NORM, v, i) = fmaf(dn, z, acc.at(D_NORM, v, i));
+                    acc.at(D_NORM, v, i) = fmaf(dn, z, acc.at(D_NORM, v, i));
                     d = fmaf(g[v][i], z, d);
                 }
             }
@@ -232,7 +246,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
         refill(it);
         d = 0.f;
         TS *const dx_row = row_of<TS>(a.dx, a.dx_stride, (uint32_t)row);
-        const void *const gates = gate_row<TW>(a, group);
+        if (on)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
@@ -249,29 +263,29 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
 #pragma unroll
                 for (int i = 0; i < 8; ++i) g[v][i] = e.get(i);
             }
-            if ((FULL || a.dx) && on) {
+            if (FULL || a.dx) {
                 e.set(g[v]);
                 e.store(dx_row, c);
             }
             Keep<true> keep;
             keep.all();
             if (a.drop.cut) keep = Keep<true>(a.drop, t + v * a.team, (uint32_t)row, offset);
-            float w[8], gate[8];
-            weights<TW>(w, a.post, c);
-            weights<TW>(gate, gates, c);
             from_ring(b, in + at_b, c);
+            const float4 lo = products[(2 * v) * blockDim.x], hi = products[(2 * v + 1) * blockDim.x];
+            const float w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 // what was dropped is 0 in both, whatever it was
-                const float cb = on && keep[i] ? b.get(i) * rb : 0.f, h = on && keep[i] ? g[v][i] * factor : 0.f;
+                const float cb = keep[i] ? b.get(i) * rb : 0.f, h = keep[i] ? g[v][i] * factor : 0.f;
                 acc.at(GATE_SUM, v, i) = fmaf(h, cb, acc.at(GATE_SUM, v, i));
-                g[v][i] = h * (gate[i] * w[i]);
+                g[v][i] = h * w[i];
                 d = fmaf(g[v][i], cb, d);
             }
         }
         pull = 0.f;
         if (post) pull = -(team_sum(d, s1, warps, t, blockDim.x) * a.inv_dim) * rb;
         TB *const db_row = row_of<TB>(a.db, a.db_stride, (uint32_t)row);
+        if (on)
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
@@ -283,7 +297,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
                 for (int i = 0; i < 8; ++i) g[v][i] = rb * fmaf(pull, b.get(i), g[v][i]);
             }
             b.set(g[v]);
-            if (on) b.store(db_row, c);
+            b.store(db_row, c);
         }
         if (!post && warps > 1) sync_some(blockDim.x);
         // the gate's sum ends with its group or with the run
@@ -294,32 +308,35 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
                 const Cols c(t + v * a.team, a.dim);
                 float w[8], gate[8];
                 weights<TW>(w, a.post, c);
-                weights<TW>(gate, gates, c);
+                weights<TW>(gate, gate_row<TW>(a, group), c);
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float sum = acc.at(GATE_SUM, v, i);
-                    acc.at(D_POST, v, i) = fmaf(gate[i], sum, acc.at(D_POST, v, i));
                     acc.at(GATE_SUM, v, i) = 0.f;
-                    if (!a.d_gate || !c.has(i)) continue;
+                    if (!c.has(i)) continue;
+                    if (a.d_post) {  // most runs end one gate's rows at most
+                        float *const to = a.part + slab * 2 * a.dim + c.col(i);
+                        *to = gate[i] * sum + (begun == first ? 0.f : *to);
+                    }
+                    if (!a.d_gate) continue;
                     if (whole) reinterpret_cast<TW *>(a.d_gate)[(int64_t)group * a.dim + c.col(i)] = down<TW>(w[i] * sum);
                     else a.part_gate[(slab * 2 + (begun != first)) * a.dim + c.col(i)] = w[i] * sum;
                 }
             }
             begun = row + 1;
-            if (begun == group_end) ++group, group_end += a.group_rows;
-            if (begun == a.rows) group = 0;  // for nothing, but inside
+            if (begun == group_end && begun < a.rows) {
+                ++group, group_end += a.group_rows;
+                multiply();
+            }
         }
     }
-    if (first < last) {
+    if (first < last && a.d_norm) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if (!c.has(i)) continue;
-                if (a.d_post) a.part[slab * 2 * a.dim + c.col(i)] = acc.at(D_POST, v, i);
-                if (a.d_norm) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = acc.at(D_NORM, v, i);
-            }
+            for (int i = 0; i < 8; ++i)
+                if (c.has(i)) a.part[(slab * 2 + 1) * a.dim + c.col(i)] = acc.at(D_NORM, v, i);
         }
     }
     if (*patience.dead) tc::let_flights_end();
