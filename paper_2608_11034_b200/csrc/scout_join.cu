@@ -315,7 +315,7 @@ Shape shape(const scout_join_t *j, bool wide, bool backward) {
         // Two to four rows of each team, of as many blocks as registers allow, in 160 KiB of an SM, so that the weights stay in the rest;
         // where two do not fit, all of shared memory, and fewer blocks.
         s.stage_bytes = s.teams * ring_row(j, backward);
-        const auto fit = [&](int bytes) { return std::min(4, (bytes / s.blocks - 1024 - 256 - (backward ? threads * 64 : 0)) / s.stage_bytes); };
+        const auto fit = [&](int bytes) { return std::min(4, (bytes / s.blocks - 1024 - 256 - threads * 64) / s.stage_bytes); };
         s.stages = fit(160 << 10);
         for (; s.stages < 2; --s.blocks)
             if ((s.stages = fit(227 << 10)) >= 2 || s.blocks == 1) break;

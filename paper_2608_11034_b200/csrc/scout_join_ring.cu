@@ -68,6 +68,23 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
     const bool post = FULL || a.post, norm = FULL || a.norm;
+    // scale times gate times post of the thread's columns, where only the thread itself reads them
+    float4 *const products = reinterpret_cast<float4 *>(ring + a.stages * stage_bytes) + threadIdx.x;
+    uint32_t group = group_of(a, min(row0 + team, a.rows - 1));
+    const auto multiply = [&] {
+#pragma unroll
+        for (int v = 0; v < V; ++v) {
+            const Cols c(t + v * a.team, a.dim);
+            float w[8], gate[8];
+            weights<TW>(w, a.post, c);
+            weights<TW>(gate, gate_row<TW>(a, group), c);
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] *= a.scale * gate[i];
+            products[(2 * v) * blockDim.x] = make_float4(w[0], w[1], w[2], w[3]);
+            products[(2 * v + 1) * blockDim.x] = make_float4(w[4], w[5], w[6], w[7]);
+        }
+    };
+    multiply();
     for (int64_t base = row0; base < a.rows; base += stride, at.next(a.stages)) {
         const int64_t row = base + team;
         const bool on = row < a.rows;
@@ -87,29 +104,23 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
         else sync_some(blockDim.x);
         refill();
         sq = 0.f;
-        const void *const gate = gate_row<TW>(a, on ? group_of(a, row) : 0);
+        if (const uint32_t now = on ? group_of(a, row) : group; now != group) group = now, multiply();
+        const float factor = (post ? rb : 1.f) * (a.drop.cut ? a.drop.factor : 1.f);
         TS *const y_row = row_of<TS>(a.y, a.y_stride, (uint32_t)row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
             const Cols c(t + v * a.team, a.dim);
-            float w[8];
-            if (post) {
-                weights<TW>(w, a.post, c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] *= rb * w[i];
-            }
-            if (a.drop.cut) {
-                const Keep<true> keep(a.drop, t + v * a.team, (uint32_t)row, offset);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] = keep[i] ? u[v][i] * a.drop.factor : 0.f;  // 0 whatever it was
-            }
-            weights<TW>(w, gate, c);
+            Keep<true> keep;
+            keep.all();
+            if (a.drop.cut) keep = Keep<true>(a.drop, t + v * a.team, (uint32_t)row, offset);
+            const float4 lo = products[(2 * v) * blockDim.x], hi = products[(2 * v + 1) * blockDim.x];
+            const float w[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
             Eight<TS> x;
             x.zero();
             if (FULL || a.x) from_ring(x, in + a.dim * sizeof(TB), c);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                u[v][i] = fmaf(a.scale * w[i], u[v][i], x.get(i));
+                u[v][i] = fmaf(w[i], keep[i] ? u[v][i] * factor : 0.f, x.get(i));  // what is dropped is 0, whatever it was
                 sq = fmaf(u[v][i], u[v][i], sq);
             }
             if (on) {
@@ -344,7 +355,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
 
 template <typename TB, typename TS, typename TW, bool FULL> int launch(const Args &a, const Shape &s, bool backward, cudaStream_t stream) {
     const unsigned threads = s.team * s.teams;
-    const int bytes = s.stages * s.stage_bytes + (backward ? s.team * s.teams * 64 : 0);
+    const int bytes = s.stages * s.stage_bytes + s.team * s.teams * 64;  // and the products
     if (backward) {
         if (int rc = allow_smem<backward_rows<TB, TS, TW, FULL>>(226 << 10)) return rc;
         backward_rows<TB, TS, TW, FULL><<<(unsigned)((s.slabs + s.teams - 1) / s.teams), threads, bytes, stream>>>(a);
