@@ -22,7 +22,8 @@
  * aligned to their element size, and rows that lie on 16-byte boundaries are faster.
  * Types are SCOUT_DT_F32, SCOUT_DT_BF16 and SCOUT_DT_F16; sums, statistics and products of
  * elements are fp32, rounded to the result's type once.  Inputs and outputs of a call do
- * not overlap, save where it says so.
+ * not overlap, save where it says so.  Waits of the join's and the loss's kernels on their
+ * own copies and products are bounded; scout_replay_waits counts those that gave up.
  */
 #ifndef SCOUT_STEP_H
 #define SCOUT_STEP_H

@@ -2,8 +2,9 @@
 //
 // Bound by memory: forward reads x, b and writes y, n; backward reads dy, dn, b, y and writes dx, db.  A row is held in registers by
 // one team of warps, so that each tensor crosses memory once although a row's sums are needed twice, and the next row is fetched while
-// the present one is worked on.  Rows are dealt to teams: in turn (forward), in
-// runs (backward, whose column sums stay with the thread that owns the column for a whole run; runs meet in a second kernel, in order).
+// the present one is worked on.  Rows are dealt to teams: in turn (forward),
+// in runs (backward, whose column sums stay with the thread that owns the column for a whole run; runs meet in a second kernel, in
+// order).  How they are dealt, and which columns a thread has, follows from the sizes and types alone.
 #include <cmath>
 #include <initializer_list>
 
@@ -15,7 +16,7 @@ namespace step {
 namespace join {
 namespace {
 
-// ---- rows in registers: off 16-byte boundaries, or wider than 4096 ----------------------------------------------------
+// ---- rows in registers: off 16-byte boundaries, not of whole eights, or wider than 4096 ----------------------------------------------------
 // The next row's elements are fetched into the registers of the present one's as soon as those are free: b once it is widened, x once y
 // is made.
 template <typename TB, typename TS, typename TW, int V, bool WIDE>
@@ -33,13 +34,13 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
     const auto fetch_b = [&](int64_t at) {
         const TB *const p = row_of<TB>(a.b, a.b_stride, (uint32_t)min(at, (int64_t)most));
 #pragma unroll
-        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim));
+        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim, a.whole));
     };
     const auto fetch_x = [&](int64_t at) {
         if (!a.x) return;
         const TS *const p = row_of<TS>(a.x, a.x_stride, (uint32_t)min(at, (int64_t)most));
 #pragma unroll
-        for (int v = 0; v < V; ++v) x[v].template load<true>(p, Cols(t + v * a.team, a.dim));
+        for (int v = 0; v < V; ++v) x[v].template load<true>(p, Cols(t + v * a.team, a.dim, a.whole));
     };
 #pragma unroll
     for (int v = 0; v < V; ++v) b[v].zero(), x[v].zero();
@@ -54,28 +55,24 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
             for (int i = 0; i < 8; ++i) u[v][i] = b[v].get(i), sq = fmaf(u[v][i], u[v][i], sq);
         fetch_b(row + stride);
         float rb = 0.f, ry = 0.f;
-        if (post) rb = rsqrtf(team_sum(sq, s0, warps, t, blockDim.x) * a.inv_dim + a.eps);
+        if (post) rb = rms_factor(a, team_sum(sq, s0, warps, t, blockDim.x));
         sq = 0.f;
+        const float factor = (post ? rb : 1.f) * (a.drop.cut ? a.drop.factor : 1.f);
         const void *const gate = gate_row<TW>(a, group_of(a, min(row, (int64_t)most)));
         TS *const y_row = row_of<TS>(a.y, a.y_stride, (uint32_t)row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Cols c(t + v * a.team, a.dim);
-            float w[8];
-            if (post) {
-                weights<TW>(w, a.post, c);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] *= rb * w[i];
-            }
-            if (a.drop.cut) {
-                const Keep<WIDE> keep(a.drop, t + v * a.team, (uint32_t)row, offset);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) u[v][i] = keep[i] ? u[v][i] * a.drop.factor : 0.f;  // 0 whatever it was
-            }
-            weights<TW>(w, gate, c);
+            const Cols c(t + v * a.team, a.dim, a.whole);
+            float w[8], gates[8];
+            weights<TW>(w, a.post, c);
+            weights<TW>(gates, gate, c);
+            Keep<WIDE> keep;
+            keep.all();
+            if (a.drop.cut) keep = Keep<WIDE>(a.drop, t + v * a.team, (uint32_t)row, offset);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                u[v][i] = fmaf(a.scale * w[i], u[v][i], x[v].get(i));
+                w[i] *= a.scale * gates[i];
+                u[v][i] = fmaf(w[i], keep[i] ? u[v][i] * factor : 0.f, x[v].get(i));  // what is dropped is 0, whatever it was
                 sq = fmaf(u[v][i], u[v][i], sq);
             }
             if (on) {
@@ -86,12 +83,12 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
         }
         fetch_x(row + stride);
         if (norm) {
-            ry = rsqrtf(team_sum(sq, s1, warps, t, blockDim.x) * a.inv_dim + a.eps);
+            ry = rms_factor(a, team_sum(sq, s1, warps, t, blockDim.x));
             TB *const n_row = row_of<TB>(a.n, a.n_stride, (uint32_t)row);
             if (on)
 #pragma unroll
                 for (int v = 0; v < V; ++v) {
-                    const Cols c(t + v * a.team, a.dim);
+                    const Cols c(t + v * a.team, a.dim, a.whole);
                     float w[8];
                     weights<TW>(w, a.norm, c);
                     Eight<TB> n;
@@ -136,7 +133,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
         const TB *const pn = row_of<TB>(a.dn, a.dn_stride, row);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Cols c(t + v * a.team, a.dim);
+            const Cols c(t + v * a.team, a.dim, a.whole);
             if (has_dn) y[v].template load<true>(py, c), n[v].template load<true>(pn, c);
             if (a.dy) g0[v].template load<true>(pg, c);
         }
@@ -146,7 +143,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
         const uint32_t row = (uint32_t)min(at, (int64_t)most);
         const TB *const p = row_of<TB>(a.b, a.b_stride, row);
 #pragma unroll
-        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim));
+        for (int v = 0; v < V; ++v) b[v].template load<true>(p, Cols(t + v * a.team, a.dim, a.whole));
         if (post) rb = a.stats_in[row];
     };
     uint32_t group = group_of(a, min(first, (int64_t)most));
@@ -160,7 +157,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
         if (has_dn) {
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                weights<TW>(g[v], a.norm, Cols(t + v * a.team, a.dim));
+                weights<TW>(g[v], a.norm, Cols(t + v * a.team, a.dim, a.whole));
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const float z = y[v].get(i) * ry, dn = n[v].get(i);
@@ -186,8 +183,8 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
         const void *const gates = gate_row<TW>(a, group);
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Cols c(t + v * a.team, a.dim);
-            if ((a.dx) && on) {
+            const Cols c(t + v * a.team, a.dim, a.whole);
+            if (a.dx && on) {
                 Eight<TS> e;
                 e.set(g[v]);
                 e.store(dx_row, c);
@@ -219,7 +216,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
                 }
                 Eight<TB> e;
                 e.set(g[v]);
-                e.store(db_row, Cols(t + v * a.team, a.dim));
+                e.store(db_row, Cols(t + v * a.team, a.dim, a.whole));
             }
         }
         if (it + 1 < a.per) fetch_b(row + 1);
@@ -229,7 +226,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
             const bool whole = begun + a.group_rows == group_end && row + 1 == group_end;
 #pragma unroll
             for (int v = 0; v < V; ++v) {
-                const Cols c(t + v * a.team, a.dim);
+                const Cols c(t + v * a.team, a.dim, a.whole);
                 float w[8], gate[8];
                 weights<TW>(w, a.post, c);
                 weights<TW>(gate, gates, c);
@@ -251,7 +248,7 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const _
     if (first < last) {
 #pragma unroll
         for (int v = 0; v < V; ++v) {
-            const Cols c(t + v * a.team, a.dim);
+            const Cols c(t + v * a.team, a.dim, a.whole);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 if (!c.has(i)) continue;
@@ -301,7 +298,7 @@ template <typename TW> __global__ void __launch_bounds__(JOIN_COLS *JOIN_WAYS) j
 
 // Bytes of a row in the ring.
 int ring_row(const scout_join_t *j, bool backward) { return (int)(j->dim * ((backward ? 2 : 1) * (size_of(j->stream_dtype) + size_of(j->dtype)))); }
-Shape shape(const scout_join_t *j, bool wide, bool backward) {
+Shape shape(const scout_join_t *j, bool backward) {
     Shape s = {};
     const uint64_t rows = j->rows, dim = j->dim;
     const int eights = (int)((dim + 255) / 256 * 32);  // whole warps' worth
@@ -311,7 +308,7 @@ Shape shape(const scout_join_t *j, bool wide, bool backward) {
     s.full = (uint64_t)s.team * s.v * 8 == dim;
     const int threads = s.team * s.teams;
     s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / threads) : 1;
-    if (wide && s.v == 2) {
+    if (dim % 8 == 0 && s.v == 2) {
         // Two to four rows of each team, of as many blocks as registers allow, in 160 KiB of an SM, so that the weights stay in the rest;
         // where two do not fit, all of shared memory, and fewer blocks.
         s.stage_bytes = s.teams * ring_row(j, backward);
@@ -325,29 +322,22 @@ Shape shape(const scout_join_t *j, bool wide, bool backward) {
     s.slabs = ((int64_t)rows + s.per - 1) / s.per;
     return s;
 }
-// the runs of the backward pass are at most these, whatever the operands lie on
-int64_t most_slabs(const scout_join_t *j) { return std::max(shape(j, false, true).slabs, shape(j, true, true).slabs); }
-
-template <typename TB, typename TS, typename TW> int run_forward(Args &a, const Shape &s, cudaStream_t stream) {
-    const unsigned grid = (unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks);
-    const auto kernel = s.v == 2 ? join_forward<TB, TS, TW, 2, false> : a.wide ? join_forward<TB, TS, TW, 4, true> : join_forward<TB, TS, TW, 4, false>;
-    kernel<<<grid, s.team * s.teams, 0, stream>>>(a);
-    SCOUT_CUDA(cudaGetLastError());
-    return SCOUT_OK;
-}
-template <typename TB, typename TS, typename TW> int run_backward(Args &a, const Shape &s, cudaStream_t stream) {
-    const unsigned grid = (unsigned)((s.slabs + s.teams - 1) / s.teams), threads = s.team * s.teams;
-    if (s.v == 2) {
-        join_backward<TB, TS, TW, 2, false><<<grid, threads, 2 * 8 * 4 * threads, stream>>>(a);
-    } else if (a.wide) {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, true>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
-        join_backward<TB, TS, TW, 4, true><<<grid, threads, 3 * 4 * 8 * 4 * threads, stream>>>(a);
+template <typename TB, typename TS, typename TW, int V, bool WIDE> int launch(const Args &a, const Shape &s, bool backward, cudaStream_t stream) {
+    const unsigned threads = s.team * s.teams;
+    if (backward) {
+        constexpr int each = (V == 2 ? 1 : 3) * V * 8 * 4;  // bytes of a thread's sums in shared memory
+        if (int rc = allow_smem<join_backward<TB, TS, TW, V, WIDE>>(each * MOST<V>)) return rc;
+        join_backward<TB, TS, TW, V, WIDE><<<(unsigned)((s.slabs + s.teams - 1) / s.teams), threads, each * threads, stream>>>(a);
     } else {
-        if (int rc = allow_smem<join_backward<TB, TS, TW, 4, false>>(3 * 4 * 8 * 4 * MOST<4>)) return rc;
-        join_backward<TB, TS, TW, 4, false><<<grid, threads, 3 * 4 * 8 * 4 * threads, stream>>>(a);
+        join_forward<TB, TS, TW, V, WIDE><<<(unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks), threads, 0, stream>>>(a);
     }
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
+}
+template <typename TB, typename TS, typename TW> int run(const Args &a, const Shape &s, bool backward, cudaStream_t stream) {
+    const bool wide = a.dim % 8 == 0;
+    if (s.v == 2) return wide ? launch<TB, TS, TW, 2, true>(a, s, backward, stream) : launch<TB, TS, TW, 2, false>(a, s, backward, stream);
+    return wide ? launch<TB, TS, TW, 4, true>(a, s, backward, stream) : launch<TB, TS, TW, 4, false>(a, s, backward, stream);
 }
 template <typename TW> int run_columns(const Args &a, int64_t groups, cudaStream_t stream) {
     if (!a.d_post && !a.d_norm && !a.d_gate) return SCOUT_OK;
@@ -425,16 +415,16 @@ extern "C" int scout_join_forward(const scout_join_t *j, const void *x, const vo
     if (int rc = check_weights(j, {gate, post, norm})) return rc;
     describe(j, &a);
     a.x = x, a.b = b, a.gate = gate, a.post = post, a.norm = norm, a.y = y, a.n = n, a.stats = stats;
-    a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!x || wide_rows(x, j->x_stride, j->stream_dtype)) && wide_rows(b, j->b_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype) &&
+    a.whole = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!x || wide_rows(x, j->x_stride, j->stream_dtype)) && wide_rows(b, j->b_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype) &&
              (!n || wide_rows(n, j->n_stride, j->dtype));
     const cudaStream_t on = (cudaStream_t)stream;
-    const Shape s = shape(j, a.wide, false);
+    const Shape s = shape(j, false);
     a.team = s.team, a.teams = s.teams, a.stages = s.stages;
-    if (s.stages) {
+    if (s.stages && a.whole) {
         if (int rc = scout::tc::gave_up_counter(&a.gave_up)) return rc;
         return ring_forward(types_of(j), a, s, s.full && x && gate && post && norm, on);
     }
-    return by_types(*j, [&](auto tb, auto ts, auto tw) { return run_forward<decltype(tb), decltype(ts), decltype(tw)>(a, s, on); });
+    return by_types(*j, [&](auto tb, auto ts, auto tw) { return run<decltype(tb), decltype(ts), decltype(tw)>(a, s, false, on); });
 }
 
 extern "C" int scout_join_backward_workspace(const scout_join_t *j, uint64_t *bytes) {
@@ -442,7 +432,7 @@ extern "C" int scout_join_backward_workspace(const scout_join_t *j, uint64_t *by
     using namespace scout::step::join;
     if (!bytes) return SCOUT_ERR_INVALID;
     if (int rc = check(j)) return rc;
-    *bytes = (uint64_t)(most_slabs(j) * 4 * j->dim * 4 + 255) & ~255ull;
+    *bytes = (uint64_t)(shape(j, true).slabs * 4 * j->dim * 4 + 255) & ~255ull;
     return SCOUT_OK;
 }
 
@@ -482,16 +472,16 @@ extern "C" int scout_join_backward(const scout_join_t *j, const void *dy, const 
     a.dy = dy, a.dn = dn, a.b = b, a.yin = y, a.stats_in = stats, a.gate = gate, a.post = post, a.norm = norm;
     a.dx = dx, a.db = db, a.d_gate = d_gate, a.d_post = d_post, a.d_norm = d_norm;
     a.part = (float *)workspace;
-    a.part_gate = a.part + most_slabs(j) * 2 * (int64_t)j->dim;
-    a.wide = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
+    a.part_gate = a.part + shape(j, true).slabs * 2 * (int64_t)j->dim;
+    a.whole = j->dim % 8 == 0 && wide_weights(j, {gate, post, norm}) && (!dy || wide_rows(dy, j->dy_stride, j->stream_dtype)) && (!dn || (wide_rows(dn, j->dn_stride, j->dtype) && wide_rows(y, j->y_stride, j->stream_dtype))) &&
              wide_rows(b, j->b_stride, j->dtype) && (!dx || wide_rows(dx, j->dx_stride, j->stream_dtype)) && wide_rows(db, j->db_stride, j->dtype);
     const cudaStream_t on = (cudaStream_t)stream;
-    const Shape s = shape(j, a.wide, true);
+    const Shape s = shape(j, true);
     a.team = s.team, a.teams = s.teams, a.stages = s.stages, a.per = s.per, a.slabs = s.slabs;
-    if (s.stages) {
+    if (s.stages && a.whole) {
         if (int rc = scout::tc::gave_up_counter(&a.gave_up)) return rc;
         if (int rc = ring_backward(types_of(j), a, s, s.full && dy && dn && gate && post && norm && dx, on)) return rc;
-    } else if (int rc = by_types(*j, [&](auto tb, auto ts, auto tw) { return run_backward<decltype(tb), decltype(ts), decltype(tw)>(a, s, on); })) {
+    } else if (int rc = by_types(*j, [&](auto tb, auto ts, auto tw) { return run<decltype(tb), decltype(ts), decltype(tw)>(a, s, true, on); })) {
         return rc;
     }
     const int64_t groups = (int64_t)j->groups;

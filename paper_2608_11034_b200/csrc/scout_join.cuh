@@ -24,15 +24,14 @@ struct Args {
     int64_t rows, group_rows, per, slabs;
     int32_t dim, team, teams;  // threads of a team, teams of a block
     float scale, eps, inv_dim;
-    bool wide;  // all rows, those of the weights too, on 16-byte boundaries and of whole eights
+    bool whole;  // all rows, those of the weights too, on 16-byte boundaries and of whole eights
     Drop drop;
     uint32_t *gave_up;
     int32_t stages;  // of the ring
 };
 
 // Sum over a team.  `slots`: the team's part of [teams][warps of a team] in shared memory, not written again before every thread has
-// passed another team_sum.
-// `threads` of the block take part.
+// passed another wait of the block's `threads`.
 __device__ __forceinline__ void sync_some(uint32_t threads) { asm volatile("bar.sync 1, %0;" ::"r"(threads) : "memory"); }
 __device__ __forceinline__ float team_sum(float x, float *slots, uint32_t warps, uint32_t t, uint32_t threads) {
     x = warp_sum(x);
@@ -41,6 +40,8 @@ __device__ __forceinline__ float team_sum(float x, float *slots, uint32_t warps,
     sync_some(threads);
     return warp_sum((t & 31) < warps ? slots[t & 31] : 0.f);
 }
+// 1 over the root mean square of what sums up to `squares`
+__device__ __forceinline__ float rms_factor(const Args &a, float squares) { return rsqrtf(fmaf(squares, a.inv_dim, a.eps)); }
 // Weights, or what stands for none.
 template <typename TW, bool WIDE, bool FULL> __device__ __forceinline__ void weights(float (&w)[8], const void *row, const Columns<WIDE, FULL> &c) {
     if (!FULL && !row) {
@@ -62,11 +63,10 @@ __device__ __forceinline__ uint32_t group_of(const Args &a, int64_t row) { retur
 template <typename T> __device__ __forceinline__ const T *row_of(const void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<const T *>(p) + (uint64_t)row * stride; }
 template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t stride, uint32_t row) { return reinterpret_cast<T *>(p) + (uint64_t)row * stride; }
 
-
 // With h = scale g (masked) and c = b rms(b) (masked), du = h gate, and over the rows of one gate S = sum of h c gives both of
 //     d_gate = post S,   d_post = sum over gates of gate S,
 // so that a row adds to two column sums, S and d_norm: in registers, or beyond 4096 columns in shared memory.  d_post takes its part
-// when a gate's rows (or the run) end, in shared memory.
+// when a gate's rows (or the run) end.
 template <int V> struct Sums {
     static constexpr bool REGS = V == 2;
     float r[REGS ? 2 : 1][REGS ? V : 1][8];
@@ -83,12 +83,12 @@ enum { D_POST, GATE_SUM, D_NORM };
 struct Shape {
     int v, team, teams, blocks;  // of an SM
     bool full;                   // the team's columns are the row's
-    int stages, stage_bytes;     // of the ring; none where rows are off 16-byte boundaries or wider than 4096
+    int stages, stage_bytes;     // of the ring; none where rows are wider than 4096 or not of whole eights
     int64_t slabs, per;
 };
 
-// The kernels that take rows through shared memory (scout_join_ring.cu), for the types that `pick` stands for: (b, stream, weights) in
-// fp32 or else in the 16-bit type.
+// The kernels that take rows through shared memory (scout_join_ring.cu), by the types of b, stream (_S: fp32) and weights (_W: fp32).
+// They give the same bits as those that hold rows in registers: the same rows to a team, columns to a thread and order of operations.
 enum Types { ALL_F32, BF16, BF16_W, BF16_S, BF16_SW, F16, F16_W, F16_S, F16_SW };
 int ring_forward(Types types, const Args &a, const Shape &s, bool full, cudaStream_t stream);
 int ring_backward(Types types, const Args &a, const Shape &s, bool full, cudaStream_t stream);

@@ -22,13 +22,15 @@ template <> __device__ __forceinline__ float down<float>(float x) { return x; }
 template <> __device__ __forceinline__ __nv_bfloat16 down<__nv_bfloat16>(float x) { return __float2bfloat16_rn(x); }
 template <> __device__ __forceinline__ __half down<__half>(float x) { return __float2half_rn(x); }
 
-// Which eight columns of a row a thread has.  Rows on 16-byte boundaries, whose length is a multiple of eight (WIDE): thread k has columns
-// 8 k .. 8 k + 7, in one or two accesses.  Other rows: the threads of a warp have its 256 columns in turn, element i of lane l being
-// column l + 32 i, so that each access of the warp is one piece of memory.  A row's dropout is made in eights either way (keep8).
-// FULL: every thread's eight are inside the row.
+// Which eight columns of a row a thread has.  Rows whose length is a multiple of eight (WIDE): thread k has columns 8 k .. 8 k + 7, in one
+// or two accesses where rows lie on 16-byte boundaries (`whole`), else one by one: what a thread adds up follows from the sizes, not
+// from where a row lies.  Other rows: the threads of a warp have its 256 columns in turn, element i of lane l being column l + 32 i,
+// so that each access of the warp is one piece of memory.  A row's dropout is made in eights either way (Keep).
+// FULL: every thread's eight are inside the row, and whole.
 template <bool WIDE, bool FULL = false> struct Columns {
     uint32_t c0, dim;  // below 2^31
-    __device__ __forceinline__ Columns(uint32_t k, uint32_t dim_) : c0(WIDE ? 8 * k : 256 * (k >> 5) + (k & 31)), dim(dim_) {}
+    bool whole;
+    __device__ __forceinline__ Columns(uint32_t k, uint32_t dim_, bool whole_ = true) : c0(WIDE ? 8 * k : 256 * (k >> 5) + (k & 31)), dim(dim_), whole(FULL || whole_) {}
     __device__ __forceinline__ uint32_t col(int i) const { return c0 + (WIDE ? i : 32 * i); }
     __device__ __forceinline__ bool has(int i) const { return FULL || (WIDE ? c0 : c0 + 32 * i) < dim; }
     __device__ __forceinline__ bool any() const { return FULL || c0 < dim; }
@@ -74,7 +76,7 @@ template <typename T> struct Eight {
     }
     // STREAM: read once
     template <bool STREAM, bool WIDE, bool FULL> __device__ __forceinline__ void load(const T *row, const Columns<WIDE, FULL> &c) {
-        if constexpr (WIDE) {
+        if (WIDE && c.whole) {
             if (c.any())
 #pragma unroll
                 for (int i = 0; i < N; ++i)
@@ -96,7 +98,7 @@ template <typename T> struct Eight {
         }
     }
     template <bool WIDE, bool FULL> __device__ __forceinline__ void store(T *row, const Columns<WIDE, FULL> &c) const {
-        if constexpr (WIDE) {
+        if (WIDE && c.whole) {
             if (c.any())
 #pragma unroll
                 for (int i = 0; i < N; ++i) reinterpret_cast<uint4 *>(row + c.c0)[i] = w[i];

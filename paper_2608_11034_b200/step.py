@@ -13,7 +13,7 @@ an order that the sizes and the token ids fix, random numbers from a counter.
                                             output projection; the scores are never kept
 
 ``include/scout_step.h`` has the definitions.  What ``replay`` says of streams, autograd (the calls raise where
-it would have to record them) and bounded waits (``replay.waits_checked``; the loss has such waits) holds here too.
+it would have to record them) and bounded waits (``replay.waits_checked``; join and loss have such waits) holds here too.
 """
 from __future__ import annotations
 

@@ -168,3 +168,33 @@ def test_refusals():
     from paper_2608_11034_b200 import binding
     with pytest.raises(binding.ScoutError):
         step.join_forward(None, torch.zeros(2, 16392, device="cuda"))
+
+
+@pytest.mark.parametrize("tb,ts,tw", [(BF, BF, BF), (H, F, F), (F, F, F)])
+@pytest.mark.parametrize("rows,dim,groups,parts", [(70, 520, 5, "xgpnd"), (41, 2048, 41, "xgpnd"), (700, 64, 1, "xpnd"), (37, 4096, 1, "gnd"), (12, 4224, 3, "xgpnd"),
+                                                   (33, 777, 3, "xgpnd"), (9, 9001, 1, "xgpnd")])
+def test_bits_do_not_depend_on_where_rows_lie(rows, dim, groups, parts, tb, ts, tw):
+    from paper_2608_11034_b200 import step
+
+    def moved(t, gap):
+        if t is None or t.dim() != 2 or t.shape[0] != rows:
+            return t
+        room = torch.full((rows, dim + gap), math.nan, dtype=t.dtype, device="cuda")
+        room[:, 1:dim + 1] = t
+        return room[:, 1:dim + 1]
+
+    s = inputs(rows, dim, groups, tb, ts, tw, parts)
+    weights = {n: s[n] for n in ("gate", "post", "norm")}
+
+    def both(s, w):
+        how = dict(gate=w["gate"], post_weight=w["post"], norm_weight=w["norm"], scale=0.7, p=0.2, seed=SEED, offset=OFFSET)
+        y, n, stats = step.join_forward(s["x"], s["block"], **how)
+        dy = None if s["dy"] is None else s["dy"].to(y.dtype)
+        return (y, n, stats, *step.join_backward(dy, s["dn"] if n is not None else None, s["block"], y, stats, **how))
+
+    want = both(s, weights)
+    # weights off 16-byte boundaries too
+    off = {n: None if w is None else torch.cat([w.new_zeros(1), w.reshape(-1)])[1:].view(w.shape) for n, w in weights.items()}
+    for gap, w in ((9, weights), (8, weights), (0, off), (9, off)):
+        there = {n: moved(t, gap) if gap else t for n, t in s.items() if n in ("x", "block", "dy", "dn")}
+        assert all(a is None or torch.equal(a, b) for a, b in zip(want, both(there, w))), gap
