@@ -16,13 +16,13 @@ namespace step {
 namespace join {
 namespace {
 
-// ---- rows in registers: off 16-byte boundaries, not of whole eights, or wider than 4096 ----------------------------------------------------
+// ---- rows in registers: off 16-byte boundaries, not of whole eights, or wider than 8192 ----------------------------------------------------
 // The next row's elements are fetched into the registers of the present one's as soon as those are free: b once it is widened, x once y
 // is made.
 template <typename TB, typename TS, typename TW, int V, bool WIDE>
-__global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __grid_constant__ Args a) {
+__global__ void __maxnreg__(V == 2 ? FORWARD_REGISTERS : BACKWARD_REGISTERS) join_forward(const __grid_constant__ Args a) {
     using Cols = Columns<WIDE>;
-    __shared__ float slots[2][MOST<V> / 32];
+    __shared__ float slots[2][MOST / 32];
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
     const uint64_t offset = a.drop.cut ? a.drop.at() : 0;
@@ -104,9 +104,9 @@ __global__ void __launch_bounds__(MOST<V>, V == 2 ? 3 : 1) join_forward(const __
 }
 
 template <typename TB, typename TS, typename TW, int V, bool WIDE>
-__global__ void __launch_bounds__(MOST<V>, V == 2 ? 2 : 1) join_backward(const __grid_constant__ Args a) {
+__global__ void __maxnreg__(BACKWARD_REGISTERS) join_backward(const __grid_constant__ Args a) {
     using Cols = Columns<WIDE>;
-    __shared__ float slots[2][MOST<V> / 32];
+    __shared__ float slots[2][MOST / 32];
     extern __shared__ float sums[];
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
@@ -302,12 +302,12 @@ Shape shape(const scout_join_t *j, bool backward) {
     Shape s = {};
     const uint64_t rows = j->rows, dim = j->dim;
     const int eights = (int)((dim + 255) / 256 * 32);  // whole warps' worth
-    s.v = eights > 2 * MOST<2> ? 4 : 2;
+    s.v = eights > 2 * MOST ? 4 : 2;
     s.team = (eights / s.v + 31) / 32 * 32;
     s.teams = std::max(1, 128 / s.team);
     s.full = (uint64_t)s.team * s.v * 8 == dim;
     const int threads = s.team * s.teams;
-    s.blocks = s.v == 2 ? (backward ? 2 : 3) * std::max(1, MOST<2> / threads) : 1;
+    s.blocks = s.v == 2 && threads <= 256 ? (backward ? 2 : 3) * (256 / threads) : 1;
     if (dim % 8 == 0 && s.v == 2) {
         // Two to four rows of each team, of as many blocks as registers allow, in 160 KiB of an SM, so that the weights stay in the rest;
         // where two do not fit, all of shared memory, and fewer blocks.
@@ -316,6 +316,7 @@ Shape shape(const scout_join_t *j, bool backward) {
         s.stages = fit(160 << 10);
         for (; s.stages < 2; --s.blocks)
             if ((s.stages = fit(227 << 10)) >= 2 || s.blocks == 1) break;
+        if (s.stages < 2) s.stages = 0;  // rows of over 100 KB: in registers
     }
     const int64_t want = (int64_t)SMS * s.blocks * s.teams;
     s.per = std::max<int64_t>(1, ((int64_t)rows + want - 1) / want);
@@ -326,7 +327,7 @@ template <typename TB, typename TS, typename TW, int V, bool WIDE> int launch(co
     const unsigned threads = s.team * s.teams;
     if (backward) {
         constexpr int each = (V == 2 ? 1 : 3) * V * 8 * 4;  // bytes of a thread's sums in shared memory
-        if (int rc = allow_smem<join_backward<TB, TS, TW, V, WIDE>>(each * MOST<V>)) return rc;
+        if (int rc = allow_smem<join_backward<TB, TS, TW, V, WIDE>>(each * MOST)) return rc;
         join_backward<TB, TS, TW, V, WIDE><<<(unsigned)((s.slabs + s.teams - 1) / s.teams), threads, each * threads, stream>>>(a);
     } else {
         join_forward<TB, TS, TW, V, WIDE><<<(unsigned)std::min<int64_t>((a.rows + s.teams - 1) / s.teams, SMS * s.blocks), threads, 0, stream>>>(a);

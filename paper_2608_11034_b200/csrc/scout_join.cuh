@@ -10,8 +10,9 @@ namespace step {
 namespace join {
 
 constexpr int MAX_DIM = 16384;
-// A thread has V eights of a row: two up to 4096 columns, four beyond.
-template <int V> constexpr int MOST = V == 2 ? 256 : 512;  // threads of a block
+// A thread has V eights of a row: two up to 8192 columns, four beyond.
+constexpr int MOST = 512;  // threads of a block
+constexpr int FORWARD_REGISTERS = 80, BACKWARD_REGISTERS = 128;  // with V = 2: 768 and 512 threads an SM
 
 struct Args {
     const void *x, *b, *dy, *dn, *yin, *gate, *post, *norm;
@@ -65,7 +66,7 @@ template <typename T> __device__ __forceinline__ T *row_of(void *p, uint32_t str
 
 // With h = scale g (masked) and c = b rms(b) (masked), du = h gate, and over the rows of one gate S = sum of h c gives both of
 //     d_gate = post S,   d_post = sum over gates of gate S,
-// so that a row adds to two column sums, S and d_norm: in registers, or beyond 4096 columns in shared memory.  d_post takes its part
+// so that a row adds to two column sums, S and d_norm: in registers, or beyond 8192 columns in shared memory.  d_post takes its part
 // when a gate's rows (or the run) end.
 template <int V> struct Sums {
     static constexpr bool REGS = V == 2;
@@ -83,7 +84,7 @@ enum { D_POST, GATE_SUM, D_NORM };
 struct Shape {
     int v, team, teams, blocks;  // of an SM
     bool full;                   // the team's columns are the row's
-    int stages, stage_bytes;     // of the ring; none where rows are wider than 4096 or not of whole eights
+    int stages, stage_bytes;     // of the ring; none where rows are wider than 8192 or not of whole eights
     int64_t slabs, per;
 };
 

@@ -1,4 +1,4 @@
-// The join's kernels for rows on 16-byte boundaries of up to 4096 columns: a team's first thread has whole rows copied into a ring in
+// The join's kernels for rows on 16-byte boundaries of up to 8192 columns: a team's first thread has whole rows copied into a ring in
 // shared memory, as far ahead as it holds, and the team takes them from there.  The wait of a row's first sum says that everybody is done
 // with the row before, whose place is then filled again.
 //
@@ -34,11 +34,11 @@ template <typename T, typename COLS> __device__ __forceinline__ void from_ring(E
 }
 
 // FULL: every operand is there and the threads' columns are the row's, so that nothing is asked on the way.
-template <typename TB, typename TS, typename TW, bool FULL> __global__ void __launch_bounds__(MOST<2>, 3) forward_rows(const __grid_constant__ Args a) {
+template <typename TB, typename TS, typename TW, bool FULL> __global__ void __maxnreg__(FORWARD_REGISTERS) forward_rows(const __grid_constant__ Args a) {
     constexpr int V = 2;
     using Cols = Columns<true, FULL>;
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ float slots[2][MOST<V> / 32];
+    __shared__ float slots[2][MOST / 32];
     __shared__ uint64_t bars[MOST_TEAMS * MOST_STAGES];
     __shared__ uint32_t dead;
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;
@@ -155,11 +155,11 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __la
     if (*patience.dead) tc::let_flights_end();
 }
 
-template <typename TB, typename TS, typename TW, bool FULL> __global__ void __launch_bounds__(MOST<2>, 2) backward_rows(const __grid_constant__ Args a) {
+template <typename TB, typename TS, typename TW, bool FULL> __global__ void __maxnreg__(BACKWARD_REGISTERS) backward_rows(const __grid_constant__ Args a) {
     constexpr int V = 2;
     using Cols = Columns<true, FULL>;
     extern __shared__ __align__(128) uint8_t ring[];
-    __shared__ float slots[2][MOST<V> / 32];
+    __shared__ float slots[2][MOST / 32];
     __shared__ uint64_t bars[MOST_TEAMS * MOST_STAGES];
     __shared__ uint32_t dead;
     const uint32_t t = threadIdx.x % a.team, team = threadIdx.x / a.team, warps = a.team / 32;

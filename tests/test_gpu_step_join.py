@@ -71,6 +71,13 @@ def test_types_and_rows_that_lie_apart(rows, dim, groups, strided, tb, ts, tw):
     check(rows, dim, groups, tb, ts, tw, "xgpnd", 0.1, strided=strided)
 
 
+@pytest.mark.parametrize("tb,ts,tw", [(BF, BF, BF), (H, F, F), (F, F, F)])
+@pytest.mark.parametrize("rows,dim", [(301, 6144), (5, 7168), (310, 8192), (150, 8200)])
+def test_wide_rows_through_shared_memory_and_not(rows, dim, tb, ts, tw):
+    """Two rows of eight thousand fp32 columns and their gradients do not fit into shared memory; those of six thousand do."""
+    check(rows, dim, 1, tb, ts, tw, "xgpnd", 0.1)
+
+
 @pytest.mark.parametrize("parts", ["", "x", "n", "xn", "xp", "xg", "xgnd", "xpnd", "gpnd", "gpn", "xgpn", "pd", "xgd"])
 @pytest.mark.parametrize("rows,dim", [(37, 200), (12, 2048), (6, 9000)])
 def test_parts_that_are_left_out(parts, rows, dim):
