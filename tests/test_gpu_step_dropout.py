@@ -79,3 +79,21 @@ def test_refusals():
                 lambda: step.dropout(x, 0.1, seed=1, offset=torch.zeros(1, dtype=torch.int64))):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("dtype", [BF, H, F])
+@pytest.mark.parametrize("rows,cols", [(1, 65), (3, 67), (40, 71), (513, 101), (7, 1001), (2, 4095), (77, 255), (1000, 1027), (5, 100001)])
+def test_rows_one_behind_the_other_of_any_length(rows, cols, dtype):
+    """Taken as one long row: the bits of rows that lie apart, and nothing behind the last element is written."""
+    from paper_2608_11034_b200 import binding as b
+    from paper_2608_11034_b200 import step
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dtype)
+    want = definition(x, 0.3, 5, 6)
+    assert torch.equal(step.dropout(x, 0.3, seed=5, offset=6), want)
+    wide = torch.full((rows, cols + 2), math.nan, dtype=dtype, device="cuda")
+    wide[:, :cols] = x
+    assert torch.equal(step.dropout(wide[:, :cols], 0.3, seed=5, offset=6), want)
+    room = torch.full((rows * cols + 64,), 7.0, dtype=dtype, device="cuda")
+    code = {BF: b.DT_BF16, H: b.DT_F16, F: b.DT_F32}[dtype]
+    b.scout_dropout(code, rows, cols, x.data_ptr(), cols, room.data_ptr(), cols, 0.3, 5, 6, 0, torch.cuda.current_stream().cuda_stream)
+    assert torch.equal(room[:rows * cols].view(rows, cols), want) and (room[rows * cols:] == 7.0).all()
