@@ -330,54 +330,89 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 128;
         for (int i = pair; i < work.items; i += pairs) {
             const Item it = work.at(i);
+            const int64_t m = (int64_t)it.m * TM + row, n0 = (int64_t)it.n * TN + half * 128;
+            // what the row's end needs, on its way while the products are made
+            int target = -1;
+            float lse = 0.f, g = 0.f, at_target = 0.f;
+            if constexpr (KIND == SCORES || KIND == GRADS) target = a.target[m];
+            if constexpr (KIND == GRADS) lse = a.row_lse[m], g = a.row_g[m], at_target = a.row_score[m];
             float sum[128];
+            if (KIND != SCORES && KIND != GRADS && it.steps == 0)
 #pragma unroll
-            for (int c = 0; c < 128; ++c) sum[c] = 0.f;
+                for (int c = 0; c < 128; ++c) sum[c] = 0.f;
             for (int k = 0; k < it.steps; k += CHAIN, ++chain) {
                 const uint32_t buf = chain & 1;
                 if (!patience.wait_warp(sum_full + 8 * buf, (chain >> 1) & 1)) goto done;
                 tc::tc_fence_after();
 #pragma unroll
-                for (int c = 0; c < 4; ++c) {
-                    uint32_t r[32];
+                for (int c = 0; c < 4; c += 2) {
+                    uint32_t r[32], q[32];
                     tc::tmem_load32(r, mine + buf * TN + c * 32);
+                    tc::tmem_load32(q, mine + buf * TN + c * 32 + 32);
                     tc::tmem_load_wait(r);
+                    tc::tmem_load_wait(q);
 #pragma unroll
-                    for (int e = 0; e < 32; ++e) sum[c * 32 + e] += __uint_as_float(r[e]);
+                    for (int e = 0; e < 32; ++e) {
+                        sum[c * 32 + e] = k == 0 ? __uint_as_float(r[e]) : sum[c * 32 + e] + __uint_as_float(r[e]);
+                        sum[c * 32 + 32 + e] = k == 0 ? __uint_as_float(q[e]) : sum[c * 32 + 32 + e] + __uint_as_float(q[e]);
+                    }
                 }
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::bar_arrive_cluster(tc::in_block(sum_empty + 8 * buf, 0));
             }
-            const int64_t m = (int64_t)it.m * TM + row, n0 = (int64_t)it.n * TN + half * 128;
             if constexpr (KIND == SCORES) {
-                const int left = (int)min(128ll, (long long)(a.pv - n0)), at = a.target[m] - (int)n0;
+                const int left = (int)min(128ll, (long long)(a.pv - n0)), at = target - (int)n0;
+                const bool here = at >= 0 && at < 128;
                 if (left < 128) {
 #pragma unroll
                     for (int c = 0; c < 128; ++c) sum[c] = c < left ? sum[c] : -CUDART_INF_F;
                 }
-                float top = -CUDART_INF_F, score = 0.f, total = 0.f;
+                if (__any_sync(0xFFFFFFFFu, here)) {
+                    float score = 0.f;
 #pragma unroll
-                for (int c = 0; c < 128; ++c) top = fmaxf(top, sum[c]), score = c == at ? sum[c] : score;
-                if (at >= 0 && at < 128) a.row_rough[m] = score;
+                    for (int c = 0; c < 128; ++c) score = c == at ? sum[c] : score;
+                    if (here) a.row_rough[m] = score;
+                }
+                float top = -CUDART_INF_F;
+#pragma unroll
+                for (int c = 0; c < 128; ++c) top = fmaxf(top, sum[c]);
                 const float from = fabsf(top) == CUDART_INF_F ? 0.f : top;
+                const tc::F2 less = tc::f2(-from, -from), scale = tc::f2(LOG2E, LOG2E);
+                tc::F2 total = tc::f2(0.f, 0.f);
 #pragma unroll
-                for (int c = 0; c < 128; ++c) total += exp2_fast((sum[c] - from) * LOG2E);
-                a.part[(int64_t)(it.n * 2 + half) * a.padded + m] = make_float2(top, total);
+                for (int c = 0; c < 128; c += 2) {
+                    const float2 e = tc::split(tc::mul2(tc::add2(tc::f2(sum[c], sum[c + 1]), less), scale));
+                    total = tc::add2(total, tc::f2(exp2_fast(e.x), exp2_fast(e.y)));
+                }
+                const float2 both = tc::split(total);
+                a.part[(int64_t)(it.n * 2 + half) * a.padded + m] = make_float2(top, both.x + both.y);
             } else if constexpr (KIND == GRADS) {
-                const int left = (int)min(128ll, (long long)(a.pv - n0)), at = a.target[m] < 0 ? -1 : (int)max(-1ll, min(128ll, (long long)a.target[m] - a.v0 - n0));
-                const float lse = a.row_lse[m], g = a.row_g[m] * power2(a.scale_log2), at_target = a.row_score[m];
-                const bool on = a.target[m] >= 0;
+                const int left = (int)min(128ll, (long long)(a.pv - n0));
+                const int64_t at = target - a.v0 - n0;
+                const bool on = target >= 0, here = on && at >= 0 && at < 128;
+                g *= power2(a.scale_log2);
+                const tc::F2 less = tc::f2(-lse, -lse), scale = tc::f2(LOG2E, LOG2E), gg = tc::f2(g, g);
+#pragma unroll
+                for (int c = 0; c < 128; c += 2) {
+                    const float2 e = tc::split(tc::mul2(tc::add2(tc::f2(sum[c], sum[c + 1]), less), scale));
+                    const float2 p = tc::split(tc::mul2(gg, tc::f2(exp2_fast(e.x), exp2_fast(e.y))));
+                    sum[c] = p.x, sum[c + 1] = p.y;
+                }
+                if (left < 128 || !__all_sync(0xFFFFFFFFu, on)) {  // columns and rows that are not there
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) sum[c] = on && c < left ? sum[c] : 0.f;
+                }
+                if (__any_sync(0xFFFFFFFFu, here)) {
+                    const float value = g * at_target;
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) sum[c] = here && c == (int)at ? value : sum[c];
+                    if (here) a.row_rest[m] = value - Half<T>::up(Half<T>::down(value));
+                }
                 T *dst = reinterpret_cast<T *>(a.gs) + m * a.piece + n0;
 #pragma unroll
                 for (int c = 0; c < 128; c += 16) {
                     uint32_t w[8];
-#pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const float p = exp2_fast((sum[c + e] - lse) * LOG2E);
-                        sum[c + e] = on && c + e < left ? g * (c + e == at ? at_target : p) : 0.f;
-                        if (c + e == at) a.row_rest[m] = sum[c + e] - Half<T>::up(Half<T>::down(sum[c + e]));
-                    }
 #pragma unroll
                     for (int e = 0; e < 8; ++e) w[e] = Half<T>::pack(sum[c + 2 * e], sum[c + 2 * e + 1]);
                     store32(dst + c, w);
