@@ -72,7 +72,7 @@ SCOUT_API int scout_embed_backward(uint32_t id_dtype, uint32_t dtype, uint32_t o
  *   p            0 <= p < 1
  *   d_offset     device, one number, or NULL; read when the kernel runs, so that a captured
  *                call can drop other places each time it is replayed
- * rows up to 2^32, cols below 2^31.  y may be x. */
+ * rows up to 2^32, cols below 2^31.  y may be x, with x's row stride. */
 SCOUT_API int scout_dropout(uint32_t dtype, uint64_t rows, uint64_t cols, const void *x, uint64_t x_stride, void *y,
                             uint64_t y_stride, double p, uint64_t seed, uint64_t offset, const uint64_t *d_offset,
                             void *stream);
