@@ -409,6 +409,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                     for (int c = 0; c < 128; ++c) sum[c] = here && c == (int)at ? value : sum[c];
                     if (here) a.row_rest[m] = value - Half<T>::up(Half<T>::down(value));
                 }
+                if (m >= (*a.count + TK - 1) / TK * TK) continue;  // TABLE takes rows in steps of TK; STATES makes nothing of others
                 T *dst = reinterpret_cast<T *>(a.gs) + m * a.piece + n0;
 #pragma unroll
                 for (int c = 0; c < 128; c += 16) {
@@ -418,6 +419,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                     store32(dst + c, w);
                 }
             } else if constexpr (KIND == STATES) {
+                if (m >= *a.count) continue;
                 float *dst = a.dxp + ((int64_t)it.split * a.padded + m) * a.dim + n0;
 #pragma unroll
                 for (int c = 0; c < 128; c += 8) {
@@ -741,9 +743,12 @@ template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t st
     a.scale_log2 = Half<T>::is_bf16 ? 0 : 13;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     CUtensorMap mx, mw, mg, mg_t, mx_t, mw_n;
+    // G has rows to whole steps of TABLE; STATES's tiles are zeros beyond (14 rows, 400 columns, 59712 of vocabulary: 82 us with all of a tile's
+    // rows written and read, 73 so).  Not so the rows of x, which stay in L2: zeros take longer than those.
+    const uint64_t taken = (a.rows + TK - 1) / TK * TK;
     if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, HALF)) return rc;
     if (int rc = map_of<T>(&mx_t, a.xc, l.padded, a.dim, a.dim, TK)) return rc;
-    if (int rc = map_of<T>(&mg, a.gs, l.padded, l.piece, l.piece, HALF)) return rc;
+    if (int rc = map_of<T>(&mg, a.gs, taken, l.piece, l.piece, HALF)) return rc;
     if (int rc = map_of<T>(&mg_t, a.gs, l.padded, l.piece, l.piece, TK)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     const int64_t row_tiles = (int64_t)(l.padded / TM), dim_tiles = (a.dim + TN - 1) / TN;
