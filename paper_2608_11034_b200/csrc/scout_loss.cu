@@ -38,7 +38,7 @@ constexpr int TM = 256, TN = 256, TK = 64, STAGES = 6, CHAIN = 1024 / TK;  // in
 constexpr int HALF = 128, THREADS = 384, BOX = 64 * TK * 2, STAGE = 2 * HALF / 64 * BOX, PAIRS = SMS / 2;
 constexpr int TURN = 32 * 33 * 4;  // a warp's 32 x 32 results on their way to rows that start anywhere
 constexpr int SMEM = STAGES * STAGE + 8 * TURN + 1024;  // 1024: the swizzle repeats every 1 KiB, dynamic shared memory starts anywhere
-constexpr int FEW = 64;
+constexpr int FEW = 64;  // rows of one box
 constexpr int GROUP = 32;  // row tiles that share a tile of w while it is in L2: 8192 rows, 64 MiB with 4096 columns
 enum { SCORES, GRADS, TABLE, STATES };
 
@@ -61,7 +61,7 @@ struct Args {
     float2 *part;       // [2 * tiles of the vocabulary][padded]: maximum and sum of 128 columns
     float *dxp;         // [splits][padded][dim]
     int64_t piece, v0, pv;  // columns of gs, first column and columns of the current piece
-    int32_t splits, per, first, id64, wide_x, out_f32, accumulate, wide, tiles_out, scale_log2;
+    int32_t splits, per, first, id64, wide_x, out_f32, accumulate, wide, tiles_out, scale_log2, thin;
     uint32_t *gave_up;
 };
 
@@ -274,18 +274,22 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
             tc::prefetch_map(&map_a);
             tc::prefetch_map(&map_b);
             uint32_t n = 0;
+            // Of up to FEW rows only those are brought; what the others' places in shared memory hold reaches their own results alone (11 rows,
+            // 3960 columns, 2125 of vocabulary: forward 42 us with all, 36 so, gradients 67 and 62).
+            const bool thin = !mn_a && a.thin;
+            const uint32_t bytes = thin ? 2 * STAGE - (2 * HALF / 64 - 1) * BOX : 2 * STAGE;
             for (int i = pair; i < work.items; i += pairs) {
                 const Item it = work.at(i);
                 for (int k = 0; k < it.steps; ++k, ++n) {
                     const uint32_t s = n % STAGES, to = base + s * STAGE;
                     const int at = (it.k0 + k) * TK, m0 = it.m * TM + (int)rank * HALF, n0 = it.n * TN + (int)rank * HALF;
                     if (!patience.wait(empty + 8 * s, ((n / STAGES) & 1) ^ 1)) goto done;
-                    if (rank == 0) tc::bar_expect(full + 8 * s, 2 * STAGE);
+                    if (rank == 0) tc::bar_expect(full + 8 * s, bytes);
                     const uint32_t bar = tc::in_block(full + 8 * s, 0);
                     if constexpr (mn_a) {
 #pragma unroll
                         for (int c = 0; c < HALF / 64; ++c) tc::pair_tma_2d(to + c * BOX, &map_a, bar, m0 + c * 64, at);
-                    } else {
+                    } else if (!thin || rank == 0) {
                         tc::pair_tma_2d(to, &map_a, bar, at, m0);
                     }
                     if constexpr (mn_b) {
@@ -689,7 +693,7 @@ int check_inputs(uint32_t dtype, uint32_t id_dtype, uint64_t dim, uint64_t vocab
 }
 void place(Args *a, const Layout &l, void *workspace, bool backward) {
     uint8_t *const ws = (uint8_t *)workspace;
-    a->padded = (int64_t)l.padded, a->piece = (int64_t)l.piece, a->splits = l.splits, a->per = l.per;
+    a->thin = a->rows <= FEW, a->padded = (int64_t)l.padded, a->piece = (int64_t)l.piece, a->splits = l.splits, a->per = l.per;
     a->count = (int32_t *)(ws + l.count), a->g_ref = (float *)(ws + l.g_ref), a->which = (int32_t *)(ws + l.which), a->target = (int32_t *)(ws + l.target);
     a->row_score = (float *)(ws + l.row_score), a->xc = ws + l.xc;
     if (backward) {
@@ -729,7 +733,7 @@ template <typename T> int map_of(CUtensorMap *m, const void *p, uint64_t rows, u
 
 template <typename T> int run_forward(Args &a, const Layout &l, cudaStream_t stream) {
     CUtensorMap mx, mw;
-    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, HALF)) return rc;
+    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, a.thin ? FEW : HALF)) return rc;
     if (int rc = map_of<T>(&mw, a.w, a.vocab, a.dim, a.w_stride, HALF)) return rc;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
@@ -746,9 +750,9 @@ template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t st
     // G has rows to whole steps of TABLE; STATES's tiles are zeros beyond (14 rows, 400 columns, 59712 of vocabulary: 82 us with all of a tile's
     // rows written and read, 73 so).  Not so the rows of x, which stay in L2: zeros take longer than those.
     const uint64_t taken = (a.rows + TK - 1) / TK * TK;
-    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, HALF)) return rc;
+    if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, a.thin ? FEW : HALF)) return rc;
     if (int rc = map_of<T>(&mx_t, a.xc, l.padded, a.dim, a.dim, TK)) return rc;
-    if (int rc = map_of<T>(&mg, a.gs, taken, l.piece, l.piece, HALF)) return rc;
+    if (int rc = map_of<T>(&mg, a.gs, taken, l.piece, l.piece, a.thin ? FEW : HALF)) return rc;
     if (int rc = map_of<T>(&mg_t, a.gs, l.padded, l.piece, l.piece, TK)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     const int64_t row_tiles = (int64_t)(l.padded / TM), dim_tiles = (a.dim + TN - 1) / TN;
