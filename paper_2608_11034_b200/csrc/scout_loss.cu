@@ -14,8 +14,8 @@
 //
 // The tensor cores truncate when they add to an accumulator; chains of products are cut at 1024 terms and added in fp32.
 //
-// What bounds it: the products.  2048 rows, 4096 columns, 32000 of vocabulary: each of the four 330 to 340 us (1.6 PFLOP/s; the tensor
-// pipe is busy for 87 to 97 % of the time).  8192 rows (a tenth of them padding) over 128000, forward and gradients: 24.4 ms, 30.9 TFLOP (of
+// What bounds it: the products.  2048 rows, 4096 columns, 32000 of vocabulary: the four take 335 to 366 us each (1.47 to 1.6 PFLOP/s; the
+// tensor pipe is busy for 80 to 89 % of the elapsed time).  8192 rows (a tenth of them padding) over 128000, forward and gradients: 24.4 ms, 30.9 TFLOP (of
 // which 7.7 make the scores again) at 1.27 PFLOP/s, which is the power limit: one library product after another runs at 1.31 to 1.40 there.
 // A tile on one SM (128 x 256) takes the same time at that limit, on pairs of SMs a tenth less where it is not reached.
 #include <algorithm>
