@@ -1,6 +1,7 @@
 // The join's kernels for rows on 16-byte boundaries of up to 8192 columns: a team's first thread has whole rows copied into a ring in
-// shared memory, as far ahead as it holds, and the team takes them from there.  The wait of a row's first sum says that everybody is done
-// with the row before, whose place is then filled again.
+// shared memory, as far ahead as it holds, and the team takes them from there.  Once everybody has come to a row's first sum, the place of
+// the row before is filled again: a wait of the block says so, or of the warp where a team is one (its sum is shuffles, which order no
+// memory).
 //
 // Bound by memory as long as 40 KB an SM are on the way all the time, which rows in registers do not reach, and then by instructions: 16384 x
 // 4096 in bf16, every part, dropout: forward 102 us (537 MB: 83), gradient 177 (805 MB: 125; 770 instructions a row and thread, of which
@@ -67,6 +68,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __ma
     At at, before;  // the present row's place, and the one that is free once everybody has come to the present row
     bool first = true;
     const auto refill = [&] {
+        __syncwarp();  // of a team of one warp, the others' reads of the row before
         if (!first) issue(before.stage), before.next(a.stages);
         first = false;
     };
@@ -195,6 +197,7 @@ template <typename TB, typename TS, typename TW, bool FULL> __global__ void __ma
     for (int s = 0; s < a.stages; ++s) issue(s);
     At at, before;  // the present row's place, and the one that is free once everybody has come to the present row
     const auto refill = [&](int64_t it) {
+        __syncwarp();  // of a team of one warp, the others' reads of the row before
         if (it > 0) issue(before.stage), before.next(a.stages);
     };
     float *const s0 = slots[0] + team * warps, *const s1 = slots[1] + team * warps;
