@@ -576,10 +576,14 @@ __global__ void __launch_bounds__(32 * JOIN_WAYS) join_scores(const __grid_const
     if (threadIdx.y == 0 && m < count) {
         for (int k = 1; k < JOIN_WAYS; ++k) take(part[k][threadIdx.x]);
         float lse = (fabsf(top) == CUDART_INF_F ? 0.f : top) + logf(total);
-        // The tensor cores' sums come out small, the more so the larger they are, and the largest is often the target's.  Its share of lse
-        // is put right with the score that take_rows made, to first order; what the others are off is an average over many.
-        const float score = a.row_score[m], rough = a.row_rough[m], off = expf(rough - lse) * (score - rough);
-        if (fabsf(off) < 1e-2f) lse += off;  // finite, that is
+        // The tensor cores' sums come out small, the more so the larger they are, and the largest is often the target's: its term goes out
+        // of the sum and comes back with the score that take_rows made.  What the others are off is an average over many.  A score of 2^13
+        // that is off by 0.045: loss 0, -0.045 as it stands.
+        const float score = a.row_score[m], rough = a.row_rough[m];
+        if (isfinite(score) && isfinite(rough) && isfinite(top) && isfinite(total)) {
+            const float others = fmaxf(total - exp2_fast((rough - top) * LOG2E), 0.f), below = top - score;
+            lse = below < 1.f ? score + log1pf(others * exp2_fast(below * LOG2E)) : top + logf(others + exp2_fast(-below * LOG2E));
+        }
         const int t = a.which[m];
         a.lse[t] = lse, a.loss[t] = lse - score;
     }

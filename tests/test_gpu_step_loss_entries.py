@@ -1,0 +1,73 @@
+"""Entries of the cross entropy that are made more exactly than the others, on inputs that show them alone."""
+import math
+
+import pytest
+import torch
+
+import step_defn as defn
+
+pytestmark = pytest.mark.gpu
+BF, H, F = torch.bfloat16, torch.float16, torch.float32
+DIM = 1024
+
+
+def truncated(dtype, score, rows, vocab):
+    """x, w, targets: all rows alike, target 1, of which the exact score is `score` + 992 * 3 * 2^-16 (None: 2^13 instead of `score`), and all
+    other scores 0.  The target's score has 2^13 as its first term, beside which the tensor cores lose what they add afterwards, less than
+    2^-10 in 16 columns; they lose that of 48 to 64 times 16 columns.  In fp32 the warp adds it exactly: the lane that has columns 0 to 7 of
+    each 256 has no small terms, the other lanes no large one."""
+    x, w = torch.zeros(DIM, dtype=torch.float64), torch.zeros(DIM, dtype=torch.float64)
+    c = torch.arange(DIM)
+    small = (c // 8) % 32 != 0
+    x[small], w[small] = 0.75 * 2.0 ** -7, 2.0 ** -7
+    x[0], w[0] = 2.0 ** 7, 2.0 ** 6
+    if score is not None:
+        x[768], w[768] = -2.0 ** 7, 2.0 ** 6
+        x[769], w[769] = 1.0, score
+    table = torch.zeros(vocab, DIM, dtype=dtype, device="cuda")
+    table[1] = w.to(dtype)
+    exact = float((x * w).sum())
+    assert exact == (2.0 ** 13 if score is None else score) + 992 * 3 * 2.0 ** -16
+    return x.to(dtype).cuda().repeat(rows, 1), table, torch.ones(rows, dtype=torch.int64, device="cuda"), exact
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("rows", [1, 70])
+def test_a_sure_row_of_large_scores_loses_nothing(rows, dtype):
+    """lse is the score here, and all that may part them is the rounding of either to fp32: half of 2^-10 around 2^13."""
+    from paper_2608_11034_b200 import step
+    x, w, targets, _ = truncated(dtype, None, rows, 300)
+    loss, lse = step.loss_forward(x, w, targets)
+    assert (loss.abs() <= 2.0 ** -11).all() and ((lse - 2.0 ** 13).abs() < 0.06).all()
+    dx, _ = step.loss_backward(x, w, targets, lse, torch.ones(rows, device="cuda"))
+    assert (dx.double().abs() <= 2.0 ** -10 * w[1].double().abs()).all()
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("score", [-3.0, 0.5, 8.0, 10.0, 14.0])
+def test_what_the_tensor_cores_lose_of_a_targets_score(score, rows, dtype):
+    """The score itself is exact in fp32 (multiples of 2^-16 below 2^6 once the large terms have met).  lse: exponentials and their sum
+    are off by 2^-20 relative (2^-22 each, and as much for an argument of up to 2^4 that is rounded to fp32), and it is rounded to fp32."""
+    from paper_2608_11034_b200 import step
+    vocab = 20000
+    x, w, targets, exact = truncated(dtype, score, rows, vocab)
+    want = math.log(vocab - 1 + math.exp(exact))
+    loss, lse = step.loss_forward(x, w, targets)
+    off = 2.0 ** -20 + 2.0 ** -23 * abs(want)
+    assert float((lse.double() - want).abs().max()) <= off
+    assert float((loss.double() - (want - exact)).abs().max()) <= off + 2.0 ** -23 * abs(want - exact)
+
+
+@pytest.mark.parametrize("rows", [1, 70])
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf])
+def test_what_is_no_number_in_another_row_of_w(bad, rows):
+    """A score that is NaN or Inf makes lse that; one of -Inf counts for nothing."""
+    from paper_2608_11034_b200 import step
+    x, w, targets, exact = truncated(BF, 8.0, rows, 2000)
+    w[7, 9] = bad
+    loss, lse = step.loss_forward(x, w, targets)
+    if bad == -math.inf:
+        assert ((lse - math.log(1998 + math.exp(exact))).abs() <= 2.0 ** -17).all()
+    else:
+        assert (lse.isnan() if bad != bad else lse == bad).all() and (loss.isnan() if bad != bad else loss == bad).all()
