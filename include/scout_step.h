@@ -146,9 +146,10 @@ SCOUT_API int scout_loss_forward(uint32_t dtype, uint32_t id_dtype, uint64_t row
  *     G_tv = g_t (exp(s_tv - lse_t) - [v = target_t]),   dx_t = sum_v G_tv w_v
  *     dw_v = (accumulate ? dw_v : 0) + sum_t G_tv x_t
  * over the rows that count.  The scores are made again, in pieces of the vocabulary; G is
- * rounded to 16 bits for its products, which have fp32 sums (a row's entry at its target
- * enters dx with what that rounding took away).  dx has x's type, dw out_dtype (dtype or
- * SCOUT_DT_F32).  Every row of dx and dw is written.
+ * rounded to 16 bits for its products, which have fp32 sums.  A row's entry at its target
+ * enters with what that rounding took away: in dx always, in a row of dw for two of its
+ * tokens (which two follows from the targets alone).  dx has x's type, dw out_dtype (dtype
+ * or SCOUT_DT_F32).  Every row of dx and dw is written.
  *   dw           device [vocab][dim], row stride dw_stride */
 SCOUT_API int scout_loss_backward(uint32_t dtype, uint32_t id_dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim,
                                   uint64_t vocab, const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,

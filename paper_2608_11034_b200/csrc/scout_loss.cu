@@ -10,7 +10,8 @@
 // G is held with g divided by the largest |g| (GREF): a loss averaged over the batch has one g for all rows, whose rounding would
 // otherwise be the same in every term; in fp16 it is held 2^13 times that, where the products still fit and a probability of 1e-11
 // is not lost.  Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of
-// dx: join_states adds what the rounding took from that entry, times the target's row of w.  TABLE does so where rows are few.
+// dx, and of its target's row of dw: what the rounding took from that entry is added, times the target's row of w (join_states) and the
+// token's row of x (TABLE, of the first two tokens of a target).
 //
 // The tensor cores truncate when they add to an accumulator; chains of products are cut at 1024 terms and added in fp32.
 //
@@ -240,6 +241,71 @@ template <int KIND> struct Work {
     }
 };
 
+// TABLE: what rounding took from G at targets is given back to dw in fp32.  A row of dw has few tokens of its own, one or two in a large
+// vocabulary, and that rounding would be most of its error; where they are more, the roundings of a sum over as many are left, so a row
+// takes back what its first MOST tokens lost, in the order in which they are found.
+// A warp's lanes are 32 rows of dw: they look for their tokens while the tensor cores make a chain, and add them side by side.  2048 rows,
+// 4096 columns, 32000 of vocabulary, all gradients: 1114 us without, 1128 so (fp32 dw 1141 and 1254: its end takes longer); 8192, 512, 1000: 115, 121 (four
+// tokens 139, 16 172; all of them, one after the other with the lanes sharing a token's columns, 817).
+struct Targets {
+    static constexpr int MOST = 2, AT_ONCE = 128, LOADS = CHAIN * TK / AT_ONCE;
+    int taken = 0, n = 0;  // tokens that the lane's row has had, and has of this chain
+    uint32_t mine = 0;     // those, counted from t0, 16 bits each
+    // first: row of dw of lane 0; t0, t1: the chain's tokens (multiples of TK; those that do not count have the target -1)
+    __device__ __forceinline__ void look(const Args &a, int first, int t0, int t1) {
+        const int lane = threadIdx.x & 31;
+        int4 v[LOADS];
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            const int t = t0 + q * AT_ONCE + 4 * lane;
+            v[q] = make_int4(-1, -1, -1, -1);
+            if (t < t1) v[q] = *reinterpret_cast<const int4 *>(a.target + t);
+        }
+        n = 0, mine = 0;
+#pragma unroll
+        for (int q = 0; q < LOADS; ++q) {
+            const int row[4] = {v[q].x - first, v[q].y - first, v[q].z - first, v[q].w - first};
+            if (!__any_sync(0xFFFFFFFFu, (uint32_t)row[0] < 32 || (uint32_t)row[1] < 32 || (uint32_t)row[2] < 32 || (uint32_t)row[3] < 32)) continue;
+            const uint32_t open = __ballot_sync(0xFFFFFFFFu, taken + n < MOST);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                uint32_t here = __ballot_sync(0xFFFFFFFFu, (uint32_t)row[e] < 32 && (open >> (row[e] & 31) & 1));
+                for (; here; here &= here - 1) {
+                    const int l = __ffs(here) - 1;
+                    if (__shfl_sync(0xFFFFFFFFu, row[e], l) == lane && taken + n < MOST) mine |= (uint32_t)(q * AT_ONCE + 4 * l + e) << (16 * n++);
+                }
+            }
+        }
+    }
+    template <typename T> __device__ __forceinline__ void give_back(const Args &a, float (&sum)[128], int t0, int64_t n0) {
+        const int rounds = __reduce_max_sync(0xFFFFFFFFu, n);
+#pragma unroll 1
+        for (int i = 0; i < rounds; ++i) {
+            const bool on = i < n;
+            const int t = t0 + (on ? (int)(mine >> (16 * i) & 0xFFFF) : 0);
+            const float by = on ? a.row_rest[t] : 0.f;
+            const T *x = reinterpret_cast<const T *>(a.xc) + (int64_t)t * a.dim + n0;
+#pragma unroll
+            for (int c = 0; c < 128; c += 64) {
+                Eight<T> e[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    e[j].zero();
+                    if (on && n0 + c + 8 * j < a.dim) e[j].w[0] = *reinterpret_cast<const uint4 *>(x + c + 8 * j);
+                }
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+#pragma unroll
+                    for (int k = 0; k < 8; k += 2) {
+                        const float2 r = tc::split(tc::fma2(tc::f2(by, by), tc::f2(e[j].get(k), e[j].get(k + 1)), tc::f2(sum[c + 8 * j + k], sum[c + 8 * j + k + 1])));
+                        sum[c + 8 * j + k] = r.x, sum[c + 8 * j + k + 1] = r.y;
+                    }
+            }
+        }
+        taken += n;
+    }
+};
+
 template <typename T, int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
                                                                                                        const __grid_constant__ CUtensorMap map_out) {
@@ -344,8 +410,10 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
             if (KIND != SCORES && KIND != GRADS && it.steps == 0)
 #pragma unroll
                 for (int c = 0; c < 128; ++c) sum[c] = 0.f;
+            Targets targets;
             for (int k = 0; k < it.steps; k += CHAIN, ++chain) {
                 const uint32_t buf = chain & 1;
+                if constexpr (KIND == TABLE) targets.look(a, (int)(a.v0 + m) - lane, k * TK, min(k + CHAIN, it.steps) * TK);
                 if (!patience.wait_warp(sum_full + 8 * buf, (chain >> 1) & 1)) goto done;
                 tc::tc_fence_after();
 #pragma unroll
@@ -364,6 +432,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 tc::tc_fence_before();
                 __syncwarp();
                 if (lane == 0) tc::bar_arrive_cluster(tc::in_block(sum_empty + 8 * buf, 0));
+                if constexpr (KIND == TABLE) targets.template give_back<T>(a, sum, k * TK, n0);
             }
             if constexpr (KIND == SCORES) {
                 const int left = (int)min(128ll, (long long)(a.pv - n0)), at = target - (int)n0;
@@ -438,28 +507,6 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 const float ref = *a.g_ref * power2(-a.scale_log2);
                 const int64_t v = a.v0 + m;
                 const bool on = m < a.pv;
-                // With few rows the rounding of G at a target is all of its row's error, and is put right; with many it is one of many.
-                if (const int count = *a.count; count <= FEW) {
-#pragma unroll
-                    for (int t0 = 0; t0 < FEW; t0 += 32) {
-                        const int64_t mine = t0 + lane < count ? a.target[t0 + lane] : -1, first = v - lane;
-                        uint32_t here = __ballot_sync(0xFFFFFFFFu, mine >= first && mine < first + 32);  // targets among the warp's rows
-                        for (; here; here &= here - 1) {
-                            const int t = __ffs(here) - 1;
-                            if (__shfl_sync(0xFFFFFFFFu, mine, t) != v) continue;
-                            const float rest = a.row_rest[t0 + t];
-                            const T *x = reinterpret_cast<const T *>(a.xc) + (int64_t)(t0 + t) * a.dim + n0;
-#pragma unroll
-                            for (int c = 0; c < 128; c += 8) {
-                                if (n0 + c >= a.dim) break;
-                                Eight<T> e;
-                                e.w[0] = *reinterpret_cast<const uint4 *>(x + c);
-#pragma unroll
-                                for (int i = 0; i < 8; ++i) sum[c + i] = fmaf(rest, e.get(i), sum[c + i]);
-                            }
-                        }
-                    }
-                }
 #pragma unroll
                 for (int c = 0; c < 128; ++c) sum[c] *= ref;
                 if (a.tiles_out) {

@@ -71,3 +71,64 @@ def test_what_is_no_number_in_another_row_of_w(bad, rows):
         assert ((lse - math.log(1998 + math.exp(exact))).abs() <= 2.0 ** -17).all()
     else:
         assert (lse.isnan() if bad != bad else lse == bad).all() and (loss.isnan() if bad != bad else loss == bad).all()
+
+
+def half_step(x, dtype):
+    """Half of the distance between numbers of this type around x."""
+    return torch.exp2(torch.floor(torch.log2(x.abs()))) * defn.U[dtype]
+
+
+@pytest.mark.parametrize("dtype", [BF, H])
+@pytest.mark.parametrize("rows,count", [(1, 1), (64, 64), (65, 65), (100, 64), (100, 65), (300, 300), (1100, 1100)])
+@pytest.mark.parametrize("tokens", [1, 2, 3, 100, 2000])
+def test_the_gradient_at_a_target_is_not_rounded_to_16_bits(tokens, rows, count, dtype):
+    """Row t alone has a number in column 64 + t of x, and its target alone in that of w: dx there is G at the target times w, dw is that
+    times x, and the others' rounding does not reach them.  G at the target, g (p - 1), is off by what score and lse are off times g p, and
+    by 2^-20 relative for expm1 and the products; 16 bits would be off by up to 2^-8 or 2^-11, which dw is at those of a target's
+    tokens that come after two others."""
+    from paper_2608_11034_b200 import step
+    g = torch.Generator(device="cuda").manual_seed(rows + count)
+
+    def rand(*shape):
+        return torch.rand(*shape, generator=g, device="cuda")
+
+    vocab, wide = 1500, 64 + -(-rows // 8) * 8
+    x, w = torch.zeros(rows, wide, device="cuda"), torch.zeros(vocab, wide, device="cuda")
+    x[:, :64] = torch.randn(rows, 64, generator=g, device="cuda")
+    w[:, :64] = torch.randn(vocab, 64, generator=g, device="cuda") / 8
+    t = torch.arange(rows, device="cuda")
+    targets = torch.randperm(vocab, generator=g, device="cuda")[:rows]
+    targets = targets[t // tokens]
+    x[t, 64 + t], w[targets, 64 + t] = 0.5 + rand(rows), 0.5 + rand(rows)
+    x, w = x.to(dtype), w.to(dtype)
+    out = torch.randperm(rows, generator=g, device="cuda")[count:]
+    dloss = 0.5 + rand(rows)
+    marked = targets.clone()
+    marked[out] = -1
+    loss, lse = step.loss_forward(x, w, marked)
+    r = defn.loss(x, w, marked)
+    live = (marked >= 0).nonzero()[:, 0]
+    t, v = t[live], targets[live]
+    xd, wd = x.double(), w.double()
+    p = torch.exp((xd[t] * wd[v]).sum(1) - r["lse"][t])
+    at = dloss[t].double() * (p - 1)
+    moved = r["b_lse"][t] + 24 * 2.0 ** -24 * (xd[t] * wd[v]).abs().sum(1)
+    off = 2.0 ** -20 + moved * p / (1 - p)
+    held = torch.zeros(vocab, dtype=torch.int64, device="cuda").index_add_(0, v, torch.ones_like(v))        # tokens of a target
+
+    def check(got, want, room):
+        """Within `room`, or beyond two of a target also within the rounding of G."""
+        wrong = (got.double() - want).abs() - room
+        assert bool((wrong <= torch.where(held[v] > 2, defn.U[dtype] * want.abs(), 0.0)).all())
+        good = torch.zeros_like(held).index_add_(0, v, (wrong <= 0).long())
+        assert bool((good >= held.clamp(max=2)).all())
+
+    for out_dtype in (F, dtype):
+        dx, dw = step.loss_backward(x, w, marked, lse, dloss, out_dtype=out_dtype)
+        want = at * wd[v, 64 + t]
+        assert bool(((dx[t, 64 + t].double() - want).abs() <= half_step(want, dtype) + off * want.abs()).all())
+        want = at * xd[t, 64 + t]
+        check(dw[v, 64 + t], want, off * want.abs() + (0 if out_dtype == F else half_step(want, dtype)))
+    was = torch.full_like(dw, 0.5, dtype=F)
+    step.loss_backward(x, w, marked, lse, dloss, grad=was)
+    check(was[v, 64 + t].double() - 0.5, want, off * want.abs() + 2.0 ** -23)
