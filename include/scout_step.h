@@ -134,7 +134,8 @@ SCOUT_API int scout_join_backward(const scout_join_t *j, const void *dy, const v
  *   loss, lse    device [rows] fp32
  * dim a multiple of 8 up to 65536, rows and vocab up to 2^24 and rows * vocab up to 2^45, else
  * SCOUT_ERR_UNSUPPORTED.  The scratch of the backward pass holds a copy of x, dx in fp32, and G for a
- * piece of the vocabulary: half a GiB, more only where 8192 columns take more. */
+ * piece of the vocabulary (in float16 in two forms): half a GiB each, more only where 8192 columns
+ * take more. */
 SCOUT_API int scout_loss_workspace(uint32_t dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
                                    uint64_t *forward_bytes, uint64_t *backward_bytes);
 SCOUT_API int scout_loss_forward(uint32_t dtype, uint32_t id_dtype, uint64_t rows, uint64_t dim, uint64_t vocab,
@@ -146,10 +147,12 @@ SCOUT_API int scout_loss_forward(uint32_t dtype, uint32_t id_dtype, uint64_t row
  *     G_tv = g_t (exp(s_tv - lse_t) - [v = target_t]),   dx_t = sum_v G_tv w_v
  *     dw_v = (accumulate ? dw_v : 0) + sum_t G_tv x_t
  * over the rows that count.  The scores are made again, in pieces of the vocabulary; G is
- * rounded to 16 bits for its products, which have fp32 sums.  A row's entry at its target
- * enters with what that rounding took away: in dx always, in a row of dw for two of its
- * tokens (which two follows from the targets alone).  dx has x's type, dw out_dtype (dtype
- * or SCOUT_DT_F32).  Every row of dx and dw is written.
+ * rounded to 16 bits for its products, which have fp32 sums: for dx before g_t is a factor in
+ * float16, so that a row's dx does not depend on what others weigh; for dw relative to the
+ * largest finite |g| (float16: entries below 2^-27 of that have fewer bits).  A row's entry
+ * at its target enters with what that rounding took away: in dx always, in a row of dw for
+ * two of its tokens (which two follows from the targets alone).  dx has x's type, dw
+ * out_dtype (dtype or SCOUT_DT_F32).  Every row of dx and dw is written.
  *   dw           device [vocab][dim], row stride dw_stride */
 SCOUT_API int scout_loss_backward(uint32_t dtype, uint32_t id_dtype, uint32_t out_dtype, uint64_t rows, uint64_t dim,
                                   uint64_t vocab, const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,

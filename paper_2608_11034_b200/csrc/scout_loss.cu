@@ -9,7 +9,9 @@
 //   STATES   dx += G w over the piece, fp32 sums in scratch; join_states makes dx from them
 // G is held with g divided by the largest |g| (GREF): a loss averaged over the batch has one g for all rows, whose rounding would
 // otherwise be the same in every term; in fp16 it is held 2^13 times that, where the products still fit and a probability of 1e-11
-// is not lost.  Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of
+// is not lost.  A row of fp16 that weighs little beside the largest would lose bits all the same, and its dx with them: STATES takes
+// P = exp(s - lse) - [target] instead there, and g comes last.  Where all rows weigh alike P is G; where they do not, G is stored
+// beside it (4000 rows, 1024 columns, 50257 of vocabulary: gradients 975 us and 1061).  Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of
 // dx, and of its target's row of dw: what the rounding took from that entry is added, times the target's row of w (join_states) and the
 // token's row of x (TABLE, of the first two tokens of a target).
 //
@@ -53,12 +55,14 @@ struct Args {
     // scratch
     int32_t *count;     // rows that count
     float *g_ref;       // largest finite |g|
+    int32_t *alike;     // whether all g are that
     int32_t *which;     // [padded]: row of x of a taken row
     int32_t *where;     // [rows]: its place among the taken rows, or -1
     int32_t *target;    // [padded]
     float *row_lse, *row_g, *row_rest;  // [padded]: lse; g / g_ref; what rounding took from G at the target
+    float *row_rest_p;                  // and from P (bf16: row_rest)
     float *row_score, *row_rough;       // [padded]: the target's score in fp32 (backward: its probability less 1), and as the tensor cores have it
-    void *xc, *gs;      // [padded][dim], [padded][piece]
+    void *xc, *gs, *ps; // [padded][dim], [padded][piece], and P like it (bf16: gs)
     float2 *part;       // [2 * tiles of the vocabulary][padded]: maximum and sum of 128 columns
     float *dxp;         // [splits][padded][dim]
     int64_t piece, v0, pv;  // columns of gs, first column and columns of the current piece
@@ -87,30 +91,31 @@ template <typename T> __device__ __forceinline__ void load_any(Eight<T> &e, cons
 // fp32: for lse (see join_scores), and for G at the target, which is the difference of a probability near 1 and 1 where a model is sure.
 template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(const __grid_constant__ Args a, int64_t per) {
     __shared__ int counts[TAKE_THREADS / 32];
-    __shared__ float tops[TAKE_THREADS / 32];
+    __shared__ float tops[TAKE_THREADS / 32], lows[TAKE_THREADS / 32];
     __shared__ int rows_at[TAKE_THREADS], targets[TAKE_THREADS];
     pdl_launch_dependents();
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t r0 = blockIdx.x * per, r1 = min(r0 + per, a.rows);
     const bool last = r1 == a.rows;
     int before = 0;
-    float top = 0.f;
+    float top = 0.f, low = CUDART_INF_F;  // low: least g, or less than any top where one is no number
     for (int64_t t = threadIdx.x; t < (a.d_loss ? a.rows : r0); t += TAKE_THREADS) {
         const bool on = target_at(a, t) >= 0;
         if (on && t < r0) ++before;
         if (on && a.d_loss) {
-            const float g = fabsf(a.d_loss[t * a.d_loss_stride]);
-            if (g < CUDART_INF_F) top = fmaxf(top, g);
+            const float g = a.d_loss[t * a.d_loss_stride];
+            if (isfinite(g)) top = fmaxf(top, fabsf(g)), low = fminf(low, g);
+            else low = -CUDART_INF_F;
         }
     }
     before = __reduce_add_sync(0xFFFFFFFFu, before);
 #pragma unroll
-    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
-    if (lane == 0) counts[warp] = before, tops[warp] = top;
+    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m)), low = fminf(low, __shfl_xor_sync(0xFFFFFFFFu, low, m));
+    if (lane == 0) counts[warp] = before, tops[warp] = top, lows[warp] = low;
     __syncthreads();
     before = 0, top = 0.f;
 #pragma unroll
-    for (int w = 0; w < TAKE_THREADS / 32; ++w) before += counts[w], top = fmaxf(top, tops[w]);
+    for (int w = 0; w < TAKE_THREADS / 32; ++w) before += counts[w], top = fmaxf(top, tops[w]), low = fminf(low, lows[w]);
     const float ref = top > 0.f ? top : 1.f;
     for (int64_t base = r0; base < r1; base += TAKE_THREADS) {
         const int64_t t = base + threadIdx.x;
@@ -166,7 +171,7 @@ template <typename T> __global__ void __launch_bounds__(TAKE_THREADS) take_rows(
     if (last) {  // the rest of the last tile
         if (threadIdx.x == 0) {
             *a.count = before;
-            if (a.d_loss) *a.g_ref = ref;
+            if (a.d_loss) *a.g_ref = ref, *a.alike = low == ref;
         }
         // tokens are TABLE's terms, taken TK at a time; rows of a tile that are not there may hold anything, but have no target
         const int64_t end = min((before + (int64_t)TM - 1) / TM * TM, a.padded), terms = (before + (int64_t)TK - 1) / TK * TK;
@@ -308,7 +313,8 @@ struct Targets {
 
 template <typename T, int KIND>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(const __grid_constant__ Args a, const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b,
-                                                                                                       const __grid_constant__ CUtensorMap map_out) {
+                                                                                                       const __grid_constant__ CUtensorMap map_out,
+                                                                                                       const __grid_constant__ CUtensorMap map_p) {
     // operands with their contraction contiguous (K) or their rows (MN)
     constexpr bool mn_a = KIND == TABLE, mn_b = KIND == TABLE || KIND == STATES;
     extern __shared__ uint8_t smem_raw[];
@@ -337,7 +343,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
     if (warp == 8) {
         tc::registers_down<56>();
         if (lane == 0) {
-            tc::prefetch_map(&map_a);
+            const CUtensorMap *const from_a = KIND == TABLE && !Half<T>::is_bf16 && *a.alike ? &map_p : &map_a;
+            tc::prefetch_map(from_a);
             tc::prefetch_map(&map_b);
             uint32_t n = 0;
             // Of up to FEW rows only those are brought; what the others' places in shared memory hold reaches their own results alone (11 rows,
@@ -354,9 +361,9 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                     const uint32_t bar = tc::in_block(full + 8 * s, 0);
                     if constexpr (mn_a) {
 #pragma unroll
-                        for (int c = 0; c < HALF / 64; ++c) tc::pair_tma_2d(to + c * BOX, &map_a, bar, m0 + c * 64, at);
+                        for (int c = 0; c < HALF / 64; ++c) tc::pair_tma_2d(to + c * BOX, from_a, bar, m0 + c * 64, at);
                     } else if (!thin || rank == 0) {
-                        tc::pair_tma_2d(to, &map_a, bar, at, m0);
+                        tc::pair_tma_2d(to, from_a, bar, at, m0);
                     }
                     if constexpr (mn_b) {
 #pragma unroll
@@ -396,6 +403,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
     } else {
         tc::registers_up<224>();
         uint32_t chain = 0;
+        const bool apart = KIND == GRADS && !Half<T>::is_bf16 && !*a.alike;  // G beside P
         const int half = warp >> 2, row = (int)rank * HALF + (warp & 3) * 32 + lane;
         const uint32_t mine = tmem + ((uint32_t)((warp & 3) * 32) << 16) + half * 128;
         for (int i = pair; i < work.items; i += pairs) {
@@ -464,8 +472,8 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 const int left = (int)min(128ll, (long long)(a.pv - n0));
                 const int64_t at = target - a.v0 - n0;
                 const bool on = target >= 0, here = on && at >= 0 && at < 128;
-                g *= power2(a.scale_log2);
-                const tc::F2 less = tc::f2(-lse, -lse), scale = tc::f2(LOG2E, LOG2E), gg = tc::f2(g, g);
+                const float by = power2(a.scale_log2) * (Half<T>::is_bf16 ? g : 1.f);
+                const tc::F2 less = tc::f2(-lse, -lse), scale = tc::f2(LOG2E, LOG2E), gg = tc::f2(by, by);
 #pragma unroll
                 for (int c = 0; c < 128; c += 2) {
                     const float2 e = tc::split(tc::mul2(tc::add2(tc::f2(sum[c], sum[c + 1]), less), scale));
@@ -476,20 +484,31 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
 #pragma unroll
                     for (int c = 0; c < 128; ++c) sum[c] = on && c < left ? sum[c] : 0.f;
                 }
-                if (__any_sync(0xFFFFFFFFu, here)) {
-                    const float value = g * at_target;
+                const bool any = __any_sync(0xFFFFFFFFu, here);
+                const float value = by * at_target;
+                if (any) {
 #pragma unroll
                     for (int c = 0; c < 128; ++c) sum[c] = here && c == (int)at ? value : sum[c];
-                    if (here) a.row_rest[m] = value - Half<T>::up(Half<T>::down(value));
                 }
+                const auto rest = [](float x) { return x - Half<T>::up(Half<T>::down(x)); };
+                if (here) a.row_rest_p[m] = rest(value);
+                if (here && !Half<T>::is_bf16) a.row_rest[m] = rest(g * value);
                 if (m >= (*a.count + TK - 1) / TK * TK) continue;  // TABLE takes rows in steps of TK; STATES makes nothing of others
-                T *dst = reinterpret_cast<T *>(a.gs) + m * a.piece + n0;
+                const auto store = [&](void *to) {
+                    T *dst = reinterpret_cast<T *>(to) + m * a.piece + n0;
 #pragma unroll
-                for (int c = 0; c < 128; c += 16) {
-                    uint32_t w[8];
+                    for (int c = 0; c < 128; c += 16) {
+                        uint32_t w[8];
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) w[e] = Half<T>::pack(sum[c + 2 * e], sum[c + 2 * e + 1]);
-                    store32(dst + c, w);
+                        for (int e = 0; e < 8; ++e) w[e] = Half<T>::pack(sum[c + 2 * e], sum[c + 2 * e + 1]);
+                        store32(dst + c, w);
+                    }
+                };
+                store(a.ps);
+                if (apart) {
+#pragma unroll
+                    for (int c = 0; c < 128; ++c) sum[c] *= g;
+                    store(a.gs);
                 }
             } else if constexpr (KIND == STATES) {
                 if (m >= *a.count) continue;
@@ -642,7 +661,7 @@ template <typename T, int WAYS> __global__ void __launch_bounds__(256) join_stat
     __shared__ float part[WAYS > 1 ? WAYS : 1][256 / WAYS][WAYS > 1 ? 9 : 1];
     const int way = threadIdx.x / (256 / WAYS), lane = threadIdx.x % (256 / WAYS);
     const int64_t per_row = a.dim / 8, all = a.rows * per_row;
-    const float ref = *a.g_ref * power2(-a.scale_log2);
+    const float ref = *a.g_ref;
     for (int64_t q0 = (int64_t)blockIdx.x * (256 / WAYS); q0 < all; q0 += (int64_t)gridDim.x * (256 / WAYS)) {  // the same for a block
         const int64_t q = min(q0 + lane, all - 1), t = q / per_row;
         const Columns<true> at((uint32_t)(q - t * per_row), (uint32_t)a.dim);
@@ -670,9 +689,9 @@ template <typename T, int WAYS> __global__ void __launch_bounds__(256) join_stat
         if (m >= 0) {
             Eight<T> w;
             w.template load<false>(reinterpret_cast<const T *>(a.w) + (int64_t)a.target[m] * a.w_stride, at);
-            const float rest = a.row_rest[m];
+            const float rest = a.row_rest_p[m], by = Half<T>::is_bf16 ? ref : a.d_loss[t * a.d_loss_stride];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) x[i] = ref * fmaf(rest, w.get(i), x[i]);
+            for (int i = 0; i < 8; ++i) x[i] = by * (power2(-a.scale_log2) * fmaf(rest, w.get(i), x[i]));
         }
         Eight<T> o;
         o.set(x);
@@ -691,13 +710,13 @@ constexpr uint64_t PIECE_BYTES = 512ull << 20, LEAST_PIECE = 8192;
 struct Layout {
     uint64_t padded, tiles, piece;
     int splits, per;
-    uint64_t count, g_ref, which, where, target, row_lse, row_g, row_rest, row_score, row_rough, xc, part, gs, dxp, forward, backward;
+    uint64_t count, g_ref, alike, which, where, target, row_lse, row_g, row_rest, row_rest_p, row_score, row_rough, xc, part, gs, ps, dxp, forward, backward;
 };
-Layout layout(uint64_t rows, uint64_t dim, uint64_t vocab) {
+Layout layout(uint32_t dtype, uint64_t rows, uint64_t dim, uint64_t vocab) {
     Layout l = {};
     l.padded = (rows + TM - 1) / TM * TM;
     l.tiles = (vocab + TN - 1) / TN;
-    // A piece of G: half a GiB, or 8192 columns where rows are so many that this is more (each piece goes over dx once).
+    // A piece of G (and of P): half a GiB, or 8192 columns where rows are so many that this is more (each piece goes over dx once).
     const uint64_t most = std::max<uint64_t>(LEAST_PIECE, PIECE_BYTES / (2 * std::max<uint64_t>(l.padded, 1)) / TN * TN);
     const uint64_t pieces = std::max<uint64_t>(1, (vocab + most - 1) / most);
     l.piece = ((vocab + pieces - 1) / pieces + TN - 1) / TN * TN;
@@ -713,15 +732,17 @@ Layout layout(uint64_t rows, uint64_t dim, uint64_t vocab) {
         at += (bytes + 255) & ~255ull;
         return was;
     };
-    l.count = take(4), l.g_ref = take(4);
+    l.count = take(4), l.g_ref = take(4), l.alike = take(4);
     l.which = take(l.padded * 4), l.target = take(l.padded * 4), l.row_score = take(l.padded * 4);
     l.xc = take(l.padded * dim * 2);
     const uint64_t common = at;
     l.row_rough = take(l.padded * 4), l.part = take(2 * l.tiles * l.padded * 8);
     l.forward = at;
     at = common;
-    l.where = take(rows * 4), l.row_lse = take(l.padded * 4), l.row_g = take(l.padded * 4), l.row_rest = take(l.padded * 4);
-    l.gs = take(l.padded * l.piece * 2), l.dxp = take(l.splits * l.padded * dim * 4);
+    l.where = take(rows * 4), l.row_lse = take(l.padded * 4), l.row_g = take(l.padded * 4), l.row_rest = l.row_rest_p = take(l.padded * 4);
+    l.gs = l.ps = take(l.padded * l.piece * 2);
+    if (dtype == SCOUT_DT_F16) l.row_rest_p = take(l.padded * 4), l.ps = take(l.padded * l.piece * 2);
+    l.dxp = take(l.splits * l.padded * dim * 4);
     l.backward = at;
     return l;
 }
@@ -745,11 +766,11 @@ int check_inputs(uint32_t dtype, uint32_t id_dtype, uint64_t dim, uint64_t vocab
 void place(Args *a, const Layout &l, void *workspace, bool backward) {
     uint8_t *const ws = (uint8_t *)workspace;
     a->thin = a->rows <= FEW, a->padded = (int64_t)l.padded, a->piece = (int64_t)l.piece, a->splits = l.splits, a->per = l.per;
-    a->count = (int32_t *)(ws + l.count), a->g_ref = (float *)(ws + l.g_ref), a->which = (int32_t *)(ws + l.which), a->target = (int32_t *)(ws + l.target);
+    a->count = (int32_t *)(ws + l.count), a->g_ref = (float *)(ws + l.g_ref), a->alike = (int32_t *)(ws + l.alike), a->which = (int32_t *)(ws + l.which), a->target = (int32_t *)(ws + l.target);
     a->row_score = (float *)(ws + l.row_score), a->xc = ws + l.xc;
     if (backward) {
         a->where = (int32_t *)(ws + l.where), a->row_lse = (float *)(ws + l.row_lse), a->row_g = (float *)(ws + l.row_g);
-        a->row_rest = (float *)(ws + l.row_rest), a->gs = ws + l.gs, a->dxp = (float *)(ws + l.dxp);
+        a->row_rest = (float *)(ws + l.row_rest), a->row_rest_p = (float *)(ws + l.row_rest_p), a->gs = ws + l.gs, a->ps = ws + l.ps, a->dxp = (float *)(ws + l.dxp);
     } else {
         a->row_rough = (float *)(ws + l.row_rough), a->part = (float2 *)(ws + l.part);
     }
@@ -761,7 +782,7 @@ template <typename T> int take(const Args &a, cudaStream_t stream) {
     SCOUT_CUDA(cudaGetLastError());
     return SCOUT_OK;
 }
-template <typename T, int KIND> int run_product(const Args &a, int64_t items, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &out, cudaStream_t stream) {
+template <typename T, int KIND> int run_product(const Args &a, int64_t items, const CUtensorMap &ma, const CUtensorMap &mb, const CUtensorMap &out, const CUtensorMap &mp, cudaStream_t stream) {
     if (int rc = allow_smem<product<T, KIND>>(SMEM)) return rc;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(2 * (unsigned)std::max<int64_t>(1, std::min<int64_t>(items, PAIRS)));
@@ -773,7 +794,7 @@ template <typename T, int KIND> int run_product(const Args &a, int64_t items, co
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     cfg.attrs = attr;
     cfg.numAttrs = 1;
-    SCOUT_CUDA(cudaLaunchKernelEx(&cfg, product<T, KIND>, a, ma, mb, out));
+    SCOUT_CUDA(cudaLaunchKernelEx(&cfg, product<T, KIND>, a, ma, mb, out, mp));
     return SCOUT_OK;
 }
 // a row-major matrix [rows][cols] for boxes of box_rows x 64
@@ -789,7 +810,7 @@ template <typename T> int run_forward(Args &a, const Layout &l, cudaStream_t str
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     a.pv = a.vocab;
-    if (int rc = run_product<T, SCORES>(a, (int64_t)(l.padded / TM * l.tiles), mx, mw, mx, stream)) return rc;
+    if (int rc = run_product<T, SCORES>(a, (int64_t)(l.padded / TM * l.tiles), mx, mw, mx, mx, stream)) return rc;
     SCOUT_CUDA(launch_dependent(join_scores, dim3((unsigned)((a.rows + 31) / 32)), dim3(32, JOIN_WAYS), stream, a, (int)(2 * l.tiles)));
     return SCOUT_OK;
 }
@@ -797,14 +818,15 @@ template <typename T> int run_forward(Args &a, const Layout &l, cudaStream_t str
 template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t stream) {
     a.scale_log2 = Half<T>::is_bf16 ? 0 : 13;
     if (int rc = tc::gave_up_counter(&a.gave_up)) return rc;
-    CUtensorMap mx, mw, mg, mg_t, mx_t, mw_n;
+    CUtensorMap mx, mw, mg, mg_t, mp_t, mx_t, mw_n;
     // G has rows to whole steps of TABLE; STATES's tiles are zeros beyond (14 rows, 400 columns, 59712 of vocabulary: 82 us with all of a tile's
     // rows written and read, 73 so).  Not so the rows of x, which stay in L2: zeros take longer than those.
     const uint64_t taken = (a.rows + TK - 1) / TK * TK;
     if (int rc = map_of<T>(&mx, a.xc, l.padded, a.dim, a.dim, a.thin ? FEW : HALF)) return rc;
     if (int rc = map_of<T>(&mx_t, a.xc, l.padded, a.dim, a.dim, TK)) return rc;
-    if (int rc = map_of<T>(&mg, a.gs, taken, l.piece, l.piece, a.thin ? FEW : HALF)) return rc;
+    if (int rc = map_of<T>(&mg, a.ps, taken, l.piece, l.piece, a.thin ? FEW : HALF)) return rc;
     if (int rc = map_of<T>(&mg_t, a.gs, l.padded, l.piece, l.piece, TK)) return rc;
+    if (int rc = map_of<T>(&mp_t, a.ps, l.padded, l.piece, l.piece, TK)) return rc;
     if (int rc = take<T>(a, stream)) return rc;
     const int64_t row_tiles = (int64_t)(l.padded / TM), dim_tiles = (a.dim + TN - 1) / TN;
     for (int64_t v0 = 0; v0 < a.vocab; v0 += a.piece) {
@@ -815,9 +837,9 @@ template <typename T> int run_backward(Args &a, const Layout &l, cudaStream_t st
         CUtensorMap out = mg;
         if (a.tiles_out)
             if (int rc = map_of<T>(&out, reinterpret_cast<T *>(a.dw) + v0 * a.dw_stride, a.pv, a.dim, a.dw_stride, 32)) return rc;
-        if (int rc = run_product<T, GRADS>(a, row_tiles * ((a.pv + TN - 1) / TN), mx, mw, mx, stream)) return rc;
-        if (int rc = run_product<T, TABLE>(a, (a.pv + TM - 1) / TM * dim_tiles, mg_t, mx_t, out, stream)) return rc;
-        if (int rc = run_product<T, STATES>(a, row_tiles * dim_tiles * a.splits, mg, mw_n, mg, stream)) return rc;
+        if (int rc = run_product<T, GRADS>(a, row_tiles * ((a.pv + TN - 1) / TN), mx, mw, mx, mx, stream)) return rc;
+        if (int rc = run_product<T, TABLE>(a, (a.pv + TM - 1) / TM * dim_tiles, mg_t, mx_t, out, mp_t, stream)) return rc;
+        if (int rc = run_product<T, STATES>(a, row_tiles * dim_tiles * a.splits, mg, mw_n, mg, mg, stream)) return rc;
     }
     const int wide = wide_rows(a.dx, a.dx_stride, SCOUT_DT_BF16);
     const int ways = a.splits > 4 ? 8 : 1;
@@ -834,7 +856,7 @@ extern "C" int scout_loss_workspace(uint32_t dtype, uint64_t rows, uint64_t dim,
     using namespace scout::step;
     if (!forward_bytes || !backward_bytes) return SCOUT_ERR_INVALID;
     if (int rc = check(dtype, SCOUT_DT_I64, rows, dim, vocab)) return rc;
-    const Layout l = layout(rows, dim, vocab);
+    const Layout l = layout(dtype, rows, dim, vocab);
     *forward_bytes = l.forward, *backward_bytes = l.backward;
     return SCOUT_OK;
 }
@@ -848,7 +870,7 @@ extern "C" int scout_loss_forward(uint32_t dtype, uint32_t id_dtype, uint64_t ro
     if (int rc = check_inputs(dtype, id_dtype, dim, vocab, x, x_stride, w, w_stride, targets)) return rc;
     if (!loss || !lse) return SCOUT_ERR_INVALID;
     if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(workspace, 256)) return SCOUT_ERR_ALIGN;
-    const Layout l = layout(rows, dim, vocab);
+    const Layout l = layout(dtype, rows, dim, vocab);
     if (!workspace || workspace_bytes < l.forward) return SCOUT_ERR_INVALID;
     const cudaStream_t s = (cudaStream_t)stream;
     if (vocab == 0) {
@@ -885,7 +907,7 @@ extern "C" int scout_loss_backward(uint32_t dtype, uint32_t id_dtype, uint32_t o
     }
     if (!lse || !d_loss || d_loss_stride > MAX_STRIDE) return SCOUT_ERR_INVALID;
     if (!aligned(lse, 4) || !aligned(d_loss, 4) || !aligned(workspace, 256)) return SCOUT_ERR_ALIGN;
-    const Layout l = layout(rows, dim, vocab);
+    const Layout l = layout(dtype, rows, dim, vocab);
     if (!workspace || workspace_bytes < l.backward) return SCOUT_ERR_INVALID;
     Args a = {};
     a.x = x, a.w = w, a.targets = targets, a.lse_in = lse, a.d_loss = d_loss, a.dx = dx, a.dw = dw;

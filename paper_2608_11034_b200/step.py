@@ -326,7 +326,8 @@ def loss_backward(x: torch.Tensor, w: torch.Tensor, targets: torch.Tensor, lse: 
     embedding, say) dw is added to it in place, and out_dtype may only repeat its dtype.
     The gradient of the scores is rounded to x's type for its products, so a float32 dw is as exact as its terms are (2^-8 of
     each in bfloat16, 2^-11 in float16), not as float32 is.  What that takes from a token's own target is given back: all of it to
-    dx, and to a row of dw that of two of its tokens."""
+    dx, and to a row of dw that of two of its tokens.  In float16 dw's terms are rounded relative to the largest dloss: of a row that weighs
+    2^-27 of that little is left there, and all of it in its dx."""
     _no_autograd(x, w, lse, dloss, grad)
     code, rows, dim, vocab, x_row, w_row, _, nbytes = _describe_scores(x, w, targets)
     targets = _flat_ids(targets, x.device, "targets")

@@ -132,3 +132,72 @@ def test_the_gradient_at_a_target_is_not_rounded_to_16_bits(tokens, rows, count,
     was = torch.full_like(dw, 0.5, dtype=F)
     step.loss_backward(x, w, marked, lse, dloss, grad=was)
     check(was[v, 64 + t].double() - 0.5, want, off * want.abs() + 2.0 ** -23)
+
+
+def test_rows_that_weigh_little_have_gradients_of_their_own():
+    """float16, half of the rows weighing 2^-27 of the others: their dx is as exact as if they were alone, and has the same bits whatever
+    the others weigh."""
+    from paper_2608_11034_b200 import step
+    rows, dim, vocab = 200, 136, 1200
+    g = torch.Generator(device="cuda").manual_seed(4)
+    x = torch.randn(rows, dim, generator=g, device="cuda").to(H)
+    w = (torch.randn(vocab, dim, generator=g, device="cuda") * dim ** -0.5).to(H)
+    targets = torch.randint(0, vocab, (rows,), generator=g, device="cuda")
+    _, lse = step.loss_forward(x, w, targets)
+    light = torch.arange(rows, device="cuda") % 2 == 1
+    dloss = torch.where(light, 2.0 ** -12, 2.0 ** 15) * (0.5 + torch.rand(rows, generator=g, device="cuda") / 2)
+    dx, dw = step.loss_backward(x, w, targets, lse, dloss)
+    r = defn.loss(x[light], w, targets[light], dloss[light])
+    assert defn.within(dx[light], r["dx"], r["b_dx"]) <= 1
+    r = defn.loss(x, w, targets, dloss)
+    assert defn.within(dx, r["dx"], r["b_dx"]) <= 1 and defn.within(dw, r["dw"], r["b_dw"] + defn.U[F] * r["dw"].abs()) <= 1
+    same, _ = step.loss_backward(x, w, targets, lse, torch.where(light, dloss, 2.0 ** -12))
+    assert torch.equal(same[light], dx[light])
+
+
+@pytest.mark.parametrize("rows", [40, 200])
+@pytest.mark.parametrize("other", [0.0, -1.0, 2.0, math.inf, math.nan])
+def test_rows_that_weigh_alike_and_one_that_does_not(other, rows):
+    """float16: one number for all rows, or for all but the last."""
+    from paper_2608_11034_b200 import step
+    dim, vocab = 72, 700
+    g = torch.Generator(device="cuda").manual_seed(9)
+    x = torch.randn(rows, dim, generator=g, device="cuda").to(H)
+    w = (torch.randn(vocab, dim, generator=g, device="cuda") * dim ** -0.5).to(H)
+    targets = torch.randint(-50, vocab, (rows,), generator=g, device="cuda")
+    targets[-1] = 5
+    _, lse = step.loss_forward(x, w, targets)
+    dloss = torch.ones(rows, device="cuda")
+    dx, dw = step.loss_backward(x, w, targets, lse, dloss)
+    r = defn.loss(x, w, targets, dloss)
+    assert defn.within(dx, r["dx"], r["b_dx"]) <= 1 and defn.within(dw, r["dw"], r["b_dw"] + defn.U[F] * r["dw"].abs()) <= 1
+    dloss[-1] = other
+    mixed, dw = step.loss_backward(x, w, targets, lse, dloss)
+    assert torch.equal(mixed[:-1], dx[:-1])
+    if math.isfinite(other):
+        r = defn.loss(x, w, targets, dloss)
+        assert defn.within(mixed, r["dx"], r["b_dx"]) <= 1 and defn.within(dw, r["dw"], r["b_dw"] + defn.U[F] * r["dw"].abs()) <= 1
+    else:
+        assert not mixed[-1].isfinite().any() and not dw.isfinite().any()
+
+
+def test_a_vocabulary_in_pieces_of_float16():
+    """G is held in two forms there."""
+    from paper_2608_11034_b200 import binding, step
+    rows, dim, vocab = 33000, 64, 17000
+    _, b = binding.scout_loss_workspace(binding.DT_F16, rows, dim, vocab)
+    assert b < 2 * rows * vocab * 2
+    g = torch.Generator(device="cuda").manual_seed(6)
+    x = torch.randn(rows, dim, generator=g, device="cuda").to(H)
+    w = (torch.randn(vocab, dim, generator=g, device="cuda") / 8).to(H)
+    targets = torch.randint(-100, vocab, (rows,), generator=g, device="cuda")
+    dloss = torch.rand(rows, generator=g, device="cuda")
+    _, lse = step.loss_forward(x, w, targets)
+    dx, dw = step.loss_backward(x, w, targets, lse, dloss)
+    want, bound = (torch.zeros(vocab, dim, dtype=torch.float64, device="cuda") for _ in range(2))
+    for part in torch.arange(rows, device="cuda").split(4000):
+        r = defn.loss(x[part], w, targets[part], dloss[part])
+        assert defn.within(dx[part], r["dx"], r["b_dx"]) <= 1
+        want += r["dw"]
+        bound += r["b_dw"]
+    assert defn.within(dw, want, bound + defn.U[F] * want.abs()) <= 1
