@@ -19,7 +19,9 @@ waited for, and ``record_stream`` if it is freed early.
 None of the calls is recorded by autograd.  Where it would be asked to (grad mode on,
 an input of attention or of the weight gradient that requires a gradient), they raise
 instead of dropping the gradient: call them under torch.no_grad(), or from the
-forward and backward of a torch.autograd.Function, where grad mode is off.
+forward and backward of a torch.autograd.Function, where grad mode is off.  So they do in
+forward mode on an input with a tangent, which torch.no_grad() does not take away: such a
+call belongs into the forward of a torch.autograd.Function with a jvp.
 
 The kernels' waits are bounded.  A call in which one gave up has no valid results, and
 cannot say so itself, since it only enqueues: ``with waits_checked(device):`` around
@@ -34,6 +36,7 @@ from typing import Optional
 
 import numpy as np
 import torch
+from torch.autograd import forward_ad
 
 from . import binding
 
@@ -67,8 +70,14 @@ def _fail(what: str):
 
 
 def _no_autograd(*tensors) -> None:
-    if torch.is_grad_enabled() and any(x.requires_grad for x in tensors):
-        _fail("autograd does not record this call: use torch.no_grad() or a torch.autograd.Function")
+    """Raises where autograd would have to record a call on these tensors (None: there is none), or to give its results a tangent."""
+    if torch.is_grad_enabled():
+        for x in tensors:
+            if x is not None and x.requires_grad:
+                _fail("autograd does not record this call: use torch.no_grad() or a torch.autograd.Function")
+    # unpack_dual alone would do, for 0.3 us a tensor; -1 says that there is no forward mode
+    if getattr(forward_ad, "_current_level", 0) >= 0 and any(x is not None and forward_ad.unpack_dual(x).tangent is not None for x in tensors):
+        _fail("autograd does not record this call in forward mode either: use a torch.autograd.Function with a jvp")
 
 
 class _Attention:
@@ -251,9 +260,9 @@ def checkpoint_wgrad(dy: torch.Tensor, codes: torch.Tensor, exps: torch.Tensor, 
     """Weight gradient dW = dy^T x of y = x W^T, x taken from its checkpoint.  dy: [rows, outs], bfloat16 or float16.
     -> dW [outs, ins] in out_dtype (float32, which is the default, or dy's); with `grad` (of those dtypes) dW is added to it in
     place, and out_dtype may only repeat its dtype."""
+    _no_autograd(dy, grad)
     rows, ins, code_stride = _checkpoint(codes.shape, codes.stride(), codes.dtype, codes.device, exps.shape, exps.stride(),
                                          exps.dtype, exps.device)
-    _no_autograd(dy) if grad is None else _no_autograd(dy, grad)
     if dy.dim() != 2:
         _fail("dy: a matrix with adjacent row elements is wanted")
     if grad is None:

@@ -13,7 +13,8 @@ an order that the sizes and the token ids fix, random numbers from a counter.
                                             output projection; the scores are never kept
 
 ``include/scout_step.h`` has the definitions.  What ``replay`` says of streams, autograd (the calls raise where
-it would have to record them) and bounded waits (``replay.waits_checked``; join and loss have such waits) holds here too.
+it would have to record them, or to give their results a tangent) and bounded waits (``replay.waits_checked``;
+join and loss have such waits) holds here too.
 """
 from __future__ import annotations
 
@@ -25,17 +26,10 @@ import numpy as np
 import torch
 
 from . import binding
-from .replay import _CODE, _enqueue, _fail, _row_stride
+from .replay import _CODE, _enqueue, _fail, _no_autograd, _row_stride
 
 _IDS = {torch.int32: binding.DT_I32, torch.int64: binding.DT_I64}
 _MASK64 = (1 << 64) - 1
-
-
-def _no_autograd(*tensors) -> None:
-    if torch.is_grad_enabled():
-        for x in tensors:
-            if x is not None and x.requires_grad:
-                _fail("autograd does not record this call: use torch.no_grad() or a torch.autograd.Function")
 
 
 def _flat_ids(ids: torch.Tensor, device, name: str) -> torch.Tensor:
@@ -258,7 +252,7 @@ def join_backward(dy: Optional[torch.Tensor], dn: Optional[torch.Tensor], block:
     pass returned; the other arguments as there.
     -> (dx, dblock, dgate, dpost_weight, dnorm_weight): dx of the stream's dtype, the weights' gradients like the weights, None
     where there is no such weight."""
-    _no_autograd(dy, dn, block, y, gate, post_weight, norm_weight)
+    _no_autograd(dy, dn, block, y, stats, gate, post_weight, norm_weight)
     if dn is not None and norm_weight is None:
         _fail("dn: without norm_weight there was no n")
     j = _join(_say(block), (_say(y), _say(dy)), _say(dn), (_say_weight(gate), _say_weight(post_weight), _say_weight(norm_weight)),
