@@ -751,7 +751,7 @@ int check(uint32_t dtype, uint32_t id_dtype, uint64_t rows, uint64_t dim, uint64
     if (dtype > SCOUT_DT_I32 || id_dtype > SCOUT_DT_I32 || dim == 0) return SCOUT_ERR_INVALID;
     if ((dtype != SCOUT_DT_BF16 && dtype != SCOUT_DT_F16) || (id_dtype != SCOUT_DT_I32 && id_dtype != SCOUT_DT_I64)) return SCOUT_ERR_UNSUPPORTED;
     if (dim % 8 || dim > 65536 || rows > 1ull << 24 || vocab > 1ull << 24) return SCOUT_ERR_UNSUPPORTED;
-    return ((rows + TM - 1) / TM) * ((vocab + TN - 1) / TN) > 0x7FFFFFFFull ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;  // tiles are counted in 32 bits
+    return rows * vocab > 1ull << 45 ? SCOUT_ERR_UNSUPPORTED : SCOUT_OK;  // tiles are counted in 32 bits: 2^29 and a border of 2^17
 }
 // what both passes are given
 int check_inputs(uint32_t dtype, uint32_t id_dtype, uint64_t dim, uint64_t vocab, const void *x, uint64_t x_stride, const void *w, uint64_t w_stride,
