@@ -133,7 +133,8 @@ SCOUT_API int scout_join_backward(const scout_join_t *j, const void *dy, const v
  *   targets      device [rows], SCOUT_DT_I32 or SCOUT_DT_I64
  *   loss, lse    device [rows] fp32
  * dim a multiple of 8 up to 65536, rows and vocab up to 2^24 and rows * vocab up to 2^45, else
- * SCOUT_ERR_UNSUPPORTED.  The scratch of the backward pass holds a copy of x, dx in fp32, and G for a
+ * SCOUT_ERR_UNSUPPORTED.  The scratch of the forward pass holds a copy of x and 8 bytes for each row and
+ * 128 of the vocabulary (64 MB for 8192 rows and 128000).  The scratch of the backward pass holds a copy of x, dx in fp32, and G for a
  * piece of the vocabulary (in float16 in two forms): half a GiB each, more only where 8192 columns
  * take more. */
 SCOUT_API int scout_loss_workspace(uint32_t dtype, uint64_t rows, uint64_t dim, uint64_t vocab,

@@ -9,8 +9,8 @@
 //                inside, and leaves what crosses a border in scratch
 //   join_pieces  adds the parts of an id that crosses borders, in order
 // Pieces of equal size keep one frequent id (a line break, say) from holding up the rest.
-// Bound by memory, the zeros above all: 16384 tokens of 4096 in bf16 into fp32 [32000][4096]: 130 us, of which 690 MB at the measured rate
-// are 107; what is left is the sort (20 us, half hidden behind zeros) and the last join (8).  16384 x 4096 rows looked up: 37 us, 190 MB.
+// Bound by memory, the zeros above all: 16384 tokens of 4096 in bf16 into fp32 [32000][4096]: 129 to 152 us on several B200s, of which
+// 658 MB at the measured rate are 102; what is left is the sort (20 us, half hidden behind zeros) and the last join (8).  16384 x 4096 rows looked up: 37 us, 190 MB.
 #include <algorithm>
 #include <cmath>
 

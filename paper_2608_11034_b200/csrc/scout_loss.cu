@@ -7,19 +7,21 @@
 //   GRADS    the same s again -> G = g (exp(s - lse) - [target]) in 16 bits, for a piece of the vocabulary
 //   TABLE    dw of the piece = G^T x
 //   STATES   dx += G w over the piece, fp32 sums in scratch; join_states makes dx from them
-// G is held with g divided by the largest |g| (GREF): a loss averaged over the batch has one g for all rows, whose rounding would
+// G is held with g divided by the largest |g| (g_ref): a loss averaged over the batch has one g for all rows, whose rounding would
 // otherwise be the same in every term; in fp16 it is held 2^13 times that, where the products still fit and a probability of 1e-11
 // is not lost.  A row of fp16 that weighs little beside the largest would lose bits all the same, and its dx with them: STATES takes
 // P = exp(s - lse) - [target] instead there, and g comes last.  Where all rows weigh alike P is G; where they do not, G is stored
-// beside it (4000 rows, 1024 columns, 50257 of vocabulary: gradients 975 us and 1061).  Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of
-// dx, and of its target's row of dw: what the rounding took from that entry is added, times the target's row of w (join_states) and the
-// token's row of x (TABLE, of the first two tokens of a target).
+// beside it (4000 rows, 1024 columns, 50257 of vocabulary: gradients 975 us and 1061).
+// Rounding G leaves errors that differ from term to term, save that a row's entry at its target may make up most of dx, and of its
+// target's row of dw: what the rounding took from that entry is added, times the target's row of w (join_states) and the token's row of x
+// (TABLE, of the first two tokens of a target).  That keeps dx at the error of its own rounding; dw is 1.05 to 1.09 times as far off as
+// with G in fp32.
 //
 // The tensor cores truncate when they add to an accumulator; chains of products are cut at 1024 terms and added in fp32.
 //
-// What bounds it: the products.  2048 rows, 4096 columns, 32000 of vocabulary: the four take 335 to 366 us each (1.47 to 1.6 PFLOP/s; the
-// tensor pipe is busy for 80 to 89 % of the elapsed time).  8192 rows (a tenth of them padding) over 128000, forward and gradients: 24.4 ms, 30.9 TFLOP (of
-// which 7.7 make the scores again) at 1.27 PFLOP/s, which is the power limit: one library product after another runs at 1.31 to 1.40 there.
+// What bounds it: the products.  2048 rows, 4096 columns, 32000 of vocabulary: the four take 331 to 366 us each (1.47 to 1.62 PFLOP/s; the
+// tensor pipe is busy for 79 to 90 % of the elapsed time).  8192 rows (a tenth of them padding) over 128000, forward and gradients: 24.6 ms, 30.9 TFLOP (of
+// which 7.7 make the scores again) at 1.26 PFLOP/s, which is the power limit: one library product after another runs at 1.31 to 1.40 there.
 // A tile on one SM (128 x 256) takes the same time at that limit, on pairs of SMs a tenth less where it is not reached.
 #include <algorithm>
 
@@ -530,7 +532,7 @@ __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(THREADS, 1) product(
                 for (int c = 0; c < 128; ++c) sum[c] *= ref;
                 if (a.tiles_out) {
                     // 32 rows x 64 columns at a time through shared memory: whole lines, where a thread's row in pieces leaves one line to eight
-                    // writes (352 rows, 1960 columns, 23945 of vocabulary: 48 us, 74 in pieces)
+                    // writes (352 rows, 1960 columns, 23945 of vocabulary, before rows took anything back: 48 us, 74 in pieces)
                     const uint32_t stage = base + STAGES * STAGE + warp * 4096;
                     const int m0 = (int)(m - lane);
 #pragma unroll
